@@ -466,6 +466,67 @@ rdcn_status rdcn_head_backward(rdcn_handle* h, int64_t batch, const void* x, con
                                float* grad_e, const rdcn_head_weights* grads, void* scratch, void* stream);
 
 /*
+ * ---------------------------------------------------------------------------
+ * Training over a large set of classes (items, tokens): a softmax loss with its
+ * gradient, the norm of all gradients, and an AdamW step. The paper names the
+ * training recipe (Adam, gradient clipping) without formulas; they are stated here.
+ * None of these calls uses the model of the handle beyond its storage dtype and
+ * its id type. Their launches are timed under the head's kernels
+ * (rdcn_profile_start): head_fwd_gemm, head_loss, head_out_bwd, head_gx_gemm,
+ * head_gw_gemm and splitk_reduce; those of the norm and the step are not timed.
+ * ---------------------------------------------------------------------------
+ * Softmax loss of `rows` samples over `classes` classes:
+ *   z[n, v]  = logit_scale * (x[n] . w[v]) + offset[v]
+ *   lse[n]   = log sum_v exp(z[n, v]),   loss[n] = lse[n] - z[n, labels[n]]
+ *   x [rows, dim], w [classes, dim] in the storage dtype, offset [classes] float
+ *   or NULL, labels [rows] in the handle's id type, loss and lse [rows] float.
+ * z is never written out: sums and maxima are float, z is a float sum of exact
+ * products (bf16 models) or of float products.
+ *   - offset: a constant per class, e.g. minus the log of its sampling frequency.
+ *     -inf masks the class: probability 0 whatever its logit. (It gets no
+ *     gradient itself.)
+ *   - A label below 0 marks a row without one (padding): loss 0, no gradient,
+ *     and its x may hold anything. Its lse is written all the same. A label of
+ *     `classes` or more does the same and raises the device error word
+ *     (RDCN_ERR_INDEX, see rdcn_check_device_errors).
+ *   - A row whose label is masked has loss +inf and the gradient of lse alone
+ *     (masked logits are constants); one with every class masked has lse -inf
+ *     and gradient 0.
+ *   - w has to be finite, in masked classes too: their zero probabilities are
+ *     still multiplied with it.
+ * dim is a multiple of 8 (bf16 models) or 4 (float); rows <= 2^24, classes <=
+ * 2^27, dim <= 2^20, rows * classes <= 2^44, else RDCN_ERR_UNSUPPORTED. x, w, grad_x and
+ * grad_w must be 16-byte aligned (RDCN_ERR_ARG otherwise); rows may be 0 (the
+ * forward then does nothing, the gradient sets grad_w to 0).
+ */
+
+/* Scratch bytes (256-byte aligned buffers) of the two calls below. */
+rdcn_status rdcn_softmax_loss_workspace(const rdcn_handle* h, int64_t rows, int64_t dim, int64_t classes,
+                                        size_t* forward_bytes, size_t* grad_bytes);
+
+/* Loss and lse alone (scoring, evaluation). exp(-loss[n]) is the label's probability. */
+rdcn_status rdcn_softmax_loss_forward(rdcn_handle* h, int64_t rows, int64_t dim, int64_t classes, const void* x,
+                                      const void* w, const float* offset, const void* labels, float logit_scale,
+                                      float* loss, float* lse, void* scratch, size_t scratch_bytes, void* stream);
+
+/*
+ * Loss, lse and the gradients of  sum_n scale * row_weight[n] * loss[n]
+ * (row_weight [rows] float, or NULL for 1; scale = 1/rows gives a mean loss):
+ * grad_x [rows, dim] and grad_w [classes, dim], both in the storage dtype and
+ * overwritten. With p = softmax(z) and G = scale * weight * logit_scale * (p - onehot):
+ * grad_x = G w, grad_w = G^T x. bf16 models round G to bf16 for the matrix
+ * products (a relative 2^-8 per element at most, label's element taken from z, so that
+ * p - 1 keeps its digits) and each gradient once at the end; sums are float and
+ * in a fixed order (deterministic).
+ * G stands in scratch for all classes while that takes 512 MiB or less; else for a
+ * piece of the classes at a time, whose logits are then computed twice.
+ */
+rdcn_status rdcn_softmax_loss_grad(rdcn_handle* h, int64_t rows, int64_t dim, int64_t classes, const void* x,
+                                   const void* w, const float* offset, const void* labels, float logit_scale,
+                                   const float* row_weight, float scale, float* loss, float* lse, void* grad_x,
+                                   void* grad_w, void* scratch, size_t scratch_bytes, void* stream);
+
+/*
  * Per-kernel timing with HIP events on the stream each kernel is launched on.
  * After rdcn_profile_start, each launch site whose bit (1 << rdcn_kernel) is
  * set in `kernel_mask` records an event before and after its kernel(s), up to

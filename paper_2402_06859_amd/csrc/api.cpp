@@ -14,6 +14,7 @@
 #include "gemm.h"
 #include "head.h"
 #include "kernels.h"
+#include "softmax_loss.h"
 
 struct rdcn_handle {
     rdcn_config cfg;
@@ -343,6 +344,144 @@ CalArgs cal_args(const rdcn_handle* h, const rdcn_head_weights* w, const float* 
     c.b = (const float*)w->cal_b;
     c.e = e;
     return c;
+}
+
+// ---------------------------------------------------------------------------
+// Softmax loss over many classes. Forward: one product whose epilogue leaves a (maximum, sum) pair
+// per row and column tile, then the join of a row's pairs. Gradient: G [rows, classes] is too large to
+// keep in general, so
+//   - where it fits SOFT_HELD_BYTES, the forward's product also writes the exponentials relative to
+//     their tile's maximum there, which become G in place: three products, 6 N V d operations;
+//   - else G is made for a piece of the classes at a time from the logits computed again (8 N V d):
+//     grad_w of a piece is final, grad_x adds up over the pieces in float.
+// bf16: the matrix loads take 8 classes at a time where classes are the contracted dimension, so the
+// last classes % 8 go through a copy padded with zero rows.
+// ---------------------------------------------------------------------------
+constexpr size_t SOFT_HELD_BYTES = (size_t)512 << 20;
+
+struct SoftPlan {
+    bool held;
+    int64_t piece, main, tail;  // classes per piece; classes in whole vectors, and behind them
+    int64_t ld;                 // row stride of G
+    int64_t tiles;              // column tiles of the forward's product
+    int tile;
+    size_t part, zlabel, forward_total, factor, kept, G, Gt, acc, wt, gwt, splitk, total;
+};
+
+int64_t split_floats(const rdcn_handle* h, int64_t M, int64_t N, int64_t K) {
+    if (M == 0 || K == 0) return 0;
+    const GemmPlan p = plan_gemm(M, N, K, h->bf16, true);
+    return p.splits > 1 ? (int64_t)p.splits * M * N : 0;
+}
+
+SoftPlan soft_plan(const rdcn_handle* h, int64_t rows, int64_t dim, int64_t classes) {
+    SoftPlan s{};
+    const size_t e = eb(h);
+    const int64_t vec = h->bf16 ? 8 : 4;
+    s.tail = h->bf16 ? classes % vec : 0;  // (float operands are loaded class by class)
+    s.main = classes - s.tail;
+    const GemmPlan p = plan_gemm(rows, classes, dim, h->bf16, false);
+    s.tiles = rows > 0 ? gemm_soft_tiles(rows, classes, dim, p, h->bf16, &s.tile) : 0;
+    const int64_t padded = (classes + vec - 1) / vec * vec;
+    s.held = classes <= ((int64_t)1 << 20) && (double)rows * (double)padded * (double)e <= (double)SOFT_HELD_BYTES;
+    if (s.held) {
+        s.piece = s.main;
+        s.ld = padded;
+    } else {
+        int64_t w = (int64_t)(SOFT_HELD_BYTES / e) / rows / 256 * 256;
+        w = std::min<int64_t>(std::max<int64_t>(w, 1024), (int64_t)1 << 20);
+        s.piece = std::min<int64_t>(w, s.main);
+        s.ld = (s.piece + vec - 1) / vec * vec;
+    }
+    const bool many = s.main > s.piece || (s.tail > 0 && s.main > 0);  // grad_x is a sum of several products
+    size_t off = 0;
+    s.part = off; off += al((size_t)s.tiles * rows * 8);
+    s.zlabel = off; off += al((size_t)rows * 4);
+    s.forward_total = off;
+    s.factor = off; off += al((size_t)rows * 4);
+    s.kept = off; off += al((size_t)rows * dim * e);
+    s.G = off; off += al((size_t)rows * s.ld * e);
+    s.Gt = off; off += s.tail && !s.held ? al((size_t)rows * vec * e) : 0;
+    s.acc = off; off += many ? al((size_t)rows * dim * 4) : 0;
+    s.wt = off; off += s.tail ? al((size_t)vec * dim * e) : 0;
+    s.gwt = off; off += s.tail ? al((size_t)vec * dim * e) : 0;
+    int64_t split = 0;
+    for (int64_t n : {s.piece, s.piece > 0 ? s.main % s.piece : 0, s.tail ? vec : 0}) {
+        split = std::max(split, split_floats(h, rows, dim, n));
+        split = std::max(split, split_floats(h, n, dim, rows));
+    }
+    s.splitk = off; off += al((size_t)split * 4);
+    s.total = off;
+    return s;
+}
+
+rdcn_status check_soft(const rdcn_handle* h, int64_t rows, int64_t dim, int64_t classes) {
+    if (!h || rows < 0 || dim <= 0 || classes <= 0) return RDCN_ERR_ARG;
+    if (dim % (h->bf16 ? 8 : 4)) return RDCN_ERR_UNSUPPORTED;
+    if (rows > ((int64_t)1 << 24) || dim > ((int64_t)1 << 20) || classes > ((int64_t)1 << 27) ||
+        rows * classes > (int64_t)1 << 44)
+        return RDCN_ERR_UNSUPPORTED;
+    return RDCN_OK;
+}
+
+// One product of the gradient (both K ranges may be split). With acc_in its result is added to that; the
+// sum goes to out (storage type) when `last`, else to acc.
+hipError_t soft_product(rdcn_handle* h, int kind, GemmArgs g, const float* acc_in, float* acc, void* out, bool last,
+                        float* splitk, hipStream_t s) {
+    const GemmPlan p = plan_gemm(g.M, g.N, g.K, h->bf16, true);
+    const int64_t n = g.M * g.N;
+    g.scale = 1.0f;
+    g.ldc = g.ldx = g.N;
+    if (p.splits > 1) {
+        g.epi = EPI_PARTIAL;
+        g.c = splitk;
+    } else if (acc_in) {
+        g.epi = EPI_RESID;
+        g.gin = acc_in; g.gin_f32 = true;
+        g.c = acc;
+    } else {
+        g.epi = last ? EPI_STORE : EPI_STORE_F32;
+        g.c = last ? out : (void*)acc;
+    }
+    {
+        ProfScope ps(h, kind, s);
+        const hipError_t e = launch_gemm(g, p, h->bf16, s);
+        if (e != hipSuccess) return e;
+    }
+    if (p.splits == 1 && (!last || !acc_in)) return hipSuccess;
+    ProfScope ps(h, RDCN_KERNEL_SPLITK_REDUCE, s);
+    if (p.splits == 1) return launch_soft_reduce(acc, 1, n, nullptr, nullptr, out, h->bf16, s);
+    return launch_soft_reduce(splitk, p.splits, n, acc_in, last ? nullptr : acc, out, h->bf16, s);
+}
+
+// The logits product and the join of its pairs; e != NULL also keeps the exponentials (row stride ld).
+rdcn_status soft_forward(rdcn_handle* h, const SoftPlan& S, int64_t rows, int64_t dim, int64_t classes, const void* x,
+                         const void* w, const float* offset, const void* labels, float logit_scale,
+                         const float* row_weight, float scale, float* loss, float* lse, char* sc, void* e, int64_t ld,
+                         float* factor, hipStream_t s) {
+    GemmArgs g{};
+    g.M = rows; g.N = classes; g.K = dim;
+    g.a = x; g.lda = dim;
+    g.b = w; g.ldb = dim;
+    g.epi = EPI_SOFT_FWD; g.scale = logit_scale;
+    g.offset = offset;
+    g.labels = labels; g.labels64 = h->ids64;
+    g.zlabel = (float*)(sc + S.zlabel);
+    g.softpart = (float2*)(sc + S.part);
+    g.c = e; g.ldc = ld;
+    {
+        ProfScope ps(h, RDCN_KERNEL_HEAD_FWD_GEMM, s);
+        RDCN_TRY(launch_gemm(g, plan_gemm(rows, classes, dim, h->bf16, false), h->bf16, s));
+    }
+    SoftRows r{};
+    r.rows = rows; r.tiles = S.tiles; r.classes = classes;
+    r.softpart = g.softpart; r.zlabel = g.zlabel;
+    r.labels = labels; r.labels64 = h->ids64;
+    r.row_weight = row_weight; r.scale = scale;
+    r.loss = loss; r.lse = lse; r.factor = factor;
+    r.err = h->err;
+    ProfScope ps(h, RDCN_KERNEL_HEAD_LOSS, s);
+    return hip_status(launch_soft_rows(r, s));
 }
 
 }  // namespace
@@ -1045,6 +1184,112 @@ rdcn_status rdcn_head_backward(rdcn_handle* h, int64_t batch, const void* x, con
     }
     ProfScope ps(h, RDCN_KERNEL_HEAD_COLSUM, s);
     return hip_status(launch_vec_sums(B, sums, s));
+}
+
+rdcn_status rdcn_softmax_loss_workspace(const rdcn_handle* h, int64_t rows, int64_t dim, int64_t classes,
+                                        size_t* forward_bytes, size_t* grad_bytes) {
+    rdcn_status st = check_soft(h, rows, dim, classes);
+    if (st != RDCN_OK) return st;
+    if (!forward_bytes || !grad_bytes) return RDCN_ERR_ARG;
+    const SoftPlan S = soft_plan(h, rows, dim, classes);
+    *forward_bytes = S.forward_total;
+    *grad_bytes = S.total;
+    return RDCN_OK;
+}
+
+rdcn_status rdcn_softmax_loss_forward(rdcn_handle* h, int64_t rows, int64_t dim, int64_t classes, const void* x,
+                                      const void* w, const float* offset, const void* labels, float logit_scale,
+                                      float* loss, float* lse, void* scratch, size_t scratch_bytes, void* stream) {
+    rdcn_status st = check_soft(h, rows, dim, classes);
+    if (st != RDCN_OK) return st;
+    if (!std::isfinite(logit_scale)) return RDCN_ERR_ARG;
+    if (rows == 0) return RDCN_OK;
+    if (!x || !a16(x) || !w || !a16(w) || !labels || !loss || !lse) return RDCN_ERR_ARG;
+    const SoftPlan S = soft_plan(h, rows, dim, classes);
+    if (!scratch || !aligned256(scratch) || scratch_bytes < S.forward_total) return RDCN_ERR_WORKSPACE;
+    return soft_forward(h, S, rows, dim, classes, x, w, offset, labels, logit_scale, nullptr, 0.0f, loss, lse,
+                        (char*)scratch, nullptr, 0, nullptr, (hipStream_t)stream);
+}
+
+rdcn_status rdcn_softmax_loss_grad(rdcn_handle* h, int64_t rows, int64_t dim, int64_t classes, const void* x,
+                                   const void* w, const float* offset, const void* labels, float logit_scale,
+                                   const float* row_weight, float scale, float* loss, float* lse, void* grad_x,
+                                   void* grad_w, void* scratch, size_t scratch_bytes, void* stream) {
+    rdcn_status st = check_soft(h, rows, dim, classes);
+    if (st != RDCN_OK) return st;
+    if (!std::isfinite(logit_scale) || !std::isfinite(scale)) return RDCN_ERR_ARG;
+    if (!w || !a16(w) || !grad_w || !a16(grad_w)) return RDCN_ERR_ARG;
+    hipStream_t s = (hipStream_t)stream;
+    const size_t e = eb(h);
+    if (rows == 0) return hip_status(launch_fill_zero((float*)grad_w, classes * dim * (int64_t)e / 4, s));
+    if (!x || !a16(x) || !labels || !loss || !lse || !grad_x || !a16(grad_x)) return RDCN_ERR_ARG;
+    const SoftPlan S = soft_plan(h, rows, dim, classes);
+    if (!scratch || !aligned256(scratch) || scratch_bytes < S.total) return RDCN_ERR_WORKSPACE;
+    char* sc = (char*)scratch;
+    float* const factor = (float*)(sc + S.factor);
+    float* const acc = (float*)(sc + S.acc);
+    float* const splitk = (float*)(sc + S.splitk);
+    const void* const kept = sc + S.kept;
+    char* const G = sc + S.G;
+    // the gradient of the logits carries the logits' own scale
+    if ((st = soft_forward(h, S, rows, dim, classes, x, w, offset, labels, logit_scale, row_weight, scale * logit_scale,
+                           loss, lse, sc, S.held ? G : nullptr, S.ld, factor, s)) != RDCN_OK)
+        return st;
+    RDCN_TRY(launch_soft_kept_rows(rows, dim, classes, x, labels, h->ids64, sc + S.kept, h->bf16, s));
+    if (S.held) {
+        SoftNorm n{};
+        n.rows = rows; n.classes = classes; n.ld = S.ld; n.tile = S.tile;
+        n.softpart = (const float2*)(sc + S.part);
+        n.zlabel = (const float*)(sc + S.zlabel);
+        n.lse = lse; n.factor = factor;
+        n.labels = labels; n.labels64 = h->ids64;
+        n.e = G;
+        ProfScope ps(h, RDCN_KERNEL_HEAD_OUT_BWD, s);
+        RDCN_TRY(launch_soft_normalize(n, h->bf16, s));
+    }
+    // `n` classes from `first` on, whose rows of w stand at wp and whose gradient rows go to gwp
+    bool begun = false;
+    auto piece = [&](int64_t first, int64_t n, int64_t real, const void* wp, void* gwp, char* g0, int64_t ldg,
+                     bool last) -> hipError_t {
+        if (!S.held) {
+            GemmArgs g{};
+            g.M = rows; g.N = real; g.K = dim;
+            g.a = x; g.lda = dim;
+            g.b = wp; g.ldb = dim;
+            g.epi = EPI_SOFT_GRAD; g.scale = logit_scale;
+            g.offset = offset ? offset + first : nullptr;
+            g.labels = labels; g.labels64 = h->ids64; g.label0 = first;
+            g.rowv = lse; g.rowg = factor;
+            g.c = g0; g.ldc = ldg;
+            ProfScope ps(h, RDCN_KERNEL_HEAD_FWD_GEMM, s);
+            const hipError_t e1 = launch_gemm(g, plan_gemm(rows, real, dim, h->bf16, false), h->bf16, s);
+            if (e1 != hipSuccess) return e1;
+        }
+        GemmArgs gx{};
+        gx.M = rows; gx.N = dim; gx.K = n;
+        gx.a = g0; gx.lda = ldg;
+        gx.b = wp; gx.ldb = dim; gx.b_kstrided = true;
+        hipError_t e2 = soft_product(h, RDCN_KERNEL_HEAD_GX_GEMM, gx, begun ? acc : nullptr, acc, grad_x, last, splitk, s);
+        if (e2 != hipSuccess) return e2;
+        begun = true;
+        GemmArgs gw{};
+        gw.M = n; gw.N = dim; gw.K = rows;
+        gw.a = g0; gw.lda = ldg; gw.a_kstrided = true;
+        gw.b = kept; gw.ldb = dim; gw.b_kstrided = true;
+        return soft_product(h, RDCN_KERNEL_HEAD_GW_GEMM, gw, nullptr, nullptr, gwp, true, splitk, s);
+    };
+    for (int64_t v = 0; v < S.main; v += S.piece) {
+        const int64_t n = std::min(S.piece, S.main - v);
+        RDCN_TRY(piece(v, n, n, (const char*)w + (size_t)v * dim * e, (char*)grad_w + (size_t)v * dim * e, G, S.ld,
+                       v + n == S.main && S.tail == 0));
+    }
+    if (S.tail) {
+        RDCN_TRY(launch_soft_pack_tail((int)S.tail, dim, (const char*)w + (size_t)S.main * dim * e, sc + S.wt, s));
+        RDCN_TRY(piece(S.main, 8, S.tail, sc + S.wt, sc + S.gwt, S.held ? G + (size_t)S.main * e : sc + S.Gt,
+                       S.held ? S.ld : 8, true));
+        RDCN_TRY(launch_soft_unpack_tail((int)S.tail, dim, sc + S.gwt, (char*)grad_w + (size_t)S.main * dim * e, s));
+    }
+    return RDCN_OK;
 }
 
 rdcn_status rdcn_profile_start(rdcn_handle* h, int32_t max_launches, uint32_t kernel_mask) {

@@ -17,11 +17,21 @@ enum GemmEpi {
     // MLP layers (bf16 storage, A K-contiguous):
     EPI_MLP_FWD = 6,    // c = ReLU(scale*acc + bias[n]) * (rowv ? sigmoid(rowv[m]) : 1);
                         // with c2: an f16 copy of c (c2_kind C2_F16, err needed)
-    EPI_MLP_BWD = 7     // v = scale*acc + (colv ? rowv[m] * colv[n] : 0);
+    EPI_MLP_BWD = 7,    // v = scale*acc + (colv ? rowv[m] * colv[n] : 0);
                         // act == NULL: c = v;
                         // else c = v * [act[m, n] > 0] * (rowg ? sigmoid(rowg[m]) : 1), and with
                         // rowpart: rowpart[(n0 / BN) * M + m] = sum over the tile's columns of v * act
+    // Softmax loss (both operands K-contiguous), z = scale*acc + offset[n], -inf where offset[n] is:
+    EPI_SOFT_FWD = 8,   // softpart[(n0 / BN) * M + m] = (max, sum of exp(z - max)) over the tile's columns;
+                        // zlabel[m] = z at the row's label, if it is one of the tile's columns; with c:
+                        // c = exp(z - max) (f16 times SOFT_E_SCALE, or float), zero in the pad of a row
+    EPI_SOFT_GRAD = 9   // c = rowg[m] * (exp(z - rowv[m]) - [n is the row's label]) (storage type), zero
+                        // where rowg[m] is 0 or z is -inf and in the pad of a row
 };
+
+// exp(z - max) of a tile's row is held in f16 times this (a power of two): values down to
+// 2^-29 of the row's largest in the tile keep all 11 bits, down to 2^-39 they are not zero.
+constexpr float SOFT_E_SCALE = 32768.f;
 
 // What an optional second output plane c2 receives (same row stride as c).
 enum GemmC2 {
@@ -66,6 +76,13 @@ struct GemmArgs {
     const float* rowg;
     const void* act;
     float* rowpart;
+    // softmax loss epilogues (rowv: log-sum-exp, rowg: the row's factor)
+    const float* offset;  // [N] or NULL
+    const void* labels;   // [M] int32 or int64; column n stands for class label0 + n
+    bool labels64;
+    int64_t label0;
+    float* zlabel;        // [M]
+    float2* softpart;     // [gemm_soft_tiles][M]
     int group_m;        // set from GemmPlan::group_m by launch_gemm
 };
 
@@ -85,6 +102,8 @@ GemmPlan plan_gemm(int64_t M, int64_t N, int64_t K, bool bf16, bool allow_split,
 hipError_t launch_gemm(const GemmArgs& g, const GemmPlan& p, bool bf16, hipStream_t s);
 // Column tiles of an MLP GEMM under plan p (the rowpart partials per row).
 inline int64_t gemm_tiles_n(int64_t N, const GemmPlan& p) { return (N + p.bn - 1) / p.bn; }
+// Column tiles of a softmax loss product (EPI_SOFT_FWD) and the columns of one: launch_gemm's choice of blocks.
+int64_t gemm_soft_tiles(int64_t M, int64_t N, int64_t K, const GemmPlan& p, bool bf16, int* columns);
 hipError_t launch_splitk_reduce(const float* part, int splits, int64_t MN, float* out, hipStream_t s);
 // dst = f16(src) for n bf16 values (n % 8 == 0, 16-byte aligned); sets ERR_BIT_F16_RANGE
 // in err when a value is beyond the f16 range.

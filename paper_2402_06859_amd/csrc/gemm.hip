@@ -273,6 +273,73 @@ __device__ __forceinline__ float mlp_epilogue8(const GemmArgs& g, int64_t m, int
     return dot;
 }
 
+// Which epilogue a kernel carries.
+enum { EK_PLAIN = 0, EK_MLP = 1, EK_SOFT = 2 };
+
+// Base-2 exponential unit for bf16 models (its error, about |x| 2^-24, is far below the rounding
+// of the gradient to bf16); the library function for float ones.
+template <typename T>
+__device__ __forceinline__ float soft_exp(float x) {
+    return sizeof(T) == 2 ? __expf(x) : expf(x);
+}
+
+// Softmax loss epilogues on W consecutive columns n .. n+W-1 of row m. The LANES threads of a
+// row are an aligned group of lanes and all call this; `in` is false for rows past M and
+// column groups past N. One pass over the logits where they stand: the tile's running maximum and
+// sum go out as two floats per row, so z itself never reaches memory.
+template <typename T, int W, int LANES>
+__device__ __forceinline__ void soft_epilogue(const GemmArgs& g, int64_t m, int64_t n, int64_t tile, bool in, float* v) {
+    const float NEG = -__builtin_huge_valf();
+    int64_t lab = -1;  // the label's column in this group, if 0 .. W-1
+    if (in) {
+        lab = (g.labels64 ? ((const int64_t*)g.labels)[m] : (int64_t)((const int32_t*)g.labels)[m]) - g.label0 - n;
+#pragma unroll
+        for (int e = 0; e < W; ++e) {
+            const float o = g.offset && n + e < g.N ? g.offset[n + e] : 0.f;
+            v[e] = n + e >= g.N || o == NEG ? NEG : v[e] * g.scale + o;
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < W; ++e) v[e] = NEG;
+    }
+    if (g.epi == EPI_SOFT_GRAD) {
+        if (!in) return;
+        const float lse = g.rowv[m], f = g.rowg[m];
+#pragma unroll
+        for (int e = 0; e < W; ++e)
+            v[e] = f == 0.f || v[e] == NEG ? 0.f : f * (soft_exp<T>(v[e] - lse) - (lab == e ? 1.f : 0.f));
+        T* const out = (T*)g.c + m * g.ldc + n;
+        if constexpr (W == 8) store8<T>(out, v);
+        else store4<T>(out, v);
+        return;
+    }
+    float mx = v[0];
+#pragma unroll
+    for (int e = 1; e < W; ++e) mx = fmaxf(mx, v[e]);
+#pragma unroll
+    for (int o = 1; o < LANES; o <<= 1) mx = fmaxf(mx, __shfl_xor(mx, o));
+    float sum = 0.f;
+#pragma unroll
+    for (int e = 0; e < W; ++e) {
+        if (lab == e) g.zlabel[m] = v[e];
+        v[e] = v[e] == NEG ? 0.f : soft_exp<T>(v[e] - mx);  // (a NaN stays one)
+        sum += v[e];
+    }
+#pragma unroll
+    for (int o = 1; o < LANES; o <<= 1) sum += __shfl_xor(sum, o);
+    if (!in) return;
+    if (n == tile * (W * LANES)) g.softpart[tile * g.M + m] = make_float2(mx, sum);
+    if (!g.c) return;
+    if constexpr (W == 8) {
+        bool ovf = false;
+#pragma unroll
+        for (int e = 0; e < W; ++e) v[e] *= SOFT_E_SCALE;
+        *(u32x4_t*)((_Float16*)g.c + m * g.ldc + n) = pack_f16x8(v, ovf);
+    } else {
+        store4<float>((float*)g.c + m * g.ldc + n, v);
+    }
+}
+
 __device__ __forceinline__ int xcd_remap(int id, int n) {
     // Workgroups are dispatched round-robin over the 8 XCDs; give each XCD a
     // contiguous range of tiles so neighbouring tiles share its L2. The last
@@ -733,7 +800,7 @@ struct Pipe {
 // C[m = tile_m + lane % 32][n = tile_n + 8 q + 4 (lane / 32) + e] in acc[4 q + e]. The
 // block is staged row-major, 64 rows at a time, then each thread applies the epilogue
 // to 8 consecutive columns of a row.
-template <int BM, int BN, int WM, int WN, bool M32, typename T, bool MLP, int THREADS, int RING, typename Acc,
+template <int BM, int BN, int WM, int WN, bool M32, typename T, int EK, int THREADS, int RING, typename Acc,
           int TM, int TN>
 __device__ __forceinline__ void block_epilogue(const GemmArgs& g, int64_t m0, int64_t n0, int z, Acc (&acc)[TM][TN],
                                                bf16_t* smem, int tid) {
@@ -773,7 +840,13 @@ __device__ __forceinline__ void block_epilogue(const GemmArgs& g, int64_t m0, in
         for (int q = tid; q < CH * (BN / 8); q += THREADS) {
             const int row = q / (BN / 8), col = (q % (BN / 8)) * 8;
             const int64_t m = m0 + h * CH + row, n = n0 + col;
-            if (!MLP) {
+            if constexpr (EK == EK_SOFT) {
+                static_assert(CH * (BN / 8) % THREADS == 0, "whole lane groups per row");
+                float v[8];
+                *(f32x4_t*)v = *(const f32x4_t*)(cs + row * CP + col);
+                *(f32x4_t*)(v + 4) = *(const f32x4_t*)(cs + row * CP + col + 4);
+                soft_epilogue<T, 8, BN / 8>(g, m, n, n0 / BN, m < g.M && n < g.N, v);
+            } else if constexpr (EK == EK_PLAIN) {
                 if (m >= g.M || n >= g.N) continue;
                 float v[8];
                 *(f32x4_t*)v = *(const f32x4_t*)(cs + row * CP + col);
@@ -799,7 +872,7 @@ __device__ __forceinline__ void block_epilogue(const GemmArgs& g, int64_t m0, in
 }
 
 // C = A B^T with an ST-stage direct-to-LDS pipeline of KB-deep stages (see layouts above).
-template <int BM, int BN, bool AKS, bool BKS, int ST, int WM, int WN, bool M32, typename T, bool MLP, bool F16, int KB>
+template <int BM, int BN, bool AKS, bool BKS, int ST, int WM, int WN, bool M32, typename T, int EK, bool F16, int KB>
 __global__ __launch_bounds__(64 * WM * WN, (ST == 2 && WM * WN == 4) ? 2 : 1)
 __attribute__((amdgpu_waves_per_eu(WM * WN == 8 ? 2 : 1, WM * WN == 8 ? 2 : 8))) void k_gemm_mfma(GemmArgs g) {
     using P = Pipe<BM, BN, AKS, BKS, ST, WM, WN, M32, F16, KB>;
@@ -874,7 +947,7 @@ __attribute__((amdgpu_waves_per_eu(WM * WN == 8 ? 2 : 1, WM * WN == 8 ? 2 : 8)))
     }
     wait_vmcnt(0);  // the trailing re-read loads land before the workgroup ends
 
-    block_epilogue<BM, BN, WM, WN, M32, T, MLP, P::THREADS, ST * P::STAGE_ELEMS>(g, c.m0, c.n0, z, acc, smem, tid);
+    block_epilogue<BM, BN, WM, WN, M32, T, EK, P::THREADS, ST * P::STAGE_ELEMS>(g, c.m0, c.n0, z, acc, smem, tid);
 }
 
 // ---------------------------------------------------------------------------
@@ -890,7 +963,7 @@ __attribute__((amdgpu_waves_per_eu(WM * WN == 8 ? 2 : 1, WM * WN == 8 ? 2 : 8)))
 // ---------------------------------------------------------------------------
 constexpr int ST_KW = 8;
 
-template <int TM, int TN, int ST, int KB, typename T, bool MLP, bool F16>
+template <int TM, int TN, int ST, int KB, typename T, int EK, bool F16>
 __global__ __launch_bounds__(64 * ST_KW) void k_gemm_stream(GemmArgs g) {
     constexpr int BM = 16 * TM, BN = 16 * TN, CP = BN + 4, ROWS = BM < 32 ? BM : 32;
     constexpr int STAGE = (BM + BN) * KB;                  // elements of one wave's stage
@@ -980,7 +1053,7 @@ __global__ __launch_bounds__(64 * ST_KW) void k_gemm_stream(GemmArgs g) {
         for (int c = threadIdx.x; c < ROWS * (BN / 8); c += 64 * ST_KW) {
             const int row = c / (BN / 8), col = c % (BN / 8) * 8;
             const int64_t m = m0 + h * ROWS + row, n = n0 + col;
-            if (m >= g.M || n >= g.N) continue;
+            if (EK != EK_SOFT && (m >= g.M || n >= g.N)) continue;
             const float* const p = cs + row * CP + col;
             f32x4_t s0 = *(const f32x4_t*)p, s1 = *(const f32x4_t*)(p + 4);
 #pragma unroll
@@ -989,7 +1062,8 @@ __global__ __launch_bounds__(64 * ST_KW) void k_gemm_stream(GemmArgs g) {
                 s1 += *(const f32x4_t*)(p + w * ROWS * CP + 4);
             }
             float v[8] = {s0.x, s0.y, s0.z, s0.w, s1.x, s1.y, s1.z, s1.w};
-            if constexpr (MLP) (void)mlp_epilogue8<T>(g, m, n, v, ovf);
+            if constexpr (EK == EK_SOFT) soft_epilogue<T, 8, BN / 8>(g, m, n, n0 / BN, m < g.M && n < g.N, v);
+            else if constexpr (EK == EK_MLP) (void)mlp_epilogue8<T>(g, m, n, v, ovf);
             else epilogue8<T>(g, m, n, 0, v, ovf);
         }
     }
@@ -1001,14 +1075,15 @@ hipError_t launch_stream(const GemmArgs& g, hipStream_t s) {
     if (g.a_kstrided || g.b_kstrided || g.epi == EPI_MLP_BWD || g.epi == EPI_PARTIAL) return hipErrorInvalidValue;
     const int64_t tiles = ((g.M + 16 * TM - 1) / (16 * TM)) * ((g.N + 16 * TN - 1) / (16 * TN));
     const dim3 grid((unsigned)tiles), block(64 * ST_KW);
-    const bool mlp = g.epi == EPI_MLP_FWD;
+    const bool mlp = g.epi == EPI_MLP_FWD, soft = g.epi == EPI_SOFT_FWD || g.epi == EPI_SOFT_GRAD;
     if (g.ops_f16) {
-        if (g.a2) return hipErrorInvalidValue;
-        if (mlp) hipLaunchKernelGGL((k_gemm_stream<TM, TN, ST, KB, bf16_t, true, true>), grid, block, 0, s, g);
-        else hipLaunchKernelGGL((k_gemm_stream<TM, TN, ST, KB, bf16_t, false, true>), grid, block, 0, s, g);
+        if (g.a2 || soft) return hipErrorInvalidValue;
+        if (mlp) hipLaunchKernelGGL((k_gemm_stream<TM, TN, ST, KB, bf16_t, EK_MLP, true>), grid, block, 0, s, g);
+        else hipLaunchKernelGGL((k_gemm_stream<TM, TN, ST, KB, bf16_t, EK_PLAIN, true>), grid, block, 0, s, g);
     } else {
-        if (mlp) hipLaunchKernelGGL((k_gemm_stream<TM, TN, ST, KB, bf16_t, true, false>), grid, block, 0, s, g);
-        else hipLaunchKernelGGL((k_gemm_stream<TM, TN, ST, KB, bf16_t, false, false>), grid, block, 0, s, g);
+        if (soft) hipLaunchKernelGGL((k_gemm_stream<TM, TN, ST, KB, bf16_t, EK_SOFT, false>), grid, block, 0, s, g);
+        else if (mlp) hipLaunchKernelGGL((k_gemm_stream<TM, TN, ST, KB, bf16_t, EK_MLP, false>), grid, block, 0, s, g);
+        else hipLaunchKernelGGL((k_gemm_stream<TM, TN, ST, KB, bf16_t, EK_PLAIN, false>), grid, block, 0, s, g);
     }
     return hipGetLastError();
 }
@@ -1047,7 +1122,7 @@ __device__ __forceinline__ f32x4_t frag_f32(const float* __restrict__ x, int64_t
     return v;
 }
 
-template <int SM, int SN, int KW, bool AKS, bool BKS>
+template <int SM, int SN, int KW, bool AKS, bool BKS, bool SOFT>
 __global__ __launch_bounds__(64 * SM * SN * KW) void k_gemm_f32(GemmArgs g) {
     constexpr int THREADS = 64 * SM * SN * KW, BM = 32 * SM, BN = 32 * SN, CP = BN + 4;
     __shared__ __attribute__((aligned(16))) float cs[KW][BM * CP];
@@ -1102,12 +1177,13 @@ __global__ __launch_bounds__(64 * SM * SN * KW) void k_gemm_f32(GemmArgs g) {
     for (int c = threadIdx.x; c < BM * BN / 4; c += THREADS) {
         const int row = c / (BN / 4), col = c % (BN / 4) * 4;
         const int64_t m = m0 + row, n = n0 + col;
-        if (m >= g.M || n >= g.N) continue;
+        if (!SOFT && (m >= g.M || n >= g.N)) continue;
         f32x4_t s = *(const f32x4_t*)(&cs[0][row * CP + col]);
 #pragma unroll
         for (int w = 1; w < KW; ++w) s += *(const f32x4_t*)(&cs[w][row * CP + col]);
         float v[4] = {s.x, s.y, s.z, s.w};
-        epilogue4<float>(g, m, n, z, v);
+        if constexpr (SOFT) soft_epilogue<float, 4, BN / 4>(g, m, n, n0 / BN, m < g.M && n < g.N, v);
+        else epilogue4<float>(g, m, n, z, v);
     }
 }
 
@@ -1115,12 +1191,15 @@ template <int SM, int SN, int KW>
 hipError_t launch_f32(const GemmArgs& g, int splits, hipStream_t s) {
     const int64_t tiles = ((g.M + 32 * SM - 1) / (32 * SM)) * ((g.N + 32 * SN - 1) / (32 * SN));
     const dim3 grid((unsigned)tiles, 1, (unsigned)splits), block(64 * SM * SN * KW);
-    if (g.a_kstrided) {
-        if (g.b_kstrided) hipLaunchKernelGGL((k_gemm_f32<SM, SN, KW, true, true>), grid, block, 0, s, g);
-        else hipLaunchKernelGGL((k_gemm_f32<SM, SN, KW, true, false>), grid, block, 0, s, g);
+    if (g.epi == EPI_SOFT_FWD || g.epi == EPI_SOFT_GRAD) {
+        if (g.a_kstrided || g.b_kstrided || splits != 1) return hipErrorInvalidValue;
+        hipLaunchKernelGGL((k_gemm_f32<SM, SN, KW, false, false, true>), grid, block, 0, s, g);
+    } else if (g.a_kstrided) {
+        if (g.b_kstrided) hipLaunchKernelGGL((k_gemm_f32<SM, SN, KW, true, true, false>), grid, block, 0, s, g);
+        else hipLaunchKernelGGL((k_gemm_f32<SM, SN, KW, true, false, false>), grid, block, 0, s, g);
     } else {
-        if (g.b_kstrided) hipLaunchKernelGGL((k_gemm_f32<SM, SN, KW, false, true>), grid, block, 0, s, g);
-        else hipLaunchKernelGGL((k_gemm_f32<SM, SN, KW, false, false>), grid, block, 0, s, g);
+        if (g.b_kstrided) hipLaunchKernelGGL((k_gemm_f32<SM, SN, KW, false, true, false>), grid, block, 0, s, g);
+        else hipLaunchKernelGGL((k_gemm_f32<SM, SN, KW, false, false, false>), grid, block, 0, s, g);
     }
     return hipGetLastError();
 }
@@ -1142,28 +1221,32 @@ template <int BM, int BN, int ST, int WM, int WN, bool M32, typename T, int KB =
 hipError_t launch_tile(const GemmArgs& g, int splits, hipStream_t s) {
     const int64_t tiles = ((g.M + BM - 1) / BM) * ((g.N + BN - 1) / BN);
     dim3 grid((unsigned)tiles, 1, (unsigned)splits);
-#define RDCN_GEMM(AK, BKS, MLP) \
-    hipLaunchKernelGGL((k_gemm_mfma<BM, BN, AK, BKS, ST, WM, WN, M32, T, MLP, false, KB>), grid, dim3(64 * WM * WN), 0, s, g)
-    if (g.ops_f16) {
+#define RDCN_GEMM(AK, BKS, EK) \
+    hipLaunchKernelGGL((k_gemm_mfma<BM, BN, AK, BKS, ST, WM, WN, M32, T, EK, false, KB>), grid, dim3(64 * WM * WN), 0, s, g)
+    if (g.epi == EPI_SOFT_FWD || g.epi == EPI_SOFT_GRAD) {
+        // softmax loss: logits in one pass over K, both K-contiguous
+        if (g.a_kstrided || g.b_kstrided || g.ops_f16 || g.a2 || splits != 1) return hipErrorInvalidValue;
+        RDCN_GEMM(false, false, EK_SOFT);
+    } else if (g.ops_f16) {
         // f16 operands: the forward products over f16 activations (both K-contiguous;
         // the cross projections and the MLP layers, no split-K for the latter)
         if (g.a_kstrided || g.b_kstrided || g.epi == EPI_MLP_BWD || g.a2) return hipErrorInvalidValue;
         if (g.epi == EPI_MLP_FWD) {
             if (splits != 1) return hipErrorInvalidValue;
-            hipLaunchKernelGGL((k_gemm_mfma<BM, BN, false, false, ST, WM, WN, M32, T, true, true, KB>), grid,
+            hipLaunchKernelGGL((k_gemm_mfma<BM, BN, false, false, ST, WM, WN, M32, T, EK_MLP, true, KB>), grid,
                                dim3(64 * WM * WN), 0, s, g);
         } else {
-            hipLaunchKernelGGL((k_gemm_mfma<BM, BN, false, false, ST, WM, WN, M32, T, false, true, KB>), grid,
+            hipLaunchKernelGGL((k_gemm_mfma<BM, BN, false, false, ST, WM, WN, M32, T, EK_PLAIN, true, KB>), grid,
                                dim3(64 * WM * WN), 0, s, g);
         }
     } else if (g.epi == EPI_MLP_FWD || g.epi == EPI_MLP_BWD) {
         // MLP layers: forward (both K-contiguous) and input gradient (B K-strided), no split-K
         if (g.a_kstrided || splits != 1) return hipErrorInvalidValue;
-        if (g.b_kstrided) RDCN_GEMM(false, true, true); else RDCN_GEMM(false, false, true);
+        if (g.b_kstrided) RDCN_GEMM(false, true, EK_MLP); else RDCN_GEMM(false, false, EK_MLP);
     } else if (g.a_kstrided) {
-        if (g.b_kstrided) RDCN_GEMM(true, true, false); else RDCN_GEMM(true, false, false);
+        if (g.b_kstrided) RDCN_GEMM(true, true, EK_PLAIN); else RDCN_GEMM(true, false, EK_PLAIN);
     } else {
-        if (g.b_kstrided) RDCN_GEMM(false, true, false); else RDCN_GEMM(false, false, false);
+        if (g.b_kstrided) RDCN_GEMM(false, true, EK_PLAIN); else RDCN_GEMM(false, false, EK_PLAIN);
     }
 #undef RDCN_GEMM
     return hipGetLastError();
@@ -1289,6 +1372,40 @@ GemmPlan plan_gemm(int64_t M, int64_t N, int64_t K, bool bf16, bool allow_split,
     return p;
 }
 
+namespace {
+
+// Which streamed block a product of two K-contiguous operands takes (0: none).
+// The streamed blocks as long as one round of them (one or two per CU) covers the
+// output: they finish a K loop in an eighth of the time, but each loads its own
+// operands, so over more rounds the 64 x 64 blocks' reuse wins. us, streamed /
+// 64 x 64, by tiles of the block (in the order below):
+//   K 1856, N 768:   50 rows, 192 tiles 5.7 / 12.8;  256 rows, 192 tiles 6.9 / 13.1;
+//                    512 rows, 192 tiles 9.5 / 13.0;  1024 rows, 384 tiles 18.1 / 13.4
+//   K 4352, N 512:   64 rows, 128 tiles 5.7 / 22.7; 512 rows, 256 tiles 10.5 / 21.8;
+//                    1024 rows, 256 tiles 18.5 / 22.1
+//   K 10624, N 3072: 16 rows, 192 tiles 13.3 / 48.3; 50 rows, 192 tiles 17.5 / 48.5;
+//                    128 rows, 192 tiles 33.5 / 48.6; 256 rows, 384 tiles 62.9 / 49.2
+//   K 256, N 1856:   128 rows, 232 tiles 4.6 / 5.6; 256 rows, 464 tiles 6.9 / 5.8
+// (64 x 32 blocks run shorter stages; at K 256 they and the 64 x 64 ones are level, 6.5 / 6.6 us
+// for 64 x 8192. Between K 512 and the line at 1536 they would be ahead: 300 x 1024 x 512
+// 6.5 / 7.5, 128 x 4096 x 1024 8.2 / 9.9.)
+int stream_block(int64_t M, int64_t N, int64_t K, const GemmPlan& p) {
+    if (p.bm != 64 || p.splits != 1) return 0;
+    auto tiles = [&](int bm, int bn) { return ((M + bm - 1) / bm) * ((N + bn - 1) / bn); };
+    if (tiles(16, 16) <= 256) return 1;
+    if (tiles(32, 32) <= 256) return 2;
+    if (tiles(64, 32) <= 256 && K >= 1536) return 3;
+    return 0;
+}
+
+}  // namespace
+
+int64_t gemm_soft_tiles(int64_t M, int64_t N, int64_t K, const GemmPlan& p, bool bf16, int* columns) {
+    const int st = bf16 ? stream_block(M, N, K, p) : 0;
+    *columns = st == 1 ? 16 : st ? 32 : p.bn;
+    return (N + *columns - 1) / *columns;
+}
+
 hipError_t launch_gemm(const GemmArgs& g, const GemmPlan& p, bool bf16, hipStream_t s) {
     if (g.M == 0 || g.N == 0) return hipSuccess;
     if (!bf16 && (g.epi == EPI_MLP_FWD || g.epi == EPI_MLP_BWD)) return hipErrorInvalidValue;
@@ -1297,25 +1414,12 @@ hipError_t launch_gemm(const GemmArgs& g, const GemmPlan& p, bool bf16, hipStrea
     }
     GemmArgs ga = g;
     ga.group_m = p.group_m;
-    if (p.bm == 64 && p.splits == 1 && !g.a_kstrided && !g.b_kstrided) {
-        // The streamed blocks as long as one round of them (one or two per CU) covers the
-        // output: they finish a K loop in an eighth of the time, but each loads its own
-        // operands, so over more rounds the 64 x 64 blocks' reuse wins. us, streamed /
-        // 64 x 64, by tiles of the block (in the order below):
-        //   K 1856, N 768:   50 rows, 192 tiles 5.7 / 12.8;  256 rows, 192 tiles 6.9 / 13.1;
-        //                    512 rows, 192 tiles 9.5 / 13.0;  1024 rows, 384 tiles 18.1 / 13.4
-        //   K 4352, N 512:   64 rows, 128 tiles 5.7 / 22.7; 512 rows, 256 tiles 10.5 / 21.8;
-        //                    1024 rows, 256 tiles 18.5 / 22.1
-        //   K 10624, N 3072: 16 rows, 192 tiles 13.3 / 48.3; 50 rows, 192 tiles 17.5 / 48.5;
-        //                    128 rows, 192 tiles 33.5 / 48.6; 256 rows, 384 tiles 62.9 / 49.2
-        //   K 256, N 1856:   128 rows, 232 tiles 4.6 / 5.6; 256 rows, 464 tiles 6.9 / 5.8
-        // (64 x 32 blocks run shorter stages; at K 256 they and the 64 x 64 ones are level, 6.5 / 6.6 us
-        // for 64 x 8192. Between K 512 and the line at 1536 they would be ahead: 300 x 1024 x 512
-        // 6.5 / 7.5, 128 x 4096 x 1024 8.2 / 9.9.)
-        auto tiles = [&](int bm, int bn) { return ((g.M + bm - 1) / bm) * ((g.N + bn - 1) / bn); };
-        if (tiles(16, 16) <= 256) return launch_stream<1, 1, 2, 64>(ga, s);
-        if (tiles(32, 32) <= 256) return launch_stream<2, 2, 2, 64>(ga, s);
-        if (tiles(64, 32) <= 256 && g.K >= 1536) return launch_stream<4, 2, 2, 32>(ga, s);
+    if (!g.a_kstrided && !g.b_kstrided) {
+        switch (stream_block(g.M, g.N, g.K, p)) {
+            case 1: return launch_stream<1, 1, 2, 64>(ga, s);
+            case 2: return launch_stream<2, 2, 2, 64>(ga, s);
+            case 3: return launch_stream<4, 2, 2, 32>(ga, s);
+        }
     }
     // the 32 x 32 multiply loops' offsets (see plan_gemm)
     if ((p.bm == 256 || (p.bm == 128 && p.stages == 3)) &&

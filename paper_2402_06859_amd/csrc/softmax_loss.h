@@ -1,0 +1,54 @@
+// Launchers of the softmax loss kernels around its products (see softmax_loss.hip).
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace rdcn {
+
+// lse, loss and (optional) the rows' gradient factors from the logits product's partials
+// softpart [tiles][rows] and zlabel [rows]. A label outside [0, classes) gives loss 0 and factor
+// 0; one at or past `classes` also sets the index bit of *err. factor = scale * (row_weight or 1).
+struct SoftRows {
+    int64_t rows, tiles, classes;
+    const float2* softpart;
+    const float* zlabel;
+    const void* labels;
+    bool labels64;
+    const float* row_weight;
+    float scale;
+    float* loss;
+    float* lse;
+    float* factor;  // may be NULL (no gradient)
+    int* err;
+};
+hipError_t launch_soft_rows(const SoftRows& a, hipStream_t s);
+
+// e [rows][ld] (f16 times SOFT_E_SCALE, or float with T float): exponentials relative to their tile's
+// maximum -> the loss's gradient in the logits, in place (storage type).
+struct SoftNorm {
+    int64_t rows, classes, ld;
+    int tile;  // columns of a tile
+    const float2* softpart;
+    const float* zlabel;
+    const float* lse;
+    const float* factor;
+    const void* labels;
+    bool labels64;
+    void* e;
+};
+hipError_t launch_soft_normalize(const SoftNorm& a, bool bf16, hipStream_t s);
+
+// out = x, with zeros in the rows that have no label in [0, classes).
+hipError_t launch_soft_kept_rows(int64_t rows, int64_t dim, int64_t classes, const void* x, const void* labels,
+                                 bool labels64, void* out, bool bf16, hipStream_t s);
+
+// dst [8][dim] = the n < 8 rows of src, then rows of zeros; and back.
+hipError_t launch_soft_pack_tail(int n, int64_t dim, const void* src, void* dst, hipStream_t s);
+hipError_t launch_soft_unpack_tail(int n, int64_t dim, const void* src, void* dst, hipStream_t s);
+
+// sum over `splits` planes of part (n floats each, in plane order), added to acc if it is not NULL;
+// written to acc_out (float) or, if that is NULL, to out (storage type). n is a multiple of 4.
+hipError_t launch_soft_reduce(const float* part, int splits, int64_t n, const float* acc, float* acc_out, void* out,
+                              bool bf16, hipStream_t s);
+
+}  // namespace rdcn

@@ -1,0 +1,194 @@
+// Softmax loss over a large set of classes: what stands around its products.
+//
+//   z[m, v] = s (x[m] . w[v]) + offset[v],  lse[m] = log sum_v exp(z[m, v]),  loss[m] = lse[m] - z[m, y[m]]
+//   G[m, v] = f[m] (exp(z[m, v] - lse[m]) - [v = y[m]]),  grad_x = G w,  grad_w = G^T x
+//
+// The logits product (gemm.hip, EPI_SOFT_FWD) leaves one (maximum, sum of exponentials) pair per row
+// and column tile; the pairs of a row are joined here: the sum of exponentials over two
+// ranges with maxima a and b is S_a exp(a - c) + S_b exp(b - c) for c = max(a, b).
+#include "device_common.h"
+#include "gemm.h"
+#include "softmax_loss.h"
+
+namespace rdcn {
+
+namespace {
+
+constexpr int ERR_BIT_INDEX = 1;
+constexpr float NEG_INF = -__builtin_huge_valf();
+
+__device__ __forceinline__ int64_t label_of(const void* labels, bool l64, int64_t m) {
+    return l64 ? ((const int64_t*)labels)[m] : (int64_t)((const int32_t*)labels)[m];
+}
+
+__device__ __forceinline__ void join(float& mx, float& sum, float m2, float s2) {
+    const float c = fmaxf(mx, m2);
+    // a range without any visible class has (-inf, 0); the sums of two such stay 0
+    sum = (mx == NEG_INF ? sum : sum * expf(mx - c)) + (m2 == NEG_INF ? s2 : s2 * expf(m2 - c));
+    mx = c;
+}
+
+// 256 threads as rpb rows x (256 / rpb) lanes that stride over the tiles. Few rows take many
+// lanes each (one request over 50000 classes has 782 pairs to join), many rows one lane or few.
+__global__ __launch_bounds__(256) void k_soft_rows(SoftRows a, int rpb) {
+    __shared__ float2 sh[256];
+    const int r = threadIdx.x % rpb, part = threadIdx.x / rpb, parts = 256 / rpb;
+    const int64_t m = (int64_t)blockIdx.x * rpb + r;
+    float mx = NEG_INF, sum = 0.f;
+    if (m < a.rows)
+        for (int64_t t = part; t < a.tiles; t += parts) {
+            const float2 p = a.softpart[t * a.rows + m];
+            join(mx, sum, p.x, p.y);
+        }
+    sh[threadIdx.x] = make_float2(mx, sum);
+    for (int o = parts / 2; o > 0; o >>= 1) {
+        __syncthreads();
+        if (part < o) {
+            const float2 p = sh[threadIdx.x + o * rpb];
+            join(mx, sum, p.x, p.y);
+            sh[threadIdx.x] = make_float2(mx, sum);
+        }
+    }
+    if (part != 0 || m >= a.rows) return;
+    const float lse = mx == NEG_INF && sum == 0.f ? NEG_INF : mx + logf(sum);
+    const int64_t y = label_of(a.labels, a.labels64, m);
+    const bool kept = y >= 0 && y < a.classes;
+    if (y >= a.classes) atomicOr(a.err, ERR_BIT_INDEX);
+    a.lse[m] = lse;
+    // a label whose own class is masked has probability 0: its loss is +inf, also where every class is
+    float loss = 0.f;
+    if (kept) loss = a.zlabel[m] == NEG_INF ? -NEG_INF : lse - a.zlabel[m];
+    a.loss[m] = loss;
+    if (a.factor) a.factor[m] = kept ? a.scale * (a.row_weight ? a.row_weight[m] : 1.f) : 0.f;
+}
+
+// One workgroup per (row, stretch of columns). Reads and writes each element once (2 + 2 bytes); the
+// factor exp(tile's maximum - lse) f is one exponential per tile and row, not per element. The label's
+// own element is taken from z itself, so p - 1 keeps its digits where p is close to 1.
+template <typename T>
+__global__ __launch_bounds__(256) void k_soft_normalize(SoftNorm a) {
+    constexpr int W = st<T>::vec;
+    const int64_t m = blockIdx.y + (int64_t)blockIdx.z * 65535;
+    if (m >= a.rows) return;
+    const float lse = a.lse[m], f = a.factor[m];
+    const int64_t y = label_of(a.labels, a.labels64, m);
+    for (int64_t n = ((int64_t)blockIdx.x * 256 + threadIdx.x) * W; n < a.ld; n += (int64_t)gridDim.x * 256 * W) {
+        const float top = a.softpart[n / a.tile * a.rows + m].x;
+        float v[W];
+        if constexpr (sizeof(T) == 2) unpack_f16x8(*(const u32x4_t*)((const _Float16*)a.e + m * a.ld + n), v);
+        else st<T>::unpack(*(const u32x4_t*)((const float*)a.e + m * a.ld + n), v);
+        const float unit = sizeof(T) == 2 ? 1.f / SOFT_E_SCALE : 1.f;
+        const float c = f == 0.f || top == NEG_INF ? 0.f : f * unit * expf(top - lse);
+#pragma unroll
+        for (int e = 0; e < W; ++e) v[e] = c == 0.f ? 0.f : c * v[e];
+        if (y >= n && y < n + W && f != 0.f) {
+            const float z = a.zlabel[m];
+#pragma unroll
+            for (int e = 0; e < W; ++e)
+                if (y - n == e) v[e] = z == NEG_INF ? 0.f : f * expm1f(z - lse);
+        }
+        *(u32x4_t*)((T*)a.e + m * a.ld + n) = st<T>::pack(v);
+    }
+}
+
+// A row without a label may hold anything (padding behind a sequence, infinities, NaN): its
+// gradient factor is 0, but 0 times such a value would still reach grad_w's sum over the rows.
+template <typename T>
+__global__ __launch_bounds__(256) void k_soft_kept_rows(int64_t rows, int64_t dim, int64_t classes, const T* x,
+                                                        const void* labels, bool labels64, T* out) {
+    constexpr int W = st<T>::vec;
+    const int64_t per = dim / W, n = rows * per;
+    for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < n; i += gridDim.x * 256ll) {
+        const int64_t y = label_of(labels, labels64, i / per);
+        u32x4_t v = {0u, 0u, 0u, 0u};
+        if (y >= 0 && y < classes) v = *(const u32x4_t*)(x + i * W);
+        *(u32x4_t*)(out + i * W) = v;
+    }
+}
+
+__global__ __launch_bounds__(256) void k_soft_pack_tail(int n, int64_t dim, const bf16_t* src, bf16_t* dst) {
+    for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < dim; i += gridDim.x * 256ll)  // 8 values of 8 rows
+        *(u32x4_t*)(dst + i * 8) = i * 8 < n * dim ? *(const u32x4_t*)(src + i * 8) : u32x4_t{0u, 0u, 0u, 0u};
+}
+
+__global__ __launch_bounds__(256) void k_soft_unpack_tail(int n, int64_t dim, const bf16_t* src, bf16_t* dst) {
+    for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < n * dim / 8; i += gridDim.x * 256ll)
+        *(u32x4_t*)(dst + i * 8) = *(const u32x4_t*)(src + i * 8);
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void k_soft_reduce(const float* part, int splits, int64_t n, const float* acc,
+                                                     float* acc_out, T* out) {
+    for (int64_t i = (blockIdx.x * 256ll + threadIdx.x) * 4; i < n; i += gridDim.x * 1024ll) {
+        f32x4_t v = *(const f32x4_t*)(part + i);
+        for (int z = 1; z < splits; ++z) v += *(const f32x4_t*)(part + z * n + i);
+        if (acc) v += *(const f32x4_t*)(acc + i);
+        if (acc_out) {
+            *(f32x4_t*)(acc_out + i) = v;
+        } else if constexpr (sizeof(T) == 4) {
+            *(f32x4_t*)(out + i) = v;
+        } else {
+            *(uint2*)(out + i) = make_uint2(pack_bf16x2(v.x, v.y), pack_bf16x2(v.z, v.w));
+        }
+    }
+}
+
+dim3 blocks_for(int64_t items, int64_t most) {
+    const int64_t b = (items + 255) / 256;
+    return dim3((unsigned)(b < 1 ? 1 : b > most ? most : b));
+}
+
+}  // namespace
+
+hipError_t launch_soft_rows(const SoftRows& a, hipStream_t s) {
+    if (a.rows == 0) return hipSuccess;
+    int rpb = 1;  // about 256 workgroups or more, as long as there are that many rows
+    while (rpb < 64 && a.rows / (2 * rpb) >= 256) rpb *= 2;
+    hipLaunchKernelGGL(k_soft_rows, dim3((unsigned)((a.rows + rpb - 1) / rpb)), dim3(256), 0, s, a, rpb);
+    return hipGetLastError();
+}
+
+hipError_t launch_soft_normalize(const SoftNorm& a, bool bf16, hipStream_t s) {
+    if (a.rows == 0 || a.ld == 0) return hipSuccess;
+    const int64_t per = a.ld / (bf16 ? 8 : 4);
+    const int64_t y = a.rows < 65535 ? a.rows : 65535, z = (a.rows + 65534) / 65535;
+    const dim3 grid(blocks_for((per + 3) / 4, 64).x, (unsigned)y, (unsigned)z);
+    if (bf16) hipLaunchKernelGGL(k_soft_normalize<bf16_t>, grid, dim3(256), 0, s, a);
+    else hipLaunchKernelGGL(k_soft_normalize<float>, grid, dim3(256), 0, s, a);
+    return hipGetLastError();
+}
+
+hipError_t launch_soft_kept_rows(int64_t rows, int64_t dim, int64_t classes, const void* x, const void* labels,
+                                 bool labels64, void* out, bool bf16, hipStream_t s) {
+    if (rows == 0) return hipSuccess;
+    const dim3 grid = blocks_for(rows * dim / (bf16 ? 8 : 4), 4096);
+    if (bf16)
+        hipLaunchKernelGGL(k_soft_kept_rows<bf16_t>, grid, dim3(256), 0, s, rows, dim, classes, (const bf16_t*)x, labels,
+                           labels64, (bf16_t*)out);
+    else
+        hipLaunchKernelGGL(k_soft_kept_rows<float>, grid, dim3(256), 0, s, rows, dim, classes, (const float*)x, labels,
+                           labels64, (float*)out);
+    return hipGetLastError();
+}
+
+hipError_t launch_soft_pack_tail(int n, int64_t dim, const void* src, void* dst, hipStream_t s) {
+    hipLaunchKernelGGL(k_soft_pack_tail, blocks_for(dim, 256), dim3(256), 0, s, n, dim, (const bf16_t*)src, (bf16_t*)dst);
+    return hipGetLastError();
+}
+
+hipError_t launch_soft_unpack_tail(int n, int64_t dim, const void* src, void* dst, hipStream_t s) {
+    hipLaunchKernelGGL(k_soft_unpack_tail, blocks_for(n * dim / 8, 256), dim3(256), 0, s, n, dim, (const bf16_t*)src,
+                       (bf16_t*)dst);
+    return hipGetLastError();
+}
+
+hipError_t launch_soft_reduce(const float* part, int splits, int64_t n, const float* acc, float* acc_out, void* out,
+                              bool bf16, hipStream_t s) {
+    if (n == 0) return hipSuccess;
+    const dim3 grid = blocks_for(n / 4, 4096);
+    if (bf16) hipLaunchKernelGGL(k_soft_reduce<bf16_t>, grid, dim3(256), 0, s, part, splits, n, acc, acc_out, (bf16_t*)out);
+    else hipLaunchKernelGGL(k_soft_reduce<float>, grid, dim3(256), 0, s, part, splits, n, acc, acc_out, (float*)out);
+    return hipGetLastError();
+}
+
+}  // namespace rdcn

@@ -28,7 +28,8 @@ EXPORTS = ["rdcn_create", "rdcn_destroy", "rdcn_dim", "rdcn_workspace_bytes", "q
            "rdcn_check_device_errors", "rdcn_status_string", "rdcn_profile_start", "rdcn_profile_stop",
            "qr_quantize_tables", "qr_embed_gather_q8", "rdcn_head_configure", "rdcn_head_workspace_bytes",
            "rdcn_head_forward", "rdcn_head_logloss", "rdcn_head_backward", "rdcn_set_side_stream",
-           "qr_embed_backward_static"]
+           "qr_embed_backward_static", "rdcn_softmax_loss_workspace", "rdcn_softmax_loss_forward",
+           "rdcn_softmax_loss_grad"]
 EMBED_STATIC_SCRATCH_BYTES = 64 << 20
 
 KERNELS = ["gather", "fwd_down_gemm", "fwd_attention", "fwd_up_gemm", "bwd_pointwise", "bwd_bias", "bwd_gu_gemm",
@@ -131,6 +132,10 @@ def load(build_if_missing: bool = True):
     L.rdcn_head_logloss.argtypes = [vp, i64, vp, vp, ctypes.c_float, vp, vp, vp]
     L.rdcn_head_backward.argtypes = [vp, i64, vp, vp, ctypes.POINTER(RdcnHeadWeights), vp, vp, vp, vp,
                                      ctypes.POINTER(RdcnHeadWeights), vp, vp]
+    f32 = ctypes.c_float
+    L.rdcn_softmax_loss_workspace.argtypes = [vp, i64, i64, i64, ctypes.POINTER(sz), ctypes.POINTER(sz)]
+    L.rdcn_softmax_loss_forward.argtypes = [vp, i64, i64, i64, vp, vp, vp, vp, f32, vp, vp, vp, sz, vp]
+    L.rdcn_softmax_loss_grad.argtypes = [vp, i64, i64, i64, vp, vp, vp, vp, f32, vp, f32, vp, vp, vp, vp, vp, sz, vp]
     L.rdcn_profile_start.argtypes = [vp, ctypes.c_int32, ctypes.c_uint32]
     L.rdcn_set_side_stream.argtypes = [vp, ctypes.c_int32]
     L.rdcn_profile_stop.argtypes = [vp, ctypes.POINTER(ctypes.c_double), ctypes.POINTER(ctypes.c_int64)]
@@ -152,6 +157,10 @@ def _check(fn: str, s: int):
 
 def _ptr(t: Optional[torch.Tensor]):
     return None if t is None else ctypes.c_void_p(t.data_ptr())
+
+
+def _bytes(t: Optional[torch.Tensor]) -> int:
+    return 0 if t is None else t.numel() * t.element_size()
 
 
 def _stream(stream=None):
@@ -298,6 +307,27 @@ class Rdcn:
         _check("rdcn_head_backward", load().rdcn_head_backward(
             self.h, batch, _ptr(x), _ptr(e_cal), ctypes.byref(w), _ptr(saved), _ptr(grad_ycal), _ptr(grad_x),
             _ptr(grad_e), ctypes.byref(g), _ptr(scratch), _stream(stream)))
+
+    # ---- training over many classes
+    def softmax_loss_workspace(self, rows: int, dim: int, classes: int):
+        """Scratch bytes of (softmax_loss_forward, softmax_loss_grad)."""
+        s, t = ctypes.c_size_t(), ctypes.c_size_t()
+        _check("rdcn_softmax_loss_workspace", load().rdcn_softmax_loss_workspace(
+            self.h, rows, dim, classes, ctypes.byref(s), ctypes.byref(t)))
+        return s.value, t.value
+
+    def softmax_loss_forward(self, rows, dim, classes, x, w, offset, labels, logit_scale, loss, lse, scratch,
+                             stream=None):
+        _check("rdcn_softmax_loss_forward", load().rdcn_softmax_loss_forward(
+            self.h, rows, dim, classes, _ptr(x), _ptr(w), _ptr(offset), _ptr(labels), logit_scale, _ptr(loss),
+            _ptr(lse), _ptr(scratch), _bytes(scratch), _stream(stream)))
+
+    def softmax_loss_grad(self, rows, dim, classes, x, w, offset, labels, logit_scale, row_weight, scale, loss, lse,
+                          grad_x, grad_w, scratch, stream=None):
+        _check("rdcn_softmax_loss_grad", load().rdcn_softmax_loss_grad(
+            self.h, rows, dim, classes, _ptr(x), _ptr(w), _ptr(offset), _ptr(labels), logit_scale, _ptr(row_weight),
+            scale, _ptr(loss), _ptr(lse), _ptr(grad_x), _ptr(grad_w), _ptr(scratch), _bytes(scratch),
+            _stream(stream)))
 
     def profile_start(self, max_launches: int = 8192, kernels=None):
         """Time the launches of `kernels` (names from KERNELS; all when None)."""
