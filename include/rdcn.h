@@ -527,6 +527,81 @@ rdcn_status rdcn_softmax_loss_grad(rdcn_handle* h, int64_t rows, int64_t dim, in
                                    void* grad_w, void* scratch, size_t scratch_bytes, void* stream);
 
 /*
+ * AdamW (decoupled weight decay) over many tensors at once. Per element, with
+ * g' = g * grad_scale * clip and t the step number (from 1):
+ *   m' = beta1 m + (1 - beta1) g'
+ *   v' = beta2 v + (1 - beta2) g' g'
+ *   p' = p (1 - lr weight_decay) - lr / (1 - beta1^t) * m' / (sqrt(v') / sqrt(1 - beta2^t) + eps)
+ * each operation one rounding to float (constants rounded once from double).
+ * Weights are float, bf16 with a float master (the master is stepped, the weight
+ * is its nearest bf16), or bf16 alone.
+ * Moments are float, or 8 bits: a block of 256 consecutive elements has one
+ * exponent per moment (the float exponent field of its largest magnitude), in
+ * exps [2 * ceil(n / 256)], first m's, then v's. With top = 127 (m) or 255 (v)
+ * and base = max(8 exponent + 7 - top, 0), a code c > 0 stands for the float
+ * whose bits are (c + base) << 20, code 0 for zero; m's sign is bit 7. So three
+ * mantissa bits, reaching 2^-15 (m) or 2^-31 (v) below the block's largest; a
+ * nonzero v has at least code 1. Zeros are the state to begin with.
+ * stochastic = 1 rounds codes, and bf16 weights without a master, up with the
+ * probability of what is cut off (under rounding to nearest, 0, small steps of a
+ * moving average in 8 bits would all be lost). Its random bits are a hash of
+ * seed, the tensor's place in the list and the element's place (modulo 2^32): pass another
+ * seed each step (with device_step, t * 0x85EBCA6B is added to it, so that a replayed step
+ * draws anew). The result depends on the arguments alone.
+ */
+typedef enum rdcn_moments { RDCN_MOMENTS_F32 = 0, RDCN_MOMENTS_8BIT = 1 } rdcn_moments;
+
+typedef struct rdcn_adamw_tensor {
+    void* param;          /* [n] float or bf16, updated */
+    float* master;        /* [n] float, updated, or NULL (bf16 params only) */
+    const void* grad;     /* [n] float or bf16 */
+    void* m;              /* [n] float or uint8, updated */
+    void* v;              /* [n] as m, updated */
+    uint8_t* exps;        /* 8-bit moments only */
+    int64_t n;            /* elements, may be 0 */
+    double weight_decay;
+    int32_t param_dtype;  /* rdcn_dtype */
+    int32_t grad_dtype;   /* rdcn_dtype */
+    int32_t moments;      /* rdcn_moments */
+    int32_t reserved;     /* must be 0 */
+} rdcn_adamw_tensor;
+
+typedef struct rdcn_adamw_config {
+    double lr, beta1, beta2, eps;  /* betas in [0, 1), eps > 0 (as a float too) */
+    double grad_scale;             /* 1, or what undoes a loss scale */
+    int64_t step;                  /* t >= 1 */
+    const float* device_lr;        /* or NULL; device memory, read by the step instead of lr */
+    const int64_t* device_step;    /* or NULL; the same for step (values below 1 count as 1). With these
+                                      a captured step follows its schedule without being captured again */
+    const float* clip;             /* or NULL; device memory, one float (rdcn_grad_norm's out + 1). A value that is
+                                      not finite leaves every weight and moment as it is */
+    int32_t stochastic;            /* 0 or 1 */
+    uint32_t seed;
+} rdcn_adamw_config;
+
+/*
+ * One step over `count` tensors (<= 65536, each of at most 2^36 elements). The list is read before the call
+ * returns. Tensors' arrays must not overlap (overlapping weights are RDCN_ERR_ARG), and be 16-byte
+ * aligned (exps need not be). 48 tensors go into a launch.
+ */
+rdcn_status rdcn_adamw_step(rdcn_handle* h, const rdcn_adamw_config* cfg, const rdcn_adamw_tensor* tensors, int32_t count,
+                            void* stream);
+
+/* The values that n 8-bit moments stand for, as bf16 (exactly): is_signed = 1 for m with its exponents, 0 for v. */
+rdcn_status rdcn_adamw_values(rdcn_handle* h, int64_t n, const uint8_t* codes, const uint8_t* exps, int32_t is_signed,
+                              void* out, void* stream);
+
+/*
+ * out[0] = |grad_scale| times the 2-norm of all tensors' gradients together, out[1] = the factor that
+ * clips it to max_norm (> 0, +inf for none): max_norm / norm above it, else 1; NaN when the norm is not finite. Only grad,
+ * grad_dtype and n of each tensor are read. Sums are in 64 bits and in a fixed order.
+ */
+rdcn_status rdcn_grad_norm_workspace(const rdcn_handle* h, const rdcn_adamw_tensor* tensors, int32_t count,
+                                     size_t* scratch_bytes);
+rdcn_status rdcn_grad_norm(rdcn_handle* h, const rdcn_adamw_tensor* tensors, int32_t count, float grad_scale,
+                           float max_norm, float* out, void* scratch, size_t scratch_bytes, void* stream);
+
+/*
  * Per-kernel timing with HIP events on the stream each kernel is launched on.
  * After rdcn_profile_start, each launch site whose bit (1 << rdcn_kernel) is
  * set in `kernel_mask` records an event before and after its kernel(s), up to

@@ -1,0 +1,391 @@
+// AdamW over many tensors at once, with moments in 32 bits or in 8, and the norm of their gradients.
+//
+//   g' = g * grad_scale * clip          m' = beta1 m + (1 - beta1) g'     v' = beta2 v + (1 - beta2) g' g'
+//   p' = p (1 - lr wd) - lr / (1 - beta1^t) * m' / (sqrt(v') / sqrt(1 - beta2^t) + eps)
+//
+// Every operation above is one rounding to float in this order (no contraction to fused ones): a step
+// is the same bits wherever an element stands, and 8-bit codes do not hang on how it was compiled.
+//
+// 8-bit moments. A block of 256 elements has one exponent, its largest element's. An
+// element's code is the upper bits of its float (exponent and 3 mantissa bits, bits 20 and up)
+// counted down from the top of the block's exponent: for m a sign and 7 bits, which reach 2^-15
+// of the block's binade, for v 8 bits, 2^-31. Code 0 is the value 0; a nonzero v gets at least
+// code 1, so that m / sqrt(v) never divides by nothing. With 3 mantissa bits a moving average whose
+// step is 1 - beta = 0.1 or 0.001 would stand still under rounding to nearest (half a step is 1/16 to 1/32 of the
+// value), so codes are rounded up with the probability of the part that is cut off: the bits below 20
+// are added to 20 random bits, a hash of (seed, tensor, element). bf16 weights without a float master
+// are rounded the same way, for the same reason.
+#include "adamw.h"
+#include "device_common.h"
+
+namespace rdcn {
+
+namespace {
+
+constexpr int EPT = 8;                      // consecutive elements of a thread
+constexpr int CHUNK = 256 * EPT;            // elements of a workgroup's step
+constexpr int PER_LAUNCH = 48;              // tensors of one launch: their descriptors are kernel arguments
+
+struct Batch {
+    AdamwTensor t[PER_LAUNCH];
+    uint32_t first[PER_LAUNCH + 1];  // first chunk of each tensor
+    int count;
+    uint32_t ordinal0;               // of t[0] among all tensors of the call
+    AdamwScalars a;
+};
+static_assert(sizeof(Batch) <= 4096, "kernel arguments");
+
+struct NormBatch {
+    const void* grad[PER_LAUNCH];
+    int64_t n[PER_LAUNCH];
+    uint32_t first[PER_LAUNCH + 1];
+    uint32_t flags[PER_LAUNCH];
+    int count;
+    double* part;
+};
+
+// The tensor of chunk c: the last one that begins at or before it (tensors of no elements have no chunk).
+__device__ __forceinline__ int tensor_of(const uint32_t* first, int count, uint32_t c) {
+    int lo = 0, hi = count - 1;
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (first[mid] <= c) lo = mid;
+        else hi = mid - 1;
+    }
+    return lo;
+}
+
+__device__ __forceinline__ uint32_t fmix32(uint32_t h) {  // MurmurHash3's 32-bit finalizer
+    h ^= h >> 16;
+    h *= 0x85EBCA6Bu;
+    h ^= h >> 13;
+    h *= 0xC2B2AE35u;
+    return h ^ (h >> 16);
+}
+
+// Bits (from bit 20 up) that code 0 of a block whose largest exponent is e counts from.
+__device__ __forceinline__ uint32_t code_base(uint32_t e, uint32_t top) {
+    const int b = (int)(8 * e + 7) - (int)top;
+    return b > 0 ? (uint32_t)b : 0u;
+}
+__device__ __forceinline__ float decode(uint32_t size, uint32_t base) {
+    return size ? __uint_as_float((size + base) << 20) : 0.f;
+}
+__device__ __forceinline__ uint32_t encode(uint32_t size, uint32_t base, uint32_t top, uint32_t rnd) {
+    const int c = (int)((size + rnd) >> 20) - (int)base;
+    return c < 0 ? 0u : c > (int)top ? top : (uint32_t)c;
+}
+
+// EPT values from p (whole: all inside; else the first `left`), zero past the end.
+__device__ __forceinline__ void load_f32(const float* p, bool whole, int left, float* v) {
+    if (whole) {
+        *(f32x4_t*)v = *(const f32x4_t*)p;
+        *(f32x4_t*)(v + 4) = *(const f32x4_t*)(p + 4);
+    } else {
+#pragma unroll
+        for (int e = 0; e < EPT; ++e) v[e] = e < left ? p[e] : 0.f;
+    }
+}
+__device__ __forceinline__ void load_bf16(const bf16_t* p, bool whole, int left, float* v) {
+    if (whole) {
+        st<bf16_t>::unpack(*(const u32x4_t*)p, v);
+    } else {
+#pragma unroll
+        for (int e = 0; e < EPT; ++e) v[e] = e < left ? bf16_to_f32(p[e]) : 0.f;
+    }
+}
+__device__ __forceinline__ void store_f32(float* p, bool whole, int left, const float* v) {
+    if (whole) {
+        *(f32x4_t*)p = *(const f32x4_t*)v;
+        *(f32x4_t*)(p + 4) = *(const f32x4_t*)(v + 4);
+    } else {
+#pragma unroll
+        for (int e = 0; e < EPT; ++e)
+            if (e < left) p[e] = v[e];
+    }
+}
+__device__ __forceinline__ void load_codes(const uint8_t* p, bool whole, int left, uint32_t* c) {
+    if (whole) {
+        const uint2 w = *(const uint2*)p;
+#pragma unroll
+        for (int e = 0; e < EPT; ++e) c[e] = ((e < 4 ? w.x : w.y) >> (8 * (e & 3))) & 255u;
+    } else {
+#pragma unroll
+        for (int e = 0; e < EPT; ++e) c[e] = e < left ? p[e] : 0u;
+    }
+}
+__device__ __forceinline__ void store_codes(uint8_t* p, bool whole, int left, const uint32_t* c) {
+    if (whole) {
+        *(uint2*)p = make_uint2(c[0] | c[1] << 8 | c[2] << 16 | c[3] << 24, c[4] | c[5] << 8 | c[6] << 16 | c[7] << 24);
+    } else {
+#pragma unroll
+        for (int e = 0; e < EPT; ++e)
+            if (e < left) p[e] = (uint8_t)c[e];
+    }
+}
+
+// The largest magnitude's exponent over the 32 lanes of a block of 256 elements.
+__device__ __forceinline__ uint32_t block_exponent(const float* v) {
+    uint32_t mx = 0;
+#pragma unroll
+    for (int e = 0; e < EPT; ++e) mx = max(mx, __float_as_uint(v[e]) & 0x7FFFFFFFu);
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) mx = max(mx, (uint32_t)__shfl_xor((int)mx, o));
+    return mx >> 23;
+}
+
+__global__ __launch_bounds__(256) void k_adamw(Batch b) {
+#pragma clang fp contract(off)
+    const AdamwScalars& a = b.a;
+    float gs = a.grad_scale;
+    if (a.clip) {
+        const float c = *a.clip;
+        if (!(fabsf(c) < __builtin_huge_valf())) return;  // not finite: the gradients' norm was not, nothing is changed
+        gs *= c;
+    }
+    float step_size = a.step_size, r2 = a.rsqrt_grown2;
+    const bool live = a.device_lr || a.device_step;
+    double lr = a.lr;
+    uint32_t seed = a.seed;
+    if (live) {
+        if (a.device_lr) lr = (double)*a.device_lr;
+        int64_t t = a.device_step ? *a.device_step : a.step;
+        if (t < 1) t = 1;
+        if (a.device_step) seed += (uint32_t)t * 0x85EBCA6Bu;  // a step that is replayed draws anew
+        step_size = (float)(lr / -expm1((double)t * a.logb1));
+        r2 = (float)(1.0 / sqrt(-expm1((double)t * a.logb2)));
+    }
+    const uint32_t chunks = b.first[b.count];
+    for (uint32_t c = blockIdx.x; c < chunks; c += gridDim.x) {
+        const int i = tensor_of(b.first, b.count, c);
+        const AdamwTensor& t = b.t[i];
+        const int64_t at = (int64_t)(c - b.first[i]) * CHUNK + threadIdx.x * EPT;
+        const bool whole = at + EPT <= t.n;
+        const int left = whole ? EPT : at < t.n ? (int)(t.n - at) : 0;
+        const float decay = live ? (float)(1.0 - lr * (double)t.weight_decay) : t.decay;
+        const bool pbf = t.flags & ADAMW_PARAM_BF16, eight = t.flags & ADAMW_8BIT;
+        const int64_t blocks = (t.n + ADAMW_BLOCK - 1) / ADAMW_BLOCK, blk = at / ADAMW_BLOCK;
+        float p[EPT], g[EPT], m[EPT], v[EPT];
+        if (t.flags & ADAMW_GRAD_BF16) load_bf16((const bf16_t*)t.grad + at, whole, left, g);
+        else load_f32((const float*)t.grad + at, whole, left, g);
+        if (t.master) load_f32(t.master + at, whole, left, p);
+        else if (pbf) load_bf16((const bf16_t*)t.param + at, whole, left, p);
+        else load_f32((const float*)t.param + at, whole, left, p);
+        if (eight) {
+            uint32_t cm[EPT], cv[EPT];
+            load_codes((const uint8_t*)t.m + at, whole, left, cm);
+            load_codes((const uint8_t*)t.v + at, whole, left, cv);
+            const uint32_t bm = left ? code_base(t.exps[blk], 127) : 0, bv = left ? code_base(t.exps[blocks + blk], 255) : 0;
+#pragma unroll
+            for (int e = 0; e < EPT; ++e) {
+                const float s = decode(cm[e] & 127u, bm);
+                m[e] = cm[e] & 128u ? -s : s;
+                v[e] = decode(cv[e], bv);
+            }
+        } else {
+            load_f32((const float*)t.m + at, whole, left, m);
+            load_f32((const float*)t.v + at, whole, left, v);
+        }
+#pragma unroll
+        for (int e = 0; e < EPT; ++e) {
+            const float x = g[e] * gs;
+            m[e] = m[e] * a.beta1 + x * a.c1;
+            v[e] = v[e] * a.beta2 + (x * x) * a.c2;
+            const float down = sqrtf(v[e]) * r2 + a.eps;
+            p[e] = p[e] * decay - (m[e] / down) * step_size;
+        }
+        uint32_t h[EPT];
+        const uint32_t key = seed + 0x9E3779B9u * (b.ordinal0 + (uint32_t)i + 1u);
+        const bool chance = a.stochastic && (eight || (pbf && !t.master));
+#pragma unroll
+        for (int e = 0; e < EPT; ++e) h[e] = chance ? fmix32((uint32_t)(at + e) ^ key) : 0;
+        if (t.master) store_f32(t.master + at, whole, left, p);
+        if (!pbf) {
+            store_f32((float*)t.param + at, whole, left, p);
+        } else {
+            bf16_t* const q = (bf16_t*)t.param + at;
+            uint32_t r[EPT];
+#pragma unroll
+            for (int e = 0; e < EPT; ++e) {
+                r[e] = f32_to_bf16(p[e]);
+                if (chance && !t.master && p[e] == p[e])
+                    r[e] = (__float_as_uint(p[e]) + ((h[e] * 0x85EBCA6Bu) >> 16)) >> 16;
+            }
+            if (whole) {
+                *(u32x4_t*)q = u32x4_t{r[0] | r[1] << 16, r[2] | r[3] << 16, r[4] | r[5] << 16, r[6] | r[7] << 16};
+            } else {
+#pragma unroll
+                for (int e = 0; e < EPT; ++e)
+                    if (e < left) q[e] = (bf16_t)r[e];
+            }
+        }
+        if (!eight) {
+            store_f32((float*)t.m + at, whole, left, m);
+            store_f32((float*)t.v + at, whole, left, v);
+            continue;
+        }
+        if (!whole) {  // past the end nothing counts towards the block's largest
+#pragma unroll
+            for (int e = 0; e < EPT; ++e)
+                if (e >= left) m[e] = v[e] = 0.f;
+        }
+        const uint32_t em = block_exponent(m), ev = block_exponent(v);
+        const uint32_t bm = code_base(em, 127), bv = code_base(ev, 255);
+        uint32_t cm[EPT], cv[EPT];
+#pragma unroll
+        for (int e = 0; e < EPT; ++e) {
+            const uint32_t um = __float_as_uint(m[e]), uv = __float_as_uint(v[e]) & 0x7FFFFFFFu;
+            const uint32_t rm = a.stochastic ? h[e] >> 12 : 0x80000u;
+            const uint32_t rv = a.stochastic ? (h[e] * 0x9E3779B1u) >> 12 : 0x80000u;
+            const uint32_t sm = um & 0x7FFFFFFFu;
+            cm[e] = (sm ? encode(sm, bm, 127, rm) : 0u) | (um >> 31) << 7;
+            const uint32_t x = encode(uv, bv, 255, rv);
+            cv[e] = uv == 0 ? 0u : x > 0 ? x : 1u;
+        }
+        store_codes((uint8_t*)t.m + at, whole, left, cm);
+        store_codes((uint8_t*)t.v + at, whole, left, cv);
+        if ((threadIdx.x & 31) == 0 && left) {
+            t.exps[blk] = (uint8_t)em;
+            t.exps[blocks + blk] = (uint8_t)ev;
+        }
+    }
+}
+
+__global__ __launch_bounds__(256) void k_adamw_values(int64_t n, const uint8_t* codes, const uint8_t* exps, uint32_t top,
+                                                      bf16_t* out) {
+    for (int64_t at = (blockIdx.x * 256ll + threadIdx.x) * EPT; at < n; at += gridDim.x * (int64_t)CHUNK) {
+        const bool whole = at + EPT <= n;
+        const int left = whole ? EPT : (int)(n - at);
+        uint32_t c[EPT], r[EPT];
+        load_codes(codes + at, whole, left, c);
+        const uint32_t base = code_base(exps[at / ADAMW_BLOCK], top);
+#pragma unroll
+        for (int e = 0; e < EPT; ++e) {
+            // 3 mantissa bits: the upper half of the float is the bf16 value itself
+            r[e] = __float_as_uint(decode(c[e] & top, base)) >> 16 | (c[e] & ~top) << 8;
+        }
+        if (whole) {
+            *(u32x4_t*)(out + at) = u32x4_t{r[0] | r[1] << 16, r[2] | r[3] << 16, r[4] | r[5] << 16, r[6] | r[7] << 16};
+        } else {
+#pragma unroll
+            for (int e = 0; e < EPT; ++e)
+                if (e < left) out[at + e] = (bf16_t)r[e];
+        }
+    }
+}
+
+// Sum of 256 doubles over a workgroup, in a fixed order; the result is thread 0's.
+__device__ __forceinline__ double block_sum(double x) {
+    __shared__ double sh[4];
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) x += __shfl_xor(x, o);
+    if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = x;
+    __syncthreads();
+    return ((sh[0] + sh[1]) + sh[2]) + sh[3];
+}
+
+// Squares are added in 64 bits: a float gradient's square is exact there, cannot overflow, and the sum of 10^9 of
+// them keeps its digits. The rate of those operations is far from the bound, which is the read.
+__global__ __launch_bounds__(256) void k_grad_norm(NormBatch b) {
+    double s = 0.0;
+    const uint32_t chunks = b.first[b.count];
+    for (uint32_t c = blockIdx.x; c < chunks; c += gridDim.x) {
+        const int i = tensor_of(b.first, b.count, c);
+        const int64_t at = (int64_t)(c - b.first[i]) * CHUNK + threadIdx.x * EPT;
+        const bool whole = at + EPT <= b.n[i];
+        const int left = whole ? EPT : at < b.n[i] ? (int)(b.n[i] - at) : 0;
+        float g[EPT];
+        if (b.flags[i] & ADAMW_GRAD_BF16) load_bf16((const bf16_t*)b.grad[i] + at, whole, left, g);
+        else load_f32((const float*)b.grad[i] + at, whole, left, g);
+#pragma unroll
+        for (int e = 0; e < EPT; ++e) s = fma((double)g[e], (double)g[e], s);
+    }
+    s = block_sum(s);
+    if (threadIdx.x == 0) b.part[blockIdx.x] = s;
+}
+
+__global__ __launch_bounds__(256) void k_grad_norm_end(const double* part, int64_t n, double scale, double max_norm, float* out) {
+    double s = 0.0;
+    for (int64_t i = threadIdx.x; i < n; i += 256) s += part[i];
+    s = block_sum(s);
+    if (threadIdx.x != 0) return;
+    const double norm = sqrt(s) * scale;
+    out[0] = (float)norm;
+    if (!(norm < (double)__builtin_huge_valf())) out[1] = __builtin_nanf("");  // the step that reads it changes nothing
+    else out[1] = norm > max_norm ? (float)(max_norm / norm) : 1.f;
+}
+
+constexpr uint32_t STEP_BLOCKS = 4096, NORM_BLOCKS = 1024;
+
+// Fills `first` for up to PER_LAUNCH tensors from t[at]; returns their chunks.
+uint32_t place(const AdamwTensor* t, int count, uint32_t* first) {
+    uint32_t c = 0;
+    for (int i = 0; i < count; ++i) {
+        first[i] = c;
+        c += (uint32_t)((t[i].n + CHUNK - 1) / CHUNK);
+    }
+    first[count] = c;
+    return c;
+}
+
+}  // namespace
+
+hipError_t launch_adamw(const AdamwTensor* t, int count, const AdamwScalars& a, hipStream_t s) {
+    for (int at = 0; at < count; at += PER_LAUNCH) {
+        Batch b;
+        b.count = count - at < PER_LAUNCH ? count - at : PER_LAUNCH;
+        for (int i = 0; i < b.count; ++i) b.t[i] = t[at + i];
+        const uint32_t chunks = place(t + at, b.count, b.first);
+        if (chunks == 0) continue;
+        b.ordinal0 = (uint32_t)at;
+        b.a = a;
+        hipLaunchKernelGGL(k_adamw, dim3(chunks < STEP_BLOCKS ? chunks : STEP_BLOCKS), dim3(256), 0, s, b);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
+
+int64_t grad_norm_partials(const AdamwTensor* t, int count) {
+    int64_t n = 0;
+    uint32_t first[PER_LAUNCH + 1];
+    for (int at = 0; at < count; at += PER_LAUNCH) {
+        const uint32_t c = place(t + at, count - at < PER_LAUNCH ? count - at : PER_LAUNCH, first);
+        n += c < NORM_BLOCKS ? c : NORM_BLOCKS;
+    }
+    return n;
+}
+
+hipError_t launch_grad_norm(const AdamwTensor* t, int count, float grad_scale, float max_norm, double* part, float* out,
+                            hipStream_t s) {
+    int64_t n = 0;
+    for (int at = 0; at < count; at += PER_LAUNCH) {
+        NormBatch b;
+        b.count = count - at < PER_LAUNCH ? count - at : PER_LAUNCH;
+        const uint32_t chunks = place(t + at, b.count, b.first);
+        for (int i = 0; i < b.count; ++i) {
+            b.grad[i] = t[at + i].grad;
+            b.n[i] = t[at + i].n;
+            b.flags[i] = t[at + i].flags;
+        }
+        if (chunks == 0) continue;
+        b.part = part + n;
+        const uint32_t blocks = chunks < NORM_BLOCKS ? chunks : NORM_BLOCKS;
+        n += blocks;
+        hipLaunchKernelGGL(k_grad_norm, dim3(blocks), dim3(256), 0, s, b);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    hipLaunchKernelGGL(k_grad_norm_end, dim3(1), dim3(256), 0, s, part, n, fabs((double)grad_scale), (double)max_norm, out);
+    return hipGetLastError();
+}
+
+hipError_t launch_adamw_values(int64_t n, const uint8_t* codes, const uint8_t* exps, bool is_signed, void* out,
+                               hipStream_t s) {
+    const int64_t b = (n + CHUNK - 1) / CHUNK;
+    hipLaunchKernelGGL(k_adamw_values, dim3((unsigned)(b < 8192 ? b : 8192)), dim3(256), 0, s, n, codes, exps,
+                       is_signed ? 127u : 255u, (bf16_t*)out);
+    return hipGetLastError();
+}
+
+}  // namespace rdcn

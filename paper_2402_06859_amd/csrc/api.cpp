@@ -10,6 +10,7 @@
 #include <vector>
 
 #include "../../include/rdcn.h"
+#include "adamw.h"
 #include "embed_bwd.h"
 #include "gemm.h"
 #include "head.h"
@@ -483,6 +484,81 @@ rdcn_status soft_forward(rdcn_handle* h, const SoftPlan& S, int64_t rows, int64_
     ProfScope ps(h, RDCN_KERNEL_HEAD_LOSS, s);
     return hip_status(launch_soft_rows(r, s));
 }
+
+// ---------------------------------------------------------------------------
+// AdamW and the gradient norm: the caller's descriptors in the kernels' form (`out` holds `count`).
+// ---------------------------------------------------------------------------
+constexpr int32_t ADAMW_MAX_TENSORS = 65536;
+
+rdcn_status check_tensors(const rdcn_handle* h, const rdcn_adamw_tensor* t, int32_t count) {
+    if (!h || count < 0 || (count > 0 && !t)) return RDCN_ERR_ARG;
+    if (count > ADAMW_MAX_TENSORS) return RDCN_ERR_UNSUPPORTED;
+    for (int32_t i = 0; i < count; ++i) {
+        if (t[i].n < 0 || (t[i].grad_dtype != RDCN_F32 && t[i].grad_dtype != RDCN_BF16)) return RDCN_ERR_ARG;
+        if (t[i].n > ((int64_t)1 << 36)) return RDCN_ERR_UNSUPPORTED;  // 32-bit chunk numbers, 48 tensors a launch
+        if (t[i].n > 0 && (!t[i].grad || !a16(t[i].grad))) return RDCN_ERR_ARG;
+    }
+    return RDCN_OK;
+}
+
+rdcn_status check_step_tensors(const rdcn_adamw_tensor* t, int32_t count) {
+    for (int32_t i = 0; i < count; ++i) {
+        const rdcn_adamw_tensor& x = t[i];
+        if ((x.param_dtype != RDCN_F32 && x.param_dtype != RDCN_BF16) ||
+            (x.moments != RDCN_MOMENTS_F32 && x.moments != RDCN_MOMENTS_8BIT) || x.reserved != 0 ||
+            !std::isfinite(x.weight_decay) || (x.master && x.param_dtype != RDCN_BF16))
+            return RDCN_ERR_ARG;
+        if (x.n == 0) continue;
+        if (!x.param || !a16(x.param) || !a16(x.master) || !x.m || !a16(x.m) || !x.v || !a16(x.v) ||
+            (x.moments == RDCN_MOMENTS_8BIT && !x.exps))
+            return RDCN_ERR_ARG;
+    }
+    return RDCN_OK;
+}
+
+AdamwTensor adamw_tensor(const rdcn_adamw_tensor& x, double lr) {
+    AdamwTensor t{};
+    t.param = x.param; t.master = x.master; t.grad = x.grad; t.m = x.m; t.v = x.v; t.exps = x.exps;
+    t.n = x.n;
+    t.decay = (float)(1.0 - lr * x.weight_decay);
+    t.weight_decay = (float)x.weight_decay;
+    t.flags = (x.param_dtype == RDCN_BF16 ? ADAMW_PARAM_BF16 : 0) | (x.grad_dtype == RDCN_BF16 ? ADAMW_GRAD_BF16 : 0) |
+              (x.moments == RDCN_MOMENTS_8BIT ? ADAMW_8BIT : 0);
+    return t;
+}
+
+// The same weights twice in one list would be a race; RDCN_OK, or RDCN_ERR_ARG if two ranges overlap.
+rdcn_status check_apart(const rdcn_adamw_tensor* t, int32_t count) {
+    struct Range {
+        uintptr_t from, to;
+    };
+    Range few[64];
+    Range* r = count <= 64 ? few : new (std::nothrow) Range[count];
+    if (!r) return RDCN_ERR_HIP;
+    for (int32_t i = 0; i < count; ++i) {
+        r[i].from = (uintptr_t)t[i].param;
+        r[i].to = r[i].from + (size_t)t[i].n * (t[i].param_dtype == RDCN_BF16 ? 2 : 4);
+    }
+    std::sort(r, r + count, [](const Range& a, const Range& b) { return a.from < b.from; });
+    rdcn_status st = RDCN_OK;
+    uintptr_t end = 0;
+    for (int32_t i = 0; i < count; ++i) {
+        if (r[i].to == r[i].from) continue;
+        if (r[i].from < end) st = RDCN_ERR_ARG;
+        end = r[i].to;
+    }
+    if (r != few) delete[] r;
+    return st;
+}
+
+struct TensorList {  // freed on every return
+    AdamwTensor few[64];
+    AdamwTensor* t;
+    explicit TensorList(int32_t count) : t(count <= 64 ? few : new (std::nothrow) AdamwTensor[count]) {}
+    ~TensorList() {
+        if (t != few) delete[] t;
+    }
+};
 
 }  // namespace
 
@@ -1290,6 +1366,71 @@ rdcn_status rdcn_softmax_loss_grad(rdcn_handle* h, int64_t rows, int64_t dim, in
         RDCN_TRY(launch_soft_unpack_tail((int)S.tail, dim, sc + S.gwt, (char*)grad_w + (size_t)S.main * dim * e, s));
     }
     return RDCN_OK;
+}
+
+rdcn_status rdcn_grad_norm_workspace(const rdcn_handle* h, const rdcn_adamw_tensor* tensors, int32_t count,
+                                     size_t* scratch_bytes) {
+    rdcn_status st = check_tensors(h, tensors, count);
+    if (st != RDCN_OK) return st;
+    if (!scratch_bytes) return RDCN_ERR_ARG;
+    TensorList l(count);
+    if (!l.t) return RDCN_ERR_HIP;
+    for (int32_t i = 0; i < count; ++i) l.t[i] = adamw_tensor(tensors[i], 0.0);
+    *scratch_bytes = al((size_t)grad_norm_partials(l.t, count) * 8);
+    return RDCN_OK;
+}
+
+rdcn_status rdcn_grad_norm(rdcn_handle* h, const rdcn_adamw_tensor* tensors, int32_t count, float grad_scale,
+                           float max_norm, float* out, void* scratch, size_t scratch_bytes, void* stream) {
+    rdcn_status st = check_tensors(h, tensors, count);
+    if (st != RDCN_OK) return st;
+    if (!out || !std::isfinite(grad_scale) || !(max_norm > 0.0f)) return RDCN_ERR_ARG;
+    TensorList l(count);
+    if (!l.t) return RDCN_ERR_HIP;
+    for (int32_t i = 0; i < count; ++i) l.t[i] = adamw_tensor(tensors[i], 0.0);
+    const size_t need = (size_t)grad_norm_partials(l.t, count) * 8;
+    if (need > 0 && (!scratch || !aligned256(scratch) || scratch_bytes < need)) return RDCN_ERR_WORKSPACE;
+    return hip_status(launch_grad_norm(l.t, count, grad_scale, max_norm, (double*)scratch, out, (hipStream_t)stream));
+}
+
+rdcn_status rdcn_adamw_step(rdcn_handle* h, const rdcn_adamw_config* cfg, const rdcn_adamw_tensor* tensors, int32_t count,
+                            void* stream) {
+    if (!h || !cfg) return RDCN_ERR_ARG;
+    const rdcn_adamw_config& c = *cfg;
+    if (!std::isfinite(c.lr) || !(c.beta1 >= 0.0 && c.beta1 < 1.0) || !(c.beta2 >= 0.0 && c.beta2 < 1.0) ||
+        !((float)c.eps > 0.0f) || !std::isfinite(c.eps) || !std::isfinite(c.grad_scale) ||
+        (!c.device_step && c.step < 1) || (c.stochastic != 0 && c.stochastic != 1))
+        return RDCN_ERR_ARG;
+    rdcn_status st = check_tensors(h, tensors, count);
+    if (st != RDCN_OK) return st;
+    if ((st = check_step_tensors(tensors, count)) != RDCN_OK) return st;
+    if ((st = check_apart(tensors, count)) != RDCN_OK) return st;
+    TensorList l(count);
+    if (!l.t) return RDCN_ERR_HIP;
+    for (int32_t i = 0; i < count; ++i) l.t[i] = adamw_tensor(tensors[i], c.lr);
+    AdamwScalars a{};
+    const double t = (double)(c.step < 1 ? 1 : c.step);
+    a.beta1 = (float)c.beta1; a.beta2 = (float)c.beta2;
+    a.c1 = (float)(1.0 - c.beta1); a.c2 = (float)(1.0 - c.beta2);
+    a.eps = (float)c.eps;
+    a.step_size = (float)(c.lr / (1.0 - std::pow(c.beta1, t)));
+    a.rsqrt_grown2 = (float)(1.0 / std::sqrt(1.0 - std::pow(c.beta2, t)));
+    a.lr = c.lr;
+    a.logb1 = std::log(c.beta1); a.logb2 = std::log(c.beta2);
+    a.step = c.step;
+    a.device_lr = c.device_lr; a.device_step = c.device_step; a.clip = c.clip;
+    a.grad_scale = (float)c.grad_scale;
+    a.stochastic = c.stochastic != 0;
+    a.seed = c.seed;
+    return hip_status(launch_adamw(l.t, count, a, (hipStream_t)stream));
+}
+
+rdcn_status rdcn_adamw_values(rdcn_handle* h, int64_t n, const uint8_t* codes, const uint8_t* exps, int32_t is_signed,
+                              void* out, void* stream) {
+    if (!h || n < 0 || (is_signed != 0 && is_signed != 1)) return RDCN_ERR_ARG;
+    if (n == 0) return RDCN_OK;
+    if (!codes || !a16(codes) || !exps || !out || !a16(out)) return RDCN_ERR_ARG;
+    return hip_status(launch_adamw_values(n, codes, exps, is_signed != 0, out, (hipStream_t)stream));
 }
 
 rdcn_status rdcn_profile_start(rdcn_handle* h, int32_t max_launches, uint32_t kernel_mask) {

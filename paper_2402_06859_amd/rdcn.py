@@ -21,6 +21,7 @@ MAX_LAYERS = 16
 F32, BF16 = 0, 1
 I32, I64 = 0, 1
 COMBINE_MUL, COMBINE_SUM = 0, 1
+MOMENTS_F32, MOMENTS_8BIT = 0, 1
 ACT_MODES = {"storage": 0, "hilo": 1, "f16": 2}   # rdcn_act_mode
 
 EXPORTS = ["rdcn_create", "rdcn_destroy", "rdcn_dim", "rdcn_workspace_bytes", "qr_embed_gather",
@@ -29,7 +30,8 @@ EXPORTS = ["rdcn_create", "rdcn_destroy", "rdcn_dim", "rdcn_workspace_bytes", "q
            "qr_quantize_tables", "qr_embed_gather_q8", "rdcn_head_configure", "rdcn_head_workspace_bytes",
            "rdcn_head_forward", "rdcn_head_logloss", "rdcn_head_backward", "rdcn_set_side_stream",
            "qr_embed_backward_static", "rdcn_softmax_loss_workspace", "rdcn_softmax_loss_forward",
-           "rdcn_softmax_loss_grad"]
+           "rdcn_softmax_loss_grad", "rdcn_adamw_step", "rdcn_adamw_values", "rdcn_grad_norm_workspace",
+           "rdcn_grad_norm"]
 EMBED_STATIC_SCRATCH_BYTES = 64 << 20
 
 KERNELS = ["gather", "fwd_down_gemm", "fwd_attention", "fwd_up_gemm", "bwd_pointwise", "bwd_bias", "bwd_gu_gemm",
@@ -64,6 +66,37 @@ class RdcnHeadWeights(ctypes.Structure):
                 ("gate_w", ctypes.c_void_p * MAX_HIDDEN), ("gate_b", ctypes.c_void_p * MAX_HIDDEN),
                 ("w_out", ctypes.c_void_p), ("b_out", ctypes.c_void_p), ("cal_w", ctypes.c_void_p),
                 ("cal_b", ctypes.c_void_p)]
+
+
+class RdcnAdamwTensor(ctypes.Structure):
+    _fields_ = [("param", ctypes.c_void_p), ("master", ctypes.c_void_p), ("grad", ctypes.c_void_p),
+                ("m", ctypes.c_void_p), ("v", ctypes.c_void_p), ("exps", ctypes.c_void_p), ("n", ctypes.c_int64),
+                ("weight_decay", ctypes.c_double), ("param_dtype", ctypes.c_int32), ("grad_dtype", ctypes.c_int32),
+                ("moments", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
+class RdcnAdamwConfig(ctypes.Structure):
+    _fields_ = [("lr", ctypes.c_double), ("beta1", ctypes.c_double), ("beta2", ctypes.c_double),
+                ("eps", ctypes.c_double), ("grad_scale", ctypes.c_double), ("step", ctypes.c_int64),
+                ("device_lr", ctypes.c_void_p), ("device_step", ctypes.c_void_p), ("clip", ctypes.c_void_p),
+                ("stochastic", ctypes.c_int32), ("seed", ctypes.c_uint32)]
+
+
+def adamw_tensors(tensors: Sequence[dict]):
+    """Descriptors of tensors to step, once for many steps. Each is a dict of device tensors
+    param, grad, m, v and, where it has them, master and exps, and its weight_decay. The caller
+    keeps the tensors alive."""
+    out = (RdcnAdamwTensor * len(tensors))()
+    for d, t in zip(out, tensors):
+        for k in ("param", "master", "grad", "m", "v", "exps"):
+            x = t.get(k)
+            setattr(d, k, None if x is None else x.data_ptr())
+        d.n = t["param"].numel()
+        d.weight_decay = t.get("weight_decay", 0.0)
+        d.param_dtype = BF16 if t["param"].dtype == torch.bfloat16 else F32
+        d.grad_dtype = BF16 if t["grad"].dtype == torch.bfloat16 else F32
+        d.moments = MOMENTS_8BIT if t["m"].dtype == torch.uint8 else MOMENTS_F32
+    return out
 
 
 def make_head_config(hidden: Sequence[int], gated: bool, num_buckets: int, bucket_lo: float,
@@ -136,6 +169,10 @@ def load(build_if_missing: bool = True):
     L.rdcn_softmax_loss_workspace.argtypes = [vp, i64, i64, i64, ctypes.POINTER(sz), ctypes.POINTER(sz)]
     L.rdcn_softmax_loss_forward.argtypes = [vp, i64, i64, i64, vp, vp, vp, vp, f32, vp, vp, vp, sz, vp]
     L.rdcn_softmax_loss_grad.argtypes = [vp, i64, i64, i64, vp, vp, vp, vp, f32, vp, f32, vp, vp, vp, vp, vp, sz, vp]
+    L.rdcn_adamw_step.argtypes = [vp, ctypes.POINTER(RdcnAdamwConfig), vp, ctypes.c_int32, vp]
+    L.rdcn_adamw_values.argtypes = [vp, i64, vp, vp, ctypes.c_int32, vp, vp]
+    L.rdcn_grad_norm_workspace.argtypes = [vp, vp, ctypes.c_int32, ctypes.POINTER(sz)]
+    L.rdcn_grad_norm.argtypes = [vp, vp, ctypes.c_int32, f32, f32, vp, vp, sz, vp]
     L.rdcn_profile_start.argtypes = [vp, ctypes.c_int32, ctypes.c_uint32]
     L.rdcn_set_side_stream.argtypes = [vp, ctypes.c_int32]
     L.rdcn_profile_stop.argtypes = [vp, ctypes.POINTER(ctypes.c_double), ctypes.POINTER(ctypes.c_int64)]
@@ -328,6 +365,31 @@ class Rdcn:
             self.h, rows, dim, classes, _ptr(x), _ptr(w), _ptr(offset), _ptr(labels), logit_scale, _ptr(row_weight),
             scale, _ptr(loss), _ptr(lse), _ptr(grad_x), _ptr(grad_w), _ptr(scratch), _bytes(scratch),
             _stream(stream)))
+
+    def grad_norm_workspace(self, tensors) -> int:
+        s = ctypes.c_size_t()
+        _check("rdcn_grad_norm_workspace", load().rdcn_grad_norm_workspace(self.h, tensors, len(tensors),
+                                                                           ctypes.byref(s)))
+        return s.value
+
+    def grad_norm(self, tensors, grad_scale, max_norm, out, scratch, stream=None):
+        """out (float [2]): the norm of all gradients of `tensors` (adamw_tensors) and the factor that clips it."""
+        _check("rdcn_grad_norm", load().rdcn_grad_norm(self.h, tensors, len(tensors), grad_scale, max_norm, _ptr(out),
+                                                       _ptr(scratch), _bytes(scratch), _stream(stream)))
+
+    def adamw_step(self, tensors, lr, beta1=0.9, beta2=0.999, eps=1e-8, step=1, grad_scale=1.0, clip=None,
+                   stochastic=False, seed=0, device_lr=None, device_step=None, stream=None):
+        c = RdcnAdamwConfig(lr, beta1, beta2, eps, grad_scale, step, _ptr(device_lr), _ptr(device_step), _ptr(clip),
+                            int(stochastic), seed & 0xFFFFFFFF)
+        _check("rdcn_adamw_step", load().rdcn_adamw_step(self.h, ctypes.byref(c), tensors, len(tensors),
+                                                         _stream(stream)))
+
+    def adamw_values(self, codes, exps, signed: bool, out=None, stream=None):
+        """The values (bf16) that 8-bit moments stand for."""
+        out = torch.empty(codes.shape, dtype=torch.bfloat16, device=codes.device) if out is None else out
+        _check("rdcn_adamw_values", load().rdcn_adamw_values(self.h, codes.numel(), _ptr(codes), _ptr(exps), int(signed),
+                                                             _ptr(out), _stream(stream)))
+        return out
 
     def profile_start(self, max_launches: int = 8192, kernels=None):
         """Time the launches of `kernels` (names from KERNELS; all when None)."""

@@ -1,0 +1,447 @@
+"""AdamW over many tensors (rdcn_adamw_step), its 8-bit moments and the gradient norm (rdcn_grad_norm).
+
+Two references. In 64 bits: the formulas, with tolerances that count roundings (u = 2^-24 for each float
+operation and each constant): m' is two products of three factors at most and one sum, 6 u of the sum of the
+terms' sizes; v' 8 u of itself (all terms are positive); p' 4 u |p| + 16 u of the update's size and the error
+of m' in it. In float32 with numpy, one rounding per operation in the documented order: the step is
+the same bits, so 8-bit codes (which a rounding in the last place could change) are compared exactly.
+"""
+import ctypes
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from gpu_helpers import need_gpu
+from paper_2402_06859_amd import rdcn
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+HYPER = dict(lr=2e-3, beta1=0.9, beta2=0.999, eps=1e-8)
+SIZES = [1, 7, 8, 255, 256, 257, 0, 2047, 2048, 2049, 5000, 100003]
+
+
+def handle():
+    return rdcn.Rdcn(rdcn.make_config(8, 4, 16, 32, 8, 1, 25, 25, 600))
+
+
+def bf16_bits(x32):
+    """float32 -> the nearest bf16's bits, ties to even (finite values)."""
+    b = x32.view(np.uint32).astype(np.uint64)
+    return ((b + 0x7FFF + ((b >> 16) & 1)) >> 16).astype(np.uint16)
+
+
+def hashed(n, ordinal, seed):
+    with np.errstate(over="ignore"):
+        h = np.arange(n, dtype=np.uint64).astype(np.uint32)
+        h = h ^ np.uint32((seed + 0x9E3779B9 * (ordinal + 1)) & 0xFFFFFFFF)
+        h = (h ^ (h >> np.uint32(16))) * np.uint32(0x85EBCA6B)
+        h = (h ^ (h >> np.uint32(13))) * np.uint32(0xC2B2AE35)
+        return h ^ (h >> np.uint32(16))
+
+
+def bases(exps, top):
+    return np.maximum(exps.astype(np.int64) * 8 + 7 - top, 0)
+
+
+def decode(codes, exps, top):
+    c = codes.astype(np.int64)
+    size = c & top
+    bits = np.where(size == 0, 0, (size + bases(exps, top).repeat(256)[:c.size]) << 20)
+    if top == 127:
+        bits |= (c >> 7) << 31
+    return bits.astype(np.uint32).view(np.float32)
+
+
+def encode(x, top, rnd):
+    bits = x.view(np.uint32).astype(np.int64)
+    size = bits & 0x7FFFFFFF
+    blocks = -(-x.size // 256)
+    exps = np.pad(size, (0, blocks * 256 - x.size)).reshape(blocks, 256).max(1) >> 23
+    code = np.clip(((size + rnd.astype(np.int64)) >> 20) - bases(exps, top).repeat(256)[:x.size], 0, top)
+    if top == 255:
+        code = np.maximum(code, 1)
+    code = np.where(size == 0, 0, code)
+    if top == 127:
+        code |= (bits >> 31) << 7
+    return code.astype(np.uint8), exps.astype(np.uint8)
+
+
+def step32(t, ordinal, hyper, step, clip, stochastic, seed, grad_scale=1.0):
+    """One step of the host copy `t` (numpy), every operation rounded to float32 once."""
+    f = np.float32
+    n = t["n"]
+    if n == 0:
+        return
+    eight = t["exps"] is not None
+    half = -(-n // 256)
+    m = decode(t["m"], t["exps"][:half], 127) if eight else t["m"]
+    v = decode(t["v"], t["exps"][half:], 255) if eight else t["v"]
+    g = t["grad"] * (f(grad_scale) * f(clip))
+    b1, b2 = hyper["beta1"], hyper["beta2"]
+    m = m * f(b1) + g * f(1 - b1)
+    v = v * f(b2) + (g * g) * f(1 - b2)
+    p = t["master"] if t["master"] is not None else t["p32"]
+    down = np.sqrt(v) * f(1 / math.sqrt(1 - b2 ** step)) + f(hyper["eps"])
+    p = p * f(1 - hyper["lr"] * t["wd"]) - (m / down) * f(hyper["lr"] / (1 - b1 ** step))
+    h = hashed(n, ordinal, seed) if stochastic else None
+    if t["master"] is not None:
+        t["master"], t["bits"] = p, bf16_bits(p)
+    elif t["bits"] is not None:
+        if stochastic:
+            with np.errstate(over="ignore"):
+                r = (h * np.uint32(0x85EBCA6B)) >> np.uint32(16)
+            t["bits"] = ((p.view(np.uint32).astype(np.uint64) + r) >> 16).astype(np.uint16)
+        else:
+            t["bits"] = bf16_bits(p)
+        p = (t["bits"].astype(np.uint32) << 16).view(np.float32)
+    t["p32"] = p
+    if eight:
+        nearest = np.full(n, 0x80000)
+        with np.errstate(over="ignore"):
+            rm = h >> np.uint32(12) if stochastic else nearest
+            rv = (h * np.uint32(0x9E3779B1)) >> np.uint32(12) if stochastic else nearest
+        t["m"], em = encode(m, 127, rm)
+        t["v"], ev = encode(v, 255, rv)
+        t["exps"] = np.concatenate((em, ev))
+    else:
+        t["m"], t["v"] = m, v
+
+
+def make(sizes, param, grad, moments, seed, wd=0.01):
+    """Host copies and device tensors (each with 32 elements behind its end that must stay as they are)."""
+    rng = np.random.default_rng(seed)
+    host, dev, keep = [], [], []
+
+    def up(a, dtype=None):
+        fill = np.full(32, 77, dtype=a.dtype)
+        full = torch.from_numpy(np.concatenate((a, fill))).cuda()
+        if dtype is not None:
+            full = full.view(dtype)
+        keep.append((full, a.size))
+        return full[:a.size]
+
+    for i, n in enumerate(sizes):
+        size = np.exp2(rng.standard_normal(n) * 3 - 10).astype(np.float32)
+        g = (rng.standard_normal(n).astype(np.float32) * size)
+        gbits = bf16_bits(g)
+        p = (rng.standard_normal(n) * 0.1).astype(np.float32)
+        t = {"n": n, "wd": wd if i % 2 else 0.0, "exps": None, "master": None, "bits": None, "p32": p}
+        d = {"weight_decay": t["wd"]}
+        if grad == "bf16":
+            t["grad"] = (gbits.astype(np.uint32) << 16).view(np.float32)
+            d["grad"] = up(gbits.view(np.int16), torch.bfloat16)
+        else:
+            t["grad"] = g
+            d["grad"] = up(g)
+        if param != "f32":
+            t["bits"] = bf16_bits(p)
+            d["param"] = up(t["bits"].view(np.int16), torch.bfloat16)
+            if param == "master":
+                t["master"] = p
+                d["master"] = up(p)
+            else:
+                t["p32"] = (t["bits"].astype(np.uint32) << 16).view(np.float32)
+        else:
+            d["param"] = up(p)
+        if moments == "8bit":
+            t["m"], t["v"] = np.zeros(n, np.uint8), np.zeros(n, np.uint8)
+            t["exps"] = np.zeros(2 * -(-n // 256), np.uint8)
+            d["exps"] = up(t["exps"])
+        else:
+            t["m"] = (rng.standard_normal(n).astype(np.float32) * size * np.float32(0.2))
+            t["v"] = (size * size * rng.random(n).astype(np.float32))
+        d["m"], d["v"] = up(t["m"]), up(t["v"])
+        host.append(t)
+        dev.append(d)
+    return host, dev, keep
+
+
+def same_bits(name, got, want):
+    got = got.cpu()
+    if got.dtype == torch.bfloat16:
+        got = got.view(torch.int16)
+    got = got.numpy()
+    got = got.view(np.uint16) if got.dtype == np.int16 else got.view(np.uint32) if got.dtype == np.float32 else got
+    want = want.view(np.uint32) if want.dtype == np.float32 else want
+    bad = got != want
+    assert not bad.any(), "%s: %d of %d differ, first at %d" % (name, bad.sum(), bad.size, int(np.argmax(bad)))
+
+
+def same_state(host, dev, keep):
+    for i, (t, d) in enumerate(zip(host, dev)):
+        name = "tensor %d (%d)" % (i, t["n"])
+        same_bits(name + " param", d["param"], t["bits"] if t["bits"] is not None else t["p32"])
+        if t["master"] is not None:
+            same_bits(name + " master", d["master"], t["master"])
+        for k in ("m", "v") + (("exps",) if t["exps"] is not None else ()):
+            same_bits(name + " " + k, d[k], t[k])
+    for full, n in keep:
+        tail = full[n:].cpu()
+        if tail.dtype == torch.bfloat16:
+            tail = tail.view(torch.int16)
+        assert (tail == 77).all(), "values behind a tensor's end were written"
+
+
+@pytest.mark.parametrize("param", ["f32", "master", "bf16"])
+@pytest.mark.parametrize("grad", ["f32", "bf16"])
+@pytest.mark.parametrize("moments,stochastic", [("f32", False), ("f32", True), ("8bit", True), ("8bit", False)])
+def test_steps_are_the_documented_bits(param, grad, moments, stochastic):
+    need_gpu()
+    print("adamw", param, grad, moments, stochastic, flush=True)
+    lib = handle()
+    host, dev, keep = make(SIZES, param, grad, moments, 3)
+    lst = rdcn.adamw_tensors(dev)
+    clip = torch.tensor([0.625], device="cuda")
+    for step in (1, 2, 3):
+        lib.adamw_step(lst, step=step, grad_scale=0.5, clip=clip, stochastic=stochastic, seed=step * 977, **HYPER)
+        for i, t in enumerate(host):
+            step32(t, i, HYPER, step, 0.625, stochastic, step * 977, 0.5)
+        same_state(host, dev, keep)
+
+
+@pytest.mark.parametrize("param,grad", [("f32", "f32"), ("master", "bf16")])
+def test_float_step_against_64_bits(param, grad):
+    need_gpu()
+    lib = handle()
+    host, dev, _ = make(SIZES, param, grad, "f32", 5)
+    lr, b1, b2, eps, t = 2e-3, 0.9, 0.999, 1e-8, 7
+    lib.adamw_step(rdcn.adamw_tensors(dev), step=t, **HYPER)
+    for h, d in zip(host, dev):
+        m0, v0, g = h["m"].astype(np.float64), h["v"].astype(np.float64), h["grad"].astype(np.float64)
+        p0 = h["p32"].astype(np.float64)
+        m, v = b1 * m0 + (1 - b1) * g, b2 * v0 + (1 - b2) * g * g
+        dm = 6 * U * (np.abs(b1 * m0) + np.abs((1 - b1) * g))
+        down = np.sqrt(v / (1 - b2 ** t)) + eps
+        rate = lr / (1 - b1 ** t)
+        p = p0 * (1 - lr * h["wd"]) - rate * m / down
+        tol = 4 * U * np.abs(p0) + rate * (16 * U * np.abs(m) + dm) / down + U * np.abs(p)
+        got = (d["master"] if param == "master" else d["param"]).cpu().numpy().astype(np.float64)
+        assert (np.abs(d["m"].cpu().numpy() - m) <= dm + 1e-44).all()
+        assert (np.abs(d["v"].cpu().numpy() - v) <= 8 * U * v + 1e-44).all()
+        assert (np.abs(got - p) <= tol).all()
+
+
+def test_more_tensors_than_a_launch_takes():
+    need_gpu()
+    lib = handle()
+    sizes = [(37 * i) % 700 for i in range(131)]
+    host, dev, keep = make(sizes, "bf16", "f32", "8bit", 8)
+    lst = rdcn.adamw_tensors(dev)
+    lib.adamw_step(lst, step=1, stochastic=True, seed=4, **HYPER)
+    for i, t in enumerate(host):
+        step32(t, i, HYPER, 1, 1.0, True, 4)
+    same_state(host, dev, keep)
+    out = torch.zeros(2, device="cuda")
+    sc = torch.empty(max(256, lib.grad_norm_workspace(lst)), dtype=torch.uint8, device="cuda")
+    lib.grad_norm(lst, 1.0, 1e9, out, sc)
+    want = math.sqrt(sum(float((t["grad"].astype(np.float64) ** 2).sum()) for t in host))
+    assert abs(float(out[0]) - want) <= 2 * U * want and float(out[1]) == 1.0
+
+
+def test_every_code_stands_for_its_value():
+    need_gpu()
+    lib = handle()
+    exps = np.array([0, 1, 15, 16, 17, 31, 32, 33, 100, 127, 200, 254], np.uint8)
+    codes = np.tile(np.arange(256, dtype=np.uint8), exps.size)
+    dc, de = torch.from_numpy(codes).cuda(), torch.from_numpy(exps).cuda()
+    for signed, top in ((True, 127), (False, 255)):
+        same_bits("values", lib.adamw_values(dc, de, signed), (decode(codes, exps, top).view(np.uint32) >> 16).astype(np.uint16))
+    part = lib.adamw_values(dc[:1003], de, True)  # not whole vectors
+    same_bits("values", part, (decode(codes[:1003], exps, 127).view(np.uint32) >> 16).astype(np.uint16))
+
+
+def test_codes_are_near_their_values_and_fair():
+    """A stored moment is off by less than one step: 2^-3 of itself, or what lies below the reach of a block. Over
+    many elements the errors cancel: each is at most s = a step wide with mean 0, so their sum stays
+    within 6 standard deviations (at most s / 2 each)."""
+    need_gpu()
+    lib = handle()
+    n = 1 << 20
+    g = torch.exp2(torch.randn(n, device="cuda") * 1.5) * torch.sign(torch.randn(n, device="cuda"))
+    d = {"param": torch.zeros(n, device="cuda"), "grad": g, "m": torch.zeros(n, dtype=torch.uint8, device="cuda"),
+         "v": torch.zeros(n, dtype=torch.uint8, device="cuda"),
+         "exps": torch.zeros(2 * n // 256, dtype=torch.uint8, device="cuda")}
+    lib.adamw_step(rdcn.adamw_tensors([d]), step=1, stochastic=True, seed=9, **HYPER)
+    for k, signed, want in (("m", True, g.double() * 0.1), ("v", False, g.double() ** 2 * 0.001)):
+        e = d["exps"][:n // 256] if signed else d["exps"][n // 256:]
+        got = lib.adamw_values(d[k], e, signed).double()
+        block = want.abs().view(-1, 256).amax(1).repeat_interleave(256)
+        reach = block * 2.0 ** (-15 if signed else -31)
+        width = want.abs() * 2.0 ** -3 * (1 + 2.0 ** -20) + reach
+        err = got - want
+        assert (err.abs() <= width).all()
+        assert float(err.sum().abs()) <= 6 * float((width / 2).square().sum().sqrt()) + float(reach.sum())
+
+
+def test_nonzero_second_moments_stay_nonzero():
+    need_gpu()
+    lib = handle()
+    n = 512
+    g = torch.full((n,), 1e-12, device="cuda")
+    g[0] = g[256] = 1e4
+    d = {"param": torch.zeros(n, device="cuda"), "grad": g, "m": torch.zeros(n, dtype=torch.uint8, device="cuda"),
+         "v": torch.zeros(n, dtype=torch.uint8, device="cuda"), "exps": torch.zeros(4, dtype=torch.uint8, device="cuda")}
+    lst = rdcn.adamw_tensors([d])
+    for t in range(1, 4):
+        lib.adamw_step(lst, step=t, stochastic=True, seed=t, **HYPER)
+    assert (d["v"] >= 1).all() and torch.isfinite(d["param"]).all()
+    z = {k: torch.zeros_like(v) for k, v in d.items()}
+    lib.adamw_step(rdcn.adamw_tensors([z]), step=1, stochastic=True, seed=1, **HYPER)
+    assert all((v == 0).all() for v in z.values())
+
+
+def test_norm_and_clip():
+    need_gpu()
+    lib = handle()
+    out = torch.zeros(2, device="cuda")
+    for grad in ("f32", "bf16"):
+        host, dev, _ = make(SIZES, "f32", grad, "f32", 6)
+        lst = rdcn.adamw_tensors(dev)
+        sc = torch.empty(lib.grad_norm_workspace(lst), dtype=torch.uint8, device="cuda")
+        want = 0.25 * math.sqrt(sum(float((t["grad"].astype(np.float64) ** 2).sum()) for t in host))
+        lib.grad_norm(lst, -0.25, want / 3, out, sc)
+        o = out.cpu().double()
+        assert abs(o[0] - want) <= 2 * U * want and abs(o[1] - 1 / 3) <= 2 * U
+        lib.grad_norm(lst, 0.25, math.inf, out, sc)
+        assert float(out[1]) == 1.0
+        again = out.clone()
+        lib.grad_norm(lst, 0.25, math.inf, out, sc)
+        assert torch.equal(again, out)
+    big = {"param": torch.zeros(5000, device="cuda"), "grad": torch.full((5000,), 1e30, device="cuda"),
+           "m": torch.zeros(5000, device="cuda"), "v": torch.zeros(5000, device="cuda")}
+    lst = rdcn.adamw_tensors([big])
+    sc = torch.empty(lib.grad_norm_workspace(lst), dtype=torch.uint8, device="cuda")
+    lib.grad_norm(lst, 1.0, 1.0, out, sc)  # squares beyond the range of a float
+    want = float(np.float32(1e30)) * math.sqrt(5000)
+    assert abs(float(out[0]) - want) <= 2 * U * want and float(out[1]) > 0
+    for bad in (math.inf, math.nan):
+        big["grad"][4999] = bad
+        lib.grad_norm(lst, 1.0, 1.0, out, sc)
+        assert not math.isfinite(float(out[0])) and math.isnan(float(out[1]))
+        before = {k: v.clone() for k, v in big.items() if k != "grad"}
+        lib.adamw_step(lst, step=1, clip=out[1:], **HYPER)
+        assert all(torch.equal(before[k], big[k]) for k in before)
+    none = rdcn.adamw_tensors([])
+    lib.grad_norm(none, 1.0, 1.0, out, None)
+    assert out.tolist() == [0.0, 1.0]
+    lib.adamw_step(none, step=1, **HYPER)
+
+
+def test_elements_past_32_bits():
+    need_gpu()
+    lib = handle()
+    n = (1 << 31) + 4099
+    print("adamw over", n, "elements", flush=True)
+    d = {"param": torch.zeros(n, dtype=torch.bfloat16, device="cuda"), "grad": torch.zeros(n, dtype=torch.bfloat16, device="cuda"),
+         "m": torch.zeros(n, dtype=torch.uint8, device="cuda"), "v": torch.zeros(n, dtype=torch.uint8, device="cuda"),
+         "exps": torch.zeros(2 * -(-n // 256), dtype=torch.uint8, device="cuda")}
+    d["grad"][-4500:] = 2.0
+    d["grad"][0] = -2.0
+    lst = rdcn.adamw_tensors([d])
+    lib.adamw_step(lst, lr=0.5, beta1=0.9, beta2=0.999, eps=1e-8, step=1)
+    # the first step moves by lr against the sign: m / sqrt(v) corrected is g / |g|
+    assert abs(float(d["param"][0]) - 0.5) <= 0.5 * 2.0 ** -8 and (d["param"][1:9] == 0).all()
+    assert ((d["param"][-4500:].float() + 0.5).abs() <= 0.5 * 2.0 ** -8).all() and (d["param"][-4600:-4500] == 0).all()
+    out = torch.zeros(2, device="cuda")
+    sc = torch.empty(lib.grad_norm_workspace(lst), dtype=torch.uint8, device="cuda")
+    lib.grad_norm(lst, 1.0, 1.0, out, sc)
+    want = 2.0 * math.sqrt(4501)
+    assert abs(float(out[0]) - want) <= 2 * U * want
+
+
+@pytest.mark.parametrize("moments", ["f32", "8bit"])
+def test_captured_steps_follow_the_schedule_on_the_device(moments):
+    """Rate and step number on the device: replays are the steps with those numbers. The growth terms are computed in
+    64 bits on both sides, so the rounded constants differ by at most one unit of a float: 2 u in p's update."""
+    need_gpu()
+    lib = handle()
+    host, dev, keep = make([3000, 77, 1025], "f32", "f32", moments, 12)
+    _, other, _ = make([3000, 77, 1025], "f32", "f32", moments, 12)
+    lst, ref = rdcn.adamw_tensors(dev), rdcn.adamw_tensors(other)
+    lr = torch.tensor([0.0], device="cuda")
+    step = torch.tensor([0], dtype=torch.int64, device="cuda")
+    start = [{k: v.clone() for k, v in d.items() if isinstance(v, torch.Tensor)} for d in dev]
+
+    def one():
+        step.add_(1)
+        lib.adamw_step(lst, lr=9.0, device_lr=lr, device_step=step, stochastic=True, seed=3, beta1=0.9, beta2=0.999, eps=1e-8)
+
+    one()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        one()
+    for d, s in zip(dev, start):
+        for k, v in s.items():
+            d[k].copy_(v)
+    step.zero_()
+    for t in range(1, 5):
+        lr.fill_(1e-3 * t)
+        graph.replay()
+        seed = (3 + t * 0x85EBCA6B) & 0xFFFFFFFF
+        lib.adamw_step(ref, lr=float(np.float32(1e-3 * t)), step=t, stochastic=True, seed=seed, beta1=0.9, beta2=0.999, eps=1e-8)
+        torch.cuda.synchronize()
+        assert int(step) == t
+        for a, b in zip(dev, other):
+            for k in ("m", "v") + (("exps",) if moments == "8bit" else ()):
+                assert torch.equal(a[k], b[k])  # no constant of theirs is computed on the device
+            assert ((a["param"] - b["param"]).abs() <= t * 4 * U * (b["param"].abs() + 4e-3 * 4)).all()
+
+
+def test_other_stream_and_repeat_give_the_same_bits():
+    need_gpu()
+    lib = handle()
+    _, a, _ = make(SIZES, "bf16", "f32", "8bit", 2)
+    _, b, _ = make(SIZES, "bf16", "f32", "8bit", 2)
+    la, lb = rdcn.adamw_tensors(a), rdcn.adamw_tensors(b)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    lib.adamw_step(la, step=1, stochastic=True, seed=6, **HYPER)
+    lib.adamw_step(lb, step=1, stochastic=True, seed=6, stream=side, **HYPER)
+    torch.cuda.synchronize()
+    for x, y in zip(a, b):
+        assert all(torch.equal(x[k].view(torch.uint8), y[k].view(torch.uint8)) for k in ("param", "m", "v", "exps"))
+
+
+def test_refusals():
+    need_gpu()
+    L = rdcn.load()
+    lib = handle()
+    t = {k: torch.zeros(512, device="cuda") for k in ("param", "grad", "m", "v")}
+    out = torch.zeros(2, device="cuda")
+    sc = torch.empty(4096, dtype=torch.uint8, device="cuda")
+    A, S, W, OK = rdcn.RDCN_ERR_ARG, rdcn.RDCN_ERR_UNSUPPORTED, rdcn.RDCN_ERR_WORKSPACE, rdcn.RDCN_OK
+
+    def step(count=1, cfg=None, **kw):
+        lst = rdcn.adamw_tensors([t, dict(t, param=t["param"][256:], grad=t["grad"][256:])][:max(1, count)])
+        for k, v in kw.items():
+            setattr(lst[0], k, v)
+        c = rdcn.RdcnAdamwConfig(1e-3, 0.9, 0.999, 1e-8, 1.0, 1, None, None, None, 0, 0)
+        for k, v in (cfg or {}).items():
+            setattr(c, k, v)
+        return L.rdcn_adamw_step(lib.h, ctypes.byref(c), lst, count, None)
+
+    assert step() == OK
+    assert step(count=2) == A                                     # overlapping weights
+    assert step(count=-1) == A and step(count=65537) == S
+    assert step(param=None) == A and step(grad=None) == A and step(m=None) == A and step(v=None) == A
+    assert step(param=t["param"].data_ptr() + 4) == A and step(m=t["m"].data_ptr() + 8) == A
+    assert step(master=t["m"].data_ptr()) == A                     # a master of float weights
+    assert step(moments=1) == A                                    # 8 bits without exponents
+    assert step(moments=2) == A and step(param_dtype=2) == A and step(grad_dtype=-1) == A and step(reserved=1) == A
+    assert step(n=-1) == A and step(n=(1 << 36) + 1) == S and step(weight_decay=math.nan) == A
+    for bad in (dict(lr=math.inf), dict(beta1=1.0), dict(beta1=-0.1), dict(beta2=math.nan), dict(eps=0.0), dict(eps=1e-60),
+                dict(grad_scale=math.nan), dict(step=0), dict(stochastic=2)):
+        assert step(cfg=bad) == A, bad
+    lst = rdcn.adamw_tensors([t])
+    norm = lambda **k: L.rdcn_grad_norm(lib.h, lst, 1, k.get("s", 1.0), k.get("mx", 1.0), k.get("out", out.data_ptr()),
+                                        k.get("sc", sc.data_ptr()), k.get("n", 4096), None)
+    assert norm() == OK and norm(mx=0.0) == A and norm(mx=math.nan) == A and norm(s=math.inf) == A and norm(out=None) == A
+    assert norm(sc=None) == W and norm(n=0) == W and norm(sc=sc.data_ptr() + 8) == W
+    val = lambda n=256, c=t["m"].data_ptr(), e=t["v"].data_ptr(), sg=1, o=t["grad"].data_ptr(): L.rdcn_adamw_values(
+        lib.h, n, c, e, sg, o, None)
+    assert val() == OK and val(n=-1) == A and val(c=None) == A and val(e=None) == A and val(sg=2) == A and val(o=None) == A
+    torch.cuda.synchronize()
