@@ -355,18 +355,17 @@ CalArgs cal_args(const rdcn_handle* h, const rdcn_head_weights* w, const float* 
 //     their tile's maximum there, which become G in place: three products, 6 N V d operations;
 //   - else G is made for a piece of the classes at a time from the logits computed again (8 N V d):
 //     grad_w of a piece is final, grad_x adds up over the pieces in float.
-// bf16: the matrix loads take 8 classes at a time where classes are the contracted dimension, so the
-// last classes % 8 go through a copy padded with zero rows.
+// G's rows are padded with zeros to whole 16-byte vectors: the matrix loads take 8 classes at a time.
 // ---------------------------------------------------------------------------
 constexpr size_t SOFT_HELD_BYTES = (size_t)512 << 20;
 
 struct SoftPlan {
     bool held;
-    int64_t piece, main, tail;  // classes per piece; classes in whole vectors, and behind them
+    int64_t piece;              // classes per piece
     int64_t ld;                 // row stride of G
     int64_t tiles;              // column tiles of the forward's product
     int tile;
-    size_t part, zlabel, forward_total, factor, kept, G, Gt, acc, wt, gwt, splitk, total;
+    size_t part, zlabel, forward_total, factor, kept, G, acc, splitk, total;
 };
 
 int64_t split_floats(const rdcn_handle* h, int64_t M, int64_t N, int64_t K) {
@@ -379,22 +378,19 @@ SoftPlan soft_plan(const rdcn_handle* h, int64_t rows, int64_t dim, int64_t clas
     SoftPlan s{};
     const size_t e = eb(h);
     const int64_t vec = h->bf16 ? 8 : 4;
-    s.tail = h->bf16 ? classes % vec : 0;  // (float operands are loaded class by class)
-    s.main = classes - s.tail;
     const GemmPlan p = plan_gemm(rows, classes, dim, h->bf16, false);
     s.tiles = rows > 0 ? gemm_soft_tiles(rows, classes, dim, p, h->bf16, &s.tile) : 0;
     const int64_t padded = (classes + vec - 1) / vec * vec;
     s.held = classes <= ((int64_t)1 << 20) && (double)rows * (double)padded * (double)e <= (double)SOFT_HELD_BYTES;
     if (s.held) {
-        s.piece = s.main;
+        s.piece = classes;
         s.ld = padded;
     } else {
         int64_t w = (int64_t)(SOFT_HELD_BYTES / e) / rows / 256 * 256;
         w = std::min<int64_t>(std::max<int64_t>(w, 1024), (int64_t)1 << 20);
-        s.piece = std::min<int64_t>(w, s.main);
+        s.piece = std::min<int64_t>(w, classes);
         s.ld = (s.piece + vec - 1) / vec * vec;
     }
-    const bool many = s.main > s.piece || (s.tail > 0 && s.main > 0);  // grad_x is a sum of several products
     size_t off = 0;
     s.part = off; off += al((size_t)s.tiles * rows * 8);
     s.zlabel = off; off += al((size_t)rows * 4);
@@ -402,12 +398,9 @@ SoftPlan soft_plan(const rdcn_handle* h, int64_t rows, int64_t dim, int64_t clas
     s.factor = off; off += al((size_t)rows * 4);
     s.kept = off; off += al((size_t)rows * dim * e);
     s.G = off; off += al((size_t)rows * s.ld * e);
-    s.Gt = off; off += s.tail && !s.held ? al((size_t)rows * vec * e) : 0;
-    s.acc = off; off += many ? al((size_t)rows * dim * 4) : 0;
-    s.wt = off; off += s.tail ? al((size_t)vec * dim * e) : 0;
-    s.gwt = off; off += s.tail ? al((size_t)vec * dim * e) : 0;
+    s.acc = off; off += classes > s.piece ? al((size_t)rows * dim * 4) : 0;  // grad_x as a sum of several products
     int64_t split = 0;
-    for (int64_t n : {s.piece, s.piece > 0 ? s.main % s.piece : 0, s.tail ? vec : 0}) {
+    for (int64_t n : {s.piece, classes % s.piece}) {
         split = std::max(split, split_floats(h, rows, dim, n));
         split = std::max(split, split_floats(h, n, dim, rows));
     }
@@ -1323,47 +1316,35 @@ rdcn_status rdcn_softmax_loss_grad(rdcn_handle* h, int64_t rows, int64_t dim, in
         ProfScope ps(h, RDCN_KERNEL_HEAD_OUT_BWD, s);
         RDCN_TRY(launch_soft_normalize(n, h->bf16, s));
     }
-    // `n` classes from `first` on, whose rows of w stand at wp and whose gradient rows go to gwp
-    bool begun = false;
-    auto piece = [&](int64_t first, int64_t n, int64_t real, const void* wp, void* gwp, char* g0, int64_t ldg,
-                     bool last) -> hipError_t {
+    for (int64_t v = 0; v < classes; v += S.piece) {
+        const int64_t n = std::min(S.piece, classes - v);
+        const void* const wp = (const char*)w + (size_t)v * dim * e;
         if (!S.held) {
             GemmArgs g{};
-            g.M = rows; g.N = real; g.K = dim;
+            g.M = rows; g.N = n; g.K = dim;
             g.a = x; g.lda = dim;
             g.b = wp; g.ldb = dim;
             g.epi = EPI_SOFT_GRAD; g.scale = logit_scale;
-            g.offset = offset ? offset + first : nullptr;
-            g.labels = labels; g.labels64 = h->ids64; g.label0 = first;
+            g.offset = offset ? offset + v : nullptr;
+            g.labels = labels; g.labels64 = h->ids64; g.label0 = v;
             g.rowv = lse; g.rowg = factor;
-            g.c = g0; g.ldc = ldg;
+            g.c = G; g.ldc = S.ld;
             ProfScope ps(h, RDCN_KERNEL_HEAD_FWD_GEMM, s);
-            const hipError_t e1 = launch_gemm(g, plan_gemm(rows, real, dim, h->bf16, false), h->bf16, s);
-            if (e1 != hipSuccess) return e1;
+            RDCN_TRY(launch_gemm(g, plan_gemm(rows, n, dim, h->bf16, false), h->bf16, s));
         }
         GemmArgs gx{};
         gx.M = rows; gx.N = dim; gx.K = n;
-        gx.a = g0; gx.lda = ldg;
+        gx.a = G; gx.lda = S.ld;
         gx.b = wp; gx.ldb = dim; gx.b_kstrided = true;
-        hipError_t e2 = soft_product(h, RDCN_KERNEL_HEAD_GX_GEMM, gx, begun ? acc : nullptr, acc, grad_x, last, splitk, s);
-        if (e2 != hipSuccess) return e2;
-        begun = true;
+        gx.rem_last = true;
+        RDCN_TRY(soft_product(h, RDCN_KERNEL_HEAD_GX_GEMM, gx, v > 0 ? acc : nullptr, acc, grad_x, v + n == classes, splitk,
+                              s));
         GemmArgs gw{};
         gw.M = n; gw.N = dim; gw.K = rows;
-        gw.a = g0; gw.lda = ldg; gw.a_kstrided = true;
+        gw.a = G; gw.lda = S.ld; gw.a_kstrided = true;
         gw.b = kept; gw.ldb = dim; gw.b_kstrided = true;
-        return soft_product(h, RDCN_KERNEL_HEAD_GW_GEMM, gw, nullptr, nullptr, gwp, true, splitk, s);
-    };
-    for (int64_t v = 0; v < S.main; v += S.piece) {
-        const int64_t n = std::min(S.piece, S.main - v);
-        RDCN_TRY(piece(v, n, n, (const char*)w + (size_t)v * dim * e, (char*)grad_w + (size_t)v * dim * e, G, S.ld,
-                       v + n == S.main && S.tail == 0));
-    }
-    if (S.tail) {
-        RDCN_TRY(launch_soft_pack_tail((int)S.tail, dim, (const char*)w + (size_t)S.main * dim * e, sc + S.wt, s));
-        RDCN_TRY(piece(S.main, 8, S.tail, sc + S.wt, sc + S.gwt, S.held ? G + (size_t)S.main * e : sc + S.Gt,
-                       S.held ? S.ld : 8, true));
-        RDCN_TRY(launch_soft_unpack_tail((int)S.tail, dim, sc + S.gwt, (char*)grad_w + (size_t)S.main * dim * e, s));
+        RDCN_TRY(soft_product(h, RDCN_KERNEL_HEAD_GW_GEMM, gw, nullptr, nullptr, (char*)grad_w + (size_t)v * dim * e, true,
+                              splitk, s));
     }
     return RDCN_OK;
 }

@@ -22,7 +22,7 @@ enum GemmEpi {
                         // else c = v * [act[m, n] > 0] * (rowg ? sigmoid(rowg[m]) : 1), and with
                         // rowpart: rowpart[(n0 / BN) * M + m] = sum over the tile's columns of v * act
     // Softmax loss (both operands K-contiguous), z = scale*acc + offset[n], -inf where offset[n] is:
-    EPI_SOFT_FWD = 8,   // softpart[(n0 / BN) * M + m] = (max, sum of exp(z - max)) over the tile's columns;
+    EPI_SOFT_FWD = 8,   // softpart[t * M + m] = (max, sum of exp(z - max)) over column tile t (gemm_soft_tiles);
                         // zlabel[m] = z at the row's label, if it is one of the tile's columns; with c:
                         // c = exp(z - max) (f16 times SOFT_E_SCALE, or float), zero in the pad of a row
     EPI_SOFT_GRAD = 9   // c = rowg[m] * (exp(z - rowv[m]) - [n is the row's label]) (storage type), zero
@@ -51,6 +51,8 @@ struct GemmArgs {
     const void* b;      // B(n, k) = b[n*ldb + k], or b[k*ldb + n] when b_kstrided
     int64_t ldb;
     bool a_kstrided, b_kstrided;
+    bool rem_last;      // K is no multiple of 8: a K-contiguous A holds zeros behind K up to one (the row strides
+                        // and whatever else is vectorised along K stay multiples of 8)
     bool ops_f16;       // A and B hold f16 values (f16 MFMAs; both K-contiguous, not EPI_MLP_BWD)
     int epi;
     float scale;
@@ -102,7 +104,7 @@ GemmPlan plan_gemm(int64_t M, int64_t N, int64_t K, bool bf16, bool allow_split,
 hipError_t launch_gemm(const GemmArgs& g, const GemmPlan& p, bool bf16, hipStream_t s);
 // Column tiles of an MLP GEMM under plan p (the rowpart partials per row).
 inline int64_t gemm_tiles_n(int64_t N, const GemmPlan& p) { return (N + p.bn - 1) / p.bn; }
-// Column tiles of a softmax loss product (EPI_SOFT_FWD) and the columns of one: launch_gemm's choice of blocks.
+// Column tiles of a softmax loss product (EPI_SOFT_FWD) and the columns of one, as launch_gemm's blocks have them.
 int64_t gemm_soft_tiles(int64_t M, int64_t N, int64_t K, const GemmPlan& p, bool bf16, int* columns);
 hipError_t launch_splitk_reduce(const float* part, int splits, int64_t MN, float* out, hipStream_t s);
 // dst = f16(src) for n bf16 values (n % 8 == 0, 16-byte aligned); sets ERR_BIT_F16_RANGE

@@ -274,7 +274,7 @@ __device__ __forceinline__ float mlp_epilogue8(const GemmArgs& g, int64_t m, int
 }
 
 // Which epilogue a kernel carries.
-enum { EK_PLAIN = 0, EK_MLP = 1, EK_SOFT = 2 };
+enum { EK_PLAIN = 0, EK_MLP = 1, EK_SOFT = 2, EK_SOFT_GRAD = 3 };  // (streamed and float blocks: EK_SOFT has both)
 
 // Base-2 exponential unit for bf16 models (its error, about |x| 2^-24, is far below the rounding
 // of the gradient to bf16); the library function for float ones.
@@ -403,9 +403,10 @@ __device__ __forceinline__ int kstr_swz(int k) {
 __device__ __align__(16) const uint32_t kZero16[4] = {0u, 0u, 0u, 0u};
 
 // Issue this thread's direct-to-LDS loads of one stage (KB deep) for one operand (NW waves).
-// Rows past `rows` re-read the last row (their results are discarded); K positions at
-// or past kend read zeros. K-contiguous operands need kend - k0 to be a multiple of 8
-// (a 16-byte piece never straddles kend: K is a multiple of 8 for bf16 models).
+// Rows past `rows` re-read the last row (K-strided: the 16-byte piece that holds it, so a row count that
+// is no multiple of 8 needs a stride that is one; their results are discarded); K positions at
+// or past kend read zeros. K-contiguous operands need kend - k0 to be a multiple of 8, or zeros behind kend
+// up to one (then a 16-byte piece that straddles kend adds nothing).
 // ROLLED keeps its addresses out of the registers and out of the prologue: for the 32 x 32 loop, whose
 // accumulators and fragments need the registers and which loads one remainder per block with it, and for
 // the streamed blocks, where one wave loads one partial stage with it and the hoisted addresses cost each
@@ -440,7 +441,7 @@ __device__ __forceinline__ void stage_load(const bf16_t* __restrict__ base, int6
             const int c = (q >> 1) ^ kstr_swz<ROWS>(kr);
             gk = k0 + kr;
             gr = row0 + c * 16 + (q & 1) * 8;
-            if (gr >= rows) gr = rows - 8;
+            if (gr >= rows) gr = (rows - 1) & ~(int64_t)7;
             const void* src = gk < kend ? (const void*)(base + gk * ld + gr) : (const void*)kZero16;
             dma16(src, lds_addr(lds) + (uint32_t)__builtin_amdgcn_readfirstlane(blk) * 1024u);
         }
@@ -489,7 +490,7 @@ __device__ __forceinline__ void stage_offsets(int64_t ld, int64_t rows, int64_t 
             const int q = lane % QPR;
             const int c = (q >> 1) ^ kstr_swz<ROWS>(kr);
             int64_t gr = row0 + c * 16 + (q & 1) * 8;
-            if (gr >= rows) gr = rows - 8;
+            if (gr >= rows) gr = (rows - 1) & ~(int64_t)7;
             off[j] = (uint32_t)((kr * ld + (gr - row_base)) * 2);
         }
     }
@@ -589,9 +590,8 @@ struct Pipe {
     __device__ __forceinline__ static void prepare(Ctx& c) {
         const GemmArgs& g = *c.g;
         const int lane = c.tid & 63, wave = c.tid >> 6;
-        // K-strided rows clamp to rows - 8, possibly below the block's first row
-        c.abase = AKS ? (c.m0 + 8 <= g.M ? c.m0 : (g.M >= 8 ? g.M - 8 : 0)) : c.m0;
-        c.bbase = BKS ? (c.n0 + 8 <= g.N ? c.n0 : (g.N >= 8 ? g.N - 8 : 0)) : c.n0;
+        c.abase = c.m0;  // (rows clamp to ones of the block: it begins before their end)
+        c.bbase = c.n0;
         // largest offset: a block's rows (or its BK k-rows) times the stride, plus a row
         const double amax = ((AKS ? KB : BM) + 1.0) * (double)g.lda * 2.0 + BM * 2.0;
         const double bmax = ((BKS ? KB : BN) + 1.0) * (double)g.ldb * 2.0 + BN * 2.0;
@@ -685,7 +685,10 @@ struct Pipe {
         };
         // A K range that is no multiple of KB starts with its remainder (per plane of A), padded
         // with zeros; every later stage is whole, so the loop's loads need no tail.
+        // (rem_last: it is the range's end that comes first, so that every stage begins at a multiple of KB
+        // though the range does not end at a multiple of 8.)
         const int rem = (int)((c.kend - c.kbeg) % KB), planes = c.g->a2 ? 2 : 1;
+        const int64_t krem = c.g->rem_last ? c.kend - rem : c.kbeg, kfull = c.g->rem_last ? c.kbeg : c.kbeg + rem;
         const int nrem = rem ? planes : 0, nf = (int)((c.kend - c.kbeg) / KB), ntot = nrem + nf * planes;
         const uint32_t la0 = lds_addr(smem) + (uint32_t)__builtin_amdgcn_readfirstlane(wave * NIA) * 1024u;
         const uint32_t lb0 = lds_addr(smem + BM * KB) + (uint32_t)__builtin_amdgcn_readfirstlane(wave * NIB) * 1024u;
@@ -694,7 +697,7 @@ struct Pipe {
         };
         auto source = [&](int t) __attribute__((always_inline)) {  // of stage t >= nrem
             const int x = t - nrem, plane = x >= nf;
-            const int64_t k0 = c.kbeg + rem + (int64_t)(x - plane * nf) * KB;
+            const int64_t k0 = kfull + (int64_t)(x - plane * nf) * KB;
             const bf16_t* a = (const bf16_t*)(plane ? c.g->a2 : c.g->a);
             const bf16_t* b = (const bf16_t*)c.g->b;
             return Src{uniform_ptr(AKS ? a + k0 * c.g->lda + c.abase : a + c.abase * c.g->lda + k0),
@@ -709,8 +712,8 @@ struct Pipe {
             bf16_t* const buf = smem + u * STAGE_ELEMS;
             if (u < nrem) {
                 const bf16_t* a = (const bf16_t*)(u ? c.g->a2 : c.g->a);
-                stage_load<BM, AKS, NW, KB, true>(a, c.g->lda, c.g->M, c.m0, c.kbeg, c.kbeg + rem, buf, wave, lane);
-                stage_load<BN, BKS, NW, KB, true>((const bf16_t*)c.g->b, c.g->ldb, c.g->N, c.n0, c.kbeg, c.kbeg + rem,
+                stage_load<BM, AKS, NW, KB, true>(a, c.g->lda, c.g->M, c.m0, krem, krem + rem, buf, wave, lane);
+                stage_load<BN, BKS, NW, KB, true>((const bf16_t*)c.g->b, c.g->ldb, c.g->N, c.n0, krem, krem + rem,
                                                   buf + BM * KB, wave, lane);
             } else {
                 const Src src = source(u);
@@ -840,13 +843,7 @@ __device__ __forceinline__ void block_epilogue(const GemmArgs& g, int64_t m0, in
         for (int q = tid; q < CH * (BN / 8); q += THREADS) {
             const int row = q / (BN / 8), col = (q % (BN / 8)) * 8;
             const int64_t m = m0 + h * CH + row, n = n0 + col;
-            if constexpr (EK == EK_SOFT) {
-                static_assert(CH * (BN / 8) % THREADS == 0, "whole lane groups per row");
-                float v[8];
-                *(f32x4_t*)v = *(const f32x4_t*)(cs + row * CP + col);
-                *(f32x4_t*)(v + 4) = *(const f32x4_t*)(cs + row * CP + col + 4);
-                soft_epilogue<T, 8, BN / 8>(g, m, n, n0 / BN, m < g.M && n < g.N, v);
-            } else if constexpr (EK == EK_PLAIN) {
+            if constexpr (EK == EK_PLAIN) {
                 if (m >= g.M || n >= g.N) continue;
                 float v[8];
                 *(f32x4_t*)v = *(const f32x4_t*)(cs + row * CP + col);
@@ -869,6 +866,123 @@ __device__ __forceinline__ void block_epilogue(const GemmArgs& g, int64_t m0, in
         }
     }
     if (ovf) atomicOr(g.err, ERR_BIT_F16_RANGE);
+}
+
+// Softmax loss epilogue of a BM x BN block, from the accumulators: a lane holds one row of each of its tiles
+// (layout above), so a row's maximum and sum over the BN / WN columns of a wave are the lane's own values and one
+// or two exchanges between lanes. Nothing goes through LDS and no wave waits for another; a (maximum, sum) pair
+// covers a wave's columns. Exponentials cost one fma and one v_exp_f32 each. (Through LDS like the other
+// epilogues, 64 rows at a time, a forward of 4096 x 32000 x 1856 took 514 us, so 419; a library product of these
+// sizes takes 405.)
+template <bool GRAD, int BM, int BN, int WM, int WN, bool M32, typename Acc, int TM, int TN>
+__device__ __forceinline__ void soft_block_epilogue(const GemmArgs& g, int64_t m0, int64_t n0, Acc (&acc)[TM][TN], int tid) {
+    constexpr int MT = M32 ? 32 : 16, Q = M32 ? 4 : 1, HALVES = 64 / MT, COLS = BN / WN;
+    constexpr float LOG2E = 1.4426950408889634f, NEG = -__builtin_huge_valf();
+    const int lane = tid & 63, wave = tid >> 6, half = lane / MT;
+    const int64_t nw = n0 + (wave % WN) * COLS;  // the wave's first column
+    const int64_t mw = m0 + (wave / WN) * (BM / WM) + lane % MT;
+    if (nw >= g.N) return;
+    // the four columns of group (j, q) begin at nw + col(j, q); their values are v[4 (j Q + q)] and on
+    auto col = [&](int j, int q) __attribute__((always_inline)) { return j * MT + 8 * q + 4 * half; };
+    constexpr int V = TN * Q * 4;
+    const bool edge = g.offset || nw + COLS > g.N;
+    float off[V];
+    if (edge) {
+#pragma unroll
+        for (int j = 0; j < TN; ++j)
+#pragma unroll
+            for (int q = 0; q < Q; ++q)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int64_t n = nw + col(j, q) + e;
+                    off[4 * (j * Q + q) + e] = n >= g.N ? NEG : g.offset ? g.offset[n] : 0.f;
+                }
+    }
+    const int64_t pad = (g.N + 7) / 8 * 8 - nw;  // columns that are stored
+#pragma unroll
+    for (int i = 0; i < TM; ++i) {
+        __builtin_amdgcn_sched_barrier(0);  // one row's values live beside the accumulators
+        const int64_t m = mw + i * MT;
+        const bool in = m < g.M;
+        int64_t lab = -1;  // the label's column, from nw
+        if (in) lab = (g.labels64 ? ((const int64_t*)g.labels)[m] : (int64_t)((const int32_t*)g.labels)[m]) - g.label0 - nw;
+        const bool hit = lab >= 0 && lab < COLS && ((int)lab / 4) % HALVES == half;
+        float v[V];
+#pragma unroll
+        for (int j = 0; j < TN; ++j)
+#pragma unroll
+            for (int e = 0; e < 4 * Q; ++e) v[4 * Q * j + e] = acc[i][j][e] * g.scale;
+        if (edge) {
+#pragma unroll
+            for (int e = 0; e < V; ++e) v[e] = off[e] == NEG ? NEG : v[e] + off[e];
+        }
+        if constexpr (GRAD) {
+            const float lse = in ? g.rowv[m] : 0.f, f = in ? g.rowg[m] : 0.f;
+#pragma unroll
+            for (int j = 0; j < TN; ++j)
+#pragma unroll
+                for (int q = 0; q < Q; ++q)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        float& z = v[4 * (j * Q + q) + e];
+                        const float hot = hit && (int)lab == col(j, q) + e ? 1.f : 0.f;
+                        z = f == 0.f || z == NEG ? 0.f : f * (soft_exp<bf16_t>(z - lse) - hot);
+                    }
+        } else {
+            float mx = v[0];
+#pragma unroll
+            for (int e = 1; e < V; ++e) mx = fmaxf(mx, v[e]);
+#pragma unroll
+            for (int o = MT; o < 64; o <<= 1) mx = fmaxf(mx, __shfl_xor(mx, o));
+            if (hit) {
+                float z = 0.f;
+#pragma unroll
+                for (int j = 0; j < TN; ++j)
+#pragma unroll
+                    for (int q = 0; q < Q; ++q)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) z = (int)lab == col(j, q) + e ? v[4 * (j * Q + q) + e] : z;
+                g.zlabel[m] = z;
+            }
+            const float down = mx == NEG ? 0.f : -mx * LOG2E;  // (all masked: exp(-inf) = 0 each)
+            float sum = 0.f;
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                v[e] = __builtin_amdgcn_exp2f(fmaf(v[e], LOG2E, down));
+                sum += v[e];
+            }
+#pragma unroll
+            for (int o = MT; o < 64; o <<= 1) sum += __shfl_xor(sum, o);
+            if (in && half == 0) g.softpart[nw / COLS * g.M + m] = make_float2(mx, sum);
+            if (!g.c) continue;
+        }
+        // 16-bit outputs: bf16 gradients, or f16 exponentials
+        auto pair = [&](float x, float y) __attribute__((always_inline)) {
+            if constexpr (GRAD) return pack_bf16x2(x, y);
+            const half2_t p = {(_Float16)(x * SOFT_E_SCALE), (_Float16)(y * SOFT_E_SCALE)};
+            return __builtin_bit_cast(uint32_t, p);
+        };
+        uint16_t* const out = (uint16_t*)g.c + m * g.ldc + nw;
+#pragma unroll
+        for (int j = 0; j < TN; ++j) {
+            const float* const a = v + 4 * Q * j;
+            if constexpr (M32) {
+                // lanes l and l + 32 hold four columns each of the same eight: they exchange, so that each stores eight
+#pragma unroll
+                for (int q = 0; q < Q; q += 2) {
+                    const auto s0 = __builtin_amdgcn_permlane32_swap(pair(a[4 * q], a[4 * q + 1]),
+                                                                    pair(a[4 * q + 4], a[4 * q + 5]), false, false);
+                    const auto s1 = __builtin_amdgcn_permlane32_swap(pair(a[4 * q + 2], a[4 * q + 3]),
+                                                                    pair(a[4 * q + 6], a[4 * q + 7]), false, false);
+                    const int c = j * 32 + 8 * q + 8 * half;
+                    if (in && c < pad) *(u32x4_t*)(out + c) = u32x4_t{s0[0], s1[0], s0[1], s1[1]};
+                }
+            } else {
+                const int c = col(j, 0);
+                if (in && c < pad) *(uint2*)(out + c) = make_uint2(pair(a[0], a[1]), pair(a[2], a[3]));
+            }
+        }
+    }
 }
 
 // C = A B^T with an ST-stage direct-to-LDS pipeline of KB-deep stages (see layouts above).
@@ -947,7 +1061,9 @@ __attribute__((amdgpu_waves_per_eu(WM * WN == 8 ? 2 : 1, WM * WN == 8 ? 2 : 8)))
     }
     wait_vmcnt(0);  // the trailing re-read loads land before the workgroup ends
 
-    block_epilogue<BM, BN, WM, WN, M32, T, EK, P::THREADS, ST * P::STAGE_ELEMS>(g, c.m0, c.n0, z, acc, smem, tid);
+    if constexpr (EK == EK_SOFT || EK == EK_SOFT_GRAD)
+        soft_block_epilogue<EK == EK_SOFT_GRAD, BM, BN, WM, WN, M32>(g, c.m0, c.n0, acc, tid);
+    else block_epilogue<BM, BN, WM, WN, M32, T, EK, P::THREADS, ST * P::STAGE_ELEMS>(g, c.m0, c.n0, z, acc, smem, tid);
 }
 
 // ---------------------------------------------------------------------------
@@ -1226,7 +1342,7 @@ hipError_t launch_tile(const GemmArgs& g, int splits, hipStream_t s) {
     if (g.epi == EPI_SOFT_FWD || g.epi == EPI_SOFT_GRAD) {
         // softmax loss: logits in one pass over K, both K-contiguous
         if (g.a_kstrided || g.b_kstrided || g.ops_f16 || g.a2 || splits != 1) return hipErrorInvalidValue;
-        RDCN_GEMM(false, false, EK_SOFT);
+        if (g.epi == EPI_SOFT_GRAD) RDCN_GEMM(false, false, EK_SOFT_GRAD); else RDCN_GEMM(false, false, EK_SOFT);
     } else if (g.ops_f16) {
         // f16 operands: the forward products over f16 activations (both K-contiguous;
         // the cross projections and the MLP layers, no split-K for the latter)
@@ -1402,7 +1518,8 @@ int stream_block(int64_t M, int64_t N, int64_t K, const GemmPlan& p) {
 
 int64_t gemm_soft_tiles(int64_t M, int64_t N, int64_t K, const GemmPlan& p, bool bf16, int* columns) {
     const int st = bf16 ? stream_block(M, N, K, p) : 0;
-    *columns = st == 1 ? 16 : st ? 32 : p.bn;
+    // (a streamed or float block's columns, or those of one wave)
+    *columns = st == 1 ? 16 : st ? 32 : !bf16 ? p.bn : p.bm == 64 ? 32 : 64;
     return (N + *columns - 1) / *columns;
 }
 

@@ -42,10 +42,6 @@ hipError_t launch_soft_normalize(const SoftNorm& a, bool bf16, hipStream_t s);
 hipError_t launch_soft_kept_rows(int64_t rows, int64_t dim, int64_t classes, const void* x, const void* labels,
                                  bool labels64, void* out, bool bf16, hipStream_t s);
 
-// dst [8][dim] = the n < 8 rows of src, then rows of zeros; and back.
-hipError_t launch_soft_pack_tail(int n, int64_t dim, const void* src, void* dst, hipStream_t s);
-hipError_t launch_soft_unpack_tail(int n, int64_t dim, const void* src, void* dst, hipStream_t s);
-
 // sum over `splits` planes of part (n floats each, in plane order), added to acc if it is not NULL;
 // written to acc_out (float) or, if that is NULL, to out (storage type). n is a multiple of 4.
 hipError_t launch_soft_reduce(const float* part, int splits, int64_t n, const float* acc, float* acc_out, void* out,

@@ -106,16 +106,6 @@ __global__ __launch_bounds__(256) void k_soft_kept_rows(int64_t rows, int64_t di
     }
 }
 
-__global__ __launch_bounds__(256) void k_soft_pack_tail(int n, int64_t dim, const bf16_t* src, bf16_t* dst) {
-    for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < dim; i += gridDim.x * 256ll)  // 8 values of 8 rows
-        *(u32x4_t*)(dst + i * 8) = i * 8 < n * dim ? *(const u32x4_t*)(src + i * 8) : u32x4_t{0u, 0u, 0u, 0u};
-}
-
-__global__ __launch_bounds__(256) void k_soft_unpack_tail(int n, int64_t dim, const bf16_t* src, bf16_t* dst) {
-    for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < n * dim / 8; i += gridDim.x * 256ll)
-        *(u32x4_t*)(dst + i * 8) = *(const u32x4_t*)(src + i * 8);
-}
-
 template <typename T>
 __global__ __launch_bounds__(256) void k_soft_reduce(const float* part, int splits, int64_t n, const float* acc,
                                                      float* acc_out, T* out) {
@@ -168,17 +158,6 @@ hipError_t launch_soft_kept_rows(int64_t rows, int64_t dim, int64_t classes, con
     else
         hipLaunchKernelGGL(k_soft_kept_rows<float>, grid, dim3(256), 0, s, rows, dim, classes, (const float*)x, labels,
                            labels64, (float*)out);
-    return hipGetLastError();
-}
-
-hipError_t launch_soft_pack_tail(int n, int64_t dim, const void* src, void* dst, hipStream_t s) {
-    hipLaunchKernelGGL(k_soft_pack_tail, blocks_for(dim, 256), dim3(256), 0, s, n, dim, (const bf16_t*)src, (bf16_t*)dst);
-    return hipGetLastError();
-}
-
-hipError_t launch_soft_unpack_tail(int n, int64_t dim, const void* src, void* dst, hipStream_t s) {
-    hipLaunchKernelGGL(k_soft_unpack_tail, blocks_for(n * dim / 8, 256), dim3(256), 0, s, n, dim, (const bf16_t*)src,
-                       (bf16_t*)dst);
     return hipGetLastError();
 }
 
