@@ -500,9 +500,10 @@ rdcn_status rdcn_head_backward(rdcn_handle* h, int64_t batch, const void* x, con
  * forward then does nothing, the gradient sets grad_w to 0).
  */
 
-/* Scratch bytes (256-byte aligned buffers) of the two calls below. */
+/* Scratch bytes (256-byte aligned buffers) of the two calls below: what the forward needs, what the gradient is
+   fastest with, and the least that it takes. */
 rdcn_status rdcn_softmax_loss_workspace(const rdcn_handle* h, int64_t rows, int64_t dim, int64_t classes,
-                                        size_t* forward_bytes, size_t* grad_bytes);
+                                        size_t* forward_bytes, size_t* grad_bytes, size_t* grad_least_bytes);
 
 /* Loss and lse alone (scoring, evaluation). exp(-loss[n]) is the label's probability. */
 rdcn_status rdcn_softmax_loss_forward(rdcn_handle* h, int64_t rows, int64_t dim, int64_t classes, const void* x,
@@ -518,8 +519,11 @@ rdcn_status rdcn_softmax_loss_forward(rdcn_handle* h, int64_t rows, int64_t dim,
  * products (a relative 2^-8 per element at most, label's element taken from z, so that
  * p - 1 keeps its digits) and each gradient once at the end; sums are float and
  * in a fixed order (deterministic).
- * G stands in scratch for all classes while that takes 512 MiB or less; else for a
- * piece of the classes at a time, whose logits are then computed twice.
+ * G stands in scratch. With grad_bytes of it (rdcn_softmax_loss_workspace) the call is fastest: G of all
+ * classes up to 4 GiB (their exponentials are then kept from the forward), in pieces of 1 GiB past that.
+ * It takes any size from grad_least_bytes on: the less, the smaller the pieces of the classes that
+ * are worked on at a time, whose logits are then computed twice. Results of different sizes of scratch
+ * differ in the order of their sums.
  */
 rdcn_status rdcn_softmax_loss_grad(rdcn_handle* h, int64_t rows, int64_t dim, int64_t classes, const void* x,
                                    const void* w, const float* offset, const void* labels, float logit_scale,

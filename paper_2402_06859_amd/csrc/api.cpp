@@ -349,18 +349,22 @@ CalArgs cal_args(const rdcn_handle* h, const rdcn_head_weights* w, const float* 
 
 // ---------------------------------------------------------------------------
 // Softmax loss over many classes. Forward: one product whose epilogue leaves a (maximum, sum) pair
-// per row and column tile, then the join of a row's pairs. Gradient: G [rows, classes] is too large to
-// keep in general, so
-//   - where it fits SOFT_HELD_BYTES, the forward's product also writes the exponentials relative to
-//     their tile's maximum there, which become G in place: three products, 6 N V d operations;
-//   - else G is made for a piece of the classes at a time from the logits computed again (8 N V d):
-//     grad_w of a piece is final, grad_x adds up over the pieces in float.
+// per row and column tile, then the join of a row's pairs. Gradient: G [rows, classes] stands in the
+// caller's scratch, and how much there is decides how it is made:
+//   - whole: the forward's product also writes the exponentials relative to their tile's maximum there,
+//     which become G in place: three products, 6 N V d operations;
+//   - a piece of the classes at a time, from the logits computed again (8 N V d): grad_w of a
+//     piece is final, grad_x adds up over the pieces in float.
+// rdcn_softmax_loss_workspace asks for the first up to SOFT_WHOLE_BYTES of G (a sixtieth of the card's memory;
+// 8192 x 4352 x 131072, 2 GiB of G: 26.3 ms whole, 33.0 in pieces of 512 MiB) and for pieces of
+// SOFT_PIECE_BYTES past it.
 // G's rows are padded with zeros to whole 16-byte vectors: the matrix loads take 8 classes at a time.
 // ---------------------------------------------------------------------------
-constexpr size_t SOFT_HELD_BYTES = (size_t)512 << 20;
+constexpr double SOFT_WHOLE_BYTES = 4294967296.0, SOFT_PIECE_BYTES = 1073741824.0;
+constexpr int64_t SOFT_LEAST_PIECE = 1024, SOFT_MOST_PIECE = (int64_t)1 << 20;
 
 struct SoftPlan {
-    bool held;
+    bool whole;                 // all classes at once, from the exponentials of the forward
     int64_t piece;              // classes per piece
     int64_t ld;                 // row stride of G
     int64_t tiles;              // column tiles of the forward's product
@@ -374,23 +378,16 @@ int64_t split_floats(const rdcn_handle* h, int64_t M, int64_t N, int64_t K) {
     return p.splits > 1 ? (int64_t)p.splits * M * N : 0;
 }
 
-SoftPlan soft_plan(const rdcn_handle* h, int64_t rows, int64_t dim, int64_t classes) {
+// The layout for G in pieces of `piece` classes, or whole.
+SoftPlan soft_layout(const rdcn_handle* h, int64_t rows, int64_t dim, int64_t classes, bool whole, int64_t piece) {
     SoftPlan s{};
     const size_t e = eb(h);
     const int64_t vec = h->bf16 ? 8 : 4;
     const GemmPlan p = plan_gemm(rows, classes, dim, h->bf16, false);
     s.tiles = rows > 0 ? gemm_soft_tiles(rows, classes, dim, p, h->bf16, &s.tile) : 0;
-    const int64_t padded = (classes + vec - 1) / vec * vec;
-    s.held = classes <= ((int64_t)1 << 20) && (double)rows * (double)padded * (double)e <= (double)SOFT_HELD_BYTES;
-    if (s.held) {
-        s.piece = classes;
-        s.ld = padded;
-    } else {
-        int64_t w = (int64_t)(SOFT_HELD_BYTES / e) / rows / 256 * 256;
-        w = std::min<int64_t>(std::max<int64_t>(w, 1024), (int64_t)1 << 20);
-        s.piece = std::min<int64_t>(w, classes);
-        s.ld = (s.piece + vec - 1) / vec * vec;
-    }
+    s.whole = whole;
+    s.piece = whole ? classes : piece;
+    s.ld = (s.piece + vec - 1) / vec * vec;
     size_t off = 0;
     s.part = off; off += al((size_t)s.tiles * rows * 8);
     s.zlabel = off; off += al((size_t)rows * 4);
@@ -407,6 +404,22 @@ SoftPlan soft_plan(const rdcn_handle* h, int64_t rows, int64_t dim, int64_t clas
     s.splitk = off; off += al((size_t)split * 4);
     s.total = off;
     return s;
+}
+
+// The fastest layout within `bytes` (whole, else the largest pieces up to SOFT_PIECE_BYTES of G, halved until
+// they fit), or the one of the smallest pieces, which may not fit.
+SoftPlan soft_plan(const rdcn_handle* h, int64_t rows, int64_t dim, int64_t classes, size_t bytes) {
+    const double column = (double)std::max<int64_t>(rows, 1) * (double)eb(h);
+    if (classes <= SOFT_MOST_PIECE && column * (double)classes <= SOFT_WHOLE_BYTES) {
+        const SoftPlan s = soft_layout(h, rows, dim, classes, true, classes);
+        if (s.total <= bytes) return s;
+    }
+    int64_t piece = (int64_t)(SOFT_PIECE_BYTES / column) / 256 * 256;
+    piece = std::min(std::max(piece, SOFT_LEAST_PIECE), SOFT_MOST_PIECE);
+    for (;; piece = std::max(piece / 512 * 256, SOFT_LEAST_PIECE)) {
+        const SoftPlan s = soft_layout(h, rows, dim, classes, false, std::min(piece, classes));
+        if (s.total <= bytes || piece == SOFT_LEAST_PIECE) return s;
+    }
 }
 
 rdcn_status check_soft(const rdcn_handle* h, int64_t rows, int64_t dim, int64_t classes) {
@@ -1256,13 +1269,14 @@ rdcn_status rdcn_head_backward(rdcn_handle* h, int64_t batch, const void* x, con
 }
 
 rdcn_status rdcn_softmax_loss_workspace(const rdcn_handle* h, int64_t rows, int64_t dim, int64_t classes,
-                                        size_t* forward_bytes, size_t* grad_bytes) {
+                                        size_t* forward_bytes, size_t* grad_bytes, size_t* grad_least_bytes) {
     rdcn_status st = check_soft(h, rows, dim, classes);
     if (st != RDCN_OK) return st;
-    if (!forward_bytes || !grad_bytes) return RDCN_ERR_ARG;
-    const SoftPlan S = soft_plan(h, rows, dim, classes);
+    if (!forward_bytes || !grad_bytes || !grad_least_bytes) return RDCN_ERR_ARG;
+    const SoftPlan S = soft_plan(h, rows, dim, classes, SIZE_MAX);
     *forward_bytes = S.forward_total;
     *grad_bytes = S.total;
+    *grad_least_bytes = std::min(S.total, soft_plan(h, rows, dim, classes, 0).total);
     return RDCN_OK;
 }
 
@@ -1274,7 +1288,7 @@ rdcn_status rdcn_softmax_loss_forward(rdcn_handle* h, int64_t rows, int64_t dim,
     if (!std::isfinite(logit_scale)) return RDCN_ERR_ARG;
     if (rows == 0) return RDCN_OK;
     if (!x || !a16(x) || !w || !a16(w) || !labels || !loss || !lse) return RDCN_ERR_ARG;
-    const SoftPlan S = soft_plan(h, rows, dim, classes);
+    const SoftPlan S = soft_layout(h, rows, dim, classes, true, classes);
     if (!scratch || !aligned256(scratch) || scratch_bytes < S.forward_total) return RDCN_ERR_WORKSPACE;
     return soft_forward(h, S, rows, dim, classes, x, w, offset, labels, logit_scale, nullptr, 0.0f, loss, lse,
                         (char*)scratch, nullptr, 0, nullptr, (hipStream_t)stream);
@@ -1292,7 +1306,7 @@ rdcn_status rdcn_softmax_loss_grad(rdcn_handle* h, int64_t rows, int64_t dim, in
     const size_t e = eb(h);
     if (rows == 0) return hip_status(launch_fill_zero((float*)grad_w, classes * dim * (int64_t)e / 4, s));
     if (!x || !a16(x) || !labels || !loss || !lse || !grad_x || !a16(grad_x)) return RDCN_ERR_ARG;
-    const SoftPlan S = soft_plan(h, rows, dim, classes);
+    const SoftPlan S = soft_plan(h, rows, dim, classes, scratch_bytes);
     if (!scratch || !aligned256(scratch) || scratch_bytes < S.total) return RDCN_ERR_WORKSPACE;
     char* sc = (char*)scratch;
     float* const factor = (float*)(sc + S.factor);
@@ -1302,10 +1316,10 @@ rdcn_status rdcn_softmax_loss_grad(rdcn_handle* h, int64_t rows, int64_t dim, in
     char* const G = sc + S.G;
     // the gradient of the logits carries the logits' own scale
     if ((st = soft_forward(h, S, rows, dim, classes, x, w, offset, labels, logit_scale, row_weight, scale * logit_scale,
-                           loss, lse, sc, S.held ? G : nullptr, S.ld, factor, s)) != RDCN_OK)
+                           loss, lse, sc, S.whole ? G : nullptr, S.ld, factor, s)) != RDCN_OK)
         return st;
     RDCN_TRY(launch_soft_kept_rows(rows, dim, classes, x, labels, h->ids64, sc + S.kept, h->bf16, s));
-    if (S.held) {
+    if (S.whole) {
         SoftNorm n{};
         n.rows = rows; n.classes = classes; n.ld = S.ld; n.tile = S.tile;
         n.softpart = (const float2*)(sc + S.part);
@@ -1319,7 +1333,7 @@ rdcn_status rdcn_softmax_loss_grad(rdcn_handle* h, int64_t rows, int64_t dim, in
     for (int64_t v = 0; v < classes; v += S.piece) {
         const int64_t n = std::min(S.piece, classes - v);
         const void* const wp = (const char*)w + (size_t)v * dim * e;
-        if (!S.held) {
+        if (!S.whole) {
             GemmArgs g{};
             g.M = rows; g.N = n; g.K = dim;
             g.a = x; g.lda = dim;

@@ -166,7 +166,7 @@ def load(build_if_missing: bool = True):
     L.rdcn_head_backward.argtypes = [vp, i64, vp, vp, ctypes.POINTER(RdcnHeadWeights), vp, vp, vp, vp,
                                      ctypes.POINTER(RdcnHeadWeights), vp, vp]
     f32 = ctypes.c_float
-    L.rdcn_softmax_loss_workspace.argtypes = [vp, i64, i64, i64, ctypes.POINTER(sz), ctypes.POINTER(sz)]
+    L.rdcn_softmax_loss_workspace.argtypes = [vp, i64, i64, i64] + [ctypes.POINTER(sz)] * 3
     L.rdcn_softmax_loss_forward.argtypes = [vp, i64, i64, i64, vp, vp, vp, vp, f32, vp, vp, vp, sz, vp]
     L.rdcn_softmax_loss_grad.argtypes = [vp, i64, i64, i64, vp, vp, vp, vp, f32, vp, f32, vp, vp, vp, vp, vp, sz, vp]
     L.rdcn_adamw_step.argtypes = [vp, ctypes.POINTER(RdcnAdamwConfig), vp, ctypes.c_int32, vp]
@@ -347,11 +347,11 @@ class Rdcn:
 
     # ---- training over many classes
     def softmax_loss_workspace(self, rows: int, dim: int, classes: int):
-        """Scratch bytes of (softmax_loss_forward, softmax_loss_grad)."""
-        s, t = ctypes.c_size_t(), ctypes.c_size_t()
+        """Scratch bytes of (softmax_loss_forward, softmax_loss_grad), and the least that the gradient takes."""
+        s, t, u = ctypes.c_size_t(), ctypes.c_size_t(), ctypes.c_size_t()
         _check("rdcn_softmax_loss_workspace", load().rdcn_softmax_loss_workspace(
-            self.h, rows, dim, classes, ctypes.byref(s), ctypes.byref(t)))
-        return s.value, t.value
+            self.h, rows, dim, classes, ctypes.byref(s), ctypes.byref(t), ctypes.byref(u)))
+        return s.value, t.value, u.value
 
     def softmax_loss_forward(self, rows, dim, classes, x, w, offset, labels, logit_scale, loss, lse, scratch,
                              stream=None):

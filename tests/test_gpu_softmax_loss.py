@@ -200,18 +200,56 @@ def test_label_past_the_classes_is_reported_and_left_out(dtype):
         assert got[0][2] == 0 and (got[2][2] == 0).all() and got[0][4] == 0
 
 
-@pytest.mark.parametrize("dtype,rows,classes", [("bf16", 2200, 131077), ("f32", 1100, 131073)])
-def test_pieces_of_the_classes(dtype, rows, classes):
-    """The gradient in the logits does not fit the scratch that is kept for it: several pieces and a tail."""
+def call_grad_within(lib, c, rows, dim, classes, size):
+    """call_grad with a scratch of that size, and 256 bytes behind it that stay as they are."""
+    loss, lse = torch.full((rows,), 7.0, device="cuda"), torch.full((rows,), 7.0, device="cuda")
+    gx, gw = torch.full_like(c["x"], 7.0), torch.full_like(c["w"], 7.0)
+    sc = torch.full((size + 256,), 0xFF, dtype=torch.uint8, device="cuda")
+    lib.softmax_loss_grad(rows, dim, classes, c["x"], c["w"], c["off"], c["y"], c["s"], c["wt"], c["scale"], loss, lse,
+                          gx, gw, sc[:size])
+    assert (sc[size:] == 0xFF).all()
+    return loss, lse, gx, gw
+
+
+@pytest.mark.parametrize("dtype,rows,dim,classes", [("bf16", 300, 264, 5003), ("f32", 130, 68, 3075), ("bf16", 2000, 64, 9000),
+                                                    ("bf16", 1100, 512, 33001)])
+def test_less_scratch_means_pieces_of_the_classes(dtype, rows, dim, classes):
     need_gpu()
-    dim = 64
-    print("softmax loss in pieces", dtype, rows, classes, flush=True)
+    print("softmax loss in pieces", dtype, rows, dim, classes, flush=True)
     lib = handle(dtype)
-    assert lib.softmax_loss_workspace(rows, dim, classes)[1] < 2 ** 30
-    c = make(dtype, rows, dim, classes, 21, ignored=0.2, masked=0.1)
+    c = make(dtype, rows, dim, classes, 21, ignored=0.2, masked=0.1, weights=True)
     c["y"][7], c["y"][8] = classes - 1, classes - 3
     c["off"][classes - 3:] = 0.25
-    check(lib, c, rows, dim, classes, dtype == "f32")
+    _, most, least = lib.softmax_loss_workspace(rows, dim, classes)
+    assert least < most
+    ref, bound = reference(c, rows, dim, classes, dtype == "f32")
+    # pieces add their sums in float: one more rounding of the running sum for each (counted in `chain`)
+    for size in (least, (least + most) // 2 // 256 * 256, most - 256, most, most + 4096):
+        got = call_grad_within(lib, c, rows, dim, classes, size)
+        for k, name in enumerate(("loss", "lse", "grad_x", "grad_w")):
+            live = (c["y"] >= 0) if k == 1 else slice(None)
+            held("%s with %d bytes" % (name, size), got[k][live], ref[k][live], bound[k][live])
+
+
+def test_a_gradient_in_the_logits_too_large_to_ask_for_whole():
+    """Past 4 GiB the workspace asks for pieces by itself: 17000 x 131077 in bf16."""
+    need_gpu()
+    rows, dim, classes = 17000, 8, 131077
+    print("softmax loss", rows, classes, flush=True)
+    lib = handle("bf16")
+    most = lib.softmax_loss_workspace(rows, dim, classes)[1]
+    assert most < 3 << 30
+    c = make("bf16", rows, dim, classes, 22, ignored=0.2)
+    got = call_grad_within(lib, c, rows, dim, classes, most)
+    # a stretch of rows against the definition (the sums over all rows: against another size of scratch)
+    part = dict(c, x=c["x"][16000:16500], y=c["y"][16000:16500])
+    ref, bound = reference(part, 500, dim, classes, False)
+    held("loss", got[0][16000:16500], ref[0], bound[0])
+    held("grad_x", got[2][16000:16500], ref[2], bound[2])
+    other = call_grad_within(lib, c, rows, dim, classes, most // 2)
+    # both are within half a step of bf16 of sums that differ by their order: 2^-7 and the chains' roundings
+    scale = got[3].float().abs() * 2.0 ** -7 + 1e-6 * got[3].float().abs().max()
+    assert ((got[3].float() - other[3].float()).abs() <= scale).all()
 
 
 def test_sharp_rows_keep_the_digits_of_one_minus_p():
@@ -379,6 +417,6 @@ def test_refusals():
     assert fwd(s=math.nan) == A and fwd(xo=2) == A
     assert fwd(scr=None) == W and fwd(scr=P(sc) + 16) == W and fwd(n=need[0] - 1) == W
     assert grad(scale=math.inf) == A and grad(s=math.inf) == A and grad(a=None) == A and grad(b=None) == A
-    assert grad(n=need[1] - 1) == W and grad(scr=None) == W
+    assert grad(n=need[2] - 1) == W and grad(scr=None) == W and grad(scr=P(sc) + 128) == W
     assert fwd() == rdcn.RDCN_OK and grad() == rdcn.RDCN_OK
     torch.cuda.synchronize()

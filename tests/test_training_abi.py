@@ -25,9 +25,9 @@ def test_adamw_struct_layouts_match_c(tmp_path):
 
 def test_null_handles_are_refused():
     L = rdcn.load()
-    s, t = ctypes.c_size_t(), ctypes.c_size_t()
+    s, t, u = ctypes.c_size_t(), ctypes.c_size_t(), ctypes.c_size_t()
     A = rdcn.RDCN_ERR_ARG
-    assert L.rdcn_softmax_loss_workspace(None, 1, 8, 8, ctypes.byref(s), ctypes.byref(t)) == A
+    assert L.rdcn_softmax_loss_workspace(None, 1, 8, 8, ctypes.byref(s), ctypes.byref(t), ctypes.byref(u)) == A
     assert L.rdcn_softmax_loss_forward(None, 1, 8, 8, None, None, None, None, 1.0, None, None, None, 0, None) == A
     assert L.rdcn_softmax_loss_grad(None, 1, 8, 8, None, None, None, None, 1.0, None, 1.0, None, None, None, None, None, 0,
                                     None) == A
