@@ -374,7 +374,7 @@ struct SoftPlan {
 
 int64_t split_floats(const rdcn_handle* h, int64_t M, int64_t N, int64_t K) {
     if (M == 0 || K == 0) return 0;
-    const GemmPlan p = plan_gemm(M, N, K, h->bf16, true);
+    const GemmPlan p = plan_gemm_long(M, N, K, h->bf16);
     return p.splits > 1 ? (int64_t)p.splits * M * N : 0;
 }
 
@@ -435,7 +435,7 @@ rdcn_status check_soft(const rdcn_handle* h, int64_t rows, int64_t dim, int64_t 
 // sum goes to out (storage type) when `last`, else to acc.
 hipError_t soft_product(rdcn_handle* h, int kind, GemmArgs g, const float* acc_in, float* acc, void* out, bool last,
                         float* splitk, hipStream_t s) {
-    const GemmPlan p = plan_gemm(g.M, g.N, g.K, h->bf16, true);
+    const GemmPlan p = plan_gemm_long(g.M, g.N, g.K, h->bf16);
     const int64_t n = g.M * g.N;
     g.scale = 1.0f;
     g.ldc = g.ldx = g.N;

@@ -101,6 +101,8 @@ struct GemmPlan {
 // bytes or more per output (the cross layer's and the residual gradient's).
 GemmPlan plan_gemm(int64_t M, int64_t N, int64_t K, bool bf16, bool allow_split, int split_blocks = 384,
                    bool fused_out = false);
+// plan_gemm (K may be split) for one long product at a time on the whole chip, whose partial sums the caller reduces.
+GemmPlan plan_gemm_long(int64_t M, int64_t N, int64_t K, bool bf16);
 hipError_t launch_gemm(const GemmArgs& g, const GemmPlan& p, bool bf16, hipStream_t s);
 // Column tiles of an MLP GEMM under plan p (the rowpart partials per row).
 inline int64_t gemm_tiles_n(int64_t N, const GemmPlan& p) { return (N + p.bn - 1) / p.bn; }

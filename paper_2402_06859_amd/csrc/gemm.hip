@@ -1488,6 +1488,35 @@ GemmPlan plan_gemm(int64_t M, int64_t N, int64_t K, bool bf16, bool allow_split,
     return p;
 }
 
+GemmPlan plan_gemm_long(int64_t M, int64_t N, int64_t K, bool bf16) {
+    const GemmPlan p = plan_gemm(M, N, K, bf16, true);
+    if (!bf16 || (double)M * (double)N * (double)K < 8.0e9 || M < 8 || N < 8 || (M > N ? M : N) >= 1500000) return p;
+    // 256 x 256 blocks run in rounds of one per CU, and a last round of few blocks costs as much as a full one:
+    // splits of K (of 1024 or more) that fill it, against the partial sums that they write and the reduction reads. us
+    // (a step of 64 with every CU busy takes 1.87 us, memory 4.5 bytes a ps). The gradients of 8192 x
+    // 4352 x 131072 (544 blocks), K whole / 2 / 4 / 7 / 8 / 15 splits: 26.2 / 24.5 / 23.8 / 23.6 / 23.7 / 24.2 ms for the
+    // whole pass; 4096 x 1856 x 32000 (128 blocks), the plan above / 1 / 2 / 3 / 4: 1558 / 1646 / 1448 / 1530 / 1476 us.
+    const int64_t T = ((M + 255) / 256) * ((N + 255) / 256);
+    if ((double)M * (double)N < 0.8 * 65536.0 * (double)T) return p;  // (blocks that are mostly padding)
+    int64_t best = 1;
+    double least = 0.0;
+    for (int64_t s = 1; s <= 16 && (s == 1 || K / s >= 1024); ++s) {
+        double us = std::ceil((double)(T * s) / 256.0) * std::ceil((double)K / (double)s / 64.0) * 1.87;
+        if (s > 1) us += 5.0 + (2.0 * (double)s + 0.5) * (double)M * (double)N * 4.0 / 4.5e6;
+        if (s == 1 || us < least) {
+            best = s;
+            least = us;
+        }
+    }
+    if (T * best < 192) return p;
+    GemmPlan q;
+    q.bm = q.bn = 256;
+    q.stages = 2;
+    q.group_m = 4;
+    q.splits = (int)best;
+    return q;
+}
+
 namespace {
 
 // Which streamed block a product of two K-contiguous operands takes (0: none).
