@@ -383,6 +383,7 @@ int64_t split_floats(const rdcn_handle* h, int64_t M, int64_t N, int64_t K) {
 // 256 x 256: 100003 classes x 1856, 16 rows 83.5 / 105.5, 50 rows 86.2 / 106.2, 128 rows 97.0 / 107.1, 200 rows 145.8 /
 // 110.2; 131072 x 4352, 16 rows 200 / 255 (5.7 TB/s), 128 rows 229 / 266, 200 rows 359 / 280.
 GemmPlan plan_logits(const rdcn_handle* h, int64_t rows, int64_t classes, int64_t dim) {
+    if (!h->bf16) return plan_f32_lds();
     GemmPlan p = plan_gemm(rows, classes, dim, h->bf16, false);
     if (p.bm == 256 && rows <= 128) {
         p.bm = p.bn = 128;

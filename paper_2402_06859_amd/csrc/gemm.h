@@ -101,6 +101,14 @@ struct GemmPlan {
 // bytes or more per output (the cross layer's and the residual gradient's).
 GemmPlan plan_gemm(int64_t M, int64_t N, int64_t K, bool bf16, bool allow_split, int split_blocks = 384,
                    bool fused_out = false);
+// Float products of 16-byte aligned rows (operands' bases and strides): 64 x 64 blocks through LDS.
+constexpr int F32_LDS_STAGES = 103;  // marks such a plan (other float plans leave GemmPlan::stages as it is)
+inline GemmPlan plan_f32_lds() {
+    GemmPlan p;
+    p.bm = p.bn = 64;
+    p.stages = F32_LDS_STAGES;
+    return p;
+}
 // plan_gemm (K may be split) for one long product at a time on the whole chip, whose partial sums the caller reduces.
 GemmPlan plan_gemm_long(int64_t M, int64_t N, int64_t K, bool bf16);
 hipError_t launch_gemm(const GemmArgs& g, const GemmPlan& p, bool bf16, hipStream_t s);

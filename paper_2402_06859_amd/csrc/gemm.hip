@@ -24,6 +24,7 @@
 // transposed in memory. The MFMA is issued with B as its first operand, so each
 // lane ends up with four consecutive output columns of one row: epilogue loads
 // and stores are 8- or 16-byte vectors along the rows of x0, x_l, t and g.
+#include <algorithm>
 #include <cmath>
 #include <type_traits>
 
@@ -1204,6 +1205,137 @@ hipError_t launch_stream(const GemmArgs& g, hipStream_t s) {
     return hipGetLastError();
 }
 
+// Float GEMM for operands whose rows are 16-byte aligned and whose strides are multiples of 4: 64 x 64 blocks of
+// four waves (32 x 32 each), K in stages of 32 through a ring of three in LDS, filled by direct global-to-LDS loads. A
+// K-contiguous stage holds rows of 128 bytes, swizzled like the bf16 ones; a K-strided one stays [k][rows], four
+// k-rows (1 KiB) at a time with 64 bytes between, so that the four k of a fragment's lanes (4 q + e for q = 0 .. 3) lie
+// 16 banks apart. Fragments are those of the kernel below; its loads straight to registers move 64 bytes of 16
+// different rows each (K-contiguous) or 4 bytes a lane (K-strided). us, that kernel / this one: FIGURES
+template <bool AKS, bool BKS, bool SOFT>
+__global__ __launch_bounds__(256) void k_gemm_f32_lds(GemmArgs g) {
+    constexpr int BM = 64, BN = 64, KB = 32, ST = 3, CP = BN + 4, LOADS = 4;
+    constexpr int KC = BM * KB, KS = (KB / 4) * (4 * BM + 16);  // floats of a stage of either kind
+    constexpr int SA = AKS ? KS : KC, STAGE = SA + (BKS ? KS : KC);
+    static_assert(BM * CP <= ST * STAGE, "C staging must fit the ring");
+    __shared__ __attribute__((aligned(1024))) float smem[ST * STAGE];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wm = wave >> 1, wn = wave & 1, i = lane & 15, q = lane >> 4;
+    const int tiles_m = (int)((g.M + BM - 1) / BM), tiles_n = (int)((g.N + BN - 1) / BN);
+    // consecutive blocks of an XCD share a panel of B
+    const int t = xcd_remap(blockIdx.x, tiles_m * tiles_n);
+    const int64_t m0 = (int64_t)(t % tiles_m) * BM, n0 = (int64_t)(t / tiles_m) * BN;
+    const int z = blockIdx.z;
+    const int64_t kchunk = ((g.K + (int64_t)gridDim.z * KB - 1) / ((int64_t)gridDim.z * KB)) * KB;
+    const int64_t kbeg = z * kchunk, kend = kbeg + kchunk < g.K ? kbeg + kchunk : g.K;
+    const int nk = kbeg < kend ? (int)((kend - kbeg + KB - 1) / KB) : 0;
+    // two 1 KiB loads per wave, operand and stage; rows past the end re-read the last ones
+    auto load = [&](auto ks, const float* base, int64_t ld, int64_t rows, int64_t row0, int64_t k0, float* stage)
+                    __attribute__((always_inline)) {
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const int blk = wave * 2 + j;
+            int64_t gk, gr, at;
+            if constexpr (!decltype(ks)::value) {
+                const int r = blk * 8 + lane / 8;
+                gk = k0 + ((lane % 8) ^ ((r >> 1) & 7)) * 4;
+                gr = row0 + r < rows ? row0 + r : rows - 1;
+                at = gr * ld + gk;
+            } else {
+                gk = k0 + blk * 4 + lane / 16;
+                gr = row0 + lane % 16 * 4;
+                if (gr >= rows) gr = (rows - 1) & ~(int64_t)3;
+                at = gk * ld + gr;
+            }
+            const void* src = gk < kend ? (const void*)(base + at) : (const void*)kZero16;
+            dma16(src, (uint32_t)__builtin_amdgcn_readfirstlane(
+                           (int)(uint32_t)(uintptr_t)(LDS_AS const char*)(stage + blk * (decltype(ks)::value ? 4 * BM + 16 : 256))));
+        }
+    };
+    auto issue = [&](int kt) __attribute__((always_inline)) {
+        float* const st = smem + kt % ST * STAGE;
+        const int64_t k0 = kbeg + (int64_t)(kt < nk ? kt : nk - 1) * KB;  // (past the last stage it is read again)
+        load(std::integral_constant<bool, AKS>{}, (const float*)g.a, g.lda, g.M, m0, k0, st);
+        load(std::integral_constant<bool, BKS>{}, (const float*)g.b, g.ldb, g.N, n0, k0, st + SA);
+    };
+    auto frag = [&](auto ks, const float* stage, int rt, int h) __attribute__((always_inline)) {
+        f32x4_t v;
+        if constexpr (!decltype(ks)::value) {
+            const int r = rt + i;
+            v = *(const f32x4_t*)(stage + r * KB + (((4 * h + q) ^ ((r >> 1) & 7)) * 4));
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = stage[(4 * h + q) * (4 * BM + 16) + e * BM + rt + i];
+        }
+        return v;
+    };
+    f32x4_t acc[2][2];
+#pragma unroll
+    for (int a = 0; a < 2; ++a)
+#pragma unroll
+        for (int b = 0; b < 2; ++b) acc[a][b] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    if (nk > 0) {
+        issue(0);
+        issue(1);
+    }
+    for (int kt = 0; kt < nk; ++kt) {
+        wait_vmcnt(LOADS * (ST - 2));
+        __builtin_amdgcn_s_barrier();
+        issue(kt + ST - 1);
+        const float* const sa = smem + kt % ST * STAGE;
+        const float* const sb = sa + SA;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            f32x4_t af[2], bf[2];
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                af[u] = frag(std::integral_constant<bool, AKS>{}, sa, wm * 32 + 16 * u, h);
+                bf[u] = frag(std::integral_constant<bool, BKS>{}, sb, wn * 32 + 16 * u, h);
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+#pragma unroll
+                for (int a = 0; a < 2; ++a)
+#pragma unroll
+                    for (int b = 0; b < 2; ++b)
+                        acc[a][b] = __builtin_amdgcn_mfma_f32_16x16x4f32(bf[b][e], af[a][e], acc[a][b], 0, 0, 0);
+        }
+    }
+    wait_vmcnt(0);  // the loads that were issued past the end have landed
+    __syncthreads();
+    // lane holds C[m = 16 a + i][n = 16 b + 4 q .. + 3]
+#pragma unroll
+    for (int a = 0; a < 2; ++a)
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+            *(f32x4_t*)(smem + (wm * 32 + 16 * a + i) * CP + wn * 32 + 16 * b + 4 * q) = acc[a][b];
+    __syncthreads();
+    for (int c = tid; c < BM * BN / 4; c += 256) {
+        const int row = c / (BN / 4), col = c % (BN / 4) * 4;
+        const int64_t m = m0 + row, n = n0 + col;
+        const f32x4_t s = *(const f32x4_t*)(smem + row * CP + col);
+        float v[4] = {s.x, s.y, s.z, s.w};
+        if constexpr (SOFT) soft_epilogue<float, 4, BN / 4>(g, m, n, n0 / BN, m < g.M && n < g.N, v);
+        else if (m < g.M && n < g.N) epilogue4<float>(g, m, n, z, v);
+    }
+}
+
+hipError_t launch_f32_lds(const GemmArgs& g, int splits, hipStream_t s) {
+    const int64_t tiles = ((g.M + 63) / 64) * ((g.N + 63) / 64);
+    const dim3 grid((unsigned)tiles, 1, (unsigned)splits), block(256);
+    if (((uintptr_t)g.a & 15) || ((uintptr_t)g.b & 15) || g.lda % 4 || g.ldb % 4) return hipErrorInvalidValue;
+    if (g.epi == EPI_SOFT_FWD || g.epi == EPI_SOFT_GRAD) {
+        if (g.a_kstrided || g.b_kstrided || splits != 1) return hipErrorInvalidValue;
+        hipLaunchKernelGGL((k_gemm_f32_lds<false, false, true>), grid, block, 0, s, g);
+    } else if (g.a_kstrided && g.b_kstrided) {
+        hipLaunchKernelGGL((k_gemm_f32_lds<true, true, false>), grid, block, 0, s, g);
+    } else if (!g.a_kstrided && g.b_kstrided) {
+        hipLaunchKernelGGL((k_gemm_f32_lds<false, true, false>), grid, block, 0, s, g);
+    } else {
+        return hipErrorInvalidValue;
+    }
+    return hipGetLastError();
+}
+
 // Float GEMM (float-storage models) on the float matrix instruction v_mfma_f32_16x16x4_f32
 // (float products and sums). Operands go from global memory straight to registers: lane
 // (q, i) holds the four k values 4 q .. 4 q + 3 of row i of a 16-row fragment (one 16-byte
@@ -1238,7 +1370,7 @@ __device__ __forceinline__ f32x4_t frag_f32(const float* __restrict__ x, int64_t
     return v;
 }
 
-template <int SM, int SN, int KW, bool AKS, bool BKS, bool SOFT>
+template <int SM, int SN, int KW, bool AKS, bool BKS>
 __global__ __launch_bounds__(64 * SM * SN * KW) void k_gemm_f32(GemmArgs g) {
     constexpr int THREADS = 64 * SM * SN * KW, BM = 32 * SM, BN = 32 * SN, CP = BN + 4;
     __shared__ __attribute__((aligned(16))) float cs[KW][BM * CP];
@@ -1293,13 +1425,12 @@ __global__ __launch_bounds__(64 * SM * SN * KW) void k_gemm_f32(GemmArgs g) {
     for (int c = threadIdx.x; c < BM * BN / 4; c += THREADS) {
         const int row = c / (BN / 4), col = c % (BN / 4) * 4;
         const int64_t m = m0 + row, n = n0 + col;
-        if (!SOFT && (m >= g.M || n >= g.N)) continue;
+        if (m >= g.M || n >= g.N) continue;
         f32x4_t s = *(const f32x4_t*)(&cs[0][row * CP + col]);
 #pragma unroll
         for (int w = 1; w < KW; ++w) s += *(const f32x4_t*)(&cs[w][row * CP + col]);
         float v[4] = {s.x, s.y, s.z, s.w};
-        if constexpr (SOFT) soft_epilogue<float, 4, BN / 4>(g, m, n, n0 / BN, m < g.M && n < g.N, v);
-        else epilogue4<float>(g, m, n, z, v);
+        epilogue4<float>(g, m, n, z, v);
     }
 }
 
@@ -1307,15 +1438,12 @@ template <int SM, int SN, int KW>
 hipError_t launch_f32(const GemmArgs& g, int splits, hipStream_t s) {
     const int64_t tiles = ((g.M + 32 * SM - 1) / (32 * SM)) * ((g.N + 32 * SN - 1) / (32 * SN));
     const dim3 grid((unsigned)tiles, 1, (unsigned)splits), block(64 * SM * SN * KW);
-    if (g.epi == EPI_SOFT_FWD || g.epi == EPI_SOFT_GRAD) {
-        if (g.a_kstrided || g.b_kstrided || splits != 1) return hipErrorInvalidValue;
-        hipLaunchKernelGGL((k_gemm_f32<SM, SN, KW, false, false, true>), grid, block, 0, s, g);
-    } else if (g.a_kstrided) {
-        if (g.b_kstrided) hipLaunchKernelGGL((k_gemm_f32<SM, SN, KW, true, true, false>), grid, block, 0, s, g);
-        else hipLaunchKernelGGL((k_gemm_f32<SM, SN, KW, true, false, false>), grid, block, 0, s, g);
+    if (g.a_kstrided) {
+        if (g.b_kstrided) hipLaunchKernelGGL((k_gemm_f32<SM, SN, KW, true, true>), grid, block, 0, s, g);
+        else hipLaunchKernelGGL((k_gemm_f32<SM, SN, KW, true, false>), grid, block, 0, s, g);
     } else {
-        if (g.b_kstrided) hipLaunchKernelGGL((k_gemm_f32<SM, SN, KW, false, true, false>), grid, block, 0, s, g);
-        else hipLaunchKernelGGL((k_gemm_f32<SM, SN, KW, false, false, false>), grid, block, 0, s, g);
+        if (g.b_kstrided) hipLaunchKernelGGL((k_gemm_f32<SM, SN, KW, false, true>), grid, block, 0, s, g);
+        else hipLaunchKernelGGL((k_gemm_f32<SM, SN, KW, false, false>), grid, block, 0, s, g);
     }
     return hipGetLastError();
 }
@@ -1489,8 +1617,15 @@ GemmPlan plan_gemm(int64_t M, int64_t N, int64_t K, bool bf16, bool allow_split,
 }
 
 GemmPlan plan_gemm_long(int64_t M, int64_t N, int64_t K, bool bf16) {
+    if (!bf16) {
+        GemmPlan p = plan_f32_lds();
+        const int64_t t = ((M + 63) / 64) * ((N + 63) / 64);
+        const int64_t sp = std::min<int64_t>({t < 512 ? 512 / t : 1, K / 256, 16});
+        p.splits = (int)(sp < 1 ? 1 : sp);
+        return p;
+    }
     const GemmPlan p = plan_gemm(M, N, K, bf16, true);
-    if (!bf16 || (double)M * (double)N * (double)K < 8.0e9 || M < 8 || N < 8 || (M > N ? M : N) >= 1500000) return p;
+    if ((double)M * (double)N * (double)K < 8.0e9 || M < 8 || N < 8 || (M > N ? M : N) >= 1500000) return p;
     // 256 x 256 blocks run in rounds of one per CU, and a last round of few blocks costs as much as a full one:
     // splits of K (of 1024 or more) that fill it, against the partial sums that they write and the reduction reads. us
     // (a step of 64 with every CU busy takes 1.87 us, memory 4.5 bytes a ps). The gradients of 8192 x
@@ -1556,6 +1691,7 @@ hipError_t launch_gemm(const GemmArgs& g, const GemmPlan& p, bool bf16, hipStrea
     if (g.M == 0 || g.N == 0) return hipSuccess;
     if (!bf16 && (g.epi == EPI_MLP_FWD || g.epi == EPI_MLP_BWD)) return hipErrorInvalidValue;
     if (!bf16) {
+        if (p.stages == F32_LDS_STAGES) return launch_f32_lds(g, p.splits, s);
         return p.bm == 64 ? launch_f32<2, 2, 2>(g, p.splits, s) : launch_f32<1, 1, 8>(g, p.splits, s);
     }
     GemmArgs ga = g;
