@@ -476,11 +476,12 @@ hipError_t soft_product(rdcn_handle* h, int kind, GemmArgs g, const float* acc_i
     return launch_soft_reduce(splitk, p.splits, n, acc_in, last ? nullptr : acc, out, h->bf16, s);
 }
 
-// The logits product and the join of its pairs; e != NULL also keeps the exponentials (row stride ld).
+// The logits product and the join of its pairs; e != NULL also keeps the exponentials (row stride ld), factor != NULL
+// also the rows' gradient factors and the rows of x that have a label.
 rdcn_status soft_forward(rdcn_handle* h, const SoftPlan& S, int64_t rows, int64_t dim, int64_t classes, const void* x,
                          const void* w, const float* offset, const void* labels, float logit_scale,
                          const float* row_weight, float scale, float* loss, float* lse, char* sc, void* e, int64_t ld,
-                         float* factor, hipStream_t s) {
+                         float* factor, void* kept, hipStream_t s) {
     GemmArgs g{};
     g.M = rows; g.N = classes; g.K = dim;
     g.a = x; g.lda = dim;
@@ -502,8 +503,9 @@ rdcn_status soft_forward(rdcn_handle* h, const SoftPlan& S, int64_t rows, int64_
     r.row_weight = row_weight; r.scale = scale;
     r.loss = loss; r.lse = lse; r.factor = factor;
     r.err = h->err;
+    r.x = x; r.kept = kept; r.dim = dim;
     ProfScope ps(h, RDCN_KERNEL_HEAD_LOSS, s);
-    return hip_status(launch_soft_rows(r, s));
+    return hip_status(launch_soft_rows(r, h->bf16, s));
 }
 
 // ---------------------------------------------------------------------------
@@ -1306,7 +1308,7 @@ rdcn_status rdcn_softmax_loss_forward(rdcn_handle* h, int64_t rows, int64_t dim,
     const SoftPlan S = soft_layout(h, rows, dim, classes, true, classes);
     if (!scratch || !aligned256(scratch) || scratch_bytes < S.forward_total) return RDCN_ERR_WORKSPACE;
     return soft_forward(h, S, rows, dim, classes, x, w, offset, labels, logit_scale, nullptr, 0.0f, loss, lse,
-                        (char*)scratch, nullptr, 0, nullptr, (hipStream_t)stream);
+                        (char*)scratch, nullptr, 0, nullptr, nullptr, (hipStream_t)stream);
 }
 
 rdcn_status rdcn_softmax_loss_grad(rdcn_handle* h, int64_t rows, int64_t dim, int64_t classes, const void* x,
@@ -1331,9 +1333,8 @@ rdcn_status rdcn_softmax_loss_grad(rdcn_handle* h, int64_t rows, int64_t dim, in
     char* const G = sc + S.G;
     // the gradient of the logits carries the logits' own scale
     if ((st = soft_forward(h, S, rows, dim, classes, x, w, offset, labels, logit_scale, row_weight, scale * logit_scale,
-                           loss, lse, sc, S.whole ? G : nullptr, S.ld, factor, s)) != RDCN_OK)
+                           loss, lse, sc, S.whole ? G : nullptr, S.ld, factor, sc + S.kept, s)) != RDCN_OK)
         return st;
-    RDCN_TRY(launch_soft_kept_rows(rows, dim, classes, x, labels, h->ids64, sc + S.kept, h->bf16, s));
     if (S.whole) {
         SoftNorm n{};
         n.rows = rows; n.classes = classes; n.ld = S.ld; n.tile = S.tile;

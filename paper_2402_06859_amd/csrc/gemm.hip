@@ -275,70 +275,69 @@ __device__ __forceinline__ float mlp_epilogue8(const GemmArgs& g, int64_t m, int
 }
 
 // Which epilogue a kernel carries.
-enum { EK_PLAIN = 0, EK_MLP = 1, EK_SOFT = 2, EK_SOFT_GRAD = 3 };  // (streamed and float blocks: EK_SOFT has both)
+enum { EK_PLAIN = 0, EK_MLP = 1, EK_SOFT = 2, EK_SOFT_GRAD = 3 };  // (streamed blocks: EK_SOFT has both)
 
-// Base-2 exponential unit for bf16 models (its error, about |x| 2^-24, is far below the rounding
-// of the gradient to bf16); the library function for float ones.
+// exp(x) for the softmax loss, from the base-2 exponential unit. bf16 models: the rounding of x log2(e), about
+// |x| 2^-24 of the result, is far below that of the gradient to bf16. Float ones: the product as a sum of two floats (fma
+// gives the first one's rounding error), whose small part multiplies the result as 1 + lo ln 2.
 template <typename T>
 __device__ __forceinline__ float soft_exp(float x) {
-    return sizeof(T) == 2 ? __expf(x) : expf(x);
+    constexpr float L = 1.44269504f, L_LO = 1.92596299e-8f, LN2 = 0.693147181f;
+    if constexpr (sizeof(T) == 2) return __builtin_amdgcn_exp2f(x * L);
+    const float hi = x * L, lo = fmaf(x, L_LO, fmaf(x, L, -hi)), e = __builtin_amdgcn_exp2f(hi);
+    return e == 0.f ? 0.f : fmaf(e, lo * LN2, e);  // (x = -inf: lo is not a number)
 }
 
-// Softmax loss epilogues on W consecutive columns n .. n+W-1 of row m. The LANES threads of a
+// Softmax loss epilogues on 8 consecutive columns n .. n+7 of row m (streamed blocks). The LANES threads of a
 // row are an aligned group of lanes and all call this; `in` is false for rows past M and
-// column groups past N. One pass over the logits where they stand: the tile's running maximum and
+// column groups past N. One pass over the logits where they stand: the tile's maximum and
 // sum go out as two floats per row, so z itself never reaches memory.
-template <typename T, int W, int LANES>
-__device__ __forceinline__ void soft_epilogue(const GemmArgs& g, int64_t m, int64_t n, int64_t tile, bool in, float* v) {
+template <int LANES>
+__device__ __forceinline__ void soft_epilogue8(const GemmArgs& g, int64_t m, int64_t n, int64_t tile, bool in, float* v) {
     const float NEG = -__builtin_huge_valf();
-    int64_t lab = -1;  // the label's column in this group, if 0 .. W-1
+    int64_t lab = -1;  // the label's column in this group, if 0 .. 7
     if (in) {
         lab = (g.labels64 ? ((const int64_t*)g.labels)[m] : (int64_t)((const int32_t*)g.labels)[m]) - g.label0 - n;
 #pragma unroll
-        for (int e = 0; e < W; ++e) {
+        for (int e = 0; e < 8; ++e) {
             const float o = g.offset && n + e < g.N ? g.offset[n + e] : 0.f;
             v[e] = n + e >= g.N || o == NEG ? NEG : v[e] * g.scale + o;
         }
     } else {
 #pragma unroll
-        for (int e = 0; e < W; ++e) v[e] = NEG;
+        for (int e = 0; e < 8; ++e) v[e] = NEG;
     }
     if (g.epi == EPI_SOFT_GRAD) {
         if (!in) return;
         const float lse = g.rowv[m], f = g.rowg[m];
 #pragma unroll
-        for (int e = 0; e < W; ++e)
-            v[e] = f == 0.f || v[e] == NEG ? 0.f : f * (soft_exp<T>(v[e] - lse) - (lab == e ? 1.f : 0.f));
-        T* const out = (T*)g.c + m * g.ldc + n;
-        if constexpr (W == 8) store8<T>(out, v);
-        else store4<T>(out, v);
+        for (int e = 0; e < 8; ++e)
+            v[e] = f == 0.f || v[e] == NEG ? 0.f : f * (soft_exp<bf16_t>(v[e] - lse) - (lab == e ? 1.f : 0.f));
+        store8<bf16_t>((bf16_t*)g.c + m * g.ldc + n, v);
         return;
     }
     float mx = v[0];
 #pragma unroll
-    for (int e = 1; e < W; ++e) mx = fmaxf(mx, v[e]);
+    for (int e = 1; e < 8; ++e) mx = fmaxf(mx, v[e]);
 #pragma unroll
     for (int o = 1; o < LANES; o <<= 1) mx = fmaxf(mx, __shfl_xor(mx, o));
+    const float top = mx == NEG ? 0.f : mx;  // (all masked: exp(-inf) = 0 each)
     float sum = 0.f;
 #pragma unroll
-    for (int e = 0; e < W; ++e) {
+    for (int e = 0; e < 8; ++e) {
         if (lab == e) g.zlabel[m] = v[e];
-        v[e] = v[e] == NEG ? 0.f : soft_exp<T>(v[e] - mx);  // (a NaN stays one)
+        v[e] = soft_exp<bf16_t>(v[e] - top);
         sum += v[e];
     }
 #pragma unroll
     for (int o = 1; o < LANES; o <<= 1) sum += __shfl_xor(sum, o);
     if (!in) return;
-    if (n == tile * (W * LANES)) g.softpart[tile * g.M + m] = make_float2(mx, sum);
+    if (n == tile * (8 * LANES)) g.softpart[tile * g.M + m] = make_float2(mx, sum);
     if (!g.c) return;
-    if constexpr (W == 8) {
-        bool ovf = false;
+    bool ovf = false;
 #pragma unroll
-        for (int e = 0; e < W; ++e) v[e] *= SOFT_E_SCALE;
-        *(u32x4_t*)((_Float16*)g.c + m * g.ldc + n) = pack_f16x8(v, ovf);
-    } else {
-        store4<float>((float*)g.c + m * g.ldc + n, v);
-    }
+    for (int e = 0; e < 8; ++e) v[e] *= SOFT_E_SCALE;
+    *(u32x4_t*)((_Float16*)g.c + m * g.ldc + n) = pack_f16x8(v, ovf);
 }
 
 __device__ __forceinline__ int xcd_remap(int id, int n) {
@@ -875,10 +874,10 @@ __device__ __forceinline__ void block_epilogue(const GemmArgs& g, int64_t m0, in
 // covers a wave's columns. Exponentials cost one fma and one v_exp_f32 each. (Through LDS like the other
 // epilogues, 64 rows at a time, a forward of 4096 x 32000 x 1856 took 514 us, so 419; a library product of these
 // sizes takes 405.)
-template <bool GRAD, int BM, int BN, int WM, int WN, bool M32, typename Acc, int TM, int TN>
+template <typename T, bool GRAD, int BM, int BN, int WM, int WN, bool M32, typename Acc, int TM, int TN>
 __device__ __forceinline__ void soft_block_epilogue(const GemmArgs& g, int64_t m0, int64_t n0, Acc (&acc)[TM][TN], int tid) {
     constexpr int MT = M32 ? 32 : 16, Q = M32 ? 4 : 1, HALVES = 64 / MT, COLS = BN / WN;
-    constexpr float LOG2E = 1.4426950408889634f, NEG = -__builtin_huge_valf();
+    constexpr float NEG = -__builtin_huge_valf();
     const int lane = tid & 63, wave = tid >> 6, half = lane / MT;
     const int64_t nw = n0 + (wave % WN) * COLS;  // the wave's first column
     const int64_t mw = m0 + (wave / WN) * (BM / WM) + lane % MT;
@@ -899,7 +898,8 @@ __device__ __forceinline__ void soft_block_epilogue(const GemmArgs& g, int64_t m
                     off[4 * (j * Q + q) + e] = n >= g.N ? NEG : g.offset ? g.offset[n] : 0.f;
                 }
     }
-    const int64_t pad = (g.N + 7) / 8 * 8 - nw;  // columns that are stored
+    constexpr int VEC = st<T>::vec;
+    const int64_t pad = (g.N + VEC - 1) / VEC * VEC - nw;  // columns that are stored
 #pragma unroll
     for (int i = 0; i < TM; ++i) {
         __builtin_amdgcn_sched_barrier(0);  // one row's values live beside the accumulators
@@ -927,7 +927,7 @@ __device__ __forceinline__ void soft_block_epilogue(const GemmArgs& g, int64_t m
                     for (int e = 0; e < 4; ++e) {
                         float& z = v[4 * (j * Q + q) + e];
                         const float hot = hit && (int)lab == col(j, q) + e ? 1.f : 0.f;
-                        z = f == 0.f || z == NEG ? 0.f : f * (soft_exp<bf16_t>(z - lse) - hot);
+                        z = f == 0.f || z == NEG ? 0.f : f * (soft_exp<T>(z - lse) - hot);
                     }
         } else {
             float mx = v[0];
@@ -945,17 +945,25 @@ __device__ __forceinline__ void soft_block_epilogue(const GemmArgs& g, int64_t m
                         for (int e = 0; e < 4; ++e) z = (int)lab == col(j, q) + e ? v[4 * (j * Q + q) + e] : z;
                 g.zlabel[m] = z;
             }
-            const float down = mx == NEG ? 0.f : -mx * LOG2E;  // (all masked: exp(-inf) = 0 each)
+            const float top = mx == NEG ? 0.f : mx;  // (all masked: exp(-inf) = 0 each)
             float sum = 0.f;
 #pragma unroll
             for (int e = 0; e < V; ++e) {
-                v[e] = __builtin_amdgcn_exp2f(fmaf(v[e], LOG2E, down));
+                v[e] = soft_exp<T>(v[e] - top);
                 sum += v[e];
             }
 #pragma unroll
             for (int o = MT; o < 64; o <<= 1) sum += __shfl_xor(sum, o);
             if (in && half == 0) g.softpart[nw / COLS * g.M + m] = make_float2(mx, sum);
             if (!g.c) continue;
+        }
+        if constexpr (sizeof(T) == 4) {
+            float* const out = (float*)g.c + m * g.ldc + nw;
+#pragma unroll
+            for (int j = 0; j < TN; ++j)
+                if (in && col(j, 0) < pad)
+                    *(f32x4_t*)(out + col(j, 0)) = f32x4_t{v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]};
+            continue;
         }
         // 16-bit outputs: bf16 gradients, or f16 exponentials
         auto pair = [&](float x, float y) __attribute__((always_inline)) {
@@ -1063,7 +1071,7 @@ __attribute__((amdgpu_waves_per_eu(WM * WN == 8 ? 2 : 1, WM * WN == 8 ? 2 : 8)))
     wait_vmcnt(0);  // the trailing re-read loads land before the workgroup ends
 
     if constexpr (EK == EK_SOFT || EK == EK_SOFT_GRAD)
-        soft_block_epilogue<EK == EK_SOFT_GRAD, BM, BN, WM, WN, M32>(g, c.m0, c.n0, acc, tid);
+        soft_block_epilogue<bf16_t, EK == EK_SOFT_GRAD, BM, BN, WM, WN, M32>(g, c.m0, c.n0, acc, tid);
     else block_epilogue<BM, BN, WM, WN, M32, T, EK, P::THREADS, ST * P::STAGE_ELEMS>(g, c.m0, c.n0, z, acc, smem, tid);
 }
 
@@ -1179,7 +1187,7 @@ __global__ __launch_bounds__(64 * ST_KW) void k_gemm_stream(GemmArgs g) {
                 s1 += *(const f32x4_t*)(p + w * ROWS * CP + 4);
             }
             float v[8] = {s0.x, s0.y, s0.z, s0.w, s1.x, s1.y, s1.z, s1.w};
-            if constexpr (EK == EK_SOFT) soft_epilogue<T, 8, BN / 8>(g, m, n, n0 / BN, m < g.M && n < g.N, v);
+            if constexpr (EK == EK_SOFT) soft_epilogue8<BN / 8>(g, m, n, n0 / BN, m < g.M && n < g.N, v);
             else if constexpr (EK == EK_MLP) (void)mlp_epilogue8<T>(g, m, n, v, ovf);
             else epilogue8<T>(g, m, n, 0, v, ovf);
         }
@@ -1206,14 +1214,17 @@ hipError_t launch_stream(const GemmArgs& g, hipStream_t s) {
 }
 
 // Float GEMM for operands whose rows are 16-byte aligned and whose strides are multiples of 4: 64 x 64 blocks of
-// four waves (32 x 32 each), K in stages of 32 through a ring of three in LDS, filled by direct global-to-LDS loads. A
+// four waves (32 x 32 each), K in stages of 32 through a ring of two in LDS (33 KiB, four blocks a CU; with
+// three stages and three blocks 1-4% slower), filled by direct global-to-LDS loads. A
 // K-contiguous stage holds rows of 128 bytes, swizzled like the bf16 ones; a K-strided one stays [k][rows], four
 // k-rows (1 KiB) at a time with 64 bytes between, so that the four k of a fragment's lanes (4 q + e for q = 0 .. 3) lie
 // 16 banks apart. Fragments are those of the kernel below; its loads straight to registers move 64 bytes of 16
-// different rows each (K-contiguous) or 4 bytes a lane (K-strided). us, that kernel / this one: FIGURES
-template <bool AKS, bool BKS, bool SOFT>
+// different rows each (K-contiguous) or 4 bytes a lane (K-strided). A gradient pass of 2000 x 512 x 16000 runs at 109
+// TFLOP/s (a library product of 4096^3 at 135), its products' steps alone at 130; 512 x 160 x 5000, 24 to 632 blocks
+// of 5 to 16 stages, takes 74 us against 85 with that kernel.
+template <bool AKS, bool BKS, int EK>
 __global__ __launch_bounds__(256) void k_gemm_f32_lds(GemmArgs g) {
-    constexpr int BM = 64, BN = 64, KB = 32, ST = 3, CP = BN + 4, LOADS = 4;
+    constexpr int BM = 64, BN = 64, KB = 32, ST = 2, CP = BN + 4, LOADS = 4;
     constexpr int KC = BM * KB, KS = (KB / 4) * (4 * BM + 16);  // floats of a stage of either kind
     constexpr int SA = AKS ? KS : KC, STAGE = SA + (BKS ? KS : KC);
     static_assert(BM * CP <= ST * STAGE, "C staging must fit the ring");
@@ -1251,11 +1262,47 @@ __global__ __launch_bounds__(256) void k_gemm_f32_lds(GemmArgs g) {
                            (int)(uint32_t)(uintptr_t)(LDS_AS const char*)(stage + blk * (decltype(ks)::value ? 4 * BM + 16 : 256))));
         }
     };
+    // whole stages: a scalar base per stage and 32-bit offsets per lane, formed once
+    const bool fast = ((AKS ? KB : BM) + 1.0) * (double)g.lda * 4.0 < 2.0e9 && ((BKS ? KB : BN) + 1.0) * (double)g.ldb * 4.0 < 2.0e9;
+    uint32_t aoff[2], boff[2];
+    auto offsets = [&](auto ks, int64_t ld, int64_t rows, int64_t row0, uint32_t (&off)[2]) __attribute__((always_inline)) {
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const int blk = wave * 2 + j;
+            if constexpr (!decltype(ks)::value) {
+                const int r = blk * 8 + lane / 8;
+                const int64_t gr = row0 + r < rows ? r : rows - 1 - row0;
+                off[j] = (uint32_t)((gr * ld + ((lane % 8) ^ ((r >> 1) & 7)) * 4) * 4);
+            } else {
+                int64_t gr = row0 + lane % 16 * 4;
+                if (gr >= rows) gr = (rows - 1) & ~(int64_t)3;
+                off[j] = (uint32_t)(((blk * 4 + lane / 16) * ld + gr - row0) * 4);
+            }
+        }
+    };
+    if (fast) {
+        offsets(std::integral_constant<bool, AKS>{}, g.lda, g.M, m0, aoff);
+        offsets(std::integral_constant<bool, BKS>{}, g.ldb, g.N, n0, boff);
+    }
     auto issue = [&](int kt) __attribute__((always_inline)) {
         float* const st = smem + kt % ST * STAGE;
         const int64_t k0 = kbeg + (int64_t)(kt < nk ? kt : nk - 1) * KB;  // (past the last stage it is read again)
-        load(std::integral_constant<bool, AKS>{}, (const float*)g.a, g.lda, g.M, m0, k0, st);
-        load(std::integral_constant<bool, BKS>{}, (const float*)g.b, g.ldb, g.N, n0, k0, st + SA);
+        const float* const a = (const float*)g.a;
+        const float* const b = (const float*)g.b;
+        if (fast && k0 + KB <= kend) {
+            const void* const pa = uniform_ptr(AKS ? a + k0 * g.lda + m0 : a + m0 * g.lda + k0);
+            const void* const pb = uniform_ptr(BKS ? b + k0 * g.ldb + n0 : b + n0 * g.ldb + k0);
+            const uint32_t l0 = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(uintptr_t)(LDS_AS const char*)st);
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const uint32_t blk = (uint32_t)(wave * 2 + j);
+                dma16_s(aoff[j], pa, l0 + blk * (AKS ? 1088u : 1024u));
+                dma16_s(boff[j], pb, l0 + SA * 4u + blk * (BKS ? 1088u : 1024u));
+            }
+            return;
+        }
+        load(std::integral_constant<bool, AKS>{}, a, g.lda, g.M, m0, k0, st);
+        load(std::integral_constant<bool, BKS>{}, b, g.ldb, g.N, n0, k0, st + SA);
     };
     auto frag = [&](auto ks, const float* stage, int rt, int h) __attribute__((always_inline)) {
         f32x4_t v;
@@ -1275,32 +1322,36 @@ __global__ __launch_bounds__(256) void k_gemm_f32_lds(GemmArgs g) {
         for (int b = 0; b < 2; ++b) acc[a][b] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     if (nk > 0) {
         issue(0);
-        issue(1);
     }
     for (int kt = 0; kt < nk; ++kt) {
         wait_vmcnt(LOADS * (ST - 2));
         __builtin_amdgcn_s_barrier();
-        issue(kt + ST - 1);
         const float* const sa = smem + kt % ST * STAGE;
         const float* const sb = sa + SA;
+        f32x4_t af[2][2], bf[2][2];
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            f32x4_t af[2], bf[2];
+        for (int h = 0; h < 2; ++h)
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
-                af[u] = frag(std::integral_constant<bool, AKS>{}, sa, wm * 32 + 16 * u, h);
-                bf[u] = frag(std::integral_constant<bool, BKS>{}, sb, wn * 32 + 16 * u, h);
+                af[h][u] = frag(std::integral_constant<bool, AKS>{}, sa, wm * 32 + 16 * u, h);
+                bf[h][u] = frag(std::integral_constant<bool, BKS>{}, sb, wn * 32 + 16 * u, h);
             }
+        issue(kt + ST - 1);
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
 #pragma unroll
             for (int e = 0; e < 4; ++e)
 #pragma unroll
                 for (int a = 0; a < 2; ++a)
 #pragma unroll
                     for (int b = 0; b < 2; ++b)
-                        acc[a][b] = __builtin_amdgcn_mfma_f32_16x16x4f32(bf[b][e], af[a][e], acc[a][b], 0, 0, 0);
-        }
+                        acc[a][b] = __builtin_amdgcn_mfma_f32_16x16x4f32(bf[h][b][e], af[h][a][e], acc[a][b], 0, 0, 0);
     }
     wait_vmcnt(0);  // the loads that were issued past the end have landed
+    if constexpr (EK == EK_SOFT || EK == EK_SOFT_GRAD) {
+        soft_block_epilogue<float, EK == EK_SOFT_GRAD, BM, BN, 2, 2, false>(g, m0, n0, acc, tid);
+        return;
+    }
     __syncthreads();
     // lane holds C[m = 16 a + i][n = 16 b + 4 q .. + 3]
 #pragma unroll
@@ -1314,8 +1365,7 @@ __global__ __launch_bounds__(256) void k_gemm_f32_lds(GemmArgs g) {
         const int64_t m = m0 + row, n = n0 + col;
         const f32x4_t s = *(const f32x4_t*)(smem + row * CP + col);
         float v[4] = {s.x, s.y, s.z, s.w};
-        if constexpr (SOFT) soft_epilogue<float, 4, BN / 4>(g, m, n, n0 / BN, m < g.M && n < g.N, v);
-        else if (m < g.M && n < g.N) epilogue4<float>(g, m, n, z, v);
+        if (m < g.M && n < g.N) epilogue4<float>(g, m, n, z, v);
     }
 }
 
@@ -1325,11 +1375,12 @@ hipError_t launch_f32_lds(const GemmArgs& g, int splits, hipStream_t s) {
     if (((uintptr_t)g.a & 15) || ((uintptr_t)g.b & 15) || g.lda % 4 || g.ldb % 4) return hipErrorInvalidValue;
     if (g.epi == EPI_SOFT_FWD || g.epi == EPI_SOFT_GRAD) {
         if (g.a_kstrided || g.b_kstrided || splits != 1) return hipErrorInvalidValue;
-        hipLaunchKernelGGL((k_gemm_f32_lds<false, false, true>), grid, block, 0, s, g);
+        if (g.epi == EPI_SOFT_GRAD) hipLaunchKernelGGL((k_gemm_f32_lds<false, false, EK_SOFT_GRAD>), grid, block, 0, s, g);
+        else hipLaunchKernelGGL((k_gemm_f32_lds<false, false, EK_SOFT>), grid, block, 0, s, g);
     } else if (g.a_kstrided && g.b_kstrided) {
-        hipLaunchKernelGGL((k_gemm_f32_lds<true, true, false>), grid, block, 0, s, g);
+        hipLaunchKernelGGL((k_gemm_f32_lds<true, true, EK_PLAIN>), grid, block, 0, s, g);
     } else if (!g.a_kstrided && g.b_kstrided) {
-        hipLaunchKernelGGL((k_gemm_f32_lds<false, true, false>), grid, block, 0, s, g);
+        hipLaunchKernelGGL((k_gemm_f32_lds<false, true, EK_PLAIN>), grid, block, 0, s, g);
     } else {
         return hipErrorInvalidValue;
     }
@@ -1624,7 +1675,14 @@ GemmPlan plan_gemm_long(int64_t M, int64_t N, int64_t K, bool bf16) {
         p.splits = (int)(sp < 1 ? 1 : sp);
         return p;
     }
-    const GemmPlan p = plan_gemm(M, N, K, bf16, true);
+    GemmPlan p = plan_gemm(M, N, K, bf16, true);
+    const int64_t t64 = ((M + 63) / 64) * ((N + 63) / 64);
+    if (p.bm == 64 && t64 < 128 && K >= 768) {
+        // few blocks of a long K each: split it down to 128, past plan_gemm's 512 (gradient pass of 333 x 136 x 1001, 18
+        // blocks: FIG2)
+        const int64_t sp = std::min<int64_t>({256 / t64, K / 128, 16});
+        if (sp > p.splits) p.splits = (int)sp;
+    }
     if ((double)M * (double)N * (double)K < 8.0e9 || M < 8 || N < 8 || (M > N ? M : N) >= 1500000) return p;
     // 256 x 256 blocks run in rounds of one per CU, and a last round of few blocks costs as much as a full one:
     // splits of K (of 1024 or more) that fill it, against the partial sums that they write and the reduction reads. us
@@ -1682,8 +1740,8 @@ int stream_block(int64_t M, int64_t N, int64_t K, const GemmPlan& p) {
 
 int64_t gemm_soft_tiles(int64_t M, int64_t N, int64_t K, const GemmPlan& p, bool bf16, int* columns) {
     const int st = bf16 ? stream_block(M, N, K, p) : 0;
-    // (a streamed or float block's columns, or those of one wave)
-    *columns = st == 1 ? 16 : st ? 32 : !bf16 ? p.bn : p.bm == 64 ? 32 : 64;
+    // (a streamed block's columns, or those of one wave)
+    *columns = st == 1 ? 16 : st || p.bm == 64 ? 32 : 64;
     return (N + *columns - 1) / *columns;
 }
 

@@ -20,8 +20,12 @@ struct SoftRows {
     float* lse;
     float* factor;  // may be NULL (no gradient)
     int* err;
+    // with factor: kept [rows, dim] = x, with zeros in the rows that have no label
+    const void* x;
+    void* kept;
+    int64_t dim;
 };
-hipError_t launch_soft_rows(const SoftRows& a, hipStream_t s);
+hipError_t launch_soft_rows(const SoftRows& a, bool bf16, hipStream_t s);
 
 // e [rows][ld] (f16 times SOFT_E_SCALE, or float with T float): exponentials relative to their tile's
 // maximum -> the loss's gradient in the logits, in place (storage type).
@@ -37,10 +41,6 @@ struct SoftNorm {
     void* e;
 };
 hipError_t launch_soft_normalize(const SoftNorm& a, bool bf16, hipStream_t s);
-
-// out = x, with zeros in the rows that have no label in [0, classes).
-hipError_t launch_soft_kept_rows(int64_t rows, int64_t dim, int64_t classes, const void* x, const void* labels,
-                                 bool labels64, void* out, bool bf16, hipStream_t s);
 
 // sum over `splits` planes of part (n floats each, in plane order), added to acc if it is not NULL;
 // written to acc_out (float) or, if that is NULL, to out (storage type). n is a multiple of 4.

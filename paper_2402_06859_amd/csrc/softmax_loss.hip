@@ -28,11 +28,32 @@ __device__ __forceinline__ void join(float& mx, float& sum, float m2, float s2) 
     mx = c;
 }
 
+// A row without a label may hold anything (padding behind a sequence, infinities, NaN): its
+// gradient factor is 0, but 0 times such a value would still reach grad_w's sum over the rows. So the product
+// for grad_w reads a copy of x with zeros there, made by the workgroups from `first` on.
+template <typename T>
+__device__ __forceinline__ void copy_kept_rows(const SoftRows& a, int64_t first) {
+    constexpr int W = st<T>::vec;
+    const int64_t per = a.dim / W, n = a.rows * per, step = (gridDim.x - first) * 256ll;
+    for (int64_t i = (blockIdx.x - first) * 256ll + threadIdx.x; i < n; i += step) {
+        const int64_t y = label_of(a.labels, a.labels64, i / per);
+        u32x4_t v = {0u, 0u, 0u, 0u};
+        if (y >= 0 && y < a.classes) v = *(const u32x4_t*)((const T*)a.x + i * W);
+        *(u32x4_t*)((T*)a.kept + i * W) = v;
+    }
+}
+
 // 256 threads as rpb rows x (256 / rpb) lanes that stride over the tiles. Few rows take many
 // lanes each (one request over 50000 classes has 782 pairs to join), many rows one lane or few.
+template <typename T>
 __global__ __launch_bounds__(256) void k_soft_rows(SoftRows a, int rpb) {
     __shared__ float2 sh[256];
-    const int r = threadIdx.x % rpb, part = threadIdx.x / rpb, parts = 256 / rpb;
+    const int64_t nrow = (a.rows + rpb - 1) / rpb;
+    if (blockIdx.x >= nrow) {
+        copy_kept_rows<T>(a, nrow);
+        return;
+    }
+    const int r = threadIdx.x % rpb, part = threadIdx.x / rpb, parts = 256 / rpb;  // (rpb a power of two)
     const int64_t m = (int64_t)blockIdx.x * rpb + r;
     float mx = NEG_INF, sum = 0.f;
     if (m < a.rows)
@@ -91,21 +112,6 @@ __global__ __launch_bounds__(256) void k_soft_normalize(SoftNorm a) {
     }
 }
 
-// A row without a label may hold anything (padding behind a sequence, infinities, NaN): its
-// gradient factor is 0, but 0 times such a value would still reach grad_w's sum over the rows.
-template <typename T>
-__global__ __launch_bounds__(256) void k_soft_kept_rows(int64_t rows, int64_t dim, int64_t classes, const T* x,
-                                                        const void* labels, bool labels64, T* out) {
-    constexpr int W = st<T>::vec;
-    const int64_t per = dim / W, n = rows * per;
-    for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < n; i += gridDim.x * 256ll) {
-        const int64_t y = label_of(labels, labels64, i / per);
-        u32x4_t v = {0u, 0u, 0u, 0u};
-        if (y >= 0 && y < classes) v = *(const u32x4_t*)(x + i * W);
-        *(u32x4_t*)(out + i * W) = v;
-    }
-}
-
 template <typename T>
 __global__ __launch_bounds__(256) void k_soft_reduce(const float* part, int splits, int64_t n, const float* acc,
                                                      float* acc_out, T* out) {
@@ -130,11 +136,14 @@ dim3 blocks_for(int64_t items, int64_t most) {
 
 }  // namespace
 
-hipError_t launch_soft_rows(const SoftRows& a, hipStream_t s) {
+hipError_t launch_soft_rows(const SoftRows& a, bool bf16, hipStream_t s) {
     if (a.rows == 0) return hipSuccess;
     int rpb = 1;  // about 256 workgroups or more, as long as there are that many rows
     while (rpb < 64 && a.rows / (2 * rpb) >= 256) rpb *= 2;
-    hipLaunchKernelGGL(k_soft_rows, dim3((unsigned)((a.rows + rpb - 1) / rpb)), dim3(256), 0, s, a, rpb);
+    const unsigned nrow = (unsigned)((a.rows + rpb - 1) / rpb);
+    const unsigned ncopy = a.factor ? blocks_for(a.rows * a.dim / (bf16 ? 8 : 4), 4096).x : 0;
+    if (bf16) hipLaunchKernelGGL(k_soft_rows<bf16_t>, dim3(nrow + ncopy), dim3(256), 0, s, a, rpb);
+    else hipLaunchKernelGGL(k_soft_rows<float>, dim3(nrow + ncopy), dim3(256), 0, s, a, rpb);
     return hipGetLastError();
 }
 
@@ -145,19 +154,6 @@ hipError_t launch_soft_normalize(const SoftNorm& a, bool bf16, hipStream_t s) {
     const dim3 grid(blocks_for((per + 3) / 4, 64).x, (unsigned)y, (unsigned)z);
     if (bf16) hipLaunchKernelGGL(k_soft_normalize<bf16_t>, grid, dim3(256), 0, s, a);
     else hipLaunchKernelGGL(k_soft_normalize<float>, grid, dim3(256), 0, s, a);
-    return hipGetLastError();
-}
-
-hipError_t launch_soft_kept_rows(int64_t rows, int64_t dim, int64_t classes, const void* x, const void* labels,
-                                 bool labels64, void* out, bool bf16, hipStream_t s) {
-    if (rows == 0) return hipSuccess;
-    const dim3 grid = blocks_for(rows * dim / (bf16 ? 8 : 4), 4096);
-    if (bf16)
-        hipLaunchKernelGGL(k_soft_kept_rows<bf16_t>, grid, dim3(256), 0, s, rows, dim, classes, (const bf16_t*)x, labels,
-                           labels64, (bf16_t*)out);
-    else
-        hipLaunchKernelGGL(k_soft_kept_rows<float>, grid, dim3(256), 0, s, rows, dim, classes, (const float*)x, labels,
-                           labels64, (float*)out);
     return hipGetLastError();
 }
 
