@@ -870,15 +870,16 @@ __device__ __forceinline__ void block_epilogue(const GemmArgs& g, int64_t m0, in
 
 // Softmax loss epilogue of a BM x BN block, from the accumulators: a lane holds one row of each of its tiles
 // (layout above), so a row's maximum and sum over the BN / WN columns of a wave are the lane's own values and one
-// or two exchanges between lanes. Nothing goes through LDS and no wave waits for another; a (maximum, sum) pair
-// covers a wave's columns. Exponentials cost one fma and one v_exp_f32 each. (Through LDS like the other
+// or two exchanges between lanes, and no wave waits for another; a (maximum, sum) pair covers a wave's columns. Exponentials cost one fma and one v_exp_f32 each. (Through LDS like the other
 // epilogues, 64 rows at a time, a forward of 4096 x 32000 x 1856 took 514 us, so 419; a library product of these
 // sizes takes 405.)
 template <typename T, bool GRAD, int BM, int BN, int WM, int WN, bool M32, typename Acc, int TM, int TN>
-__device__ __forceinline__ void soft_block_epilogue(const GemmArgs& g, int64_t m0, int64_t n0, Acc (&acc)[TM][TN], int tid) {
+__device__ __forceinline__ void soft_block_epilogue(const GemmArgs& g, int64_t m0, int64_t n0, Acc (&acc)[TM][TN], int tid,
+                                                    uint32_t* stage) {
     constexpr int MT = M32 ? 32 : 16, Q = M32 ? 4 : 1, HALVES = 64 / MT, COLS = BN / WN;
     constexpr float NEG = -__builtin_huge_valf();
     const int lane = tid & 63, wave = tid >> 6, half = lane / MT;
+    constexpr int PITCH = 36;  // words of a staged row: 16 rows' 16-byte pieces lie in 16 groups of banks
     const int64_t nw = n0 + (wave % WN) * COLS;  // the wave's first column
     const int64_t mw = m0 + (wave / WN) * (BM / WM) + lane % MT;
     if (nw >= g.N) return;
@@ -971,22 +972,40 @@ __device__ __forceinline__ void soft_block_epilogue(const GemmArgs& g, int64_t m
             const half2_t p = {(_Float16)(x * SOFT_E_SCALE), (_Float16)(y * SOFT_E_SCALE)};
             return __builtin_bit_cast(uint32_t, p);
         };
-        uint16_t* const out = (uint16_t*)g.c + m * g.ldc + nw;
+        if constexpr (M32) {
+            // The tiles' rows through LDS (a stretch of the wave's own), so that a store covers whole rows of 128 bytes:
+            // straight from the lanes it would be 32 bytes of each of 32 rows. Past the caches, which hold the operands'
+            // panels. (8192 x 131072 x 4352: 7.34 ms; 7.45 with plain stores; 8.84 past the caches from the lanes.)
+            static_assert(COLS == 64, "rows of 128 bytes");
+            uint32_t* const rows = stage + wave * (32 * PITCH);
 #pragma unroll
-        for (int j = 0; j < TN; ++j) {
-            const float* const a = v + 4 * Q * j;
-            if constexpr (M32) {
-                // lanes l and l + 32 hold four columns each of the same eight: they exchange, so that each stores eight
+            for (int j = 0; j < TN; ++j) {
+                const float* const a = v + 4 * Q * j;
+                // lanes l and l + 32 hold four columns each of the same eight: they exchange, so that each holds eight
 #pragma unroll
                 for (int q = 0; q < Q; q += 2) {
                     const auto s0 = __builtin_amdgcn_permlane32_swap(pair(a[4 * q], a[4 * q + 1]),
                                                                     pair(a[4 * q + 4], a[4 * q + 5]), false, false);
                     const auto s1 = __builtin_amdgcn_permlane32_swap(pair(a[4 * q + 2], a[4 * q + 3]),
                                                                     pair(a[4 * q + 6], a[4 * q + 7]), false, false);
-                    const int c = j * 32 + 8 * q + 8 * half;
-                    if (in && c < pad) *(u32x4_t*)(out + c) = u32x4_t{s0[0], s1[0], s0[1], s1[1]};
+                    *(u32x4_t*)(rows + lane % 32 * PITCH + j * 16 + 4 * q + 4 * half) = u32x4_t{s0[0], s1[0], s0[1], s1[1]};
                 }
-            } else {
+            }
+            __builtin_amdgcn_wave_barrier();  // one wave's LDS accesses are in order
+            const int64_t first = m - lane % 32;
+#pragma unroll
+            for (int r = 0; r < 32; r += 8) {
+                const int64_t mr = first + r + lane / 8;
+                const int c = lane % 8 * 8;
+                const u32x4_t w = *(const u32x4_t*)(rows + (r + lane / 8) * PITCH + c / 2);
+                if (mr < g.M && c < pad) __builtin_nontemporal_store(w, (u32x4_t*)((uint16_t*)g.c + mr * g.ldc + nw + c));
+            }
+            __builtin_amdgcn_wave_barrier();
+        } else {
+            uint16_t* const out = (uint16_t*)g.c + m * g.ldc + nw;
+#pragma unroll
+            for (int j = 0; j < TN; ++j) {
+                const float* const a = v + 4 * j;
                 const int c = col(j, 0);
                 if (in && c < pad) *(uint2*)(out + c) = make_uint2(pair(a[0], a[1]), pair(a[2], a[3]));
             }
@@ -1070,8 +1089,11 @@ __attribute__((amdgpu_waves_per_eu(WM * WN == 8 ? 2 : 1, WM * WN == 8 ? 2 : 8)))
     }
     wait_vmcnt(0);  // the trailing re-read loads land before the workgroup ends
 
-    if constexpr (EK == EK_SOFT || EK == EK_SOFT_GRAD)
-        soft_block_epilogue<bf16_t, EK == EK_SOFT_GRAD, BM, BN, WM, WN, M32>(g, c.m0, c.n0, acc, tid);
+    if constexpr (EK == EK_SOFT || EK == EK_SOFT_GRAD) {
+        static_assert(!M32 || WM * WN * 32 * 36 * 4 <= ST * P::STAGE_ELEMS * 2, "the waves' staged rows fit the ring");
+        if (M32 && g.c) __syncthreads();  // every wave is done with the ring
+        soft_block_epilogue<bf16_t, EK == EK_SOFT_GRAD, BM, BN, WM, WN, M32>(g, c.m0, c.n0, acc, tid, (uint32_t*)smem);
+    }
     else block_epilogue<BM, BN, WM, WN, M32, T, EK, P::THREADS, ST * P::STAGE_ELEMS>(g, c.m0, c.n0, z, acc, smem, tid);
 }
 
@@ -1349,7 +1371,7 @@ __global__ __launch_bounds__(256) void k_gemm_f32_lds(GemmArgs g) {
     }
     wait_vmcnt(0);  // the loads that were issued past the end have landed
     if constexpr (EK == EK_SOFT || EK == EK_SOFT_GRAD) {
-        soft_block_epilogue<float, EK == EK_SOFT_GRAD, BM, BN, 2, 2, false>(g, m0, n0, acc, tid);
+        soft_block_epilogue<float, EK == EK_SOFT_GRAD, BM, BN, 2, 2, false>(g, m0, n0, acc, tid, nullptr);
         return;
     }
     __syncthreads();
@@ -1679,7 +1701,7 @@ GemmPlan plan_gemm_long(int64_t M, int64_t N, int64_t K, bool bf16) {
     const int64_t t64 = ((M + 63) / 64) * ((N + 63) / 64);
     if (p.bm == 64 && t64 < 128 && K >= 768) {
         // few blocks of a long K each: split it down to 128, past plan_gemm's 512 (gradient pass of 333 x 136 x 1001, 18
-        // blocks: FIG2)
+        // blocks: 33.0 -> 29.7 us)
         const int64_t sp = std::min<int64_t>({256 / t64, K / 128, 16});
         if (sp > p.splits) p.splits = (int)sp;
     }

@@ -21,11 +21,19 @@ __device__ __forceinline__ int64_t label_of(const void* labels, bool l64, int64_
     return l64 ? ((const int64_t*)labels)[m] : (int64_t)((const int32_t*)labels)[m];
 }
 
-__device__ __forceinline__ void join(float& mx, float& sum, float m2, float s2) {
-    const float c = fmaxf(mx, m2);
-    // a range without any visible class has (-inf, 0); the sums of two such stay 0
-    sum = (mx == NEG_INF ? sum : sum * expf(mx - c)) + (m2 == NEG_INF ? s2 : s2 * expf(m2 - c));
+// Joins N more ranges to (mx, sum): one maximum, then N + 1 exponentials that do not wait for each other. A range
+// without any visible class has (-inf, 0) and adds nothing.
+template <int N>
+__device__ __forceinline__ void join(float& mx, float& sum, const float2 (&p)[N]) {
+    float c = mx;
+#pragma unroll
+    for (int k = 0; k < N; ++k) c = fmaxf(c, p[k].x);
+    const float top = c == NEG_INF ? 0.f : c;
+    float s = sum * __expf(mx - top);
+#pragma unroll
+    for (int k = 0; k < N; ++k) s += p[k].y * __expf(p[k].x - top);
     mx = c;
+    sum = s;
 }
 
 // A row without a label may hold anything (padding behind a sequence, infinities, NaN): its
@@ -57,16 +65,19 @@ __global__ __launch_bounds__(256) void k_soft_rows(SoftRows a, int rpb) {
     const int64_t m = (int64_t)blockIdx.x * rpb + r;
     float mx = NEG_INF, sum = 0.f;
     if (m < a.rows)
-        for (int64_t t = part; t < a.tiles; t += parts) {
-            const float2 p = a.softpart[t * a.rows + m];
-            join(mx, sum, p.x, p.y);
+        for (int64_t t = part; t < a.tiles; t += 8 * parts) {
+            float2 p[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                p[k] = t + k * parts < a.tiles ? a.softpart[(t + k * parts) * a.rows + m] : make_float2(NEG_INF, 0.f);
+            join(mx, sum, p);
         }
     sh[threadIdx.x] = make_float2(mx, sum);
     for (int o = parts / 2; o > 0; o >>= 1) {
         __syncthreads();
         if (part < o) {
-            const float2 p = sh[threadIdx.x + o * rpb];
-            join(mx, sum, p.x, p.y);
+            const float2 p[1] = {sh[threadIdx.x + o * rpb]};
+            join(mx, sum, p);
             sh[threadIdx.x] = make_float2(mx, sum);
         }
     }
