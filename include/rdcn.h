@@ -536,7 +536,8 @@ rdcn_status rdcn_softmax_loss_grad(rdcn_handle* h, int64_t rows, int64_t dim, in
  *   m' = beta1 m + (1 - beta1) g'
  *   v' = beta2 v + (1 - beta2) g' g'
  *   p' = p (1 - lr weight_decay) - lr / (1 - beta1^t) * m' / (sqrt(v') / sqrt(1 - beta2^t) + eps)
- * each operation one rounding to float (constants rounded once from double).
+ * each operation one rounding to float (constants rounded once from double; with 8-bit
+ * moments the root and the quotient are within a unit in the last place instead).
  * Weights are float, bf16 with a float master (the master is stepped, the weight
  * is its nearest bf16), or bf16 alone.
  * Moments are float, or 8 bits: a block of 256 consecutive elements has one
@@ -571,7 +572,7 @@ typedef struct rdcn_adamw_tensor {
 } rdcn_adamw_tensor;
 
 typedef struct rdcn_adamw_config {
-    double lr, beta1, beta2, eps;  /* betas in [0, 1), eps > 0 (as a float too) */
+    double lr, beta1, beta2, eps;  /* betas in [0, 1), eps a normal float > 0 */
     double grad_scale;             /* 1, or what undoes a loss scale */
     int64_t step;                  /* t >= 1 */
     const float* device_lr;        /* or NULL; device memory, read by the step instead of lr */

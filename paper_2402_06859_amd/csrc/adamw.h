@@ -17,9 +17,9 @@ struct AdamwTensor {
     int64_t n;
     float decay;       // 1 - lr * weight_decay (host lr)
     float weight_decay;
-    uint32_t flags;    // ADAMW_*
+    uint32_t flags;    // ADAMW_*, and from bit ADAMW_ORDINAL on the tensor's place in the caller's list
 };
-enum { ADAMW_PARAM_BF16 = 1, ADAMW_GRAD_BF16 = 2, ADAMW_8BIT = 4 };
+enum { ADAMW_PARAM_BF16 = 1, ADAMW_GRAD_BF16 = 2, ADAMW_8BIT = 4, ADAMW_ORDINAL = 8 };
 
 struct AdamwScalars {
     float beta1, beta2, c1, c2, eps;  // c = 1 - beta, rounded once from double

@@ -4,7 +4,8 @@
 //   p' = p (1 - lr wd) - lr / (1 - beta1^t) * m' / (sqrt(v') / sqrt(1 - beta2^t) + eps)
 //
 // Every operation above is one rounding to float in this order (no contraction to fused ones): a step
-// is the same bits wherever an element stands, and 8-bit codes do not hang on how it was compiled.
+// is the same bits wherever an element stands, and 8-bit codes do not hang on how it was compiled. (With 8-bit
+// moments the root and the quotient, which only p' depends on, are within a unit in the last place each.)
 //
 // 8-bit moments. A block of 256 elements has one exponent, its largest element's. An
 // element's code is the upper bits of its float (exponent and 3 mantissa bits, bits 20 and up)
@@ -30,7 +31,6 @@ struct Batch {
     AdamwTensor t[PER_LAUNCH];
     uint32_t first[PER_LAUNCH + 1];  // first chunk of each tensor
     int count;
-    uint32_t ordinal0;               // of t[0] among all tensors of the call
     AdamwScalars a;
 };
 static_assert(sizeof(Batch) <= 4096, "kernel arguments");
@@ -71,14 +71,10 @@ __device__ __forceinline__ uint32_t code_base(uint32_t e, uint32_t top) {
 __device__ __forceinline__ float decode(uint32_t size, uint32_t base) {
     return size ? __uint_as_float((size + base) << 20) : 0.f;
 }
-__device__ __forceinline__ uint32_t encode(uint32_t size, uint32_t base, uint32_t top, uint32_t rnd) {
-    const int c = (int)((size + rnd) >> 20) - (int)base;
-    return c < 0 ? 0u : c > (int)top ? top : (uint32_t)c;
-}
-
-// EPT values from p (whole: all inside; else the first `left`), zero past the end.
-__device__ __forceinline__ void load_f32(const float* p, bool whole, int left, float* v) {
-    if (whole) {
+// EPT values at p: all of them (WHOLE), or the first `left` and zeros.
+template <bool WHOLE>
+__device__ __forceinline__ void load_f32(const float* p, int left, float* v) {
+    if constexpr (WHOLE) {
         *(f32x4_t*)v = *(const f32x4_t*)p;
         *(f32x4_t*)(v + 4) = *(const f32x4_t*)(p + 4);
     } else {
@@ -86,16 +82,18 @@ __device__ __forceinline__ void load_f32(const float* p, bool whole, int left, f
         for (int e = 0; e < EPT; ++e) v[e] = e < left ? p[e] : 0.f;
     }
 }
-__device__ __forceinline__ void load_bf16(const bf16_t* p, bool whole, int left, float* v) {
-    if (whole) {
+template <bool WHOLE>
+__device__ __forceinline__ void load_bf16(const bf16_t* p, int left, float* v) {
+    if constexpr (WHOLE) {
         st<bf16_t>::unpack(*(const u32x4_t*)p, v);
     } else {
 #pragma unroll
         for (int e = 0; e < EPT; ++e) v[e] = e < left ? bf16_to_f32(p[e]) : 0.f;
     }
 }
-__device__ __forceinline__ void store_f32(float* p, bool whole, int left, const float* v) {
-    if (whole) {
+template <bool WHOLE>
+__device__ __forceinline__ void store_f32(float* p, int left, const float* v) {
+    if constexpr (WHOLE) {
         *(f32x4_t*)p = *(const f32x4_t*)v;
         *(f32x4_t*)(p + 4) = *(const f32x4_t*)(v + 4);
     } else {
@@ -104,8 +102,19 @@ __device__ __forceinline__ void store_f32(float* p, bool whole, int left, const 
             if (e < left) p[e] = v[e];
     }
 }
-__device__ __forceinline__ void load_codes(const uint8_t* p, bool whole, int left, uint32_t* c) {
-    if (whole) {
+template <bool WHOLE>
+__device__ __forceinline__ void store_u16(bf16_t* p, int left, const uint32_t* r) {  // r < 2^16
+    if constexpr (WHOLE) {
+        *(u32x4_t*)p = u32x4_t{r[0] | r[1] << 16, r[2] | r[3] << 16, r[4] | r[5] << 16, r[6] | r[7] << 16};
+    } else {
+#pragma unroll
+        for (int e = 0; e < EPT; ++e)
+            if (e < left) p[e] = (bf16_t)r[e];
+    }
+}
+template <bool WHOLE>
+__device__ __forceinline__ void load_codes(const uint8_t* p, int left, uint32_t* c) {
+    if constexpr (WHOLE) {
         const uint2 w = *(const uint2*)p;
 #pragma unroll
         for (int e = 0; e < EPT; ++e) c[e] = ((e < 4 ? w.x : w.y) >> (8 * (e & 3))) & 255u;
@@ -114,8 +123,9 @@ __device__ __forceinline__ void load_codes(const uint8_t* p, bool whole, int lef
         for (int e = 0; e < EPT; ++e) c[e] = e < left ? p[e] : 0u;
     }
 }
-__device__ __forceinline__ void store_codes(uint8_t* p, bool whole, int left, const uint32_t* c) {
-    if (whole) {
+template <bool WHOLE>
+__device__ __forceinline__ void store_codes(uint8_t* p, int left, const uint32_t* c) {
+    if constexpr (WHOLE) {
         *(uint2*)p = make_uint2(c[0] | c[1] << 8 | c[2] << 16 | c[3] << 24, c[4] | c[5] << 8 | c[6] << 16 | c[7] << 24);
     } else {
 #pragma unroll
@@ -124,26 +134,133 @@ __device__ __forceinline__ void store_codes(uint8_t* p, bool whole, int left, co
     }
 }
 
-// The largest magnitude's exponent over the 32 lanes of a block of 256 elements.
-__device__ __forceinline__ uint32_t block_exponent(const float* v) {
-    uint32_t mx = 0;
-#pragma unroll
-    for (int e = 0; e < EPT; ++e) mx = max(mx, __float_as_uint(v[e]) & 0x7FFFFFFFu);
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) mx = max(mx, (uint32_t)__shfl_xor((int)mx, o));
-    return mx >> 23;
+// The largest value over the 32 lanes of a block of 256 elements: exchanges within rows of 16 lanes as part of the
+// maximum's own operands, then one of two rows.
+__device__ __forceinline__ uint32_t max_of_block(uint32_t x) {
+    x = max(x, (uint32_t)__builtin_amdgcn_update_dpp((int)x, (int)x, 0xB1, 0xF, 0xF, true));   // lane ^ 1
+    x = max(x, (uint32_t)__builtin_amdgcn_update_dpp((int)x, (int)x, 0x4E, 0xF, 0xF, true));   // lane ^ 2
+    x = max(x, (uint32_t)__builtin_amdgcn_update_dpp((int)x, (int)x, 0x141, 0xF, 0xF, true));  // mirrored in 8
+    x = max(x, (uint32_t)__builtin_amdgcn_update_dpp((int)x, (int)x, 0x140, 0xF, 0xF, true));  // mirrored in 16
+    const auto r = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+    return max(r[0], r[1]);
 }
 
-__global__ __launch_bounds__(256) void k_adamw(Batch b) {
+struct StepScalars {
+    float gs, step_size, r2, decay;
+    uint32_t key;
+};
+
+// One thread's EPT elements from `at` on of one tensor.
+template <bool EIGHT, bool WHOLE>
+__device__ __forceinline__ void adamw_elements(const AdamwTensor& t, const AdamwScalars& a, const StepScalars& k, int64_t at) {
 #pragma clang fp contract(off)
+    const int left = WHOLE ? EPT : at < t.n ? (int)(t.n - at < EPT ? t.n - at : EPT) : 0;
+    const bool pbf = t.flags & ADAMW_PARAM_BF16;
+    const int64_t blocks = (t.n + ADAMW_BLOCK - 1) / ADAMW_BLOCK, blk = at / ADAMW_BLOCK;
+    float p[EPT], g[EPT], m[EPT], v[EPT];
+    if (t.flags & ADAMW_GRAD_BF16) load_bf16<WHOLE>((const bf16_t*)t.grad + at, left, g);
+    else load_f32<WHOLE>((const float*)t.grad + at, left, g);
+    if (t.master) load_f32<WHOLE>(t.master + at, left, p);
+    else if (pbf) load_bf16<WHOLE>((const bf16_t*)t.param + at, left, p);
+    else load_f32<WHOLE>((const float*)t.param + at, left, p);
+    if constexpr (EIGHT) {
+        uint32_t cm[EPT], cv[EPT];
+        load_codes<WHOLE>((const uint8_t*)t.m + at, left, cm);
+        load_codes<WHOLE>((const uint8_t*)t.v + at, left, cv);
+        const uint32_t bm = left ? code_base(t.exps[blk], 127) : 0, bv = left ? code_base(t.exps[blocks + blk], 255) : 0;
+#pragma unroll
+        for (int e = 0; e < EPT; ++e) {
+            m[e] = __uint_as_float(__float_as_uint(decode(cm[e] & 127u, bm)) | (cm[e] & 128u) << 24);
+            v[e] = decode(cv[e], bv);
+        }
+    } else {
+        load_f32<WHOLE>((const float*)t.m + at, left, m);
+        load_f32<WHOLE>((const float*)t.v + at, left, v);
+    }
+#pragma unroll
+    for (int e = 0; e < EPT; ++e) {
+        const float x = g[e] * k.gs;
+        m[e] = m[e] * a.beta1 + x * a.c1;
+        v[e] = v[e] * a.beta2 + (x * x) * a.c2;
+        // 8-bit moments: the root and the quotient from the units alone (each within a unit in the last place, far
+        // below what the codes' 3 bits carry); the rounded ones cost 24 more operations, and these kernels are bound by those
+        const float down = (EIGHT ? __builtin_amdgcn_sqrtf(v[e]) : sqrtf(v[e])) * k.r2 + a.eps;
+        const float q = EIGHT ? m[e] * __builtin_amdgcn_rcpf(down) : m[e] / down;
+        p[e] = p[e] * k.decay - q * k.step_size;
+    }
+    uint32_t h[EPT];
+    if (a.stochastic && (EIGHT || (pbf && !t.master))) {
+#pragma unroll
+        for (int e = 0; e < EPT; ++e) h[e] = fmix32((uint32_t)(at + e) ^ k.key);
+    }
+    if (t.master) store_f32<WHOLE>(t.master + at, left, p);
+    if (!pbf) {
+        store_f32<WHOLE>((float*)t.param + at, left, p);
+    } else {
+        uint32_t r[EPT];
+        if (a.stochastic && !t.master) {
+#pragma unroll
+            for (int e = 0; e < EPT; ++e) {
+                r[e] = (__float_as_uint(p[e]) + ((h[e] * 0x85EBCA6Bu) >> 16)) >> 16;
+                r[e] = p[e] == p[e] ? r[e] : 0x7FC0u;  // (a NaN's bits could carry into its sign)
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < EPT; ++e) r[e] = f32_to_bf16(p[e]);
+        }
+        store_u16<WHOLE>((bf16_t*)t.param + at, left, r);
+    }
+    if constexpr (!EIGHT) {
+        store_f32<WHOLE>((float*)t.m + at, left, m);
+        store_f32<WHOLE>((float*)t.v + at, left, v);
+    } else {
+        if constexpr (!WHOLE) {  // past the end nothing counts towards the block's largest
+#pragma unroll
+            for (int e = 0; e < EPT; ++e)
+                if (e >= left) m[e] = v[e] = 0.f;
+        }
+        uint32_t um[EPT], uv[EPT], mm = 0, mv = 0;
+#pragma unroll
+        for (int e = 0; e < EPT; ++e) {
+            um[e] = __float_as_uint(m[e]) & 0x7FFFFFFFu;
+            uv[e] = __float_as_uint(v[e]) & 0x7FFFFFFFu;
+            mm = max(mm, um[e]);
+            mv = max(mv, uv[e]);
+        }
+        const uint32_t em = max_of_block(mm) >> 23, ev = max_of_block(mv) >> 23;
+        const uint32_t bm = code_base(em, 127) << 20, bv = code_base(ev, 255) << 20;
+        uint32_t cm[EPT], cv[EPT];
+#pragma unroll
+        for (int e = 0; e < EPT; ++e) {
+            const uint32_t rm = a.stochastic ? h[e] >> 12 : 0x80000u;
+            const uint32_t rv = a.stochastic ? (h[e] * 0x9E3779B1u) >> 12 : 0x80000u;
+            // (a value of the block is at most 8 2^20 above its exponent's base + top: the differences fit an int; of a
+            // zero and what lies below the reach they are negative or round to 0)
+            const int x = (int)(um[e] + rm - bm) >> 20, y = (int)(uv[e] + rv - bv) >> 20;
+            cm[e] = (uint32_t)min(max(x, 0), 127) | (__float_as_uint(m[e]) >> 24 & 128u);
+            cv[e] = (uint32_t)min(max(y, (int)min(uv[e], 1u)), 255);
+        }
+        store_codes<WHOLE>((uint8_t*)t.m + at, left, cm);
+        store_codes<WHOLE>((uint8_t*)t.v + at, left, cv);
+        if ((threadIdx.x & 31) == 0 && left) {
+            t.exps[blk] = (uint8_t)em;
+            t.exps[blocks + blk] = (uint8_t)ev;
+        }
+    }
+}
+
+template <bool EIGHT>
+__global__ __launch_bounds__(256) void k_adamw(Batch b) {
     const AdamwScalars& a = b.a;
-    float gs = a.grad_scale;
+    StepScalars k;
+    k.gs = a.grad_scale;
     if (a.clip) {
         const float c = *a.clip;
         if (!(fabsf(c) < __builtin_huge_valf())) return;  // not finite: the gradients' norm was not, nothing is changed
-        gs *= c;
+        k.gs *= c;
     }
-    float step_size = a.step_size, r2 = a.rsqrt_grown2;
+    k.step_size = a.step_size;
+    k.r2 = a.rsqrt_grown2;
     const bool live = a.device_lr || a.device_step;
     double lr = a.lr;
     uint32_t seed = a.seed;
@@ -152,125 +269,37 @@ __global__ __launch_bounds__(256) void k_adamw(Batch b) {
         int64_t t = a.device_step ? *a.device_step : a.step;
         if (t < 1) t = 1;
         if (a.device_step) seed += (uint32_t)t * 0x85EBCA6Bu;  // a step that is replayed draws anew
-        step_size = (float)(lr / -expm1((double)t * a.logb1));
-        r2 = (float)(1.0 / sqrt(-expm1((double)t * a.logb2)));
+        k.step_size = (float)(lr / -expm1((double)t * a.logb1));
+        k.r2 = (float)(1.0 / sqrt(-expm1((double)t * a.logb2)));
     }
     const uint32_t chunks = b.first[b.count];
     for (uint32_t c = blockIdx.x; c < chunks; c += gridDim.x) {
         const int i = tensor_of(b.first, b.count, c);
         const AdamwTensor& t = b.t[i];
-        const int64_t at = (int64_t)(c - b.first[i]) * CHUNK + threadIdx.x * EPT;
-        const bool whole = at + EPT <= t.n;
-        const int left = whole ? EPT : at < t.n ? (int)(t.n - at) : 0;
-        const float decay = live ? (float)(1.0 - lr * (double)t.weight_decay) : t.decay;
-        const bool pbf = t.flags & ADAMW_PARAM_BF16, eight = t.flags & ADAMW_8BIT;
-        const int64_t blocks = (t.n + ADAMW_BLOCK - 1) / ADAMW_BLOCK, blk = at / ADAMW_BLOCK;
-        float p[EPT], g[EPT], m[EPT], v[EPT];
-        if (t.flags & ADAMW_GRAD_BF16) load_bf16((const bf16_t*)t.grad + at, whole, left, g);
-        else load_f32((const float*)t.grad + at, whole, left, g);
-        if (t.master) load_f32(t.master + at, whole, left, p);
-        else if (pbf) load_bf16((const bf16_t*)t.param + at, whole, left, p);
-        else load_f32((const float*)t.param + at, whole, left, p);
-        if (eight) {
-            uint32_t cm[EPT], cv[EPT];
-            load_codes((const uint8_t*)t.m + at, whole, left, cm);
-            load_codes((const uint8_t*)t.v + at, whole, left, cv);
-            const uint32_t bm = left ? code_base(t.exps[blk], 127) : 0, bv = left ? code_base(t.exps[blocks + blk], 255) : 0;
-#pragma unroll
-            for (int e = 0; e < EPT; ++e) {
-                const float s = decode(cm[e] & 127u, bm);
-                m[e] = cm[e] & 128u ? -s : s;
-                v[e] = decode(cv[e], bv);
-            }
-        } else {
-            load_f32((const float*)t.m + at, whole, left, m);
-            load_f32((const float*)t.v + at, whole, left, v);
-        }
-#pragma unroll
-        for (int e = 0; e < EPT; ++e) {
-            const float x = g[e] * gs;
-            m[e] = m[e] * a.beta1 + x * a.c1;
-            v[e] = v[e] * a.beta2 + (x * x) * a.c2;
-            const float down = sqrtf(v[e]) * r2 + a.eps;
-            p[e] = p[e] * decay - (m[e] / down) * step_size;
-        }
-        uint32_t h[EPT];
-        const uint32_t key = seed + 0x9E3779B9u * (b.ordinal0 + (uint32_t)i + 1u);
-        const bool chance = a.stochastic && (eight || (pbf && !t.master));
-#pragma unroll
-        for (int e = 0; e < EPT; ++e) h[e] = chance ? fmix32((uint32_t)(at + e) ^ key) : 0;
-        if (t.master) store_f32(t.master + at, whole, left, p);
-        if (!pbf) {
-            store_f32((float*)t.param + at, whole, left, p);
-        } else {
-            bf16_t* const q = (bf16_t*)t.param + at;
-            uint32_t r[EPT];
-#pragma unroll
-            for (int e = 0; e < EPT; ++e) {
-                r[e] = f32_to_bf16(p[e]);
-                if (chance && !t.master && p[e] == p[e])
-                    r[e] = (__float_as_uint(p[e]) + ((h[e] * 0x85EBCA6Bu) >> 16)) >> 16;
-            }
-            if (whole) {
-                *(u32x4_t*)q = u32x4_t{r[0] | r[1] << 16, r[2] | r[3] << 16, r[4] | r[5] << 16, r[6] | r[7] << 16};
-            } else {
-#pragma unroll
-                for (int e = 0; e < EPT; ++e)
-                    if (e < left) q[e] = (bf16_t)r[e];
-            }
-        }
-        if (!eight) {
-            store_f32((float*)t.m + at, whole, left, m);
-            store_f32((float*)t.v + at, whole, left, v);
-            continue;
-        }
-        if (!whole) {  // past the end nothing counts towards the block's largest
-#pragma unroll
-            for (int e = 0; e < EPT; ++e)
-                if (e >= left) m[e] = v[e] = 0.f;
-        }
-        const uint32_t em = block_exponent(m), ev = block_exponent(v);
-        const uint32_t bm = code_base(em, 127), bv = code_base(ev, 255);
-        uint32_t cm[EPT], cv[EPT];
-#pragma unroll
-        for (int e = 0; e < EPT; ++e) {
-            const uint32_t um = __float_as_uint(m[e]), uv = __float_as_uint(v[e]) & 0x7FFFFFFFu;
-            const uint32_t rm = a.stochastic ? h[e] >> 12 : 0x80000u;
-            const uint32_t rv = a.stochastic ? (h[e] * 0x9E3779B1u) >> 12 : 0x80000u;
-            const uint32_t sm = um & 0x7FFFFFFFu;
-            cm[e] = (sm ? encode(sm, bm, 127, rm) : 0u) | (um >> 31) << 7;
-            const uint32_t x = encode(uv, bv, 255, rv);
-            cv[e] = uv == 0 ? 0u : x > 0 ? x : 1u;
-        }
-        store_codes((uint8_t*)t.m + at, whole, left, cm);
-        store_codes((uint8_t*)t.v + at, whole, left, cv);
-        if ((threadIdx.x & 31) == 0 && left) {
-            t.exps[blk] = (uint8_t)em;
-            t.exps[blocks + blk] = (uint8_t)ev;
-        }
+        const int64_t from = (int64_t)(c - b.first[i]) * CHUNK, at = from + threadIdx.x * EPT;
+        k.decay = live ? (float)(1.0 - lr * (double)t.weight_decay) : t.decay;
+        k.key = seed + 0x9E3779B9u * ((t.flags >> ADAMW_ORDINAL) + 1u);
+        if (from + CHUNK <= t.n) adamw_elements<EIGHT, true>(t, a, k, at);
+        else adamw_elements<EIGHT, false>(t, a, k, at);
     }
+}
+
+template <bool WHOLE>
+__device__ __forceinline__ void code_values(const uint8_t* codes, uint32_t base, uint32_t top, int left, bf16_t* out) {
+    uint32_t c[EPT], r[EPT];
+    load_codes<WHOLE>(codes, left, c);
+    // 3 mantissa bits: the upper half of the float is the bf16 value itself
+#pragma unroll
+    for (int e = 0; e < EPT; ++e) r[e] = __float_as_uint(decode(c[e] & top, base)) >> 16 | (c[e] & ~top) << 8;
+    store_u16<WHOLE>(out, left, r);
 }
 
 __global__ __launch_bounds__(256) void k_adamw_values(int64_t n, const uint8_t* codes, const uint8_t* exps, uint32_t top,
                                                       bf16_t* out) {
     for (int64_t at = (blockIdx.x * 256ll + threadIdx.x) * EPT; at < n; at += gridDim.x * (int64_t)CHUNK) {
-        const bool whole = at + EPT <= n;
-        const int left = whole ? EPT : (int)(n - at);
-        uint32_t c[EPT], r[EPT];
-        load_codes(codes + at, whole, left, c);
         const uint32_t base = code_base(exps[at / ADAMW_BLOCK], top);
-#pragma unroll
-        for (int e = 0; e < EPT; ++e) {
-            // 3 mantissa bits: the upper half of the float is the bf16 value itself
-            r[e] = __float_as_uint(decode(c[e] & top, base)) >> 16 | (c[e] & ~top) << 8;
-        }
-        if (whole) {
-            *(u32x4_t*)(out + at) = u32x4_t{r[0] | r[1] << 16, r[2] | r[3] << 16, r[4] | r[5] << 16, r[6] | r[7] << 16};
-        } else {
-#pragma unroll
-            for (int e = 0; e < EPT; ++e)
-                if (e < left) out[at + e] = (bf16_t)r[e];
-        }
+        if (at + EPT <= n) code_values<true>(codes + at, base, top, EPT, out + at);
+        else code_values<false>(codes + at, base, top, (int)(n - at), out + at);
     }
 }
 
@@ -292,11 +321,16 @@ __global__ __launch_bounds__(256) void k_grad_norm(NormBatch b) {
     for (uint32_t c = blockIdx.x; c < chunks; c += gridDim.x) {
         const int i = tensor_of(b.first, b.count, c);
         const int64_t at = (int64_t)(c - b.first[i]) * CHUNK + threadIdx.x * EPT;
-        const bool whole = at + EPT <= b.n[i];
-        const int left = whole ? EPT : at < b.n[i] ? (int)(b.n[i] - at) : 0;
+        const int left = at < b.n[i] ? (int)(b.n[i] - at < EPT ? b.n[i] - at : EPT) : 0;
+        const bool bf = b.flags[i] & ADAMW_GRAD_BF16;
         float g[EPT];
-        if (b.flags[i] & ADAMW_GRAD_BF16) load_bf16((const bf16_t*)b.grad[i] + at, whole, left, g);
-        else load_f32((const float*)b.grad[i] + at, whole, left, g);
+        if (left == EPT) {
+            if (bf) load_bf16<true>((const bf16_t*)b.grad[i] + at, left, g);
+            else load_f32<true>((const float*)b.grad[i] + at, left, g);
+        } else {
+            if (bf) load_bf16<false>((const bf16_t*)b.grad[i] + at, left, g);
+            else load_f32<false>((const float*)b.grad[i] + at, left, g);
+        }
 #pragma unroll
         for (int e = 0; e < EPT; ++e) s = fma((double)g[e], (double)g[e], s);
     }
@@ -331,17 +365,20 @@ uint32_t place(const AdamwTensor* t, int count, uint32_t* first) {
 }  // namespace
 
 hipError_t launch_adamw(const AdamwTensor* t, int count, const AdamwScalars& a, hipStream_t s) {
-    for (int at = 0; at < count; at += PER_LAUNCH) {
-        Batch b;
-        b.count = count - at < PER_LAUNCH ? count - at : PER_LAUNCH;
-        for (int i = 0; i < b.count; ++i) b.t[i] = t[at + i];
-        const uint32_t chunks = place(t + at, b.count, b.first);
-        if (chunks == 0) continue;
-        b.ordinal0 = (uint32_t)at;
-        b.a = a;
-        hipLaunchKernelGGL(k_adamw, dim3(chunks < STEP_BLOCKS ? chunks : STEP_BLOCKS), dim3(256), 0, s, b);
-        const hipError_t e = hipGetLastError();
-        if (e != hipSuccess) return e;
+    Batch b;
+    b.a = a;
+    for (int kind = 0; kind < 2; ++kind) {  // tensors with float moments, then those with 8-bit ones
+        b.count = 0;
+        for (int i = 0; i <= count; ++i) {
+            if (i < count && t[i].n > 0 && ((t[i].flags & ADAMW_8BIT) != 0) == (kind == 1)) b.t[b.count++] = t[i];
+            if (b.count < PER_LAUNCH && (i < count || b.count == 0)) continue;
+            const uint32_t chunks = place(b.t, b.count, b.first), grid = chunks < STEP_BLOCKS ? chunks : STEP_BLOCKS;
+            if (kind) hipLaunchKernelGGL(k_adamw<true>, dim3(grid), dim3(256), 0, s, b);
+            else hipLaunchKernelGGL(k_adamw<false>, dim3(grid), dim3(256), 0, s, b);
+            const hipError_t e = hipGetLastError();
+            if (e != hipSuccess) return e;
+            b.count = 0;
+        }
     }
     return hipSuccess;
 }

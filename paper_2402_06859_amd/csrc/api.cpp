@@ -4,6 +4,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <cfloat>
 #include <cmath>
 #include <new>
 #include <string.h>
@@ -539,14 +540,14 @@ rdcn_status check_step_tensors(const rdcn_adamw_tensor* t, int32_t count) {
     return RDCN_OK;
 }
 
-AdamwTensor adamw_tensor(const rdcn_adamw_tensor& x, double lr) {
+AdamwTensor adamw_tensor(const rdcn_adamw_tensor& x, int32_t ordinal, double lr) {
     AdamwTensor t{};
     t.param = x.param; t.master = x.master; t.grad = x.grad; t.m = x.m; t.v = x.v; t.exps = x.exps;
     t.n = x.n;
     t.decay = (float)(1.0 - lr * x.weight_decay);
     t.weight_decay = (float)x.weight_decay;
     t.flags = (x.param_dtype == RDCN_BF16 ? ADAMW_PARAM_BF16 : 0) | (x.grad_dtype == RDCN_BF16 ? ADAMW_GRAD_BF16 : 0) |
-              (x.moments == RDCN_MOMENTS_8BIT ? ADAMW_8BIT : 0);
+              (x.moments == RDCN_MOMENTS_8BIT ? ADAMW_8BIT : 0) | (uint32_t)ordinal << ADAMW_ORDINAL;
     return t;
 }
 
@@ -1386,7 +1387,7 @@ rdcn_status rdcn_grad_norm_workspace(const rdcn_handle* h, const rdcn_adamw_tens
     if (!scratch_bytes) return RDCN_ERR_ARG;
     TensorList l(count);
     if (!l.t) return RDCN_ERR_HIP;
-    for (int32_t i = 0; i < count; ++i) l.t[i] = adamw_tensor(tensors[i], 0.0);
+    for (int32_t i = 0; i < count; ++i) l.t[i] = adamw_tensor(tensors[i], i, 0.0);
     *scratch_bytes = al((size_t)grad_norm_partials(l.t, count) * 8);
     return RDCN_OK;
 }
@@ -1398,7 +1399,7 @@ rdcn_status rdcn_grad_norm(rdcn_handle* h, const rdcn_adamw_tensor* tensors, int
     if (!out || !std::isfinite(grad_scale) || !(max_norm > 0.0f)) return RDCN_ERR_ARG;
     TensorList l(count);
     if (!l.t) return RDCN_ERR_HIP;
-    for (int32_t i = 0; i < count; ++i) l.t[i] = adamw_tensor(tensors[i], 0.0);
+    for (int32_t i = 0; i < count; ++i) l.t[i] = adamw_tensor(tensors[i], i, 0.0);
     const size_t need = (size_t)grad_norm_partials(l.t, count) * 8;
     if (need > 0 && (!scratch || !aligned256(scratch) || scratch_bytes < need)) return RDCN_ERR_WORKSPACE;
     return hip_status(launch_grad_norm(l.t, count, grad_scale, max_norm, (double*)scratch, out, (hipStream_t)stream));
@@ -1409,7 +1410,7 @@ rdcn_status rdcn_adamw_step(rdcn_handle* h, const rdcn_adamw_config* cfg, const 
     if (!h || !cfg) return RDCN_ERR_ARG;
     const rdcn_adamw_config& c = *cfg;
     if (!std::isfinite(c.lr) || !(c.beta1 >= 0.0 && c.beta1 < 1.0) || !(c.beta2 >= 0.0 && c.beta2 < 1.0) ||
-        !((float)c.eps > 0.0f) || !std::isfinite(c.eps) || !std::isfinite(c.grad_scale) ||
+        !((float)c.eps >= FLT_MIN) || !std::isfinite(c.eps) || !std::isfinite(c.grad_scale) ||
         (!c.device_step && c.step < 1) || (c.stochastic != 0 && c.stochastic != 1))
         return RDCN_ERR_ARG;
     rdcn_status st = check_tensors(h, tensors, count);
@@ -1418,7 +1419,7 @@ rdcn_status rdcn_adamw_step(rdcn_handle* h, const rdcn_adamw_config* cfg, const 
     if ((st = check_apart(tensors, count)) != RDCN_OK) return st;
     TensorList l(count);
     if (!l.t) return RDCN_ERR_HIP;
-    for (int32_t i = 0; i < count; ++i) l.t[i] = adamw_tensor(tensors[i], c.lr);
+    for (int32_t i = 0; i < count; ++i) l.t[i] = adamw_tensor(tensors[i], i, c.lr);
     AdamwScalars a{};
     const double t = (double)(c.step < 1 ? 1 : c.step);
     a.beta1 = (float)c.beta1; a.beta2 = (float)c.beta2;
