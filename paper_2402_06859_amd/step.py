@@ -1,18 +1,25 @@
 """Device buffers for one synthetic batch and the sequence of librdcn calls that
 make one training step of the path: gather -> forward -> backward -> embedding
-backward. Only allocation and call order live here; all arithmetic is in the
-library's kernels.
+backward, with a head's loss between them (DeviceHead, DeviceClasses) and the
+weights' update after them (DeviceAdamW). Only allocation and call order live
+here; all arithmetic is in the library's kernels.
 """
 from __future__ import annotations
 
-from typing import Optional
+import contextlib
+from typing import Optional, Sequence
 
 import torch
 
-from .rdcn import Rdcn, config_for
+from .rdcn import Rdcn, adamw_tensors, config_for
 from .synth import Workload
 
 _DT = {"bf16": torch.bfloat16, "f32": torch.float32}
+
+
+def _on(stream):
+    """Torch's own operations on `stream` (None: the current one)."""
+    return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
 
 
 class DeviceBatch:
@@ -69,6 +76,16 @@ class DeviceBatch:
         self.lib.qr_embed_backward(self.B, self.nnz, self.ids, self.offsets, self.q_tables, self.r_tables,
                                    self.grad_x0 if grad_x0 is None else grad_x0, self.grad_q, self.grad_r,
                                    self.emb_scratch, stream)
+
+    def trained(self):
+        """(weight, gradient) of everything that the path trains."""
+        return (list(zip(self.w_down, self.g_w_down)) + list(zip(self.u, self.g_u)) + list(zip(self.bias, self.g_bias)) +
+                [(self.q_tables, self.grad_q), (self.r_tables, self.grad_r)])
+
+    def zero_table_grads(self, stream=None):
+        with _on(stream):
+            self.grad_q.zero_()
+            self.grad_r.zero_()
 
     def step(self, stream=None):
         """One pass of the whole path (table gradients accumulate)."""
@@ -134,3 +151,92 @@ class DeviceHead:
         self.backward(db.x_out, stream=stream)
         db.backward(self.grad_x, stream)
         db.embed_backward(stream=stream)
+
+
+class DeviceClasses:
+    """Softmax loss over a large set of classes (items, tokens) on x [B, dim], normally x_L of the
+    handle `lib`: class weights w [classes, dim], labels [B] (below 0: a row without one), their
+    gradients and the call's scratch."""
+
+    def __init__(self, lib: Rdcn, w: torch.Tensor, labels: torch.Tensor, offset: Optional[torch.Tensor] = None,
+                 row_weight: Optional[torch.Tensor] = None, logit_scale: float = 1.0):
+        self.lib, self.w, self.labels, self.offset, self.row_weight = lib, w, labels, offset, row_weight
+        self.logit_scale = logit_scale
+        self.B = labels.numel()
+        self.classes, self.dim = w.shape
+        dev = w.device
+        self.loss = torch.empty(self.B, dtype=torch.float32, device=dev)
+        self.lse = torch.empty(self.B, dtype=torch.float32, device=dev)
+        self.grad_x = torch.empty((self.B, self.dim), dtype=w.dtype, device=dev)
+        self.grad_w = torch.empty_like(w)
+        self.scratch = torch.empty(max(lib.softmax_loss_workspace(self.B, self.dim, self.classes)[:2]),
+                                   dtype=torch.uint8, device=dev)
+
+    def trained(self):
+        return [(self.w, self.grad_w)]
+
+    def forward(self, x: torch.Tensor, stream=None):
+        """Loss and lse of every row, without gradients."""
+        self.lib.softmax_loss_forward(self.B, self.dim, self.classes, x, self.w, self.offset, self.labels,
+                                      self.logit_scale, self.loss, self.lse, self.scratch, stream)
+
+    def loss_grad(self, x: torch.Tensor, scale: Optional[float] = None, stream=None):
+        """Loss of every row and the gradients of scale (1 / B) times their (weighted) sum."""
+        self.lib.softmax_loss_grad(self.B, self.dim, self.classes, x, self.w, self.offset, self.labels,
+                                   self.logit_scale, self.row_weight, 1.0 / max(self.B, 1) if scale is None else scale,
+                                   self.loss, self.lse, self.grad_x, self.grad_w, self.scratch, stream)
+
+    def train_step(self, db: DeviceBatch, opt: Optional["DeviceAdamW"] = None, stream=None):
+        """One training step: gather -> cross stack -> softmax loss and its gradient -> cross-stack backward ->
+        embedding backward -> update."""
+        db.zero_table_grads(stream)
+        db.gather(stream)
+        db.forward(stream)
+        self.loss_grad(db.x_out, stream=stream)
+        db.backward(self.grad_x, stream)
+        db.embed_backward(stream=stream)
+        if opt is not None:
+            opt.update(stream)
+
+
+class DeviceAdamW:
+    """AdamW over (weight, gradient) pairs: moments in float or 8 bits, float masters of bf16 weights or none, and
+    the gradients clipped to max_norm together. Rate and step number stand on the device, so that an update
+    can be captured in a graph: change lr with set_lr."""
+
+    def __init__(self, lib: Rdcn, pairs: Sequence, lr: float, weight_decay: float = 0.0, moments: str = "f32",
+                 master: bool = True, max_norm: Optional[float] = None, beta1: float = 0.9, beta2: float = 0.999,
+                 eps: float = 1e-8, seed: int = 0):
+        self.lib, self.max_norm = lib, max_norm
+        self.hyper = dict(beta1=beta1, beta2=beta2, eps=eps, stochastic=True, seed=seed)
+        self.tensors = []
+        for p, g in pairs:
+            n, dev = p.numel(), p.device
+            mt = torch.uint8 if moments == "8bit" else torch.float32
+            t = {"param": p, "grad": g, "m": torch.zeros(n, dtype=mt, device=dev),
+                 "v": torch.zeros(n, dtype=mt, device=dev), "weight_decay": weight_decay if p.dim() > 1 else 0.0}
+            if moments == "8bit":
+                t["exps"] = torch.zeros(2 * -(-n // 256), dtype=torch.uint8, device=dev)
+            if master and p.dtype == torch.bfloat16:
+                t["master"] = p.float()
+            self.tensors.append(t)
+        self.list = adamw_tensors(self.tensors)
+        dev = self.tensors[0]["param"].device
+        self.lr = torch.full((1,), lr, dtype=torch.float32, device=dev)
+        self.steps = torch.zeros(1, dtype=torch.int64, device=dev)
+        self.norm = torch.zeros(2, dtype=torch.float32, device=dev)   # norm of the gradients, clip factor
+        self.scratch = torch.empty(max(256, lib.grad_norm_workspace(self.list)), dtype=torch.uint8, device=dev)
+
+    def set_lr(self, lr: float, stream=None):
+        with _on(stream):
+            self.lr.fill_(lr)
+
+    def update(self, stream=None):
+        with _on(stream):
+            self.steps.add_(1)
+        clip = None
+        if self.max_norm is not None:
+            self.lib.grad_norm(self.list, 1.0, self.max_norm, self.norm, self.scratch, stream)
+            clip = self.norm[1:]
+        self.lib.adamw_step(self.list, lr=0.0, device_lr=self.lr, device_step=self.steps, clip=clip, stream=stream,
+                            **self.hyper)

@@ -1,0 +1,125 @@
+"""The training calls as they are used together: gather -> cross stack -> softmax loss over many classes -> backward
+-> embedding backward -> gradient norm -> AdamW, eager and as one captured graph."""
+import numpy as np
+import pytest
+import torch
+
+import oracle
+from gpu_helpers import need_gpu, relerr
+from paper_2402_06859_amd import rdcn
+from paper_2402_06859_amd.step import DeviceAdamW, DeviceBatch, DeviceClasses
+from paper_2402_06859_amd.synth import WORKLOADS, make_inputs
+from test_gpu_softmax_loss import held, reference
+
+pytestmark = pytest.mark.gpu
+
+
+def build(name="small", batch=300, classes=2003, seed=0, **opt):
+    wl = WORKLOADS[name].with_(batch=batch, num_layers=2)
+    db = DeviceBatch(wl, make_inputs(wl, bias_std=0.1))
+    g = torch.Generator().manual_seed(seed)
+    dt = torch.bfloat16 if wl.dtype == "bf16" else torch.float32
+    w = (torch.randn(classes, wl.d, generator=g) * 0.02).to(dt).cuda()
+    labels = torch.randint(0, classes, (batch,), generator=g)
+    labels[5:9] = -1
+    dc = DeviceClasses(db.lib, w, labels.cuda(), offset=torch.randn(classes, generator=g).cuda(), logit_scale=0.5)
+    do = DeviceAdamW(db.lib, db.trained() + dc.trained(), lr=1e-3, weight_decay=0.01, **opt)
+    return wl, db, dc, do
+
+
+def state(db, dc, do):
+    out = [dc.loss, dc.grad_x, dc.grad_w, db.grad_x0, do.norm, do.steps] + [g for _, g in db.trained()]
+    for t in do.tensors:
+        out += [t[k] for k in ("param", "master", "m", "v", "exps") if t.get(k) is not None]
+    return out
+
+
+def same(a, b):
+    return all(torch.equal(x.contiguous().view(torch.uint8), y.contiguous().view(torch.uint8)) for x, y in zip(a, b))
+
+
+@pytest.mark.parametrize("name", ["small", "tiny"])
+def test_gradients_of_a_step(name):
+    need_gpu()
+    wl, db, dc, do = build(name, batch=96, max_norm=0.5)
+    w0 = [p.float().cpu().numpy().astype(np.float64) for p, _ in db.trained()]
+    L = wl.num_layers
+    dc.train_step(db, None)
+    torch.cuda.synchronize()
+    c = dict(x=db.x_out, w=dc.w, y=dc.labels, off=dc.offset, wt=None, s=0.5, scale=1.0 / dc.B)
+    ref, bound = reference(c, dc.B, dc.dim, dc.classes, wl.dtype == "f32")
+    for i, (tag, got) in enumerate((("loss", dc.loss), ("lse", dc.lse), ("grad_x", dc.grad_x), ("grad_w", dc.grad_w))):
+        held(tag, got, ref[i], bound[i])
+    # the stack's gradients for that grad_x, as the library's other tests bound them
+    x0 = db.x0.float().cpu().numpy().astype(np.float64)
+    W, U, b = w0[:L], w0[L:2 * L], w0[2 * L:3 * L]
+    gx0, gW, gU, gb = oracle.backward(x0, W, U, b, dc.grad_x.float().cpu().numpy().astype(np.float64), wl.alpha, wl.beta,
+                                      wl.temperature)
+    tol = 5e-2 if wl.dtype == "bf16" else 1e-4
+    assert relerr(db.grad_x0.cpu().numpy(), gx0) <= tol
+    for l in range(L):
+        assert relerr(db.g_w_down[l].cpu().numpy(), gW[l]) <= tol
+        assert relerr(db.g_u[l].cpu().numpy(), gU[l]) <= tol
+    # the update reads exactly these gradients
+    before = [t["m"].clone() for t in do.tensors]
+    do.update()
+    want = np.sqrt(sum(float((g.double() ** 2).sum()) for _, g in db.trained() + dc.trained()))
+    assert abs(float(do.norm[0]) - want) <= 2.0 ** -22 * want
+    f = float(do.norm[1])
+    assert abs(f - min(1.0, 0.5 / want)) <= 2.0 ** -22
+    for t, m in zip(do.tensors, before):
+        # m = 0.1 f g: three roundings of 2^-24 and that of 0.1
+        exact = t["grad"].double().flatten() * 0.1 * f
+        assert ((t["m"].double() - exact).abs() <= 4 * 2.0 ** -24 * exact.abs() + 1e-44).all()
+
+
+@pytest.mark.parametrize("opt", [dict(), dict(max_norm=0.05), dict(moments="8bit", master=False, max_norm=0.05)])
+def test_captured_steps_are_the_eager_ones(opt):
+    need_gpu()
+    print("training step", opt, flush=True)
+    _, db, dc, do = build(**opt)
+    _, db2, dc2, do2 = build(**opt)
+    assert same(state(db, dc, do)[-4:], state(db2, dc2, do2)[-4:])
+    start = [x.clone() for x in state(db, dc, do)]
+    dc.train_step(db, do)  # warm-up outside the capture
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        dc.train_step(db, do)
+    for x, s in zip(state(db, dc, do), start):
+        x.copy_(s)
+    for i in range(4):
+        if i == 2:
+            do.set_lr(5e-3)
+            do2.set_lr(5e-3)
+        graph.replay()
+        dc2.train_step(db2, do2)  # eager work between the replays
+        torch.cuda.synchronize()
+        assert same(state(db, dc, do), state(db2, dc2, do2)), "replay %d" % i
+    assert int(do.steps) == 4
+    assert not torch.equal(start[0], dc.loss)
+
+
+def test_a_step_on_another_stream():
+    need_gpu()
+    _, db, dc, do = build(max_norm=1.0, moments="8bit")
+    _, db2, dc2, do2 = build(max_norm=1.0, moments="8bit")
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    for _ in range(2):
+        dc.train_step(db, do)
+        dc2.train_step(db2, do2, side)
+    torch.cuda.synchronize()
+    assert same(state(db, dc, do), state(db2, dc2, do2))
+
+
+def test_a_gradient_that_is_not_finite_changes_nothing():
+    need_gpu()
+    _, db, dc, do = build(max_norm=1.0)
+    dc.train_step(db, do)
+    before = [t[k].clone() for t in do.tensors for k in ("param", "m", "v")]
+    dc.grad_w[3, 5] = float("nan")
+    do.update()
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(before, [t[k] for t in do.tensors for k in ("param", "m", "v")]))
+    assert db.lib.check_device_errors() == rdcn.RDCN_OK
