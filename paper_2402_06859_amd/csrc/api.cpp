@@ -477,12 +477,12 @@ hipError_t soft_product(rdcn_handle* h, int kind, GemmArgs g, const float* acc_i
     return launch_soft_reduce(splitk, p.splits, n, acc_in, last ? nullptr : acc, out, h->bf16, s);
 }
 
-// The logits product and the join of its pairs; e != NULL also keeps the exponentials (row stride ld), factor != NULL
-// also the rows' gradient factors and the rows of x that have a label.
+// The logits product and the join of its pairs. With `G` (S.whole) its exponentials are kept there and become the
+// gradient in the logits; with `factor` the rows' gradient factors go out, and to `kept` the rows of x that have a label.
 rdcn_status soft_forward(rdcn_handle* h, const SoftPlan& S, int64_t rows, int64_t dim, int64_t classes, const void* x,
                          const void* w, const float* offset, const void* labels, float logit_scale,
-                         const float* row_weight, float scale, float* loss, float* lse, char* sc, void* e, int64_t ld,
-                         float* factor, void* kept, hipStream_t s) {
+                         const float* row_weight, float scale, float* loss, float* lse, char* sc, void* G, float* factor,
+                         void* kept, hipStream_t s) {
     GemmArgs g{};
     g.M = rows; g.N = classes; g.K = dim;
     g.a = x; g.lda = dim;
@@ -492,7 +492,7 @@ rdcn_status soft_forward(rdcn_handle* h, const SoftPlan& S, int64_t rows, int64_
     g.labels = labels; g.labels64 = h->ids64;
     g.zlabel = (float*)(sc + S.zlabel);
     g.softpart = (float2*)(sc + S.part);
-    g.c = e; g.ldc = ld;
+    g.c = G; g.ldc = S.ld;
     {
         ProfScope ps(h, RDCN_KERNEL_HEAD_FWD_GEMM, s);
         RDCN_TRY(launch_gemm(g, plan_logits(h, rows, classes, dim), h->bf16, s));
@@ -505,8 +505,21 @@ rdcn_status soft_forward(rdcn_handle* h, const SoftPlan& S, int64_t rows, int64_
     r.loss = loss; r.lse = lse; r.factor = factor;
     r.err = h->err;
     r.x = x; r.kept = kept; r.dim = dim;
-    ProfScope ps(h, RDCN_KERNEL_HEAD_LOSS, s);
-    return hip_status(launch_soft_rows(r, h->bf16, s));
+    SoftNorm n{};
+    n.rows = rows; n.classes = classes; n.ld = S.ld; n.tile = S.tile;
+    n.softpart = g.softpart; n.zlabel = g.zlabel;
+    n.lse = lse; n.factor = factor;
+    n.labels = labels; n.labels64 = h->ids64;
+    n.e = G;
+    const bool at_once = G && soft_row_at_once(rows, S.tiles, S.ld);
+    {
+        ProfScope ps(h, RDCN_KERNEL_HEAD_LOSS, s);
+        if (at_once) RDCN_TRY(launch_soft_row(r, n, h->bf16, s));
+        else RDCN_TRY(launch_soft_rows(r, h->bf16, s));
+    }
+    if (!G || at_once) return RDCN_OK;
+    ProfScope ps(h, RDCN_KERNEL_HEAD_OUT_BWD, s);
+    return hip_status(launch_soft_normalize(n, h->bf16, s));
 }
 
 // ---------------------------------------------------------------------------
@@ -1309,7 +1322,7 @@ rdcn_status rdcn_softmax_loss_forward(rdcn_handle* h, int64_t rows, int64_t dim,
     const SoftPlan S = soft_layout(h, rows, dim, classes, true, classes);
     if (!scratch || !aligned256(scratch) || scratch_bytes < S.forward_total) return RDCN_ERR_WORKSPACE;
     return soft_forward(h, S, rows, dim, classes, x, w, offset, labels, logit_scale, nullptr, 0.0f, loss, lse,
-                        (char*)scratch, nullptr, 0, nullptr, nullptr, (hipStream_t)stream);
+                        (char*)scratch, nullptr, nullptr, nullptr, (hipStream_t)stream);
 }
 
 rdcn_status rdcn_softmax_loss_grad(rdcn_handle* h, int64_t rows, int64_t dim, int64_t classes, const void* x,
@@ -1334,19 +1347,8 @@ rdcn_status rdcn_softmax_loss_grad(rdcn_handle* h, int64_t rows, int64_t dim, in
     char* const G = sc + S.G;
     // the gradient of the logits carries the logits' own scale
     if ((st = soft_forward(h, S, rows, dim, classes, x, w, offset, labels, logit_scale, row_weight, scale * logit_scale,
-                           loss, lse, sc, S.whole ? G : nullptr, S.ld, factor, sc + S.kept, s)) != RDCN_OK)
+                           loss, lse, sc, S.whole ? G : nullptr, factor, sc + S.kept, s)) != RDCN_OK)
         return st;
-    if (S.whole) {
-        SoftNorm n{};
-        n.rows = rows; n.classes = classes; n.ld = S.ld; n.tile = S.tile;
-        n.softpart = (const float2*)(sc + S.part);
-        n.zlabel = (const float*)(sc + S.zlabel);
-        n.lse = lse; n.factor = factor;
-        n.labels = labels; n.labels64 = h->ids64;
-        n.e = G;
-        ProfScope ps(h, RDCN_KERNEL_HEAD_OUT_BWD, s);
-        RDCN_TRY(launch_soft_normalize(n, h->bf16, s));
-    }
     for (int64_t v = 0; v < classes; v += S.piece) {
         const int64_t n = std::min(S.piece, classes - v);
         const void* const wp = (const char*)w + (size_t)v * dim * e;

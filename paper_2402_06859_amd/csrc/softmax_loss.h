@@ -41,6 +41,9 @@ struct SoftNorm {
     void* e;
 };
 hipError_t launch_soft_normalize(const SoftNorm& a, bool bf16, hipStream_t s);
+// launch_soft_rows (with factor) and launch_soft_normalize in one, where soft_row_at_once says so.
+bool soft_row_at_once(int64_t rows, int64_t tiles, int64_t ld);
+hipError_t launch_soft_row(const SoftRows& a, const SoftNorm& n, bool bf16, hipStream_t s);
 
 // sum over `splits` planes of part (n floats each, in plane order), added to acc if it is not NULL;
 // written to acc_out (float) or, if that is NULL, to out (storage type). n is a multiple of 4.

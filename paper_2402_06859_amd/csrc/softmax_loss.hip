@@ -51,6 +51,24 @@ __device__ __forceinline__ void copy_kept_rows(const SoftRows& a, int64_t first)
     }
 }
 
+// Row m's lse (x) and gradient factor (y) from its maximum and sum; `write`: they and the loss go out.
+__device__ __forceinline__ float2 finish_row(const SoftRows& a, int64_t m, float mx, float sum, bool write) {
+    const float lse = mx == NEG_INF && sum == 0.f ? NEG_INF : mx + logf(sum);
+    const int64_t y = label_of(a.labels, a.labels64, m);
+    const bool kept = y >= 0 && y < a.classes;
+    const float f = a.factor && kept ? a.scale * (a.row_weight ? a.row_weight[m] : 1.f) : 0.f;
+    if (write) {
+        if (y >= a.classes) atomicOr(a.err, ERR_BIT_INDEX);
+        a.lse[m] = lse;
+        // a label whose own class is masked has probability 0: its loss is +inf, also where every class is
+        float loss = 0.f;
+        if (kept) loss = a.zlabel[m] == NEG_INF ? -NEG_INF : lse - a.zlabel[m];
+        a.loss[m] = loss;
+        if (a.factor) a.factor[m] = f;
+    }
+    return make_float2(lse, f);
+}
+
 // 256 threads as rpb rows x (256 / rpb) lanes that stride over the tiles. Few rows take many
 // lanes each (one request over 50000 classes has 782 pairs to join), many rows one lane or few.
 template <typename T>
@@ -82,29 +100,17 @@ __global__ __launch_bounds__(256) void k_soft_rows(SoftRows a, int rpb) {
         }
     }
     if (part != 0 || m >= a.rows) return;
-    const float lse = mx == NEG_INF && sum == 0.f ? NEG_INF : mx + logf(sum);
-    const int64_t y = label_of(a.labels, a.labels64, m);
-    const bool kept = y >= 0 && y < a.classes;
-    if (y >= a.classes) atomicOr(a.err, ERR_BIT_INDEX);
-    a.lse[m] = lse;
-    // a label whose own class is masked has probability 0: its loss is +inf, also where every class is
-    float loss = 0.f;
-    if (kept) loss = a.zlabel[m] == NEG_INF ? -NEG_INF : lse - a.zlabel[m];
-    a.loss[m] = loss;
-    if (a.factor) a.factor[m] = kept ? a.scale * (a.row_weight ? a.row_weight[m] : 1.f) : 0.f;
+    (void)finish_row(a, m, mx, sum, true);
 }
 
-// One workgroup per (row, stretch of columns). Reads and writes each element once (2 + 2 bytes); the
-// factor exp(tile's maximum - lse) f is one exponential per tile and row, not per element. The label's
+// Columns first, first + step, .. (vectors) of row m of E -> G. Reads and writes each element once (2 + 2 bytes, 4 + 4
+// in float); the factor exp(tile's maximum - lse) f is one exponential per vector, not per element. The label's
 // own element is taken from z itself, so p - 1 keeps its digits where p is close to 1.
 template <typename T>
-__global__ __launch_bounds__(256) void k_soft_normalize(SoftNorm a) {
+__device__ __forceinline__ void normalize_row(const SoftNorm& a, int64_t m, float lse, float f, int64_t y, int64_t first,
+                                              int64_t step) {
     constexpr int W = st<T>::vec;
-    const int64_t m = blockIdx.y + (int64_t)blockIdx.z * 65535;
-    if (m >= a.rows) return;
-    const float lse = a.lse[m], f = a.factor[m];
-    const int64_t y = label_of(a.labels, a.labels64, m);
-    for (int64_t n = ((int64_t)blockIdx.x * 256 + threadIdx.x) * W; n < a.ld; n += (int64_t)gridDim.x * 256 * W) {
+    for (int64_t n = first * W; n < a.ld; n += step * W) {
         const float top = a.softpart[n / a.tile * a.rows + m].x;
         float v[W];
         if constexpr (sizeof(T) == 2) unpack_f16x8(*(const u32x4_t*)((const _Float16*)a.e + m * a.ld + n), v);
@@ -120,6 +126,48 @@ __global__ __launch_bounds__(256) void k_soft_normalize(SoftNorm a) {
                 if (y - n == e) v[e] = z == NEG_INF ? 0.f : f * expm1f(z - lse);
         }
         *(u32x4_t*)((T*)a.e + m * a.ld + n) = st<T>::pack(v);
+    }
+}
+
+// One workgroup per (row, stretch of columns).
+template <typename T>
+__global__ __launch_bounds__(256) void k_soft_normalize(SoftNorm a) {
+    const int64_t m = blockIdx.y + (int64_t)blockIdx.z * 65535;
+    if (m >= a.rows) return;
+    normalize_row<T>(a, m, a.lse[m], a.factor[m], label_of(a.labels, a.labels64, m), blockIdx.x * 256ll + threadIdx.x,
+                     gridDim.x * 256ll);
+}
+
+// The join, G's row and the kept row of x in one workgroup per row: a launch less where its pairs are few.
+template <typename T>
+__global__ __launch_bounds__(256) void k_soft_row(SoftRows a, SoftNorm b) {
+    __shared__ float2 sh[4];
+    const int64_t m = blockIdx.x;
+    float mx = NEG_INF, sum = 0.f;
+    for (int64_t t = threadIdx.x; t < a.tiles; t += 256) {
+        const float2 p[1] = {a.softpart[t * a.rows + m]};
+        join(mx, sum, p);
+    }
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) {
+        const float2 p[1] = {make_float2(__shfl_xor(mx, o), __shfl_xor(sum, o))};
+        join(mx, sum, p);
+    }
+    if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = make_float2(mx, sum);
+    __syncthreads();
+    const float2 p[4] = {sh[0], sh[1], sh[2], sh[3]};
+    mx = NEG_INF;
+    sum = 0.f;
+    join(mx, sum, p);
+    const float2 r = finish_row(a, m, mx, sum, threadIdx.x == 0);
+    const int64_t y = label_of(a.labels, a.labels64, m);
+    normalize_row<T>(b, m, r.x, r.y, y, threadIdx.x, 256);
+    constexpr int W = st<T>::vec;
+    const bool kept = y >= 0 && y < a.classes;
+    for (int64_t i = threadIdx.x; i < a.dim / W; i += 256) {
+        u32x4_t v = {0u, 0u, 0u, 0u};
+        if (kept) v = *(const u32x4_t*)((const T*)a.x + m * a.dim + i * W);
+        *(u32x4_t*)((T*)a.kept + m * a.dim + i * W) = v;
     }
 }
 
@@ -155,6 +203,19 @@ hipError_t launch_soft_rows(const SoftRows& a, bool bf16, hipStream_t s) {
     const unsigned ncopy = a.factor ? blocks_for(a.rows * a.dim / (bf16 ? 8 : 4), 4096).x : 0;
     if (bf16) hipLaunchKernelGGL(k_soft_rows<bf16_t>, dim3(nrow + ncopy), dim3(256), 0, s, a, rpb);
     else hipLaunchKernelGGL(k_soft_rows<float>, dim3(nrow + ncopy), dim3(256), 0, s, a, rpb);
+    return hipGetLastError();
+}
+
+bool soft_row_at_once(int64_t rows, int64_t tiles, int64_t ld) {
+    // a workgroup per row has to fill the chip, unless rows are short; pairs of one row lie far apart (us, at once / apart:
+    // 157 pairs of 512 rows 8.4 / 11, 500 of 4096 132 / 105)
+    return tiles <= 192 && (rows >= 256 || ld <= 8192);
+}
+
+hipError_t launch_soft_row(const SoftRows& a, const SoftNorm& n, bool bf16, hipStream_t s) {
+    if (a.rows == 0) return hipSuccess;
+    if (bf16) hipLaunchKernelGGL(k_soft_row<bf16_t>, dim3((unsigned)a.rows), dim3(256), 0, s, a, n);
+    else hipLaunchKernelGGL(k_soft_row<float>, dim3((unsigned)a.rows), dim3(256), 0, s, a, n);
     return hipGetLastError();
 }
 
