@@ -193,7 +193,7 @@ __device__ __forceinline__ void adamw_elements(const AdamwTensor& t, const Adamw
     uint32_t h[EPT];
     if (a.stochastic && (EIGHT || (pbf && !t.master))) {
 #pragma unroll
-        for (int e = 0; e < EPT; ++e) h[e] = fmix32((uint32_t)(at + e) ^ k.key);
+        for (int e = 0; e < EPT; ++e) h[e] = fmix32(((uint32_t)at ^ k.key) ^ (uint32_t)e);  // (at is a multiple of EPT)
     }
     if (t.master) store_f32<WHOLE>(t.master + at, left, p);
     if (!pbf) {
@@ -230,7 +230,7 @@ __device__ __forceinline__ void adamw_elements(const AdamwTensor& t, const Adamw
             mv = max(mv, uv[e]);
         }
         const uint32_t em = max_of_block(mm) >> 23, ev = max_of_block(mv) >> 23;
-        const uint32_t bm = code_base(em, 127) << 20, bv = code_base(ev, 255) << 20;
+        const uint32_t bm = 0u - (code_base(em, 127) << 20), bv = 0u - (code_base(ev, 255) << 20);
         uint32_t cm[EPT], cv[EPT];
 #pragma unroll
         for (int e = 0; e < EPT; ++e) {
@@ -238,7 +238,7 @@ __device__ __forceinline__ void adamw_elements(const AdamwTensor& t, const Adamw
             const uint32_t rv = a.stochastic ? (h[e] * 0x9E3779B1u) >> 12 : 0x80000u;
             // (a value of the block is at most 8 2^20 above its exponent's base + top: the differences fit an int; of a
             // zero and what lies below the reach they are negative or round to 0)
-            const int x = (int)(um[e] + rm - bm) >> 20, y = (int)(uv[e] + rv - bv) >> 20;
+            const int x = (int)(um[e] + rm + bm) >> 20, y = (int)(uv[e] + rv + bv) >> 20;
             cm[e] = (uint32_t)min(max(x, 0), 127) | (__float_as_uint(m[e]) >> 24 & 128u);
             cv[e] = (uint32_t)min(max(y, (int)min(uv[e], 1u)), 255);
         }
