@@ -495,7 +495,7 @@ rdcn_status rdcn_head_backward(rdcn_handle* h, int64_t batch, const void* x, con
  *   - w has to be finite, in masked classes too: their zero probabilities are
  *     still multiplied with it.
  * dim is a multiple of 8 (bf16 models) or 4 (float); rows <= 2^24, classes <=
- * 2^27, dim <= 2^20, rows * classes <= 2^44, else RDCN_ERR_UNSUPPORTED. x, w, grad_x and
+ * 2^27, dim <= 2^20, rows * classes <= 2^42, else RDCN_ERR_UNSUPPORTED. x, w, grad_x and
  * grad_w must be 16-byte aligned (RDCN_ERR_ARG otherwise); rows may be 0 (the
  * forward then does nothing, the gradient sets grad_w to 0).
  */
@@ -512,7 +512,8 @@ rdcn_status rdcn_softmax_loss_forward(rdcn_handle* h, int64_t rows, int64_t dim,
 
 /*
  * Loss, lse and the gradients of  sum_n scale * row_weight[n] * loss[n]
- * (row_weight [rows] float, or NULL for 1; scale = 1/rows gives a mean loss):
+ * (row_weight [rows] float, or NULL for 1; scale = 1/rows gives a mean loss; the x of
+ * a row of weight 0 may hold anything, like that of a row without a label):
  * grad_x [rows, dim] and grad_w [classes, dim], both in the storage dtype and
  * overwritten. With p = softmax(z) and G = scale * weight * logit_scale * (p - onehot):
  * grad_x = G w, grad_w = G^T x. bf16 models round G to bf16 for the matrix

@@ -442,7 +442,7 @@ rdcn_status check_soft(const rdcn_handle* h, int64_t rows, int64_t dim, int64_t 
     if (!h || rows < 0 || dim <= 0 || classes <= 0) return RDCN_ERR_ARG;
     if (dim % (h->bf16 ? 8 : 4)) return RDCN_ERR_UNSUPPORTED;
     if (rows > ((int64_t)1 << 24) || dim > ((int64_t)1 << 20) || classes > ((int64_t)1 << 27) ||
-        rows * classes > (int64_t)1 << 44)
+        rows * classes > (int64_t)1 << 42)  // 64 x 64 blocks stay below 2^31
         return RDCN_ERR_UNSUPPORTED;
     return RDCN_OK;
 }

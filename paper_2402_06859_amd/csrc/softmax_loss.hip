@@ -36,17 +36,20 @@ __device__ __forceinline__ void join(float& mx, float& sum, const float2 (&p)[N]
     sum = s;
 }
 
-// A row without a label may hold anything (padding behind a sequence, infinities, NaN): its
+// A row without a label, or of weight 0, may hold anything (padding behind a sequence, infinities, NaN): its
 // gradient factor is 0, but 0 times such a value would still reach grad_w's sum over the rows. So the product
 // for grad_w reads a copy of x with zeros there, made by the workgroups from `first` on.
+__device__ __forceinline__ bool row_counts(const SoftRows& a, int64_t m) {
+    const int64_t y = label_of(a.labels, a.labels64, m);
+    return y >= 0 && y < a.classes && !(a.row_weight && a.row_weight[m] == 0.f);
+}
 template <typename T>
 __device__ __forceinline__ void copy_kept_rows(const SoftRows& a, int64_t first) {
     constexpr int W = st<T>::vec;
     const int64_t per = a.dim / W, n = a.rows * per, step = (gridDim.x - first) * 256ll;
     for (int64_t i = (blockIdx.x - first) * 256ll + threadIdx.x; i < n; i += step) {
-        const int64_t y = label_of(a.labels, a.labels64, i / per);
         u32x4_t v = {0u, 0u, 0u, 0u};
-        if (y >= 0 && y < a.classes) v = *(const u32x4_t*)((const T*)a.x + i * W);
+        if (row_counts(a, i / per)) v = *(const u32x4_t*)((const T*)a.x + i * W);
         *(u32x4_t*)((T*)a.kept + i * W) = v;
     }
 }
@@ -163,7 +166,7 @@ __global__ __launch_bounds__(256) void k_soft_row(SoftRows a, SoftNorm b) {
     const int64_t y = label_of(a.labels, a.labels64, m);
     normalize_row<T>(b, m, r.x, r.y, y, threadIdx.x, 256);
     constexpr int W = st<T>::vec;
-    const bool kept = y >= 0 && y < a.classes;
+    const bool kept = row_counts(a, m);
     for (int64_t i = threadIdx.x; i < a.dim / W; i += 256) {
         u32x4_t v = {0u, 0u, 0u, 0u};
         if (kept) v = *(const u32x4_t*)((const T*)a.x + m * a.dim + i * W);

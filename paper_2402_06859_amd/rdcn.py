@@ -88,6 +88,15 @@ def adamw_tensors(tensors: Sequence[dict]):
     keeps the tensors alive."""
     out = (RdcnAdamwTensor * len(tensors))()
     for d, t in zip(out, tensors):
+        n = t["param"].numel()
+        for k in ("param", "master", "grad", "m", "v"):
+            x = t.get(k)
+            if x is not None and (x.numel() != n or not x.is_contiguous()):
+                raise ValueError("adamw_tensors: %s must be contiguous, of as many elements as param" % k)
+        if t["m"].dtype != t["v"].dtype or t["m"].dtype not in (torch.uint8, torch.float32):
+            raise ValueError("adamw_tensors: m and v are both float32 or both uint8")
+        if t["m"].dtype == torch.uint8 and t["exps"].numel() < 2 * -(-n // 256):
+            raise ValueError("adamw_tensors: exps holds two exponents per 256 elements")
         for k in ("param", "master", "grad", "m", "v", "exps"):
             x = t.get(k)
             setattr(d, k, None if x is None else x.data_ptr())

@@ -463,7 +463,7 @@ def test_refusals():
     A, S, W, OK = rdcn.RDCN_ERR_ARG, rdcn.RDCN_ERR_UNSUPPORTED, rdcn.RDCN_ERR_WORKSPACE, rdcn.RDCN_OK
 
     def step(count=1, cfg=None, **kw):
-        lst = rdcn.adamw_tensors([t, dict(t, param=t["param"][256:], grad=t["grad"][256:])][:max(1, count)])
+        lst = rdcn.adamw_tensors([t, {k: x[256:] for k, x in t.items()}][:max(1, count)])
         for k, v in kw.items():
             setattr(lst[0], k, v)
         c = rdcn.RdcnAdamwConfig(1e-3, 0.9, 0.999, 1e-8, 1.0, 1, None, None, None, 0, 0)

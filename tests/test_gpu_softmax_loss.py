@@ -135,7 +135,8 @@ def check(lib, c, rows, dim, classes, f32):
 
 SIZES = [(1, 8, 1), (1, 8, 3), (2, 16, 8), (1, 64, 1000), (7, 136, 9), (9, 24, 4097), (33, 72, 257), (50, 1856, 1003),
          (64, 512, 4096), (129, 160, 2049), (257, 264, 777), (300, 512, 8197), (1000, 64, 33), (1025, 8, 40),
-         (2000, 256, 5003), (5, 4352, 130), (4096, 64, 4), (600, 1024, 9000)]
+         (2000, 256, 5003), (5, 4352, 130), (4096, 64, 4), (600, 1024, 9000),
+         (1024, 1024, 2700), (4096, 1024, 2000), (2000, 1024, 20003), (40, 1856, 40001)]
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
@@ -159,11 +160,29 @@ def test_masks_padding_rows_and_weights(dtype, id_type, rows, dim, classes):
     c["y"][-1] = -7
     c["x"][c["y"] < 0] = math.nan          # padding rows may hold anything
     c["x"][-1] = math.inf
+    c["x"][0] = -math.inf                  # a row of weight 0 too (its loss is what its x makes of it)
+    c["y"][0] = -1
     got = check(lib, c, rows, dim, classes, dtype == "f32")
     pad = c["y"] < 0
     assert (got[0][pad] == 0).all() and (got[2][pad] == 0).all()
     assert (got[3][torch.isneginf(c["off"])] == 0).all()
     assert lib.check_device_errors() == rdcn.RDCN_OK
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,dim,classes", [(20, 32, 300), (300, 64, 9000)])
+def test_rows_of_weight_zero_add_nothing(dtype, rows, dim, classes):
+    need_gpu()
+    lib = handle(dtype)
+    c = make(dtype, rows, dim, classes, 19, weights=True)
+    clean = call_grad(lib, c, rows, dim, classes)
+    c["wt"][7] = 0.0
+    c["x"][0], c["x"][7] = math.nan, math.inf
+    got = call_grad(lib, c, rows, dim, classes)
+    assert (got[2][0] == 0).all() and (got[2][7] == 0).all() and torch.isfinite(got[3].float()).all()
+    c["x"][0], c["x"][7] = 0.0, 0.0
+    assert torch.equal(call_grad(lib, c, rows, dim, classes)[3], got[3])
+    assert torch.equal(clean[2][1:7], got[2][1:7])
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
@@ -212,7 +231,8 @@ def call_grad_within(lib, c, rows, dim, classes, size):
 
 
 @pytest.mark.parametrize("dtype,rows,dim,classes", [("bf16", 300, 264, 5003), ("f32", 130, 68, 3075), ("bf16", 2000, 64, 9000),
-                                                    ("bf16", 1100, 512, 33001)])
+                                                    ("bf16", 1100, 512, 33001), ("bf16", 4096, 1024, 4099),
+                                                    ("bf16", 1280, 1024, 4100)])
 def test_less_scratch_means_pieces_of_the_classes(dtype, rows, dim, classes):
     need_gpu()
     print("softmax loss in pieces", dtype, rows, dim, classes, flush=True)

@@ -3,6 +3,9 @@ import ctypes
 import os
 import subprocess
 
+import pytest
+import torch
+
 from paper_2402_06859_amd import rdcn
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
@@ -37,3 +40,20 @@ def test_null_handles_are_refused():
     assert L.rdcn_adamw_values(None, 1, None, None, 0, None, None) == A
     assert L.rdcn_grad_norm_workspace(None, lst, 1, ctypes.byref(s)) == A
     assert L.rdcn_grad_norm(None, lst, 1, 1.0, 1.0, None, None, 0, None) == A
+
+
+def test_descriptors_check_their_tensors():
+    def t(**kw):
+        d = {k: torch.zeros(600) for k in ("param", "grad", "m", "v")}
+        d.update(kw)
+        return d
+
+    lst = rdcn.adamw_tensors([t(), t(weight_decay=0.5, m=torch.zeros(600, dtype=torch.uint8), v=torch.zeros(600, dtype=torch.uint8),
+                                     exps=torch.zeros(6, dtype=torch.uint8))])
+    assert [x.n for x in lst] == [600, 600] and lst[1].weight_decay == 0.5 and [x.moments for x in lst] == [0, 1]
+    for bad in (t(grad=torch.zeros(599)), t(m=torch.zeros(600, dtype=torch.uint8)), t(v=torch.zeros(601)),
+                t(param=torch.zeros(1200)[::2]), t(master=torch.zeros(1)),
+                t(m=torch.zeros(600, dtype=torch.uint8), v=torch.zeros(600, dtype=torch.uint8),
+                  exps=torch.zeros(5, dtype=torch.uint8))):
+        with pytest.raises(ValueError):
+            rdcn.adamw_tensors([bad])
