@@ -1693,7 +1693,7 @@ GemmPlan plan_gemm_long(int64_t M, int64_t N, int64_t K, bool bf16) {
     if (!bf16) {
         GemmPlan p = plan_f32_lds();
         const int64_t t = ((M + 63) / 64) * ((N + 63) / 64);
-        const int64_t sp = std::min<int64_t>({t < 512 ? 512 / t : 1, K / 256, 16});
+        const int64_t sp = std::min<int64_t>({t < 512 ? 512 / t : 1, K / 256, K < 16384 ? 16 : K / 1024, 64});
         p.splits = (int)(sp < 1 ? 1 : sp);
         return p;
     }
@@ -1701,8 +1701,9 @@ GemmPlan plan_gemm_long(int64_t M, int64_t N, int64_t K, bool bf16) {
     const int64_t t64 = ((M + 63) / 64) * ((N + 63) / 64);
     if (p.bm == 64 && t64 < 128 && K >= 768) {
         // few blocks of a long K each: split it down to 128, past plan_gemm's 512 (gradient pass of 333 x 136 x 1001, 18
-        // blocks: 33.0 -> 29.7 us)
-        const int64_t sp = std::min<int64_t>({256 / t64, K / 128, 16});
+        // blocks: 33.0 -> 29.7 us), and in up to 64 ranges of 1024 (55 x 112 x 107466, 2 blocks: 86.6
+        // -> 61.7)
+        const int64_t sp = std::min<int64_t>({256 / t64, K / 128, K < 16384 ? 16 : K / 1024, 64});
         if (sp > p.splits) p.splits = (int)sp;
     }
     if ((double)M * (double)N * (double)K < 8.0e9 || M < 8 || N < 8 || (M > N ? M : N) >= 1500000) return p;

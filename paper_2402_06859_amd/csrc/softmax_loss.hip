@@ -174,12 +174,30 @@ __global__ __launch_bounds__(256) void k_soft_row(SoftRows a, SoftNorm b) {
     }
 }
 
-template <typename T>
+// LANES > 1: that many groups of a workgroup's threads take every LANES-th plane of the same outputs, and their sums are
+// added in group order (few outputs with many planes: a serial chain of loads otherwise).
+template <typename T, int LANES>
 __global__ __launch_bounds__(256) void k_soft_reduce(const float* part, int splits, int64_t n, const float* acc,
                                                      float* acc_out, T* out) {
-    for (int64_t i = (blockIdx.x * 256ll + threadIdx.x) * 4; i < n; i += gridDim.x * 1024ll) {
-        f32x4_t v = *(const f32x4_t*)(part + i);
-        for (int z = 1; z < splits; ++z) v += *(const f32x4_t*)(part + z * n + i);
+    constexpr int PER = 256 / LANES;  // threads of a group
+    __shared__ f32x4_t sh[LANES > 1 ? 256 : 1];
+    const int lane = threadIdx.x / PER;
+    for (int64_t i0 = (int64_t)blockIdx.x * PER * 4; i0 < n; i0 += (int64_t)gridDim.x * PER * 4) {
+        const int64_t i = i0 + threadIdx.x % PER * 4;
+        f32x4_t v = {0.f, 0.f, 0.f, 0.f};
+        if (i < n) {
+#pragma unroll 4
+            for (int z = lane; z < splits; z += LANES) v += *(const f32x4_t*)(part + z * n + i);
+        }
+        if constexpr (LANES > 1) {
+            __syncthreads();
+            sh[threadIdx.x] = v;
+            __syncthreads();
+            if (lane != 0) continue;
+#pragma unroll
+            for (int k = 1; k < LANES; ++k) v += sh[threadIdx.x + k * PER];
+        }
+        if (i >= n) continue;
         if (acc) v += *(const f32x4_t*)(acc + i);
         if (acc_out) {
             *(f32x4_t*)(acc_out + i) = v;
@@ -235,9 +253,15 @@ hipError_t launch_soft_normalize(const SoftNorm& a, bool bf16, hipStream_t s) {
 hipError_t launch_soft_reduce(const float* part, int splits, int64_t n, const float* acc, float* acc_out, void* out,
                               bool bf16, hipStream_t s) {
     if (n == 0) return hipSuccess;
-    const dim3 grid = blocks_for(n / 4, 4096);
-    if (bf16) hipLaunchKernelGGL(k_soft_reduce<bf16_t>, grid, dim3(256), 0, s, part, splits, n, acc, acc_out, (bf16_t*)out);
-    else hipLaunchKernelGGL(k_soft_reduce<float>, grid, dim3(256), 0, s, part, splits, n, acc, acc_out, (float*)out);
+    if (splits > 8 && n / 4 <= 256 * 256) {
+        const dim3 grid = blocks_for(n / 4 * 8, 4096);
+        if (bf16) hipLaunchKernelGGL((k_soft_reduce<bf16_t, 8>), grid, dim3(256), 0, s, part, splits, n, acc, acc_out, (bf16_t*)out);
+        else hipLaunchKernelGGL((k_soft_reduce<float, 8>), grid, dim3(256), 0, s, part, splits, n, acc, acc_out, (float*)out);
+    } else {
+        const dim3 grid = blocks_for(n / 4, 4096);
+        if (bf16) hipLaunchKernelGGL((k_soft_reduce<bf16_t, 1>), grid, dim3(256), 0, s, part, splits, n, acc, acc_out, (bf16_t*)out);
+        else hipLaunchKernelGGL((k_soft_reduce<float, 1>), grid, dim3(256), 0, s, part, splits, n, acc, acc_out, (float*)out);
+    }
     return hipGetLastError();
 }
 
