@@ -870,9 +870,9 @@ __device__ __forceinline__ void block_epilogue(const GemmArgs& g, int64_t m0, in
 
 // Softmax loss epilogue of a BM x BN block, from the accumulators: a lane holds one row of each of its tiles
 // (layout above), so a row's maximum and sum over the BN / WN columns of a wave are the lane's own values and one
-// or two exchanges between lanes, and no wave waits for another; a (maximum, sum) pair covers a wave's columns. Exponentials cost one fma and one v_exp_f32 each. (Through LDS like the other
-// epilogues, 64 rows at a time, a forward of 4096 x 32000 x 1856 took 514 us, so 419; a library product of these
-// sizes takes 405.)
+// or two exchanges between lanes, and no wave waits for another; a (maximum, sum) pair covers a wave's columns. z itself
+// never reaches memory. (Through LDS like the other epilogues, 64 rows at a time, a forward of 4096 x 32000 x 1856
+// took 514 us, so 406; a library product of these sizes takes 405.)
 template <typename T, bool GRAD, int BM, int BN, int WM, int WN, bool M32, typename Acc, int TM, int TN>
 __device__ __forceinline__ void soft_block_epilogue(const GemmArgs& g, int64_t m0, int64_t n0, Acc (&acc)[TM][TN], int tid,
                                                     uint32_t* stage) {
