@@ -1331,7 +1331,7 @@ rdcn_status rdcn_softmax_loss_grad(rdcn_handle* h, int64_t rows, int64_t dim, in
                                    void* grad_w, void* scratch, size_t scratch_bytes, void* stream) {
     rdcn_status st = check_soft(h, rows, dim, classes);
     if (st != RDCN_OK) return st;
-    if (!std::isfinite(logit_scale) || !std::isfinite(scale)) return RDCN_ERR_ARG;
+    if (!std::isfinite(logit_scale) || !std::isfinite(scale) || !std::isfinite(scale * logit_scale)) return RDCN_ERR_ARG;
     if (!w || !a16(w) || !grad_w || !a16(grad_w)) return RDCN_ERR_ARG;
     hipStream_t s = (hipStream_t)stream;
     const size_t e = eb(h);
@@ -1411,8 +1411,8 @@ rdcn_status rdcn_adamw_step(rdcn_handle* h, const rdcn_adamw_config* cfg, const 
                             void* stream) {
     if (!h || !cfg) return RDCN_ERR_ARG;
     const rdcn_adamw_config& c = *cfg;
-    if (!std::isfinite(c.lr) || !(c.beta1 >= 0.0 && c.beta1 < 1.0) || !(c.beta2 >= 0.0 && c.beta2 < 1.0) ||
-        !((float)c.eps >= FLT_MIN) || !std::isfinite(c.eps) || !std::isfinite(c.grad_scale) ||
+    if (!std::isfinite((float)c.lr) || !(c.beta1 >= 0.0 && c.beta1 < 1.0) || !(c.beta2 >= 0.0 && c.beta2 < 1.0) ||
+        !((float)c.eps >= FLT_MIN) || !std::isfinite((float)c.eps) || !std::isfinite((float)c.grad_scale) ||
         (!c.device_step && c.step < 1) || (c.stochastic != 0 && c.stochastic != 1))
         return RDCN_ERR_ARG;
     rdcn_status st = check_tensors(h, tensors, count);

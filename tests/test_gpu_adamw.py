@@ -480,7 +480,7 @@ def test_refusals():
     assert step(moments=1) == A                                    # 8 bits without exponents
     assert step(moments=2) == A and step(param_dtype=2) == A and step(grad_dtype=-1) == A and step(reserved=1) == A
     assert step(n=-1) == A and step(n=(1 << 36) + 1) == S and step(weight_decay=math.nan) == A
-    for bad in (dict(lr=math.inf), dict(beta1=1.0), dict(beta1=-0.1), dict(beta2=math.nan), dict(eps=0.0), dict(eps=1e-39),
+    for bad in (dict(lr=math.inf), dict(lr=1e39), dict(grad_scale=1e40), dict(eps=1e39), dict(beta1=1.0), dict(beta1=-0.1), dict(beta2=math.nan), dict(eps=0.0), dict(eps=1e-39),
                 dict(grad_scale=math.nan), dict(step=0), dict(stochastic=2)):
         assert step(cfg=bad) == A, bad
     lst = rdcn.adamw_tensors([t])

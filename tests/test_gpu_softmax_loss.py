@@ -436,7 +436,7 @@ def test_refusals():
     assert fwd(x=None) == A and fwd(w=None) == A and fwd(y=None) == A and fwd(lo=None) == A and fwd(ls=None) == A
     assert fwd(s=math.nan) == A and fwd(xo=2) == A
     assert fwd(scr=None) == W and fwd(scr=P(sc) + 16) == W and fwd(n=need[0] - 1) == W
-    assert grad(scale=math.inf) == A and grad(s=math.inf) == A and grad(a=None) == A and grad(b=None) == A
+    assert grad(scale=math.inf) == A and grad(s=math.inf) == A and grad(scale=1e30, s=1e30) == A and grad(a=None) == A and grad(b=None) == A
     assert grad(n=need[2] - 1) == W and grad(scr=None) == W and grad(scr=P(sc) + 128) == W
     assert fwd() == rdcn.RDCN_OK and grad() == rdcn.RDCN_OK
     torch.cuda.synchronize()
