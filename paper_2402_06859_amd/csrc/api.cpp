@@ -370,7 +370,7 @@ struct SoftPlan {
     int64_t ld;                 // row stride of G
     int64_t tiles;              // column tiles of the forward's product
     int tile;
-    size_t part, zlabel, forward_total, factor, kept, G, acc, splitk, total;
+    size_t part, zlabel, forward_total, factor, kept, G, acc, splitk, splitw, total;
 };
 
 int64_t split_floats(const rdcn_handle* h, int64_t M, int64_t N, int64_t K) {
@@ -412,12 +412,13 @@ SoftPlan soft_layout(const rdcn_handle* h, int64_t rows, int64_t dim, int64_t cl
     s.kept = off; off += al((size_t)rows * dim * e);
     s.G = off; off += al((size_t)rows * s.ld * e);
     s.acc = off; off += classes > s.piece ? al((size_t)rows * dim * 4) : 0;  // grad_x as a sum of several products
-    int64_t split = 0;
+    int64_t split = 0, splitw = 0;
     for (int64_t n : {s.piece, classes % s.piece}) {
         split = std::max(split, split_floats(h, rows, dim, n));
-        split = std::max(split, split_floats(h, n, dim, rows));
+        splitw = std::max(splitw, split_floats(h, n, dim, rows));
     }
     s.splitk = off; off += al((size_t)split * 4);
+    s.splitw = off; off += al((size_t)splitw * 4);
     s.total = off;
     return s;
 }
@@ -447,34 +448,68 @@ rdcn_status check_soft(const rdcn_handle* h, int64_t rows, int64_t dim, int64_t 
     return RDCN_OK;
 }
 
-// One product of the gradient (both K ranges may be split). With acc_in its result is added to that; the
-// sum goes to out (storage type) when `last`, else to acc.
-hipError_t soft_product(rdcn_handle* h, int kind, GemmArgs g, const float* acc_in, float* acc, void* out, bool last,
-                        float* splitk, hipStream_t s) {
-    const GemmPlan p = plan_gemm_long(g.M, g.N, g.K, h->bf16);
-    const int64_t n = g.M * g.N;
+// One product of the gradient on its way: where it goes, and the sum that ends it (splits of K, or a running sum in
+// acc that becomes the output), if it needs one. With acc_in its result is added to that; the sum goes to out (storage type)
+// when `last`, else to acc.
+struct SoftProduct {
+    GemmArgs g;
+    GemmPlan p;
+    SoftSum sum;
+    bool summed;
+};
+
+SoftProduct soft_product(const rdcn_handle* h, GemmArgs g, const float* acc_in, float* acc, void* out, bool last,
+                         float* splitk) {
+    SoftProduct r{};
+    r.p = plan_gemm_long(g.M, g.N, g.K, h->bf16);
     g.scale = 1.0f;
     g.ldc = g.ldx = g.N;
-    if (p.splits > 1) {
+    r.sum.n = g.M * g.N;
+    r.sum.out = out;
+    if (r.p.splits > 1) {
         g.epi = EPI_PARTIAL;
         g.c = splitk;
+        r.summed = true;
+        r.sum.part = splitk;
+        r.sum.splits = r.p.splits;
+        r.sum.acc = acc_in;
+        r.sum.acc_out = last ? nullptr : acc;
     } else if (acc_in) {
         g.epi = EPI_RESID;
         g.gin = acc_in; g.gin_f32 = true;
         g.c = acc;
+        r.summed = last;
+        r.sum.part = acc;
+        r.sum.splits = 1;
     } else {
         g.epi = last ? EPI_STORE : EPI_STORE_F32;
         g.c = last ? out : (void*)acc;
     }
-    {
-        ProfScope ps(h, kind, s);
-        const hipError_t e = launch_gemm(g, p, h->bf16, s);
-        if (e != hipSuccess) return e;
+    r.g = g;
+    return r;
+}
+
+// Both gradients from G: products of few small blocks go in one launch, and so do the sums that end either's.
+hipError_t soft_gradients(rdcn_handle* h, const SoftProduct& x, const SoftProduct& w, hipStream_t s) {
+    hipError_t e;
+    if (gemm_pairs(x.g, x.p, w.g, w.p, h->bf16)) {
+        ProfScope ps(h, RDCN_KERNEL_HEAD_GX_GEMM, s);
+        if ((e = launch_gemm_pair(x.g, x.p, w.g, w.p, h->bf16, s)) != hipSuccess) return e;
+    } else {
+        {
+            ProfScope ps(h, RDCN_KERNEL_HEAD_GX_GEMM, s);
+            if ((e = launch_gemm(x.g, x.p, h->bf16, s)) != hipSuccess) return e;
+        }
+        ProfScope ps(h, RDCN_KERNEL_HEAD_GW_GEMM, s);
+        if ((e = launch_gemm(w.g, w.p, h->bf16, s)) != hipSuccess) return e;
     }
-    if (p.splits == 1 && (!last || !acc_in)) return hipSuccess;
+    SoftSum sums[2];
+    int n = 0;
+    if (x.summed) sums[n++] = x.sum;
+    if (w.summed) sums[n++] = w.sum;
+    if (n == 0) return hipSuccess;
     ProfScope ps(h, RDCN_KERNEL_SPLITK_REDUCE, s);
-    if (p.splits == 1) return launch_soft_reduce(acc, 1, n, nullptr, nullptr, out, h->bf16, s);
-    return launch_soft_reduce(splitk, p.splits, n, acc_in, last ? nullptr : acc, out, h->bf16, s);
+    return launch_soft_reduce(sums, n, h->bf16, s);
 }
 
 // The logits product and the join of its pairs. With `G` (S.whole) its exponentials are kept there and become the
@@ -1370,14 +1405,14 @@ rdcn_status rdcn_softmax_loss_grad(rdcn_handle* h, int64_t rows, int64_t dim, in
         gx.a = G; gx.lda = S.ld;
         gx.b = wp; gx.ldb = dim; gx.b_kstrided = true;
         gx.rem_last = true;
-        RDCN_TRY(soft_product(h, RDCN_KERNEL_HEAD_GX_GEMM, gx, v > 0 ? acc : nullptr, acc, grad_x, v + n == classes, splitk,
-                              s));
         GemmArgs gw{};
         gw.M = n; gw.N = dim; gw.K = rows;
         gw.a = G; gw.lda = S.ld; gw.a_kstrided = true;
         gw.b = kept; gw.ldb = dim; gw.b_kstrided = true;
-        RDCN_TRY(soft_product(h, RDCN_KERNEL_HEAD_GW_GEMM, gw, nullptr, nullptr, (char*)grad_w + (size_t)v * dim * e, true,
-                              splitk, s));
+        const SoftProduct px = soft_product(h, gx, v > 0 ? acc : nullptr, acc, grad_x, v + n == classes, splitk);
+        const SoftProduct pw = soft_product(h, gw, nullptr, nullptr, (char*)grad_w + (size_t)v * dim * e, true,
+                                            (float*)(sc + S.splitw));
+        RDCN_TRY(soft_gradients(h, px, pw, s));
     }
     return RDCN_OK;
 }

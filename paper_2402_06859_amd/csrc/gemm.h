@@ -116,6 +116,11 @@ hipError_t launch_gemm(const GemmArgs& g, const GemmPlan& p, bool bf16, hipStrea
 inline int64_t gemm_tiles_n(int64_t N, const GemmPlan& p) { return (N + p.bn - 1) / p.bn; }
 // Column tiles of a softmax loss product (EPI_SOFT_FWD) and the columns of one, as launch_gemm's blocks have them.
 int64_t gemm_soft_tiles(int64_t M, int64_t N, int64_t K, const GemmPlan& p, bool bf16, int* columns);
+// Two products in one launch, with plain epilogues: x with A K-contiguous and B K-strided, y with both K-strided. gemm_pairs:
+// their plans are of 64 x 64 blocks, and so few of them that a launch each would leave the chip part empty.
+bool gemm_pairs(const GemmArgs& x, const GemmPlan& px, const GemmArgs& y, const GemmPlan& py, bool bf16);
+hipError_t launch_gemm_pair(const GemmArgs& x, const GemmPlan& px, const GemmArgs& y, const GemmPlan& py, bool bf16,
+                            hipStream_t s);
 hipError_t launch_splitk_reduce(const float* part, int splits, int64_t MN, float* out, hipStream_t s);
 // dst = f16(src) for n bf16 values (n % 8 == 0, 16-byte aligned); sets ERR_BIT_F16_RANGE
 // in err when a value is beyond the f16 range.

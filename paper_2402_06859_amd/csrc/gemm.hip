@@ -1013,18 +1013,16 @@ __device__ __forceinline__ void soft_block_epilogue(const GemmArgs& g, int64_t m
     }
 }
 
-// C = A B^T with an ST-stage direct-to-LDS pipeline of KB-deep stages (see layouts above).
+// C = A B^T with an ST-stage direct-to-LDS pipeline of KB-deep stages (see layouts above): one workgroup's block, tile
+// `block` of the product in range z of `splits`. `smem` holds the ST stages: the ring during the K loop, the C staging area
+// afterwards.
 template <int BM, int BN, bool AKS, bool BKS, int ST, int WM, int WN, bool M32, typename T, int EK, bool F16, int KB>
-__global__ __launch_bounds__(64 * WM * WN, (ST == 2 && WM * WN == 4) ? 2 : 1)
-__attribute__((amdgpu_waves_per_eu(WM * WN == 8 ? 2 : 1, WM * WN == 8 ? 2 : 8))) void k_gemm_mfma(GemmArgs g) {
+__device__ __forceinline__ void gemm_block(const GemmArgs& g, int block, int z, int splits, bf16_t* smem) {
     using P = Pipe<BM, BN, AKS, BKS, ST, WM, WN, M32, F16, KB>;
-    // one buffer: the stage ring during the K loop, the C staging area afterwards
-    __shared__ __attribute__((aligned(1024))) bf16_t smem[ST * P::STAGE_ELEMS];
-
     const int tid = threadIdx.x;
     const int tiles_n = (int)((g.N + BN - 1) / BN);
     const int tiles_m = (int)((g.M + BM - 1) / BM);
-    const int t = xcd_remap(blockIdx.x, tiles_m * tiles_n);
+    const int t = xcd_remap(block, tiles_m * tiles_n);
     int tm, tn;
     if (g.group_m > 1) {
         // groups of group_m tile rows, walked column by column: the blocks that run
@@ -1044,9 +1042,8 @@ __attribute__((amdgpu_waves_per_eu(WM * WN == 8 ? 2 : 1, WM * WN == 8 ? 2 : 8)))
     c.tid = tid;
     c.m0 = (int64_t)tm * BM;
     c.n0 = (int64_t)tn * BN;
-    const int z = blockIdx.z;
     // split-K ranges are multiples of BK (itself a multiple of every KB)
-    const int64_t kchunk = ((g.K + (int64_t)gridDim.z * BK - 1) / ((int64_t)gridDim.z * BK)) * BK;
+    const int64_t kchunk = ((g.K + (int64_t)splits * BK - 1) / ((int64_t)splits * BK)) * BK;
     c.kbeg = z * kchunk;
     c.kend = c.kbeg + kchunk < g.K ? c.kbeg + kchunk : g.K;
     c.nk = c.kbeg < c.kend ? (int)((c.kend - c.kbeg + KB - 1) / KB) : 0;
@@ -1095,6 +1092,23 @@ __attribute__((amdgpu_waves_per_eu(WM * WN == 8 ? 2 : 1, WM * WN == 8 ? 2 : 8)))
         soft_block_epilogue<bf16_t, EK == EK_SOFT_GRAD, BM, BN, WM, WN, M32>(g, c.m0, c.n0, acc, tid, (uint32_t*)smem);
     }
     else block_epilogue<BM, BN, WM, WN, M32, T, EK, P::THREADS, ST * P::STAGE_ELEMS>(g, c.m0, c.n0, z, acc, smem, tid);
+}
+
+template <int BM, int BN, bool AKS, bool BKS, int ST, int WM, int WN, bool M32, typename T, int EK, bool F16, int KB>
+__global__ __launch_bounds__(64 * WM * WN, (ST == 2 && WM * WN == 4) ? 2 : 1)
+__attribute__((amdgpu_waves_per_eu(WM * WN == 8 ? 2 : 1, WM * WN == 8 ? 2 : 8))) void k_gemm_mfma(GemmArgs g) {
+    __shared__ __attribute__((aligned(1024))) bf16_t smem[ST * Pipe<BM, BN, AKS, BKS, ST, WM, WN, M32, F16, KB>::STAGE_ELEMS];
+    gemm_block<BM, BN, AKS, BKS, ST, WM, WN, M32, T, EK, F16, KB>(g, blockIdx.x, blockIdx.z, gridDim.z, smem);
+}
+
+// Two products of 64 x 64 blocks in one launch: x (A K-contiguous, B K-strided) in the first nx workgroups, y (both
+// K-strided) in the rest, each with its own splits of K.
+__global__ __launch_bounds__(256) void k_gemm_pair(GemmArgs x, GemmArgs y, int nx, int xtiles, int xsplits, int ytiles,
+                                                   int ysplits) {
+    __shared__ __attribute__((aligned(1024))) bf16_t smem[3 * (64 + 64) * 64];
+    const int b = blockIdx.x, c = b - nx;
+    if (c < 0) gemm_block<64, 64, false, true, 3, 2, 2, false, bf16_t, EK_PLAIN, false, 64>(x, b % xtiles, b / xtiles, xsplits, smem);
+    else gemm_block<64, 64, true, true, 3, 2, 2, false, bf16_t, EK_PLAIN, false, 64>(y, c % ytiles, c / ytiles, ysplits, smem);
 }
 
 // ---------------------------------------------------------------------------
@@ -1235,6 +1249,11 @@ hipError_t launch_stream(const GemmArgs& g, hipStream_t s) {
     return hipGetLastError();
 }
 
+// two stages of both operands
+constexpr int f32_lds_floats(bool aks, bool bks) {
+    return 2 * ((aks ? 32 / 4 * (4 * 64 + 16) : 64 * 32) + (bks ? 32 / 4 * (4 * 64 + 16) : 64 * 32));
+}
+
 // Float GEMM for operands whose rows are 16-byte aligned and whose strides are multiples of 4: 64 x 64 blocks of
 // four waves (32 x 32 each), K in stages of 32 through a ring of two in LDS (33 KiB, four blocks a CU; with
 // three stages and three blocks 1-4% slower), filled by direct global-to-LDS loads. A
@@ -1245,20 +1264,19 @@ hipError_t launch_stream(const GemmArgs& g, hipStream_t s) {
 // TFLOP/s (a library product of 4096^3 at 135), its products' steps alone at 130; 512 x 160 x 5000, 24 to 632 blocks
 // of 5 to 16 stages, takes 74 us against 85 with that kernel.
 template <bool AKS, bool BKS, int EK>
-__global__ __launch_bounds__(256) void k_gemm_f32_lds(GemmArgs g) {
+__device__ __forceinline__ void f32_lds_block(const GemmArgs& g, int block, int z, int splits, float* smem) {
     constexpr int BM = 64, BN = 64, KB = 32, ST = 2, CP = BN + 4, LOADS = 4;
     constexpr int KC = BM * KB, KS = (KB / 4) * (4 * BM + 16);  // floats of a stage of either kind
     constexpr int SA = AKS ? KS : KC, STAGE = SA + (BKS ? KS : KC);
     static_assert(BM * CP <= ST * STAGE, "C staging must fit the ring");
-    __shared__ __attribute__((aligned(1024))) float smem[ST * STAGE];
+    static_assert(ST * STAGE == f32_lds_floats(AKS, BKS), "the kernels' shared memory");
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wm = wave >> 1, wn = wave & 1, i = lane & 15, q = lane >> 4;
     const int tiles_m = (int)((g.M + BM - 1) / BM), tiles_n = (int)((g.N + BN - 1) / BN);
     // consecutive blocks of an XCD share a panel of B
-    const int t = xcd_remap(blockIdx.x, tiles_m * tiles_n);
+    const int t = xcd_remap(block, tiles_m * tiles_n);
     const int64_t m0 = (int64_t)(t % tiles_m) * BM, n0 = (int64_t)(t / tiles_m) * BN;
-    const int z = blockIdx.z;
-    const int64_t kchunk = ((g.K + (int64_t)gridDim.z * KB - 1) / ((int64_t)gridDim.z * KB)) * KB;
+    const int64_t kchunk = ((g.K + (int64_t)splits * KB - 1) / ((int64_t)splits * KB)) * KB;
     const int64_t kbeg = z * kchunk, kend = kbeg + kchunk < g.K ? kbeg + kchunk : g.K;
     const int nk = kbeg < kend ? (int)((kend - kbeg + KB - 1) / KB) : 0;
     // two 1 KiB loads per wave, operand and stage; rows past the end re-read the last ones
@@ -1389,6 +1407,21 @@ __global__ __launch_bounds__(256) void k_gemm_f32_lds(GemmArgs g) {
         float v[4] = {s.x, s.y, s.z, s.w};
         if (m < g.M && n < g.N) epilogue4<float>(g, m, n, z, v);
     }
+}
+
+template <bool AKS, bool BKS, int EK>
+__global__ __launch_bounds__(256) void k_gemm_f32_lds(GemmArgs g) {
+    __shared__ __attribute__((aligned(1024))) float smem[f32_lds_floats(AKS, BKS)];
+    f32_lds_block<AKS, BKS, EK>(g, blockIdx.x, blockIdx.z, gridDim.z, smem);
+}
+
+// As k_gemm_pair, for float products.
+__global__ __launch_bounds__(256) void k_gemm_f32_pair(GemmArgs x, GemmArgs y, int nx, int xtiles, int xsplits, int ytiles,
+                                                       int ysplits) {
+    __shared__ __attribute__((aligned(1024))) float smem[f32_lds_floats(true, true)];  // (the larger)
+    const int b = blockIdx.x, c = b - nx;
+    if (c < 0) f32_lds_block<false, true, EK_PLAIN>(x, b % xtiles, b / xtiles, xsplits, smem);
+    else f32_lds_block<true, true, EK_PLAIN>(y, c % ytiles, c / ytiles, ysplits, smem);
 }
 
 hipError_t launch_f32_lds(const GemmArgs& g, int splits, hipStream_t s) {
@@ -1797,6 +1830,38 @@ hipError_t launch_gemm(const GemmArgs& g, const GemmPlan& p, bool bf16, hipStrea
         return launch_tile<128, 128, 3, 2, 2, true, bf16_t>(ga, p.splits, s);
     }
     return launch_tile<64, 64, 3, 2, 2, false, bf16_t>(ga, p.splits, s);
+}
+
+namespace {
+
+int64_t pair_blocks(const GemmArgs& g, const GemmPlan& p) { return ((g.M + 63) / 64) * ((g.N + 63) / 64) * p.splits; }
+
+}  // namespace
+
+// Both gradients of the softmax loss, a launch each / one for both, the whole gradient and forward, us: bf16 1024 x 512 x
+// 1000 34.6 / 29.4, 4096 x 64 x 2000 49.4 / 41.3, 333 x 136 x 1001 26.8 / 24.6; float 512 x 160 x 5000 62.9 / 55.3, 2048 x
+// 512 x 8192 (1536 blocks) 466 / 467, 4096 x 1024 x 16384 (5120) 3345 / 3368; bf16 1 x 4352 x 32000 (34000) 243 / 245. So:
+// up to eight blocks a CU.
+bool gemm_pairs(const GemmArgs& x, const GemmPlan& px, const GemmArgs& y, const GemmPlan& py, bool bf16) {
+    if (bf16 ? px.bm != 64 || py.bm != 64 : px.stages != F32_LDS_STAGES || py.stages != F32_LDS_STAGES) return false;
+    return pair_blocks(x, px) + pair_blocks(y, py) <= 2048;
+}
+
+hipError_t launch_gemm_pair(const GemmArgs& x, const GemmPlan& px, const GemmArgs& y, const GemmPlan& py, bool bf16,
+                            hipStream_t s) {
+    if (x.a_kstrided || !x.b_kstrided || !y.a_kstrided || !y.b_kstrided || x.M <= 0 || x.N <= 0 || y.M <= 0 || y.N <= 0 ||
+        !gemm_pairs(x, px, y, py, bf16))
+        return hipErrorInvalidValue;
+    for (const GemmArgs* g : {&x, &y}) {
+        if (g->ops_f16 || g->a2 || (g->epi != EPI_STORE && g->epi != EPI_STORE_F32 && g->epi != EPI_RESID && g->epi != EPI_PARTIAL))
+            return hipErrorInvalidValue;
+        if (!bf16 && (((uintptr_t)g->a & 15) || ((uintptr_t)g->b & 15) || g->lda % 4 || g->ldb % 4)) return hipErrorInvalidValue;
+    }
+    const int nx = (int)pair_blocks(x, px), xt = nx / px.splits, ny = (int)pair_blocks(y, py), yt = ny / py.splits;
+    const dim3 grid((unsigned)(nx + ny)), block(256);
+    if (bf16) hipLaunchKernelGGL(k_gemm_pair, grid, block, 0, s, x, y, nx, xt, px.splits, yt, py.splits);
+    else hipLaunchKernelGGL(k_gemm_f32_pair, grid, block, 0, s, x, y, nx, xt, px.splits, yt, py.splits);
+    return hipGetLastError();
 }
 
 // dst = f16(src), 8 values per thread and step; err bit on values beyond the f16 range.

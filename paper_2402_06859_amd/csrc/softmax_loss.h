@@ -45,9 +45,16 @@ hipError_t launch_soft_normalize(const SoftNorm& a, bool bf16, hipStream_t s);
 bool soft_row_at_once(int64_t rows, int64_t tiles, int64_t ld);
 hipError_t launch_soft_row(const SoftRows& a, const SoftNorm& n, bool bf16, hipStream_t s);
 
-// sum over `splits` planes of part (n floats each, in plane order), added to acc if it is not NULL;
-// written to acc_out (float) or, if that is NULL, to out (storage type). n is a multiple of 4.
-hipError_t launch_soft_reduce(const float* part, int splits, int64_t n, const float* acc, float* acc_out, void* out,
-                              bool bf16, hipStream_t s);
+// Sums over planes: over `splits` planes of part (n floats each, in plane order), added to acc if it is not NULL;
+// written to acc_out (float) or, if that is NULL, to out (storage type). n is a multiple of 4. Two go in one launch if they are split alike.
+struct SoftSum {
+    const float* part;
+    int splits;
+    int64_t n;
+    const float* acc;
+    float* acc_out;
+    void* out;
+};
+hipError_t launch_soft_reduce(const SoftSum* sums, int count, bool bf16, hipStream_t s);
 
 }  // namespace rdcn

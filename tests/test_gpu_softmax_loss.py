@@ -150,6 +150,19 @@ def test_matches_definition(dtype, rows, dim, classes):
     assert lib.check_device_errors() == rdcn.RDCN_OK
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,dim,classes", [(5, 1024, 4000), (5, 2048, 4200), (1, 8, 20000), (700, 64, 70), (3, 1600, 64)])
+def test_few_and_many_small_blocks(dtype, rows, dim, classes):
+    """Gradients whose products go in one launch (up to 2048 blocks together) and those that take one each; with one of
+    them much the larger, and with one split along its sum and the other not."""
+    need_gpu()
+    print("softmax loss blocks", dtype, rows, dim, classes, flush=True)
+    lib = handle(dtype)
+    c = make(dtype, rows, dim, classes, 29, ignored=0.1, masked=0.1, weights=True)
+    check(lib, c, rows, dim, classes, dtype == "f32")
+    assert lib.check_device_errors() == rdcn.RDCN_OK
+
+
 @pytest.mark.parametrize("dtype,id_type", [("bf16", "i64"), ("bf16", "i32"), ("f32", "i32")])
 @pytest.mark.parametrize("rows,dim,classes", [(3, 40, 65), (70, 72, 515), (333, 136, 1001), (520, 264, 4099)])
 def test_masks_padding_rows_and_weights(dtype, id_type, rows, dim, classes):
