@@ -517,14 +517,16 @@ rdcn_status rdcn_softmax_loss_forward(rdcn_handle* h, int64_t rows, int64_t dim,
  * grad_x [rows, dim] and grad_w [classes, dim], both in the storage dtype and
  * overwritten. With p = softmax(z) and G = scale * weight * logit_scale * (p - onehot):
  * grad_x = G w, grad_w = G^T x. bf16 models round G to bf16 for the matrix
- * products (a relative 2^-8 per element at most, label's element taken from z, so that
- * p - 1 keeps its digits) and each gradient once at the end; sums are float and
- * in a fixed order (deterministic).
+ * products (half a step, 2^-8 of an element) and each gradient once at the end; sums are float and
+ * in a fixed order (deterministic). Where they keep all exponentials (below), those are in f16: 2^-11 of an
+ * element more, growing from 2^-29 of the largest of the 16 to 64 classes around it on, and 0 below 2^-40.
+ * The label's element, scale * weight * logit_scale * (p - 1), and the loss are taken from the sum of the other
+ * classes' exponentials: they keep their digits where p is near 1, in float models too.
  * G stands in scratch. With grad_bytes of it (rdcn_softmax_loss_workspace) the call is fastest: G of all
  * classes up to 4 GiB (their exponentials are then kept from the forward), in pieces of 1 GiB past that.
  * It takes any size from grad_least_bytes on: the less, the smaller the pieces of the classes that
  * are worked on at a time, whose logits are then computed twice. Results of different sizes of scratch
- * differ in the order of their sums.
+ * differ in the order of their sums and in bf16 models by the roundings to f16.
  */
 rdcn_status rdcn_softmax_loss_grad(rdcn_handle* h, int64_t rows, int64_t dim, int64_t classes, const void* x,
                                    const void* w, const float* offset, const void* labels, float logit_scale,

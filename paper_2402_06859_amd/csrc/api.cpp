@@ -370,7 +370,7 @@ struct SoftPlan {
     int64_t ld;                 // row stride of G
     int64_t tiles;              // column tiles of the forward's product
     int tile;
-    size_t part, zlabel, forward_total, factor, kept, G, acc, splitk, splitw, total;
+    size_t part, zlabel, forward_total, row, kept, G, acc, splitk, splitw, total;
 };
 
 int64_t split_floats(const rdcn_handle* h, int64_t M, int64_t N, int64_t K) {
@@ -408,7 +408,7 @@ SoftPlan soft_layout(const rdcn_handle* h, int64_t rows, int64_t dim, int64_t cl
     s.part = off; off += al((size_t)s.tiles * rows * 8);
     s.zlabel = off; off += al((size_t)rows * 4);
     s.forward_total = off;
-    s.factor = off; off += al((size_t)rows * 4);
+    s.row = off; off += al((size_t)rows * sizeof(SoftRow));
     s.kept = off; off += al((size_t)rows * dim * e);
     s.G = off; off += al((size_t)rows * s.ld * e);
     s.acc = off; off += classes > s.piece ? al((size_t)rows * dim * 4) : 0;  // grad_x as a sum of several products
@@ -513,10 +513,10 @@ hipError_t soft_gradients(rdcn_handle* h, const SoftProduct& x, const SoftProduc
 }
 
 // The logits product and the join of its pairs. With `G` (S.whole) its exponentials are kept there and become the
-// gradient in the logits; with `factor` the rows' gradient factors go out, and to `kept` the rows of x that have a label.
+// gradient in the logits; with `row` the rows' part of it goes out, and to `kept` the rows of x that have a label.
 rdcn_status soft_forward(rdcn_handle* h, const SoftPlan& S, int64_t rows, int64_t dim, int64_t classes, const void* x,
                          const void* w, const float* offset, const void* labels, float logit_scale,
-                         const float* row_weight, float scale, float* loss, float* lse, char* sc, void* G, float* factor,
+                         const float* row_weight, float scale, float* loss, float* lse, char* sc, void* G, SoftRow* row,
                          void* kept, hipStream_t s) {
     GemmArgs g{};
     g.M = rows; g.N = classes; g.K = dim;
@@ -537,13 +537,12 @@ rdcn_status soft_forward(rdcn_handle* h, const SoftPlan& S, int64_t rows, int64_
     r.softpart = g.softpart; r.zlabel = g.zlabel;
     r.labels = labels; r.labels64 = h->ids64;
     r.row_weight = row_weight; r.scale = scale;
-    r.loss = loss; r.lse = lse; r.factor = factor;
+    r.loss = loss; r.lse = lse; r.row = row;
     r.err = h->err;
     r.x = x; r.kept = kept; r.dim = dim;
     SoftNorm n{};
     n.rows = rows; n.classes = classes; n.ld = S.ld; n.tile = S.tile;
-    n.softpart = g.softpart; n.zlabel = g.zlabel;
-    n.lse = lse; n.factor = factor;
+    n.softpart = g.softpart; n.row = row;
     n.labels = labels; n.labels64 = h->ids64;
     n.e = G;
     const bool at_once = G && soft_row_at_once(rows, S.tiles, S.ld);
@@ -1375,14 +1374,14 @@ rdcn_status rdcn_softmax_loss_grad(rdcn_handle* h, int64_t rows, int64_t dim, in
     const SoftPlan S = soft_plan(h, rows, dim, classes, scratch_bytes);
     if (!scratch || !aligned256(scratch) || scratch_bytes < S.total) return RDCN_ERR_WORKSPACE;
     char* sc = (char*)scratch;
-    float* const factor = (float*)(sc + S.factor);
+    SoftRow* const row = (SoftRow*)(sc + S.row);
     float* const acc = (float*)(sc + S.acc);
     float* const splitk = (float*)(sc + S.splitk);
     const void* const kept = sc + S.kept;
     char* const G = sc + S.G;
     // the gradient of the logits carries the logits' own scale
     if ((st = soft_forward(h, S, rows, dim, classes, x, w, offset, labels, logit_scale, row_weight, scale * logit_scale,
-                           loss, lse, sc, S.whole ? G : nullptr, factor, sc + S.kept, s)) != RDCN_OK)
+                           loss, lse, sc, S.whole ? G : nullptr, row, sc + S.kept, s)) != RDCN_OK)
         return st;
     for (int64_t v = 0; v < classes; v += S.piece) {
         const int64_t n = std::min(S.piece, classes - v);
@@ -1395,7 +1394,7 @@ rdcn_status rdcn_softmax_loss_grad(rdcn_handle* h, int64_t rows, int64_t dim, in
             g.epi = EPI_SOFT_GRAD; g.scale = logit_scale;
             g.offset = offset ? offset + v : nullptr;
             g.labels = labels; g.labels64 = h->ids64; g.label0 = v;
-            g.rowv = lse; g.rowg = factor;
+            g.softrow = row;
             g.c = G; g.ldc = S.ld;
             ProfScope ps(h, RDCN_KERNEL_HEAD_FWD_GEMM, s);
             RDCN_TRY(launch_gemm(g, plan_logits(h, rows, n, dim), h->bf16, s));

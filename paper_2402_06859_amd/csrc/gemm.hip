@@ -309,10 +309,12 @@ __device__ __forceinline__ void soft_epilogue8(const GemmArgs& g, int64_t m, int
     }
     if (g.epi == EPI_SOFT_GRAD) {
         if (!in) return;
-        const float lse = g.rowv[m], f = g.rowg[m];
+        const SoftRow r = g.softrow[m];
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-            v[e] = f == 0.f || v[e] == NEG ? 0.f : f * (soft_exp<bf16_t>(v[e] - lse) - (lab == e ? 1.f : 0.f));
+        for (int e = 0; e < 8; ++e) {
+            v[e] = r.c == 0.f || v[e] == NEG ? 0.f : r.c * soft_exp<bf16_t>(v[e] - r.max);
+            if (lab == e) v[e] = r.label;
+        }
         store8<bf16_t>((bf16_t*)g.c + m * g.ldc + n, v);
         return;
     }
@@ -325,7 +327,10 @@ __device__ __forceinline__ void soft_epilogue8(const GemmArgs& g, int64_t m, int
     float sum = 0.f;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-        if (lab == e) g.zlabel[m] = v[e];
+        if (lab == e) {
+            g.zlabel[m] = v[e];
+            v[e] = NEG;  // (its exponential is added where the row's pairs are joined)
+        }
         v[e] = soft_exp<bf16_t>(v[e] - top);
         sum += v[e];
     }
@@ -919,7 +924,7 @@ __device__ __forceinline__ void soft_block_epilogue(const GemmArgs& g, int64_t m
             for (int e = 0; e < V; ++e) v[e] = off[e] == NEG ? NEG : v[e] + off[e];
         }
         if constexpr (GRAD) {
-            const float lse = in ? g.rowv[m] : 0.f, f = in ? g.rowg[m] : 0.f;
+            const SoftRow r = in ? g.softrow[m] : SoftRow{};
 #pragma unroll
             for (int j = 0; j < TN; ++j)
 #pragma unroll
@@ -927,8 +932,8 @@ __device__ __forceinline__ void soft_block_epilogue(const GemmArgs& g, int64_t m
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         float& z = v[4 * (j * Q + q) + e];
-                        const float hot = hit && (int)lab == col(j, q) + e ? 1.f : 0.f;
-                        z = f == 0.f || z == NEG ? 0.f : f * (soft_exp<T>(z - lse) - hot);
+                        z = r.c == 0.f || z == NEG ? 0.f : r.c * soft_exp<T>(z - r.max);
+                        if (hit && (int)lab == col(j, q) + e) z = r.label;
                     }
         } else {
             float mx = v[0];
@@ -943,7 +948,13 @@ __device__ __forceinline__ void soft_block_epilogue(const GemmArgs& g, int64_t m
 #pragma unroll
                     for (int q = 0; q < Q; ++q)
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) z = (int)lab == col(j, q) + e ? v[4 * (j * Q + q) + e] : z;
+                        for (int e = 0; e < 4; ++e) {
+                            float& a = v[4 * (j * Q + q) + e];
+                            if ((int)lab == col(j, q) + e) {
+                                z = a;
+                                a = NEG;  // (its exponential is added where the row's pairs are joined)
+                            }
+                        }
                 g.zlabel[m] = z;
             }
             const float top = mx == NEG ? 0.f : mx;  // (all masked: exp(-inf) = 0 each)

@@ -3,11 +3,13 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include "gemm.h"
+
 namespace rdcn {
 
-// lse, loss and (optional) the rows' gradient factors from the logits product's partials
-// softpart [tiles][rows] and zlabel [rows]. A label outside [0, classes) gives loss 0 and factor
-// 0; one at or past `classes` also sets the index bit of *err. factor = scale * (row_weight or 1).
+// lse, loss and (optional) what the rows' gradients need from the logits product's partials
+// softpart [tiles][rows] and zlabel [rows]. A label outside [0, classes) gives loss 0 and a row
+// of zeros; one at or past `classes` also sets the index bit of *err. A row's factor = scale * (row_weight or 1).
 struct SoftRows {
     int64_t rows, tiles, classes;
     const float2* softpart;
@@ -18,9 +20,9 @@ struct SoftRows {
     float scale;
     float* loss;
     float* lse;
-    float* factor;  // may be NULL (no gradient)
+    SoftRow* row;  // may be NULL (no gradient)
     int* err;
-    // with factor: kept [rows, dim] = x, with zeros in the rows that have no label
+    // with row: kept [rows, dim] = x, with zeros in the rows that have no label
     const void* x;
     void* kept;
     int64_t dim;
@@ -33,15 +35,13 @@ struct SoftNorm {
     int64_t rows, classes, ld;
     int tile;  // columns of a tile
     const float2* softpart;
-    const float* zlabel;
-    const float* lse;
-    const float* factor;
+    const SoftRow* row;
     const void* labels;
     bool labels64;
     void* e;
 };
 hipError_t launch_soft_normalize(const SoftNorm& a, bool bf16, hipStream_t s);
-// launch_soft_rows (with factor) and launch_soft_normalize in one, where soft_row_at_once says so.
+// launch_soft_rows (with row) and launch_soft_normalize in one, where soft_row_at_once says so.
 bool soft_row_at_once(int64_t rows, int64_t tiles, int64_t ld);
 hipError_t launch_soft_row(const SoftRows& a, const SoftNorm& n, bool bf16, hipStream_t s);
 

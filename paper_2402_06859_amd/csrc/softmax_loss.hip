@@ -6,6 +6,11 @@
 // The logits product (gemm.hip, EPI_SOFT_FWD) leaves one (maximum, sum of exponentials) pair per row
 // and column tile; the pairs of a row are joined here: the sum of exponentials over two
 // ranges with maxima a and b is S_a exp(a - c) + S_b exp(b - c) for c = max(a, b).
+//
+// A row stays (maximum, sum) to the end: a difference from lse, rounded to float, is off by |lse| 2^-24 and loses log(sum)
+// itself where all logits are far from 0 (an offset of -10^9 on every class). And the pairs leave the label out:
+// with R the sum over the other classes and e = exp(z[y] - max) the label's, 1 - p = R / (R + e) and loss = log(1 + R / e)
+// keep their digits where p is near 1, which neither p - 1 nor lse - z[y] would.
 #include "device_common.h"
 #include "gemm.h"
 #include "softmax_loss.h"
@@ -54,22 +59,30 @@ __device__ __forceinline__ void copy_kept_rows(const SoftRows& a, int64_t first)
     }
 }
 
-// Row m's lse (x) and gradient factor (y) from its maximum and sum; `write`: they and the loss go out.
-__device__ __forceinline__ float2 finish_row(const SoftRows& a, int64_t m, float mx, float sum, bool write) {
-    const float lse = mx == NEG_INF && sum == 0.f ? NEG_INF : mx + logf(sum);
+// Row m's gradient from its maximum and the sum over the classes other than its label; `write`: it, loss and lse go out.
+__device__ __forceinline__ SoftRow finish_row(const SoftRows& a, int64_t m, float mx, float rest, bool write) {
     const int64_t y = label_of(a.labels, a.labels64, m);
     const bool kept = y >= 0 && y < a.classes;
-    const float f = a.factor && kept ? a.scale * (a.row_weight ? a.row_weight[m] : 1.f) : 0.f;
+    const float f = a.row && kept ? a.scale * (a.row_weight ? a.row_weight[m] : 1.f) : 0.f;
+    const float z = kept ? a.zlabel[m] : NEG_INF;
+    const bool seen = z != NEG_INF;  // the row's label has a probability
+    const float own = seen ? expf(z - mx) : 0.f, sum = rest + own;
+    SoftRow r{};
+    r.max = mx;
+    if (f != 0.f && mx != NEG_INF) {
+        r.c = f / sum;
+        r.label = seen ? -f * (rest / sum) : 0.f;
+    }
     if (write) {
         if (y >= a.classes) atomicOr(a.err, ERR_BIT_INDEX);
-        a.lse[m] = lse;
+        a.lse[m] = mx == NEG_INF ? NEG_INF : mx + logf(sum);
         // a label whose own class is masked has probability 0: its loss is +inf, also where every class is
         float loss = 0.f;
-        if (kept) loss = a.zlabel[m] == NEG_INF ? -NEG_INF : lse - a.zlabel[m];
+        if (kept) loss = !seen ? -NEG_INF : rest < own ? log1pf(rest / own) : (mx - z) + logf(sum);
         a.loss[m] = loss;
-        if (a.factor) a.factor[m] = f;
+        if (a.row) a.row[m] = r;
     }
-    return make_float2(lse, f);
+    return r;
 }
 
 // 256 threads as rpb rows x (256 / rpb) lanes that stride over the tiles. Few rows take many
@@ -107,10 +120,10 @@ __global__ __launch_bounds__(256) void k_soft_rows(SoftRows a, int rpb) {
 }
 
 // Columns first, first + step, .. (vectors) of row m of E -> G. Reads and writes each element once (2 + 2 bytes, 4 + 4
-// in float); the factor exp(tile's maximum - lse) f is one exponential per vector, not per element. The label's
-// own element is taken from z itself, so p - 1 keeps its digits where p is close to 1.
+// in float); the factor exp(tile's maximum - row's) f / S is one exponential per vector, not per element. The label's
+// own element is the row's.
 template <typename T>
-__device__ __forceinline__ void normalize_row(const SoftNorm& a, int64_t m, float lse, float f, int64_t y, int64_t first,
+__device__ __forceinline__ void normalize_row(const SoftNorm& a, int64_t m, const SoftRow& r, int64_t y, int64_t first,
                                               int64_t step) {
     constexpr int W = st<T>::vec;
     for (int64_t n = first * W; n < a.ld; n += step * W) {
@@ -119,14 +132,13 @@ __device__ __forceinline__ void normalize_row(const SoftNorm& a, int64_t m, floa
         if constexpr (sizeof(T) == 2) unpack_f16x8(*(const u32x4_t*)((const _Float16*)a.e + m * a.ld + n), v);
         else st<T>::unpack(*(const u32x4_t*)((const float*)a.e + m * a.ld + n), v);
         const float unit = sizeof(T) == 2 ? 1.f / SOFT_E_SCALE : 1.f;
-        const float c = f == 0.f || top == NEG_INF ? 0.f : f * unit * expf(top - lse);
+        const float c = r.c == 0.f || top == NEG_INF ? 0.f : r.c * unit * expf(top - r.max);
 #pragma unroll
         for (int e = 0; e < W; ++e) v[e] = c == 0.f ? 0.f : c * v[e];
-        if (y >= n && y < n + W && f != 0.f) {
-            const float z = a.zlabel[m];
+        if (y >= n && y < n + W) {
 #pragma unroll
             for (int e = 0; e < W; ++e)
-                if (y - n == e) v[e] = z == NEG_INF ? 0.f : f * expm1f(z - lse);
+                if (y - n == e) v[e] = r.label;
         }
         *(u32x4_t*)((T*)a.e + m * a.ld + n) = st<T>::pack(v);
     }
@@ -137,7 +149,7 @@ template <typename T>
 __global__ __launch_bounds__(256) void k_soft_normalize(SoftNorm a) {
     const int64_t m = blockIdx.y + (int64_t)blockIdx.z * 65535;
     if (m >= a.rows) return;
-    normalize_row<T>(a, m, a.lse[m], a.factor[m], label_of(a.labels, a.labels64, m), blockIdx.x * 256ll + threadIdx.x,
+    normalize_row<T>(a, m, a.row[m], label_of(a.labels, a.labels64, m), blockIdx.x * 256ll + threadIdx.x,
                      gridDim.x * 256ll);
 }
 
@@ -162,9 +174,9 @@ __global__ __launch_bounds__(256) void k_soft_row(SoftRows a, SoftNorm b) {
     mx = NEG_INF;
     sum = 0.f;
     join(mx, sum, p);
-    const float2 r = finish_row(a, m, mx, sum, threadIdx.x == 0);
+    const SoftRow r = finish_row(a, m, mx, sum, threadIdx.x == 0);
     const int64_t y = label_of(a.labels, a.labels64, m);
-    normalize_row<T>(b, m, r.x, r.y, y, threadIdx.x, 256);
+    normalize_row<T>(b, m, r, y, threadIdx.x, 256);
     constexpr int W = st<T>::vec;
     const bool kept = row_counts(a, m);
     for (int64_t i = threadIdx.x; i < a.dim / W; i += 256) {
@@ -227,7 +239,7 @@ hipError_t launch_soft_rows(const SoftRows& a, bool bf16, hipStream_t s) {
     int rpb = 1;  // about 256 workgroups or more, as long as there are that many rows
     while (rpb < 64 && a.rows / (2 * rpb) >= 256) rpb *= 2;
     const unsigned nrow = (unsigned)((a.rows + rpb - 1) / rpb);
-    const unsigned ncopy = a.factor ? blocks_for(a.rows * a.dim / (bf16 ? 8 : 4), 4096).x : 0;
+    const unsigned ncopy = a.row ? blocks_for(a.rows * a.dim / (bf16 ? 8 : 4), 4096).x : 0;
     if (bf16) hipLaunchKernelGGL(k_soft_rows<bf16_t>, dim3(nrow + ncopy), dim3(256), 0, s, a, rpb);
     else hipLaunchKernelGGL(k_soft_rows<float>, dim3(nrow + ncopy), dim3(256), 0, s, a, rpb);
     return hipGetLastError();
