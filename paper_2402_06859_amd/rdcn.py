@@ -85,7 +85,7 @@ class RdcnAdamwConfig(ctypes.Structure):
 def adamw_tensors(tensors: Sequence[dict]):
     """Descriptors of tensors to step, once for many steps. Each is a dict of device tensors
     param, grad, m, v and, where it has them, master and exps, and its weight_decay. The caller
-    keeps the tensors alive."""
+    keeps the tensors alive. The kernels go by pointers alone, so what does not fit is a ValueError here."""
     out = (RdcnAdamwTensor * len(tensors))()
     for d, t in zip(out, tensors):
         n = t["param"].numel()
@@ -93,10 +93,19 @@ def adamw_tensors(tensors: Sequence[dict]):
             x = t.get(k)
             if x is not None and (x.numel() != n or not x.is_contiguous()):
                 raise ValueError("adamw_tensors: %s must be contiguous, of as many elements as param" % k)
+        for k in ("param", "grad"):
+            if t[k].dtype not in (torch.float32, torch.bfloat16):
+                raise ValueError("adamw_tensors: %s must be float32 or bfloat16, not %s" % (k, t[k].dtype))
+        if t.get("master") is not None and (t["master"].dtype != torch.float32 or t["param"].dtype != torch.bfloat16):
+            raise ValueError("adamw_tensors: a master is float32, of a bfloat16 param")
         if t["m"].dtype != t["v"].dtype or t["m"].dtype not in (torch.uint8, torch.float32):
             raise ValueError("adamw_tensors: m and v are both float32 or both uint8")
-        if t["m"].dtype == torch.uint8 and t["exps"].numel() < 2 * -(-n // 256):
-            raise ValueError("adamw_tensors: exps holds two exponents per 256 elements")
+        if t["m"].dtype == torch.uint8:
+            e = t.get("exps")
+            if e is None or e.dtype != torch.uint8 or not e.is_contiguous() or e.numel() < 2 * -(-n // 256):
+                raise ValueError("adamw_tensors: exps holds two exponents per 256 elements, contiguous uint8")
+        if any(t[k].device != tensors[0]["param"].device for k in t if isinstance(t[k], torch.Tensor)):
+            raise ValueError("adamw_tensors: tensors on more than one device")
         for k in ("param", "master", "grad", "m", "v", "exps"):
             x = t.get(k)
             setattr(d, k, None if x is None else x.data_ptr())

@@ -57,3 +57,34 @@ def test_descriptors_check_their_tensors():
                   exps=torch.zeros(5, dtype=torch.uint8))):
         with pytest.raises(ValueError):
             rdcn.adamw_tensors([bad])
+
+
+def test_descriptors_refuse_types_that_the_kernels_do_not_read():
+    """The kernels go by the descriptor's types: a tensor of 2 bytes an element taken for one of 4 would be read and
+    written past its end."""
+    n = 600
+    f, h, b, u8 = torch.float32, torch.float16, torch.bfloat16, torch.uint8
+
+    def t(eight=False, **types):
+        d = {k: torch.zeros(n, dtype=types.pop(k, f)) for k in ("param", "grad")}
+        d.update({k: torch.zeros(n, dtype=types.pop(k, u8 if eight else f)) for k in ("m", "v")})
+        if eight:
+            d["exps"] = torch.zeros(6, dtype=types.pop("exps", u8))
+        d.update({k: torch.zeros(n, dtype=v) for k, v in types.items()})
+        return d
+
+    fine = [t(), t(param=b), t(grad=b), t(param=b, master=f), t(eight=True), t(eight=True, param=b, grad=b, master=f)]
+    lst = rdcn.adamw_tensors(fine)
+    assert [(x.param_dtype, x.grad_dtype) for x in lst] == [(0, 0), (1, 0), (0, 1), (1, 0), (0, 0), (1, 1)]
+    bad = [t(param=h), t(param=torch.float64), t(grad=h), t(grad=torch.float64), t(param=torch.int32), t(param=h, master=f),
+           t(param=b, master=b), t(param=b, master=h), t(param=b, master=torch.float64), t(master=f), t(m=h, v=h),
+           t(eight=True, exps=torch.int32), t(eight=True, exps=torch.int8),
+           dict(t(eight=True), exps=torch.zeros(12, dtype=u8)[::2]), dict(t(eight=True), exps=None),
+           dict(t(), grad=torch.zeros(n, device="meta")), dict(t(eight=True), exps=torch.zeros(6, dtype=u8, device="meta"))]
+    no_exps = t(eight=True)
+    del no_exps["exps"]
+    for d in bad + [no_exps]:
+        with pytest.raises(ValueError):
+            rdcn.adamw_tensors([d])
+    with pytest.raises(ValueError):
+        rdcn.adamw_tensors([t(), {k: x.to("meta") for k, x in t().items()}])
