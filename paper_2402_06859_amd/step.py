@@ -11,7 +11,7 @@ from typing import Optional, Sequence
 
 import torch
 
-from .rdcn import Rdcn, adamw_tensors, config_for
+from .rdcn import BF16, I64, Rdcn, adamw_tensors, config_for
 from .synth import Workload
 
 _DT = {"bf16": torch.bfloat16, "f32": torch.float32}
@@ -155,8 +155,8 @@ class DeviceHead:
 
 class DeviceClasses:
     """Softmax loss over a large set of classes (items, tokens) on x [B, dim], normally x_L of the
-    handle `lib`: class weights w [classes, dim], labels [B] (below 0: a row without one), their
-    gradients and the call's scratch."""
+    handle `lib`: class weights w [classes, dim] of its storage type, labels [B] of its id type (below 0: a row
+    without one), their gradients and the call's scratch. What does not fit is a ValueError: the kernels go by pointers alone."""
 
     def __init__(self, lib: Rdcn, w: torch.Tensor, labels: torch.Tensor, offset: Optional[torch.Tensor] = None,
                  row_weight: Optional[torch.Tensor] = None, logit_scale: float = 1.0):
@@ -164,6 +164,11 @@ class DeviceClasses:
         self.logit_scale = logit_scale
         self.B = labels.numel()
         self.classes, self.dim = w.shape
+        self._fits("w", w, _DT["bf16" if lib.cfg.dtype == BF16 else "f32"], self.classes * self.dim)
+        self._fits("labels", labels, torch.int64 if lib.cfg.id_type == I64 else torch.int32, self.B)
+        for name, t, n in (("offset", offset, self.classes), ("row_weight", row_weight, self.B)):
+            if t is not None:
+                self._fits(name, t, torch.float32, n)
         dev = w.device
         self.loss = torch.empty(self.B, dtype=torch.float32, device=dev)
         self.lse = torch.empty(self.B, dtype=torch.float32, device=dev)
@@ -172,16 +177,22 @@ class DeviceClasses:
         self.scratch = torch.empty(max(lib.softmax_loss_workspace(self.B, self.dim, self.classes)[:2]),
                                    dtype=torch.uint8, device=dev)
 
+    def _fits(self, name, t, dtype, n):
+        if t.dtype != dtype or t.numel() != n or not t.is_contiguous() or t.device != self.w.device:
+            raise ValueError("DeviceClasses: %s must be %d contiguous values of %s on %s" % (name, n, dtype, self.w.device))
+
     def trained(self):
         return [(self.w, self.grad_w)]
 
     def forward(self, x: torch.Tensor, stream=None):
         """Loss and lse of every row, without gradients."""
+        self._fits("x", x, self.w.dtype, self.B * self.dim)
         self.lib.softmax_loss_forward(self.B, self.dim, self.classes, x, self.w, self.offset, self.labels,
                                       self.logit_scale, self.loss, self.lse, self.scratch, stream)
 
     def loss_grad(self, x: torch.Tensor, scale: Optional[float] = None, stream=None):
         """Loss of every row and the gradients of scale (1 / B) times their (weighted) sum."""
+        self._fits("x", x, self.w.dtype, self.B * self.dim)
         self.lib.softmax_loss_grad(self.B, self.dim, self.classes, x, self.w, self.offset, self.labels,
                                    self.logit_scale, self.row_weight, 1.0 / max(self.B, 1) if scale is None else scale,
                                    self.loss, self.lse, self.grad_x, self.grad_w, self.scratch, stream)

@@ -7,6 +7,7 @@ import pytest
 import torch
 
 from paper_2402_06859_amd import rdcn
+from paper_2402_06859_amd.step import DeviceClasses
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
@@ -88,3 +89,45 @@ def test_descriptors_refuse_types_that_the_kernels_do_not_read():
             rdcn.adamw_tensors([d])
     with pytest.raises(ValueError):
         rdcn.adamw_tensors([t(), {k: x.to("meta") for k, x in t().items()}])
+
+
+class NoDevice:
+    """The library's calls as far as DeviceClasses makes them, without a GPU."""
+
+    def __init__(self, dtype, id_type):
+        self.cfg = rdcn.make_config(8, 4, 16, 32, 8, 1, 25, 25, 600, dtype=dtype, id_type=id_type)
+        self.calls = 0
+
+    def softmax_loss_workspace(self, rows, dim, classes):
+        return 256, 256, 256
+
+    def softmax_loss_forward(self, *a):
+        self.calls += 1
+
+    softmax_loss_grad = softmax_loss_forward
+
+
+@pytest.mark.parametrize("dtype,id_type", [("bf16", "i64"), ("bf16", "i32"), ("f32", "i64"), ("f32", "i32")])
+def test_classes_refuse_tensors_that_the_kernels_would_read_past(dtype, id_type):
+    B, dim, V = 6, 16, 10
+    dt, other = (torch.bfloat16, torch.float32) if dtype == "bf16" else (torch.float32, torch.bfloat16)
+    it, wrong = (torch.int64, torch.int32) if id_type == "i64" else (torch.int32, torch.int64)
+    lib = NoDevice(dtype, id_type)
+    w, y = torch.zeros(V, dim, dtype=dt), torch.zeros(B, dtype=it)
+    dc = DeviceClasses(lib, w, y, offset=torch.zeros(V), row_weight=torch.ones(B))
+    x = torch.zeros(B, dim, dtype=dt)
+    dc.forward(x)
+    dc.loss_grad(x)
+    assert lib.calls == 2
+    for bad in (x.to(other), x[:5], torch.zeros(B, dim + 8, dtype=dt), torch.zeros(B, 2 * dim, dtype=dt)[:, ::2],
+                torch.zeros(B, 2 * dim, dtype=dt)[:, :dim], x.to("meta")):
+        for call in (dc.forward, dc.loss_grad):
+            with pytest.raises(ValueError):
+                call(bad)
+    for kw in (dict(w=w.to(other)), dict(w=w.half()), dict(w=torch.zeros(dim, V, dtype=dt).t()), dict(labels=y.to(wrong)),
+               dict(labels=y.float()), dict(labels=torch.zeros(2 * B, dtype=it)[::2]), dict(offset=torch.zeros(V - 1)),
+               dict(offset=torch.zeros(V, dtype=torch.bfloat16)), dict(row_weight=torch.ones(B, dtype=torch.float64)),
+               dict(row_weight=torch.ones(B - 1)), dict(labels=y.to("meta"))):
+        with pytest.raises(ValueError):
+            DeviceClasses(**{**dict(lib=lib, w=w, labels=y), **kw})
+    assert lib.calls == 2
