@@ -582,7 +582,8 @@ typedef struct rdcn_adamw_config {
     const int64_t* device_step;    /* or NULL; the same for step (values below 1 count as 1). With these
                                       a captured step follows its schedule without being captured again */
     const float* clip;             /* or NULL; device memory, one float (rdcn_grad_norm's out + 1). A value that is
-                                      not finite leaves every weight and moment as it is */
+                                      not finite leaves every weight and moment as it is: such a step does not
+                                      count in t, so advance device_step only where the value is finite */
     int32_t stochastic;            /* 0 or 1 */
     uint32_t seed;
 } rdcn_adamw_config;

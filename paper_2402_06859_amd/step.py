@@ -213,7 +213,8 @@ class DeviceClasses:
 class DeviceAdamW:
     """AdamW over (weight, gradient) pairs: moments in float or 8 bits, float masters of bf16 weights or none, and
     the gradients clipped to max_norm together. Rate and step number stand on the device, so that an update
-    can be captured in a graph: change lr with set_lr."""
+    can be captured in a graph: change lr with set_lr. With max_norm, an update whose gradients' norm is not finite
+    is left out whole: weights, moments and the step number stay."""
 
     def __init__(self, lib: Rdcn, pairs: Sequence, lr: float, weight_decay: float = 0.0, moments: str = "f32",
                  master: bool = True, max_norm: Optional[float] = None, beta1: float = 0.9, beta2: float = 0.999,
@@ -236,6 +237,7 @@ class DeviceAdamW:
         self.lr = torch.full((1,), lr, dtype=torch.float32, device=dev)
         self.steps = torch.zeros(1, dtype=torch.int64, device=dev)
         self.norm = torch.zeros(2, dtype=torch.float32, device=dev)   # norm of the gradients, clip factor
+        self.taken = torch.zeros(1, dtype=torch.bool, device=dev)     # whether the update is taken
         self.scratch = torch.empty(max(256, lib.grad_norm_workspace(self.list)), dtype=torch.uint8, device=dev)
 
     def set_lr(self, lr: float, stream=None):
@@ -243,11 +245,14 @@ class DeviceAdamW:
             self.lr.fill_(lr)
 
     def update(self, stream=None):
-        with _on(stream):
-            self.steps.add_(1)
         clip = None
         if self.max_norm is not None:
             self.lib.grad_norm(self.list, 1.0, self.max_norm, self.norm, self.scratch, stream)
             clip = self.norm[1:]
+        with _on(stream):
+            if clip is None:
+                self.steps.add_(1)
+            else:  # (the factor is NaN where the norm is not finite; a step that is not taken has no part in 1 - beta^t)
+                self.steps.add_(torch.eq(clip, clip, out=self.taken))
         self.lib.adamw_step(self.list, lr=0.0, device_lr=self.lr, device_step=self.steps, clip=clip, stream=stream,
                             **self.hyper)

@@ -123,3 +123,38 @@ def test_a_gradient_that_is_not_finite_changes_nothing():
     torch.cuda.synchronize()
     assert all(torch.equal(a, b) for a, b in zip(before, [t[k] for t in do.tensors for k in ("param", "m", "v")]))
     assert db.lib.check_device_errors() == rdcn.RDCN_OK
+
+
+@pytest.mark.parametrize("opt", [dict(), dict(moments="8bit", master=False)])
+@pytest.mark.parametrize("captured", [False, True])
+def test_an_update_that_is_left_out_does_not_count(opt, captured):
+    """Updates with a gradient that is not finite, before the first one and between others, leave the step number (and with it
+    the bias corrections and the random bits) of the ones that are taken as if they had not been: the same bits."""
+    need_gpu()
+    _, db, dc, do = build(max_norm=1.0, **opt)
+    _, db2, dc2, do2 = build(max_norm=1.0, **opt)
+    for d, c in ((db, dc), (db2, dc2)):
+        c.train_step(d)
+    update = do.update
+    if captured:
+        start = [x.clone() for x in state(db, dc, do)]
+        graph = torch.cuda.CUDAGraph()
+        do.update()
+        torch.cuda.synchronize()
+        with torch.cuda.graph(graph):
+            do.update()
+        for x, s in zip(state(db, dc, do), start):
+            x.copy_(s)
+        update = graph.replay
+    fine = float(dc.grad_w[3, 5])
+    taken = 0
+    for bad in (float("nan"), float("inf"), 0.0, -float("inf"), float("nan"), 0.0):
+        dc.grad_w[3, 5] = bad if bad else fine
+        update()
+        if not bad:
+            do2.update()
+            taken += 1
+        torch.cuda.synchronize()
+        assert int(do.steps) == taken
+        assert same(state(db, dc, do)[5:], state(db2, dc2, do2)[5:])
+    assert taken == 2 and float(do.norm[1]) > 0
