@@ -495,8 +495,9 @@ rdcn_status rdcn_head_backward(rdcn_handle* h, int64_t batch, const void* x, con
  *   - w has to be finite, in masked classes too: their zero probabilities are
  *     still multiplied with it.
  * dim is a multiple of 8 (bf16 models) or 4 (float); rows <= 2^24, classes <=
- * 2^27, dim <= 2^20, rows * classes <= 2^42, else RDCN_ERR_UNSUPPORTED. x, w, grad_x and
- * grad_w must be 16-byte aligned (RDCN_ERR_ARG otherwise); rows may be 0 (the
+ * 2^27, dim <= 2^20, and each of [rows, classes], x and w of less than 2^24 blocks of 64 x 64 elements in float models
+ * and less than 2^23 of 128 x 128 in bf16 ones ([rows, classes] more, where the logits' own blocks are larger: up to 2^39
+ * elements), else RDCN_ERR_UNSUPPORTED. x, w, grad_x and grad_w must be 16-byte aligned (RDCN_ERR_ARG otherwise); rows may be 0 (the
  * forward then does nothing, the gradient sets grad_w to 0).
  */
 

@@ -442,9 +442,14 @@ SoftPlan soft_plan(const rdcn_handle* h, int64_t rows, int64_t dim, int64_t clas
 rdcn_status check_soft(const rdcn_handle* h, int64_t rows, int64_t dim, int64_t classes) {
     if (!h || rows < 0 || dim <= 0 || classes <= 0) return RDCN_ERR_ARG;
     if (dim % (h->bf16 ? 8 : 4)) return RDCN_ERR_UNSUPPORTED;
-    if (rows > ((int64_t)1 << 24) || dim > ((int64_t)1 << 20) || classes > ((int64_t)1 << 27) ||
-        rows * classes > (int64_t)1 << 42)  // 64 x 64 blocks stay below 2^31
-        return RDCN_ERR_UNSUPPORTED;
+    if (rows > ((int64_t)1 << 24) || dim > ((int64_t)1 << 20) || classes > ((int64_t)1 << 27)) return RDCN_ERR_UNSUPPORTED;
+    // The products' grids. Logits: as planned (a piece's have 2^34 elements at most). Gradients: float 64 x 64 blocks; bf16
+    // 128 x 128 or larger wherever there are many, so less than 2^23 of those keep any plan below 2^32 threads (512 in a block
+    // of 256 rows).
+    const int64_t side = h->bf16 ? 128 : 64, most = (int64_t)1 << (h->bf16 ? 23 : 24);
+    for (int64_t n : {rows, classes})
+        if (((n + side - 1) / side) * ((dim + side - 1) / side) >= most) return RDCN_ERR_UNSUPPORTED;
+    if (rows > 0 && !gemm_fits_grid(rows, classes, plan_logits(h, rows, classes, dim), h->bf16)) return RDCN_ERR_UNSUPPORTED;
     return RDCN_OK;
 }
 

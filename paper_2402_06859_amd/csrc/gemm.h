@@ -117,6 +117,8 @@ inline GemmPlan plan_f32_lds() {
     p.stages = F32_LDS_STAGES;
     return p;
 }
+// Whether a product's grid is one that can be launched: less than 2^32 threads along x.
+bool gemm_fits_grid(int64_t M, int64_t N, const GemmPlan& p, bool bf16);
 // plan_gemm (K may be split) for one long product at a time on the whole chip, whose partial sums the caller reduces.
 GemmPlan plan_gemm_long(int64_t M, int64_t N, int64_t K, bool bf16);
 hipError_t launch_gemm(const GemmArgs& g, const GemmPlan& p, bool bf16, hipStream_t s);

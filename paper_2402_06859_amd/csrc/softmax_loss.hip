@@ -248,7 +248,7 @@ hipError_t launch_soft_rows(const SoftRows& a, bool bf16, hipStream_t s) {
 bool soft_row_at_once(int64_t rows, int64_t tiles, int64_t ld) {
     // a workgroup per row has to fill the chip, unless rows are short; pairs of one row lie far apart (us, at once / apart:
     // 157 pairs of 512 rows 8.4 / 11, 500 of 4096 132 / 105)
-    return tiles <= 192 && (rows >= 256 || ld <= 8192);
+    return tiles <= 192 && (rows >= 256 || ld <= 8192) && rows < 1 << 24;  // (a grid has less than 2^32 threads)
 }
 
 hipError_t launch_soft_row(const SoftRows& a, const SoftNorm& n, bool bf16, hipStream_t s) {
