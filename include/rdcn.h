@@ -551,13 +551,18 @@ rdcn_status rdcn_softmax_loss_grad(rdcn_handle* h, int64_t rows, int64_t dim, in
  * whose bits are (c + base) << 20, code 0 for zero; m's sign is bit 7. So three
  * mantissa bits, reaching 2^-15 (m) or 2^-31 (v) below the block's largest; a
  * nonzero v has at least code 1. Zeros are the state to begin with.
- * stochastic = 1 rounds codes, and bf16 weights without a master, up with the
- * probability of what is cut off (under rounding to nearest, 0, small steps of a
- * moving average in 8 bits would all be lost). Its random bits are a hash of
+ * stochastic (rdcn_rounding): RDCN_ROUND_CHANCE rounds codes, and bf16 weights without a master, up with the
+ * probability of what is cut off (under rounding to nearest small steps of a
+ * moving average in 8 bits would all be lost). A code past the block's last one becomes that last
+ * one, 1.875 times 2 to the block's exponent, and a block's largest elements cannot leave it by small steps: a v of normal gradients
+ * settles at about half of its value. RDCN_ROUND_CHANCE_CARRY, the one to train with, raises the
+ * block's exponent by one there, for all of its codes; moments then keep the mean that they have in float.
+ * The random bits are a hash of
  * seed, the tensor's place in the list and the element's place (modulo 2^32): pass another
  * seed each step (with device_step, t * 0x85EBCA6B is added to it, so that a replayed step
  * draws anew). The result depends on the arguments alone.
  */
+typedef enum rdcn_rounding { RDCN_ROUND_NEAREST = 0, RDCN_ROUND_CHANCE = 1, RDCN_ROUND_CHANCE_CARRY = 3 } rdcn_rounding;
 typedef enum rdcn_moments { RDCN_MOMENTS_F32 = 0, RDCN_MOMENTS_8BIT = 1 } rdcn_moments;
 
 typedef struct rdcn_adamw_tensor {
@@ -585,7 +590,7 @@ typedef struct rdcn_adamw_config {
     const float* clip;             /* or NULL; device memory, one float (rdcn_grad_norm's out + 1). A value that is
                                       not finite leaves every weight and moment as it is: such a step does not
                                       count in t, so advance device_step only where the value is finite */
-    int32_t stochastic;            /* 0 or 1 */
+    int32_t stochastic;            /* rdcn_rounding */
     uint32_t seed;
 } rdcn_adamw_config;
 

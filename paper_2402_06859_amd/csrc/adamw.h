@@ -30,7 +30,7 @@ struct AdamwScalars {
     const int64_t* device_step;       // or NULL
     const float* clip;                // or NULL
     float grad_scale;
-    bool stochastic;
+    bool stochastic, carry;
     uint32_t seed;
 };
 

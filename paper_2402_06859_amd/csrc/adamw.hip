@@ -15,7 +15,10 @@
 // step is 1 - beta = 0.1 or 0.001 would stand still under rounding to nearest (half a step is 1/16 to 1/32 of the
 // value), so codes are rounded up with the probability of the part that is cut off: the bits below 20
 // are added to 20 random bits, a hash of (seed, tensor, element). bf16 weights without a float master
-// are rounded the same way, for the same reason.
+// are rounded the same way, for the same reason. With `carry` a block's exponent goes up by one where that takes an element
+// past its last code. Without, the block's largest elements stand still at that code, 1.875 of their binade, as long as no single
+// step leaves the binade: v of gradients of one size then stays at 0.03 of its value, of normal ones at half of it. (585 M
+// elements, without / with: 1299 / 1298 us.)
 #include "adamw.h"
 #include "device_common.h"
 
@@ -229,18 +232,39 @@ __device__ __forceinline__ void adamw_elements(const AdamwTensor& t, const Adamw
             mm = max(mm, um[e]);
             mv = max(mv, uv[e]);
         }
-        const uint32_t em = max_of_block(mm) >> 23, ev = max_of_block(mv) >> 23;
+        uint32_t em = max_of_block(mm) >> 23, ev = max_of_block(mv) >> 23;
         const uint32_t bm = 0u - (code_base(em, 127) << 20), bv = 0u - (code_base(ev, 255) << 20);
-        uint32_t cm[EPT], cv[EPT];
+        int x[EPT], y[EPT];
 #pragma unroll
         for (int e = 0; e < EPT; ++e) {
             const uint32_t rm = a.stochastic ? h[e] >> 12 : 0x80000u;
             const uint32_t rv = a.stochastic ? (h[e] * 0x9E3779B1u) >> 12 : 0x80000u;
             // (a value of the block is at most 8 2^20 above its exponent's base + top: the differences fit an int; of a
             // zero and what lies below the reach they are negative or round to 0)
-            const int x = (int)(um[e] + rm + bm) >> 20, y = (int)(uv[e] + rv + bv) >> 20;
-            cm[e] = (uint32_t)min(max(x, 0), 127) | (__float_as_uint(m[e]) >> 24 & 128u);
-            cv[e] = (uint32_t)min(max(y, (int)min(uv[e], 1u)), 255);
+            x[e] = (int)(um[e] + rm + bm) >> 20;
+            y[e] = (int)(uv[e] + rv + bv) >> 20;
+        }
+        if (a.carry) {  // a code past the last one: the block's exponent is one more, its codes count from 8 further up
+            int mx = x[0], my = y[0];
+#pragma unroll
+            for (int e = 1; e < EPT; ++e) mx = max(mx, x[e]), my = max(my, y[e]);
+            const uint64_t px = __ballot(mx > 127), py = __ballot(my > 255);
+            if (px | py) {  // (about a step in ten, of the two blocks of a wave)
+                const bool ux = (uint32_t)(px >> (threadIdx.x & 32)) && em < 254, uy = (uint32_t)(py >> (threadIdx.x & 32)) && ev < 254;
+                em += ux;  // (past 254 there is no value)
+                ev += uy;
+#pragma unroll
+                for (int e = 0; e < EPT; ++e) {
+                    x[e] -= ux ? 8 : 0;
+                    y[e] -= uy ? 8 : 0;
+                }
+            }
+        }
+        uint32_t cm[EPT], cv[EPT];
+#pragma unroll
+        for (int e = 0; e < EPT; ++e) {
+            cm[e] = (uint32_t)min(max(x[e], 0), 127) | (__float_as_uint(m[e]) >> 24 & 128u);
+            cv[e] = (uint32_t)min(max(y[e], (int)min(uv[e], 1u)), 255);
         }
         store_codes<WHOLE>((uint8_t*)t.m + at, left, cm);
         store_codes<WHOLE>((uint8_t*)t.v + at, left, cv);

@@ -1452,7 +1452,8 @@ rdcn_status rdcn_adamw_step(rdcn_handle* h, const rdcn_adamw_config* cfg, const 
     const rdcn_adamw_config& c = *cfg;
     if (!std::isfinite((float)c.lr) || !(c.beta1 >= 0.0 && c.beta1 < 1.0) || !(c.beta2 >= 0.0 && c.beta2 < 1.0) ||
         !((float)c.eps >= FLT_MIN) || !std::isfinite((float)c.eps) || !std::isfinite((float)c.grad_scale) ||
-        (!c.device_step && c.step < 1) || (c.stochastic != 0 && c.stochastic != 1))
+        (!c.device_step && c.step < 1) ||
+        (c.stochastic != RDCN_ROUND_NEAREST && c.stochastic != RDCN_ROUND_CHANCE && c.stochastic != RDCN_ROUND_CHANCE_CARRY))
         return RDCN_ERR_ARG;
     rdcn_status st = check_tensors(h, tensors, count);
     if (st != RDCN_OK) return st;
@@ -1473,7 +1474,8 @@ rdcn_status rdcn_adamw_step(rdcn_handle* h, const rdcn_adamw_config* cfg, const 
     a.step = c.step;
     a.device_lr = c.device_lr; a.device_step = c.device_step; a.clip = c.clip;
     a.grad_scale = (float)c.grad_scale;
-    a.stochastic = c.stochastic != 0;
+    a.stochastic = c.stochastic != RDCN_ROUND_NEAREST;
+    a.carry = c.stochastic == RDCN_ROUND_CHANCE_CARRY;
     a.seed = c.seed;
     return hip_status(launch_adamw(l.t, count, a, (hipStream_t)stream));
 }

@@ -22,6 +22,7 @@ F32, BF16 = 0, 1
 I32, I64 = 0, 1
 COMBINE_MUL, COMBINE_SUM = 0, 1
 MOMENTS_F32, MOMENTS_8BIT = 0, 1
+ROUND_CARRY = 2   # with stochastic: RDCN_ROUND_CHANCE_CARRY
 ACT_MODES = {"storage": 0, "hilo": 1, "f16": 2}   # rdcn_act_mode
 
 EXPORTS = ["rdcn_create", "rdcn_destroy", "rdcn_dim", "rdcn_workspace_bytes", "qr_embed_gather",
@@ -397,9 +398,9 @@ class Rdcn:
                                                        _ptr(scratch), _bytes(scratch), _stream(stream)))
 
     def adamw_step(self, tensors, lr, beta1=0.9, beta2=0.999, eps=1e-8, step=1, grad_scale=1.0, clip=None,
-                   stochastic=False, seed=0, device_lr=None, device_step=None, stream=None):
+                   stochastic=False, seed=0, device_lr=None, device_step=None, stream=None, carry=False):
         c = RdcnAdamwConfig(lr, beta1, beta2, eps, grad_scale, step, _ptr(device_lr), _ptr(device_step), _ptr(clip),
-                            int(stochastic), seed & 0xFFFFFFFF)
+                            int(stochastic) | (ROUND_CARRY if carry else 0), seed & 0xFFFFFFFF)
         _check("rdcn_adamw_step", load().rdcn_adamw_step(self.h, ctypes.byref(c), tensors, len(tensors),
                                                          _stream(stream)))
 

@@ -220,7 +220,7 @@ class DeviceAdamW:
                  master: bool = True, max_norm: Optional[float] = None, beta1: float = 0.9, beta2: float = 0.999,
                  eps: float = 1e-8, seed: int = 0):
         self.lib, self.max_norm = lib, max_norm
-        self.hyper = dict(beta1=beta1, beta2=beta2, eps=eps, stochastic=True, seed=seed)
+        self.hyper = dict(beta1=beta1, beta2=beta2, eps=eps, stochastic=True, carry=True, seed=seed)
         self.tensors = []
         for p, g in pairs:
             n, dev = p.numel(), p.device
