@@ -211,7 +211,8 @@ class DeviceClasses:
 
 
 class DeviceAdamW:
-    """AdamW over (weight, gradient) pairs: moments in float or 8 bits, float masters of bf16 weights or none, and
+    """AdamW over (weight, gradient) pairs, or (weight, gradient, weight_decay) where a weight has a decay of its own (an
+    embedding table often none); the others decay by weight_decay if they have more than one dimension. Moments in float or 8 bits, float masters of bf16 weights or none, and
     the gradients clipped to max_norm together. Rate and step number stand on the device, so that an update
     can be captured in a graph: change lr with set_lr. With max_norm, an update whose gradients' norm is not finite
     is left out whole: weights, moments and the step number stay."""
@@ -222,11 +223,11 @@ class DeviceAdamW:
         self.lib, self.max_norm = lib, max_norm
         self.hyper = dict(beta1=beta1, beta2=beta2, eps=eps, stochastic=True, carry=True, seed=seed)
         self.tensors = []
-        for p, g in pairs:
+        for p, g, *own in pairs:
             n, dev = p.numel(), p.device
             mt = torch.uint8 if moments == "8bit" else torch.float32
             t = {"param": p, "grad": g, "m": torch.zeros(n, dtype=mt, device=dev),
-                 "v": torch.zeros(n, dtype=mt, device=dev), "weight_decay": weight_decay if p.dim() > 1 else 0.0}
+                 "v": torch.zeros(n, dtype=mt, device=dev), "weight_decay": own[0] if own else weight_decay if p.dim() > 1 else 0.0}
             if moments == "8bit":
                 t["exps"] = torch.zeros(2 * -(-n // 256), dtype=torch.uint8, device=dev)
             if master and p.dtype == torch.bfloat16:

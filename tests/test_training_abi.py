@@ -7,7 +7,7 @@ import pytest
 import torch
 
 from paper_2402_06859_amd import rdcn
-from paper_2402_06859_amd.step import DeviceClasses
+from paper_2402_06859_amd.step import DeviceAdamW, DeviceClasses
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
@@ -106,6 +106,9 @@ class NoDevice:
 
     softmax_loss_grad = softmax_loss_forward
 
+    def grad_norm_workspace(self, tensors):
+        return 256
+
 
 @pytest.mark.parametrize("dtype,id_type", [("bf16", "i64"), ("bf16", "i32"), ("f32", "i64"), ("f32", "i32")])
 def test_classes_refuse_tensors_that_the_kernels_would_read_past(dtype, id_type):
@@ -131,3 +134,10 @@ def test_classes_refuse_tensors_that_the_kernels_would_read_past(dtype, id_type)
         with pytest.raises(ValueError):
             DeviceClasses(**{**dict(lib=lib, w=w, labels=y), **kw})
     assert lib.calls == 2
+
+
+def test_weights_with_a_decay_of_their_own():
+    pair = lambda *shape: (torch.zeros(shape), torch.zeros(shape))
+    opt = DeviceAdamW(NoDevice("f32", "i64"), [pair(4, 8), pair(8), (*pair(100, 4), 0.0), (*pair(8), 0.5), (*pair(4, 8), 0.25)],
+                      lr=1e-3, weight_decay=0.125)
+    assert [t.weight_decay for t in opt.list] == [0.125, 0.0, 0.0, 0.5, 0.25]
