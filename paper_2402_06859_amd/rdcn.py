@@ -219,10 +219,17 @@ def _bytes(t: Optional[torch.Tensor]) -> int:
     return 0 if t is None else t.numel() * t.element_size()
 
 
+# The raw handle of torch's current stream, which the object around it takes 2.7 us more to build: not part of torch's
+# public interface, so a version without it takes the object.
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+_raw_device = getattr(torch._C, "_cuda_getDevice", None)
+
+
 def _stream(stream=None):
-    # (the raw handle of torch's current stream; the object around it takes 2.7 us more to build)
     if stream is None:
-        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+        if _raw_stream is not None and _raw_device is not None:
+            return _raw_stream(_raw_device())
+        stream = torch.cuda.current_stream()
     return stream.cuda_stream
 
 

@@ -141,3 +141,13 @@ def test_weights_with_a_decay_of_their_own():
     opt = DeviceAdamW(NoDevice("f32", "i64"), [pair(4, 8), pair(8), (*pair(100, 4), 0.0), (*pair(8), 0.5), (*pair(4, 8), 0.25)],
                       lr=1e-3, weight_decay=0.125)
     assert [t.weight_decay for t in opt.list] == [0.125, 0.0, 0.0, 0.5, 0.25]
+
+
+@pytest.mark.parametrize("name", ["_raw_stream", "_raw_device"])
+def test_the_current_stream_without_torchs_private_calls(name, monkeypatch):
+    class Stream:
+        cuda_stream = 77
+
+    monkeypatch.setattr(rdcn, name, None)
+    monkeypatch.setattr(torch.cuda, "current_stream", Stream)
+    assert rdcn._stream() == 77 and rdcn._stream(Stream()) == 77
