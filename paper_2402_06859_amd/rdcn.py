@@ -215,6 +215,11 @@ def _ptr(t: Optional[torch.Tensor]):
     return None if t is None else t.data_ptr()
 
 
+def _fits(fn: str, name: str, t: torch.Tensor, dtype: torch.dtype, n: int):
+    if t.dtype != dtype or t.numel() < n or not t.is_contiguous():
+        raise ValueError("%s: %s must be contiguous %s, %d or more" % (fn, name, dtype, n))
+
+
 def _bytes(t: Optional[torch.Tensor]) -> int:
     return 0 if t is None else t.numel() * t.element_size()
 
@@ -401,11 +406,18 @@ class Rdcn:
 
     def grad_norm(self, tensors, grad_scale, max_norm, out, scratch, stream=None):
         """out (float [2]): the norm of all gradients of `tensors` (adamw_tensors) and the factor that clips it."""
+        _fits("grad_norm", "out", out, torch.float32, 2)
         _check("rdcn_grad_norm", load().rdcn_grad_norm(self.h, tensors, len(tensors), grad_scale, max_norm, _ptr(out),
                                                        _ptr(scratch), _bytes(scratch), _stream(stream)))
 
     def adamw_step(self, tensors, lr, beta1=0.9, beta2=0.999, eps=1e-8, step=1, grad_scale=1.0, clip=None,
                    stochastic=False, seed=0, device_lr=None, device_step=None, stream=None, carry=False):
+        """One step over `tensors` (adamw_tensors). On the device: device_lr (float) and device_step (int64) in place of lr and
+        step, and clip (float), the factor that grad_norm leaves. carry: with 8-bit moments, the rounding to train with."""
+        for name, t, dtype in (("device_lr", device_lr, torch.float32), ("device_step", device_step, torch.int64),
+                               ("clip", clip, torch.float32)):
+            if t is not None:
+                _fits("adamw_step", name, t, dtype, 1)
         c = RdcnAdamwConfig(lr, beta1, beta2, eps, grad_scale, step, _ptr(device_lr), _ptr(device_step), _ptr(clip),
                             int(stochastic) | (ROUND_CARRY if carry else 0), seed & 0xFFFFFFFF)
         _check("rdcn_adamw_step", load().rdcn_adamw_step(self.h, ctypes.byref(c), tensors, len(tensors),
@@ -413,8 +425,15 @@ class Rdcn:
 
     def adamw_values(self, codes, exps, signed: bool, out=None, stream=None):
         """The values (bf16) that 8-bit moments stand for."""
-        out = torch.empty(codes.shape, dtype=torch.bfloat16, device=codes.device) if out is None else out
-        _check("rdcn_adamw_values", load().rdcn_adamw_values(self.h, codes.numel(), _ptr(codes), _ptr(exps), int(signed),
+        n = codes.numel()
+        if (codes.dtype is not torch.uint8 or exps.dtype is not torch.uint8 or exps.numel() * 256 < n or
+                not codes.is_contiguous() or not exps.is_contiguous()):
+            raise ValueError("adamw_values: codes and one exponent for 256 of them, both contiguous uint8")
+        if out is None:
+            out = torch.empty(codes.shape, dtype=torch.bfloat16, device=codes.device)
+        else:
+            _fits("adamw_values", "out", out, torch.bfloat16, n)
+        _check("rdcn_adamw_values", load().rdcn_adamw_values(self.h, n, _ptr(codes), _ptr(exps), int(signed),
                                                              _ptr(out), _stream(stream)))
         return out
 

@@ -151,3 +151,29 @@ def test_the_current_stream_without_torchs_private_calls(name, monkeypatch):
     monkeypatch.setattr(rdcn, name, None)
     monkeypatch.setattr(torch.cuda, "current_stream", Stream)
     assert rdcn._stream() == 77 and rdcn._stream(Stream()) == 77
+
+
+def test_small_arguments_of_other_types_are_refused(monkeypatch):
+    """What the kernels read as one float, one int64 or a byte per value and block."""
+    lib = object.__new__(rdcn.Rdcn)  # a handle that refuses: nothing is launched
+    lib.h = None
+    lst = rdcn.adamw_tensors([{k: torch.zeros(300) for k in ("param", "grad", "m", "v")}])
+    z = lambda n, dtype=torch.float32: torch.zeros(n, dtype=dtype)
+    u8, bf16 = torch.uint8, torch.bfloat16
+    monkeypatch.setattr(rdcn, "_stream", lambda stream=None: None)
+    for fine in (lambda: lib.grad_norm(lst, 1.0, 1.0, z(2), z(64)),
+                 lambda: lib.adamw_step(lst, 1e-3, device_lr=z(1), device_step=z(1, torch.int64), clip=z(1)),
+                 lambda: lib.adamw_values(z(300, u8), z(2, u8), True, z(300, bf16))):
+        with pytest.raises(rdcn.RdcnError):  # the library's own refusal, of the handle
+            fine()
+    for bad in (lambda: lib.grad_norm(lst, 1.0, 1.0, z(1), z(64)), lambda: lib.grad_norm(lst, 1.0, 1.0, z(2, bf16), z(64)),
+                lambda: lib.adamw_step(lst, 1e-3, device_lr=z(1, bf16)),
+                lambda: lib.adamw_step(lst, 1e-3, device_step=z(1, torch.int32)),
+                lambda: lib.adamw_step(lst, 1e-3, device_step=z(0, torch.int64)),
+                lambda: lib.adamw_step(lst, 1e-3, clip=z(1, torch.float64)),
+                lambda: lib.adamw_values(z(300, torch.int32), z(2, u8), True),
+                lambda: lib.adamw_values(z(300, u8), z(1, u8), True), lambda: lib.adamw_values(z(600, u8)[::2], z(2, u8), True),
+                lambda: lib.adamw_values(z(300, u8), z(2, u8), True, z(300)),
+                lambda: lib.adamw_values(z(300, u8), z(2, u8), True, z(299, bf16))):
+        with pytest.raises(ValueError):
+            bad()
