@@ -216,7 +216,7 @@ def _ptr(t: Optional[torch.Tensor]):
 
 
 def _fits(fn: str, name: str, t: torch.Tensor, dtype: torch.dtype, n: int):
-    if t.dtype != dtype or t.numel() < n or not t.is_contiguous():
+    if t.dtype is not dtype or t.numel() < n or not t.is_contiguous():
         raise ValueError("%s: %s must be contiguous %s, %d or more" % (fn, name, dtype, n))
 
 
@@ -414,10 +414,12 @@ class Rdcn:
                    stochastic=False, seed=0, device_lr=None, device_step=None, stream=None, carry=False):
         """One step over `tensors` (adamw_tensors). On the device: device_lr (float) and device_step (int64) in place of lr and
         step, and clip (float), the factor that grad_norm leaves. carry: with 8-bit moments, the rounding to train with."""
-        for name, t, dtype in (("device_lr", device_lr, torch.float32), ("device_step", device_step, torch.int64),
-                               ("clip", clip, torch.float32)):
-            if t is not None:
-                _fits("adamw_step", name, t, dtype, 1)
+        if clip is not None:
+            _fits("adamw_step", "clip", clip, torch.float32, 1)
+        if device_lr is not None:
+            _fits("adamw_step", "device_lr", device_lr, torch.float32, 1)
+        if device_step is not None:
+            _fits("adamw_step", "device_step", device_step, torch.int64, 1)
         c = RdcnAdamwConfig(lr, beta1, beta2, eps, grad_scale, step, _ptr(device_lr), _ptr(device_step), _ptr(clip),
                             int(stochastic) | (ROUND_CARRY if carry else 0), seed & 0xFFFFFFFF)
         _check("rdcn_adamw_step", load().rdcn_adamw_step(self.h, ctypes.byref(c), tensors, len(tensors),
