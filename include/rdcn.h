@@ -520,7 +520,7 @@ rdcn_status rdcn_softmax_loss_forward(rdcn_handle* h, int64_t rows, int64_t dim,
  * grad_x = G w, grad_w = G^T x. bf16 models round G to bf16 for the matrix
  * products (half a step, 2^-8 of an element) and each gradient once at the end; sums are float and
  * in a fixed order (deterministic). Where they keep all exponentials (below), those are in f16: 2^-11 of an
- * element more, growing from 2^-29 of the largest of the 16 to 64 classes around it on, and 0 below 2^-40.
+ * element more, growing from 2^-29 of the largest of the 16 to 64 classes around it (but the label) on, and 0 below 2^-40.
  * The label's element, scale * weight * logit_scale * (p - 1), and the loss are taken from the sum of the other
  * classes' exponentials: they keep their digits where p is near 1, in float models too.
  * G stands in scratch. With grad_bytes of it (rdcn_softmax_loss_workspace) the call is fastest: G of all

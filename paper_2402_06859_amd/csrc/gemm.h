@@ -22,8 +22,8 @@ enum GemmEpi {
                         // else c = v * [act[m, n] > 0] * (rowg ? sigmoid(rowg[m]) : 1), and with
                         // rowpart: rowpart[(n0 / BN) * M + m] = sum over the tile's columns of v * act
     // Softmax loss (both operands K-contiguous), z = scale*acc + offset[n], -inf where offset[n] is:
-    EPI_SOFT_FWD = 8,   // softpart[t * M + m] over column tile t (gemm_soft_tiles) = (max, sum of exp(z - max) without
-                        // the row's label); zlabel[m] = z at the label, if it is one of the tile's columns; with c:
+    EPI_SOFT_FWD = 8,   // softpart[t * M + m] over the classes of column tile t (gemm_soft_tiles) other than the row's
+                        // label = (max, sum of exp(z - max)); zlabel[m] = z at the label, if it is one of the tile's columns; with c:
                         // c = exp(z - max) (f16 times SOFT_E_SCALE, or float), zero at the label and in the pad of a row
     EPI_SOFT_GRAD = 9   // c = r.c * exp(z - r.max) for r = softrow[m], r.label at the row's label (storage type), zero
                         // where r.c is 0 or z is -inf and in the pad of a row
@@ -33,8 +33,8 @@ enum GemmEpi {
 // 2^-29 of the row's largest in the tile keep all 11 bits, down to 2^-39 they are not zero.
 constexpr float SOFT_E_SCALE = 32768.f;
 
-// A row of the softmax loss. With f its gradient factor and S its sum of exp(z - max): c = f / S, and label =
-// -f (S - the label's own exponential) / S, the gradient in the label's logit: f (p - 1), which a subtraction of 1
+// A row of the softmax loss. With f its gradient factor, max its largest logit and S its sum of exp(z - max): c = f / S, and
+// label = -f (S - the label's own exponential) / S, the gradient in the label's logit: f (p - 1), which a subtraction of 1
 // from p, or a log-sum-exp rounded to float, would leave few digits of where p is near 1.
 struct SoftRow {
     float max, c, label, unused;

@@ -318,6 +318,12 @@ __device__ __forceinline__ void soft_epilogue8(const GemmArgs& g, int64_t m, int
         store8<bf16_t>((bf16_t*)g.c + m * g.ldc + n, v);
         return;
     }
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+        if (lab == e) {
+            g.zlabel[m] = v[e];
+            v[e] = NEG;  // (it joins the row's pairs by itself)
+        }
     float mx = v[0];
 #pragma unroll
     for (int e = 1; e < 8; ++e) mx = fmaxf(mx, v[e]);
@@ -327,10 +333,6 @@ __device__ __forceinline__ void soft_epilogue8(const GemmArgs& g, int64_t m, int
     float sum = 0.f;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-        if (lab == e) {
-            g.zlabel[m] = v[e];
-            v[e] = NEG;  // (its exponential is added where the row's pairs are joined)
-        }
         v[e] = soft_exp<bf16_t>(v[e] - top);
         sum += v[e];
     }
@@ -936,11 +938,6 @@ __device__ __forceinline__ void soft_block_epilogue(const GemmArgs& g, int64_t m
                         if (hit && (int)lab == col(j, q) + e) z = r.label;
                     }
         } else {
-            float mx = v[0];
-#pragma unroll
-            for (int e = 1; e < V; ++e) mx = fmaxf(mx, v[e]);
-#pragma unroll
-            for (int o = MT; o < 64; o <<= 1) mx = fmaxf(mx, __shfl_xor(mx, o));
             if (hit) {
                 float z = 0.f;
 #pragma unroll
@@ -952,11 +949,16 @@ __device__ __forceinline__ void soft_block_epilogue(const GemmArgs& g, int64_t m
                             float& a = v[4 * (j * Q + q) + e];
                             if ((int)lab == col(j, q) + e) {
                                 z = a;
-                                a = NEG;  // (its exponential is added where the row's pairs are joined)
+                                a = NEG;  // (it joins the row's pairs by itself)
                             }
                         }
                 g.zlabel[m] = z;
             }
+            float mx = v[0];
+#pragma unroll
+            for (int e = 1; e < V; ++e) mx = fmaxf(mx, v[e]);
+#pragma unroll
+            for (int o = MT; o < 64; o <<= 1) mx = fmaxf(mx, __shfl_xor(mx, o));
             const float top = mx == NEG ? 0.f : mx;  // (all masked: exp(-inf) = 0 each)
             float sum = 0.f;
 #pragma unroll

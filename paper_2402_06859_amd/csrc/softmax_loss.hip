@@ -8,9 +8,9 @@
 // ranges with maxima a and b is S_a exp(a - c) + S_b exp(b - c) for c = max(a, b).
 //
 // A row stays (maximum, sum) to the end: a difference from lse, rounded to float, is off by |lse| 2^-24 and loses log(sum)
-// itself where all logits are far from 0 (an offset of -10^9 on every class). And the pairs leave the label out:
-// with R the sum over the other classes and e = exp(z[y] - max) the label's, 1 - p = R / (R + e) and loss = log(1 + R / e)
-// keep their digits where p is near 1, which neither p - 1 nor lse - z[y] would.
+// itself where all logits are far from 0 (an offset of -10^9 on every class). And the pairs leave the label out, which joins
+// them last: with R the sum over the other classes and e the label's exponential, 1 - p = R / (R + e) and loss = log(1 + R / e)
+// keep their digits where p is near 1, which neither p - 1 nor lse - z[y] would, and so do the other classes' p.
 #include "device_common.h"
 #include "gemm.h"
 #include "softmax_loss.h"
@@ -59,23 +59,26 @@ __device__ __forceinline__ void copy_kept_rows(const SoftRows& a, int64_t first)
     }
 }
 
-// Row m's gradient from its maximum and the sum over the classes other than its label; `write`: it, loss and lse go out.
-__device__ __forceinline__ SoftRow finish_row(const SoftRows& a, int64_t m, float mx, float rest, bool write) {
+// Row m's gradient from the maximum and sum over the classes other than its label; `write`: it, loss and lse go out.
+__device__ __forceinline__ SoftRow finish_row(const SoftRows& a, int64_t m, float others, float rest, bool write) {
     const int64_t y = label_of(a.labels, a.labels64, m);
     const bool kept = y >= 0 && y < a.classes;
     const float f = a.row && kept ? a.scale * (a.row_weight ? a.row_weight[m] : 1.f) : 0.f;
     const float z = kept ? a.zlabel[m] : NEG_INF;
     const bool seen = z != NEG_INF;  // the row's label has a probability
-    const float own = seen ? expf(z - mx) : 0.f, sum = rest + own;
+    const bool alone = others == NEG_INF && rest == 0.f, none = alone && !seen;  // (a row of NaN has such a maximum, but that sum)
+    const float mx = fmaxf(others, z), own = seen ? expf(z - mx) : 0.f;
+    if (!alone) rest *= expf(others - mx);
+    const float sum = rest + own;
     SoftRow r{};
     r.max = mx;
-    if (f != 0.f && mx != NEG_INF) {
+    if (f != 0.f && !none) {
         r.c = f / sum;
         r.label = seen ? -f * (rest / sum) : 0.f;
     }
     if (write) {
         if (y >= a.classes) atomicOr(a.err, ERR_BIT_INDEX);
-        a.lse[m] = mx == NEG_INF ? NEG_INF : mx + logf(sum);
+        a.lse[m] = none ? NEG_INF : mx + logf(sum);
         // a label whose own class is masked has probability 0: its loss is +inf, also where every class is
         float loss = 0.f;
         if (kept) loss = !seen ? -NEG_INF : rest < own ? log1pf(rest / own) : (mx - z) + logf(sum);

@@ -125,3 +125,63 @@ def test_the_lowest_value_masks_like_minus_infinity(dtype):
         assert all(torch.equal(a, b) for a, b in zip(*got))
         assert (got[1][3][masked.cuda()] == 0).all() and torch.isfinite(got[1][0]).all()
     assert lib.check_device_errors() == rdcn.RDCN_OK
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,classes", [(12, 50), (40, 1500), (200, 1301), (700, 1025)])
+def test_the_other_classes_of_labels_near_probability_one(dtype, rows, classes):
+    """Every class's gradient in the logits, read off in a column of its own (w has 1 there), where the label is up to e^-50 of the
+    way to 1: the classes beside it in a tile keep their digits too. f p for each of the others, with the tolerance above and, for
+    bf16, half a step of f16 (2^-11) besides that of bf16."""
+    need_gpu()
+    print("softmax digits of all classes", dtype, rows, classes, flush=True)
+    lib = handle(dtype)
+    g = torch.Generator().manual_seed(1)
+    n = torch.arange(rows)
+    dim = (classes + rows + 7) // 8 * 8
+    y = torch.randint(0, classes, (rows,), generator=g)
+    b = torch.linspace(0.5, 50.0 / 6, rows).to(DT[dtype])
+    x, w = torch.zeros(rows, dim), torch.zeros(classes, dim)
+    x[n, classes + n] = 8.0
+    w[torch.arange(classes), torch.arange(classes)] = 1.0
+    w[y, classes + n] = b.float()
+    c = dict(x=x.to(DT[dtype]).cuda(), w=w.to(DT[dtype]).cuda(), y=y.cuda(), off=None, wt=None, s=0.75, scale=0.5)
+    z = torch.zeros(rows, classes, dtype=torch.float64)
+    z[n, y] = 0.75 * 8.0 * b.double()
+    p = torch.softmax(z, 1)
+    miss = (classes - 1) * torch.exp(-z[n, y])
+    p[n, y] = -miss / (1 + miss)
+    want = 0.75 * 0.5 * p
+    tol = 4 * U * z.amax(1, keepdim=True) + 2.0 ** -16 + ((1 + 2.0 ** -8) * (1 + 2.0 ** -11) - 1 if dtype == "bf16" else 2 * U)
+    _, most, least = lib.softmax_loss_workspace(rows, dim, classes)
+    for size in (most, least):
+        _, _, gx, _ = call_grad_within(lib, c, rows, dim, classes, size)
+        held("grad_x, %d bytes" % size, gx.cpu()[:, :classes], want, tol * want.abs())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,classes", [(40, 33), (40, 5003), (300, 2001), (1000, 20000)])
+@pytest.mark.parametrize("value", [math.nan, math.inf])
+def test_a_row_that_is_not_finite_is_not_hidden(dtype, rows, classes, value):
+    """Its loss, lse and gradient are NaN, and with them grad_w, so that the norm of the gradients sees it; other rows' results are
+    those of a batch without it."""
+    need_gpu()
+    lib = handle(dtype)
+    dim = 64
+    g = torch.Generator().manual_seed(6)
+    c = dict(x=torch.randn(rows, dim, generator=g).to(DT[dtype]).cuda(), off=None, wt=None, s=0.75, scale=0.25,
+             w=(torch.randn(classes, dim, generator=g) * 0.3).to(DT[dtype]).cuda(),
+             y=torch.randint(0, classes, (rows,), generator=g).cuda())
+    _, most, least = lib.softmax_loss_workspace(rows, dim, classes)
+    for size in sorted({most, least}):
+        clean = call_grad_within(lib, c, rows, dim, classes, size)
+        x = c["x"].clone()
+        x[7] = value
+        got = call_grad_within(lib, dict(c, x=x), rows, dim, classes, size)
+        for a, b in zip(got[:3], clean[:3]):
+            assert torch.isnan(a[7]).all() and torch.isfinite(b).all()
+            a[7] = b[7]
+            assert torch.equal(a, b)
+        assert torch.isnan(got[3]).any()
+        loss, lse = call_forward(lib, dict(c, x=x), rows, dim, classes)
+        assert torch.isnan(loss[7]) and torch.isnan(lse[7]) and int(torch.isnan(loss).sum()) == 1
