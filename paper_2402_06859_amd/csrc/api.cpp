@@ -370,7 +370,7 @@ struct SoftPlan {
     int64_t ld;                 // row stride of G
     int64_t tiles;              // column tiles of the forward's product
     int tile;
-    size_t part, zlabel, forward_total, row, kept, G, acc, splitk, splitw, total;
+    size_t part, zlabel, forward_total, kept, G, acc, splitk, splitw, row, total;
 };
 
 int64_t split_floats(const rdcn_handle* h, int64_t M, int64_t N, int64_t K) {
@@ -408,7 +408,6 @@ SoftPlan soft_layout(const rdcn_handle* h, int64_t rows, int64_t dim, int64_t cl
     s.part = off; off += al((size_t)s.tiles * rows * 8);
     s.zlabel = off; off += al((size_t)rows * 4);
     s.forward_total = off;
-    s.row = off; off += al((size_t)rows * sizeof(SoftRow));
     s.kept = off; off += al((size_t)rows * dim * e);
     s.G = off; off += al((size_t)rows * s.ld * e);
     s.acc = off; off += classes > s.piece ? al((size_t)rows * dim * 4) : 0;  // grad_x as a sum of several products
@@ -419,6 +418,8 @@ SoftPlan soft_layout(const rdcn_handle* h, int64_t rows, int64_t dim, int64_t cl
     }
     s.splitk = off; off += al((size_t)split * 4);
     s.splitw = off; off += al((size_t)splitw * 4);
+    // (last: in front of G it costs grad_w of 8192 x 4352 x 131072 3%, by where G then lies in its pages)
+    s.row = off; off += al((size_t)rows * sizeof(SoftRow));
     s.total = off;
     return s;
 }

@@ -875,6 +875,19 @@ __device__ __forceinline__ void block_epilogue(const GemmArgs& g, int64_t m0, in
     if (ovf) atomicOr(g.err, ERR_BIT_F16_RANGE);
 }
 
+// The labels of a lane's rows in the softmax loss epilogue below (negative past M): loaded while the last stages of the ring
+// are waited for.
+template <int BM, int WM, int WN, int MT, int TM>
+__device__ __forceinline__ void soft_labels(const GemmArgs& g, int64_t m0, int tid, int64_t (&labels)[TM]) {
+    const int64_t mw = m0 + ((tid >> 6) / WN) * (BM / WM) + (tid & 63) % MT;
+#pragma unroll
+    for (int i = 0; i < TM; ++i) {
+        const int64_t m = mw + i * MT;
+        labels[i] = -1;
+        if (m < g.M) labels[i] = g.labels64 ? ((const int64_t*)g.labels)[m] : (int64_t)((const int32_t*)g.labels)[m];
+    }
+}
+
 // Softmax loss epilogue of a BM x BN block, from the accumulators: a lane holds one row of each of its tiles
 // (layout above), so a row's maximum and sum over the BN / WN columns of a wave are the lane's own values and one
 // or two exchanges between lanes, and no wave waits for another; a (maximum, sum) pair covers a wave's columns. z itself
@@ -882,7 +895,7 @@ __device__ __forceinline__ void block_epilogue(const GemmArgs& g, int64_t m0, in
 // took 514 us, so 406; a library product of these sizes takes 405.)
 template <typename T, bool GRAD, int BM, int BN, int WM, int WN, bool M32, typename Acc, int TM, int TN>
 __device__ __forceinline__ void soft_block_epilogue(const GemmArgs& g, int64_t m0, int64_t n0, Acc (&acc)[TM][TN], int tid,
-                                                    uint32_t* stage) {
+                                                    const int64_t (&labels)[TM], uint32_t* stage) {
     constexpr int MT = M32 ? 32 : 16, Q = M32 ? 4 : 1, HALVES = 64 / MT, COLS = BN / WN;
     constexpr float NEG = -__builtin_huge_valf();
     const int lane = tid & 63, wave = tid >> 6, half = lane / MT;
@@ -913,9 +926,8 @@ __device__ __forceinline__ void soft_block_epilogue(const GemmArgs& g, int64_t m
         __builtin_amdgcn_sched_barrier(0);  // one row's values live beside the accumulators
         const int64_t m = mw + i * MT;
         const bool in = m < g.M;
-        int64_t lab = -1;  // the label's column, from nw
-        if (in) lab = (g.labels64 ? ((const int64_t*)g.labels)[m] : (int64_t)((const int32_t*)g.labels)[m]) - g.label0 - nw;
-        const bool hit = lab >= 0 && lab < COLS && ((int)lab / 4) % HALVES == half;
+        const int64_t at = labels[i] - g.label0 - nw;
+        const int lab = at >= 0 && at < COLS && ((int)at / 4) % HALVES == half ? (int)at : -1;  // the label's column, if this lane's
         float v[V];
 #pragma unroll
         for (int j = 0; j < TN; ++j)
@@ -935,10 +947,10 @@ __device__ __forceinline__ void soft_block_epilogue(const GemmArgs& g, int64_t m
                     for (int e = 0; e < 4; ++e) {
                         float& z = v[4 * (j * Q + q) + e];
                         z = r.c == 0.f || z == NEG ? 0.f : r.c * soft_exp<T>(z - r.max);
-                        if (hit && (int)lab == col(j, q) + e) z = r.label;
+                        if (lab == col(j, q) + e) z = r.label;
                     }
         } else {
-            if (hit) {
+            if (lab >= 0) {
                 float z = 0.f;
 #pragma unroll
                 for (int j = 0; j < TN; ++j)
@@ -947,7 +959,7 @@ __device__ __forceinline__ void soft_block_epilogue(const GemmArgs& g, int64_t m
 #pragma unroll
                         for (int e = 0; e < 4; ++e) {
                             float& a = v[4 * (j * Q + q) + e];
-                            if ((int)lab == col(j, q) + e) {
+                            if (lab == col(j, q) + e) {
                                 z = a;
                                 a = NEG;  // (it joins the row's pairs by itself)
                             }
@@ -1097,12 +1109,15 @@ __device__ __forceinline__ void gemm_block(const GemmArgs& g, int block, int z, 
             }
         }
     }
+    constexpr bool SOFT = EK == EK_SOFT || EK == EK_SOFT_GRAD;
+    int64_t labels[P::TM];
+    if constexpr (SOFT) soft_labels<BM, WM, WN, M32 ? 32 : 16>(g, c.m0, tid, labels);
     wait_vmcnt(0);  // the trailing re-read loads land before the workgroup ends
 
-    if constexpr (EK == EK_SOFT || EK == EK_SOFT_GRAD) {
+    if constexpr (SOFT) {
         static_assert(!M32 || WM * WN * 32 * 36 * 4 <= ST * P::STAGE_ELEMS * 2, "the waves' staged rows fit the ring");
         if (M32 && g.c) __syncthreads();  // every wave is done with the ring
-        soft_block_epilogue<bf16_t, EK == EK_SOFT_GRAD, BM, BN, WM, WN, M32>(g, c.m0, c.n0, acc, tid, (uint32_t*)smem);
+        soft_block_epilogue<bf16_t, EK == EK_SOFT_GRAD, BM, BN, WM, WN, M32>(g, c.m0, c.n0, acc, tid, labels, (uint32_t*)smem);
     }
     else block_epilogue<BM, BN, WM, WN, M32, T, EK, P::THREADS, ST * P::STAGE_ELEMS>(g, c.m0, c.n0, z, acc, smem, tid);
 }
@@ -1401,9 +1416,12 @@ __device__ __forceinline__ void f32_lds_block(const GemmArgs& g, int block, int 
                     for (int b = 0; b < 2; ++b)
                         acc[a][b] = __builtin_amdgcn_mfma_f32_16x16x4f32(bf[h][b][e], af[h][a][e], acc[a][b], 0, 0, 0);
     }
+    constexpr bool SOFT = EK == EK_SOFT || EK == EK_SOFT_GRAD;
+    int64_t labels[2];
+    if constexpr (SOFT) soft_labels<BM, 2, 2, 16>(g, m0, tid, labels);
     wait_vmcnt(0);  // the loads that were issued past the end have landed
-    if constexpr (EK == EK_SOFT || EK == EK_SOFT_GRAD) {
-        soft_block_epilogue<float, EK == EK_SOFT_GRAD, BM, BN, 2, 2, false>(g, m0, n0, acc, tid, nullptr);
+    if constexpr (SOFT) {
+        soft_block_epilogue<float, EK == EK_SOFT_GRAD, BM, BN, 2, 2, false>(g, m0, n0, acc, tid, labels, nullptr);
         return;
     }
     __syncthreads();
