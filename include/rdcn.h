@@ -480,8 +480,9 @@ rdcn_status rdcn_head_backward(rdcn_handle* h, int64_t batch, const void* x, con
  *   lse[n]   = log sum_v exp(z[n, v]),   loss[n] = lse[n] - z[n, labels[n]]
  *   x [rows, dim], w [classes, dim] in the storage dtype, offset [classes] float
  *   or NULL, labels [rows] in the handle's id type, loss and lse [rows] float.
- * z is never written out: sums and maxima are float, z is a float sum of exact
- * products (bf16 models) or of float products.
+ * The forward writes no logits. The gradient keeps one value of the storage type's size for each
+ * (row, class) of the classes that it works on at a time in scratch (below). Sums and maxima are
+ * float, z is a float sum of exact products (bf16 models) or of float products.
  *   - offset: a constant per class, e.g. minus the log of its sampling frequency.
  *     -inf masks the class: probability 0 whatever its logit. (It gets no
  *     gradient itself.)
@@ -495,10 +496,12 @@ rdcn_status rdcn_head_backward(rdcn_handle* h, int64_t batch, const void* x, con
  *   - w has to be finite, in masked classes too: their zero probabilities are
  *     still multiplied with it.
  * dim is a multiple of 8 (bf16 models) or 4 (float); rows <= 2^24, classes <=
- * 2^27, dim <= 2^20, and each of [rows, classes], x and w of less than 2^24 blocks of 64 x 64 elements in float models
- * and less than 2^23 of 128 x 128 in bf16 ones ([rows, classes] more, where the logits' own blocks are larger: up to 2^39
- * elements), else RDCN_ERR_UNSUPPORTED. x, w, grad_x and grad_w must be 16-byte aligned (RDCN_ERR_ARG otherwise); rows may be 0 (the
- * forward then does nothing, the gradient sets grad_w to 0).
+ * 2^27, dim <= 2^20, and each of [rows, classes], x and w of less than 2^24 blocks of
+ * 64 x 64 elements in float models and less than 2^23 of 128 x 128 in bf16 ones
+ * ([rows, classes] more where the logits' own blocks are larger: up to 2^39 elements),
+ * else RDCN_ERR_UNSUPPORTED. x, w, grad_x and grad_w must be 16-byte aligned
+ * (RDCN_ERR_ARG otherwise); rows may be 0 (the forward then does nothing, the gradient
+ * sets grad_w to 0).
  */
 
 /* Scratch bytes (256-byte aligned buffers) of the two calls below: what the forward needs, what the gradient is
@@ -551,14 +554,14 @@ rdcn_status rdcn_softmax_loss_grad(rdcn_handle* h, int64_t rows, int64_t dim, in
  * whose bits are (c + base) << 20, code 0 for zero; m's sign is bit 7. So three
  * mantissa bits, reaching 2^-15 (m) or 2^-31 (v) below the block's largest; a
  * nonzero v has at least code 1. Zeros are the state to begin with.
- * stochastic (rdcn_rounding): RDCN_ROUND_CHANCE rounds codes, and bf16 weights without a master, up with the
- * probability of what is cut off (under rounding to nearest small steps of a
- * moving average in 8 bits would all be lost). A code past the block's last one becomes that last
- * one, 1.875 times 2 to the block's exponent, and a block's largest elements cannot leave it by small steps: a v of normal gradients
- * settles at about half of its value. RDCN_ROUND_CHANCE_CARRY, the one to train with, raises the
- * block's exponent by one there, for all of its codes; moments then keep the mean that they have in float.
- * The random bits are a hash of
- * seed, the tensor's place in the list and the element's place (modulo 2^32): pass another
+ * stochastic (rdcn_rounding): RDCN_ROUND_CHANCE rounds codes, and bf16 weights without a
+ * master, up with the probability of what is cut off (under rounding to nearest small steps of
+ * a moving average in 8 bits would all be lost). A code past the block's last one becomes that
+ * last one, 1.875 times 2 to the block's exponent, and a block's largest elements cannot leave
+ * it by small steps: a v of normal gradients settles at about half of its value.
+ * RDCN_ROUND_CHANCE_CARRY, the one to train with, raises the block's exponent by one there, for
+ * all of its codes; moments then keep the mean that they have in float.
+ * The random bits are a hash of seed, the tensor's place in the list and the element's place (modulo 2^32): pass another
  * seed each step (with device_step, t * 0x85EBCA6B is added to it, so that a replayed step
  * draws anew). The result depends on the arguments alone.
  */

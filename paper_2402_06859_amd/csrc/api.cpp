@@ -382,7 +382,9 @@ int64_t split_floats(const rdcn_handle* h, int64_t M, int64_t N, int64_t K) {
 // Blocks of a logits product over `classes` columns. Up to 128 rows it is bound by the read of w, and two
 // 128 x 128 blocks a CU keep more loads in flight than one of 256 rows, most of them padding. us, 128 x 128 /
 // 256 x 256: 100003 classes x 1856, 16 rows 83.5 / 105.5, 50 rows 86.2 / 106.2, 128 rows 97.0 / 107.1, 200 rows 145.8 /
-// 110.2; 131072 x 4352, 16 rows 200 / 255 (5.7 TB/s), 128 rows 229 / 266, 200 rows 359 / 280.
+// 110.2; 131072 x 4352, 16 rows 200 / 255 (5.7 TB/s), 128 rows 229 / 266, 200 rows 359 / 280. Two sides where the
+// other form would be ahead: 129 to 256 rows that plan_gemm leaves on 128 x 128 blocks (200 x 50000 x 512 30.7, on 256 x 256
+// 24.1), and 64 x 64 blocks up to 32 rows over 100003 x 1856 (79 to 81, here 83).
 GemmPlan plan_logits(const rdcn_handle* h, int64_t rows, int64_t classes, int64_t dim) {
     if (!h->bf16) return plan_f32_lds();
     GemmPlan p = plan_gemm(rows, classes, dim, h->bf16, false);

@@ -212,8 +212,8 @@ class DeviceClasses:
 
 class DeviceAdamW:
     """AdamW over (weight, gradient) pairs, or (weight, gradient, weight_decay) where a weight has a decay of its own (an
-    embedding table often none); the others decay by weight_decay if they have more than one dimension. Moments in float or 8 bits, float masters of bf16 weights or none, and
-    the gradients clipped to max_norm together. Rate and step number stand on the device, so that an update
+    embedding table often none); the others decay by weight_decay if they have more than one dimension. Moments in float
+    or 8 bits, float masters of bf16 weights or none, and the gradients clipped to max_norm together. Rate and step number stand on the device, so that an update
     can be captured in a graph: change lr with set_lr. With max_norm, an update whose gradients' norm is not finite
     is left out whole: weights, moments and the step number stay."""
 
