@@ -560,7 +560,7 @@ rdcn_status rdcn_softmax_loss_grad(rdcn_handle* h, int64_t rows, int64_t dim, in
  * last one, 1.875 times 2 to the block's exponent, and a block's largest elements cannot leave
  * it by small steps: a v of normal gradients settles at about half of its value.
  * RDCN_ROUND_CHANCE_CARRY, the one to train with, raises the block's exponent by one there, for
- * all of its codes; moments then keep the mean that they have in float.
+ * all of its codes; moments within the codes' reach then keep the mean that they have in float.
  * The random bits are a hash of seed, the tensor's place in the list and the element's place (modulo 2^32): pass another
  * seed each step (with device_step, t * 0x85EBCA6B is added to it, so that a replayed step
  * draws anew). The result depends on the arguments alone.

@@ -413,7 +413,7 @@ class Rdcn:
     def adamw_step(self, tensors, lr, beta1=0.9, beta2=0.999, eps=1e-8, step=1, grad_scale=1.0, clip=None,
                    stochastic=False, seed=0, device_lr=None, device_step=None, stream=None, carry=False):
         """One step over `tensors` (adamw_tensors). On the device: device_lr (float) and device_step (int64) in place of lr and
-        step, and clip (float), the factor that grad_norm leaves. carry: with 8-bit moments, the rounding to train with."""
+        step, and clip (float), the factor that grad_norm leaves. carry, with stochastic: the rounding to train 8-bit moments with."""
         if clip is not None:
             _fits("adamw_step", "clip", clip, torch.float32, 1)
         if device_lr is not None:
