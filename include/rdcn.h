@@ -538,6 +538,55 @@ rdcn_status rdcn_softmax_loss_grad(rdcn_handle* h, int64_t rows, int64_t dim, in
                                    void* grad_w, void* scratch, size_t scratch_bytes, void* stream);
 
 /*
+ * Log probabilities of given classes, for learning from recorded choices and for answering: with z as for the softmax
+ * loss (same operands, masks and limits),
+ *   lse[n]     = log sum_v exp(z[n, v])
+ *   logprob[n] = z[n, labels[n]] - lse[n]
+ *   entropy[n] = -sum_v p[n, v] log p[n, v],  p = softmax(z)
+ *   top_ids[n], top_logprob[n] [rows, top]: the `top` classes of the largest z in falling order and their log probabilities;
+ *                equal ones by class, the lowest first
+ * No logits are written. Sums are float and in a fixed order (deterministic), and none is a difference of near values: logprob and
+ * entropy of a row whose probability is nearly all on one class keep their digits. The order of the most probable classes
+ * is that of logits summed in 64 bits, for every class whose logit in float is among the top + 4 largest of the row.
+ *   - labels [rows] in the handle's id type, or NULL: no given classes (logprob then NULL too). A label below 0 marks a
+ *     row without one: logprob 0, and no gradient of its entropy either; everything else of the row is written all the same. A label
+ *     of `classes` or more does the same and raises the device error word (RDCN_ERR_INDEX).
+ *   - A masked class has probability 0 and is never among the most probable ones: where fewer than `top` are visible, the
+ *     others have id -1 and log probability -inf. A row whose label is masked has logprob -inf; one with every class masked
+ *     lse -inf and entropy 0.
+ *   - A row whose logits hold NaN or +inf has NaN results, and ids of its own choice (in range, or -1).
+ * top is 0 (no lists) .. RDCN_LOGPROBS_TOP_MAX; top_ids in the handle's id type. logprob, entropy, lse, top_logprob and stats may
+ * be NULL. stats [rows, 4] float, 16-byte aligned, and `kept` are for the gradient: what it needs of a row, and of the logits.
+ */
+#define RDCN_LOGPROBS_TOP_MAX 32
+
+/* Bytes (256-byte aligned buffers): scratch of the forward, `kept`, and scratch of the gradient, what it is fastest with and the
+   least that it takes. */
+rdcn_status rdcn_logprobs_workspace(const rdcn_handle* h, int64_t rows, int64_t dim, int64_t classes, int32_t top,
+                                    size_t* forward_bytes, size_t* kept_bytes, size_t* grad_bytes,
+                                    size_t* grad_least_bytes);
+
+rdcn_status rdcn_logprobs_forward(rdcn_handle* h, int64_t rows, int64_t dim, int64_t classes, const void* x, const void* w,
+                                  const float* offset, const void* labels, float logit_scale, int32_t top, float* logprob,
+                                  float* entropy, float* lse, void* top_ids, float* top_logprob, float* stats, void* kept,
+                                  size_t kept_bytes, void* scratch, size_t scratch_bytes, void* stream);
+
+/*
+ * The gradients of any loss in x and w, from its gradients in logprob and entropy ([rows] float, either may be NULL for 0):
+ *   dL/dz[n, v] = g ([v = label] - p) - h p (log p + entropy),  g = grad_logprob[n], h = grad_entropy[n]
+ *   grad_x = s dL/dz w, grad_w = s (dL/dz)^T x, both in the storage dtype and overwritten.
+ * stats must be those of a forward with the same x, w, offset, labels and logit_scale. Rows without a label (when labels are given), and rows whose
+ * g and h are both 0, have no gradient and may hold anything in x and stats. Masked logits are constants. bf16 models round dL/dz
+ * to bf16 for the products (half a step, 2^-8 of an element) and each gradient once at the end; sums are float and in a fixed order.
+ * 1 - p of a label keeps its digits where p is near 1. With grad_bytes of scratch the call is fastest; it takes any size from
+ * grad_least_bytes on, working on fewer classes at a time.
+ */
+rdcn_status rdcn_logprobs_grad(rdcn_handle* h, int64_t rows, int64_t dim, int64_t classes, const void* x, const void* w,
+                               const float* offset, const void* labels, float logit_scale, const float* stats,
+                               const void* kept, size_t kept_bytes, const float* grad_logprob, const float* grad_entropy,
+                               void* grad_x, void* grad_w, void* scratch, size_t scratch_bytes, void* stream);
+
+/*
  * AdamW (decoupled weight decay) over many tensors at once. Per element, with
  * g' = g * grad_scale * clip and t the step number (from 1):
  *   m' = beta1 m + (1 - beta1) g'

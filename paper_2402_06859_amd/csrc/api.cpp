@@ -16,6 +16,7 @@
 #include "gemm.h"
 #include "head.h"
 #include "kernels.h"
+#include "logprobs.h"
 #include "softmax_loss.h"
 
 struct rdcn_handle {
@@ -565,6 +566,65 @@ rdcn_status soft_forward(rdcn_handle* h, const SoftPlan& S, int64_t rows, int64_
 }
 
 // ---------------------------------------------------------------------------
+// Log probabilities. Forward: the logits product, whose epilogue leaves a ChoiceStat per row and column tile and (for the most
+// probable classes) a pair per group of classes, then one kernel over the rows. Gradient: G [rows, classes] stands in scratch, for as
+// many classes at a time as it holds, from the logits computed again; its two products are the softmax loss's.
+// ---------------------------------------------------------------------------
+struct ChoicePlan {
+    int64_t tiles, piece, ld;
+    ChoiceGroups g;
+    size_t stat, zlabel, groups, forward_total;
+    size_t kept, G, acc, splitk, splitw, row, total;
+};
+
+// Results for G in pieces of `piece` classes.
+ChoicePlan choice_layout(const rdcn_handle* h, int64_t rows, int64_t dim, int64_t classes, int32_t top, int64_t piece) {
+    ChoicePlan s{};
+    const size_t e = eb(h);
+    const int64_t vec = h->bf16 ? 8 : 4;
+    const GemmPlan p = plan_logits(h, rows, classes, dim);
+    int tile = 0;
+    s.tiles = rows > 0 ? gemm_soft_tiles(rows, classes, dim, p, h->bf16, &tile) : 0;
+    if (rows > 0) s.g = gemm_choice_groups(rows, classes, dim, p, h->bf16);
+    size_t off = 0;
+    s.stat = off; off += al((size_t)s.tiles * rows * sizeof(ChoiceStat));
+    s.zlabel = off; off += al((size_t)rows * 4);
+    s.groups = off; off += top > 0 ? al((size_t)s.g.count * rows * 8) : 0;
+    s.forward_total = off;
+    s.piece = piece;
+    s.ld = (piece + vec - 1) / vec * vec;
+    off = 0;
+    s.kept = off; off += al((size_t)rows * dim * e);
+    s.G = off; off += al((size_t)rows * s.ld * e);
+    s.acc = off; off += classes > piece ? al((size_t)rows * dim * 4) : 0;  // grad_x as a sum of several products
+    int64_t split = 0, splitw = 0;
+    for (int64_t n : {piece, classes % piece}) {
+        split = std::max(split, split_floats(h, rows, dim, n));
+        splitw = std::max(splitw, split_floats(h, n, dim, rows));
+    }
+    s.splitk = off; off += al((size_t)split * 4);
+    s.splitw = off; off += al((size_t)splitw * 4);
+    s.row = off; off += al((size_t)rows * sizeof(ChoiceRow));
+    s.total = off;
+    return s;
+}
+
+// The largest pieces whose layout fits `bytes` (all classes up to SOFT_WHOLE_BYTES of G, else pieces of SOFT_PIECE_BYTES of it,
+// halved until they fit), or the smallest, which may not.
+ChoicePlan choice_plan(const rdcn_handle* h, int64_t rows, int64_t dim, int64_t classes, size_t bytes) {
+    const double column = (double)std::max<int64_t>(rows, 1) * (double)eb(h);
+    int64_t piece = classes;
+    if (classes > SOFT_MOST_PIECE || column * (double)classes > SOFT_WHOLE_BYTES) {
+        piece = (int64_t)(SOFT_PIECE_BYTES / column) / 256 * 256;
+        piece = std::min(std::max(piece, SOFT_LEAST_PIECE), SOFT_MOST_PIECE);
+    }
+    for (;; piece = std::max(piece / 512 * 256, SOFT_LEAST_PIECE)) {
+        const ChoicePlan s = choice_layout(h, rows, dim, classes, 0, std::min(piece, classes));
+        if (s.total <= bytes || piece <= SOFT_LEAST_PIECE) return s;
+    }
+}
+
+// ---------------------------------------------------------------------------
 // AdamW and the gradient norm: the caller's descriptors in the kernels' form (`out` holds `count`).
 // ---------------------------------------------------------------------------
 constexpr int32_t ADAMW_MAX_TENSORS = 65536;
@@ -643,6 +703,7 @@ struct TensorList {  // freed on every return
 
 static_assert(RDCN_EMBED_STATIC_SCRATCH_BYTES == rdcn::EMB_STATIC_SCRATCH_BYTES,
               "the header states the static workspace size");
+static_assert(RDCN_LOGPROBS_TOP_MAX == rdcn::CHOICE_TOP_MAX, "the header states the most probable classes' limit");
 
 extern "C" {
 
@@ -1417,6 +1478,129 @@ rdcn_status rdcn_softmax_loss_grad(rdcn_handle* h, int64_t rows, int64_t dim, in
         gw.a = G; gw.lda = S.ld; gw.a_kstrided = true;
         gw.b = kept; gw.ldb = dim; gw.b_kstrided = true;
         const SoftProduct px = soft_product(h, gx, v > 0 ? acc : nullptr, acc, grad_x, v + n == classes, splitk);
+        const SoftProduct pw = soft_product(h, gw, nullptr, nullptr, (char*)grad_w + (size_t)v * dim * e, true,
+                                            (float*)(sc + S.splitw));
+        RDCN_TRY(soft_gradients(h, px, pw, s));
+    }
+    return RDCN_OK;
+}
+
+rdcn_status rdcn_logprobs_workspace(const rdcn_handle* h, int64_t rows, int64_t dim, int64_t classes, int32_t top,
+                                    size_t* forward_bytes, size_t* kept_bytes, size_t* grad_bytes,
+                                    size_t* grad_least_bytes) {
+    rdcn_status st = check_soft(h, rows, dim, classes);
+    if (st != RDCN_OK) return st;
+    if (!forward_bytes || !kept_bytes || !grad_bytes || !grad_least_bytes || top < 0) return RDCN_ERR_ARG;
+    if (top > RDCN_LOGPROBS_TOP_MAX) return RDCN_ERR_UNSUPPORTED;
+    *forward_bytes = choice_layout(h, rows, dim, classes, top, classes).forward_total;
+    *kept_bytes = 0;
+    const ChoicePlan S = choice_plan(h, rows, dim, classes, SIZE_MAX);
+    *grad_bytes = S.total;
+    *grad_least_bytes = std::min(S.total, choice_plan(h, rows, dim, classes, 0).total);
+    return RDCN_OK;
+}
+
+rdcn_status rdcn_logprobs_forward(rdcn_handle* h, int64_t rows, int64_t dim, int64_t classes, const void* x, const void* w,
+                                  const float* offset, const void* labels, float logit_scale, int32_t top, float* logprob,
+                                  float* entropy, float* lse, void* top_ids, float* top_logprob, float* stats, void* kept,
+                                  size_t kept_bytes, void* scratch, size_t scratch_bytes, void* stream) {
+    rdcn_status st = check_soft(h, rows, dim, classes);
+    if (st != RDCN_OK) return st;
+    if (!std::isfinite(logit_scale) || top < 0) return RDCN_ERR_ARG;
+    if (top > RDCN_LOGPROBS_TOP_MAX) return RDCN_ERR_UNSUPPORTED;
+    if (rows == 0) return RDCN_OK;
+    if (!x || !a16(x) || !w || !a16(w) || (logprob && !labels) || (top > 0 && !top_ids) || !a16(stats)) return RDCN_ERR_ARG;
+    const ChoicePlan S = choice_layout(h, rows, dim, classes, top, classes);
+    if (!scratch || !aligned256(scratch) || scratch_bytes < S.forward_total) return RDCN_ERR_WORKSPACE;
+    char* const sc = (char*)scratch;
+    hipStream_t s = (hipStream_t)stream;
+    (void)kept; (void)kept_bytes;
+    GemmArgs g{};
+    g.M = rows; g.N = classes; g.K = dim;
+    g.a = x; g.lda = dim;
+    g.b = w; g.ldb = dim;
+    g.epi = EPI_CHOICE_FWD; g.scale = logit_scale;
+    g.offset = offset;
+    g.labels = labels; g.labels64 = h->ids64;
+    g.zlabel = (float*)(sc + S.zlabel);
+    g.stat = (ChoiceStat*)(sc + S.stat); g.tiles = S.tiles;
+    if (top > 0) g.groups = (uint2*)(sc + S.groups);
+    g.ngroups = S.g.count;
+    {
+        ProfScope ps(h, RDCN_KERNEL_HEAD_FWD_GEMM, s);
+        RDCN_TRY(launch_gemm(g, plan_logits(h, rows, classes, dim), h->bf16, s));
+    }
+    ChoiceRows r{};
+    r.rows = rows; r.dim = dim; r.classes = classes; r.tiles = S.tiles;
+    r.stat = g.stat; r.zlabel = g.zlabel;
+    r.labels = labels; r.ids64 = h->ids64;
+    r.logprob = logprob; r.entropy = entropy; r.lse = lse; r.stats = (float4*)stats;
+    r.err = h->err;
+    r.top = top; r.g = S.g; r.groups = g.groups;
+    r.x = x; r.w = w; r.offset = offset; r.logit_scale = logit_scale;
+    r.top_ids = top_ids; r.top_logprob = top_logprob;
+    ProfScope ps(h, RDCN_KERNEL_HEAD_LOSS, s);
+    return hip_status(launch_choice_rows(r, h->bf16, s));
+}
+
+rdcn_status rdcn_logprobs_grad(rdcn_handle* h, int64_t rows, int64_t dim, int64_t classes, const void* x, const void* w,
+                               const float* offset, const void* labels, float logit_scale, const float* stats,
+                               const void* kept, size_t kept_bytes, const float* grad_logprob, const float* grad_entropy,
+                               void* grad_x, void* grad_w, void* scratch, size_t scratch_bytes, void* stream) {
+    rdcn_status st = check_soft(h, rows, dim, classes);
+    if (st != RDCN_OK) return st;
+    if (!std::isfinite(logit_scale) || (grad_logprob && !labels)) return RDCN_ERR_ARG;
+    if (!w || !a16(w) || !grad_w || !a16(grad_w)) return RDCN_ERR_ARG;
+    hipStream_t s = (hipStream_t)stream;
+    const size_t e = eb(h);
+    if (rows == 0) return hip_status(launch_fill_zero((float*)grad_w, classes * dim * (int64_t)e / 4, s));
+    if (!x || !a16(x) || !stats || !a16(stats) || !grad_x || !a16(grad_x)) return RDCN_ERR_ARG;
+    const ChoicePlan S = choice_plan(h, rows, dim, classes, scratch_bytes);
+    if (!scratch || !aligned256(scratch) || scratch_bytes < S.total) return RDCN_ERR_WORKSPACE;
+    (void)kept; (void)kept_bytes;
+    char* const sc = (char*)scratch;
+    ChoiceRow* const row = (ChoiceRow*)(sc + S.row);
+    float* const acc = (float*)(sc + S.acc);
+    char* const G = sc + S.G;
+    ChoicePrepare p{};
+    p.rows = rows; p.dim = dim; p.classes = classes;
+    p.stats = (const float4*)stats;
+    p.labels = labels; p.ids64 = h->ids64;
+    p.grad_logprob = grad_logprob; p.grad_entropy = grad_entropy;
+    p.logit_scale = logit_scale;
+    p.x = x; p.kept = sc + S.kept;
+    p.row = row; p.err = h->err;
+    {
+        ProfScope ps(h, RDCN_KERNEL_HEAD_OUT_BWD, s);
+        RDCN_TRY(launch_choice_prepare(p, h->bf16, s));
+    }
+    for (int64_t v = 0; v < classes; v += S.piece) {
+        const int64_t n = std::min(S.piece, classes - v);
+        const void* const wp = (const char*)w + (size_t)v * dim * e;
+        GemmArgs g{};
+        g.M = rows; g.N = n; g.K = dim;
+        g.a = x; g.lda = dim;
+        g.b = wp; g.ldb = dim;
+        g.epi = EPI_CHOICE_GRAD; g.scale = logit_scale;
+        g.offset = offset ? offset + v : nullptr;
+        g.labels = labels; g.labels64 = h->ids64; g.label0 = v;
+        g.choicerow = row;
+        g.c = G; g.ldc = S.ld;
+        {
+            ProfScope ps(h, RDCN_KERNEL_HEAD_FWD_GEMM, s);
+            RDCN_TRY(launch_gemm(g, plan_logits(h, rows, n, dim), h->bf16, s));
+        }
+        GemmArgs gx{};
+        gx.M = rows; gx.N = dim; gx.K = n;
+        gx.a = G; gx.lda = S.ld;
+        gx.b = wp; gx.ldb = dim; gx.b_kstrided = true;
+        gx.rem_last = true;
+        GemmArgs gw{};
+        gw.M = n; gw.N = dim; gw.K = rows;
+        gw.a = G; gw.lda = S.ld; gw.a_kstrided = true;
+        gw.b = p.kept; gw.ldb = dim; gw.b_kstrided = true;
+        const SoftProduct px = soft_product(h, gx, v > 0 ? acc : nullptr, acc, grad_x, v + n == classes,
+                                            (float*)(sc + S.splitk));
         const SoftProduct pw = soft_product(h, gw, nullptr, nullptr, (char*)grad_w + (size_t)v * dim * e, true,
                                             (float*)(sc + S.splitw));
         RDCN_TRY(soft_gradients(h, px, pw, s));

@@ -25,8 +25,13 @@ enum GemmEpi {
     EPI_SOFT_FWD = 8,   // softpart[t * M + m] over the classes of column tile t (gemm_soft_tiles) other than the row's
                         // label = (max, sum of exp(z - max)); zlabel[m] = z at the label, if it is one of the tile's columns; with c:
                         // c = exp(z - max) (f16 times SOFT_E_SCALE, or float), zero at the label and in the pad of a row
-    EPI_SOFT_GRAD = 9   // c = r.c * exp(z - r.max) for r = softrow[m], r.label at the row's label (storage type), zero
+    EPI_SOFT_GRAD = 9,  // c = r.c * exp(z - r.max) for r = softrow[m], r.label at the row's label (storage type), zero
                         // where r.c is 0 or z is -inf and in the pad of a row
+    // Log probabilities (both operands K-contiguous), z as above:
+    EPI_CHOICE_FWD = 10,  // stat[m * tiles + t] = ChoiceStat of the classes of column tile t (gemm_soft_tiles); zlabel[m] = z at
+                          // the label; with groups: groups[m * ngroups + u] of the classes of group u (gemm_choice_groups)
+    EPI_CHOICE_GRAD = 11  // c = exp(d) (r.a + r.b d) for d = z - r.max, r = choicerow[m], r.label at the row's label (storage
+                          // type), zero where r.a and r.b are 0 or z is -inf and in the pad of a row
 };
 
 // exp(z - max) of a tile's row is held in f16 times this (a power of two): values down to
@@ -38,6 +43,24 @@ constexpr float SOFT_E_SCALE = 32768.f;
 // from p, or a log-sum-exp rounded to float, would leave few digits of where p is near 1.
 struct SoftRow {
     float max, c, label, unused;
+};
+
+// A row's logits over some classes. With max the largest of them and d = z - max: rest = the sum of exp(d) over all but one
+// class of that size (-1 where no class is visible), mean = the sum of exp(d) d. Nothing here is a difference of near values: rest keeps
+// its digits where one class has nearly all of the probability, and so do 1 - p = rest / (1 + rest) and the entropy.
+struct ChoiceStat {
+    float max, rest, mean, unused;
+};
+// A row of the gradient: see EPI_CHOICE_GRAD.
+struct ChoiceRow {
+    float max, a, b, label;
+};
+// The classes of a group: the `columns / span` runs of four that begin at base + pitch k + 4 g, base = u / (pitch / 4) * span
+// and g = u % (pitch / 4) for group u: what one lane of a product's block holds of a row. In memory: x = the largest logit's float bits, y =
+// a bound that no other class of the group exceeds, with the largest one's place in its low 4 bits.
+struct ChoiceGroups {
+    int64_t count;
+    int span, pitch, size;  // size: classes of a group, 8 or 16
 };
 
 // What an optional second output plane c2 receives (same row stride as c).
@@ -93,6 +116,12 @@ struct GemmArgs {
     int64_t label0;
     float* zlabel;        // [M]
     float2* softpart;     // [gemm_soft_tiles][M]
+    // log probability epilogues (and offset .. zlabel above)
+    ChoiceStat* stat;     // [M][tiles]
+    int64_t tiles;
+    uint2* groups;        // [M][ngroups] or NULL
+    int64_t ngroups;
+    const ChoiceRow* choicerow;  // [M]
     int group_m;        // set from GemmPlan::group_m by launch_gemm
 };
 
@@ -126,6 +155,7 @@ hipError_t launch_gemm(const GemmArgs& g, const GemmPlan& p, bool bf16, hipStrea
 inline int64_t gemm_tiles_n(int64_t N, const GemmPlan& p) { return (N + p.bn - 1) / p.bn; }
 // Column tiles of a softmax loss product (EPI_SOFT_FWD) and the columns of one, as launch_gemm's blocks have them.
 int64_t gemm_soft_tiles(int64_t M, int64_t N, int64_t K, const GemmPlan& p, bool bf16, int* columns);
+ChoiceGroups gemm_choice_groups(int64_t M, int64_t N, int64_t K, const GemmPlan& p, bool bf16);
 // Two products in one launch, with plain epilogues: x with A K-contiguous and B K-strided, y with both K-strided. gemm_pairs:
 // their plans are of 64 x 64 blocks, and so few of them that a launch each would leave the chip part empty.
 bool gemm_pairs(const GemmArgs& x, const GemmPlan& px, const GemmArgs& y, const GemmPlan& py, bool bf16);

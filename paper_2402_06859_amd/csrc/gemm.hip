@@ -275,7 +275,8 @@ __device__ __forceinline__ float mlp_epilogue8(const GemmArgs& g, int64_t m, int
 }
 
 // Which epilogue a kernel carries.
-enum { EK_PLAIN = 0, EK_MLP = 1, EK_SOFT = 2, EK_SOFT_GRAD = 3 };  // (streamed blocks: EK_SOFT has both)
+enum { EK_PLAIN = 0, EK_MLP = 1, EK_SOFT = 2, EK_SOFT_GRAD = 3, EK_CHOICE = 4, EK_CHOICE_GRAD = 5 };
+// (streamed blocks: EK_SOFT and EK_CHOICE have both)
 
 // exp(x) for the softmax loss, from the base-2 exponential unit. bf16 models: the rounding of x log2(e), about
 // |x| 2^-24 of the result, is far below that of the gradient to bf16. Float ones: the product as a sum of two floats (fma
@@ -345,6 +346,87 @@ __device__ __forceinline__ void soft_epilogue8(const GemmArgs& g, int64_t m, int
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] *= SOFT_E_SCALE;
     *(u32x4_t*)((_Float16*)g.c + m * g.ldc + n) = pack_f16x8(v, ovf);
+}
+
+// A group's largest value, its place, and the largest of the others: N values of one lane.
+template <int N, typename F>
+__device__ __forceinline__ uint2 choice_group(F value) {
+    float top = value(0), second = -__builtin_huge_valf();
+    int at = 0;
+#pragma unroll
+    for (int i = 1; i < N; ++i) {
+        const float x = value(i);
+        const bool more = x > top;
+        second = fmaxf(second, more ? top : x);
+        at = more ? i : at;
+        top = more ? x : top;
+    }
+    // rounded up in its last 4 bits, which hold the place
+    const uint32_t b = __float_as_uint(second);
+    return make_uint2(__float_as_uint(top), (((int)b < 0 ? b - 16u : b + 16u) & ~15u) | (uint32_t)at);
+}
+
+// exp(d) of N logits less their maximum: adds to the sum over those below the maximum, counts those at it, and
+// adds up exp(d) d. (An exponential of 1 is one at the maximum, or as near as a float tells.)
+template <typename T, int N, typename F>
+__device__ __forceinline__ void choice_sums(F z, float top, float& below, float& at_top, float& mean) {
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+        const float x = z(e), d = x - top, t = soft_exp<T>(d);
+        const bool one = t == 1.f;
+        below += one ? 0.f : t;
+        at_top += one ? 1.f : 0.f;
+        mean += t == 0.f ? 0.f : t * d;  // (d may be -inf)
+    }
+}
+
+// Log probability epilogues on 8 consecutive columns, as soft_epilogue8.
+template <int LANES>
+__device__ __forceinline__ void choice_epilogue8(const GemmArgs& g, int64_t m, int64_t n, int64_t tile, bool in, float* v) {
+    const float NEG = -__builtin_huge_valf();
+    int64_t lab = -1;
+    if (in) {
+        if (g.labels) lab = (g.labels64 ? ((const int64_t*)g.labels)[m] : (int64_t)((const int32_t*)g.labels)[m]) - g.label0 - n;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const float o = g.offset && n + e < g.N ? g.offset[n + e] : 0.f;
+            v[e] = n + e >= g.N || o == NEG ? NEG : v[e] * g.scale + o;
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = NEG;
+    }
+    if (g.epi == EPI_CHOICE_GRAD) {
+        if (!in) return;
+        const ChoiceRow r = g.choicerow[m];
+        const bool none = r.a == 0.f && r.b == 0.f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const float d = v[e] - r.max;
+            v[e] = none || v[e] == NEG ? 0.f : soft_exp<bf16_t>(d) * fmaf(r.b, d, r.a);
+            if (lab == e) v[e] = r.label;
+        }
+        store8<bf16_t>((bf16_t*)g.c + m * g.ldc + n, v);
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+        if (lab == e) g.zlabel[m] = v[e];
+    if (in && g.groups) g.groups[m * g.ngroups + n / 8] = choice_group<8>([&](int i) { return v[i]; });
+    float mx = v[0];
+#pragma unroll
+    for (int e = 1; e < 8; ++e) mx = fmaxf(mx, v[e]);
+#pragma unroll
+    for (int o = 1; o < LANES; o <<= 1) mx = fmaxf(mx, __shfl_xor(mx, o));
+    float below = 0.f, at_top = 0.f, mean = 0.f;
+    choice_sums<bf16_t, 8>([&](int i) { return v[i]; }, mx == NEG ? 0.f : mx, below, at_top, mean);
+#pragma unroll
+    for (int o = 1; o < LANES; o <<= 1) {
+        below += __shfl_xor(below, o);
+        at_top += __shfl_xor(at_top, o);
+        mean += __shfl_xor(mean, o);
+    }
+    if (in && n == tile * (8 * LANES)) g.stat[m * g.tiles + tile] = ChoiceStat{mx, below + (at_top - 1.f), mean, 0.f};
 }
 
 __device__ __forceinline__ int xcd_remap(int id, int n) {
@@ -884,7 +966,7 @@ __device__ __forceinline__ void soft_labels(const GemmArgs& g, int64_t m0, int t
     for (int i = 0; i < TM; ++i) {
         const int64_t m = mw + i * MT;
         labels[i] = -1;
-        if (m < g.M) labels[i] = g.labels64 ? ((const int64_t*)g.labels)[m] : (int64_t)((const int32_t*)g.labels)[m];
+        if (m < g.M && g.labels) labels[i] = g.labels64 ? ((const int64_t*)g.labels)[m] : (int64_t)((const int32_t*)g.labels)[m];
     }
 }
 
@@ -1038,6 +1120,107 @@ __device__ __forceinline__ void soft_block_epilogue(const GemmArgs& g, int64_t m
     }
 }
 
+// Log probability epilogue of a BM x BN block, from the accumulators, laid out as for the softmax loss: a lane's values of a row
+// are also the classes of a group (or, of 32 x 32 tiles, of one group per tile).
+template <typename T, bool GRAD, int BM, int BN, int WM, int WN, bool M32, typename Acc, int TM, int TN>
+__device__ __forceinline__ void choice_block_epilogue(const GemmArgs& g, int64_t m0, int64_t n0, Acc (&acc)[TM][TN], int tid,
+                                                      const int64_t (&labels)[TM]) {
+    constexpr int MT = M32 ? 32 : 16, Q = M32 ? 4 : 1, HALVES = 64 / MT, COLS = BN / WN;
+    constexpr float NEG = -__builtin_huge_valf();
+    const int lane = tid & 63, wave = tid >> 6, half = lane / MT;
+    const int64_t nw = n0 + (wave % WN) * COLS;  // the wave's first column
+    const int64_t mw = m0 + (wave / WN) * (BM / WM) + lane % MT;
+    if (nw >= g.N) return;
+    auto col = [&](int j, int q) __attribute__((always_inline)) { return j * MT + 8 * q + 4 * half; };
+    constexpr int V = TN * Q * 4;
+    const bool edge = g.offset || nw + COLS > g.N;
+    float off[V];
+    if (edge) {
+#pragma unroll
+        for (int j = 0; j < TN; ++j)
+#pragma unroll
+            for (int q = 0; q < Q; ++q)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int64_t n = nw + col(j, q) + e;
+                    off[4 * (j * Q + q) + e] = n >= g.N ? NEG : g.offset ? g.offset[n] : 0.f;
+                }
+    }
+    constexpr int VEC = st<T>::vec;
+    const int64_t pad = (g.N + VEC - 1) / VEC * VEC - nw;  // columns that are stored
+#pragma unroll
+    for (int i = 0; i < TM; ++i) {
+        __builtin_amdgcn_sched_barrier(0);  // one row's values live beside the accumulators
+        const int64_t m = mw + i * MT;
+        const bool in = m < g.M;
+        const int64_t at = labels[i] - g.label0 - nw;
+        const int lab = at >= 0 && at < COLS && ((int)at / 4) % HALVES == half ? (int)at : -1;  // the label's column, if this lane's
+        float v[V];
+#pragma unroll
+        for (int j = 0; j < TN; ++j)
+#pragma unroll
+            for (int e = 0; e < 4 * Q; ++e) v[4 * Q * j + e] = acc[i][j][e] * g.scale;
+        if (edge) {
+#pragma unroll
+            for (int e = 0; e < V; ++e) v[e] = off[e] == NEG ? NEG : v[e] + off[e];
+        }
+        if constexpr (GRAD) {
+            const ChoiceRow r = in ? g.choicerow[m] : ChoiceRow{};
+            const bool none = r.a == 0.f && r.b == 0.f;
+#pragma unroll
+            for (int j = 0; j < TN; ++j)
+#pragma unroll
+                for (int q = 0; q < Q; ++q) {
+                    float* const a = v + 4 * (j * Q + q);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float d = a[e] - r.max;
+                        a[e] = none || a[e] == NEG ? 0.f : soft_exp<T>(d) * fmaf(r.b, d, r.a);
+                        if (lab == col(j, q) + e) a[e] = r.label;
+                    }
+                    if (in && col(j, q) < pad) store4<T>((T*)g.c + m * g.ldc + nw + col(j, q), a);
+                }
+        } else {
+            if (lab >= 0) {
+                float z = 0.f;
+#pragma unroll
+                for (int j = 0; j < TN; ++j)
+#pragma unroll
+                    for (int q = 0; q < Q; ++q)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            if (lab == col(j, q) + e) z = v[4 * (j * Q + q) + e];
+                g.zlabel[m] = z;
+            }
+            if (g.groups && in) {
+                if constexpr (M32) {
+#pragma unroll
+                    for (int j = 0; j < TN; ++j)
+                        if (nw + 32 * j < g.N)
+                            g.groups[m * g.ngroups + (nw / 32 + j) * 2 + half] =
+                                choice_group<16>([&](int k) { return v[16 * j + k]; });
+                } else {
+                    g.groups[m * g.ngroups + nw / COLS * 4 + half] = choice_group<V>([&](int k) { return v[k]; });
+                }
+            }
+            float mx = v[0];
+#pragma unroll
+            for (int e = 1; e < V; ++e) mx = fmaxf(mx, v[e]);
+#pragma unroll
+            for (int o = MT; o < 64; o <<= 1) mx = fmaxf(mx, __shfl_xor(mx, o));
+            float below = 0.f, at_top = 0.f, mean = 0.f;
+            choice_sums<T, V>([&](int k) { return v[k]; }, mx == NEG ? 0.f : mx, below, at_top, mean);
+#pragma unroll
+            for (int o = MT; o < 64; o <<= 1) {
+                below += __shfl_xor(below, o);
+                at_top += __shfl_xor(at_top, o);
+                mean += __shfl_xor(mean, o);
+            }
+            if (in && half == 0) g.stat[m * g.tiles + nw / COLS] = ChoiceStat{mx, below + (at_top - 1.f), mean, 0.f};
+        }
+    }
+}
+
 // C = A B^T with an ST-stage direct-to-LDS pipeline of KB-deep stages (see layouts above): one workgroup's block, tile
 // `block` of the product in range z of `splits`. `smem` holds the ST stages: the ring during the K loop, the C staging area
 // afterwards.
@@ -1109,16 +1292,16 @@ __device__ __forceinline__ void gemm_block(const GemmArgs& g, int block, int z, 
             }
         }
     }
-    constexpr bool SOFT = EK == EK_SOFT || EK == EK_SOFT_GRAD;
+    constexpr bool SOFT = EK == EK_SOFT || EK == EK_SOFT_GRAD, CHOICE = EK == EK_CHOICE || EK == EK_CHOICE_GRAD;
     int64_t labels[P::TM];
-    if constexpr (SOFT) soft_labels<BM, WM, WN, M32 ? 32 : 16>(g, c.m0, tid, labels);
+    if constexpr (SOFT || CHOICE) soft_labels<BM, WM, WN, M32 ? 32 : 16>(g, c.m0, tid, labels);
     wait_vmcnt(0);  // the trailing re-read loads land before the workgroup ends
 
     if constexpr (SOFT) {
         static_assert(!M32 || WM * WN * 32 * 36 * 4 <= ST * P::STAGE_ELEMS * 2, "the waves' staged rows fit the ring");
         if (M32 && g.c) __syncthreads();  // every wave is done with the ring
         soft_block_epilogue<bf16_t, EK == EK_SOFT_GRAD, BM, BN, WM, WN, M32>(g, c.m0, c.n0, acc, tid, labels, (uint32_t*)smem);
-    }
+    } else if constexpr (CHOICE) choice_block_epilogue<bf16_t, EK == EK_CHOICE_GRAD, BM, BN, WM, WN, M32>(g, c.m0, c.n0, acc, tid, labels);
     else block_epilogue<BM, BN, WM, WN, M32, T, EK, P::THREADS, ST * P::STAGE_ELEMS>(g, c.m0, c.n0, z, acc, smem, tid);
 }
 
@@ -1243,7 +1426,7 @@ __global__ __launch_bounds__(64 * ST_KW) void k_gemm_stream(GemmArgs g) {
         for (int c = threadIdx.x; c < ROWS * (BN / 8); c += 64 * ST_KW) {
             const int row = c / (BN / 8), col = c % (BN / 8) * 8;
             const int64_t m = m0 + h * ROWS + row, n = n0 + col;
-            if (EK != EK_SOFT && (m >= g.M || n >= g.N)) continue;
+            if (EK != EK_SOFT && EK != EK_CHOICE && (m >= g.M || n >= g.N)) continue;
             const float* const p = cs + row * CP + col;
             f32x4_t s0 = *(const f32x4_t*)p, s1 = *(const f32x4_t*)(p + 4);
 #pragma unroll
@@ -1253,6 +1436,7 @@ __global__ __launch_bounds__(64 * ST_KW) void k_gemm_stream(GemmArgs g) {
             }
             float v[8] = {s0.x, s0.y, s0.z, s0.w, s1.x, s1.y, s1.z, s1.w};
             if constexpr (EK == EK_SOFT) soft_epilogue8<BN / 8>(g, m, n, n0 / BN, m < g.M && n < g.N, v);
+            else if constexpr (EK == EK_CHOICE) choice_epilogue8<BN / 8>(g, m, n, n0 / BN, m < g.M && n < g.N, v);
             else if constexpr (EK == EK_MLP) (void)mlp_epilogue8<T>(g, m, n, v, ovf);
             else epilogue8<T>(g, m, n, 0, v, ovf);
         }
@@ -1266,12 +1450,14 @@ hipError_t launch_stream(const GemmArgs& g, hipStream_t s) {
     const int64_t tiles = ((g.M + 16 * TM - 1) / (16 * TM)) * ((g.N + 16 * TN - 1) / (16 * TN));
     const dim3 grid((unsigned)tiles), block(64 * ST_KW);
     const bool mlp = g.epi == EPI_MLP_FWD, soft = g.epi == EPI_SOFT_FWD || g.epi == EPI_SOFT_GRAD;
+    const bool choice = g.epi == EPI_CHOICE_FWD || g.epi == EPI_CHOICE_GRAD;
     if (g.ops_f16) {
-        if (g.a2 || soft) return hipErrorInvalidValue;
+        if (g.a2 || soft || choice) return hipErrorInvalidValue;
         if (mlp) hipLaunchKernelGGL((k_gemm_stream<TM, TN, ST, KB, bf16_t, EK_MLP, true>), grid, block, 0, s, g);
         else hipLaunchKernelGGL((k_gemm_stream<TM, TN, ST, KB, bf16_t, EK_PLAIN, true>), grid, block, 0, s, g);
     } else {
         if (soft) hipLaunchKernelGGL((k_gemm_stream<TM, TN, ST, KB, bf16_t, EK_SOFT, false>), grid, block, 0, s, g);
+        else if (choice) hipLaunchKernelGGL((k_gemm_stream<TM, TN, ST, KB, bf16_t, EK_CHOICE, false>), grid, block, 0, s, g);
         else if (mlp) hipLaunchKernelGGL((k_gemm_stream<TM, TN, ST, KB, bf16_t, EK_MLP, false>), grid, block, 0, s, g);
         else hipLaunchKernelGGL((k_gemm_stream<TM, TN, ST, KB, bf16_t, EK_PLAIN, false>), grid, block, 0, s, g);
     }
@@ -1416,12 +1602,16 @@ __device__ __forceinline__ void f32_lds_block(const GemmArgs& g, int block, int 
                     for (int b = 0; b < 2; ++b)
                         acc[a][b] = __builtin_amdgcn_mfma_f32_16x16x4f32(bf[h][b][e], af[h][a][e], acc[a][b], 0, 0, 0);
     }
-    constexpr bool SOFT = EK == EK_SOFT || EK == EK_SOFT_GRAD;
+    constexpr bool SOFT = EK == EK_SOFT || EK == EK_SOFT_GRAD, CHOICE = EK == EK_CHOICE || EK == EK_CHOICE_GRAD;
     int64_t labels[2];
-    if constexpr (SOFT) soft_labels<BM, 2, 2, 16>(g, m0, tid, labels);
+    if constexpr (SOFT || CHOICE) soft_labels<BM, 2, 2, 16>(g, m0, tid, labels);
     wait_vmcnt(0);  // the loads that were issued past the end have landed
     if constexpr (SOFT) {
         soft_block_epilogue<float, EK == EK_SOFT_GRAD, BM, BN, 2, 2, false>(g, m0, n0, acc, tid, labels, nullptr);
+        return;
+    }
+    if constexpr (CHOICE) {
+        choice_block_epilogue<float, EK == EK_CHOICE_GRAD, BM, BN, 2, 2, false>(g, m0, n0, acc, tid, labels);
         return;
     }
     __syncthreads();
@@ -1464,6 +1654,10 @@ hipError_t launch_f32_lds(const GemmArgs& g, int splits, hipStream_t s) {
         if (g.a_kstrided || g.b_kstrided || splits != 1) return hipErrorInvalidValue;
         if (g.epi == EPI_SOFT_GRAD) hipLaunchKernelGGL((k_gemm_f32_lds<false, false, EK_SOFT_GRAD>), grid, block, 0, s, g);
         else hipLaunchKernelGGL((k_gemm_f32_lds<false, false, EK_SOFT>), grid, block, 0, s, g);
+    } else if (g.epi == EPI_CHOICE_FWD || g.epi == EPI_CHOICE_GRAD) {
+        if (g.a_kstrided || g.b_kstrided || splits != 1) return hipErrorInvalidValue;
+        if (g.epi == EPI_CHOICE_GRAD) hipLaunchKernelGGL((k_gemm_f32_lds<false, false, EK_CHOICE_GRAD>), grid, block, 0, s, g);
+        else hipLaunchKernelGGL((k_gemm_f32_lds<false, false, EK_CHOICE>), grid, block, 0, s, g);
     } else if (g.a_kstrided && g.b_kstrided) {
         hipLaunchKernelGGL((k_gemm_f32_lds<true, true, EK_PLAIN>), grid, block, 0, s, g);
     } else if (!g.a_kstrided && g.b_kstrided) {
@@ -1609,6 +1803,9 @@ hipError_t launch_tile(const GemmArgs& g, int splits, hipStream_t s) {
         // softmax loss: logits in one pass over K, both K-contiguous
         if (g.a_kstrided || g.b_kstrided || g.ops_f16 || g.a2 || splits != 1) return hipErrorInvalidValue;
         if (g.epi == EPI_SOFT_GRAD) RDCN_GEMM(false, false, EK_SOFT_GRAD); else RDCN_GEMM(false, false, EK_SOFT);
+    } else if (g.epi == EPI_CHOICE_FWD || g.epi == EPI_CHOICE_GRAD) {
+        if (g.a_kstrided || g.b_kstrided || g.ops_f16 || g.a2 || splits != 1) return hipErrorInvalidValue;
+        if (g.epi == EPI_CHOICE_GRAD) RDCN_GEMM(false, false, EK_CHOICE_GRAD); else RDCN_GEMM(false, false, EK_CHOICE);
     } else if (g.ops_f16) {
         // f16 operands: the forward products over f16 activations (both K-contiguous;
         // the cross projections and the MLP layers, no split-K for the latter)
@@ -1837,6 +2034,16 @@ int64_t gemm_soft_tiles(int64_t M, int64_t N, int64_t K, const GemmPlan& p, bool
     // (a streamed block's columns, or those of one wave)
     *columns = st == 1 ? 16 : st || p.bm == 64 ? 32 : 64;
     return (N + *columns - 1) / *columns;
+}
+
+ChoiceGroups gemm_choice_groups(int64_t M, int64_t N, int64_t K, const GemmPlan& p, bool bf16) {
+    ChoiceGroups c;
+    if (bf16 && stream_block(M, N, K, p)) c.span = 8, c.pitch = 4, c.size = 8;
+    else if (p.bm == 256 || (p.bm == 128 && p.stages == 3)) c.span = 32, c.pitch = 8, c.size = 16;  // 32 x 32 tiles
+    else if (p.bm == 128) c.span = 64, c.pitch = 16, c.size = 16;
+    else c.span = 32, c.pitch = 16, c.size = 8;
+    c.count = (N + c.span - 1) / c.span * (c.pitch / 4);
+    return c;
 }
 
 hipError_t launch_gemm(const GemmArgs& g, const GemmPlan& p, bool bf16, hipStream_t s) {

@@ -31,7 +31,8 @@ EXPORTS = ["rdcn_create", "rdcn_destroy", "rdcn_dim", "rdcn_workspace_bytes", "q
            "qr_quantize_tables", "qr_embed_gather_q8", "rdcn_head_configure", "rdcn_head_workspace_bytes",
            "rdcn_head_forward", "rdcn_head_logloss", "rdcn_head_backward", "rdcn_set_side_stream",
            "qr_embed_backward_static", "rdcn_softmax_loss_workspace", "rdcn_softmax_loss_forward",
-           "rdcn_softmax_loss_grad", "rdcn_adamw_step", "rdcn_adamw_values", "rdcn_grad_norm_workspace",
+           "rdcn_softmax_loss_grad", "rdcn_logprobs_workspace", "rdcn_logprobs_forward", "rdcn_logprobs_grad",
+           "rdcn_adamw_step", "rdcn_adamw_values", "rdcn_grad_norm_workspace",
            "rdcn_grad_norm"]
 EMBED_STATIC_SCRATCH_BYTES = 64 << 20
 
@@ -40,6 +41,7 @@ KERNELS = ["gather", "fwd_down_gemm", "fwd_attention", "fwd_up_gemm", "bwd_point
            "emb_reduce", "gather_q8", "quantize", "head_gate", "head_fwd_gemm", "head_out", "head_loss",
            "head_out_bwd", "head_gw_gemm", "head_gx_gemm", "head_gate_bwd", "head_colsum", "emb_fused"]
 MAX_HIDDEN = 8
+LOGPROBS_TOP_MAX = 32
 
 
 class RdcnConfig(ctypes.Structure):
@@ -188,6 +190,10 @@ def load(build_if_missing: bool = True):
     L.rdcn_softmax_loss_workspace.argtypes = [vp, i64, i64, i64] + [ctypes.POINTER(sz)] * 3
     L.rdcn_softmax_loss_forward.argtypes = [vp, i64, i64, i64, vp, vp, vp, vp, f32, vp, vp, vp, sz, vp]
     L.rdcn_softmax_loss_grad.argtypes = [vp, i64, i64, i64, vp, vp, vp, vp, f32, vp, f32, vp, vp, vp, vp, vp, sz, vp]
+    L.rdcn_logprobs_workspace.argtypes = [vp, i64, i64, i64, ctypes.c_int32] + [ctypes.POINTER(sz)] * 4
+    L.rdcn_logprobs_forward.argtypes = [vp, i64, i64, i64, vp, vp, vp, vp, f32, ctypes.c_int32, vp, vp, vp, vp, vp, vp, vp,
+                                        sz, vp, sz, vp]
+    L.rdcn_logprobs_grad.argtypes = [vp, i64, i64, i64, vp, vp, vp, vp, f32, vp, vp, sz, vp, vp, vp, vp, vp, sz, vp]
     L.rdcn_adamw_step.argtypes = [vp, ctypes.POINTER(RdcnAdamwConfig), vp, ctypes.c_int32, vp]
     L.rdcn_adamw_values.argtypes = [vp, i64, vp, vp, ctypes.c_int32, vp, vp]
     L.rdcn_grad_norm_workspace.argtypes = [vp, vp, ctypes.c_int32, ctypes.POINTER(sz)]
@@ -397,6 +403,58 @@ class Rdcn:
             self.h, rows, dim, classes, _ptr(x), _ptr(w), _ptr(offset), _ptr(labels), logit_scale, _ptr(row_weight),
             scale, _ptr(loss), _ptr(lse), _ptr(grad_x), _ptr(grad_w), _ptr(scratch), _bytes(scratch),
             _stream(stream)))
+
+    def logprobs_workspace(self, rows: int, dim: int, classes: int, top: int = 0):
+        """Bytes of logprobs_forward's scratch, of `kept`, of logprobs_grad's scratch, and the least that it takes."""
+        s = [ctypes.c_size_t() for _ in range(4)]
+        _check("rdcn_logprobs_workspace", load().rdcn_logprobs_workspace(self.h, rows, dim, classes, top,
+                                                                         *[ctypes.byref(x) for x in s]))
+        return tuple(x.value for x in s)
+
+    def _choices(self, fn, rows, dim, classes, x, w, offset, labels, stats):
+        dt = torch.bfloat16 if self.cfg.dtype == BF16 else torch.float32
+        _fits(fn, "x", x, dt, rows * dim)
+        _fits(fn, "w", w, dt, classes * dim)
+        if labels is not None:
+            _fits(fn, "labels", labels, torch.int64 if self.cfg.id_type == I64 else torch.int32, rows)
+        if offset is not None:
+            _fits(fn, "offset", offset, torch.float32, classes)
+        if stats is not None:
+            _fits(fn, "stats", stats, torch.float32, 4 * rows)
+
+    def logprobs_forward(self, rows, dim, classes, x, w, offset, labels, logit_scale, logprob, entropy, lse, scratch, top=0,
+                         top_ids=None, top_logprob=None, stats=None, kept=None, stream=None):
+        """log p of `labels` [rows], entropies and log sums of every row (float [rows]; each may be None), and, with top, its
+        most probable classes (top_ids, the id type, and top_logprob, float, [rows, top]). stats (float [rows, 4]) and
+        kept are what logprobs_grad reads."""
+        fn = "logprobs_forward"
+        self._choices(fn, rows, dim, classes, x, w, offset, labels, stats)
+        for name, t in (("logprob", logprob), ("entropy", entropy), ("lse", lse)):
+            if t is not None:
+                _fits(fn, name, t, torch.float32, rows)
+        if top_ids is not None:
+            _fits(fn, "top_ids", top_ids, torch.int64 if self.cfg.id_type == I64 else torch.int32, rows * top)
+        if top_logprob is not None:
+            _fits(fn, "top_logprob", top_logprob, torch.float32, rows * top)
+        _check("rdcn_logprobs_forward", load().rdcn_logprobs_forward(
+            self.h, rows, dim, classes, _ptr(x), _ptr(w), _ptr(offset), _ptr(labels), logit_scale, top, _ptr(logprob),
+            _ptr(entropy), _ptr(lse), _ptr(top_ids), _ptr(top_logprob), _ptr(stats), _ptr(kept), _bytes(kept),
+            _ptr(scratch), _bytes(scratch), _stream(stream)))
+
+    def logprobs_grad(self, rows, dim, classes, x, w, offset, labels, logit_scale, stats, grad_logprob, grad_entropy, grad_x,
+                      grad_w, scratch, kept=None, stream=None):
+        """Gradients in x and w from those in log p and entropy (float [rows], or None)."""
+        fn = "logprobs_grad"
+        self._choices(fn, rows, dim, classes, x, w, offset, labels, stats)
+        for name, t in (("grad_logprob", grad_logprob), ("grad_entropy", grad_entropy)):
+            if t is not None:
+                _fits(fn, name, t, torch.float32, rows)
+        _fits(fn, "grad_x", grad_x, x.dtype, rows * dim)
+        _fits(fn, "grad_w", grad_w, w.dtype, classes * dim)
+        _check("rdcn_logprobs_grad", load().rdcn_logprobs_grad(
+            self.h, rows, dim, classes, _ptr(x), _ptr(w), _ptr(offset), _ptr(labels), logit_scale, _ptr(stats), _ptr(kept),
+            _bytes(kept), _ptr(grad_logprob), _ptr(grad_entropy), _ptr(grad_x), _ptr(grad_w), _ptr(scratch),
+            _bytes(scratch), _stream(stream)))
 
     def grad_norm_workspace(self, tensors) -> int:
         s = ctypes.c_size_t()
