@@ -669,6 +669,59 @@ rdcn_status rdcn_grad_norm(rdcn_handle* h, const rdcn_adamw_tensor* tensors, int
                            float max_norm, float* out, void* scratch, size_t scratch_bytes, void* stream);
 
 /*
+ * Muon: a momentum whose update of a matrix is made nearly orthogonal (its singular values taken to about 1, its singular
+ * vectors kept) by Newton-Schulz products. For the matrices of a model; vectors, tables and classes stay with rdcn_adamw_step. With
+ * g' = g * grad_scale * clip, over each [rows, cols] matrix:
+ *   m' = momentum m + (1 - momentum) g',  U = nesterov ? momentum m' + (1 - momentum) g' : m'
+ *   X  = U / |U| (the 2-norm of its elements; 0 where that is 0),  then `steps` times
+ *   X <- a X + b A X + c A A X,  A = X X^T
+ *   p' = p (1 - lr weight_decay) - lr scale X
+ * |U| is summed in 64 bits; the products carry 22 bits and float sums: X is within 2e-5 of its own norm (the more uneven its
+ * singular values, the nearer to that), where float products leave 1e-5; the other operations are one rounding to float each. The weights
+ * are as for rdcn_adamw_step: float, bf16 with a float master, or bf16 alone, rounded to nearest or (stochastic) by chance, with its bits.
+ * a, b, c = 3.4445, -4.7750, 2.0315 in 5 steps take all but the smallest singular values to within 0.7 to 1.2; 2, -1.5, 0.5
+ * in more steps to 1 itself. Coefficients whose iteration leaves the range of its f16 pairs (|a + b s^2 + c s^4| multiplied up to
+ * 10^6 between two fresh starts, or singular values beyond 8) are RDCN_ERR_UNSUPPORTED. `scale` evens out the shapes: sqrt(max(1, rows /
+ * cols)), or 0.2 sqrt(max(rows, cols)) for elements of AdamW's size.
+ */
+typedef struct rdcn_muon_tensor {
+    void* param;          /* [rows, cols] float or bf16, updated */
+    float* master;        /* [rows, cols] float, updated, or NULL (bf16 params only) */
+    const void* grad;     /* [rows, cols] float or bf16 */
+    float* m;             /* [rows, cols], updated; zeros to begin with */
+    int64_t rows, cols;   /* either may be 0; the longer at most 2^20, the shorter at most 2^14 */
+    double weight_decay;
+    double scale;
+    int32_t param_dtype;  /* rdcn_dtype */
+    int32_t grad_dtype;   /* rdcn_dtype */
+} rdcn_muon_tensor;
+
+typedef struct rdcn_muon_config {
+    double lr, momentum;           /* momentum in [0, 1) */
+    double grad_scale;             /* 1, or what undoes a loss scale */
+    double a, b, c;
+    int32_t steps;                 /* 1 .. 16 */
+    int32_t nesterov;              /* 0 or 1 */
+    const float* device_lr;        /* or NULL; device memory, read by the step instead of lr */
+    const int64_t* device_step;    /* or NULL; device memory, a step number for the random bits, so that a replayed step draws anew */
+    const float* clip;             /* or NULL; device memory, one float (rdcn_grad_norm's out + 1). A value that is not finite
+                                      leaves every weight and momentum as it is */
+    int32_t stochastic;            /* rdcn_rounding (RDCN_ROUND_CHANCE_CARRY as RDCN_ROUND_CHANCE) */
+    uint32_t seed;
+} rdcn_muon_config;
+
+/* Scratch bytes (256-byte aligned) of a step over these matrices; only rows and cols are read. */
+rdcn_status rdcn_muon_workspace(const rdcn_handle* h, const rdcn_muon_tensor* tensors, int32_t count, size_t* scratch_bytes);
+
+/*
+ * One step over `count` matrices (<= 65536). The list is read before the call returns. Arrays must be 16-byte
+ * aligned and must not overlap (overlapping weights are RDCN_ERR_ARG). Results depend on the arguments alone, not on
+ * what else is in the list (but for the random bits, which go by the place in it).
+ */
+rdcn_status rdcn_muon_step(rdcn_handle* h, const rdcn_muon_config* cfg, const rdcn_muon_tensor* tensors, int32_t count,
+                           void* scratch, size_t scratch_bytes, void* stream);
+
+/*
  * Per-kernel timing with HIP events on the stream each kernel is launched on.
  * After rdcn_profile_start, each launch site whose bit (1 << rdcn_kernel) is
  * set in `kernel_mask` records an event before and after its kernel(s), up to

@@ -60,14 +60,6 @@ __device__ __forceinline__ int tensor_of(const uint32_t* first, int count, uint3
     return lo;
 }
 
-__device__ __forceinline__ uint32_t fmix32(uint32_t h) {  // MurmurHash3's 32-bit finalizer
-    h ^= h >> 16;
-    h *= 0x85EBCA6Bu;
-    h ^= h >> 13;
-    h *= 0xC2B2AE35u;
-    return h ^ (h >> 16);
-}
-
 // Bits (from bit 20 up) that code 0 of a block whose largest exponent is e counts from.
 __device__ __forceinline__ uint32_t code_base(uint32_t e, uint32_t top) {
     const int b = (int)(8 * e + 7) - (int)top;

@@ -17,6 +17,7 @@
 #include "head.h"
 #include "kernels.h"
 #include "logprobs.h"
+#include "muon.h"
 #include "softmax_loss.h"
 
 struct rdcn_handle {
@@ -667,7 +668,10 @@ AdamwTensor adamw_tensor(const rdcn_adamw_tensor& x, int32_t ordinal, double lr)
 }
 
 // The same weights twice in one list would be a race; RDCN_OK, or RDCN_ERR_ARG if two ranges overlap.
-rdcn_status check_apart(const rdcn_adamw_tensor* t, int32_t count) {
+inline int64_t elements(const rdcn_adamw_tensor& t) { return t.n; }
+inline int64_t elements(const rdcn_muon_tensor& t) { return t.rows * t.cols; }
+template <typename Tensor>
+rdcn_status check_apart(const Tensor* t, int32_t count) {
     struct Range {
         uintptr_t from, to;
     };
@@ -676,7 +680,7 @@ rdcn_status check_apart(const rdcn_adamw_tensor* t, int32_t count) {
     if (!r) return RDCN_ERR_HIP;
     for (int32_t i = 0; i < count; ++i) {
         r[i].from = (uintptr_t)t[i].param;
-        r[i].to = r[i].from + (size_t)t[i].n * (t[i].param_dtype == RDCN_BF16 ? 2 : 4);
+        r[i].to = r[i].from + (size_t)elements(t[i]) * (t[i].param_dtype == RDCN_BF16 ? 2 : 4);
     }
     std::sort(r, r + count, [](const Range& a, const Range& b) { return a.from < b.from; });
     rdcn_status st = RDCN_OK;
@@ -690,14 +694,35 @@ rdcn_status check_apart(const rdcn_adamw_tensor* t, int32_t count) {
     return st;
 }
 
-struct TensorList {  // freed on every return
-    AdamwTensor few[64];
-    AdamwTensor* t;
-    explicit TensorList(int32_t count) : t(count <= 64 ? few : new (std::nothrow) AdamwTensor[count]) {}
-    ~TensorList() {
+template <typename Tensor>
+struct List {  // freed on every return
+    Tensor few[64];
+    Tensor* t;
+    explicit List(int32_t count) : t(count <= 64 ? few : new (std::nothrow) Tensor[count]) {}
+    ~List() {
         if (t != few) delete[] t;
     }
 };
+using TensorList = List<AdamwTensor>;
+
+// The caller's matrices in the kernels' form (`out` holds `count`). `step`: what a step reads is checked too.
+rdcn_status muon_list(const rdcn_handle* h, const rdcn_muon_tensor* t, int32_t count, bool step, MuonTensor* out) {
+    for (int32_t i = 0; i < count; ++i) {
+        const rdcn_muon_tensor& x = t[i];
+        if (x.rows < 0 || x.cols < 0) return RDCN_ERR_ARG;
+        if (std::max(x.rows, x.cols) > MUON_SIDE_MAX || std::min(x.rows, x.cols) > MUON_SHORT_MAX) return RDCN_ERR_UNSUPPORTED;
+        out[i] = MuonTensor{x.param, x.master, x.grad, x.m, x.rows, x.cols, x.weight_decay, x.scale,
+                            (x.param_dtype == RDCN_BF16 ? MUON_PARAM_BF16 : 0u) | (x.grad_dtype == RDCN_BF16 ? MUON_GRAD_BF16 : 0u) |
+                                (uint32_t)i << MUON_ORDINAL};
+        if (!step) continue;
+        if ((x.param_dtype != RDCN_F32 && x.param_dtype != RDCN_BF16) || (x.grad_dtype != RDCN_F32 && x.grad_dtype != RDCN_BF16) ||
+            !std::isfinite(x.weight_decay) || !std::isfinite(x.scale) || (x.master && x.param_dtype != RDCN_BF16))
+            return RDCN_ERR_ARG;
+        if (x.rows == 0 || x.cols == 0) continue;
+        if (!x.param || !a16(x.param) || !a16(x.master) || !x.grad || !a16(x.grad) || !x.m || !a16(x.m)) return RDCN_ERR_ARG;
+    }
+    return RDCN_OK;
+}
 
 }  // namespace
 
@@ -1673,6 +1698,49 @@ rdcn_status rdcn_adamw_values(rdcn_handle* h, int64_t n, const uint8_t* codes, c
     if (n == 0) return RDCN_OK;
     if (!codes || !a16(codes) || !exps || !out || !a16(out)) return RDCN_ERR_ARG;
     return hip_status(launch_adamw_values(n, codes, exps, is_signed != 0, out, (hipStream_t)stream));
+}
+
+rdcn_status rdcn_muon_workspace(const rdcn_handle* h, const rdcn_muon_tensor* tensors, int32_t count, size_t* scratch_bytes) {
+    if (!h || count < 0 || (count > 0 && !tensors) || !scratch_bytes) return RDCN_ERR_ARG;
+    if (count > ADAMW_MAX_TENSORS) return RDCN_ERR_UNSUPPORTED;
+    List<MuonTensor> l(count);
+    if (!l.t) return RDCN_ERR_HIP;
+    const rdcn_status st = muon_list(h, tensors, count, false, l.t);
+    if (st != RDCN_OK) return st;
+    *scratch_bytes = al(muon_scratch(l.t, count));
+    return RDCN_OK;
+}
+
+rdcn_status rdcn_muon_step(rdcn_handle* h, const rdcn_muon_config* cfg, const rdcn_muon_tensor* tensors, int32_t count,
+                           void* scratch, size_t scratch_bytes, void* stream) {
+    if (!h || !cfg || count < 0 || (count > 0 && !tensors)) return RDCN_ERR_ARG;
+    if (count > ADAMW_MAX_TENSORS) return RDCN_ERR_UNSUPPORTED;
+    const rdcn_muon_config& c = *cfg;
+    MuonScales q;
+    if (!std::isfinite((float)c.lr) || !(c.momentum >= 0.0 && c.momentum < 1.0) || !std::isfinite((float)c.grad_scale) ||
+        c.steps < 1 || (c.nesterov != 0 && c.nesterov != 1) ||
+        (c.stochastic != RDCN_ROUND_NEAREST && c.stochastic != RDCN_ROUND_CHANCE && c.stochastic != RDCN_ROUND_CHANCE_CARRY) ||
+        !std::isfinite((float)c.a) || !std::isfinite((float)c.b) || !std::isfinite((float)c.c))
+        return RDCN_ERR_ARG;
+    if (c.steps > MUON_STEPS_MAX) return RDCN_ERR_UNSUPPORTED;
+    if (!muon_scales(c.a, c.b, c.c, c.steps, &q)) return RDCN_ERR_UNSUPPORTED;
+    List<MuonTensor> l(count);
+    if (!l.t) return RDCN_ERR_HIP;
+    rdcn_status st = muon_list(h, tensors, count, true, l.t);
+    if (st != RDCN_OK) return st;
+    if ((st = check_apart(tensors, count)) != RDCN_OK) return st;
+    const size_t need = muon_scratch(l.t, count);
+    if (need > 0 && (!scratch || !aligned256(scratch) || scratch_bytes < need)) return RDCN_ERR_WORKSPACE;
+    MuonScalars a{};
+    a.mu = (float)c.momentum; a.c1 = (float)(1.0 - c.momentum);
+    a.nesterov = c.nesterov != 0;
+    a.stochastic = c.stochastic != RDCN_ROUND_NEAREST;
+    a.grad_scale = (float)c.grad_scale;
+    a.lr = c.lr;
+    a.device_lr = c.device_lr; a.device_step = c.device_step; a.clip = c.clip;
+    a.seed = c.seed;
+    a.a = c.a; a.b = c.b; a.c = c.c; a.steps = c.steps;
+    return hip_status(launch_muon(l.t, count, a, q, scratch, (hipStream_t)stream));
 }
 
 rdcn_status rdcn_profile_start(rdcn_handle* h, int32_t max_launches, uint32_t kernel_mask) {

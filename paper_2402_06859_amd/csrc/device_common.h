@@ -121,4 +121,12 @@ __device__ __forceinline__ uint64_t murmur64a_8(uint64_t key, uint64_t seed) {
     return h;
 }
 
+__device__ __forceinline__ uint32_t fmix32(uint32_t h) {  // MurmurHash3's 32-bit finalizer
+    h ^= h >> 16;
+    h *= 0x85EBCA6Bu;
+    h ^= h >> 13;
+    h *= 0xC2B2AE35u;
+    return h ^ (h >> 16);
+}
+
 }  // namespace rdcn

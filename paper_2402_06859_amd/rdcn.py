@@ -33,7 +33,7 @@ EXPORTS = ["rdcn_create", "rdcn_destroy", "rdcn_dim", "rdcn_workspace_bytes", "q
            "qr_embed_backward_static", "rdcn_softmax_loss_workspace", "rdcn_softmax_loss_forward",
            "rdcn_softmax_loss_grad", "rdcn_logprobs_workspace", "rdcn_logprobs_forward", "rdcn_logprobs_grad",
            "rdcn_adamw_step", "rdcn_adamw_values", "rdcn_grad_norm_workspace",
-           "rdcn_grad_norm"]
+           "rdcn_grad_norm", "rdcn_muon_workspace", "rdcn_muon_step"]
 EMBED_STATIC_SCRATCH_BYTES = 64 << 20
 
 KERNELS = ["gather", "fwd_down_gemm", "fwd_attention", "fwd_up_gemm", "bwd_pointwise", "bwd_bias", "bwd_gu_gemm",
@@ -83,6 +83,49 @@ class RdcnAdamwConfig(ctypes.Structure):
                 ("eps", ctypes.c_double), ("grad_scale", ctypes.c_double), ("step", ctypes.c_int64),
                 ("device_lr", ctypes.c_void_p), ("device_step", ctypes.c_void_p), ("clip", ctypes.c_void_p),
                 ("stochastic", ctypes.c_int32), ("seed", ctypes.c_uint32)]
+
+
+class RdcnMuonTensor(ctypes.Structure):
+    _fields_ = [("param", ctypes.c_void_p), ("master", ctypes.c_void_p), ("grad", ctypes.c_void_p),
+                ("m", ctypes.c_void_p), ("rows", ctypes.c_int64), ("cols", ctypes.c_int64),
+                ("weight_decay", ctypes.c_double), ("scale", ctypes.c_double), ("param_dtype", ctypes.c_int32),
+                ("grad_dtype", ctypes.c_int32)]
+
+
+class RdcnMuonConfig(ctypes.Structure):
+    _fields_ = [("lr", ctypes.c_double), ("momentum", ctypes.c_double), ("grad_scale", ctypes.c_double),
+                ("a", ctypes.c_double), ("b", ctypes.c_double), ("c", ctypes.c_double), ("steps", ctypes.c_int32),
+                ("nesterov", ctypes.c_int32), ("device_lr", ctypes.c_void_p), ("device_step", ctypes.c_void_p),
+                ("clip", ctypes.c_void_p), ("stochastic", ctypes.c_int32), ("seed", ctypes.c_uint32)]
+
+
+def muon_tensors(tensors: Sequence[dict]):
+    """Descriptors of matrices to step, once for many steps. Each is a dict of device tensors param, grad, m (float) and, where
+    it has one, master, all [rows, cols], and its weight_decay and scale. The caller keeps the tensors alive. What does not
+    fit is a ValueError here: the kernels go by pointers alone."""
+    out = (RdcnMuonTensor * len(tensors))()
+    for d, t in zip(out, tensors):
+        p = t["param"]
+        if p.dim() != 2:
+            raise ValueError("muon_tensors: param must have two dimensions")
+        for k in ("param", "master", "grad", "m"):
+            x = t.get(k)
+            if x is not None and (x.shape != p.shape or not x.is_contiguous() or x.device != tensors[0]["param"].device):
+                raise ValueError("muon_tensors: %s must be contiguous, of param's shape, and all on one device" % k)
+        for k in ("param", "grad"):
+            if t[k].dtype not in (torch.float32, torch.bfloat16):
+                raise ValueError("muon_tensors: %s must be float32 or bfloat16, not %s" % (k, t[k].dtype))
+        if t.get("master") is not None and (t["master"].dtype != torch.float32 or p.dtype != torch.bfloat16):
+            raise ValueError("muon_tensors: a master is float32, of a bfloat16 param")
+        if t["m"].dtype != torch.float32:
+            raise ValueError("muon_tensors: m must be float32")
+        for k in ("param", "master", "grad", "m"):
+            setattr(d, k, _ptr(t.get(k)))
+        d.rows, d.cols = p.shape
+        d.weight_decay, d.scale = t.get("weight_decay", 0.0), t.get("scale", 1.0)
+        d.param_dtype = BF16 if p.dtype == torch.bfloat16 else F32
+        d.grad_dtype = BF16 if t["grad"].dtype == torch.bfloat16 else F32
+    return out
 
 
 def adamw_tensors(tensors: Sequence[dict]):
@@ -198,6 +241,8 @@ def load(build_if_missing: bool = True):
     L.rdcn_adamw_values.argtypes = [vp, i64, vp, vp, ctypes.c_int32, vp, vp]
     L.rdcn_grad_norm_workspace.argtypes = [vp, vp, ctypes.c_int32, ctypes.POINTER(sz)]
     L.rdcn_grad_norm.argtypes = [vp, vp, ctypes.c_int32, f32, f32, vp, vp, sz, vp]
+    L.rdcn_muon_workspace.argtypes = [vp, vp, ctypes.c_int32, ctypes.POINTER(sz)]
+    L.rdcn_muon_step.argtypes = [vp, ctypes.POINTER(RdcnMuonConfig), vp, ctypes.c_int32, vp, sz, vp]
     L.rdcn_profile_start.argtypes = [vp, ctypes.c_int32, ctypes.c_uint32]
     L.rdcn_set_side_stream.argtypes = [vp, ctypes.c_int32]
     L.rdcn_profile_stop.argtypes = [vp, ctypes.POINTER(ctypes.c_double), ctypes.POINTER(ctypes.c_int64)]
@@ -496,6 +541,24 @@ class Rdcn:
         _check("rdcn_adamw_values", load().rdcn_adamw_values(self.h, n, _ptr(codes), _ptr(exps), int(signed),
                                                              _ptr(out), _stream(stream)))
         return out
+
+    def muon_workspace(self, tensors) -> int:
+        s = ctypes.c_size_t()
+        _check("rdcn_muon_workspace", load().rdcn_muon_workspace(self.h, tensors, len(tensors), ctypes.byref(s)))
+        return s.value
+
+    def muon_step(self, tensors, scratch, lr, momentum=0.95, nesterov=True, coefficients=(3.4445, -4.7750, 2.0315), steps=5,
+                  grad_scale=1.0, clip=None, stochastic=False, seed=0, device_lr=None, device_step=None, stream=None):
+        """One step over `tensors` (muon_tensors). On the device: device_lr (float) in place of lr, device_step (int64) for the
+        random bits, and clip (float), the factor that grad_norm leaves."""
+        for name, t, dt in (("clip", clip, torch.float32), ("device_lr", device_lr, torch.float32),
+                            ("device_step", device_step, torch.int64)):
+            if t is not None:
+                _fits("muon_step", name, t, dt, 1)
+        c = RdcnMuonConfig(lr, momentum, grad_scale, *coefficients, steps, int(nesterov), _ptr(device_lr), _ptr(device_step),
+                           _ptr(clip), int(stochastic), seed & 0xFFFFFFFF)
+        _check("rdcn_muon_step", load().rdcn_muon_step(self.h, ctypes.byref(c), tensors, len(tensors), _ptr(scratch),
+                                                       _bytes(scratch), _stream(stream)))
 
     def profile_start(self, max_launches: int = 8192, kernels=None):
         """Time the launches of `kernels` (names from KERNELS; all when None)."""
