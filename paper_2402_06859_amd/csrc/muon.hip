@@ -20,6 +20,7 @@
 // multiples of 64: zero rows stay zero rows of X, and no load needs a bound.
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "device_common.h"
 #include "mfma_tiles.h"
@@ -30,7 +31,9 @@ namespace rdcn {
 namespace {
 
 constexpr int PAD = 64;              // sides are padded to multiples of this
-constexpr int PARTS = 1024;          // most partial sums of a matrix's norm
+constexpr int PARTS = 512;           // most partial sums of a matrix's norm, each of at least PART elements
+constexpr int PART = 8192;
+constexpr int SPLIT_ROWS = 64, SPLIT_COLS = 128;
 constexpr int PER_LAUNCH = 24;       // matrices, or products, of one launch: their descriptors are kernel arguments
 constexpr int NAMES = 5;             // m x m matrices in scratch
 enum { GRAM = 0, HALF = 1, FREE = 2 };  // A, T A, and three for T and P in turn
@@ -61,10 +64,11 @@ struct Elements {  // the momentum and the split of many matrices
 };
 static_assert(sizeof(Elements) <= 4096, "kernel arguments");
 
+// The entry that workgroup b belongs to: one load for all of them, lane by lane (a search would wait for each in turn).
 __device__ __forceinline__ int entry_of(const uint32_t* first, int count, uint32_t b) {
-    int i = 0;
-    while (i + 1 < count && first[i + 1] <= b) ++i;
-    return i;
+    const int lane = threadIdx.x & 63;
+    const bool begun = lane < count && first[lane < PER_LAUNCH ? lane : PER_LAUNCH] <= b;
+    return __builtin_amdgcn_readfirstlane(__popcll(__ballot(begun)) - 1);
 }
 
 // Sum of 256 doubles over a workgroup, in a fixed order, for every thread.
@@ -87,8 +91,48 @@ __device__ __forceinline__ bool gradient_scale(const MuonScalars& a, float& gs) 
     return fabsf(c) < __builtin_huge_valf();
 }
 
-__device__ __forceinline__ float grad_at(const Matrix& t, int64_t i) {
-    return t.flags & MUON_GRAD_BF16 ? bf16_to_f32(((const bf16_t*)t.grad)[i]) : ((const float*)t.grad)[i];
+// Elements from <= e < to of v[8], as a pair.
+__device__ __forceinline__ void store_pair(uint16_t* c, int64_t plane, const float* v, int from, int to) {
+    if (to <= 0 || from >= 8) return;
+    bool ovf = false;
+    float hi[8], lo[8];
+    const u32x4_t h = pack_f16x8(v, ovf);
+    unpack_f16x8(h, hi);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) lo[e] = v[e] - hi[e];
+    const u32x4_t l = pack_f16x8(lo, ovf);
+    if (from <= 0 && to >= 8) {
+        *(u32x4_t*)c = h;
+        *(u32x4_t*)(c + plane) = l;
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        if (e < from || e >= to) continue;
+        c[e] = (uint16_t)(h[e / 2] >> (16 * (e & 1)));
+        c[plane + e] = (uint16_t)(l[e / 2] >> (16 * (e & 1)));
+    }
+}
+
+// Eight values of an array from element i on, `left` of which exist; whole: all of them, 16-byte aligned.
+__device__ __forceinline__ void load_f32(const float* p, int64_t i, int left, bool whole, float* v) {
+    if (whole) {
+        st<float>::unpack(*(const u32x4_t*)(p + i), v);
+        st<float>::unpack(*(const u32x4_t*)(p + i + 4), v + 4);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = e < left ? p[i + e] : 0.f;
+    }
+}
+__device__ __forceinline__ void load_grad(const Matrix& t, int64_t i, int left, bool whole, float* v) {
+    if (!(t.flags & MUON_GRAD_BF16)) {
+        load_f32((const float*)t.grad, i, left, whole, v);
+    } else if (whole) {
+        st<bf16_t>::unpack(*(const u32x4_t*)((const bf16_t*)t.grad + i), v);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = e < left ? bf16_to_f32(((const bf16_t*)t.grad)[i + e]) : 0.f;
+    }
 }
 __device__ __forceinline__ float update_of(const MuonScalars& a, float m, float g) {
 #pragma clang fp contract(off)
@@ -104,19 +148,36 @@ __global__ __launch_bounds__(256) void k_muon_momentum(Elements b) {
     const Matrix& t = b.t[i];
     const int64_t n = t.rows * t.cols, from = (int64_t)(blockIdx.x - b.first[i]) * t.per;
     const int64_t to = from + t.per < n ? from + t.per : n;
-    double s = 0.0;
-    for (int64_t k = from + threadIdx.x; k < to; k += 256) {
-        const float g = grad_at(t, k) * gs, m = t.m[k] * b.a.mu + g * b.a.c1;
-        if (taken) t.m[k] = m;
-        const double u = (double)update_of(b.a, m, g);
-        s = fma(u, u, s);
+    double s[2] = {0.0, 0.0};
+    for (int64_t k = from + threadIdx.x * 8; k < to; k += 2048) {
+        const int left = to - k < 8 ? (int)(to - k) : 8;
+        float g[8], m[8];
+        load_grad(t, k, left, left == 8, g);
+        load_f32(t.m, k, left, left == 8, m);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const float x = g[e] * gs;
+            m[e] = m[e] * b.a.mu + x * b.a.c1;
+            const double u = (double)update_of(b.a, m[e], x);
+            s[e & 1] = fma(u, u, s[e & 1]);
+        }
+        if (!taken) continue;
+        if (left == 8) {
+            *(u32x4_t*)(t.m + k) = st<float>::pack(m);
+            *(u32x4_t*)(t.m + k + 4) = st<float>::pack(m + 4);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (e < left) t.m[k + e] = m[e];
+        }
     }
-    s = block_sum(s);
-    if (threadIdx.x == 0) t.part[blockIdx.x - b.first[i]] = s;
+    const double sum = block_sum(s[0] + s[1]);
+    if (threadIdx.x == 0) t.part[blockIdx.x - b.first[i]] = sum;
 }
 
-// X = U / |U| as a pair of f16, padded with zeros; a workgroup per 64 x 64 block.
+// X = U / |U| as a pair of f16, padded with zeros; a workgroup per SPLIT_ROWS x SPLIT_COLS block, eight columns a thread.
 __global__ __launch_bounds__(256) void k_muon_split(Elements b) {
+#pragma clang fp contract(off)
     float gs;
     const bool taken = gradient_scale(b.a, gs);
     const int i = entry_of(b.first, b.count, blockIdx.x);
@@ -126,18 +187,23 @@ __global__ __launch_bounds__(256) void k_muon_split(Elements b) {
     s = block_sum(s);
     // (a norm of 0: X is 0, and only the decay moves the weights)
     const double inv = s == 0.0 ? 0.0 : (double)b.scale / sqrt(s);
-    const int block = (int)(blockIdx.x - b.first[i]), tiles = t.cp / 64;
-    const int r0 = block / tiles * 64, c = block % tiles * 64 + (threadIdx.x & 63);
+    const int block = (int)(blockIdx.x - b.first[i]), across = (t.cp + SPLIT_COLS - 1) / SPLIT_COLS;
+    const int r0 = block / across * SPLIT_ROWS, c = block % across * SPLIT_COLS + (threadIdx.x % (SPLIT_COLS / 8)) * 8;
+    if (c >= t.cp) return;
     const int64_t plane = (int64_t)t.rp * t.cp;
-    for (int r = r0 + (threadIdx.x >> 6); r < r0 + 64; r += 4) {
-        float v = 0.f;
+    for (int r = r0 + threadIdx.x / (SPLIT_COLS / 8); r < r0 + SPLIT_ROWS && r < t.rp; r += 256 / (SPLIT_COLS / 8)) {
+        float v[8] = {};
         if (taken && r < t.rows && c < t.cols) {
             const int64_t k = (int64_t)r * t.cols + c;
-            v = (float)((double)update_of(b.a, t.m[k], grad_at(t, k) * gs) * inv);
+            const int left = t.cols - c < 8 ? (int)(t.cols - c) : 8;
+            const bool whole = left == 8 && (k & 7) == 0;
+            float g[8], m[8];
+            load_grad(t, k, left, whole, g);
+            load_f32(t.m, k, left, whole, m);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = e < left ? (float)((double)update_of(b.a, m[e], g[e] * gs) * inv) : 0.f;
         }
-        const _Float16 hi = (_Float16)v, lo = (_Float16)(v - (float)hi);
-        t.x[(int64_t)r * t.cp + c] = __builtin_bit_cast(uint16_t, hi);
-        t.x[plane + (int64_t)r * t.cp + c] = __builtin_bit_cast(uint16_t, lo);
+        store_pair(t.x + (int64_t)r * t.cp + c, plane, v, 0, 8);
     }
 }
 
@@ -149,7 +215,7 @@ struct Product {
     int64_t ap, bp;          // (c's planes and aux's are M * N apart)
     int32_t lda, ldb;
     int32_t M, N, K;
-    int32_t matrix;          // STEP: its place in the launch's matrices
+    int32_t tall;
 };
 struct Destination {         // STEP: where the update goes
     void* param;
@@ -160,6 +226,82 @@ struct Destination {         // STEP: where the update goes
     uint32_t flags;
 };
 enum { PAIR = 0, POLY = 1, STEP = 2 };
+
+struct StepFactors {
+    float decay, size;
+    uint32_t key;
+};
+__device__ __forceinline__ bool step_factors(const MuonScalars& a, const Destination& d, StepFactors& f) {
+    float gs;
+    if (!gradient_scale(a, gs)) return false;
+    const double lr = a.device_lr ? (double)*a.device_lr : a.lr;
+    f.decay = (float)(1.0 - lr * (double)d.weight_decay);
+    f.size = (float)(lr * d.scale);
+    uint32_t seed = a.seed;
+    if (a.device_step) {  // a step that is replayed draws anew
+        const int64_t t = *a.device_step;
+        seed += (uint32_t)(t < 1 ? 1 : t) * 0x85EBCA6Bu;
+    }
+    f.key = seed + 0x9E3779B9u * ((d.flags >> MUON_ORDINAL) + 1u);
+    return true;
+}
+
+// p' of the elements (m, n) .. (m, n + 7) that the matrix has, v their X.
+__device__ __forceinline__ void step_elements(const MuonScalars& a, const Destination& d, const StepFactors& f, int64_t m, int64_t n,
+                                              const float* v) {
+#pragma clang fp contract(off)
+    if (m >= d.rows || n >= d.cols) return;
+    const int64_t at = m * d.cols + n;
+    const int left = d.cols - n < 8 ? (int)(d.cols - n) : 8;
+    const bool pbf = d.flags & MUON_PARAM_BF16, whole = left == 8 && (at & 7) == 0;
+    float p[8];
+    if (whole) {
+        if (d.master || !pbf) {
+            const float* const q = (d.master ? d.master : (const float*)d.param) + at;
+            st<float>::unpack(*(const u32x4_t*)q, p);
+            st<float>::unpack(*(const u32x4_t*)(q + 4), p + 4);
+        } else {
+            st<bf16_t>::unpack(*(const u32x4_t*)((const bf16_t*)d.param + at), p);
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            p[e] = e >= left ? 0.f : d.master ? d.master[at + e] : pbf ? bf16_to_f32(((const bf16_t*)d.param)[at + e]) : ((const float*)d.param)[at + e];
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) p[e] = p[e] * f.decay - v[e] * f.size;
+    if (d.master || !pbf) {
+        float* const q = (d.master ? d.master : (float*)d.param) + at;
+        if (whole) {
+            *(u32x4_t*)q = st<float>::pack(p);
+            *(u32x4_t*)(q + 4) = st<float>::pack(p + 4);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (e < left) q[e] = p[e];
+        }
+    }
+    if (!pbf) return;
+    uint32_t r[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        if (a.stochastic && !d.master) {
+            const uint32_t h = fmix32((uint32_t)(at + e) ^ f.key);
+            r[e] = (__float_as_uint(p[e]) + ((h * 0x85EBCA6Bu) >> 16)) >> 16;
+            r[e] = p[e] == p[e] ? r[e] : 0x7FC0u;  // (a NaN's bits could carry into its sign)
+        } else {
+            r[e] = f32_to_bf16(p[e]);
+        }
+    }
+    bf16_t* const q = (bf16_t*)d.param + at;
+    if (whole) {
+        *(u32x4_t*)q = u32x4_t{r[0] | r[1] << 16, r[2] | r[3] << 16, r[4] | r[5] << 16, r[6] | r[7] << 16};
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (e < left) q[e] = (bf16_t)r[e];
+    }
+}
 
 struct Products {
     Product p[PER_LAUNCH];
@@ -175,185 +317,260 @@ struct Products {
 };
 static_assert(sizeof(Products) <= 4096, "kernel arguments");
 
-template <int BM, int BN, bool AKS, bool BKS, int KB, int ST, bool SYM, int EPI>
-__global__ __launch_bounds__(256) void k_muon_product(Products b) {
-    constexpr int NW = 4, NIA = BM * KB / (512 * NW), NIB = BN * KB / (512 * NW), LOADS = 2 * (NIA + NIB);
-    constexpr int TM = BM / 64, TN = BN / 64, CP = BN + 4;
-    constexpr int EA = BM * KB, EB = BN * KB, STAGE = 2 * (EA + EB);  // a stage: A hi, A lo, B hi, B lo
-    static_assert(BM * CP * 4 <= ST * STAGE * 2, "the block's staged sums fit the ring");
-    __shared__ __attribute__((aligned(1024))) bf16_t smem[ST * STAGE];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, wm = wave >> 1, wn = wave & 1;
-    const int block = xcd_remap(blockIdx.x, gridDim.x);
-    const int i = entry_of(b.first, b.count, (uint32_t)block);
-    const Product& p = b.p[i];
-    const int t = block - (int)b.first[i], tiles_n = (p.N + BN - 1) / BN;
+// BM x BM blocks of WM x WN waves, each of 32 x 32 tiles; K in stages of KB through a ring of ST in LDS, filled by direct
+// global-to-LDS loads. One barrier a stage, before its last substep's multiplies, whose fragments are then in registers: behind it the
+// slot just read is filled again and the next stage's first fragments are read, every read and load between two multiplies.
+template <int BM, int WM, int WN, int KW, bool AKS, bool BKS, int KB, int ST, bool SYM, int EPI>
+__device__ __forceinline__ void product_block(const Products& b, int i, int t, bf16_t* smem) {
+    constexpr int NW = WM * WN * KW, THREADS = 64 * NW, NI = BM * KB / (512 * NW), LOADS = 4 * NI;
+    constexpr int TM = BM / WM / 32, TN = BM / WN / 32, NS = KB / 16 / KW, CH = 64, CP = BM + 4;
+    constexpr int EO = BM * KB, STAGE = 4 * EO;  // a stage: A hi, A lo, B hi, B lo
+    constexpr int MU = 3 * TM * TN, FR = 2 * (TM + TN);  // multiplies and fragments of a substep
+    constexpr int SUMS = TM * TN == 1 ? 3 : 1;           // one tile a wave: a sum for each of the three products, so that none waits
+    static_assert(NS % 2 == 0, "the fragment buffers alternate");
+    static_assert(CH * CP * 4 <= ST * STAGE * 2, "the staged sums fit the ring");
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, kw = wave / (WM * WN);
+    const int wm = wave / WN % WM, wn = wave % WN;
+    const Product p = b.p[i];  // (a copy: the loads' asm would have the arguments read again in every step)
+    // Groups of GROUP tile rows, walked column by column: the blocks that run together on an XCD share their panels in its L2.
+    constexpr int GROUP = BM == 256 ? 4 : 8;
+    const int tiles_m = (p.M + BM - 1) / BM, tiles_n = (p.N + BM - 1) / BM;
     int tm, tn;
-    if constexpr (SYM) {  // t = tm (tm + 1) / 2 + tn, tn <= tm
-        tm = (int)((sqrtf(8.f * (float)t + 1.f) - 1.f) * 0.5f);
-        while (tm * (tm + 1) / 2 > t) --tm;
-        while ((tm + 1) * (tm + 2) / 2 <= t) ++tm;
-        tn = t - tm * (tm + 1) / 2;
-    } else {
-        tm = t / tiles_n;
-        tn = t % tiles_n;
-    }
-    const int64_t m0 = (int64_t)tm * BM, n0 = (int64_t)tn * BN;
-
-    uint32_t aoff[NIA], boff[NIB];
-    stage_offsets<BM, AKS, NW, KB>(p.lda, p.M, m0, m0, wave, lane, aoff);
-    stage_offsets<BN, BKS, NW, KB>(p.ldb, p.N, n0, n0, wave, lane, boff);
-    const int nk = p.K / KB;
-    auto issue = [&](int kt) __attribute__((always_inline)) {
-        const int64_t k0 = (int64_t)(kt < nk ? kt : nk - 1) * KB;  // (past the last stage it is read again)
-        const uint16_t* const a = p.a + (AKS ? k0 * p.lda + m0 : m0 * p.lda + k0);
-        const uint16_t* const bb = p.b + (BKS ? k0 * p.ldb + n0 : n0 * p.ldb + k0);
-        const uint32_t base = (uint32_t)__builtin_amdgcn_readfirstlane((int)lds_addr(smem + kt % ST * STAGE));
-        const uint32_t wa = (uint32_t)__builtin_amdgcn_readfirstlane(wave * NIA) * 1024u;
-        const uint32_t wb = (uint32_t)__builtin_amdgcn_readfirstlane(wave * NIB) * 1024u;
-#pragma unroll
-        for (int q = 0; q < 2; ++q) {
-            const void* const sa = uniform_ptr(a + q * p.ap);
-            const void* const sb = uniform_ptr(bb + q * p.bp);
-#pragma unroll
-            for (int j = 0; j < NIA; ++j) dma16_s(aoff[j], sa, base + q * EA * 2u + wa + 1024u * j);
-#pragma unroll
-            for (int j = 0; j < NIB; ++j) dma16_s(boff[j], sb, base + 4u * EA + q * EB * 2u + wb + 1024u * j);
+    if constexpr (SYM) {
+        // on and under the diagonal: in front of group g lie GROUP^2 g (g - 1) / 2 + g GROUP (GROUP + 1) / 2 tiles; it has
+        // GROUP g whole columns, then a triangle
+        auto before = [](int g) { return GROUP * GROUP * (g * (g - 1) / 2) + g * (GROUP * (GROUP + 1) / 2); };
+        int g = (int)(sqrtf(2.f * (float)t) * (1.f / GROUP));
+        while (before(g) > t) --g;
+        while (before(g + 1) <= t) ++g;
+        const int rows = tiles_m - g * GROUP < GROUP ? tiles_m - g * GROUP : GROUP, r = t - before(g), whole = rows * g * GROUP;
+        if (r < whole) {
+            tn = r / rows;
+            tm = g * GROUP + r - tn * rows;
+        } else {
+            int row = 0, q = r - whole;
+            while (q > row) q -= ++row;
+            tm = g * GROUP + row;
+            tn = g * GROUP + q;
         }
+    } else {
+        const int per = GROUP * tiles_n, g = t / per, r = t - g * per;
+        const int rows = tiles_m - g * GROUP < GROUP ? tiles_m - g * GROUP : GROUP;
+        tn = r / rows;
+        tm = g * GROUP + r - tn * rows;
+    }
+    const int64_t m0 = (int64_t)tm * BM, n0 = (int64_t)tn * BM;
+
+    uint32_t aoff[NI], boff[NI];
+    stage_offsets<BM, AKS, NW, KB>(p.lda, p.M, m0, m0, wave, lane, aoff);
+    stage_offsets<BM, BKS, NW, KB>(p.ldb, p.N, n0, n0, wave, lane, boff);
+    const int nk = p.K / KB;
+    const uint32_t ring = (uint32_t)__builtin_amdgcn_readfirstlane((int)lds_addr(smem));
+    const uint32_t mine = (uint32_t)__builtin_amdgcn_readfirstlane(wave * NI) * 1024u;
+    struct Source {
+        const void* at[4];  // A hi, A lo, B hi, B lo
     };
-    f32x16_t acc[TM][TN];
+    auto source = [&](int kt) __attribute__((always_inline)) {
+        const int64_t k0 = (int64_t)kt * KB;
+        const uint16_t* const x = p.a + (AKS ? k0 * p.lda + m0 : m0 * p.lda + k0);
+        const uint16_t* const y = p.b + (BKS ? k0 * p.ldb + n0 : n0 * p.ldb + k0);
+        return Source{{uniform_ptr(x), uniform_ptr(x + p.ap), uniform_ptr(y), uniform_ptr(y + p.bp)}};
+    };
+    auto load = [&](int j, const Source& src, uint32_t off) __attribute__((always_inline)) {  // load j of a stage
+        const int o = j / NI, u = j % NI;
+        dma16_s(o < 2 ? aoff[u] : boff[u], src.at[o], ring + off + o * (EO * 2u) + mine + 1024u * u);
+    };
+    f32x16_t acc[SUMS][TM][TN];
 #pragma unroll
-    for (int x = 0; x < TM; ++x)
+    for (int z = 0; z < SUMS; ++z)
 #pragma unroll
-        for (int y = 0; y < TN; ++y)
+        for (int x = 0; x < TM; ++x)
 #pragma unroll
-            for (int e = 0; e < 16; ++e) acc[x][y][e] = 0.f;
+            for (int y = 0; y < TN; ++y)
 #pragma unroll
-    for (int u = 0; u < ST - 1; ++u) issue(u);
-    const uint32_t fa = frag_base<BM, AKS, KB>(smem, wm * (BM / 2), lane);
-    const uint32_t fb = frag_base<BN, BKS, KB>(smem + 2 * EA, wn * (BN / 2), lane);
-    for (int kt = 0; kt < nk; ++kt) {
-        wait_vmcnt(LOADS * (ST - 2));
-        __builtin_amdgcn_s_barrier();
-        issue(kt + ST - 1);
-        const uint32_t off = (uint32_t)(kt % ST) * (STAGE * 2u);
+                for (int e = 0; e < 16; ++e) acc[z][x][y][e] = 0.f;
+    uint32_t fa = frag_base<BM, AKS, KB>(smem, wm * (BM / WM), lane);
+    uint32_t fb = frag_base<BM, BKS, KB>(smem + 2 * EO, wn * (BM / WN), lane);
+    // (the substeps of wave group kw: NS from kw NS on)
+    if constexpr (!AKS) fa ^= (uint32_t)(kw * NS * 32);
+    else fa += (uint32_t)(kw * NS * 16 * BM * 2);
+    if constexpr (!BKS) fb ^= (uint32_t)(kw * NS * 32);
+    else fb += (uint32_t)(kw * NS * 16 * BM * 2);
+    bf16x8_t af[2][2][TM], bf[2][2][TN];  // [buffer][hi, lo]
+    auto frag = [&](int f, uint32_t off, int buf, int s) __attribute__((always_inline)) {
+        const int q = f / (TM + TN), g = f % (TM + TN);  // hi first
+        if (g < TN) bf[buf][q][g] = frag_at<BM, BKS, KB>(fb, off + q * (EO * 2u), g, s);
+        else af[buf][q][g - TN] = frag_at<BM, AKS, KB>(fa, off + q * (EO * 2u), g - TN, s);
+    };
+    // the small products first
+    auto mul = [&](int u, int buf) __attribute__((always_inline)) {
+        const int k = u / (TM * TN), x = u % (TM * TN) / TN, y = u % TN;
+        f32x16_t& c = acc[SUMS == 3 ? k : 0][x][y];
+        c = mfma32x32x16<true>(bf[buf][k == 0][y], af[buf][k == 1][x], c);
+    };
+    // QUARTIC's block of the Gram matrix, where a thread has little of it: on its way before the operands
+    constexpr int AHEAD = EPI == POLY && BM == 64 ? CH * (BM / 8) / THREADS : 0;
+    u32x4_t ahead[AHEAD + 1][2];
+    if constexpr (AHEAD > 0) {
 #pragma unroll
-        for (int s = 0; s < KB / 16; ++s) {
-            bf16x8_t ah[TM], al[TM], bh[TN], bl[TN];
+        for (int u = 0; u < AHEAD; ++u) {  // (sides are multiples of 64: the block is whole)
+            const int q = tid + u * THREADS;
+            const uint16_t* const at = p.aux + (m0 + q / (BM / 8)) * p.N + n0 + q % (BM / 8) * 8;
+            ahead[u][0] = *(const u32x4_t*)at;
+            ahead[u][1] = *(const u32x4_t*)(at + (int64_t)p.M * p.N);
+        }
+    }
+    constexpr uint32_t SB = STAGE * 2u;
+    for (int u = 0; u < ST && u < nk; ++u) {
+        const Source src = source(u);
 #pragma unroll
-            for (int x = 0; x < TM; ++x) {
-                ah[x] = frag_at<BM, AKS, KB>(fa, off, x, s);
-                al[x] = frag_at<BM, AKS, KB>(fa, off + EA * 2u, x, s);
+        for (int j = 0; j < LOADS; ++j) load(j, src, u * SB);
+    }
+    if (nk >= ST) wait_vmcnt(LOADS * (ST - 1));  // the first stage has landed
+    else wait_vmcnt(0);
+    __builtin_amdgcn_s_barrier();
+#pragma unroll
+    for (int f = 0; f < FR; ++f) frag(f, 0, 0, 0);
+    constexpr int RPM = MU > 4 ? (FR + MU - 3) / (MU - 2) : 2;  // fragments read behind a multiply
+    uint32_t cur = 0;
+    auto step = [&](int kt, auto refill_c) __attribute__((always_inline)) {
+        constexpr bool REFILL = decltype(refill_c)::value;
+        const uint32_t nxt = cur == (ST - 1) * SB ? 0 : cur + SB;
+        asm volatile("" : "+v"(fa), "+v"(fb));  // (addresses are formed here, not kept for every fragment)
+        const Source src = REFILL ? source(kt + ST) : Source{};
+#pragma unroll
+        for (int s = 0; s < NS; ++s) {
+            const bool last = s == NS - 1;
+            if (last) {
+                wait_lgkm0();                               // this wave's last reads of `cur` are done,
+                wait_vmcnt(REFILL ? LOADS * (ST - 2) : 0);  // and its loads of `nxt` have landed
+                __builtin_amdgcn_s_barrier();
             }
 #pragma unroll
-            for (int y = 0; y < TN; ++y) {
-                bh[y] = frag_at<BN, BKS, KB>(fb, off, y, s);
-                bl[y] = frag_at<BN, BKS, KB>(fb, off + EB * 2u, y, s);
+            for (int u = 0; u < MU; ++u) {
+                __builtin_amdgcn_sched_barrier(0);
+                mul(u, s & 1);
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int f = u * RPM; f < (u + 1) * RPM && f < FR; ++f)
+                    frag(f, last ? nxt : cur, (s + 1) & 1, last ? 0 : s + 1);
+                if (last && REFILL) {
+#pragma unroll
+                    for (int j = u * LOADS / MU; j < (u + 1) * LOADS / MU; ++j) load(j, src, cur);
+                }
             }
+        }
+        cur = nxt;
+    };
+    int kt = 0;
+#pragma unroll 1
+    for (; kt + ST < nk; ++kt) step(kt, std::true_type{});
+#pragma unroll 1
+    for (; kt < nk; ++kt) step(kt, std::false_type{});
+
+    float* const cs = (float*)smem;
+    const int64_t plane = (int64_t)p.M * p.N;
+    const float scale = i >= b.second ? b.scale2 : b.scale, out = i >= b.second ? b.out2 : b.out;
+    const bool diagonal = SYM && tm == tn;
+    StepFactors f;
+    if constexpr (EPI == STEP) {
+        if (!step_factors(b.s, b.d[i], f)) return;
+    }
+    // 64 rows at a time through LDS. Lane holds C[m = 32 x + lane % 32][n = 32 y + 8 q + 4 (lane / 32) + e] in acc[4 q + e].
 #pragma unroll
-            for (int x = 0; x < TM; ++x)
+    for (int h = 0; h < BM / CH; ++h) {
+        __syncthreads();
 #pragma unroll
-                for (int y = 0; y < TN; ++y) {
-                    acc[x][y] = mfma32x32x16<true>(bl[y], ah[x], acc[x][y]);
-                    acc[x][y] = mfma32x32x16<true>(bh[y], al[x], acc[x][y]);
-                    acc[x][y] = mfma32x32x16<true>(bh[y], ah[x], acc[x][y]);
+        for (int g = KW - 1; g >= 0; --g) {  // the wave groups' sums, added in turn
+            if (g < KW - 1) __syncthreads();
+            if (kw != g) continue;
+#pragma unroll
+        for (int x = 0; x < TM; ++x) {
+            const int row = wm * (BM / WM) + x * 32 + (lane & 31) - h * CH;
+            if (row < 0 || row >= CH) continue;
+#pragma unroll
+            for (int y = 0; y < TN; ++y)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    f32x4_t v;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        v[e] = acc[0][x][y][4 * q + e];
+                        if constexpr (SUMS == 3) v[e] = (v[e] + acc[1][x][y][4 * q + e]) + acc[2][x][y][4 * q + e];
+                    }
+                    f32x4_t* const at = (f32x4_t*)(cs + row * CP + wn * (BM / WN) + y * 32 + 8 * q + 4 * (lane >> 5));
+                    *at = g < KW - 1 ? *at + v : v;
                 }
         }
-    }
-    wait_vmcnt(0);  // the loads that were issued past the end have landed
-    __syncthreads();
-    // lane holds C[m = 32 x + lane % 32][n = 32 y + 8 q + 4 (lane / 32) + e] in acc[4 q + e]
-    float* const cs = (float*)smem;
-#pragma unroll
-    for (int x = 0; x < TM; ++x)
-#pragma unroll
-        for (int y = 0; y < TN; ++y)
-#pragma unroll
-            for (int q = 0; q < 4; ++q)
-                *(f32x4_t*)(cs + (wm * (BM / 2) + x * 32 + (lane & 31)) * CP + wn * (BN / 2) + y * 32 + 8 * q + 4 * (lane >> 5)) =
-                    f32x4_t{acc[x][y][4 * q], acc[x][y][4 * q + 1], acc[x][y][4 * q + 2], acc[x][y][4 * q + 3]};
-    __syncthreads();
-    if constexpr (EPI == STEP) {
-        const Destination& d = b.d[p.matrix];
-        float gs;
-        if (!gradient_scale(b.s, gs)) return;
-        const double lr = b.s.device_lr ? (double)*b.s.device_lr : b.s.lr;
-        const float decay = (float)(1.0 - lr * (double)d.weight_decay), size = (float)(lr * d.scale);
-        uint32_t seed = b.s.seed;
-        if (b.s.device_step) {  // a step that is replayed draws anew
-            int64_t st = *b.s.device_step;
-            seed += (uint32_t)(st < 1 ? 1 : st) * 0x85EBCA6Bu;
         }
-        const uint32_t key = seed + 0x9E3779B9u * ((d.flags >> MUON_ORDINAL) + 1u);
-        const bool pbf = d.flags & MUON_PARAM_BF16;
-        for (int q = tid; q < BM * BN; q += 256) {
-#pragma clang fp contract(off)
-            const int64_t m = m0 + q / BN, n = n0 + q % BN;
-            if (m >= d.rows || n >= d.cols) continue;
-            const int64_t at = m * d.cols + n;
-            float v = d.master ? d.master[at] : pbf ? bf16_to_f32(((const bf16_t*)d.param)[at]) : ((const float*)d.param)[at];
-            v = v * decay - (cs[q / BN * CP + q % BN] * b.scale) * size;
-            if (d.master) d.master[at] = v;
-            if (!pbf) {
-                ((float*)d.param)[at] = v;
-            } else if (b.s.stochastic && !d.master) {
-                const uint32_t h = fmix32((uint32_t)at ^ key);
-                const uint32_t r = (__float_as_uint(v) + ((h * 0x85EBCA6Bu) >> 16)) >> 16;
-                ((bf16_t*)d.param)[at] = (bf16_t)(v == v ? r : 0x7FC0u);  // (a NaN's bits could carry into its sign)
-            } else {
-                ((bf16_t*)d.param)[at] = (bf16_t)f32_to_bf16(v);
-            }
-        }
-    } else {
-        const int64_t plane = (int64_t)p.M * p.N;
-        const float scale = i >= b.second ? b.scale2 : b.scale, out = i >= b.second ? b.out2 : b.out;
-        const bool diagonal = SYM && tm == tn;
-        auto put = [&](int64_t at, const float* v) __attribute__((always_inline)) {
-            bool ovf = false;
-            float hi[8], lo[8];
-            const u32x4_t h = pack_f16x8(v, ovf);
-            unpack_f16x8(h, hi);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) lo[e] = v[e] - hi[e];
-            *(u32x4_t*)(p.c + at) = h;
-            *(u32x4_t*)(p.c + plane + at) = pack_f16x8(lo, ovf);
-        };
-        for (int q = tid; q < BM * (BN / 8); q += 256) {
-            const int r = q / (BN / 8), c = q % (BN / 8) * 8;
-            const int64_t m = m0 + r, n = n0 + c;
+        __syncthreads();
+#pragma unroll(AHEAD > 0 ? AHEAD : 1)
+        for (int u = 0; u < CH * (BM / 8) / THREADS; ++u) {
+            const int q = tid + u * THREADS, r = q / (BM / 8), c = q % (BM / 8) * 8;
+            const int64_t m = m0 + h * CH + r, n = n0 + c;
             if (m >= p.M || n >= p.N) continue;
             float v[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                // (a block on the diagonal is its lower half, twice: the matrix is symmetric to the bit)
-                const float x = diagonal && c + e > r ? cs[(c + e) * CP + r] : cs[r * CP + c + e];
-                v[e] = x * scale;
+            for (int e = 0; e < 8; ++e) v[e] = cs[r * CP + c + e] * scale;
+            if constexpr (EPI == STEP) {
+                step_elements(b.s, b.d[i], f, m, n, v);
+                continue;
             }
             if constexpr (EPI == POLY) {
-                float h[8], l[8];
-                unpack_f16x8(*(const u32x4_t*)(p.aux + m * p.N + n), h);
-                unpack_f16x8(*(const u32x4_t*)(p.aux + plane + m * p.N + n), l);
+                float hi[8], lo[8];
+                if constexpr (AHEAD > 0) {
+                    unpack_f16x8(ahead[u][0], hi);
+                    unpack_f16x8(ahead[u][1], lo);
+                } else {
+                    unpack_f16x8(*(const u32x4_t*)(p.aux + m * p.N + n), hi);
+                    unpack_f16x8(*(const u32x4_t*)(p.aux + plane + m * p.N + n), lo);
+                }
 #pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] = fmaf(b.pc, v[e], fmaf(b.pb, h[e] + l[e], m == n + e ? b.pa : 0.f));
+                for (int e = 0; e < 8; ++e) v[e] = fmaf(b.pc, v[e], fmaf(b.pb, hi[e] + lo[e], m == n + e ? b.pa : 0.f));
             }
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 v[e] *= out;
-                if (SYM && !diagonal) cs[r * CP + c + e] = v[e];
+                if (SYM) cs[r * CP + c + e] = v[e];
             }
-            put(m * p.N + n, v);
+            // (a block on the diagonal is its lower half, twice: the matrix is symmetric to the bit)
+            store_pair(p.c + m * p.N + n, plane, v, 0, diagonal ? (int)(m - n) + 1 : 8);
         }
-        if (SYM && !diagonal) {  // the block above the diagonal: rows n, columns m
+        if constexpr (SYM) {  // the block above the diagonal: rows n, columns m
             __syncthreads();
-            for (int q = tid; q < BN * (BM / 8); q += 256) {
-                const int r = q / (BM / 8), c = q % (BM / 8) * 8;
-                const int64_t n = n0 + r, m = m0 + c;
+            for (int q = tid; q < BM * (CH / 8); q += THREADS) {
+                const int r = q / (CH / 8), c = q % (CH / 8) * 8;
+                const int64_t n = n0 + r, m = m0 + h * CH + c;
                 if (m >= p.M || n >= p.N) continue;
                 float v[8];
 #pragma unroll
                 for (int e = 0; e < 8; ++e) v[e] = cs[(c + e) * CP + r];
-                put(n * p.N + m, v);
+                store_pair(p.c + n * p.N + m, plane, v, diagonal ? (int)(n - m) + 1 : 0, 8);
             }
         }
+    }
+}
+
+// Which operands' rows are K-strided, and what becomes of the sums.
+//   SQUARE, QUARTIC  products of symmetric matrices (symmetric too), QUARTIC with the polynomial in its epilogue
+//   GRAM             X X^T, or X^T X of a tall matrix
+//   NEXT, LAST       P X, or X P of a tall matrix: the next X, or the weights' step
+enum { SQUARE = 0, QUARTIC = 1, OF_X = 2, NEXT = 3, LAST = 4 };
+
+template <int BM, int WM, int WN, int KW, int KB, int ST, int KIND>
+__global__ __launch_bounds__(64 * WM * WN * KW) void k_muon_product(Products b) {
+    __shared__ __attribute__((aligned(1024))) bf16_t smem[ST * 4 * BM * KB];
+    const int block = xcd_remap(blockIdx.x, gridDim.x);
+    const int i = entry_of(b.first, b.count, (uint32_t)block), t = block - (int)b.first[i];
+    if constexpr (KIND == SQUARE) product_block<BM, WM, WN, KW, false, false, KB, ST, true, PAIR>(b, i, t, smem);
+    else if constexpr (KIND == QUARTIC) product_block<BM, WM, WN, KW, false, false, KB, ST, true, POLY>(b, i, t, smem);
+    else if constexpr (KIND == OF_X) {
+        if (b.p[i].tall) product_block<BM, WM, WN, KW, true, true, KB, ST, true, PAIR>(b, i, t, smem);
+        else product_block<BM, WM, WN, KW, false, false, KB, ST, true, PAIR>(b, i, t, smem);
+    } else {
+        constexpr int EPI = KIND == LAST ? STEP : PAIR;
+        if (b.p[i].tall) product_block<BM, WM, WN, KW, false, false, KB, ST, false, EPI>(b, i, t, smem);
+        else product_block<BM, WM, WN, KW, false, true, KB, ST, false, EPI>(b, i, t, smem);
     }
 }
 
@@ -378,24 +595,62 @@ Layout layout(const MuonTensor& t, size_t at) {
     for (size_t& x : l.x) x = take(l.rp * l.cp * 4);
     for (size_t& q : l.square) q = take(l.mp * l.mp * 4);
     const int64_t n = t.rows * t.cols;
-    l.per = std::max<int64_t>(2048, (n + PARTS - 1) / PARTS);
+    l.per = std::max<int64_t>(PART, ((n + PARTS - 1) / PARTS + 2047) / 2048 * 2048);
     l.parts = (n + l.per - 1) / l.per;
     l.part = take(l.parts * 8);
     l.total = at;
     return l;
 }
 
-template <bool SYM, int EPI, bool AKS, bool BKS>
+template <int KIND>
+int64_t blocks_of(const Product& p, int side) {
+    const int64_t tm = (p.M + side - 1) / side, tn = (p.N + side - 1) / side;
+    return KIND <= OF_X ? tm * (tm + 1) / 2 : tm * tn;
+}
+
+// How a launch's products are cut: whichever is through first. A K step of 64 takes, in us, `one` where a block has a CU for
+// itself, and `more` for every block of a CU where all of them are busy.
+struct Plan {
+    int side, per_cu;
+    double one, more;
+};
+constexpr Plan PLANS[] = {{64, 2, 0.9, 0.62}, {64, 1, 0.5, 0.75}, {128, 2, 1.75, 1.9}, {256, 1, 5.5, 5.5}};
+
+template <int KIND>
+const Plan& plan_of(const Products& b) {
+    const Plan* best = nullptr;
+    double least = 0.0;
+    for (const Plan& q : PLANS) {
+        double blocks = 0.0, steps = 0.0, longest = 0.0;
+        for (int i = 0; i < b.count; ++i) {
+            const double n = (double)blocks_of<KIND>(b.p[i], q.side), k = b.p[i].K / 64.0;
+            blocks += n;
+            steps += n * k;
+            longest = std::max(longest, k);
+        }
+        const double mean = steps / blocks, us = std::max(longest * q.one, std::ceil(blocks / 256.0) * mean * (blocks > 256.0 ? q.more : q.one));
+        if (!best || us < least) {
+            best = &q;
+            least = us;
+        }
+    }
+    return *best;
+}
+
+template <int KIND>
 hipError_t launch_products(Products& b, hipStream_t s) {
+    if (b.count == 0) return hipSuccess;
+    const Plan& plan = plan_of<KIND>(b);
     uint32_t n = 0;
     for (int i = 0; i < b.count; ++i) {
         b.first[i] = n;
-        const int64_t tm = b.p[i].M / 64, tn = b.p[i].N / 64;
-        n += (uint32_t)(SYM ? tm * (tm + 1) / 2 : tm * tn);
+        n += (uint32_t)blocks_of<KIND>(b.p[i], plan.side);
     }
     b.first[b.count] = n;
-    if (n == 0) return hipSuccess;
-    hipLaunchKernelGGL((k_muon_product<64, 64, AKS, BKS, 64, 3, SYM, EPI>), dim3(n), dim3(256), 0, s, b);
+    if (plan.side == 256) hipLaunchKernelGGL((k_muon_product<256, 2, 4, 1, 32, 2, KIND>), dim3(n), dim3(512), 0, s, b);
+    else if (plan.side == 128) hipLaunchKernelGGL((k_muon_product<128, 2, 2, 1, 32, 2, KIND>), dim3(n), dim3(256), 0, s, b);
+    else if (plan.per_cu == 1) hipLaunchKernelGGL((k_muon_product<64, 2, 2, 2, 64, 4, KIND>), dim3(n), dim3(512), 0, s, b);
+    else hipLaunchKernelGGL((k_muon_product<64, 2, 2, 2, 64, 2, KIND>), dim3(n), dim3(512), 0, s, b);
     return hipGetLastError();
 }
 
@@ -461,7 +716,7 @@ hipError_t run_batch(const MuonTensor* t, const Layout* l, int count, const Muon
         n = 0;
         for (int i = 0; i < count; ++i) {
             b.first[i] = n;
-            n += (uint32_t)((l[i].rp / 64) * (l[i].cp / 64));
+            n += (uint32_t)((l[i].rp + SPLIT_ROWS - 1) / SPLIT_ROWS * ((l[i].cp + SPLIT_COLS - 1) / SPLIT_COLS));
         }
         b.first[count] = n;
         hipLaunchKernelGGL(k_muon_split, dim3(n), dim3(256), 0, s, b);
@@ -483,55 +738,44 @@ hipError_t run_batch(const MuonTensor* t, const Layout* l, int count, const Muon
         p.lda = p.ldb = p.M = p.N = p.K = (int32_t)l[i].mp;
     };
     // A from X
-    auto gram = [&](int x, float sx, float sa) -> hipError_t {
-        for (int tall = 0; tall < 2; ++tall) {
-            begin();
-            b.scale = 1.f / (sx * sx);
-            b.out = sa;
-            for (int i = 0; i < count; ++i) {
-                if (l[i].tall != (tall == 1)) continue;
-                Product& p = b.p[b.count++];
-                p = Product{};
-                p.a = p.b = (uint16_t*)(sc + l[i].x[x]);
-                p.ap = p.bp = l[i].rp * l[i].cp;
-                p.lda = p.ldb = (int32_t)l[i].cp;
-                p.M = p.N = (int32_t)l[i].mp;
-                p.K = (int32_t)(tall ? l[i].rp : l[i].cp);
-                p.c = square(i, GRAM);
-            }
-            const hipError_t r = tall ? launch_products<true, PAIR, true, true>(b, s) : launch_products<true, PAIR, false, false>(b, s);
-            if (r != hipSuccess) return r;
+    auto gram = [&](int x, float sx, float sa) {
+        begin();
+        b.scale = 1.f / (sx * sx);
+        b.out = sa;
+        for (int i = 0; i < count; ++i) {
+            Product& p = b.p[b.count++];
+            p = Product{};
+            p.tall = l[i].tall;
+            p.a = p.b = (uint16_t*)(sc + l[i].x[x]);
+            p.ap = p.bp = l[i].rp * l[i].cp;
+            p.lda = p.ldb = (int32_t)l[i].cp;
+            p.M = p.N = (int32_t)l[i].mp;
+            p.K = (int32_t)(l[i].tall ? l[i].rp : l[i].cp);
+            p.c = square(i, GRAM);
         }
-        return hipSuccess;
+        return launch_products<OF_X>(b, s);
     };
     // P X (X P of a tall matrix): the next X, or the weights' step
-    auto apply = [&](int x, int pw, float sx, float sp, float out, bool step) -> hipError_t {
-        for (int tall = 0; tall < 2; ++tall) {
-            begin();
-            b.scale = 1.f / (sx * sp);
-            b.out = out;
-            for (int i = 0; i < count; ++i) {
-                if (l[i].tall != (tall == 1)) continue;
-                Product& p = b.p[b.count];
-                p = Product{};
-                const uint16_t* const xs = (uint16_t*)(sc + l[i].x[x]);
-                const int64_t xp = l[i].rp * l[i].cp, pp = l[i].mp * l[i].mp;
-                p.a = tall ? xs : square(i, pw); p.ap = tall ? xp : pp;
-                p.b = tall ? square(i, pw) : xs; p.bp = tall ? pp : xp;
-                p.lda = (int32_t)(tall ? l[i].cp : l[i].mp);
-                p.ldb = (int32_t)(tall ? l[i].mp : l[i].cp);
-                p.M = (int32_t)l[i].rp; p.N = (int32_t)l[i].cp; p.K = (int32_t)l[i].mp;
-                p.c = (uint16_t*)(sc + l[i].x[1 - x]);
-                p.matrix = b.count;
-                b.d[b.count++] = Destination{t[i].param, t[i].master, t[i].rows, t[i].cols, t[i].scale,
-                                             (float)t[i].weight_decay, t[i].flags};
-            }
-            hipError_t r;
-            if (step) r = tall ? launch_products<false, STEP, false, false>(b, s) : launch_products<false, STEP, false, true>(b, s);
-            else r = tall ? launch_products<false, PAIR, false, false>(b, s) : launch_products<false, PAIR, false, true>(b, s);
-            if (r != hipSuccess) return r;
+    auto apply = [&](int x, int pw, float sx, float sp, float out, bool step) {
+        begin();
+        b.scale = 1.f / (sx * sp);
+        b.out = out;
+        for (int i = 0; i < count; ++i) {
+            const bool tall = l[i].tall;
+            const uint16_t* const xs = (uint16_t*)(sc + l[i].x[x]);
+            const int64_t xp = l[i].rp * l[i].cp, pp = l[i].mp * l[i].mp;
+            b.d[b.count] = Destination{t[i].param, t[i].master, t[i].rows, t[i].cols, t[i].scale, (float)t[i].weight_decay, t[i].flags};
+            Product& p = b.p[b.count++];
+            p = Product{};
+            p.tall = tall;
+            p.a = tall ? xs : square(i, pw); p.ap = tall ? xp : pp;
+            p.b = tall ? square(i, pw) : xs; p.bp = tall ? pp : xp;
+            p.lda = (int32_t)(tall ? l[i].cp : l[i].mp);
+            p.ldb = (int32_t)(tall ? l[i].mp : l[i].cp);
+            p.M = (int32_t)l[i].rp; p.N = (int32_t)l[i].cp; p.K = (int32_t)l[i].mp;
+            p.c = (uint16_t*)(sc + l[i].x[1 - x]);
         }
-        return hipSuccess;
+        return step ? launch_products<LAST>(b, s) : launch_products<NEXT>(b, s);
     };
 
     int x = 0, power = -1;  // the X that stands, and the name of P (none yet: I)
@@ -549,7 +793,7 @@ hipError_t run_batch(const MuonTensor* t, const Layout* l, int count, const Muon
         b.scale = 1.f / (q.gram[k] * q.gram[k]);
         b.out = q.poly[k];
         b.pa = (float)a.a; b.pb = (float)(a.b / q.gram[k]); b.pc = (float)a.c;
-        if ((e = launch_products<true, POLY, false, false>(b, s)) != hipSuccess) return e;
+        if ((e = launch_products<QUARTIC>(b, s)) != hipSuccess) return e;
         // T A (where another A follows) and T P beside it
         begin();
         if (!last && !anew)
@@ -565,7 +809,7 @@ hipError_t run_batch(const MuonTensor* t, const Layout* l, int count, const Muon
             while (next == poly || next == power) ++next;
             for (int i = 0; i < count; ++i) add(i, poly, power, next);
         }
-        if (b.count && (e = launch_products<true, PAIR, false, false>(b, s)) != hipSuccess) return e;
+        if (b.count && (e = launch_products<SQUARE>(b, s)) != hipSuccess) return e;
         sp = power >= 0 ? q.power[k] : q.poly[k];
         power = next;
         if (anew) {
@@ -579,7 +823,7 @@ hipError_t run_batch(const MuonTensor* t, const Layout* l, int count, const Muon
             for (int i = 0; i < count; ++i) add(i, poly, HALF, GRAM);
             b.scale = 1.f / (q.poly[k] * q.half[k]);
             b.out = q.gram[k + 1];
-            if ((e = launch_products<true, PAIR, false, false>(b, s)) != hipSuccess) return e;
+            if ((e = launch_products<SQUARE>(b, s)) != hipSuccess) return e;
         }
     }
     return apply(x, power, sx, sp, 1.f, true);
@@ -602,9 +846,16 @@ int next_run(const MuonTensor* t, int i, int count, Run* r) {
         const int64_t n = padded(t[i].rows) / 64 * (padded(t[i].cols) / 64);
         if (r->count > 0 && blocks + n > (int64_t)1 << 22) break;
         blocks += n;
-        r->t[r->count] = t[i];
-        r->l[r->count] = layout(t[i], r->total);
-        r->total = r->l[r->count++].total;
+        r->t[r->count++] = t[i];
+    }
+    // those with the longest sums first: a launch's last blocks are then short ones
+    std::sort(r->t, r->t + r->count, [](const MuonTensor& x, const MuonTensor& y) {
+        const int64_t a = std::min(x.rows, x.cols), b = std::min(y.rows, y.cols);
+        return a != b ? a > b : x.flags < y.flags;
+    });
+    for (int k = 0; k < r->count; ++k) {
+        r->l[k] = layout(r->t[k], r->total);
+        r->total = r->l[k].total;
     }
     return i;
 }
