@@ -556,7 +556,9 @@ rdcn_status rdcn_softmax_loss_grad(rdcn_handle* h, int64_t rows, int64_t dim, in
  *     lse -inf and entropy 0.
  *   - A row whose logits hold NaN or +inf has NaN results, and ids of its own choice (in range, or -1).
  * top is 0 (no lists) .. RDCN_LOGPROBS_TOP_MAX; top_ids in the handle's id type. logprob, entropy, lse, top_logprob and stats may
- * be NULL. stats [rows, 4] float, 16-byte aligned, and `kept` are for the gradient: what it needs of a row, and of the logits.
+ * be NULL. stats [rows, 4] float, 16-byte aligned, is what the gradient needs of a row. `kept` (or NULL) saves the gradient a
+ * product: it takes every class's exponential, as f16 in bf16 models (2^-11 of it, growing from 2^-29 of the largest of the 16 to 64 classes
+ * around it on, and 0 below 2^-40), as float in float ones.
  */
 #define RDCN_LOGPROBS_TOP_MAX 32
 
@@ -575,7 +577,7 @@ rdcn_status rdcn_logprobs_forward(rdcn_handle* h, int64_t rows, int64_t dim, int
  * The gradients of any loss in x and w, from its gradients in logprob and entropy ([rows] float, either may be NULL for 0):
  *   dL/dz[n, v] = g ([v = label] - p) - h p (log p + entropy),  g = grad_logprob[n], h = grad_entropy[n]
  *   grad_x = s dL/dz w, grad_w = s (dL/dz)^T x, both in the storage dtype and overwritten.
- * stats must be those of a forward with the same x, w, offset, labels and logit_scale. Rows without a label (when labels are given), and rows whose
+ * stats (and kept, or NULL) must be those of a forward with the same x, w, offset, labels and logit_scale; both stay as they are. Rows without a label (when labels are given), and rows whose
  * g and h are both 0, have no gradient and may hold anything in x and stats. Masked logits are constants. bf16 models round dL/dz
  * to bf16 for the products (half a step, 2^-8 of an element) and each gradient once at the end; sums are float and in a fixed order.
  * 1 - p of a label keeps its digits where p is near 1. With grad_bytes of scratch the call is fastest; it takes any size from

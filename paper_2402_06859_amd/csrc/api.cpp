@@ -569,10 +569,13 @@ rdcn_status soft_forward(rdcn_handle* h, const SoftPlan& S, int64_t rows, int64_
 // ---------------------------------------------------------------------------
 // Log probabilities. Forward: the logits product, whose epilogue leaves a ChoiceStat per row and column tile and (for the most
 // probable classes) a pair per group of classes, then one kernel over the rows. Gradient: G [rows, classes] stands in scratch, for as
-// many classes at a time as it holds, from the logits computed again; its two products are the softmax loss's.
+// many classes at a time as it holds, from the exponentials that the forward kept (2 bytes each, 4 in float models: one read and
+// one write in place of a product) or from the logits computed again; its two products are the softmax loss's.
 // ---------------------------------------------------------------------------
 struct ChoicePlan {
-    int64_t tiles, piece, ld;
+    int64_t tiles, tile, piece, ld;
+    int64_t kept_ld;
+    size_t kept_stat, kept_total;  // of `kept`: the exponentials, then the tiles' ChoiceStats
     ChoiceGroups g;
     size_t stat, zlabel, groups, forward_total;
     size_t kept, G, acc, splitk, splitw, row, total;
@@ -588,6 +591,10 @@ ChoicePlan choice_layout(const rdcn_handle* h, int64_t rows, int64_t dim, int64_
     s.tiles = rows > 0 ? gemm_soft_tiles(rows, classes, dim, p, h->bf16, &tile) : 0;
     if (rows > 0) s.g = gemm_choice_groups(rows, classes, dim, p, h->bf16);
     size_t off = 0;
+    s.tile = tile;
+    s.kept_ld = (classes + vec - 1) / vec * vec;
+    s.kept_stat = al((size_t)rows * s.kept_ld * e);
+    s.kept_total = s.kept_stat + al((size_t)s.tiles * rows * sizeof(ChoiceStat));
     s.stat = off; off += al((size_t)s.tiles * rows * sizeof(ChoiceStat));
     s.zlabel = off; off += al((size_t)rows * 4);
     s.groups = off; off += top > 0 ? al((size_t)s.g.count * rows * 8) : 0;
@@ -1517,8 +1524,9 @@ rdcn_status rdcn_logprobs_workspace(const rdcn_handle* h, int64_t rows, int64_t 
     if (st != RDCN_OK) return st;
     if (!forward_bytes || !kept_bytes || !grad_bytes || !grad_least_bytes || top < 0) return RDCN_ERR_ARG;
     if (top > RDCN_LOGPROBS_TOP_MAX) return RDCN_ERR_UNSUPPORTED;
-    *forward_bytes = choice_layout(h, rows, dim, classes, top, classes).forward_total;
-    *kept_bytes = 0;
+    const ChoicePlan F = choice_layout(h, rows, dim, classes, top, classes);
+    *forward_bytes = F.forward_total;
+    *kept_bytes = F.kept_total;
     const ChoicePlan S = choice_plan(h, rows, dim, classes, SIZE_MAX);
     *grad_bytes = S.total;
     *grad_least_bytes = std::min(S.total, choice_plan(h, rows, dim, classes, 0).total);
@@ -1537,9 +1545,9 @@ rdcn_status rdcn_logprobs_forward(rdcn_handle* h, int64_t rows, int64_t dim, int
     if (!x || !a16(x) || !w || !a16(w) || (logprob && !labels) || (top > 0 && !top_ids) || !a16(stats)) return RDCN_ERR_ARG;
     const ChoicePlan S = choice_layout(h, rows, dim, classes, top, classes);
     if (!scratch || !aligned256(scratch) || scratch_bytes < S.forward_total) return RDCN_ERR_WORKSPACE;
+    if (kept && (!aligned256(kept) || kept_bytes < S.kept_total)) return RDCN_ERR_WORKSPACE;
     char* const sc = (char*)scratch;
     hipStream_t s = (hipStream_t)stream;
-    (void)kept; (void)kept_bytes;
     GemmArgs g{};
     g.M = rows; g.N = classes; g.K = dim;
     g.a = x; g.lda = dim;
@@ -1548,7 +1556,8 @@ rdcn_status rdcn_logprobs_forward(rdcn_handle* h, int64_t rows, int64_t dim, int
     g.offset = offset;
     g.labels = labels; g.labels64 = h->ids64;
     g.zlabel = (float*)(sc + S.zlabel);
-    g.stat = (ChoiceStat*)(sc + S.stat); g.tiles = S.tiles;
+    g.stat = (ChoiceStat*)(kept ? (char*)kept + S.kept_stat : sc + S.stat); g.tiles = S.tiles;
+    g.c = kept; g.ldc = S.kept_ld;
     if (top > 0) g.groups = (uint2*)(sc + S.groups);
     g.ngroups = S.g.count;
     {
@@ -1582,7 +1591,7 @@ rdcn_status rdcn_logprobs_grad(rdcn_handle* h, int64_t rows, int64_t dim, int64_
     if (!x || !a16(x) || !stats || !a16(stats) || !grad_x || !a16(grad_x)) return RDCN_ERR_ARG;
     const ChoicePlan S = choice_plan(h, rows, dim, classes, scratch_bytes);
     if (!scratch || !aligned256(scratch) || scratch_bytes < S.total) return RDCN_ERR_WORKSPACE;
-    (void)kept; (void)kept_bytes;
+    if (kept && (!aligned256(kept) || kept_bytes < S.kept_total)) return RDCN_ERR_WORKSPACE;
     char* const sc = (char*)scratch;
     ChoiceRow* const row = (ChoiceRow*)(sc + S.row);
     float* const acc = (float*)(sc + S.acc);
@@ -1602,16 +1611,27 @@ rdcn_status rdcn_logprobs_grad(rdcn_handle* h, int64_t rows, int64_t dim, int64_
     for (int64_t v = 0; v < classes; v += S.piece) {
         const int64_t n = std::min(S.piece, classes - v);
         const void* const wp = (const char*)w + (size_t)v * dim * e;
-        GemmArgs g{};
-        g.M = rows; g.N = n; g.K = dim;
-        g.a = x; g.lda = dim;
-        g.b = wp; g.ldb = dim;
-        g.epi = EPI_CHOICE_GRAD; g.scale = logit_scale;
-        g.offset = offset ? offset + v : nullptr;
-        g.labels = labels; g.labels64 = h->ids64; g.label0 = v;
-        g.choicerow = row;
-        g.c = G; g.ldc = S.ld;
-        {
+        if (kept) {
+            ChoiceNormalize q{};
+            q.rows = rows; q.tiles = S.tiles; q.tile = S.tile;
+            q.first = v; q.width = v + n == classes ? S.kept_ld - v : n;
+            q.ld = S.ld; q.kept_ld = S.kept_ld;
+            q.stat = (const ChoiceStat*)((const char*)kept + S.kept_stat);
+            q.row = row;
+            q.labels = labels; q.ids64 = h->ids64;
+            q.kept = kept; q.out = G;
+            ProfScope ps(h, RDCN_KERNEL_HEAD_OUT_BWD, s);
+            RDCN_TRY(launch_choice_normalize(q, h->bf16, s));
+        } else {
+            GemmArgs g{};
+            g.M = rows; g.N = n; g.K = dim;
+            g.a = x; g.lda = dim;
+            g.b = wp; g.ldb = dim;
+            g.epi = EPI_CHOICE_GRAD; g.scale = logit_scale;
+            g.offset = offset ? offset + v : nullptr;
+            g.labels = labels; g.labels64 = h->ids64; g.label0 = v;
+            g.choicerow = row;
+            g.c = G; g.ldc = S.ld;
             ProfScope ps(h, RDCN_KERNEL_HEAD_FWD_GEMM, s);
             RDCN_TRY(launch_gemm(g, plan_logits(h, rows, n, dim), h->bf16, s));
         }

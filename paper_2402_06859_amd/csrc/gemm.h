@@ -29,7 +29,8 @@ enum GemmEpi {
                         // where r.c is 0 or z is -inf and in the pad of a row
     // Log probabilities (both operands K-contiguous), z as above:
     EPI_CHOICE_FWD = 10,  // stat[m * tiles + t] = ChoiceStat of the classes of column tile t (gemm_soft_tiles); zlabel[m] = z at
-                          // the label; with groups: groups[m * ngroups + u] of the classes of group u (gemm_choice_groups)
+                          // the label; with groups: groups[m * ngroups + u] of the classes of group u (gemm_choice_groups);
+                          // with c: c = exp(z - max of the tile) (f16 times SOFT_E_SCALE, or float), zero in the pad of a row
     EPI_CHOICE_GRAD = 11  // c = exp(d) (r.a + r.b d) for d = z - r.max, r = choicerow[m], r.label at the row's label (storage
                           // type), zero where r.a and r.b are 0 or z is -inf and in the pad of a row
 };

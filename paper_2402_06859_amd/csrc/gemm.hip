@@ -357,28 +357,43 @@ __device__ __forceinline__ uint2 choice_group(F value) {
 #pragma unroll
     for (int i = 1; i < N; ++i) {
         const float x = value(i);
-        const bool more = x > top;
-        second = fmaxf(second, more ? top : x);
-        at = more ? i : at;
-        top = more ? x : top;
+        at = x > top ? i : at;
+        second = __builtin_amdgcn_fmed3f(top, second, x);  // (second <= top: the middle of the three is the new second)
+        top = fmaxf(top, x);
     }
     // rounded up in its last 4 bits, which hold the place
     const uint32_t b = __float_as_uint(second);
     return make_uint2(__float_as_uint(top), (((int)b < 0 ? b - 16u : b + 16u) & ~15u) | (uint32_t)at);
 }
 
-// exp(d) of N logits less their maximum: adds to the sum over those below the maximum, counts those at it, and
-// adds up exp(d) d. (An exponential of 1 is one at the maximum, or as near as a float tells.)
-template <typename T, int N, typename F>
-__device__ __forceinline__ void choice_sums(F z, float top, float& below, float& at_top, float& mean) {
+// exp(d), d = z - top, of N logits whose row's maximum in the tile is top: t[] = exp(d) 2^r, their sum over the classes below the maximum,
+// the count of those at it, and the sum of t d log2 e. One fma takes z to the base-2 exponent, z log2 e - (top log2 e rounded): the
+// rounding r, the same for every class of the row, is undone by choice_stat. CLAMP: z may be -inf, or so large that the product overflows:
+// the difference first, and no r.
+template <int N, bool CLAMP>
+__device__ __forceinline__ void choice_sums(float (&z)[N], float top, float& below, int& at_top, float& mean) {
+    constexpr float L = 1.44269504f;
+    const float base = top * L;
 #pragma unroll
     for (int e = 0; e < N; ++e) {
-        const float x = z(e), d = x - top, t = soft_exp<T>(d);
-        const bool one = t == 1.f;
+        const float d = CLAMP ? fmaxf((z[e] - top) * L, -1e4f) : fmaf(z[e], L, -base);
+        const bool one = z[e] == top;
+        const float t = __builtin_amdgcn_exp2f(d);
         below += one ? 0.f : t;
-        at_top += one ? 1.f : 0.f;
-        mean += t == 0.f ? 0.f : t * d;  // (d may be -inf)
+        at_top += one;
+        mean = fmaf(t, d, mean);
+        z[e] = t;
     }
+}
+// The row's statistics from those sums. log2 e is L + 1.92596299e-8: what a float leaves out of it is put back to first order, by the mean.
+template <bool CLAMP>
+__device__ __forceinline__ ChoiceStat choice_stat(float top, float below, float at_top, float mean, float& undo) {
+    constexpr float L = 1.44269504f, LN2 = 0.693147181f, REST = 9.25328596e-9f;  // ln 2 * 1.92596299e-8 / L
+    const float r = CLAMP ? 0.f : fmaf(top, L, -(top * L));
+    undo = __builtin_amdgcn_exp2f(-r);
+    mean = mean - at_top * (__builtin_amdgcn_exp2f(r) * r);  // (the maximum's own terms: to the bit, so that a class alone leaves 0)
+    mean = (mean - r * below) * undo;
+    return ChoiceStat{top, fmaf(below, undo, at_top - 1.f) + REST * mean, mean * LN2, 0.f};
 }
 
 // Log probability epilogues on 8 consecutive columns, as soft_epilogue8.
@@ -419,15 +434,28 @@ __device__ __forceinline__ void choice_epilogue8(const GemmArgs& g, int64_t m, i
     for (int e = 1; e < 8; ++e) mx = fmaxf(mx, v[e]);
 #pragma unroll
     for (int o = 1; o < LANES; o <<= 1) mx = fmaxf(mx, __shfl_xor(mx, o));
-    float below = 0.f, at_top = 0.f, mean = 0.f;
-    choice_sums<bf16_t, 8>([&](int i) { return v[i]; }, mx == NEG ? 0.f : mx, below, at_top, mean);
+    float below = 0.f, mean = 0.f;
+    int count = 0;
+    float z[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) z[e] = v[e];
+    choice_sums<8, true>(z, mx == NEG ? 0.f : mx, below, count, mean);
+    float at_top = (float)count;
 #pragma unroll
     for (int o = 1; o < LANES; o <<= 1) {
         below += __shfl_xor(below, o);
         at_top += __shfl_xor(at_top, o);
         mean += __shfl_xor(mean, o);
     }
-    if (in && n == tile * (8 * LANES)) g.stat[m * g.tiles + tile] = ChoiceStat{mx, below + (at_top - 1.f), mean, 0.f};
+    if (!in) return;
+    float undo = 1.f;
+    const ChoiceStat r = mx == NEG ? ChoiceStat{NEG, -1.f, 0.f, 0.f} : choice_stat<true>(mx, below, at_top, mean, undo);
+    if (n == tile * (8 * LANES)) g.stat[m * g.tiles + tile] = r;
+    if (!g.c) return;
+    bool ovf = false;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) z[e] *= undo * SOFT_E_SCALE;
+    *(u32x4_t*)((_Float16*)g.c + m * g.ldc + n) = pack_f16x8(z, ovf);
 }
 
 // Block tile BM x BN over WM x WN waves; each wave owns a (BM/WM) x (BN/WN) block of
@@ -870,22 +898,46 @@ __device__ __forceinline__ void soft_block_epilogue(const GemmArgs& g, int64_t m
     }
 }
 
+// Stores 16-bit values v (TN tiles of a row, as the accumulators hold them) of 32 rows from `first` on through a stretch of LDS of
+// the wave's own, so that a store covers whole rows of 128 bytes (see soft_block_epilogue), past the caches.
+template <int TN, typename Pair>
+__device__ __forceinline__ void store_rows16(const GemmArgs& g, int64_t first, int64_t nw, int64_t pad, const float* v, Pair pair,
+                                             uint32_t* rows, int lane) {
+    constexpr int PITCH = 36;
+    const int half = lane >> 5;
+#pragma unroll
+    for (int j = 0; j < TN; ++j) {
+        const float* const a = v + 16 * j;
+#pragma unroll
+        for (int q = 0; q < 4; q += 2) {
+            const auto s0 = __builtin_amdgcn_permlane32_swap(pair(a[4 * q], a[4 * q + 1]), pair(a[4 * q + 4], a[4 * q + 5]), false, false);
+            const auto s1 = __builtin_amdgcn_permlane32_swap(pair(a[4 * q + 2], a[4 * q + 3]), pair(a[4 * q + 6], a[4 * q + 7]), false, false);
+            *(u32x4_t*)(rows + lane % 32 * PITCH + j * 16 + 4 * q + 4 * half) = u32x4_t{s0[0], s1[0], s0[1], s1[1]};
+        }
+    }
+    __builtin_amdgcn_wave_barrier();  // one wave's LDS accesses are in order
+#pragma unroll
+    for (int r = 0; r < 32; r += 8) {
+        const int64_t m = first + r + lane / 8;
+        const int c = lane % 8 * 8;
+        const u32x4_t w = *(const u32x4_t*)(rows + (r + lane / 8) * PITCH + c / 2);
+        if (m < g.M && c < pad) __builtin_nontemporal_store(w, (u32x4_t*)((uint16_t*)g.c + m * g.ldc + nw + c));
+    }
+    __builtin_amdgcn_wave_barrier();
+}
+
 // Log probability epilogue of a BM x BN block, from the accumulators, laid out as for the softmax loss: a lane's values of a row
-// are also the classes of a group (or, of 32 x 32 tiles, of one group per tile).
-template <typename T, bool GRAD, int BM, int BN, int WM, int WN, bool M32, typename Acc, int TM, int TN>
-__device__ __forceinline__ void choice_block_epilogue(const GemmArgs& g, int64_t m0, int64_t n0, Acc (&acc)[TM][TN], int tid,
-                                                      const int64_t (&labels)[TM]) {
+// are also the classes of a group (or, of 32 x 32 tiles, of one group per tile). EDGE: columns past N, or offsets.
+template <typename T, bool GRAD, bool EDGE, int BM, int BN, int WM, int WN, bool M32, typename Acc, int TM, int TN>
+__device__ __forceinline__ void choice_rows(const GemmArgs& g, int64_t mw, int64_t nw, Acc (&acc)[TM][TN], int tid,
+                                            const int64_t (&labels)[TM], uint32_t* stage) {
     constexpr int MT = M32 ? 32 : 16, Q = M32 ? 4 : 1, HALVES = 64 / MT, COLS = BN / WN;
     constexpr float NEG = -__builtin_huge_valf();
     const int lane = tid & 63, wave = tid >> 6, half = lane / MT;
-    const int64_t nw = n0 + (wave % WN) * COLS;  // the wave's first column
-    const int64_t mw = m0 + (wave / WN) * (BM / WM) + lane % MT;
-    if (nw >= g.N) return;
     auto col = [&](int j, int q) __attribute__((always_inline)) { return j * MT + 8 * q + 4 * half; };
     constexpr int V = TN * Q * 4;
-    const bool edge = g.offset || nw + COLS > g.N;
-    float off[V];
-    if (edge) {
+    float off[EDGE ? V : 1];
+    if constexpr (EDGE) {
 #pragma unroll
         for (int j = 0; j < TN; ++j)
 #pragma unroll
@@ -898,6 +950,28 @@ __device__ __forceinline__ void choice_block_epilogue(const GemmArgs& g, int64_t
     }
     constexpr int VEC = st<T>::vec;
     const int64_t pad = (g.N + VEC - 1) / VEC * VEC - nw;  // columns that are stored
+    // v as whole rows of the output, in the storage type (GRAD) or as exponentials times `unit`
+    auto store = [&](const float* v, int64_t m, bool in, float unit) __attribute__((always_inline)) {
+        auto pair = [&](float x, float y) __attribute__((always_inline)) {
+            if constexpr (GRAD) return pack_bf16x2(x, y);
+            const half2_t p = {(_Float16)(x * unit), (_Float16)(y * unit)};
+            return __builtin_bit_cast(uint32_t, p);
+        };
+        if constexpr (sizeof(T) == 4) {
+#pragma unroll
+            for (int j = 0; j < TN; ++j)
+                if (in && col(j, 0) < pad)
+                    *(f32x4_t*)((float*)g.c + m * g.ldc + nw + col(j, 0)) = f32x4_t{v[4 * j] * unit, v[4 * j + 1] * unit, v[4 * j + 2] * unit, v[4 * j + 3] * unit};
+        } else if constexpr (M32) {
+            static_assert(COLS == 64, "rows of 128 bytes");
+            store_rows16<TN>(g, m - lane % 32, nw, pad, v, pair, stage + wave * (32 * 36), lane);
+        } else {
+#pragma unroll
+            for (int j = 0; j < TN; ++j)
+                if (in && col(j, 0) < pad)
+                    *(uint2*)((uint16_t*)g.c + m * g.ldc + nw + col(j, 0)) = make_uint2(pair(v[4 * j], v[4 * j + 1]), pair(v[4 * j + 2], v[4 * j + 3]));
+        }
+    };
 #pragma unroll
     for (int i = 0; i < TM; ++i) {
         __builtin_amdgcn_sched_barrier(0);  // one row's values live beside the accumulators
@@ -910,7 +984,7 @@ __device__ __forceinline__ void choice_block_epilogue(const GemmArgs& g, int64_t
         for (int j = 0; j < TN; ++j)
 #pragma unroll
             for (int e = 0; e < 4 * Q; ++e) v[4 * Q * j + e] = acc[i][j][e] * g.scale;
-        if (edge) {
+        if constexpr (EDGE) {
 #pragma unroll
             for (int e = 0; e < V; ++e) v[e] = off[e] == NEG ? NEG : v[e] + off[e];
         }
@@ -928,8 +1002,8 @@ __device__ __forceinline__ void choice_block_epilogue(const GemmArgs& g, int64_t
                         a[e] = none || a[e] == NEG ? 0.f : soft_exp<T>(d) * fmaf(r.b, d, r.a);
                         if (lab == col(j, q) + e) a[e] = r.label;
                     }
-                    if (in && col(j, q) < pad) store4<T>((T*)g.c + m * g.ldc + nw + col(j, q), a);
                 }
+            store(v, m, in, 1.f);
         } else {
             if (lab >= 0) {
                 float z = 0.f;
@@ -942,33 +1016,48 @@ __device__ __forceinline__ void choice_block_epilogue(const GemmArgs& g, int64_t
                             if (lab == col(j, q) + e) z = v[4 * (j * Q + q) + e];
                 g.zlabel[m] = z;
             }
-            if (g.groups && in) {
-                if constexpr (M32) {
+            float mx = NEG;
+            if (g.groups) {
+                constexpr int PER = M32 ? 16 : V;
 #pragma unroll
-                    for (int j = 0; j < TN; ++j)
-                        if (nw + 32 * j < g.N)
-                            g.groups[m * g.ngroups + (nw / 32 + j) * 2 + half] =
-                                choice_group<16>([&](int k) { return v[16 * j + k]; });
-                } else {
-                    g.groups[m * g.ngroups + nw / COLS * 4 + half] = choice_group<V>([&](int k) { return v[k]; });
+                for (int j = 0; j < V / PER; ++j) {
+                    const uint2 u = choice_group<PER>([&](int k) { return v[PER * j + k]; });
+                    const int64_t at = M32 ? (nw / 32 + j) * 2 + half : nw / COLS * 4 + half;
+                    if (in && (!EDGE || !M32 || nw + 32 * j < g.N)) g.groups[m * g.ngroups + at] = u;
+                    mx = fmaxf(mx, __uint_as_float(u.x));
                 }
-            }
-            float mx = v[0];
+            } else {
 #pragma unroll
-            for (int e = 1; e < V; ++e) mx = fmaxf(mx, v[e]);
+                for (int e = 0; e < V; ++e) mx = fmaxf(mx, v[e]);
+            }
 #pragma unroll
             for (int o = MT; o < 64; o <<= 1) mx = fmaxf(mx, __shfl_xor(mx, o));
-            float below = 0.f, at_top = 0.f, mean = 0.f;
-            choice_sums<T, V>([&](int k) { return v[k]; }, mx == NEG ? 0.f : mx, below, at_top, mean);
+            float below = 0.f, mean = 0.f;
+            int count = 0;
+            choice_sums<V, EDGE || sizeof(T) == 4>(v, mx == NEG ? 0.f : mx, below, count, mean);
+            float at_top = (float)count;
 #pragma unroll
             for (int o = MT; o < 64; o <<= 1) {
                 below += __shfl_xor(below, o);
                 at_top += __shfl_xor(at_top, o);
                 mean += __shfl_xor(mean, o);
             }
-            if (in && half == 0) g.stat[m * g.tiles + nw / COLS] = ChoiceStat{mx, below + (at_top - 1.f), mean, 0.f};
+            float undo = 1.f;
+            const ChoiceStat r = mx == NEG ? ChoiceStat{NEG, -1.f, 0.f, 0.f} : choice_stat<EDGE || sizeof(T) == 4>(mx, below, at_top, mean, undo);
+            if (in && half == 0) g.stat[m * g.tiles + nw / COLS] = r;
+            if (g.c) store(v, m, in, sizeof(T) == 4 ? undo : undo * SOFT_E_SCALE);
         }
     }
+}
+template <typename T, bool GRAD, int BM, int BN, int WM, int WN, bool M32, typename Acc, int TM, int TN>
+__device__ __forceinline__ void choice_block_epilogue(const GemmArgs& g, int64_t m0, int64_t n0, Acc (&acc)[TM][TN], int tid,
+                                                      const int64_t (&labels)[TM], uint32_t* stage) {
+    const int lane = tid & 63, wave = tid >> 6;
+    const int64_t nw = n0 + (wave % WN) * (BN / WN);  // the wave's first column
+    const int64_t mw = m0 + (wave / WN) * (BM / WM) + lane % (M32 ? 32 : 16);
+    if (nw >= g.N) return;
+    if (g.offset || nw + BN / WN > g.N) choice_rows<T, GRAD, true, BM, BN, WM, WN, M32>(g, mw, nw, acc, tid, labels, stage);
+    else choice_rows<T, GRAD, false, BM, BN, WM, WN, M32>(g, mw, nw, acc, tid, labels, stage);
 }
 
 // C = A B^T with an ST-stage direct-to-LDS pipeline of KB-deep stages (see layouts above): one workgroup's block, tile
@@ -1051,7 +1140,11 @@ __device__ __forceinline__ void gemm_block(const GemmArgs& g, int block, int z, 
         static_assert(!M32 || WM * WN * 32 * 36 * 4 <= ST * P::STAGE_ELEMS * 2, "the waves' staged rows fit the ring");
         if (M32 && g.c) __syncthreads();  // every wave is done with the ring
         soft_block_epilogue<bf16_t, EK == EK_SOFT_GRAD, BM, BN, WM, WN, M32>(g, c.m0, c.n0, acc, tid, labels, (uint32_t*)smem);
-    } else if constexpr (CHOICE) choice_block_epilogue<bf16_t, EK == EK_CHOICE_GRAD, BM, BN, WM, WN, M32>(g, c.m0, c.n0, acc, tid, labels);
+    } else if constexpr (CHOICE) {
+        static_assert(!M32 || WM * WN * 32 * 36 * 4 <= ST * P::STAGE_ELEMS * 2, "the waves' staged rows fit the ring");
+        if (M32 && g.c) __syncthreads();  // every wave is done with the ring
+        choice_block_epilogue<bf16_t, EK == EK_CHOICE_GRAD, BM, BN, WM, WN, M32>(g, c.m0, c.n0, acc, tid, labels, (uint32_t*)smem);
+    }
     else block_epilogue<BM, BN, WM, WN, M32, T, EK, P::THREADS, ST * P::STAGE_ELEMS>(g, c.m0, c.n0, z, acc, smem, tid);
 }
 
@@ -1361,7 +1454,7 @@ __device__ __forceinline__ void f32_lds_block(const GemmArgs& g, int block, int 
         return;
     }
     if constexpr (CHOICE) {
-        choice_block_epilogue<float, EK == EK_CHOICE_GRAD, BM, BN, 2, 2, false>(g, m0, n0, acc, tid, labels);
+        choice_block_epilogue<float, EK == EK_CHOICE_GRAD, BM, BN, 2, 2, false>(g, m0, n0, acc, tid, labels, nullptr);
         return;
     }
     __syncthreads();

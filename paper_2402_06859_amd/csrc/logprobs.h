@@ -50,4 +50,17 @@ struct ChoicePrepare {
 };
 hipError_t launch_choice_prepare(const ChoicePrepare& a, bool bf16, hipStream_t s);
 
+// out [rows][ld], `width` columns (whole vectors) of classes from `first` on: the gradient in the logits, from kept [rows][kept_ld]
+// (f16 times SOFT_E_SCALE, or float) and the tiles' maxima.
+struct ChoiceNormalize {
+    int64_t rows, tiles, tile, first, width, ld, kept_ld;
+    const ChoiceStat* stat;
+    const ChoiceRow* row;
+    const void* labels;
+    bool ids64;
+    const void* kept;
+    void* out;
+};
+hipError_t launch_choice_normalize(const ChoiceNormalize& a, bool bf16, hipStream_t s);
+
 }  // namespace rdcn

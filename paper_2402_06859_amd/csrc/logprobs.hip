@@ -26,6 +26,7 @@ namespace {
 constexpr int ERR_BIT_INDEX = 1;
 constexpr float NEG_INF = -__builtin_huge_valf();
 constexpr int SLACK = 4, GROUPS_MAX = CHOICE_TOP_MAX + SLACK, CANDIDATES_MAX = GROUPS_MAX * 16;
+constexpr int LISTED = 512;  // groups among which the largest are ranked
 
 __device__ __forceinline__ int64_t id_of(const void* ids, bool i64, int64_t m) {
     return i64 ? ((const int64_t*)ids)[m] : (int64_t)((const int32_t*)ids)[m];
@@ -45,23 +46,132 @@ __device__ __forceinline__ ChoiceStat shuffled(const ChoiceStat& p, int o) {
 }
 
 // (value, id) a ahead of b in the order of the answer: larger first, then the lower id.
-__device__ __forceinline__ bool ahead(float a, int64_t ia, float b, int64_t ib) { return a > b || (a == b && ia < ib); }
+__device__ __forceinline__ bool ahead(float a, int ia, float b, int ib) { return a > b || (a == b && ia < ib); }
 
 __device__ __forceinline__ float key_of(uint2 g) {  // a group's largest logit; NaN counts as not visible
     const float v = __uint_as_float(g.x);
     return v == v ? v : NEG_INF;
 }
 
+// The groups of the `want` largest maxima, ordered, into chosen; returns how many there are (fewer where fewer hold a visible
+// class). Every four threads' largest is ranked among the 64 of them; the want-th of those is no larger than the want-th of all
+// groups, so all that reach it are listed, a few more than wanted, and ranked in turn.
+struct Chosen {
+    int group[GROUPS_MAX];
+    float key[GROUPS_MAX];
+    uint32_t bound[GROUPS_MAX];
+    float keys[64];
+    int list[LISTED];
+    float list_key[LISTED];
+    uint32_t list_bound[LISTED];
+    float wave_key[4];
+    int count, wave_group[4];
+};
+__device__ __forceinline__ float lane_value(float x, int lane) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), lane)); }
+
+__device__ __forceinline__ int choose_groups(const uint2* groups, int n, int want, Chosen& c) {
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    constexpr int AHEAD = 8;  // loads in flight
+    float mine = NEG_INF;
+    for (int u0 = tid; u0 < n; u0 += 256 * AHEAD) {
+        uint2 g[AHEAD];
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) g[i] = groups[u0 + 256 * i < n ? u0 + 256 * i : u0];
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) mine = fmaxf(mine, key_of(g[i]));
+    }
+    float four = fmaxf(mine, __shfl_xor(mine, 1));
+    four = fmaxf(four, __shfl_xor(four, 2));
+    if (lane % 4 == 0) c.keys[tid / 4] = four;
+    if (tid == 0) c.count = 0;
+    __syncthreads();
+    const float k64 = c.keys[lane];
+    int rank = 0;
+#pragma unroll
+    for (int j = 0; j < 64; ++j) {
+        const float k = lane_value(k64, j);
+        rank += k > k64 || (k == k64 && j < lane);
+    }
+    const float bar = lane_value(k64, __builtin_ctzll(__ballot(rank == want - 1)));  // (of every wave alike)
+    if (mine >= bar && mine != NEG_INF) {
+        for (int u0 = tid; u0 < n; u0 += 256 * AHEAD) {
+            uint2 g[AHEAD];
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i) g[i] = groups[u0 + 256 * i < n ? u0 + 256 * i : u0];
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i) {
+                const float k = key_of(g[i]);
+                if (u0 + 256 * i >= n || k < bar || k == NEG_INF) continue;
+                const int at = atomicAdd(&c.count, 1);
+                if (at < LISTED) c.list[at] = u0 + 256 * i, c.list_key[at] = k, c.list_bound[at] = g[i].y;
+            }
+        }
+    }
+    __syncthreads();
+    const int listed = c.count;
+    if (listed <= LISTED) {  // (the list's order is by chance, its ranks are not)
+        if (listed <= 64) {
+            if (wave == 0) {
+                const float k = lane < listed ? c.list_key[lane] : NEG_INF;
+                const int u = lane < listed ? c.list[lane] : 0x7FFFFFFF;
+                int r = 0;
+                for (int j = 0; j < listed; ++j) r += ahead(lane_value(k, j), __builtin_amdgcn_readlane(u, j), k, u);
+                if (lane < listed && r < want) c.group[r] = u, c.key[r] = k, c.bound[r] = c.list_bound[lane];
+            }
+        } else {
+            for (int i = tid; i < listed; i += 256) {
+                const float k = c.list_key[i];
+                const int u = c.list[i];
+                int r = 0;
+                for (int j = 0; j < listed; ++j) r += ahead(c.list_key[j], c.list[j], k, u);
+                if (r < want) c.group[r] = u, c.key[r] = k, c.bound[r] = c.list_bound[i];
+            }
+        }
+        __syncthreads();
+        return listed < want ? listed : want;
+    }
+    // many equal ones at the bar: one group at a time, each thread holding the best of its own behind the last one taken
+    float last = __builtin_huge_valf(), best = NEG_INF;
+    int last_at = -1, best_at = n;
+    auto rescan = [&]() {
+        best = NEG_INF;
+        best_at = n;
+        for (int u = tid; u < n; u += 256) {
+            const float k = key_of(groups[u]);
+            if (ahead(last, last_at, k, u) && ahead(k, u, best, best_at)) best = k, best_at = u;
+        }
+    };
+    rescan();
+    for (int i = 0; i < want; ++i) {
+        float k = best;
+        int at = best_at;
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) {
+            const float ok = __shfl_xor(k, o);
+            const int oat = __shfl_xor(at, o);
+            if (ahead(ok, oat, k, at)) k = ok, at = oat;
+        }
+        if (lane == 0) c.wave_key[wave] = k, c.wave_group[wave] = at;
+        __syncthreads();
+        k = c.wave_key[0], at = c.wave_group[0];
+#pragma unroll
+        for (int v = 1; v < 4; ++v)
+            if (ahead(c.wave_key[v], c.wave_group[v], k, at)) k = c.wave_key[v], at = c.wave_group[v];
+        if (tid == 0) c.group[i] = at, c.key[i] = k, c.bound[i] = groups[at].y;
+        last = k, last_at = at;
+        if (at == best_at) rescan();
+        __syncthreads();
+    }
+    return want;
+}
+
 // One workgroup per row.
 template <typename T>
 __global__ __launch_bounds__(256) void k_choice_rows(ChoiceRows a) {
     __shared__ ChoiceStat wave_stat[4];
-    __shared__ float wave_key[4];
-    __shared__ int64_t wave_group[4];
-    __shared__ int64_t chosen[GROUPS_MAX];
-    __shared__ float chosen_key[GROUPS_MAX];
+    __shared__ Chosen chosen;
     __shared__ int count;
-    __shared__ int64_t cand[CANDIDATES_MAX];
+    __shared__ int cand[CANDIDATES_MAX];
     __shared__ double cand_z[CANDIDATES_MAX];
     __shared__ double best;
     const int64_t m = blockIdx.x + (int64_t)blockIdx.y * gridDim.x;
@@ -69,10 +179,18 @@ __global__ __launch_bounds__(256) void k_choice_rows(ChoiceRows a) {
     if (m >= a.rows) return;
 
     ChoiceStat r{NEG_INF, -1.f, 0.f, 0.f};
-    for (int64_t t = tid; t < a.tiles; t += 256) r = join(r, a.stat[m * a.tiles + t]);
+    for (int64_t t0 = tid; t0 < a.tiles; t0 += 1024) {
+        ChoiceStat q[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) q[i] = a.stat[m * a.tiles + (t0 + 256 * i < a.tiles ? t0 + 256 * i : t0)];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (t0 + 256 * i < a.tiles) r = join(r, q[i]);
+    }
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) r = join(r, shuffled(r, o));
     if (lane == 0) wave_stat[wave] = r;
+    if (tid == 0) count = 0;
     __syncthreads();
     r = join(join(wave_stat[0], wave_stat[1]), join(wave_stat[2], wave_stat[3]));
     const bool none = r.max == NEG_INF && r.rest == -1.f;  // every class is masked
@@ -95,89 +213,69 @@ __global__ __launch_bounds__(256) void k_choice_rows(ChoiceRows a) {
     }
     if (a.top == 0) return;
 
-    // the top + SLACK groups of the largest maxima, one at a time: each thread holds the best of its own that is
-    // behind the last one taken
     const uint2* const groups = a.groups + m * a.g.count;
     const int want = (int)(a.g.count < a.top + SLACK ? a.g.count : a.top + SLACK);
-    float last = __builtin_huge_valf(), mine = NEG_INF;
-    int64_t last_at = -1, mine_at = a.g.count;
-    auto rescan = [&]() {
-        mine = NEG_INF;
-        mine_at = a.g.count;
-        for (int64_t u = tid; u < a.g.count; u += 256) {
-            const float k = key_of(groups[u]);
-            if (ahead(last, last_at, k, u) && ahead(k, u, mine, mine_at)) mine = k, mine_at = u;
-        }
-    };
-    rescan();
-    for (int i = 0; i < want; ++i) {
-        float k = mine;
-        int64_t at = mine_at;
-#pragma unroll
-        for (int o = 32; o > 0; o >>= 1) {
-            const float ok = __shfl_xor(k, o);
-            const int64_t oat = __shfl_xor(at, o);
-            if (ahead(ok, oat, k, at)) k = ok, at = oat;
-        }
-        if (lane == 0) wave_key[wave] = k, wave_group[wave] = at;
-        __syncthreads();
-        k = wave_key[0], at = wave_group[0];
-#pragma unroll
-        for (int v = 1; v < 4; ++v)
-            if (ahead(wave_key[v], wave_group[v], k, at)) k = wave_key[v], at = wave_group[v];
-        if (tid == 0) chosen[i] = at, chosen_key[i] = k;
-        last = k, last_at = at;
-        if (at == mine_at) rescan();
-        __syncthreads();
-    }
-
-    // their candidates: the largest class, and all where another may be as large as the last group's
-    if (tid == 0) count = 0;
-    __syncthreads();
-    const float least = want < a.g.count ? chosen_key[want - 1] : NEG_INF;
-    if (tid < want) {
-        const int64_t u = chosen[tid];
-        const uint2 g = groups[u];
-        const int per = a.g.pitch / 4;
-        const int64_t base = u / per * a.g.span + u % per * 4;
-        auto cls = [&](int k) { return base + (int64_t)(k / 4) * a.g.pitch + k % 4; };
-        const bool all = !(__uint_as_float(g.y & ~15u) < least);
-        for (int k = 0; k < a.g.size; ++k)
-            if ((all || k == (int)(g.y & 15u)) && cls(k) < a.classes) cand[atomicAdd(&count, 1)] = cls(k);
+    const int got = choose_groups(groups, (int)a.g.count, want, chosen);
+    // the candidates: each group's largest class, and all of its classes where another may be as large as the last group's
+    const float least = got == want && want < a.g.count ? chosen.key[want - 1] : NEG_INF;
+    for (int i = tid; i < got * a.g.size; i += 256) {
+        const int u = chosen.group[i / a.g.size], k = i % a.g.size, per = a.g.pitch / 4;
+        const uint32_t bound = chosen.bound[i / a.g.size];
+        const int64_t v = (int64_t)(u / per) * a.g.span + u % per * 4 + k / 4 * a.g.pitch + k % 4;
+        const bool all = !(__uint_as_float(bound & ~15u) < least);
+        if ((all || k == (int)(bound & 15u)) && v < a.classes) cand[atomicAdd(&count, 1)] = (int)v;
     }
     __syncthreads();
     const int n = count;
-    for (int c = wave; c < n; c += 4) {
-        const int64_t v = cand[c];
-        const T* const x = (const T*)a.x + m * a.dim;
-        const T* const w = (const T*)a.w + v * a.dim;
-        double z = 0.0;
-        constexpr int W = st<T>::vec;
+    // their logits, four at a time in a wave
+    constexpr int W = st<T>::vec, AT_ONCE = 4;
+    const T* const x = (const T*)a.x + m * a.dim;
+    for (int c0 = wave * AT_ONCE; c0 < n; c0 += 4 * AT_ONCE) {
+        const T* w[AT_ONCE];
+        double z[AT_ONCE];
+#pragma unroll
+        for (int i = 0; i < AT_ONCE; ++i) {
+            w[i] = (const T*)a.w + cand[c0 + i < n ? c0 + i : n - 1] * a.dim;
+            z[i] = 0.0;
+        }
+#pragma unroll 2
         for (int64_t k = lane * W; k < a.dim; k += 64 * W) {
             float p[W], q[W];
-            st<T>::unpack(*(const u32x4_t*)(x + k), p);
-            st<T>::unpack(*(const u32x4_t*)(w + k), q);
+            u32x4_t raw[AT_ONCE];
 #pragma unroll
-            for (int e = 0; e < W; ++e) z = fma((double)p[e], (double)q[e], z);
+            for (int i = 0; i < AT_ONCE; ++i) raw[i] = *(const u32x4_t*)(w[i] + k);
+            st<T>::unpack(*(const u32x4_t*)(x + k), p);
+#pragma unroll
+            for (int i = 0; i < AT_ONCE; ++i) {
+                st<T>::unpack(raw[i], q);
+#pragma unroll
+                for (int e = 0; e < W; ++e) z[i] = fma((double)p[e], (double)q[e], z[i]);
+            }
         }
 #pragma unroll
-        for (int o = 32; o > 0; o >>= 1) z += __shfl_xor(z, o);
-        const float off = a.offset ? a.offset[v] : 0.f;
-        z = off == NEG_INF ? -__builtin_huge_val() : z * (double)a.logit_scale + (double)off;
-        if (lane == 0) cand_z[c] = z == z ? z : -__builtin_huge_val();
+        for (int o = 32; o > 0; o >>= 1)
+#pragma unroll
+            for (int i = 0; i < AT_ONCE; ++i) z[i] += __shfl_xor(z[i], o);
+        if (lane < AT_ONCE && c0 + lane < n) {
+            double mine = z[0];
+#pragma unroll
+            for (int i = 1; i < AT_ONCE; ++i) mine = lane == i ? z[i] : mine;
+            const float off = a.offset ? a.offset[cand[c0 + lane]] : 0.f;
+            mine = off == NEG_INF ? -__builtin_huge_val() : mine * (double)a.logit_scale + (double)off;
+            cand_z[c0 + lane] = mine == mine ? mine : -__builtin_huge_val();
+        }
     }
     __syncthreads();
-    // ranks
-    auto rank = [&](int c) {
-        int k = 0;
-        for (int i = 0; i < n; ++i) k += cand_z[i] > cand_z[c] || (cand_z[i] == cand_z[c] && cand[i] < cand[c]);
-        return k;
-    };
-    int ranks[(CANDIDATES_MAX + 255) / 256];
+    constexpr int MOST = (CANDIDATES_MAX + 255) / 256;
+    int ranks[MOST];
 #pragma unroll
-    for (int i = 0; i < (CANDIDATES_MAX + 255) / 256; ++i) {
+    for (int i = 0; i < MOST; ++i) {
         const int c = tid + 256 * i;
-        ranks[i] = c < n ? rank(c) : a.top;
+        ranks[i] = a.top;
+        if (c >= n) continue;
+        ranks[i] = 0;
+#pragma unroll 4
+        for (int j = 0; j < n; ++j) ranks[i] += cand_z[j] > cand_z[c] || (cand_z[j] == cand_z[c] && cand[j] < cand[c]);
         if (ranks[i] == 0) best = cand_z[c];
     }
     __syncthreads();
@@ -187,13 +285,13 @@ __global__ __launch_bounds__(256) void k_choice_rows(ChoiceRows a) {
         if (a.top_logprob) a.top_logprob[m * a.top + k] = v;
     };
 #pragma unroll
-    for (int i = 0; i < (CANDIDATES_MAX + 255) / 256; ++i) {
+    for (int i = 0; i < MOST; ++i) {
         if (ranks[i] >= a.top) continue;
         const int c = tid + 256 * i;
         const bool seen = cand_z[c] != -__builtin_huge_val();
         put(ranks[i], seen ? cand[c] : -1, seen ? (float)(cand_z[c] - best) - log_all : NEG_INF);
     }
-    for (int k = n + tid; k < a.top; k += 256) put(k, -1, NEG_INF);  // fewer classes than wanted
+    for (int k = n + tid; k < a.top; k += 256) put(k, -1, NEG_INF);  // fewer visible classes than wanted
 }
 
 // Whether row m has a gradient at all. Rows without one (no label, or both upstream gradients 0) may hold anything in x: 0 times
@@ -237,7 +335,48 @@ __global__ __launch_bounds__(256) void k_choice_prepare(ChoicePrepare a) {
     }
 }
 
+// Columns first .. of row m of the gradient in the logits, from the exponentials that the forward kept: p = e exp(tile's
+// maximum - row's) / (1 + rest), and d from e's logarithm. Reads and writes each element once (2 + 2 bytes, 4 + 4 in float).
+template <typename T>
+__global__ __launch_bounds__(256) void k_choice_normalize(ChoiceNormalize a) {
+    constexpr int W = st<T>::vec;
+    constexpr float UNIT = sizeof(T) == 2 ? 1.f / SOFT_E_SCALE : 1.f, LN2 = 0.693147181f;
+    const int64_t m = blockIdx.y + (int64_t)blockIdx.z * 65535;
+    if (m >= a.rows) return;
+    const ChoiceRow r = a.row[m];
+    const bool none = r.a == 0.f && r.b == 0.f;
+    const int64_t y = a.labels ? id_of(a.labels, a.ids64, m) : -1;
+    for (int64_t n = (blockIdx.x * 256ll + threadIdx.x) * W; n < a.width; n += gridDim.x * 256ll * W) {
+        const int64_t v = a.first + n;  // the class
+        const float top = a.stat[m * a.tiles + v / a.tile].max;
+        float e[W];
+        if constexpr (sizeof(T) == 2) unpack_f16x8(*(const u32x4_t*)((const _Float16*)a.kept + m * a.kept_ld + v), e);
+        else st<T>::unpack(*(const u32x4_t*)((const float*)a.kept + m * a.kept_ld + v), e);
+        const float gap = top - r.max, f = none || top == NEG_INF ? 0.f : UNIT * expf(gap);
+#pragma unroll
+        for (int i = 0; i < W; ++i) {
+            const float d = fmaf(__builtin_amdgcn_logf(e[i] * UNIT), LN2, gap);
+            e[i] = f == 0.f || e[i] == 0.f ? 0.f : e[i] * f * fmaf(r.b, d, r.a);
+        }
+        if (y >= v && y < v + W) {
+#pragma unroll
+            for (int i = 0; i < W; ++i)
+                if (y - v == i) e[i] = r.label;
+        }
+        *(u32x4_t*)((T*)a.out + m * a.ld + n) = st<T>::pack(e);
+    }
+}
+
 }  // namespace
+
+hipError_t launch_choice_normalize(const ChoiceNormalize& a, bool bf16, hipStream_t s) {
+    if (a.rows == 0 || a.width == 0) return hipSuccess;
+    const int64_t per = (a.width / (bf16 ? 8 : 4) + 1023) / 1024, y = a.rows < 65535 ? a.rows : 65535;  // four vectors a thread
+    const dim3 grid((unsigned)(per > 64 ? 64 : per), (unsigned)y, (unsigned)((a.rows + 65534) / 65535));
+    if (bf16) hipLaunchKernelGGL(k_choice_normalize<bf16_t>, grid, dim3(256), 0, s, a);
+    else hipLaunchKernelGGL(k_choice_normalize<float>, grid, dim3(256), 0, s, a);
+    return hipGetLastError();
+}
 
 hipError_t launch_choice_rows(const ChoiceRows& a, bool bf16, hipStream_t s) {
     if (a.rows == 0) return hipSuccess;

@@ -15,7 +15,8 @@ sum of exp(d) over all classes but that one, and tau = sum p d:
   tau     terms exp(d) |d| (e + 2 u) + exp(d) 2 dz, divided by 1 + rest, and tau times log1p's error.
   lse     dz, log1p's error and 2 u of itself.
   gradient  an element p (-g - h (d - tau)): relative e for p, h times the errors of d (2 dz + u |d|) and tau, half a step of bf16
-          (2^-8) for bf16 models, then the products' chains as in the softmax loss's test, and one rounding at the end.
+          (2^-8) for bf16 models, of f16 (2^-11) for p and, by its logarithm, for d where the exponentials are kept, and 2^-40 of
+          the row's largest for those that f16 cannot hold, then the products' chains as in the softmax loss's test, and one rounding at the end.
 All terms beside these are of second order; every bound is taken 1 + 2^-4 times.
 """
 import ctypes
@@ -137,6 +138,7 @@ def reference(c, rows, dim, classes, f32, top=0):
         else:
             chain_x, chain_w, r = (classes / 4 + 40) * U, (rows / 4 + 40) * U, 2.0 ** -8
             ep = (1 + ep) * (1 + 2.0 ** -11) * (1 + 2.0 ** -8) - 1
+            loose = loose + p * h.abs() * 2.0 ** -10
         least = torch.where(live[:, None], (g.abs() + h.abs() * 30) * p.amax(1, keepdim=True) * 2.0 ** -40, 0.0) if not f32 else 0.0
         spread = c["s"] * more
         of_live = lambda t: torch.where(live[:, None], spread * t, 0.0)  # (other rows may hold anything)
