@@ -717,8 +717,8 @@ rdcn_status rdcn_muon_workspace(const rdcn_handle* h, const rdcn_muon_tensor* te
 
 /*
  * One step over `count` matrices (<= 65536). The list is read before the call returns. Arrays must be 16-byte
- * aligned and must not overlap (overlapping weights are RDCN_ERR_ARG). Results depend on the arguments alone, not on
- * what else is in the list (but for the random bits, which go by the place in it).
+ * aligned and must not overlap (overlapping weights are RDCN_ERR_ARG). A list gives the same bits every time; which other
+ * matrices are in it may change the order of a matrix's sums, and its random bits go by its place in it.
  */
 rdcn_status rdcn_muon_step(rdcn_handle* h, const rdcn_muon_config* cfg, const rdcn_muon_tensor* tensors, int32_t count,
                            void* scratch, size_t scratch_bytes, void* stream);

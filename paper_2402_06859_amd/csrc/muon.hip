@@ -139,15 +139,10 @@ __device__ __forceinline__ float update_of(const MuonScalars& a, float m, float 
     return a.nesterov ? m * a.mu + g * a.c1 : m;
 }
 
-// M' and the partial sums of |U|^2, in 64 bits: the squares of floats cannot overflow there, or vanish.
-__global__ __launch_bounds__(256) void k_muon_momentum(Elements b) {
+// M' of elements from <= k < to (from a multiple of 8) by a workgroup, and its threads' shares of |U|^2, in 64 bits: the squares of
+// floats cannot overflow there, or vanish.
+__device__ __forceinline__ double momentum_range(const Matrix& t, const MuonScalars& a, float gs, bool taken, int64_t from, int64_t to) {
 #pragma clang fp contract(off)
-    float gs;
-    const bool taken = gradient_scale(b.a, gs);
-    const int i = entry_of(b.first, b.count, blockIdx.x);
-    const Matrix& t = b.t[i];
-    const int64_t n = t.rows * t.cols, from = (int64_t)(blockIdx.x - b.first[i]) * t.per;
-    const int64_t to = from + t.per < n ? from + t.per : n;
     double s[2] = {0.0, 0.0};
     for (int64_t k = from + threadIdx.x * 8; k < to; k += 2048) {
         const int left = to - k < 8 ? (int)(to - k) : 8;
@@ -157,8 +152,8 @@ __global__ __launch_bounds__(256) void k_muon_momentum(Elements b) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             const float x = g[e] * gs;
-            m[e] = m[e] * b.a.mu + x * b.a.c1;
-            const double u = (double)update_of(b.a, m[e], x);
+            m[e] = m[e] * a.mu + x * a.c1;
+            const double u = (double)update_of(a, m[e], x);
             s[e & 1] = fma(u, u, s[e & 1]);
         }
         if (!taken) continue;
@@ -171,13 +166,38 @@ __global__ __launch_bounds__(256) void k_muon_momentum(Elements b) {
                 if (e < left) t.m[k + e] = m[e];
         }
     }
-    const double sum = block_sum(s[0] + s[1]);
+    return s[0] + s[1];
+}
+
+// X's elements (r, c) .. (r, c + 7), 0 outside the matrix.
+__device__ __forceinline__ void x_elements(const Matrix& t, const MuonScalars& a, float gs, bool taken, double inv, int64_t r, int64_t c,
+                                           float (&v)[8]) {
+#pragma clang fp contract(off)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = 0.f;
+    if (!taken || r >= t.rows || c >= t.cols) return;
+    const int64_t k = r * t.cols + c;
+    const int left = t.cols - c < 8 ? (int)(t.cols - c) : 8;
+    const bool whole = left == 8 && (k & 7) == 0;
+    float g[8], m[8];
+    load_grad(t, k, left, whole, g);
+    load_f32(t.m, k, left, whole, m);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = e < left ? (float)((double)update_of(a, m[e], g[e] * gs) * inv) : 0.f;
+}
+
+__global__ __launch_bounds__(256) void k_muon_momentum(Elements b) {
+    float gs;
+    const bool taken = gradient_scale(b.a, gs);
+    const int i = entry_of(b.first, b.count, blockIdx.x);
+    const Matrix& t = b.t[i];
+    const int64_t n = t.rows * t.cols, from = (int64_t)(blockIdx.x - b.first[i]) * t.per;
+    const double sum = block_sum(momentum_range(t, b.a, gs, taken, from, from + t.per < n ? from + t.per : n));
     if (threadIdx.x == 0) t.part[blockIdx.x - b.first[i]] = sum;
 }
 
 // X = U / |U| as a pair of f16, padded with zeros; a workgroup per SPLIT_ROWS x SPLIT_COLS block, eight columns a thread.
 __global__ __launch_bounds__(256) void k_muon_split(Elements b) {
-#pragma clang fp contract(off)
     float gs;
     const bool taken = gradient_scale(b.a, gs);
     const int i = entry_of(b.first, b.count, blockIdx.x);
@@ -192,17 +212,8 @@ __global__ __launch_bounds__(256) void k_muon_split(Elements b) {
     if (c >= t.cp) return;
     const int64_t plane = (int64_t)t.rp * t.cp;
     for (int r = r0 + threadIdx.x / (SPLIT_COLS / 8); r < r0 + SPLIT_ROWS && r < t.rp; r += 256 / (SPLIT_COLS / 8)) {
-        float v[8] = {};
-        if (taken && r < t.rows && c < t.cols) {
-            const int64_t k = (int64_t)r * t.cols + c;
-            const int left = t.cols - c < 8 ? (int)(t.cols - c) : 8;
-            const bool whole = left == 8 && (k & 7) == 0;
-            float g[8], m[8];
-            load_grad(t, k, left, whole, g);
-            load_f32(t.m, k, left, whole, m);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = e < left ? (float)((double)update_of(b.a, m[e], g[e] * gs) * inv) : 0.f;
-        }
+        float v[8];
+        x_elements(t, b.a, gs, taken, inv, r, c, v);
         store_pair(t.x + (int64_t)r * t.cp + c, plane, v, 0, 8);
     }
 }
@@ -574,6 +585,231 @@ __global__ __launch_bounds__(64 * WM * WN * KW) void k_muon_product(Products b) 
     }
 }
 
+// The whole step of matrices whose shorter side is at most 64, a workgroup each: the 64 x 64 matrices stay in LDS, and X (in scratch, a
+// pair, the shorter side's index first) is passed through by 64 columns at a time. A launch for each product would cost
+// such a matrix 19 starts and ends of kernels of some 5 us.
+constexpr int SMALL = 64, SMALL_LENGTH = 1024;
+struct Small {
+    Matrix t[PER_LAUNCH];
+    MuonScalars a;
+    MuonScales q;
+};
+static_assert(sizeof(Small) <= 4096, "kernel arguments");
+
+// Whether X and A are made anew after step k.
+__host__ __device__ inline bool anew_after(int k, int steps) { return k < steps - 1 && (k == 1 || (k > 1 && (k - 1) % 3 == 0)); }
+
+__global__ __launch_bounds__(256) void k_muon_small(Small b) {
+    constexpr int E = SMALL * SMALL, CP = SMALL + 4;  // elements of a plane
+    __shared__ __attribute__((aligned(1024))) bf16_t squares[4][2 * E];  // A, T A, T, P
+    __shared__ __attribute__((aligned(1024))) bf16_t xk[2 * E];          // a block of X, K-contiguous along the longer side
+    __shared__ __attribute__((aligned(1024))) bf16_t xs[2 * E];          // the same, K-strided along the shorter
+    __shared__ __attribute__((aligned(16))) float cs[SMALL * CP];
+    const Matrix t = b.t[blockIdx.x];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, wm = wave >> 1, wn = wave & 1;
+    const bool tall = t.rows > t.cols;
+    const int64_t length = tall ? t.rp : t.cp;  // of the longer side, padded
+    float gs;
+    const bool taken = gradient_scale(b.a, gs);
+    const double sum = block_sum(momentum_range(t, b.a, gs, taken, 0, t.rows * t.cols));
+    const double inv = sum == 0.0 ? 0.0 : (double)b.q.x[0] / sqrt(sum);
+
+    using Acc = f32x16_t[3];
+    auto clear = [&](Acc& c) {
+#pragma unroll
+        for (int z = 0; z < 3; ++z)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) c[z][e] = 0.f;
+    };
+    // c += x y^T for pairs x (K-contiguous) and y, this wave's 32 x 32 of it
+    auto product = [&](const bf16_t* x, const bf16_t* y, auto strided, Acc& c) __attribute__((always_inline)) {
+        constexpr bool KS = decltype(strided)::value;
+        const uint32_t fx = frag_base<SMALL, false, SMALL>(x, wm * 32, lane), fy = frag_base<SMALL, KS, SMALL>(y, wn * 32, lane);
+#pragma unroll
+        for (int s = 0; s < 4; ++s) {
+            const bf16x8_t xh = frag_at<SMALL, false, SMALL>(fx, 0, 0, s), xl = frag_at<SMALL, false, SMALL>(fx, E * 2u, 0, s);
+            const bf16x8_t yh = frag_at<SMALL, KS, SMALL>(fy, 0, 0, s), yl = frag_at<SMALL, KS, SMALL>(fy, E * 2u, 0, s);
+            c[0] = mfma32x32x16<true>(yl, xh, c[0]);
+            c[1] = mfma32x32x16<true>(yh, xl, c[1]);
+            c[2] = mfma32x32x16<true>(yh, xh, c[2]);
+        }
+    };
+    // the four values of group g (0 .. 3) of a lane: C[m][n .. n + 3]
+    const int m = wm * 32 + (lane & 31);
+    auto column = [&](int g) { return wn * 32 + 8 * g + 4 * (lane >> 5); };
+    auto value = [&](const Acc& c, int i) { return (c[0][i] + c[1][i]) + c[2][i]; };
+    auto at = [](int r, int k) { return r * SMALL + (((k >> 3) ^ kc_swz<SMALL>(r)) * 8) + (k & 7); };  // K-contiguous
+    auto strided_at = [](int k, int r) { return k * SMALL + (((r >> 4) ^ kstr_swz<SMALL>(k)) * 16) + (r & 15); };
+    auto put4 = [&](bf16_t* x, int off, int64_t plane, const float* v) __attribute__((always_inline)) {
+        uint32_t h[4], l[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const _Float16 hi = (_Float16)v[e], lo = (_Float16)(v[e] - (float)hi);
+            h[e] = __builtin_bit_cast(uint16_t, hi);
+            l[e] = __builtin_bit_cast(uint16_t, lo);
+        }
+        *(uint2*)(x + off) = make_uint2(h[0] | h[1] << 16, h[2] | h[3] << 16);
+        *(uint2*)(x + off + plane) = make_uint2(l[0] | l[1] << 16, l[2] | l[3] << 16);
+    };
+    auto store = [&](bf16_t* x, const Acc& c, float scale) __attribute__((always_inline)) {
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            float v[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = value(c, 4 * g + e) * scale;
+            put4(x, at(m, column(g)), E, v);
+        }
+    };
+    auto half_value = [](bf16_t x) { return (float)__builtin_bit_cast(_Float16, x); };
+
+    // X0, and A from it
+    Acc gram, c;
+    clear(gram);
+    const int row = tid >> 2, first = (tid & 3) * 16;  // a thread's 16 values of a block's row
+    for (int64_t l0 = 0; l0 < length; l0 += SMALL) {
+        __syncthreads();
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const int k = first + 8 * u;
+            float v[8];
+            if (!tall) {
+                x_elements(t, b.a, gs, taken, inv, row, l0 + k, v);
+                store_pair(xk + at(row, k), E, v, 0, 8);
+            } else {
+                x_elements(t, b.a, gs, taken, inv, l0 + row, k, v);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const _Float16 hi = (_Float16)v[e], lo = (_Float16)(v[e] - (float)hi);
+                    xk[at(k + e, row)] = __builtin_bit_cast(uint16_t, hi);
+                    xk[E + at(k + e, row)] = __builtin_bit_cast(uint16_t, lo);
+                }
+            }
+        }
+        __syncthreads();
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {  // (hi and lo, two pieces each)
+            const int k = first + 8 * (u & 1);
+            *(u32x4_t*)(t.x + (u >> 1) * SMALL * length + row * length + l0 + k) = *(const u32x4_t*)(xk + (u >> 1) * E + at(row, k));
+        }
+        product(xk, xk, std::false_type{}, gram);
+    }
+    bf16_t* const A = squares[0];
+    bf16_t* const TA = squares[1];
+    bf16_t *T = squares[2], *P = squares[3];
+    store(A, gram, b.q.gram[0] / (b.q.x[0] * b.q.x[0]));
+    __syncthreads();
+
+    // a block of X as a K-strided operand
+    auto load_block = [&](int64_t l0) {
+        __syncthreads();
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const int k = first + 8 * (u & 1);
+            *(u32x4_t*)(xs + (u >> 1) * E + strided_at(row, k)) = *(const u32x4_t*)(t.x + (u >> 1) * SMALL * length + row * length + l0 + k);
+        }
+        __syncthreads();
+    };
+    bool power = false;  // whether P stands (else it is I)
+    float sx = b.q.x[0], sp = 1.f;
+    const int steps = b.a.steps;
+    for (int k = 0; k < steps; ++k) {
+        const bool last = k == steps - 1, anew = anew_after(k, steps);
+        const float sg = b.q.gram[k], st_ = b.q.poly[k];
+        clear(c);
+        product(A, A, std::false_type{}, c);
+        {
+            const float pa = (float)b.a.a, pb = (float)b.a.b / sg, pc = (float)b.a.c / (sg * sg);
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const int n = column(g);
+                float v[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float x = half_value(A[at(m, n + e)]) + half_value(A[E + at(m, n + e)]);
+                    v[e] = fmaf(pc, value(c, 4 * g + e), fmaf(pb, x, m == n + e ? pa : 0.f)) * st_;
+                }
+                put4(T, at(m, n), E, v);
+            }
+        }
+        __syncthreads();
+        if (!last && !anew) {
+            clear(c);
+            product(T, A, std::false_type{}, c);
+            store(TA, c, b.q.half[k] / (st_ * sg));
+        }
+        if (power) {
+            clear(c);
+            product(T, P, std::false_type{}, c);
+            __syncthreads();
+            store(P, c, b.q.power[k] / (st_ * sp));
+            sp = b.q.power[k];
+            __syncthreads();
+        }
+        if (!last && !anew) {
+            __syncthreads();
+            clear(c);
+            product(T, TA, std::false_type{}, c);
+            store(A, c, b.q.gram[k + 1] / (st_ * b.q.half[k]));
+            __syncthreads();
+        }
+        if (!power) {
+            bf16_t* const x = T;
+            T = P;
+            P = x;
+            sp = st_;
+            power = true;
+        }
+        if (!anew) continue;
+        clear(gram);
+        const float sn = b.q.x[k + 1];
+        for (int64_t l0 = 0; l0 < length; l0 += SMALL) {
+            load_block(l0);
+            clear(c);
+            product(P, xs, std::true_type{}, c);
+            store(xk, c, sn / (sx * sp));
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                float v[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] = value(c, 4 * g + e) * (sn / (sx * sp));
+                put4(t.x, (int)(m * length + l0) + column(g), SMALL * length, v);
+            }
+            __syncthreads();
+            product(xk, xk, std::false_type{}, gram);
+        }
+        sx = sn;
+        power = false;
+        __syncthreads();
+        store(A, gram, b.q.gram[k + 1] / (sx * sx));
+        __syncthreads();
+    }
+    StepFactors f;
+    Destination d{t.param, t.master, t.rows, t.cols, t.scale, t.weight_decay, t.flags};
+    if (!step_factors(b.a, d, f)) return;
+    for (int64_t l0 = 0; l0 < length; l0 += SMALL) {
+        load_block(l0);
+        clear(c);
+        product(P, xs, std::true_type{}, c);
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            f32x4_t v;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = value(c, 4 * g + e) * (1.f / (sx * sp));
+            *(f32x4_t*)(cs + m * CP + column(g)) = v;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const int k = first + 8 * u;
+            float v[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = tall ? cs[(k + e) * CP + row] : cs[row * CP + k + e];
+            if (tall) step_elements(b.a, d, f, l0 + row, k, v);
+            else step_elements(b.a, d, f, row, l0 + k, v);
+        }
+    }
+}
+
 // What the host knows of a matrix's scratch.
 struct Layout {
     int64_t rp, cp, mp;
@@ -688,9 +924,31 @@ bool muon_scales(double a, double b, double c, int steps, MuonScales* out) {
 namespace {
 
 // The launches of up to PER_LAUNCH / 2 matrices.
+void fill(Matrix& m, const MuonTensor& t, const Layout& l, char* sc) {
+    m.grad = t.grad; m.m = t.m; m.param = t.param; m.master = t.master;
+    m.x = (uint16_t*)(sc + l.x[0]);
+    m.part = (double*)(sc + l.part);
+    m.rows = t.rows; m.cols = t.cols;
+    m.rp = (int32_t)l.rp; m.cp = (int32_t)l.cp;
+    m.parts = (int32_t)l.parts; m.per = (int32_t)l.per;
+    m.flags = t.flags;
+    m.weight_decay = (float)t.weight_decay; m.scale = t.scale;
+}
+
+// Matrices that one workgroup is through with sooner than many are with theirs, launch by launch.
+bool is_small(const MuonTensor& t) { return std::min(t.rows, t.cols) <= SMALL && std::max(t.rows, t.cols) <= SMALL_LENGTH; }
+
 hipError_t run_batch(const MuonTensor* t, const Layout* l, int count, const MuonScalars& a, const MuonScales& q, char* sc,
                      hipStream_t s) {
     hipError_t e;
+    if (std::all_of(t, t + count, is_small)) {  // (beside larger ones they cost nothing in those's launches)
+        Small b;
+        b.a = a;
+        b.q = q;
+        for (int i = 0; i < count; ++i) fill(b.t[i], t[i], l[i], sc);
+        hipLaunchKernelGGL(k_muon_small, dim3((unsigned)count), dim3(256), 0, s, b);
+        return hipGetLastError();
+    }
     {
         Elements b;
         b.a = a;
@@ -698,15 +956,7 @@ hipError_t run_batch(const MuonTensor* t, const Layout* l, int count, const Muon
         b.scale = q.x[0];
         uint32_t n = 0;
         for (int i = 0; i < count; ++i) {
-            Matrix& m = b.t[i];
-            m.grad = t[i].grad; m.m = t[i].m; m.param = t[i].param; m.master = t[i].master;
-            m.x = (uint16_t*)(sc + l[i].x[0]);
-            m.part = (double*)(sc + l[i].part);
-            m.rows = t[i].rows; m.cols = t[i].cols;
-            m.rp = (int32_t)l[i].rp; m.cp = (int32_t)l[i].cp;
-            m.parts = (int32_t)l[i].parts; m.per = (int32_t)l[i].per;
-            m.flags = t[i].flags;
-            m.weight_decay = (float)t[i].weight_decay; m.scale = t[i].scale;
+            fill(b.t[i], t[i], l[i], sc);
             b.first[i] = n;
             n += (uint32_t)l[i].parts;
         }
@@ -782,7 +1032,7 @@ hipError_t run_batch(const MuonTensor* t, const Layout* l, int count, const Muon
     float sx = q.x[0], sp = 1.f;
     if ((e = gram(x, sx, q.gram[0])) != hipSuccess) return e;
     for (int k = 0; k < a.steps; ++k) {
-        const bool last = k == a.steps - 1, anew = !last && (k == 1 || (k > 1 && (k - 1) % 3 == 0));
+        const bool last = k == a.steps - 1, anew = anew_after(k, a.steps);
         int poly = FREE;
         while (poly == power) ++poly;
         begin();

@@ -92,7 +92,8 @@ def held(got, ref, tol=TOL):
 
 
 SHAPES = [(1, 1), (1, 7), (9, 1), (3, 5), (64, 64), (65, 63), (32, 160), (160, 32), (100, 37), (129, 1000), (1000, 130), (257, 257),
-          (333, 1001), (37, 20011), (512, 512), (768, 1856), (1856, 256), (1024, 640), (1500, 1500)]
+          (333, 1001), (37, 20011), (512, 512), (768, 1856), (1856, 256), (1024, 640), (1500, 1500),
+          (64, 1024), (1024, 63), (1, 1024), (64, 1025), (65, 1024)]
 
 
 @pytest.mark.parametrize("rows,cols", SHAPES)
@@ -176,18 +177,41 @@ def test_bf16_weights_rounded_by_chance():
         assert torch.equal(got, (bits >> 16) & 0xFFFF)
 
 
-def test_many_matrices_are_as_each_alone():
+def test_many_matrices_in_one_list():
+    """More than one run of launches, matrices of no elements, short ones among them and alone. Which others share a launch may change
+    the order of a matrix's sums (each result holds the definition's tolerance), but not its momentum, and a list's results are the same
+    bits every time."""
     need_gpu()
     lib = handle()
     shapes = [(33 + 7 * i, 40 + 13 * ((i * 5) % 9)) for i in range(27)] + [(0, 5), (5, 0)]
-    ts = [matrix(r, c, i, ("f32", "master")[i % 2], ("f32", "bf16")[i % 3 == 0]) if r * c else
-          dict(param=torch.zeros(r, c, device="cuda"), grad=torch.zeros(r, c, device="cuda"), m=torch.zeros(r, c, device="cuda"))
-          for i, (r, c) in enumerate(shapes)]
-    alone = [{k: v.clone() if isinstance(v, torch.Tensor) else v for k, v in t.items()} for t in ts]
+
+    def make():
+        return [matrix(r, c, i, ("f32", "master")[i % 2], ("f32", "bf16")[i % 3 == 0]) if r * c else
+                dict(param=torch.zeros(r, c, device="cuda"), grad=torch.zeros(r, c, device="cuda"), m=torch.zeros(r, c, device="cuda"))
+                for i, (r, c) in enumerate(shapes)]
+
+    ts, again, alone = make(), make(), make()
+    want = []
+    for t in ts:
+        if t["param"].numel():
+            m, u = momentum_of(t, 0.95, True)
+            w = t.get("master")
+            want.append((m, (t["param"] if w is None else w).double(), newton_schulz(u)))
+        else:
+            want.append(None)
     step(lib, ts, lr=0.01)
-    for t, o in zip(ts, alone):
-        step(lib, [o], lr=0.01)
+    step(lib, again, lr=0.01)
+    for t, o, one, ref in zip(ts, again, alone, want):
         assert torch.equal(t["param"], o["param"]) and torch.equal(t["m"], o["m"])
+        if ref is None:
+            continue
+        step(lib, [one], lr=0.01)
+        m, p0, x = ref
+        for got in (t, one):
+            assert torch.equal(got["m"], m)
+            w = got["param"] if got.get("master") is None else got["master"]
+            room = 8 * U * float(p0.norm()) + 0.01 * 1.5 * TOL * float(x.norm())
+            assert float((w.double() - (p0 * (1 - 0.01 * 0.02) - 0.01 * 1.5 * x)).norm()) <= room
 
 
 @pytest.mark.parametrize("size", [1e-30, 1e-18, 1.0, 1e18, 1e30])
