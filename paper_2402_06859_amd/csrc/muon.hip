@@ -328,6 +328,13 @@ struct Products {
 };
 static_assert(sizeof(Products) <= 4096, "kernel arguments");
 
+// A barrier for what is in LDS alone: __syncthreads() also waits until the stores to memory have arrived, some 0.7 us.
+__device__ __forceinline__ void lds_barrier() {
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+
 // BM x BM blocks of WM x WN waves, each of 32 x 32 tiles; K in stages of KB through a ring of ST in LDS, filled by direct
 // global-to-LDS loads. One barrier a stage, before its last substep's multiplies, whose fragments are then in registers: behind it the
 // slot just read is filled again and the next stage's first fragments are read, every read and load between two multiplies.
@@ -339,7 +346,7 @@ __device__ __forceinline__ void product_block(const Products& b, int i, int t, b
     constexpr int MU = 3 * TM * TN, FR = 2 * (TM + TN);  // multiplies and fragments of a substep
     constexpr int SUMS = TM * TN == 1 ? 3 : 1;           // one tile a wave: a sum for each of the three products, so that none waits
     static_assert(NS % 2 == 0, "the fragment buffers alternate");
-    static_assert(CH * CP * 4 <= ST * STAGE * 2, "the staged sums fit the ring");
+    static_assert(KW * CH * CP * 4 <= ST * STAGE * 2, "the staged sums fit the ring");
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, kw = wave / (WM * WN);
     const int wm = wave / WN % WM, wn = wave % WN;
     const Product p = b.p[i];  // (a copy: the loads' asm would have the arguments read again in every step)
@@ -419,6 +426,16 @@ __device__ __forceinline__ void product_block(const Products& b, int i, int t, b
         f32x16_t& c = acc[SUMS == 3 ? k : 0][x][y];
         c = mfma32x32x16<true>(bf[buf][k == 0][y], af[buf][k == 1][x], c);
     };
+    // what the epilogue needs of the arguments, read before the loop: behind it each would be waited for
+    const int64_t plane = (int64_t)p.M * p.N;
+    float scale = i >= b.second ? b.scale2 : b.scale, out = i >= b.second ? b.out2 : b.out;
+    float pa = b.pa, pb = b.pb, pc = b.pc;
+    asm volatile("" : "+s"(scale), "+s"(out), "+s"(pa), "+s"(pb), "+s"(pc));
+    const bool diagonal = SYM && tm == tn;
+    StepFactors f;
+    if constexpr (EPI == STEP) {
+        if (!step_factors(b.s, b.d[i], f)) return;
+    }
     // QUARTIC's block of the Gram matrix, where a thread has little of it: on its way before the operands
     constexpr int AHEAD = EPI == POLY && BM == 64 ? CH * (BM / 8) / THREADS : 0;
     u32x4_t ahead[AHEAD + 1][2];
@@ -480,21 +497,10 @@ __device__ __forceinline__ void product_block(const Products& b, int i, int t, b
     for (; kt < nk; ++kt) step(kt, std::false_type{});
 
     float* const cs = (float*)smem;
-    const int64_t plane = (int64_t)p.M * p.N;
-    const float scale = i >= b.second ? b.scale2 : b.scale, out = i >= b.second ? b.out2 : b.out;
-    const bool diagonal = SYM && tm == tn;
-    StepFactors f;
-    if constexpr (EPI == STEP) {
-        if (!step_factors(b.s, b.d[i], f)) return;
-    }
     // 64 rows at a time through LDS. Lane holds C[m = 32 x + lane % 32][n = 32 y + 8 q + 4 (lane / 32) + e] in acc[4 q + e].
 #pragma unroll
     for (int h = 0; h < BM / CH; ++h) {
-        __syncthreads();
-#pragma unroll
-        for (int g = KW - 1; g >= 0; --g) {  // the wave groups' sums, added in turn
-            if (g < KW - 1) __syncthreads();
-            if (kw != g) continue;
+        lds_barrier();
 #pragma unroll
         for (int x = 0; x < TM; ++x) {
             const int row = wm * (BM / WM) + x * 32 + (lane & 31) - h * CH;
@@ -509,12 +515,10 @@ __device__ __forceinline__ void product_block(const Products& b, int i, int t, b
                         v[e] = acc[0][x][y][4 * q + e];
                         if constexpr (SUMS == 3) v[e] = (v[e] + acc[1][x][y][4 * q + e]) + acc[2][x][y][4 * q + e];
                     }
-                    f32x4_t* const at = (f32x4_t*)(cs + row * CP + wn * (BM / WN) + y * 32 + 8 * q + 4 * (lane >> 5));
-                    *at = g < KW - 1 ? *at + v : v;
+                    *(f32x4_t*)(cs + (kw * CH + row) * CP + wn * (BM / WN) + y * 32 + 8 * q + 4 * (lane >> 5)) = v;
                 }
         }
-        }
-        __syncthreads();
+        lds_barrier();
 #pragma unroll(AHEAD > 0 ? AHEAD : 1)
         for (int u = 0; u < CH * (BM / 8) / THREADS; ++u) {
             const int q = tid + u * THREADS, r = q / (BM / 8), c = q % (BM / 8) * 8;
@@ -522,7 +526,12 @@ __device__ __forceinline__ void product_block(const Products& b, int i, int t, b
             if (m >= p.M || n >= p.N) continue;
             float v[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = cs[r * CP + c + e] * scale;
+            for (int e = 0; e < 8; ++e) {
+                v[e] = cs[r * CP + c + e];
+#pragma unroll
+                for (int g = 1; g < KW; ++g) v[e] += cs[(g * CH + r) * CP + c + e];  // (the wave groups' sums)
+                v[e] *= scale;
+            }
             if constexpr (EPI == STEP) {
                 step_elements(b.s, b.d[i], f, m, n, v);
                 continue;
@@ -537,7 +546,7 @@ __device__ __forceinline__ void product_block(const Products& b, int i, int t, b
                     unpack_f16x8(*(const u32x4_t*)(p.aux + plane + m * p.N + n), lo);
                 }
 #pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] = fmaf(b.pc, v[e], fmaf(b.pb, hi[e] + lo[e], m == n + e ? b.pa : 0.f));
+                for (int e = 0; e < 8; ++e) v[e] = fmaf(pc, v[e], fmaf(pb, hi[e] + lo[e], m == n + e ? pa : 0.f));
             }
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
@@ -548,7 +557,7 @@ __device__ __forceinline__ void product_block(const Products& b, int i, int t, b
             store_pair(p.c + m * p.N + n, plane, v, 0, diagonal ? (int)(m - n) + 1 : 8);
         }
         if constexpr (SYM) {  // the block above the diagonal: rows n, columns m
-            __syncthreads();
+            lds_barrier();
             for (int q = tid; q < BM * (CH / 8); q += THREADS) {
                 const int r = q / (CH / 8), c = q % (CH / 8) * 8;
                 const int64_t n = n0 + r, m = m0 + h * CH + c;
@@ -884,6 +893,8 @@ hipError_t launch_products(Products& b, hipStream_t s) {
     }
     b.first[b.count] = n;
     if (plan.side == 256) hipLaunchKernelGGL((k_muon_product<256, 2, 4, 1, 32, 2, KIND>), dim3(n), dim3(512), 0, s, b);
+    // (the weights' step has more to do behind its sums: eight waves, 512 x 4352 eight times 105 -> 91 us; elsewhere four are as fast or faster)
+    else if (plan.side == 128 && KIND == LAST) hipLaunchKernelGGL((k_muon_product<128, 2, 4, 1, 32, 2, KIND>), dim3(n), dim3(512), 0, s, b);
     else if (plan.side == 128) hipLaunchKernelGGL((k_muon_product<128, 2, 2, 1, 32, 2, KIND>), dim3(n), dim3(256), 0, s, b);
     else if (plan.per_cu == 1) hipLaunchKernelGGL((k_muon_product<64, 2, 2, 2, 64, 4, KIND>), dim3(n), dim3(512), 0, s, b);
     else hipLaunchKernelGGL((k_muon_product<64, 2, 2, 2, 64, 2, KIND>), dim3(n), dim3(512), 0, s, b);
