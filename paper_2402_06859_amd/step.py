@@ -7,11 +7,12 @@ here; all arithmetic is in the library's kernels.
 from __future__ import annotations
 
 import contextlib
-from typing import Optional, Sequence
+import math
+from typing import Callable, Optional, Sequence
 
 import torch
 
-from .rdcn import BF16, I64, Rdcn, adamw_tensors, config_for
+from .rdcn import BF16, I64, Rdcn, adamw_tensors, config_for, muon_tensors
 from .synth import Workload
 
 _DT = {"bf16": torch.bfloat16, "f32": torch.float32}
@@ -210,6 +211,65 @@ class DeviceClasses:
             opt.update(stream)
 
 
+class DeviceChoices:
+    """Learning from recorded choices over a large set of classes, and answering from them, on x [B, dim], normally x_L of the handle
+    `lib`: class weights w [classes, dim] of its storage type, the chosen class of each row (labels [B] of its id type; below 0: a row
+    without one), offsets per class (-inf masks one). forward leaves logprob, entropy and lse [B] and, with top, the most
+    probable classes (top_ids, top_logprob [B, top]); backward takes the loss's gradients in logprob and entropy to grad_x and
+    grad_w. keep: whether forward keeps every class's exponential (2 bytes each, 4 in float models) and so saves backward a product.
+    What does not fit is a ValueError."""
+
+    def __init__(self, lib: Rdcn, w: torch.Tensor, labels: torch.Tensor, offset: Optional[torch.Tensor] = None,
+                 logit_scale: float = 1.0, top: int = 0, keep: bool = True):
+        self.lib, self.w, self.labels, self.offset, self.logit_scale, self.top = lib, w, labels, offset, logit_scale, top
+        self.B = labels.numel()
+        self.classes, self.dim = w.shape
+        dev = w.device
+        for name, t in (("labels", labels), ("offset", offset)):
+            if t is not None and t.device != dev:
+                raise ValueError("DeviceChoices: %s must be on %s" % (name, dev))
+        f = dict(dtype=torch.float32, device=dev)
+        self.logprob, self.entropy, self.lse = (torch.empty(self.B, **f) for _ in range(3))
+        self.top_ids = torch.empty((self.B, top), dtype=labels.dtype, device=dev) if top else None
+        self.top_logprob = torch.empty((self.B, top), **f) if top else None
+        self.stats = torch.empty((self.B, 4), **f)
+        self.grad_x = torch.empty((self.B, self.dim), dtype=w.dtype, device=dev)
+        self.grad_w = torch.empty_like(w)
+        forward, kept, grad, _ = lib.logprobs_workspace(self.B, self.dim, self.classes, top)
+        self.kept = torch.empty(max(kept, 256), dtype=torch.uint8, device=dev) if keep else None
+        self.scratch = torch.empty(max(forward, grad, 256), dtype=torch.uint8, device=dev)
+
+    def trained(self):
+        return [(self.w, self.grad_w)]
+
+    def forward(self, x: torch.Tensor, stream=None):
+        self.lib.logprobs_forward(self.B, self.dim, self.classes, x, self.w, self.offset, self.labels, self.logit_scale,
+                                  self.logprob, self.entropy, self.lse, self.scratch, top=self.top, top_ids=self.top_ids,
+                                  top_logprob=self.top_logprob, stats=self.stats, kept=self.kept, stream=stream)
+
+    def backward(self, x: torch.Tensor, grad_logprob: Optional[torch.Tensor], grad_entropy: Optional[torch.Tensor] = None,
+                 stream=None):
+        """The gradients of the loss of the last forward on the same x."""
+        self.lib.logprobs_grad(self.B, self.dim, self.classes, x, self.w, self.offset, self.labels, self.logit_scale,
+                               self.stats, grad_logprob, grad_entropy, self.grad_x, self.grad_w, self.scratch,
+                               kept=self.kept, stream=stream)
+
+    def train_step(self, db: DeviceBatch, upstream: Callable, opts: Sequence = (), stream=None):
+        """One training step: gather -> cross stack -> log probabilities -> upstream(logprob, entropy), which returns the loss's
+        gradients in them -> their gradient -> cross-stack backward -> embedding backward -> the updates of opts."""
+        db.zero_table_grads(stream)
+        db.gather(stream)
+        db.forward(stream)
+        self.forward(db.x_out, stream)
+        with _on(stream):
+            g, h = upstream(self.logprob, self.entropy)
+        self.backward(db.x_out, g, h, stream)
+        db.backward(self.grad_x, stream)
+        db.embed_backward(stream=stream)
+        for opt in opts:
+            opt.update(stream)
+
+
 class DeviceAdamW:
     """AdamW over (weight, gradient) pairs, or (weight, gradient, weight_decay) where a weight has a decay of its own (an
     embedding table often none); the others decay by weight_decay if they have more than one dimension. Moments in float
@@ -257,3 +317,48 @@ class DeviceAdamW:
                 self.steps.add_(torch.eq(clip, clip, out=self.taken))
         self.lib.adamw_step(self.list, lr=0.0, device_lr=self.lr, device_step=self.steps, clip=clip, stream=stream,
                             **self.hyper)
+
+
+class DeviceMuon:
+    """Muon over (weight, gradient) pairs of matrices, or (weight, gradient, weight_decay), beside a DeviceAdamW for everything
+    else. A matrix that stacks several maps steps them apart where each one's rows are a pair of their own. Every update's elements are
+    of size 0.2 lr, whatever the matrix's shape, like AdamW's. Float masters of bf16 weights or none, and the
+    gradients clipped to max_norm together. Rate and step number stand on the device: change lr with set_lr. With max_norm,
+    an update whose gradients' norm is not finite is left out whole."""
+
+    def __init__(self, lib: Rdcn, pairs: Sequence, lr: float, weight_decay: float = 0.0, momentum: float = 0.95,
+                 nesterov: bool = True, master: bool = True, max_norm: Optional[float] = None, steps: int = 5,
+                 coefficients=(3.4445, -4.7750, 2.0315), seed: int = 0):
+        self.lib, self.max_norm = lib, max_norm
+        self.hyper = dict(momentum=momentum, nesterov=nesterov, steps=steps, coefficients=coefficients, stochastic=True,
+                          seed=seed)
+        self.tensors = []
+        for p, g, *own in pairs:
+            t = {"param": p, "grad": g, "m": torch.zeros(p.shape, dtype=torch.float32, device=p.device),
+                 "weight_decay": own[0] if own else weight_decay, "scale": 0.2 * math.sqrt(max(p.shape))}
+            if master and p.dtype == torch.bfloat16:
+                t["master"] = p.float()
+            self.tensors.append(t)
+        self.list = muon_tensors(self.tensors)
+        # (the norm reads the gradients alone)
+        self.norm_list = adamw_tensors([{"param": t["grad"], "grad": t["grad"], "m": t["m"], "v": t["m"]} for t in self.tensors])
+        dev = self.tensors[0]["param"].device
+        self.lr = torch.full((1,), lr, dtype=torch.float32, device=dev)
+        self.steps = torch.zeros(1, dtype=torch.int64, device=dev)
+        self.norm = torch.zeros(2, dtype=torch.float32, device=dev)   # norm of the gradients, clip factor
+        self.scratch = torch.empty(max(256, lib.muon_workspace(self.list), lib.grad_norm_workspace(self.norm_list)),
+                                   dtype=torch.uint8, device=dev)
+
+    def set_lr(self, lr: float, stream=None):
+        with _on(stream):
+            self.lr.fill_(lr)
+
+    def update(self, stream=None):
+        clip = None
+        if self.max_norm is not None:
+            self.lib.grad_norm(self.norm_list, 1.0, self.max_norm, self.norm, self.scratch, stream)
+            clip = self.norm[1:]
+        with _on(stream):
+            self.steps.add_(1)
+        self.lib.muon_step(self.list, self.scratch, lr=0.0, device_lr=self.lr, device_step=self.steps, clip=clip,
+                           stream=stream, **self.hyper)
