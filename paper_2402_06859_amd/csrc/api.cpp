@@ -499,6 +499,26 @@ SoftProduct soft_product(const rdcn_handle* h, GemmArgs g, const float* acc_in, 
     return r;
 }
 
+// grad_x of a G of hi and lo rows: the planes of its sum are `rows` rows each, in order (a split's hi, its lo, the next split's ..).
+SoftProduct soft_product_fine(const rdcn_handle* h, GemmArgs g, int64_t rows, const float* acc_in, float* acc, void* out, bool last,
+                              float* splitk) {
+    SoftProduct r{};
+    r.p = plan_gemm_long(g.M, g.N, g.K, h->bf16);
+    g.scale = 1.0f;
+    g.ldc = g.ldx = g.N;
+    g.epi = r.p.splits > 1 ? EPI_PARTIAL : EPI_STORE_F32;
+    g.c = splitk;
+    r.summed = true;
+    r.sum.part = splitk;
+    r.sum.splits = 2 * r.p.splits;
+    r.sum.n = rows * g.N;
+    r.sum.acc = acc_in;
+    r.sum.acc_out = last ? nullptr : acc;
+    r.sum.out = out;
+    r.g = g;
+    return r;
+}
+
 // Both gradients from G: products of few small blocks go in one launch, and so do the sums that end either's.
 hipError_t soft_gradients(rdcn_handle* h, const SoftProduct& x, const SoftProduct& w, hipStream_t s) {
     hipError_t e;
@@ -572,7 +592,13 @@ rdcn_status soft_forward(rdcn_handle* h, const SoftPlan& S, int64_t rows, int64_
 // many classes at a time as it holds, from the exponentials that the forward kept (2 bytes each, 4 in float models: one read and
 // one write in place of a product) or from the logits computed again; its two products are the softmax loss's.
 // ---------------------------------------------------------------------------
+// Rows of a bf16 model's G up to which it stands as hi + lo, 2 rows of it for one: the products over so few rows are bound by w and by
+// their starts, and over few rows and classes the roundings of G to bf16 do not average out in the gradients.
+constexpr int64_t CHOICE_FINE_ROWS = 32;
+int64_t choice_copies(const rdcn_handle* h, int64_t rows) { return h->bf16 && rows <= CHOICE_FINE_ROWS ? 2 : 1; }
+
 struct ChoicePlan {
+    int64_t copies;  // rows of G for one
     int64_t tiles, tile, piece, ld;
     int64_t kept_ld;
     size_t kept_stat, kept_total;  // of `kept`: the exponentials, then the tiles' ChoiceStats
@@ -602,13 +628,15 @@ ChoicePlan choice_layout(const rdcn_handle* h, int64_t rows, int64_t dim, int64_
     s.piece = piece;
     s.ld = (piece + vec - 1) / vec * vec;
     off = 0;
-    s.kept = off; off += al((size_t)rows * dim * e);
-    s.G = off; off += al((size_t)rows * s.ld * e);
+    s.copies = choice_copies(h, rows);
+    const int64_t grows = s.copies * rows;
+    s.kept = off; off += al((size_t)grows * dim * e);
+    s.G = off; off += al((size_t)grows * s.ld * e);
     s.acc = off; off += classes > piece ? al((size_t)rows * dim * 4) : 0;  // grad_x as a sum of several products
-    int64_t split = 0, splitw = 0;
+    int64_t split = s.copies > 1 ? grows * dim : 0, splitw = 0;
     for (int64_t n : {piece, classes % piece}) {
-        split = std::max(split, split_floats(h, rows, dim, n));
-        splitw = std::max(splitw, split_floats(h, n, dim, rows));
+        split = std::max(split, split_floats(h, grows, dim, n));
+        splitw = std::max(splitw, split_floats(h, n, dim, grows));
     }
     s.splitk = off; off += al((size_t)split * 4);
     s.splitw = off; off += al((size_t)splitw * 4);
@@ -1602,8 +1630,9 @@ rdcn_status rdcn_logprobs_grad(rdcn_handle* h, int64_t rows, int64_t dim, int64_
     p.labels = labels; p.ids64 = h->ids64;
     p.grad_logprob = grad_logprob; p.grad_entropy = grad_entropy;
     p.logit_scale = logit_scale;
-    p.x = x; p.kept = sc + S.kept;
+    p.x = x; p.kept = sc + S.kept; p.copies = (int)S.copies;
     p.row = row; p.err = h->err;
+    char* const lo = S.copies > 1 ? G + (size_t)rows * S.ld * e : nullptr;
     {
         ProfScope ps(h, RDCN_KERNEL_HEAD_OUT_BWD, s);
         RDCN_TRY(launch_choice_prepare(p, h->bf16, s));
@@ -1619,7 +1648,7 @@ rdcn_status rdcn_logprobs_grad(rdcn_handle* h, int64_t rows, int64_t dim, int64_
             q.stat = (const ChoiceStat*)((const char*)kept + S.kept_stat);
             q.row = row;
             q.labels = labels; q.ids64 = h->ids64;
-            q.kept = kept; q.out = G;
+            q.kept = kept; q.out = G; q.out_lo = lo;
             ProfScope ps(h, RDCN_KERNEL_HEAD_OUT_BWD, s);
             RDCN_TRY(launch_choice_normalize(q, h->bf16, s));
         } else {
@@ -1631,21 +1660,24 @@ rdcn_status rdcn_logprobs_grad(rdcn_handle* h, int64_t rows, int64_t dim, int64_
             g.offset = offset ? offset + v : nullptr;
             g.labels = labels; g.labels64 = h->ids64; g.label0 = v;
             g.choicerow = row;
-            g.c = G; g.ldc = S.ld;
+            g.c = G; g.c2 = lo; g.ldc = S.ld;
             ProfScope ps(h, RDCN_KERNEL_HEAD_FWD_GEMM, s);
             RDCN_TRY(launch_gemm(g, plan_logits(h, rows, n, dim), h->bf16, s));
         }
         GemmArgs gx{};
-        gx.M = rows; gx.N = dim; gx.K = n;
+        gx.M = S.copies * rows; gx.N = dim; gx.K = n;
         gx.a = G; gx.lda = S.ld;
         gx.b = wp; gx.ldb = dim; gx.b_kstrided = true;
         gx.rem_last = true;
         GemmArgs gw{};
-        gw.M = n; gw.N = dim; gw.K = rows;
+        gw.M = n; gw.N = dim; gw.K = S.copies * rows;
         gw.a = G; gw.lda = S.ld; gw.a_kstrided = true;
         gw.b = p.kept; gw.ldb = dim; gw.b_kstrided = true;
-        const SoftProduct px = soft_product(h, gx, v > 0 ? acc : nullptr, acc, grad_x, v + n == classes,
-                                            (float*)(sc + S.splitk));
+        const float* const before = v > 0 ? acc : nullptr;
+        float* const splitk = (float*)(sc + S.splitk);
+        const bool last = v + n == classes;
+        const SoftProduct px = S.copies > 1 ? soft_product_fine(h, gx, rows, before, acc, grad_x, last, splitk)
+                                            : soft_product(h, gx, before, acc, grad_x, last, splitk);
         const SoftProduct pw = soft_product(h, gw, nullptr, nullptr, (char*)grad_w + (size_t)v * dim * e, true,
                                             (float*)(sc + S.splitw));
         RDCN_TRY(soft_gradients(h, px, pw, s));

@@ -32,7 +32,7 @@ enum GemmEpi {
                           // the label; with groups: groups[m * ngroups + u] of the classes of group u (gemm_choice_groups);
                           // with c: c = exp(z - max of the tile) (f16 times SOFT_E_SCALE, or float), zero in the pad of a row
     EPI_CHOICE_GRAD = 11  // c = exp(d) (r.a + r.b d) for d = z - r.max, r = choicerow[m], r.label at the row's label (storage
-                          // type), zero where r.a and r.b are 0 or z is -inf and in the pad of a row
+                          // type; with c2: hi in c, lo in c2), zero where r.a and r.b are 0 or z is -inf and in the pad of a row
 };
 
 // exp(z - max) of a tile's row is held in f16 times this (a power of two): values down to

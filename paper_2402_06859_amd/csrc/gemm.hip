@@ -422,7 +422,8 @@ __device__ __forceinline__ void choice_epilogue8(const GemmArgs& g, int64_t m, i
             v[e] = none || v[e] == NEG ? 0.f : soft_exp<bf16_t>(d) * fmaf(r.b, d, r.a);
             if (lab == e) v[e] = r.label;
         }
-        store8<bf16_t>((bf16_t*)g.c + m * g.ldc + n, v);
+        if (g.c2) store_split8((bf16_t*)g.c + m * g.ldc + n, (bf16_t*)g.c2 + m * g.ldc + n, v);
+        else store8<bf16_t>((bf16_t*)g.c + m * g.ldc + n, v);
         return;
     }
 #pragma unroll
@@ -1003,7 +1004,16 @@ __device__ __forceinline__ void choice_rows(const GemmArgs& g, int64_t mw, int64
                         if (lab == col(j, q) + e) a[e] = r.label;
                     }
                 }
-            store(v, m, in, 1.f);
+            if (sizeof(T) == 2 && g.c2) {  // (of few rows: straight from the lanes)
+#pragma unroll
+                for (int j = 0; j < TN; ++j)
+#pragma unroll
+                    for (int q = 0; q < Q; ++q)
+                        if (in && col(j, q) < pad)
+                            store_split4<T>((T*)g.c + m * g.ldc + nw + col(j, q), (T*)g.c2 + m * g.ldc + nw + col(j, q), v + 4 * (j * Q + q));
+            } else {
+                store(v, m, in, 1.f);
+            }
         } else {
             if (lab >= 0) {
                 float z = 0.f;

@@ -34,7 +34,7 @@ struct ChoiceRows {
 };
 hipError_t launch_choice_rows(const ChoiceRows& a, bool bf16, hipStream_t s);
 
-// row[m] (ChoiceRow) from stats and the upstream gradients, and kept [rows, dim] = x with zeros in rows without gradient.
+// row[m] (ChoiceRow) from stats and the upstream gradients, and kept [rows, dim] = x with zeros in rows without gradient, `copies` times.
 struct ChoicePrepare {
     int64_t rows, dim, classes;
     const float4* stats;
@@ -45,6 +45,7 @@ struct ChoicePrepare {
     float logit_scale;
     const void* x;
     void* kept;
+    int copies;
     ChoiceRow* row;
     int* err;
 };
@@ -60,6 +61,7 @@ struct ChoiceNormalize {
     bool ids64;
     const void* kept;
     void* out;
+    void* out_lo;  // or NULL; bf16: what rounding leaves of out
 };
 hipError_t launch_choice_normalize(const ChoiceNormalize& a, bool bf16, hipStream_t s);
 

@@ -331,7 +331,7 @@ __global__ __launch_bounds__(256) void k_choice_prepare(ChoicePrepare a) {
     for (int64_t i = t; i < n; i += step) {
         u32x4_t v = {0u, 0u, 0u, 0u};
         if (upstream(a, i / per, y, g, h)) v = *(const u32x4_t*)((const T*)a.x + i * W);
-        *(u32x4_t*)((T*)a.kept + i * W) = v;
+        for (int k = 0; k < a.copies; ++k) *(u32x4_t*)((T*)a.kept + k * a.rows * a.dim + i * W) = v;
     }
 }
 
@@ -364,6 +364,11 @@ __global__ __launch_bounds__(256) void k_choice_normalize(ChoiceNormalize a) {
                 if (y - v == i) e[i] = r.label;
         }
         *(u32x4_t*)((T*)a.out + m * a.ld + n) = st<T>::pack(e);
+        if (sizeof(T) == 2 && a.out_lo) {
+#pragma unroll
+            for (int i = 0; i < W; ++i) e[i] -= st<T>::round(e[i]);
+            *(u32x4_t*)((T*)a.out_lo + m * a.ld + n) = st<T>::pack(e);
+        }
     }
 }
 

@@ -322,7 +322,8 @@ def test_label_past_the_classes_is_reported_and_left_out(dtype):
 
 
 @pytest.mark.parametrize("dtype,rows,dim,classes", [("bf16", 300, 264, 5003), ("f32", 130, 68, 3075), ("bf16", 2000, 64, 9000),
-                                                    ("bf16", 1100, 512, 33001)])
+                                                    ("bf16", 1100, 512, 33001), ("bf16", 20, 136, 9001), ("bf16", 32, 1024, 5003),
+                                                    ("bf16", 33, 1024, 5003)])
 def test_less_scratch_means_pieces_of_the_classes(dtype, rows, dim, classes):
     need_gpu()
     print("logprobs in pieces", dtype, rows, dim, classes, flush=True)
