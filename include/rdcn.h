@@ -579,7 +579,7 @@ rdcn_status rdcn_logprobs_forward(rdcn_handle* h, int64_t rows, int64_t dim, int
  *   grad_x = s dL/dz w, grad_w = s (dL/dz)^T x, both in the storage dtype and overwritten.
  * stats (and kept, or NULL) must be those of a forward with the same x, w, offset, labels and logit_scale; both stay as they are. Rows without a label (when labels are given), and rows whose
  * g and h are both 0, have no gradient and may hold anything in x and stats. Masked logits are constants. bf16 models round dL/dz
- * to bf16 for the products (half a step, 2^-8 of an element; to bf16 hi + lo, 2^-16, up to 32 rows) and each gradient once at the end; sums are
+ * to bf16 for the products (half a step, 2^-8 of an element; to bf16 hi + lo, 2^-16, where rows are few or the products small) and each gradient once at the end; sums are
  * float and in a fixed order. 1 - p of a label keeps its digits where p is near 1. With grad_bytes of scratch the call is fastest; it takes any size from
  * grad_least_bytes on, working on fewer classes at a time.
  */

@@ -592,10 +592,14 @@ rdcn_status soft_forward(rdcn_handle* h, const SoftPlan& S, int64_t rows, int64_
 // many classes at a time as it holds, from the exponentials that the forward kept (2 bytes each, 4 in float models: one read and
 // one write in place of a product) or from the logits computed again; its two products are the softmax loss's.
 // ---------------------------------------------------------------------------
-// Rows of a bf16 model's G up to which it stands as hi + lo, 2 rows of it for one: the products over so few rows are bound by w and by
-// their starts, and over few rows and classes the roundings of G to bf16 do not average out in the gradients.
+// Where a bf16 model's G stands as hi + lo, two rows of it for one: over few rows and classes its roundings to bf16 do not average out in the
+// gradients, and products of few rows are bound by w, small ones by their starts. The gradient's us, one / two: 32 x 1856 x 32000 87 / 89,
+// 64 x 1856 x 32000 86 / 103; 333 x 136 x 1001 17.4 / 19.6; 500 x 512 x 1000 19.4 / 19.0; 4000 x 64 x 400 20.4 / 24.3.
 constexpr int64_t CHOICE_FINE_ROWS = 32;
-int64_t choice_copies(const rdcn_handle* h, int64_t rows) { return h->bf16 && rows <= CHOICE_FINE_ROWS ? 2 : 1; }
+constexpr double CHOICE_FINE_SIZE = 2.5e8;
+int64_t choice_copies(const rdcn_handle* h, int64_t rows, int64_t dim, int64_t classes) {
+    return h->bf16 && (rows <= CHOICE_FINE_ROWS || (double)rows * (double)dim * (double)classes <= CHOICE_FINE_SIZE) ? 2 : 1;
+}
 
 struct ChoicePlan {
     int64_t copies;  // rows of G for one
@@ -628,7 +632,7 @@ ChoicePlan choice_layout(const rdcn_handle* h, int64_t rows, int64_t dim, int64_
     s.piece = piece;
     s.ld = (piece + vec - 1) / vec * vec;
     off = 0;
-    s.copies = choice_copies(h, rows);
+    s.copies = choice_copies(h, rows, dim, classes);
     const int64_t grows = s.copies * rows;
     s.kept = off; off += al((size_t)grows * dim * e);
     s.G = off; off += al((size_t)grows * s.ld * e);
