@@ -114,25 +114,29 @@ __device__ __forceinline__ void store_pair(uint16_t* c, int64_t plane, const flo
     }
 }
 
-// Eight values of an array from element i on, `left` of which exist; whole: all of them, 16-byte aligned.
-__device__ __forceinline__ void load_f32(const float* p, int64_t i, int left, bool whole, float* v) {
-    if (whole) {
-        st<float>::unpack(*(const u32x4_t*)(p + i), v);
-        st<float>::unpack(*(const u32x4_t*)(p + i + 4), v + 4);
+// Eight values of an array from element i on, `left` of which exist (eight: a vector, whatever its alignment: rows of an odd length).
+typedef u32x4_t u32x4_a4_t __attribute__((aligned(4)));
+typedef u32x4_t u32x4_a2_t __attribute__((aligned(2)));
+__device__ __forceinline__ void load_f32(const float* p, int64_t i, int left, float* v) {
+    if (left == 8) {
+        st<float>::unpack(*(const u32x4_a4_t*)(p + i), v);
+        st<float>::unpack(*(const u32x4_a4_t*)(p + i + 4), v + 4);
     } else {
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] = e < left ? p[i + e] : 0.f;
     }
 }
-__device__ __forceinline__ void load_grad(const Matrix& t, int64_t i, int left, bool whole, float* v) {
-    if (!(t.flags & MUON_GRAD_BF16)) {
-        load_f32((const float*)t.grad, i, left, whole, v);
-    } else if (whole) {
-        st<bf16_t>::unpack(*(const u32x4_t*)((const bf16_t*)t.grad + i), v);
+__device__ __forceinline__ void load_bf16(const bf16_t* p, int64_t i, int left, float* v) {
+    if (left == 8) {
+        st<bf16_t>::unpack(*(const u32x4_a2_t*)(p + i), v);
     } else {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = e < left ? bf16_to_f32(((const bf16_t*)t.grad)[i + e]) : 0.f;
+        for (int e = 0; e < 8; ++e) v[e] = e < left ? bf16_to_f32(p[i + e]) : 0.f;
     }
+}
+__device__ __forceinline__ void load_grad(const Matrix& t, int64_t i, int left, float* v) {
+    if (t.flags & MUON_GRAD_BF16) load_bf16((const bf16_t*)t.grad, i, left, v);
+    else load_f32((const float*)t.grad, i, left, v);
 }
 __device__ __forceinline__ float update_of(const MuonScalars& a, float m, float g) {
 #pragma clang fp contract(off)
@@ -147,8 +151,8 @@ __device__ __forceinline__ double momentum_range(const Matrix& t, const MuonScal
     for (int64_t k = from + threadIdx.x * 8; k < to; k += 2048) {
         const int left = to - k < 8 ? (int)(to - k) : 8;
         float g[8], m[8];
-        load_grad(t, k, left, left == 8, g);
-        load_f32(t.m, k, left, left == 8, m);
+        load_grad(t, k, left, g);
+        load_f32(t.m, k, left, m);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             const float x = g[e] * gs;
@@ -178,10 +182,9 @@ __device__ __forceinline__ void x_elements(const Matrix& t, const MuonScalars& a
     if (!taken || r >= t.rows || c >= t.cols) return;
     const int64_t k = r * t.cols + c;
     const int left = t.cols - c < 8 ? (int)(t.cols - c) : 8;
-    const bool whole = left == 8 && (k & 7) == 0;
     float g[8], m[8];
-    load_grad(t, k, left, whole, g);
-    load_f32(t.m, k, left, whole, m);
+    load_grad(t, k, left, g);
+    load_f32(t.m, k, left, m);
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] = e < left ? (float)((double)update_of(a, m[e], g[e] * gs) * inv) : 0.f;
 }
@@ -264,28 +267,18 @@ __device__ __forceinline__ void step_elements(const MuonScalars& a, const Destin
     if (m >= d.rows || n >= d.cols) return;
     const int64_t at = m * d.cols + n;
     const int left = d.cols - n < 8 ? (int)(d.cols - n) : 8;
-    const bool pbf = d.flags & MUON_PARAM_BF16, whole = left == 8 && (at & 7) == 0;
+    const bool pbf = d.flags & MUON_PARAM_BF16;
     float p[8];
-    if (whole) {
-        if (d.master || !pbf) {
-            const float* const q = (d.master ? d.master : (const float*)d.param) + at;
-            st<float>::unpack(*(const u32x4_t*)q, p);
-            st<float>::unpack(*(const u32x4_t*)(q + 4), p + 4);
-        } else {
-            st<bf16_t>::unpack(*(const u32x4_t*)((const bf16_t*)d.param + at), p);
-        }
-    } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-            p[e] = e >= left ? 0.f : d.master ? d.master[at + e] : pbf ? bf16_to_f32(((const bf16_t*)d.param)[at + e]) : ((const float*)d.param)[at + e];
-    }
+    if (d.master) load_f32(d.master, at, left, p);
+    else if (pbf) load_bf16((const bf16_t*)d.param, at, left, p);
+    else load_f32((const float*)d.param, at, left, p);
 #pragma unroll
     for (int e = 0; e < 8; ++e) p[e] = p[e] * f.decay - v[e] * f.size;
     if (d.master || !pbf) {
         float* const q = (d.master ? d.master : (float*)d.param) + at;
-        if (whole) {
-            *(u32x4_t*)q = st<float>::pack(p);
-            *(u32x4_t*)(q + 4) = st<float>::pack(p + 4);
+        if (left == 8) {
+            *(u32x4_a4_t*)q = st<float>::pack(p);
+            *(u32x4_a4_t*)(q + 4) = st<float>::pack(p + 4);
         } else {
 #pragma unroll
             for (int e = 0; e < 8; ++e)
@@ -305,8 +298,8 @@ __device__ __forceinline__ void step_elements(const MuonScalars& a, const Destin
         }
     }
     bf16_t* const q = (bf16_t*)d.param + at;
-    if (whole) {
-        *(u32x4_t*)q = u32x4_t{r[0] | r[1] << 16, r[2] | r[3] << 16, r[4] | r[5] << 16, r[6] | r[7] << 16};
+    if (left == 8) {
+        *(u32x4_a2_t*)q = u32x4_t{r[0] | r[1] << 16, r[2] | r[3] << 16, r[4] | r[5] << 16, r[6] | r[7] << 16};
     } else {
 #pragma unroll
         for (int e = 0; e < 8; ++e)
@@ -853,13 +846,20 @@ int64_t blocks_of(const Product& p, int side) {
     return KIND <= OF_X ? tm * (tm + 1) / 2 : tm * tn;
 }
 
-// How a launch's products are cut: whichever is through first. A K step of 64 takes, in us, `one` where a block has a CU for
-// itself, and `more` for every block of a CU where all of them are busy.
+// How a launch's products are cut: whichever is through first. `slots` blocks run at once; a K step of 64 takes them `full` us where
+// all slots are taken, and base + slope * their share where fewer are (measured with 2048^2, six of 1000^2, two of 2086 x 5534, 4096^2, and the models
+// of 512 x 4352 and 768 x 1856; in the order below, us of a squaring: 2048^2 57 / 54 / 57 / 47 / 118; six of 1000^2 42 / 46 / 40 / 33 / 75; 4096^2
+// 275 / 284 / 285 / 252 / 250; and of the apply of 4096^2 521 / 604 / 361 / 381 / 313).
+enum { SMALL_TWO, SMALL_DEEP, MIDDLE_TWO, MIDDLE_DEEP, LARGE };
 struct Plan {
-    int side, per_cu;
-    double one, more;
+    int id, side, slots;
+    double full, base, slope;
 };
-constexpr Plan PLANS[] = {{64, 2, 0.9, 0.62}, {64, 1, 0.5, 0.75}, {128, 2, 1.75, 1.9}, {256, 1, 5.5, 5.5}};
+constexpr Plan PLANS[] = {{SMALL_TWO, 64, 512, 1.1, 0.72, 0.38},  // 64 KiB of LDS: two blocks a CU
+                          {SMALL_DEEP, 64, 256, 0.65, 0.38, 0.22},  // a ring of four stages, one block a CU
+                          {MIDDLE_TWO, 128, 512, 2.8, 1.4, 1.4},
+                          {MIDDLE_DEEP, 128, 256, 1.45, 1.1, 0.4},  // stages of 64, eight waves in two groups along K
+                          {LARGE, 256, 256, 5.2, 3.4, 1.6}};
 
 template <int KIND>
 const Plan& plan_of(const Products& b) {
@@ -873,7 +873,8 @@ const Plan& plan_of(const Products& b) {
             steps += n * k;
             longest = std::max(longest, k);
         }
-        const double mean = steps / blocks, us = std::max(longest * q.one, std::ceil(blocks / 256.0) * mean * (blocks > 256.0 ? q.more : q.one));
+        const double rounds = std::floor(blocks / q.slots), rest = blocks / q.slots - rounds;
+        const double us = std::max(longest * q.base, steps / blocks * (rounds * q.full + (rest > 0.0 ? q.base + q.slope * rest : 0.0)));
         if (!best || us < least) {
             best = &q;
             least = us;
@@ -892,12 +893,15 @@ hipError_t launch_products(Products& b, hipStream_t s) {
         n += (uint32_t)blocks_of<KIND>(b.p[i], plan.side);
     }
     b.first[b.count] = n;
-    if (plan.side == 256) hipLaunchKernelGGL((k_muon_product<256, 2, 4, 1, 32, 2, KIND>), dim3(n), dim3(512), 0, s, b);
     // (the weights' step has more to do behind its sums: eight waves, 512 x 4352 eight times 105 -> 91 us; elsewhere four are as fast or faster)
-    else if (plan.side == 128 && KIND == LAST) hipLaunchKernelGGL((k_muon_product<128, 2, 4, 1, 32, 2, KIND>), dim3(n), dim3(512), 0, s, b);
-    else if (plan.side == 128) hipLaunchKernelGGL((k_muon_product<128, 2, 2, 1, 32, 2, KIND>), dim3(n), dim3(256), 0, s, b);
-    else if (plan.per_cu == 1) hipLaunchKernelGGL((k_muon_product<64, 2, 2, 2, 64, 4, KIND>), dim3(n), dim3(512), 0, s, b);
-    else hipLaunchKernelGGL((k_muon_product<64, 2, 2, 2, 64, 2, KIND>), dim3(n), dim3(512), 0, s, b);
+    constexpr int MIDDLE_WN = KIND == LAST ? 4 : 2;
+    switch (plan.id) {
+        case LARGE: hipLaunchKernelGGL((k_muon_product<256, 2, 4, 1, 32, 2, KIND>), dim3(n), dim3(512), 0, s, b); break;
+        case MIDDLE_TWO: hipLaunchKernelGGL((k_muon_product<128, 2, MIDDLE_WN, 1, 32, 2, KIND>), dim3(n), dim3(128 * MIDDLE_WN), 0, s, b); break;
+        case MIDDLE_DEEP: hipLaunchKernelGGL((k_muon_product<128, 2, 2, 2, 64, 2, KIND>), dim3(n), dim3(512), 0, s, b); break;
+        case SMALL_DEEP: hipLaunchKernelGGL((k_muon_product<64, 2, 2, 2, 64, 4, KIND>), dim3(n), dim3(512), 0, s, b); break;
+        default: hipLaunchKernelGGL((k_muon_product<64, 2, 2, 2, 64, 2, KIND>), dim3(n), dim3(512), 0, s, b); break;
+    }
     return hipGetLastError();
 }
 
