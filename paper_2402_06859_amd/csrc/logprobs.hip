@@ -85,15 +85,17 @@ __device__ __forceinline__ int choose_groups(const uint2* groups, int n, int wan
     if (lane % 4 == 0) c.keys[tid / 4] = four;
     if (tid == 0) c.count = 0;
     __syncthreads();
-    const float k64 = c.keys[lane];
-    int rank = 0;
+    // the want-th largest of 64, its first 20 bits (what is cut off makes it no larger), bit by bit from the top: each counts the lanes that
+    // reach it. (Ranking the lanes against each other takes four times the instructions, and this part is bound by those.)
+    const uint32_t raw = __float_as_uint(c.keys[lane]), key = raw ^ ((int)raw < 0 ? 0xFFFFFFFFu : 0x80000000u);
+    uint32_t bits = 0;
 #pragma unroll
-    for (int j = 0; j < 64; ++j) {
-        const float k = lane_value(k64, j);
-        rank += k > k64 || (k == k64 && j < lane);
+    for (int j = 31; j >= 12; --j) {
+        const uint32_t next = bits | 1u << j;
+        bits = __popcll(__ballot(key >= next)) >= want ? next : bits;
     }
-    const float bar = lane_value(k64, __builtin_ctzll(__ballot(rank == want - 1)));  // (of every wave alike)
-    if (mine >= bar && mine != NEG_INF) {
+    const float bar = __uint_as_float(bits & 0x80000000u ? bits ^ 0x80000000u : ~bits);  // (of every wave alike)
+    if (!(mine < bar) && mine != NEG_INF) {  // (a bar below all is NaN)
         for (int u0 = tid; u0 < n; u0 += 256 * AHEAD) {
             uint2 g[AHEAD];
 #pragma unroll
@@ -174,42 +176,52 @@ __global__ __launch_bounds__(256) void k_choice_rows(ChoiceRows a) {
     __shared__ int cand[CANDIDATES_MAX];
     __shared__ double cand_z[CANDIDATES_MAX];
     __shared__ double best;
+    __shared__ float row_log_all;
     const int64_t m = blockIdx.x + (int64_t)blockIdx.y * gridDim.x;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     if (m >= a.rows) return;
 
-    ChoiceStat r{NEG_INF, -1.f, 0.f, 0.f};
-    for (int64_t t0 = tid; t0 < a.tiles; t0 += 1024) {
-        ChoiceStat q[4];
+    // One wave joins the tiles, unless they are very many: the others go on to the groups (this kernel is bound by its instructions, and a
+    // join has 45 of them).
+    const int joiners = a.tiles <= 1024 ? 64 : 256;
+    if (tid < joiners) {
+        ChoiceStat r{NEG_INF, -1.f, 0.f, 0.f};
+        for (int64_t t0 = tid; t0 < a.tiles; t0 += 4 * joiners) {
+            ChoiceStat q[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) q[i] = a.stat[m * a.tiles + (t0 + 256 * i < a.tiles ? t0 + 256 * i : t0)];
+            for (int i = 0; i < 4; ++i) q[i] = a.stat[m * a.tiles + (t0 + joiners * i < a.tiles ? t0 + joiners * i : t0)];
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (t0 + 256 * i < a.tiles) r = join(r, q[i]);
-    }
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) r = join(r, shuffled(r, o));
-    if (lane == 0) wave_stat[wave] = r;
-    if (tid == 0) count = 0;
-    __syncthreads();
-    r = join(join(wave_stat[0], wave_stat[1]), join(wave_stat[2], wave_stat[3]));
-    const bool none = r.max == NEG_INF && r.rest == -1.f;  // every class is masked
-    const float log_all = none ? 0.f : log1pf(r.rest), tau = none ? 0.f : r.mean / (1.f + r.rest);
-    if (tid == 0) {
-        int64_t y = -1;
-        if (a.labels) {
-            y = id_of(a.labels, a.ids64, m);
-            if (y >= a.classes) {
-                atomicOr(a.err, ERR_BIT_INDEX);
-                y = -1;
-            }
+            for (int i = 0; i < 4; ++i)
+                if (t0 + joiners * i < a.tiles) r = join(r, q[i]);
         }
-        float dy = NEG_INF;
-        if (y >= 0 && a.zlabel[m] != NEG_INF) dy = a.zlabel[m] - r.max;
-        if (a.logprob) a.logprob[m] = y >= 0 ? dy - log_all : 0.f;
-        if (a.lse) a.lse[m] = none ? NEG_INF : r.max + log_all;
-        if (a.entropy) a.entropy[m] = log_all - tau;
-        if (a.stats) a.stats[m] = make_float4(r.max, r.rest, tau, dy);
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) r = join(r, shuffled(r, o));
+        if (lane == 0) wave_stat[wave] = r;
+    }
+    if (tid == 0) count = 0;
+    if (joiners == 256) __syncthreads();
+    if (wave == 0) {
+        ChoiceStat r = wave_stat[0];
+        if (joiners == 256) r = join(join(r, wave_stat[1]), join(wave_stat[2], wave_stat[3]));
+        const bool none = r.max == NEG_INF && r.rest == -1.f;  // every class is masked
+        const float log_all = none ? 0.f : log1pf(r.rest), tau = none ? 0.f : r.mean / (1.f + r.rest);
+        if (lane == 0) {
+            int64_t y = -1;
+            if (a.labels) {
+                y = id_of(a.labels, a.ids64, m);
+                if (y >= a.classes) {
+                    atomicOr(a.err, ERR_BIT_INDEX);
+                    y = -1;
+                }
+            }
+            float dy = NEG_INF;
+            if (y >= 0 && a.zlabel[m] != NEG_INF) dy = a.zlabel[m] - r.max;
+            if (a.logprob) a.logprob[m] = y >= 0 ? dy - log_all : 0.f;
+            if (a.lse) a.lse[m] = none ? NEG_INF : r.max + log_all;
+            if (a.entropy) a.entropy[m] = log_all - tau;
+            if (a.stats) a.stats[m] = make_float4(r.max, r.rest, tau, dy);
+            row_log_all = log_all;
+        }
     }
     if (a.top == 0) return;
 
@@ -218,10 +230,11 @@ __global__ __launch_bounds__(256) void k_choice_rows(ChoiceRows a) {
     const int got = choose_groups(groups, (int)a.g.count, want, chosen);
     // the candidates: each group's largest class, and all of its classes where another may be as large as the last group's
     const float least = got == want && want < a.g.count ? chosen.key[want - 1] : NEG_INF;
-    for (int i = tid; i < got * a.g.size; i += 256) {
-        const int u = chosen.group[i / a.g.size], k = i % a.g.size, per = a.g.pitch / 4;
-        const uint32_t bound = chosen.bound[i / a.g.size];
-        const int64_t v = (int64_t)(u / per) * a.g.span + u % per * 4 + k / 4 * a.g.pitch + k % 4;
+    const int size_log = 31 - __builtin_clz(a.g.size), per_log = 29 - __builtin_clz(a.g.pitch);  // (powers of two)
+    for (int i = tid; i < got << size_log; i += 256) {
+        const int u = chosen.group[i >> size_log], k = i & (a.g.size - 1);
+        const uint32_t bound = chosen.bound[i >> size_log];
+        const int64_t v = (int64_t)(u >> per_log) * a.g.span + (u & ((1 << per_log) - 1)) * 4 + (k >> 2) * a.g.pitch + (k & 3);
         const bool all = !(__uint_as_float(bound & ~15u) < least);
         if ((all || k == (int)(bound & 15u)) && v < a.classes) cand[atomicAdd(&count, 1)] = (int)v;
     }
@@ -229,6 +242,7 @@ __global__ __launch_bounds__(256) void k_choice_rows(ChoiceRows a) {
     const int n = count;
     // their logits, four at a time in a wave
     constexpr int W = st<T>::vec, AT_ONCE = 4;
+    static_assert(AT_ONCE == 4, "the exchanges below");
     const T* const x = (const T*)a.x + m * a.dim;
     for (int c0 = wave * AT_ONCE; c0 < n; c0 += 4 * AT_ONCE) {
         const T* w[AT_ONCE];
@@ -252,17 +266,18 @@ __global__ __launch_bounds__(256) void k_choice_rows(ChoiceRows a) {
                 for (int e = 0; e < W; ++e) z[i] = fma((double)p[e], (double)q[e], z[i]);
             }
         }
+        // four sums over 64 lanes at once: every exchange halves the values that a lane goes on with
+        const bool high = lane & 32, odd = lane & 16;
+        double y0 = (high ? z[2] : z[0]) + __shfl_xor(high ? z[0] : z[2], 32);
+        const double y1 = (high ? z[3] : z[1]) + __shfl_xor(high ? z[1] : z[3], 32);
+        y0 = (odd ? y1 : y0) + __shfl_xor(odd ? y0 : y1, 16);
 #pragma unroll
-        for (int o = 32; o > 0; o >>= 1)
-#pragma unroll
-            for (int i = 0; i < AT_ONCE; ++i) z[i] += __shfl_xor(z[i], o);
-        if (lane < AT_ONCE && c0 + lane < n) {
-            double mine = z[0];
-#pragma unroll
-            for (int i = 1; i < AT_ONCE; ++i) mine = lane == i ? z[i] : mine;
-            const float off = a.offset ? a.offset[cand[c0 + lane]] : 0.f;
-            mine = off == NEG_INF ? -__builtin_huge_val() : mine * (double)a.logit_scale + (double)off;
-            cand_z[c0 + lane] = mine == mine ? mine : -__builtin_huge_val();
+        for (int o = 8; o > 0; o >>= 1) y0 += __shfl_xor(y0, o);
+        const int at = c0 + (lane >> 4);  // (lanes from 16 i on have the sum of candidate i)
+        if ((lane & 15) == 0 && at < n) {
+            const float off = a.offset ? a.offset[cand[at]] : 0.f;
+            const double v = off == NEG_INF ? -__builtin_huge_val() : y0 * (double)a.logit_scale + (double)off;
+            cand_z[at] = v == v ? v : -__builtin_huge_val();
         }
     }
     __syncthreads();
@@ -279,6 +294,7 @@ __global__ __launch_bounds__(256) void k_choice_rows(ChoiceRows a) {
         if (ranks[i] == 0) best = cand_z[c];
     }
     __syncthreads();
+    const float log_all = row_log_all;
     auto put = [&](int k, int64_t id, float v) {
         if (a.ids64) ((int64_t*)a.top_ids)[m * a.top + k] = id;
         else ((int32_t*)a.top_ids)[m * a.top + k] = (int32_t)id;

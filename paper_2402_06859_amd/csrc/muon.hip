@@ -857,8 +857,8 @@ struct Plan {
 };
 constexpr Plan PLANS[] = {{SMALL_TWO, 64, 512, 1.1, 0.72, 0.38},  // 64 KiB of LDS: two blocks a CU
                           {SMALL_DEEP, 64, 256, 0.65, 0.38, 0.22},  // a ring of four stages, one block a CU
-                          {MIDDLE_TWO, 128, 512, 2.8, 1.4, 1.4},
-                          {MIDDLE_DEEP, 128, 256, 1.45, 1.1, 0.4},  // stages of 64, eight waves in two groups along K
+                          {MIDDLE_TWO, 128, 512, 2.7, 1.4, 1.3},
+                          {MIDDLE_DEEP, 128, 256, 1.5, 1.1, 0.4},  // stages of 64, eight waves in two groups along K
                           {LARGE, 256, 256, 5.2, 3.4, 1.6}};
 
 template <int KIND>
