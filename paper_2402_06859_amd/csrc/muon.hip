@@ -316,6 +316,7 @@ struct Products {
     float pa, pb, pc;        // POLY: pa I + pb aux + pc sum, aux as it is held
     float scale2, out2;      // of the products from `second` on
     int second;
+    int from;                // quarters: blocks of twice the side in front of this launch's, which are all cut in four; else -1
     Destination d[PER_LAUNCH];
     MuonScalars s;
 };
@@ -332,7 +333,7 @@ __device__ __forceinline__ void lds_barrier() {
 // global-to-LDS loads. One barrier a stage, before its last substep's multiplies, whose fragments are then in registers: behind it the
 // slot just read is filled again and the next stage's first fragments are read, every read and load between two multiplies.
 template <int BM, int WM, int WN, int KW, bool AKS, bool BKS, int KB, int ST, bool SYM, int EPI>
-__device__ __forceinline__ void product_block(const Products& b, int i, int t, bf16_t* smem) {
+__device__ __forceinline__ void product_block(const Products& b, int i, int t, int quarter, bf16_t* smem) {
     constexpr int NW = WM * WN * KW, THREADS = 64 * NW, NI = BM * KB / (512 * NW), LOADS = 4 * NI;
     constexpr int TM = BM / WM / 32, TN = BM / WN / 32, NS = KB / 16 / KW, CH = 64, CP = BM + 4;
     constexpr int EO = BM * KB, STAGE = 4 * EO;  // a stage: A hi, A lo, B hi, B lo
@@ -344,14 +345,15 @@ __device__ __forceinline__ void product_block(const Products& b, int i, int t, b
     const int wm = wave / WN % WM, wn = wave % WN;
     const Product p = b.p[i];  // (a copy: the loads' asm would have the arguments read again in every step)
     // Groups of GROUP tile rows, walked column by column: the blocks that run together on an XCD share their panels in its L2.
-    constexpr int GROUP = BM == 256 ? 4 : 8;
-    const int tiles_m = (p.M + BM - 1) / BM, tiles_n = (p.N + BM - 1) / BM;
+    const bool quarters = BM == 128 && quarter >= 0;
+    const int GROUP = BM == 256 || quarters ? 4 : 8, side = quarters ? 2 * BM : BM;
+    const int tiles_m = (p.M + side - 1) / side, tiles_n = (p.N + side - 1) / side;
     int tm, tn;
     if constexpr (SYM) {
         // on and under the diagonal: in front of group g lie GROUP^2 g (g - 1) / 2 + g GROUP (GROUP + 1) / 2 tiles; it has
         // GROUP g whole columns, then a triangle
-        auto before = [](int g) { return GROUP * GROUP * (g * (g - 1) / 2) + g * (GROUP * (GROUP + 1) / 2); };
-        int g = (int)(sqrtf(2.f * (float)t) * (1.f / GROUP));
+        auto before = [&](int g) { return GROUP * GROUP * (g * (g - 1) / 2) + g * (GROUP * (GROUP + 1) / 2); };
+        int g = (int)(sqrtf(2.f * (float)t) / (float)GROUP);
         while (before(g) > t) --g;
         while (before(g + 1) <= t) ++g;
         const int rows = tiles_m - g * GROUP < GROUP ? tiles_m - g * GROUP : GROUP, r = t - before(g), whole = rows * g * GROUP;
@@ -369,6 +371,11 @@ __device__ __forceinline__ void product_block(const Products& b, int i, int t, b
         const int rows = tiles_m - g * GROUP < GROUP ? tiles_m - g * GROUP : GROUP;
         tn = r / rows;
         tm = g * GROUP + r - tn * rows;
+    }
+    if (quarters) {
+        tm = 2 * tm + (quarter >> 1);
+        tn = 2 * tn + (quarter & 1);
+        if ((SYM && tn > tm) || tm * BM >= p.M || tn * BM >= p.N) return;
     }
     const int64_t m0 = (int64_t)tm * BM, n0 = (int64_t)tn * BM;
 
@@ -573,17 +580,21 @@ enum { SQUARE = 0, QUARTIC = 1, OF_X = 2, NEXT = 3, LAST = 4 };
 template <int BM, int WM, int WN, int KW, int KB, int ST, int KIND>
 __global__ __launch_bounds__(64 * WM * WN * KW) void k_muon_product(Products b) {
     __shared__ __attribute__((aligned(1024))) bf16_t smem[ST * 4 * BM * KB];
-    const int block = xcd_remap(blockIdx.x, gridDim.x);
+    int block = xcd_remap(blockIdx.x, gridDim.x), quarter = -1;
+    if (BM == 128 && b.from >= 0) {
+        quarter = block & 3;
+        block = b.from + (block >> 2);
+    }
     const int i = entry_of(b.first, b.count, (uint32_t)block), t = block - (int)b.first[i];
-    if constexpr (KIND == SQUARE) product_block<BM, WM, WN, KW, false, false, KB, ST, true, PAIR>(b, i, t, smem);
-    else if constexpr (KIND == QUARTIC) product_block<BM, WM, WN, KW, false, false, KB, ST, true, POLY>(b, i, t, smem);
+    if constexpr (KIND == SQUARE) product_block<BM, WM, WN, KW, false, false, KB, ST, true, PAIR>(b, i, t, quarter, smem);
+    else if constexpr (KIND == QUARTIC) product_block<BM, WM, WN, KW, false, false, KB, ST, true, POLY>(b, i, t, quarter, smem);
     else if constexpr (KIND == OF_X) {
-        if (b.p[i].tall) product_block<BM, WM, WN, KW, true, true, KB, ST, true, PAIR>(b, i, t, smem);
-        else product_block<BM, WM, WN, KW, false, false, KB, ST, true, PAIR>(b, i, t, smem);
+        if (b.p[i].tall) product_block<BM, WM, WN, KW, true, true, KB, ST, true, PAIR>(b, i, t, quarter, smem);
+        else product_block<BM, WM, WN, KW, false, false, KB, ST, true, PAIR>(b, i, t, quarter, smem);
     } else {
         constexpr int EPI = KIND == LAST ? STEP : PAIR;
-        if (b.p[i].tall) product_block<BM, WM, WN, KW, false, false, KB, ST, false, EPI>(b, i, t, smem);
-        else product_block<BM, WM, WN, KW, false, true, KB, ST, false, EPI>(b, i, t, smem);
+        if (b.p[i].tall) product_block<BM, WM, WN, KW, false, false, KB, ST, false, EPI>(b, i, t, quarter, smem);
+        else product_block<BM, WM, WN, KW, false, true, KB, ST, false, EPI>(b, i, t, quarter, smem);
     }
 }
 
@@ -847,52 +858,39 @@ int64_t blocks_of(const Product& p, int side) {
 }
 
 // How a launch's products are cut: whichever is through first. `slots` blocks run at once; a K step of 64 takes them `full` us where
-// all slots are taken, and base + slope * their share where fewer are (measured with 2048^2, six of 1000^2, two of 2086 x 5534, 4096^2, and the models
-// of 512 x 4352 and 768 x 1856; in the order below, us of a squaring: 2048^2 57 / 54 / 57 / 47 / 118; six of 1000^2 42 / 46 / 40 / 33 / 75; 4096^2
-// 275 / 284 / 285 / 252 / 250; and of the apply of 4096^2 521 / 604 / 361 / 381 / 313).
+// all slots are taken, and base + slope * their share where fewer are. Fitted to times of all five plans, and of the large one with a tail, for each kind
+// of product of twenty lists, 12 of 160 x 640 up to those of two layers of 4096 x 10624: the plans chosen make a list's step 0.7% slower than the best ones would on average, 3% at worst.
+// (us of a squaring, in the order below: 2048^2 54 / 53 / 57 / 45 / 114; six of 1000^2 35 / 41 / 37 / 29 / 68; 4096^2 259 / 261 / 266 / 234 / 216, two of
+// them 524 / 571 / 472 / 449 / 552 and 419 with a tail; and of the product with X of 4096^2 503 / 586 / 350 / 366 / 299.)
 enum { SMALL_TWO, SMALL_DEEP, MIDDLE_TWO, MIDDLE_DEEP, LARGE };
 struct Plan {
     int id, side, slots;
     double full, base, slope;
 };
-constexpr Plan PLANS[] = {{SMALL_TWO, 64, 512, 1.1, 0.72, 0.38},  // 64 KiB of LDS: two blocks a CU
-                          {SMALL_DEEP, 64, 256, 0.65, 0.38, 0.22},  // a ring of four stages, one block a CU
-                          {MIDDLE_TWO, 128, 512, 2.7, 1.4, 1.3},
-                          {MIDDLE_DEEP, 128, 256, 1.5, 1.1, 0.4},  // stages of 64, eight waves in two groups along K
-                          {LARGE, 256, 256, 5.2, 3.4, 1.6}};
+constexpr Plan PLANS[] = {{SMALL_TWO, 64, 512, 0.96, 0.52, 0.38},  // 64 KiB of LDS: two blocks a CU
+                          {SMALL_DEEP, 64, 256, 0.52, 0.42, 0.02},  // a ring of four stages, one block a CU
+                          {MIDDLE_TWO, 128, 512, 2.87, 1.32, 1.33},
+                          {MIDDLE_DEEP, 128, 256, 1.54, 0.92, 0.61},  // stages of 64, eight waves in two groups along K
+                          {LARGE, 256, 256, 4.59, 2.7, 1.82}};
+constexpr double TAIL = 24.0;  // us, for a second launch
 
-template <int KIND>
-const Plan& plan_of(const Products& b) {
-    const Plan* best = nullptr;
-    double least = 0.0;
-    for (const Plan& q : PLANS) {
-        double blocks = 0.0, steps = 0.0, longest = 0.0;
-        for (int i = 0; i < b.count; ++i) {
-            const double n = (double)blocks_of<KIND>(b.p[i], q.side), k = b.p[i].K / 64.0;
-            blocks += n;
-            steps += n * k;
-            longest = std::max(longest, k);
-        }
-        const double rounds = std::floor(blocks / q.slots), rest = blocks / q.slots - rounds;
-        const double us = std::max(longest * q.base, steps / blocks * (rounds * q.full + (rest > 0.0 ? q.base + q.slope * rest : 0.0)));
-        if (!best || us < least) {
-            best = &q;
-            least = us;
-        }
+struct Share {  // blocks of a plan's side, and their K steps of 64
+    double blocks = 0.0, steps = 0.0, longest = 0.0;
+    void add(double n, double k) {
+        blocks += n;
+        steps += n * k;
+        if (n > 0.0) longest = std::max(longest, k);
     }
-    return *best;
+};
+double time_of(const Plan& q, const Share& x) {
+    if (x.blocks == 0.0) return 0.0;
+    const double rounds = std::floor(x.blocks / q.slots), rest = x.blocks / q.slots - rounds;
+    return std::max(x.longest * (q.base + q.slope * std::min(1.0, x.blocks / q.slots)),  // (beside others, short ones too)
+                    x.steps / x.blocks * (rounds * q.full + (rest > 0.0 ? q.base + q.slope * rest : 0.0)));
 }
 
 template <int KIND>
-hipError_t launch_products(Products& b, hipStream_t s) {
-    if (b.count == 0) return hipSuccess;
-    const Plan& plan = plan_of<KIND>(b);
-    uint32_t n = 0;
-    for (int i = 0; i < b.count; ++i) {
-        b.first[i] = n;
-        n += (uint32_t)blocks_of<KIND>(b.p[i], plan.side);
-    }
-    b.first[b.count] = n;
+hipError_t launch_blocks(const Plan& plan, Products& b, uint32_t n, hipStream_t s) {
     // (the weights' step has more to do behind its sums: eight waves, 512 x 4352 eight times 105 -> 91 us; elsewhere four are as fast or faster)
     constexpr int MIDDLE_WN = KIND == LAST ? 4 : 2;
     switch (plan.id) {
@@ -903,6 +901,58 @@ hipError_t launch_products(Products& b, hipStream_t s) {
         default: hipLaunchKernelGGL((k_muon_product<64, 2, 2, 2, 64, 2, KIND>), dim3(n), dim3(512), 0, s, b); break;
     }
     return hipGetLastError();
+}
+
+template <int KIND>
+hipError_t launch_products(Products& b, hipStream_t s) {
+    if (b.count == 0) return hipSuccess;
+    const Plan* head = nullptr;
+    const Plan* tail = nullptr;
+    double least = 0.0;
+    for (const Plan& q : PLANS) {
+        Share x;
+        for (int i = 0; i < b.count; ++i) x.add((double)blocks_of<KIND>(b.p[i], q.side), b.p[i].K / 64.0);
+        const double us = time_of(q, x);
+        if (!head || us < least) {
+            head = &q;
+            least = us;
+        }
+    }
+    // Whole rounds of the largest blocks, which take the fewest loads, and what is left of them in a launch of its own, in quarters, so that the
+    // last round is not one of a few blocks (two of 4096 x 10624 and two of 2048 x 10624: 344 blocks on 256 CUs, 552 -> 474 us a squaring, the step 15.8 -> 14.2 ms)
+    const Plan& large = PLANS[LARGE];
+    int64_t blocks = 0;
+    for (int i = 0; i < b.count; ++i) blocks += blocks_of<KIND>(b.p[i], large.side);
+    const int64_t whole = blocks / large.slots * large.slots;
+    if (whole > 0 && whole < blocks) {
+        Share x, y;
+        int64_t free = whole;
+        for (int i = 0; i < b.count; ++i) {
+            const int64_t n = blocks_of<KIND>(b.p[i], large.side), m = std::min(n, free);
+            free -= m;
+            x.add((double)m, b.p[i].K / 64.0);
+            y.add(4.0 * (double)(n - m), b.p[i].K / 64.0);
+        }
+        for (int id : {MIDDLE_TWO, MIDDLE_DEEP}) {
+            const double us = time_of(large, x) + time_of(PLANS[id], y) + TAIL;
+            if (us < least) {
+                head = &large;
+                tail = &PLANS[id];
+                least = us;
+            }
+        }
+    }
+    uint32_t n = 0;
+    for (int i = 0; i < b.count; ++i) {
+        b.first[i] = n;
+        n += (uint32_t)blocks_of<KIND>(b.p[i], head->side);
+    }
+    b.first[b.count] = n;
+    b.from = -1;
+    hipError_t e = launch_blocks<KIND>(*head, b, tail ? (uint32_t)whole : n, s);
+    if (e != hipSuccess || !tail) return e;
+    b.from = (int)whole;
+    return launch_blocks<KIND>(*tail, b, 4 * (n - (uint32_t)whole), s);
 }
 
 }  // namespace

@@ -110,6 +110,20 @@ def test_update_matches_definition(rows, cols):
         held(t["param"], newton_schulz(u))
 
 
+@pytest.mark.parametrize("shapes", [[(5701, 5733)], [(5733, 5701)], [(4100, 4300), (4500, 4100)]])
+def test_more_than_a_round_of_large_blocks(shapes):
+    """Whole rounds of 256 x 256 blocks, and what is left of the last matrix in quarters, some of which lie behind its end."""
+    need_gpu()
+    lib = handle()
+    ts = [only_update(matrix(r, c, i, falling=False)) for i, (r, c) in enumerate(shapes)]
+    us = [momentum_of(t, 0.95, True) for t in ts]
+    step(lib, ts)
+    torch.cuda.synchronize()
+    for t, (m, u) in zip(ts, us):
+        assert torch.equal(t["m"], m)
+        held(t["param"], newton_schulz(u))
+
+
 @pytest.mark.parametrize("steps", [1, 2, 3, 4, 6, 8])
 def test_other_numbers_of_steps(steps):
     need_gpu()
