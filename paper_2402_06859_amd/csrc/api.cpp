@@ -1637,7 +1637,8 @@ rdcn_status rdcn_logprobs_grad(rdcn_handle* h, int64_t rows, int64_t dim, int64_
     p.x = x; p.kept = sc + S.kept; p.copies = (int)S.copies;
     p.row = row; p.err = h->err;
     char* const lo = S.copies > 1 ? G + (size_t)rows * S.ld * e : nullptr;
-    {
+    const bool prepared = !kept || rows * S.kept_ld > (int64_t)1 << 26;  // (see k_choice_normalize)
+    if (prepared) {
         ProfScope ps(h, RDCN_KERNEL_HEAD_OUT_BWD, s);
         RDCN_TRY(launch_choice_prepare(p, h->bf16, s));
     }
@@ -1646,12 +1647,11 @@ rdcn_status rdcn_logprobs_grad(rdcn_handle* h, int64_t rows, int64_t dim, int64_
         const void* const wp = (const char*)w + (size_t)v * dim * e;
         if (kept) {
             ChoiceNormalize q{};
-            q.rows = rows; q.tiles = S.tiles; q.tile = S.tile;
+            q.p = p; q.prepared = prepared;
+            q.tiles = S.tiles; q.tile = S.tile;
             q.first = v; q.width = v + n == classes ? S.kept_ld - v : n;
             q.ld = S.ld; q.kept_ld = S.kept_ld;
             q.stat = (const ChoiceStat*)((const char*)kept + S.kept_stat);
-            q.row = row;
-            q.labels = labels; q.ids64 = h->ids64;
             q.kept = kept; q.out = G; q.out_lo = lo;
             ProfScope ps(h, RDCN_KERNEL_HEAD_OUT_BWD, s);
             RDCN_TRY(launch_choice_normalize(q, h->bf16, s));

@@ -52,13 +52,13 @@ struct ChoicePrepare {
 hipError_t launch_choice_prepare(const ChoicePrepare& a, bool bf16, hipStream_t s);
 
 // out [rows][ld], `width` columns (whole vectors) of classes from `first` on: the gradient in the logits, from kept [rows][kept_ld]
-// (f16 times SOFT_E_SCALE, or float) and the tiles' maxima.
+// (f16 times SOFT_E_SCALE, or float) and the tiles' maxima; without `prepared` (k_choice_prepare ran for p) the
+// first classes' launch makes p's copies of x too, and p.row is not used.
 struct ChoiceNormalize {
-    int64_t rows, tiles, tile, first, width, ld, kept_ld;
+    ChoicePrepare p;
+    bool prepared;
+    int64_t tiles, tile, first, width, ld, kept_ld;
     const ChoiceStat* stat;
-    const ChoiceRow* row;
-    const void* labels;
-    bool ids64;
     const void* kept;
     void* out;
     void* out_lo;  // or NULL; bf16: what rounding leaves of out

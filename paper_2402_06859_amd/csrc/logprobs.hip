@@ -320,6 +320,23 @@ __device__ __forceinline__ bool upstream(const ChoicePrepare& a, int64_t m, int6
     return g != 0.f || h != 0.f;
 }
 
+__device__ __forceinline__ ChoiceRow choice_row(const ChoicePrepare& a, int64_t m, bool any, int64_t y, float g, float h) {
+    ChoiceRow r{};
+    const float4 q = a.stats[m];  // max, rest, tau, label's d
+    r.max = q.x;
+    if (any && !(q.x == NEG_INF && q.y == -1.f)) {
+        const float all = 1.f + q.y, inv = a.logit_scale / all;
+        r.a = -inv * (g - h * q.z);
+        r.b = -inv * h;
+        if (y >= 0 && q.w != NEG_INF) {
+            // 1 - p: the largest class's own share is left out of rest, another's is in it
+            const float e = expf(q.w), others = q.w == 0.f ? q.y : q.y + (1.f - e);
+            r.label = a.logit_scale * (g * (others / all) - h * (e / all) * (q.w - q.z));
+        }
+    }
+    return r;
+}
+
 template <typename T>
 __global__ __launch_bounds__(256) void k_choice_prepare(ChoicePrepare a) {
     constexpr int W = st<T>::vec;
@@ -327,22 +344,9 @@ __global__ __launch_bounds__(256) void k_choice_prepare(ChoicePrepare a) {
     int64_t y;
     float g, h;
     for (int64_t m = t; m < a.rows; m += step) {
-        ChoiceRow r{};
         const bool any = upstream(a, m, y, g, h);
         if (y >= a.classes) atomicOr(a.err, ERR_BIT_INDEX);
-        const float4 q = a.stats[m];  // max, rest, tau, label's d
-        r.max = q.x;
-        if (any && !(q.x == NEG_INF && q.y == -1.f)) {
-            const float all = 1.f + q.y, inv = a.logit_scale / all;
-            r.a = -inv * (g - h * q.z);
-            r.b = -inv * h;
-            if (y >= 0 && q.w != NEG_INF) {
-                // 1 - p: the largest class's own share is left out of rest, another's is in it
-                const float e = expf(q.w), others = q.w == 0.f ? q.y : q.y + (1.f - e);
-                r.label = a.logit_scale * (g * (others / all) - h * (e / all) * (q.w - q.z));
-            }
-        }
-        a.row[m] = r;
+        a.row[m] = choice_row(a, m, any, y, g, h);
     }
     for (int64_t i = t; i < n; i += step) {
         u32x4_t v = {0u, 0u, 0u, 0u};
@@ -352,16 +356,28 @@ __global__ __launch_bounds__(256) void k_choice_prepare(ChoicePrepare a) {
 }
 
 // Columns first .. of row m of the gradient in the logits, from the exponentials that the forward kept: p = e exp(tile's
-// maximum - row's) / (1 + rest), and d from e's logarithm. Reads and writes each element once (2 + 2 bytes, 4 + 4 in float).
+// maximum - row's) / (1 + rest), and d from e's logarithm. Reads and writes each element once (2 + 2 bytes, 4 + 4 in float). Where
+// little is to be written, no k_choice_prepare runs in front: every thread computes its row's factors, and the first piece's workgroups copy x on
+// the way (333 x 1001, dim 136: 3.5 + 4.1 us in two launches, 5.1 in one; 4096 x 32000: 101 and 104; 8192 x 131072: 816 and 869).
 template <typename T>
 __global__ __launch_bounds__(256) void k_choice_normalize(ChoiceNormalize a) {
     constexpr int W = st<T>::vec;
     constexpr float UNIT = sizeof(T) == 2 ? 1.f / SOFT_E_SCALE : 1.f, LN2 = 0.693147181f;
     const int64_t m = blockIdx.y + (int64_t)blockIdx.z * 65535;
-    if (m >= a.rows) return;
-    const ChoiceRow r = a.row[m];
+    if (m >= a.p.rows) return;
+    int64_t y;
+    float g, h;
+    const bool any = upstream(a.p, m, y, g, h);
+    if (!a.prepared && a.first == 0) {
+        if (y >= a.p.classes && blockIdx.x == 0 && threadIdx.x == 0) atomicOr(a.p.err, ERR_BIT_INDEX);
+        for (int64_t i = (blockIdx.x * 256ll + threadIdx.x) * W; i < a.p.dim; i += gridDim.x * 256ll * W) {
+            u32x4_t v = {0u, 0u, 0u, 0u};
+            if (any) v = *(const u32x4_t*)((const T*)a.p.x + m * a.p.dim + i);
+            for (int k = 0; k < a.p.copies; ++k) *(u32x4_t*)((T*)a.p.kept + (k * a.p.rows + m) * a.p.dim + i) = v;
+        }
+    }
+    const ChoiceRow r = a.prepared ? a.p.row[m] : choice_row(a.p, m, any, y, g, h);
     const bool none = r.a == 0.f && r.b == 0.f;
-    const int64_t y = a.labels ? id_of(a.labels, a.ids64, m) : -1;
     for (int64_t n = (blockIdx.x * 256ll + threadIdx.x) * W; n < a.width; n += gridDim.x * 256ll * W) {
         const int64_t v = a.first + n;  // the class
         const float top = a.stat[m * a.tiles + v / a.tile].max;
@@ -391,9 +407,9 @@ __global__ __launch_bounds__(256) void k_choice_normalize(ChoiceNormalize a) {
 }  // namespace
 
 hipError_t launch_choice_normalize(const ChoiceNormalize& a, bool bf16, hipStream_t s) {
-    if (a.rows == 0 || a.width == 0) return hipSuccess;
-    const int64_t per = (a.width / (bf16 ? 8 : 4) + 1023) / 1024, y = a.rows < 65535 ? a.rows : 65535;  // four vectors a thread
-    const dim3 grid((unsigned)(per > 64 ? 64 : per), (unsigned)y, (unsigned)((a.rows + 65534) / 65535));
+    if (a.p.rows == 0 || a.width == 0) return hipSuccess;
+    const int64_t per = (a.width / (bf16 ? 8 : 4) + 1023) / 1024, y = a.p.rows < 65535 ? a.p.rows : 65535;  // four vectors a thread
+    const dim3 grid((unsigned)(per > 64 ? 64 : per), (unsigned)y, (unsigned)((a.p.rows + 65534) / 65535));
     if (bf16) hipLaunchKernelGGL(k_choice_normalize<bf16_t>, grid, dim3(256), 0, s, a);
     else hipLaunchKernelGGL(k_choice_normalize<float>, grid, dim3(256), 0, s, a);
     return hipGetLastError();

@@ -337,6 +337,20 @@ def test_less_scratch_means_pieces_of_the_classes(dtype, rows, dim, classes):
         check(lib, c, rows, dim, classes, dtype == "f32", size=size)
 
 
+@pytest.mark.parametrize("dtype,rows,dim", [("bf16", 2100, 64), ("f32", 2100, 24)])
+def test_gradient_where_the_rows_have_a_launch_of_their_own(dtype, rows, dim):
+    """More than 2^26 kept exponentials, whole and in pieces, with a label that is out of range."""
+    need_gpu()
+    classes = 32003
+    lib = handle(dtype)
+    c = upstream(make(dtype, rows, dim, classes, 23, ignored=0.1, masked=0.1), rows, 7)
+    c["y"][5] = classes + 3
+    most, least = lib.logprobs_workspace(rows, dim, classes, 0)[2:]
+    for size in (most, (most + least) // 2 // 256 * 256):
+        check(lib, c, rows, dim, classes, dtype == "f32", size=size)
+        assert lib.check_device_errors() == rdcn.RDCN_ERR_INDEX
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_no_rows(dtype):
     need_gpu()
