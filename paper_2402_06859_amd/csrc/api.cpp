@@ -398,6 +398,16 @@ GemmPlan plan_logits(const rdcn_handle* h, int64_t rows, int64_t classes, int64_
     return p;
 }
 
+// The same where log probabilities are made of the logits. Up to 16 rows, more classes than one round of streamed blocks covers: the product is
+// the read of w, and streamed 16 x 64 blocks have all of a 512-wide block's loads on their way at once, two blocks a CU. us, 128 x 128 (or 64 x 64)
+// blocks / streamed: 1 x 100003 classes x 1856 81 / 64 (5.8 TB/s), 16 rows 80 / 68; 1 x 50000 x 512 18.2 / 16.9, 16 rows 18.1 / 17.2; 16 x 20000 x 1000 17.2 /
+// 16.3; 1 x 30000 x 160 7.0 / 6.5; 8 x 131072 x 4352 197 / 187. Blocks of 32 rows: 16 x 100003 x 1856 73, but 16 x 50000 x 512 20.
+GemmPlan plan_choice(const rdcn_handle* h, int64_t rows, int64_t classes, int64_t dim) {
+    const GemmPlan p = plan_logits(h, rows, classes, dim);
+    const GemmPlan few = plan_few_rows();
+    return h->bf16 && rows <= 16 && !gemm_streams(rows, classes, dim, p) && gemm_fits_grid(rows, classes, few, true) ? few : p;
+}
+
 // The layout for G in pieces of `piece` classes, or whole.
 SoftPlan soft_layout(const rdcn_handle* h, int64_t rows, int64_t dim, int64_t classes, bool whole, int64_t piece) {
     SoftPlan s{};
@@ -616,7 +626,7 @@ ChoicePlan choice_layout(const rdcn_handle* h, int64_t rows, int64_t dim, int64_
     ChoicePlan s{};
     const size_t e = eb(h);
     const int64_t vec = h->bf16 ? 8 : 4;
-    const GemmPlan p = plan_logits(h, rows, classes, dim);
+    const GemmPlan p = plan_choice(h, rows, classes, dim);
     int tile = 0;
     s.tiles = rows > 0 ? gemm_soft_tiles(rows, classes, dim, p, h->bf16, &tile) : 0;
     if (rows > 0) s.g = gemm_choice_groups(rows, classes, dim, p, h->bf16);
@@ -1594,7 +1604,7 @@ rdcn_status rdcn_logprobs_forward(rdcn_handle* h, int64_t rows, int64_t dim, int
     g.ngroups = S.g.count;
     {
         ProfScope ps(h, RDCN_KERNEL_HEAD_FWD_GEMM, s);
-        RDCN_TRY(launch_gemm(g, plan_logits(h, rows, classes, dim), h->bf16, s));
+        RDCN_TRY(launch_gemm(g, plan_choice(h, rows, classes, dim), h->bf16, s));
     }
     ChoiceRows r{};
     r.rows = rows; r.dim = dim; r.classes = classes; r.tiles = S.tiles;
@@ -1666,7 +1676,7 @@ rdcn_status rdcn_logprobs_grad(rdcn_handle* h, int64_t rows, int64_t dim, int64_
             g.choicerow = row;
             g.c = G; g.c2 = lo; g.ldc = S.ld;
             ProfScope ps(h, RDCN_KERNEL_HEAD_FWD_GEMM, s);
-            RDCN_TRY(launch_gemm(g, plan_logits(h, rows, n, dim), h->bf16, s));
+            RDCN_TRY(launch_gemm(g, plan_choice(h, rows, n, dim), h->bf16, s));
         }
         GemmArgs gx{};
         gx.M = S.copies * rows; gx.N = dim; gx.K = n;

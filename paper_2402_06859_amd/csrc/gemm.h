@@ -147,6 +147,17 @@ inline GemmPlan plan_f32_lds() {
     p.stages = F32_LDS_STAGES;
     return p;
 }
+// Logits of up to 16 rows (EPI_CHOICE_*): streamed 16 x 64 blocks, however many.
+constexpr int FEW_ROWS_STAGES = 104;  // marks such a plan
+inline GemmPlan plan_few_rows() {
+    GemmPlan p;
+    p.bm = 16;
+    p.bn = 64;
+    p.stages = FEW_ROWS_STAGES;
+    return p;
+}
+// Whether launch_gemm takes streamed blocks for a product of two K-contiguous operands under plan p.
+bool gemm_streams(int64_t M, int64_t N, int64_t K, const GemmPlan& p);
 // Whether a product's grid is one that can be launched: less than 2^32 threads along x.
 bool gemm_fits_grid(int64_t M, int64_t N, const GemmPlan& p, bool bf16);
 // plan_gemm (K may be split) for one long product at a time on the whole chip, whose partial sums the caller reduces.

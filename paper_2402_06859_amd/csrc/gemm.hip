@@ -429,7 +429,14 @@ __device__ __forceinline__ void choice_epilogue8(const GemmArgs& g, int64_t m, i
 #pragma unroll
     for (int e = 0; e < 8; ++e)
         if (lab == e) g.zlabel[m] = v[e];
-    if (in && g.groups) g.groups[m * g.ngroups + n / 8] = choice_group<8>([&](int i) { return v[i]; });
+    if (g.groups) {
+        if constexpr (LANES == 8) {  // groups of 16: half as many for k_choice_rows to go through
+            float w[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) w[e] = __shfl_xor(v[e], 1);
+            if (in && n % 16 == 0) g.groups[m * g.ngroups + n / 16] = choice_group<16>([&](int i) { return i < 8 ? v[i] : w[i - 8]; });
+        } else if (in) g.groups[m * g.ngroups + n / 8] = choice_group<8>([&](int i) { return v[i]; });
+    }
     float mx = v[0];
 #pragma unroll
     for (int e = 1; e < 8; ++e) mx = fmaxf(mx, v[e]);
@@ -1850,7 +1857,7 @@ GemmPlan plan_gemm_long(int64_t M, int64_t N, int64_t K, bool bf16) {
 
 bool gemm_fits_grid(int64_t M, int64_t N, const GemmPlan& p, bool bf16) {
     // (launch_gemm's workgroups; the streamed blocks' are 256 at most)
-    const int64_t threads = bf16 && p.bm == 256 ? 512 : 256;
+    const int64_t threads = bf16 && (p.bm == 256 || p.stages == FEW_ROWS_STAGES) ? 512 : 256;
     return ((M + p.bm - 1) / p.bm) * ((N + p.bn - 1) / p.bn) * threads < (int64_t)1 << 32;
 }
 
@@ -1882,6 +1889,8 @@ int stream_block(int64_t M, int64_t N, int64_t K, const GemmPlan& p) {
 
 }  // namespace
 
+bool gemm_streams(int64_t M, int64_t N, int64_t K, const GemmPlan& p) { return stream_block(M, N, K, p) != 0; }
+
 int64_t gemm_soft_tiles(int64_t M, int64_t N, int64_t K, const GemmPlan& p, bool bf16, int* columns) {
     const int st = bf16 ? stream_block(M, N, K, p) : 0;
     // (a streamed block's columns, or those of one wave)
@@ -1891,7 +1900,8 @@ int64_t gemm_soft_tiles(int64_t M, int64_t N, int64_t K, const GemmPlan& p, bool
 
 ChoiceGroups gemm_choice_groups(int64_t M, int64_t N, int64_t K, const GemmPlan& p, bool bf16) {
     ChoiceGroups c;
-    if (bf16 && stream_block(M, N, K, p)) c.span = 8, c.pitch = 4, c.size = 8;
+    if (p.stages == FEW_ROWS_STAGES) c.span = 16, c.pitch = 4, c.size = 16;
+    else if (bf16 && stream_block(M, N, K, p)) c.span = 8, c.pitch = 4, c.size = 8;
     else if (p.bm == 256 || (p.bm == 128 && p.stages == 3)) c.span = 32, c.pitch = 8, c.size = 16;  // 32 x 32 tiles
     else if (p.bm == 128) c.span = 64, c.pitch = 16, c.size = 16;
     else c.span = 32, c.pitch = 16, c.size = 8;
@@ -1908,6 +1918,12 @@ hipError_t launch_gemm(const GemmArgs& g, const GemmPlan& p, bool bf16, hipStrea
     }
     GemmArgs ga = g;
     ga.group_m = p.group_m;
+    if (p.stages == FEW_ROWS_STAGES) {
+        if (g.a_kstrided || g.b_kstrided || g.ops_f16 || g.a2 || (g.epi != EPI_CHOICE_FWD && g.epi != EPI_CHOICE_GRAD)) return hipErrorInvalidValue;
+        const int64_t tiles = ((g.M + 15) / 16) * ((g.N + 63) / 64);
+        hipLaunchKernelGGL((k_gemm_stream<1, 4, 1, 64, bf16_t, EK_CHOICE, false>), dim3((unsigned)tiles), dim3(64 * ST_KW), 0, s, ga);
+        return hipGetLastError();
+    }
     if (!g.a_kstrided && !g.b_kstrided) {
         switch (stream_block(g.M, g.N, g.K, p)) {
             case 1: return launch_stream<1, 1, 2, 64>(ga, s);

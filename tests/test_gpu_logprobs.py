@@ -337,6 +337,22 @@ def test_less_scratch_means_pieces_of_the_classes(dtype, rows, dim, classes):
         check(lib, c, rows, dim, classes, dtype == "f32", size=size)
 
 
+@pytest.mark.parametrize("rows,dim,classes,top", [(1, 8, 8201, 3), (16, 136, 9001, 32), (13, 4352, 8209, 5), (2, 512, 50000, 8),
+                                                  (16, 1856, 20003, 8), (17, 512, 20003, 8)])
+def test_few_rows_of_many_classes(rows, dim, classes, top):
+    need_gpu()
+    print("logprobs of few rows", rows, dim, classes, flush=True)
+    lib = handle("bf16")
+    c = upstream(make("bf16", rows, dim, classes, 31 * rows, ignored=0.1, masked=0.1), rows, 8)
+    c["off"][:70] = -math.inf  # a tile without any class
+    c["y"][0] = classes - 1
+    c["off"][classes - 1] = 0.5
+    most, least = lib.logprobs_workspace(rows, dim, classes, top)[2:]
+    for size in (most, least):
+        check(lib, c, rows, dim, classes, False, top, size=size)
+    assert lib.check_device_errors() == rdcn.RDCN_OK
+
+
 @pytest.mark.parametrize("dtype,rows,dim", [("bf16", 2100, 64), ("f32", 2100, 24)])
 def test_gradient_where_the_rows_have_a_launch_of_their_own(dtype, rows, dim):
     """More than 2^26 kept exponentials, whole and in pieces, with a label that is out of range."""
