@@ -577,10 +577,11 @@ rdcn_status rdcn_logprobs_forward(rdcn_handle* h, int64_t rows, int64_t dim, int
  * The gradients of any loss in x and w, from its gradients in logprob and entropy ([rows] float, either may be NULL for 0):
  *   dL/dz[n, v] = g ([v = label] - p) - h p (log p + entropy),  g = grad_logprob[n], h = grad_entropy[n]
  *   grad_x = s dL/dz w, grad_w = s (dL/dz)^T x, both in the storage dtype and overwritten.
- * stats (and kept, or NULL) must be those of a forward with the same x, w, offset, labels and logit_scale; both stay as they are. Rows without a label (when labels are given), and rows whose
- * g and h are both 0, have no gradient and may hold anything in x and stats. Masked logits are constants. bf16 models round dL/dz
- * to bf16 for the products (half a step, 2^-8 of an element; to bf16 hi + lo, 2^-16, where rows are few or the products small) and each gradient once at the end; sums are
- * float and in a fixed order. 1 - p of a label keeps its digits where p is near 1. With grad_bytes of scratch the call is fastest; it takes any size from
+ * stats (and kept, or NULL) must be those of a forward with the same x, w, offset, labels and logit_scale; both stay as they are.
+ * Rows without a label (when labels are given), and rows whose g and h are both 0, have no gradient and may hold anything in x and
+ * stats. Masked logits are constants. bf16 models round dL/dz to bf16 for the products (half a step, 2^-8 of an element; to bf16 hi +
+ * lo, 2^-16, where rows are few or the products small) and each gradient once at the end; sums are float and in a fixed order. 1 - p
+ * of a label keeps its digits where p is near 1. With grad_bytes of scratch the call is fastest; it takes any size from
  * grad_least_bytes on, working on fewer classes at a time.
  */
 rdcn_status rdcn_logprobs_grad(rdcn_handle* h, int64_t rows, int64_t dim, int64_t classes, const void* x, const void* w,
@@ -678,7 +679,7 @@ rdcn_status rdcn_grad_norm(rdcn_handle* h, const rdcn_adamw_tensor* tensors, int
  *   X  = U / |U| (the 2-norm of its elements; 0 where that is 0),  then `steps` times
  *   X <- a X + b A X + c A A X,  A = X X^T
  *   p' = p (1 - lr weight_decay) - lr scale X
- * |U| is summed in 64 bits; the products carry 22 bits and float sums: X is within 2e-5 of its own norm (the more uneven its
+ * |U| is summed in 64 bits; the products carry 22 bits and float sums: X is within 4e-5 of its own norm (the more uneven its
  * singular values, the nearer to that), where float products leave 1e-5; the other operations are one rounding to float each. The weights
  * are as for rdcn_adamw_step: float, bf16 with a float master, or bf16 alone, rounded to nearest or (stochastic) by chance, with its bits.
  * a, b, c = 3.4445, -4.7750, 2.0315 in 5 steps take all but the smallest singular values to within 0.7 to 1.2; 2, -1.5, 0.5

@@ -404,8 +404,7 @@ GemmPlan plan_logits(const rdcn_handle* h, int64_t rows, int64_t classes, int64_
 // 16.3; 1 x 30000 x 160 7.0 / 6.5; 8 x 131072 x 4352 197 / 187. Blocks of 32 rows: 16 x 100003 x 1856 73, but 16 x 50000 x 512 20.
 GemmPlan plan_choice(const rdcn_handle* h, int64_t rows, int64_t classes, int64_t dim) {
     const GemmPlan p = plan_logits(h, rows, classes, dim);
-    const GemmPlan few = plan_few_rows();
-    return h->bf16 && rows <= 16 && !gemm_streams(rows, classes, dim, p) && gemm_fits_grid(rows, classes, few, true) ? few : p;
+    return h->bf16 && rows <= 16 && !gemm_streams(rows, classes, dim, p) ? plan_few_rows() : p;
 }
 
 // The layout for G in pieces of `piece` classes, or whole.

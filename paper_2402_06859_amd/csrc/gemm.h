@@ -147,7 +147,7 @@ inline GemmPlan plan_f32_lds() {
     p.stages = F32_LDS_STAGES;
     return p;
 }
-// Logits of up to 16 rows (EPI_CHOICE_*): streamed 16 x 64 blocks, however many.
+// Logits of up to 16 rows over at most 2^27 classes (EPI_CHOICE_*): streamed 16 x 64 blocks, 512 threads each.
 constexpr int FEW_ROWS_STAGES = 104;  // marks such a plan
 inline GemmPlan plan_few_rows() {
     GemmPlan p;

@@ -1857,7 +1857,7 @@ GemmPlan plan_gemm_long(int64_t M, int64_t N, int64_t K, bool bf16) {
 
 bool gemm_fits_grid(int64_t M, int64_t N, const GemmPlan& p, bool bf16) {
     // (launch_gemm's workgroups; the streamed blocks' are 256 at most)
-    const int64_t threads = bf16 && (p.bm == 256 || p.stages == FEW_ROWS_STAGES) ? 512 : 256;
+    const int64_t threads = bf16 && p.bm == 256 ? 512 : 256;
     return ((M + p.bm - 1) / p.bm) * ((N + p.bn - 1) / p.bn) * threads < (int64_t)1 << 32;
 }
 
