@@ -41,8 +41,22 @@ __device__ __forceinline__ ChoiceStat join(const ChoiceStat& p, const ChoiceStat
     const float t = b.max - a.max, e = expf(t), all = 1.f + b.rest;
     return ChoiceStat{a.max, fmaf(e, all, a.rest), e == 0.f ? a.mean : fmaf(e, fmaf(t, all, b.mean), a.mean), 0.f};
 }
-__device__ __forceinline__ ChoiceStat shuffled(const ChoiceStat& p, int o) {
-    return ChoiceStat{__shfl_xor(p.max, o), __shfl_xor(p.rest, o), __shfl_xor(p.mean, o), 0.f};
+// The join of a wave's: the largest maximum first, then sums of what each adds to it (a tree of joins has three times the instructions).
+__device__ __forceinline__ ChoiceStat wave_join(const ChoiceStat& p) {
+    float top = p.max;
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
+    const uint64_t at_top = __ballot(p.max == top);
+    const float t = p.max - top, e = expf(t), all = 1.f + p.rest;
+    float rest = e * all, mean = e == 0.f ? 0.f : e * fmaf(t, all, p.mean);
+    if (p.max == NEG_INF) rest = p.rest == -1.f ? 0.f : p.rest, mean = 0.f;
+    if ((int)(threadIdx.x & 63) == __ffsll((unsigned long long)at_top) - 1) rest = p.rest, mean = p.mean;  // (the one whose maximum stands for all)
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) {
+        rest += __shfl_xor(rest, o);
+        mean += __shfl_xor(mean, o);
+    }
+    return ChoiceStat{top, rest, mean, 0.f};
 }
 
 // (value, id) a ahead of b in the order of the answer: larger first, then the lower id.
@@ -67,6 +81,11 @@ struct Chosen {
     float wave_key[4];
     int count, wave_group[4];
 };
+__device__ __forceinline__ double lane_double(double x, int lane) {
+    const uint64_t b = (uint64_t)__double_as_longlong(x);
+    const uint32_t lo = __builtin_amdgcn_readlane((uint32_t)b, lane), hi = __builtin_amdgcn_readlane((uint32_t)(b >> 32), lane);
+    return __longlong_as_double((long long)((uint64_t)hi << 32 | lo));
+}
 __device__ __forceinline__ float lane_value(float x, int lane) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), lane)); }
 
 __device__ __forceinline__ int choose_groups(const uint2* groups, int n, int want, Chosen& c) {
@@ -184,6 +203,8 @@ __global__ __launch_bounds__(256) void k_choice_rows(ChoiceRows a) {
     // One wave joins the tiles, unless they are very many: the others go on to the groups (this kernel is bound by its instructions, and a
     // join has 45 of them).
     const int joiners = a.tiles <= 1024 ? 64 : 256;
+    const int64_t label = a.labels ? id_of(a.labels, a.ids64, m) : -1;
+    const float zlabel = a.labels ? a.zlabel[m] : 0.f;  // (written where the label is in range)
     if (tid < joiners) {
         ChoiceStat r{NEG_INF, -1.f, 0.f, 0.f};
         for (int64_t t0 = tid; t0 < a.tiles; t0 += 4 * joiners) {
@@ -194,8 +215,7 @@ __global__ __launch_bounds__(256) void k_choice_rows(ChoiceRows a) {
             for (int i = 0; i < 4; ++i)
                 if (t0 + joiners * i < a.tiles) r = join(r, q[i]);
         }
-#pragma unroll
-        for (int o = 32; o > 0; o >>= 1) r = join(r, shuffled(r, o));
+        r = wave_join(r);
         if (lane == 0) wave_stat[wave] = r;
     }
     if (tid == 0) count = 0;
@@ -206,16 +226,13 @@ __global__ __launch_bounds__(256) void k_choice_rows(ChoiceRows a) {
         const bool none = r.max == NEG_INF && r.rest == -1.f;  // every class is masked
         const float log_all = none ? 0.f : log1pf(r.rest), tau = none ? 0.f : r.mean / (1.f + r.rest);
         if (lane == 0) {
-            int64_t y = -1;
-            if (a.labels) {
-                y = id_of(a.labels, a.ids64, m);
-                if (y >= a.classes) {
-                    atomicOr(a.err, ERR_BIT_INDEX);
-                    y = -1;
-                }
+            int64_t y = label;
+            if (y >= a.classes) {
+                atomicOr(a.err, ERR_BIT_INDEX);
+                y = -1;
             }
             float dy = NEG_INF;
-            if (y >= 0 && a.zlabel[m] != NEG_INF) dy = a.zlabel[m] - r.max;
+            if (y >= 0 && zlabel != NEG_INF) dy = zlabel - r.max;
             if (a.logprob) a.logprob[m] = y >= 0 ? dy - log_all : 0.f;
             if (a.lse) a.lse[m] = none ? NEG_INF : r.max + log_all;
             if (a.entropy) a.entropy[m] = log_all - tau;
@@ -281,6 +298,27 @@ __global__ __launch_bounds__(256) void k_choice_rows(ChoiceRows a) {
         }
     }
     __syncthreads();
+    const float log_all = row_log_all;
+    auto put = [&](int k, int64_t id, float v) {
+        if (a.ids64) ((int64_t*)a.top_ids)[m * a.top + k] = id;
+        else ((int32_t*)a.top_ids)[m * a.top + k] = (int32_t)id;
+        if (a.top_logprob) a.top_logprob[m * a.top + k] = v;
+    };
+    if (n <= 64) {  // one wave ranks them, from its registers
+        if (wave > 0) return;
+        const double z = lane < n ? cand_z[lane] : 0.0;
+        const int id = lane < n ? cand[lane] : -1;
+        int r = 0;
+        for (int j = 0; j < n; ++j) {
+            const double zj = lane_double(z, j);
+            r += zj > z || (zj == z && __builtin_amdgcn_readlane(id, j) < id);
+        }
+        const double first = lane_double(z, __ffsll((unsigned long long)__ballot(lane < n && r == 0)) - 1);
+        const bool seen = z != -__builtin_huge_val();
+        if (lane < n && r < a.top) put(r, seen ? id : -1, seen ? (float)(z - first) - log_all : NEG_INF);
+        if (lane >= n && lane < a.top) put(lane, -1, NEG_INF);  // fewer visible classes than wanted
+        return;
+    }
     constexpr int MOST = (CANDIDATES_MAX + 255) / 256;
     int ranks[MOST];
 #pragma unroll
@@ -294,12 +332,6 @@ __global__ __launch_bounds__(256) void k_choice_rows(ChoiceRows a) {
         if (ranks[i] == 0) best = cand_z[c];
     }
     __syncthreads();
-    const float log_all = row_log_all;
-    auto put = [&](int k, int64_t id, float v) {
-        if (a.ids64) ((int64_t*)a.top_ids)[m * a.top + k] = id;
-        else ((int32_t*)a.top_ids)[m * a.top + k] = (int32_t)id;
-        if (a.top_logprob) a.top_logprob[m * a.top + k] = v;
-    };
 #pragma unroll
     for (int i = 0; i < MOST; ++i) {
         if (ranks[i] >= a.top) continue;
@@ -307,7 +339,6 @@ __global__ __launch_bounds__(256) void k_choice_rows(ChoiceRows a) {
         const bool seen = cand_z[c] != -__builtin_huge_val();
         put(ranks[i], seen ? cand[c] : -1, seen ? (float)(cand_z[c] - best) - log_all : NEG_INF);
     }
-    for (int k = n + tid; k < a.top; k += 256) put(k, -1, NEG_INF);  // fewer visible classes than wanted
 }
 
 // Whether row m has a gradient at all. Rows without one (no label, or both upstream gradients 0) may hold anything in x: 0 times
