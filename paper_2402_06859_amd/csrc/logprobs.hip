@@ -88,7 +88,9 @@ __device__ __forceinline__ double lane_double(double x, int lane) {
 }
 __device__ __forceinline__ float lane_value(float x, int lane) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), lane)); }
 
-__device__ __forceinline__ int choose_groups(const uint2* groups, int n, int want, Chosen& c) {
+// `beside` runs where one wave ranks what is listed and the others wait.
+template <typename F>
+__device__ __forceinline__ int choose_groups(const uint2* groups, int n, int want, Chosen& c, F beside) {
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     constexpr int AHEAD = 8;  // loads in flight
     float mine = NEG_INF;
@@ -130,6 +132,7 @@ __device__ __forceinline__ int choose_groups(const uint2* groups, int n, int wan
     }
     __syncthreads();
     const int listed = c.count;
+    beside();
     if (listed <= LISTED) {  // (the list's order is by chance, its ranks are not)
         if (listed <= 64) {
             if (wave == 0) {
@@ -187,7 +190,7 @@ __device__ __forceinline__ int choose_groups(const uint2* groups, int n, int wan
 }
 
 // One workgroup per row.
-template <typename T>
+template <typename T, bool LATE>
 __global__ __launch_bounds__(256) void k_choice_rows(ChoiceRows a) {
     __shared__ ChoiceStat wave_stat[4];
     __shared__ Chosen chosen;
@@ -201,28 +204,28 @@ __global__ __launch_bounds__(256) void k_choice_rows(ChoiceRows a) {
     if (m >= a.rows) return;
 
     // One wave joins the tiles, unless they are very many: the others go on to the groups (this kernel is bound by its instructions, and a
-    // join has 45 of them).
-    const int joiners = a.tiles <= 1024 ? 64 : 256;
+    // join has 45 of them). LATE: the second wave, from loads made ahead, while the first one ranks groups.
+    const int joiners = !LATE && a.tiles > 1024 ? 256 : 64, joiner = LATE ? 1 : 0;
     const int64_t label = a.labels ? id_of(a.labels, a.ids64, m) : -1;
     const float zlabel = a.labels ? a.zlabel[m] : 0.f;  // (written where the label is in range)
-    if (tid < joiners) {
-        ChoiceStat r{NEG_INF, -1.f, 0.f, 0.f};
-        for (int64_t t0 = tid; t0 < a.tiles; t0 += 4 * joiners) {
-            ChoiceStat q[4];
+    const bool joins = joiners == 256 || wave == joiner;
+    const int64_t from = joiners == 256 ? tid : lane;
+    ChoiceStat q[4];
+    auto load = [&](int64_t t0) __attribute__((always_inline)) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) q[i] = a.stat[m * a.tiles + (t0 + joiners * i < a.tiles ? t0 + joiners * i : t0)];
+        for (int i = 0; i < 4; ++i) q[i] = a.stat[m * a.tiles + (t0 + joiners * i < a.tiles ? t0 + joiners * i : a.tiles - 1)];
+    };
+    auto joined = [&]() __attribute__((always_inline)) {
+        ChoiceStat r{NEG_INF, -1.f, 0.f, 0.f};
+        for (int64_t t0 = from; t0 < a.tiles; t0 += 4 * joiners) {
+            if (!LATE || t0 != from) load(t0);
 #pragma unroll
             for (int i = 0; i < 4; ++i)
                 if (t0 + joiners * i < a.tiles) r = join(r, q[i]);
         }
-        r = wave_join(r);
-        if (lane == 0) wave_stat[wave] = r;
-    }
-    if (tid == 0) count = 0;
-    if (joiners == 256) __syncthreads();
-    if (wave == 0) {
-        ChoiceStat r = wave_stat[0];
-        if (joiners == 256) r = join(join(r, wave_stat[1]), join(wave_stat[2], wave_stat[3]));
+        return wave_join(r);
+    };
+    auto answer = [&](const ChoiceStat& r) __attribute__((always_inline)) {
         const bool none = r.max == NEG_INF && r.rest == -1.f;  // every class is masked
         const float log_all = none ? 0.f : log1pf(r.rest), tau = none ? 0.f : r.mean / (1.f + r.rest);
         if (lane == 0) {
@@ -239,12 +242,28 @@ __global__ __launch_bounds__(256) void k_choice_rows(ChoiceRows a) {
             if (a.stats) a.stats[m] = make_float4(r.max, r.rest, tau, dy);
             row_log_all = log_all;
         }
+    };
+    if (tid == 0) count = 0;
+    if (LATE) {
+        if (joins) load(from);
+    } else {
+        if (joins) {
+            const ChoiceStat r = joined();
+            if (joiners == 64) answer(r);
+            else if (lane == 0) wave_stat[wave] = r;
+        }
+        if (joiners == 256) {
+            __syncthreads();
+            if (wave == 0) answer(join(join(wave_stat[0], wave_stat[1]), join(wave_stat[2], wave_stat[3])));
+        }
+        if (a.top == 0) return;
     }
-    if (a.top == 0) return;
 
     const uint2* const groups = a.groups + m * a.g.count;
     const int want = (int)(a.g.count < a.top + SLACK ? a.g.count : a.top + SLACK);
-    const int got = choose_groups(groups, (int)a.g.count, want, chosen);
+    const int got = choose_groups(groups, (int)a.g.count, want, chosen, [&]() {
+        if (LATE && joins) answer(joined());
+    });
     // the candidates: each group's largest class, and all of its classes where another may be as large as the last group's
     const float least = got == want && want < a.g.count ? chosen.key[want - 1] : NEG_INF;
     const int size_log = 31 - __builtin_clz(a.g.size), per_log = 29 - __builtin_clz(a.g.pitch);  // (powers of two)
@@ -450,8 +469,15 @@ hipError_t launch_choice_rows(const ChoiceRows& a, bool bf16, hipStream_t s) {
     if (a.rows == 0) return hipSuccess;
     const int64_t x = a.rows < 1 << 20 ? a.rows : 1 << 20;  // (less than 2^32 threads along x)
     const dim3 grid((unsigned)x, (unsigned)((a.rows + x - 1) / x));
-    if (bf16) hipLaunchKernelGGL(k_choice_rows<bf16_t>, grid, dim3(256), 0, s, a);
-    else hipLaunchKernelGGL(k_choice_rows<float>, grid, dim3(256), 0, s, a);
+    // us, join first / late: 64 x 5000 classes 10.6 / 9.5, 1024 x 5000 17.3 / 16.0, 1 x 50000 12.4 / 11.4; 2000 x 5000 23.6 / 24.4, 8192 x 1000 73 / 80 (more
+    // rows hide one another's waits); 50 x 100003 in float (1563 tiles) 25.8 / 29.8
+    if (a.top > 0 && a.rows <= 1024 && a.tiles <= 1024) {
+        if (bf16) hipLaunchKernelGGL((k_choice_rows<bf16_t, true>), grid, dim3(256), 0, s, a);
+        else hipLaunchKernelGGL((k_choice_rows<float, true>), grid, dim3(256), 0, s, a);
+    } else {
+        if (bf16) hipLaunchKernelGGL((k_choice_rows<bf16_t, false>), grid, dim3(256), 0, s, a);
+        else hipLaunchKernelGGL((k_choice_rows<float, false>), grid, dim3(256), 0, s, a);
+    }
     return hipGetLastError();
 }
 
