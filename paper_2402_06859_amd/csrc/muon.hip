@@ -182,8 +182,8 @@ __device__ __forceinline__ void x_elements(const Matrix& t, const MuonScalars& a
     if (!taken || r >= t.rows || c >= t.cols) return;
     const int64_t k = r * t.cols + c;
     const int left = t.cols - c < 8 ? (int)(t.cols - c) : 8;
-    float g[8], m[8];
-    load_grad(t, k, left, g);
+    float g[8] = {}, m[8];
+    if (a.nesterov) load_grad(t, k, left, g);  // (else U is the momentum itself)
     load_f32(t.m, k, left, m);
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] = e < left ? (float)((double)update_of(a, m[e], g[e] * gs) * inv) : 0.f;
