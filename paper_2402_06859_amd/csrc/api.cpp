@@ -398,13 +398,19 @@ GemmPlan plan_logits(const rdcn_handle* h, int64_t rows, int64_t classes, int64_
     return p;
 }
 
-// The same where log probabilities are made of the logits. Up to 16 rows, more classes than one round of streamed blocks covers: the product is
-// the read of w, and streamed 16 x 64 blocks have all of a 512-wide block's loads on their way at once, two blocks a CU. us, 128 x 128 (or 64 x 64)
-// blocks / streamed: 1 x 100003 classes x 1856 81 / 64 (5.8 TB/s), 16 rows 80 / 68; 1 x 50000 x 512 18.2 / 16.9, 16 rows 18.1 / 17.2; 16 x 20000 x 1000 17.2 /
-// 16.3; 1 x 30000 x 160 7.0 / 6.5; 8 x 131072 x 4352 197 / 187. Blocks of 32 rows: 16 x 100003 x 1856 73, but 16 x 50000 x 512 20.
+// The same where log probabilities are made of the logits, up to 64 rows. The product is the read of w, through LDS beside as many rows of x as a
+// block has, so few: 64 x 256 blocks, two a CU, where the last round of them is nearly full, else 64 x 128 ones, three a CU. Up to 16 rows streamed 16 x 64
+// blocks, which have 512 columns of w a block on their way at once, where one round of them is enough or K long. us, 128 x 128 blocks / the one taken (and the
+// others): 50 x 100003 x 1856 83 / 72 (64 x 128 87), 64 x 131072 x 4352 206 / 192 (228), 50 x 120000 x 512 35.9 / 29.8 (33.0); 50 x 50000 x 512 19.1 / 15.0 (64 x
+// 256 18.3), 50 x 70000 x 1856 73.8 / 57.2 (61.3), 50 x 150000 x 1856 122 / 111 (125); 1 x 100003 x 1856 81 / 64 (5.8 TB/s; 64 x 256 67), 16 rows 80 / 68 (70), 1 x
+// 40000 x 1856 36 / 30 (64 x 128 35), 1 x 30000 x 160 7.0 / 6.4 (7.7), 16 x 50000 x 512 18.1 / 13.9 (streamed 17.0).
 GemmPlan plan_choice(const rdcn_handle* h, int64_t rows, int64_t classes, int64_t dim) {
     const GemmPlan p = plan_logits(h, rows, classes, dim);
-    return h->bf16 && rows <= 16 && !gemm_streams(rows, classes, dim, p) ? plan_few_rows() : p;
+    if (!h->bf16 || rows > 64 || gemm_streams(rows, classes, dim, p)) return p;
+    if (rows <= 16 && (classes <= 32768 || dim >= 1000)) return plan_few_rows(16, 64);
+    if (p.bm != 128) return p;
+    const int64_t blocks = (classes + 255) / 256, rest = blocks % 512;
+    return plan_few_rows(64, blocks >= 352 && (rest == 0 || rest >= 352) ? 256 : 128);
 }
 
 // The layout for G in pieces of `piece` classes, or whole.

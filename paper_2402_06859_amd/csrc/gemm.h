@@ -147,12 +147,12 @@ inline GemmPlan plan_f32_lds() {
     p.stages = F32_LDS_STAGES;
     return p;
 }
-// Logits of up to 16 rows over at most 2^27 classes (EPI_CHOICE_*): streamed 16 x 64 blocks, 512 threads each.
+// Logits of few rows (EPI_CHOICE_*), over at most 2^27 classes: streamed 16 x 64 blocks, or 64 x 128 or 64 x 256 ones.
 constexpr int FEW_ROWS_STAGES = 104;  // marks such a plan
-inline GemmPlan plan_few_rows() {
+inline GemmPlan plan_few_rows(int bm, int bn) {
     GemmPlan p;
-    p.bm = 16;
-    p.bn = 64;
+    p.bm = bm;
+    p.bn = bn;
     p.stages = FEW_ROWS_STAGES;
     return p;
 }

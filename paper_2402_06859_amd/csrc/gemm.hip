@@ -1691,6 +1691,20 @@ hipError_t launch_tile(const GemmArgs& g, int splits, hipStream_t s) {
     return hipGetLastError();
 }
 
+// See plan_choice.
+template <int BM, int BN>
+hipError_t launch_few(const GemmArgs& g, hipStream_t s) {
+    const dim3 grid((unsigned)(((g.M + BM - 1) / BM) * ((g.N + BN - 1) / BN)));
+    if constexpr (BM == 16) {
+        hipLaunchKernelGGL((k_gemm_stream<1, 4, 1, 64, bf16_t, EK_CHOICE, false>), grid, dim3(64 * ST_KW), 0, s, g);
+    } else {
+        constexpr int WM = BN == 256 ? 1 : 2, WN = 4 / WM;
+        if (g.epi == EPI_CHOICE_GRAD) hipLaunchKernelGGL((k_gemm_mfma<BM, BN, false, false, 2, WM, WN, false, bf16_t, EK_CHOICE_GRAD, false, 64>), grid, dim3(256), 0, s, g);
+        else hipLaunchKernelGGL((k_gemm_mfma<BM, BN, false, false, 2, WM, WN, false, bf16_t, EK_CHOICE, false, 64>), grid, dim3(256), 0, s, g);
+    }
+    return hipGetLastError();
+}
+
 }  // namespace
 
 GemmPlan plan_gemm(int64_t M, int64_t N, int64_t K, bool bf16, bool allow_split, int split_blocks, bool fused_out) {
@@ -1879,7 +1893,7 @@ namespace {
 // for 64 x 8192. Between K 512 and the line at 1536 they would be ahead: 300 x 1024 x 512
 // 6.5 / 7.5, 128 x 4096 x 1024 8.2 / 9.9.)
 int stream_block(int64_t M, int64_t N, int64_t K, const GemmPlan& p) {
-    if (p.bm != 64 || p.splits != 1) return 0;
+    if (p.bm != 64 || p.splits != 1 || p.stages == FEW_ROWS_STAGES) return 0;
     auto tiles = [&](int bm, int bn) { return ((M + bm - 1) / bm) * ((N + bn - 1) / bn); };
     if (tiles(16, 16) <= 256) return 1;
     if (tiles(32, 32) <= 256) return 2;
@@ -1894,13 +1908,14 @@ bool gemm_streams(int64_t M, int64_t N, int64_t K, const GemmPlan& p) { return s
 int64_t gemm_soft_tiles(int64_t M, int64_t N, int64_t K, const GemmPlan& p, bool bf16, int* columns) {
     const int st = bf16 ? stream_block(M, N, K, p) : 0;
     // (a streamed block's columns, or those of one wave)
-    *columns = st == 1 ? 16 : st || p.bm == 64 ? 32 : 64;
+    *columns = st == 1 ? 16 : p.stages == FEW_ROWS_STAGES ? 64 : st || p.bm == 64 ? 32 : 64;
     return (N + *columns - 1) / *columns;
 }
 
 ChoiceGroups gemm_choice_groups(int64_t M, int64_t N, int64_t K, const GemmPlan& p, bool bf16) {
     ChoiceGroups c;
-    if (p.stages == FEW_ROWS_STAGES) c.span = 16, c.pitch = 4, c.size = 16;
+    if (p.stages == FEW_ROWS_STAGES && p.bm == 16) c.span = 16, c.pitch = 4, c.size = 16;
+    else if (p.stages == FEW_ROWS_STAGES) c.span = 64, c.pitch = 16, c.size = 16;
     else if (bf16 && stream_block(M, N, K, p)) c.span = 8, c.pitch = 4, c.size = 8;
     else if (p.bm == 256 || (p.bm == 128 && p.stages == 3)) c.span = 32, c.pitch = 8, c.size = 16;  // 32 x 32 tiles
     else if (p.bm == 128) c.span = 64, c.pitch = 16, c.size = 16;
@@ -1920,9 +1935,7 @@ hipError_t launch_gemm(const GemmArgs& g, const GemmPlan& p, bool bf16, hipStrea
     ga.group_m = p.group_m;
     if (p.stages == FEW_ROWS_STAGES) {
         if (g.a_kstrided || g.b_kstrided || g.ops_f16 || g.a2 || (g.epi != EPI_CHOICE_FWD && g.epi != EPI_CHOICE_GRAD)) return hipErrorInvalidValue;
-        const int64_t tiles = ((g.M + 15) / 16) * ((g.N + 63) / 64);
-        hipLaunchKernelGGL((k_gemm_stream<1, 4, 1, 64, bf16_t, EK_CHOICE, false>), dim3((unsigned)tiles), dim3(64 * ST_KW), 0, s, ga);
-        return hipGetLastError();
+        return p.bm == 16 ? launch_few<16, 64>(ga, s) : p.bn == 256 ? launch_few<64, 256>(ga, s) : launch_few<64, 128>(ga, s);
     }
     if (!g.a_kstrided && !g.b_kstrided) {
         switch (stream_block(g.M, g.N, g.K, p)) {

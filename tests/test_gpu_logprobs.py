@@ -338,7 +338,8 @@ def test_less_scratch_means_pieces_of_the_classes(dtype, rows, dim, classes):
 
 
 @pytest.mark.parametrize("rows,dim,classes,top", [(1, 8, 8201, 3), (16, 136, 9001, 32), (13, 4352, 8209, 5), (2, 512, 50000, 8),
-                                                  (16, 1856, 20003, 8), (17, 512, 20003, 8)])
+                                                  (16, 1856, 20003, 8), (17, 512, 20003, 8), (16, 1000, 33001, 8), (64, 512, 50001, 8),
+                                                  (17, 72, 31003, 4), (40, 72, 100003, 8), (1, 64, 90113, 32), (64, 1000, 91003, 5)])
 def test_few_rows_of_many_classes(rows, dim, classes, top):
     need_gpu()
     print("logprobs of few rows", rows, dim, classes, flush=True)
