@@ -612,14 +612,20 @@ static_assert(sizeof(Small) <= 4096, "kernel arguments");
 // Whether X and A are made anew after step k.
 __host__ __device__ inline bool anew_after(int k, int steps) { return k < steps - 1 && (k == 1 || (k > 1 && (k - 1) % 3 == 0)); }
 
+// S: 64, or 32 for a shorter side of at most that (half of every sum, a quarter of the elements). Tiles of 16 x 16: what bounds a product here is the way from
+// the sums through the pairs to the next product's fragments, so the elements are spread over all lanes (four of 32 x 160, 32 x 32 tiles of 64 x 64: 34 us,
+// this 22; 64 x 64 24 and 22).
+template <int S>
 __global__ __launch_bounds__(256) void k_muon_small(Small b) {
     constexpr int E = SMALL * SMALL, CP = SMALL + 4;  // elements of a plane
+    constexpr int TS = S / 32;                        // a wave's tiles, down, and in a square matrix across (a block of X: two)
     __shared__ __attribute__((aligned(1024))) bf16_t squares[4][2 * E];  // A, T A, T, P
     __shared__ __attribute__((aligned(1024))) bf16_t xk[2 * E];          // a block of X, K-contiguous along the longer side
     __shared__ __attribute__((aligned(1024))) bf16_t xs[2 * E];          // the same, K-strided along the shorter
     __shared__ __attribute__((aligned(16))) float cs[SMALL * CP];
     const Matrix t = b.t[blockIdx.x];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, wm = wave >> 1, wn = wave & 1;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int down = (wave >> 1) * 16 * TS, along = (wave & 1) * 16 * TS, across = (wave & 1) * 32;  // the wave's first row, and column of either kind
     const bool tall = t.rows > t.cols;
     const int64_t length = tall ? t.rp : t.cp;  // of the longer side, padded
     float gs;
@@ -627,33 +633,49 @@ __global__ __launch_bounds__(256) void k_muon_small(Small b) {
     const double sum = block_sum(momentum_range(t, b.a, gs, taken, 0, t.rows * t.cols));
     const double inv = sum == 0.0 ? 0.0 : (double)b.q.x[0] / sqrt(sum);
 
-    using Acc = f32x16_t[3];
-    auto clear = [&](Acc& c) {
-#pragma unroll
-        for (int z = 0; z < 3; ++z)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) c[z][e] = 0.f;
-    };
-    // c += x y^T for pairs x (K-contiguous) and y, this wave's 32 x 32 of it
-    auto product = [&](const bf16_t* x, const bf16_t* y, auto strided, Acc& c) __attribute__((always_inline)) {
+    // c = (add: c +) x y^T for pairs x (K-contiguous) and y, this wave's tiles of it, from column n0 on
+    auto product = [&](const bf16_t* x, const bf16_t* y, auto strided, auto depth, bool add, int n0, auto& c) __attribute__((always_inline)) {
         constexpr bool KS = decltype(strided)::value;
-        const uint32_t fx = frag_base<SMALL, false, SMALL>(x, wm * 32, lane), fy = frag_base<SMALL, KS, SMALL>(y, wn * 32, lane);
+        constexpr int TN = sizeof(c[0]) / sizeof(c[0][0]);
 #pragma unroll
-        for (int s = 0; s < 4; ++s) {
-            const bf16x8_t xh = frag_at<SMALL, false, SMALL>(fx, 0, 0, s), xl = frag_at<SMALL, false, SMALL>(fx, E * 2u, 0, s);
-            const bf16x8_t yh = frag_at<SMALL, KS, SMALL>(fy, 0, 0, s), yl = frag_at<SMALL, KS, SMALL>(fy, E * 2u, 0, s);
-            c[0] = mfma32x32x16<true>(yl, xh, c[0]);
-            c[1] = mfma32x32x16<true>(yh, xl, c[1]);
-            c[2] = mfma32x32x16<true>(yh, xh, c[2]);
+        for (int ks = 0; ks < decltype(depth)::value; ks += 32) {
+            bf16x8_t xh[TS], xl[TS];
+#pragma unroll
+            for (int u = 0; u < TS; ++u) {
+                xh[u] = load_frag<SMALL, false, SMALL>(x, down + 16 * u, ks, lane);
+                xl[u] = load_frag<SMALL, false, SMALL>(x + E, down + 16 * u, ks, lane);
+            }
+#pragma unroll
+            for (int w = 0; w < TN; ++w) {
+                const bf16x8_t yh = load_frag<SMALL, KS, SMALL>(y, n0 + 16 * w, ks, lane);
+                const bf16x8_t yl = load_frag<SMALL, KS, SMALL>(y + E, n0 + 16 * w, ks, lane);
+#pragma unroll
+                for (int u = 0; u < TS; ++u) {
+                    if (ks == 0 && !add) {
+#pragma unroll
+                        for (int z = 0; z < 3; ++z) c[u][w][z] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+                    }
+                    c[u][w][0] = mfma16x16x32<true>(yl, xh[u], c[u][w][0]);
+                    c[u][w][1] = mfma16x16x32<true>(yh, xl[u], c[u][w][1]);
+                    c[u][w][2] = mfma16x16x32<true>(yh, xh[u], c[u][w][2]);
+                }
+            }
         }
     };
-    // the four values of group g (0 .. 3) of a lane: C[m][n .. n + 3]
-    const int m = wm * 32 + (lane & 31);
-    auto column = [&](int g) { return wn * 32 + 8 * g + 4 * (lane >> 5); };
-    auto value = [&](const Acc& c, int i) { return (c[0][i] + c[1][i]) + c[2][i]; };
+    const std::integral_constant<int, S> side{};
+    const std::integral_constant<int, SMALL> block{};
+    // f(row, column, values) for the four elements of each tile that a lane has
+    auto each = [&](auto& c, int n0, auto f) __attribute__((always_inline)) {
+        constexpr int TN = sizeof(c[0]) / sizeof(c[0][0]);
+#pragma unroll
+        for (int u = 0; u < TS; ++u)
+#pragma unroll
+            for (int w = 0; w < TN; ++w)
+                f(down + 16 * u + (lane & 15), n0 + 16 * w + 4 * (lane >> 4), (c[u][w][0] + c[u][w][1]) + c[u][w][2]);
+    };
     auto at = [](int r, int k) { return r * SMALL + (((k >> 3) ^ kc_swz<SMALL>(r)) * 8) + (k & 7); };  // K-contiguous
     auto strided_at = [](int k, int r) { return k * SMALL + (((r >> 4) ^ kstr_swz<SMALL>(k)) * 16) + (r & 15); };
-    auto put4 = [&](bf16_t* x, int off, int64_t plane, const float* v) __attribute__((always_inline)) {
+    auto put4 = [&](bf16_t* x, int off, int64_t plane, const f32x4_t& v) __attribute__((always_inline)) {
         uint32_t h[4], l[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
@@ -664,20 +686,13 @@ __global__ __launch_bounds__(256) void k_muon_small(Small b) {
         *(uint2*)(x + off) = make_uint2(h[0] | h[1] << 16, h[2] | h[3] << 16);
         *(uint2*)(x + off + plane) = make_uint2(l[0] | l[1] << 16, l[2] | l[3] << 16);
     };
-    auto store = [&](bf16_t* x, const Acc& c, float scale) __attribute__((always_inline)) {
-#pragma unroll
-        for (int g = 0; g < 4; ++g) {
-            float v[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] = value(c, 4 * g + e) * scale;
-            put4(x, at(m, column(g)), E, v);
-        }
+    auto store = [&](bf16_t* x, auto& c, int n0, float scale) __attribute__((always_inline)) {
+        each(c, n0, [&](int m, int n, const f32x4_t& v) __attribute__((always_inline)) { put4(x, at(m, n), E, v * scale); });
     };
     auto half_value = [](bf16_t x) { return (float)__builtin_bit_cast(_Float16, x); };
 
     // X0, and A from it
-    Acc gram, c;
-    clear(gram);
+    f32x4_t gram[TS][TS][3], c[TS][TS][3], cx[TS][2][3];
     const int row = tid >> 2, first = (tid & 3) * 16;  // a thread's 16 values of a block's row
     for (int64_t l0 = 0; l0 < length; l0 += SMALL) {
         __syncthreads();
@@ -704,23 +719,26 @@ __global__ __launch_bounds__(256) void k_muon_small(Small b) {
             const int k = first + 8 * (u & 1);
             *(u32x4_t*)(t.x + (u >> 1) * SMALL * length + row * length + l0 + k) = *(const u32x4_t*)(xk + (u >> 1) * E + at(row, k));
         }
-        product(xk, xk, std::false_type{}, gram);
+        product(xk, xk, std::false_type{}, block, l0 > 0, along, gram);
     }
     bf16_t* const A = squares[0];
     bf16_t* const TA = squares[1];
     bf16_t *T = squares[2], *P = squares[3];
-    store(A, gram, b.q.gram[0] / (b.q.x[0] * b.q.x[0]));
+    store(A, gram, along, b.q.gram[0] / (b.q.x[0] * b.q.x[0]));
     __syncthreads();
 
-    // a block of X as a K-strided operand
-    auto load_block = [&](int64_t l0) {
+    // a block of X as a K-strided operand, its loads ahead of the block in front
+    u32x4_t ahead[4];
+    auto fetch = [&](int64_t l0) {
+#pragma unroll
+        for (int u = 0; u < 4; ++u) ahead[u] = *(const u32x4_t*)(t.x + (u >> 1) * SMALL * length + row * length + l0 + first + 8 * (u & 1));
+    };
+    auto take_block = [&](int64_t l0) {
         __syncthreads();
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            const int k = first + 8 * (u & 1);
-            *(u32x4_t*)(xs + (u >> 1) * E + strided_at(row, k)) = *(const u32x4_t*)(t.x + (u >> 1) * SMALL * length + row * length + l0 + k);
-        }
+        for (int u = 0; u < 4; ++u) *(u32x4_t*)(xs + (u >> 1) * E + strided_at(row, first + 8 * (u & 1))) = ahead[u];
         __syncthreads();
+        if (l0 + SMALL < length) fetch(l0 + SMALL);
     };
     bool power = false;  // whether P stands (else it is I)
     float sx = b.q.x[0], sp = 1.f;
@@ -728,41 +746,35 @@ __global__ __launch_bounds__(256) void k_muon_small(Small b) {
     for (int k = 0; k < steps; ++k) {
         const bool last = k == steps - 1, anew = anew_after(k, steps);
         const float sg = b.q.gram[k], st_ = b.q.poly[k];
-        clear(c);
-        product(A, A, std::false_type{}, c);
+        product(A, A, std::false_type{}, side, false, along, c);
         {
             const float pa = (float)b.a.a, pb = (float)b.a.b / sg, pc = (float)b.a.c / (sg * sg);
-#pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                const int n = column(g);
-                float v[4];
+            each(c, along, [&](int m, int n, const f32x4_t& v) __attribute__((always_inline)) {
+                f32x4_t p;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const float x = half_value(A[at(m, n + e)]) + half_value(A[E + at(m, n + e)]);
-                    v[e] = fmaf(pc, value(c, 4 * g + e), fmaf(pb, x, m == n + e ? pa : 0.f)) * st_;
+                    p[e] = fmaf(pc, v[e], fmaf(pb, x, m == n + e ? pa : 0.f)) * st_;
                 }
-                put4(T, at(m, n), E, v);
-            }
+                put4(T, at(m, n), E, p);
+            });
         }
         __syncthreads();
         if (!last && !anew) {
-            clear(c);
-            product(T, A, std::false_type{}, c);
-            store(TA, c, b.q.half[k] / (st_ * sg));
+            product(T, A, std::false_type{}, side, false, along, c);
+            store(TA, c, along, b.q.half[k] / (st_ * sg));
         }
         if (power) {
-            clear(c);
-            product(T, P, std::false_type{}, c);
+            product(T, P, std::false_type{}, side, false, along, c);
             __syncthreads();
-            store(P, c, b.q.power[k] / (st_ * sp));
+            store(P, c, along, b.q.power[k] / (st_ * sp));
             sp = b.q.power[k];
             __syncthreads();
         }
         if (!last && !anew) {
             __syncthreads();
-            clear(c);
-            product(T, TA, std::false_type{}, c);
-            store(A, c, b.q.gram[k + 1] / (st_ * b.q.half[k]));
+            product(T, TA, std::false_type{}, side, false, along, c);
+            store(A, c, along, b.q.gram[k + 1] / (st_ * b.q.half[k]));
             __syncthreads();
         }
         if (!power) {
@@ -773,43 +785,34 @@ __global__ __launch_bounds__(256) void k_muon_small(Small b) {
             power = true;
         }
         if (!anew) continue;
-        clear(gram);
         const float sn = b.q.x[k + 1];
+        __syncthreads();
+        fetch(0);
         for (int64_t l0 = 0; l0 < length; l0 += SMALL) {
-            load_block(l0);
-            clear(c);
-            product(P, xs, std::true_type{}, c);
-            store(xk, c, sn / (sx * sp));
-#pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                float v[4];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) v[e] = value(c, 4 * g + e) * (sn / (sx * sp));
-                put4(t.x, (int)(m * length + l0) + column(g), SMALL * length, v);
-            }
+            take_block(l0);
+            product(P, xs, std::true_type{}, side, false, across, cx);
+            each(cx, across, [&](int m, int n, const f32x4_t& v) __attribute__((always_inline)) {
+                put4(xk, at(m, n), E, v * (sn / (sx * sp)));
+                put4(t.x, (int)(m * length + l0) + n, SMALL * length, v * (sn / (sx * sp)));
+            });
             __syncthreads();
-            product(xk, xk, std::false_type{}, gram);
+            product(xk, xk, std::false_type{}, block, l0 > 0, along, gram);
         }
         sx = sn;
         power = false;
         __syncthreads();
-        store(A, gram, b.q.gram[k + 1] / (sx * sx));
+        store(A, gram, along, b.q.gram[k + 1] / (sx * sx));
         __syncthreads();
     }
     StepFactors f;
     Destination d{t.param, t.master, t.rows, t.cols, t.scale, t.weight_decay, t.flags};
     if (!step_factors(b.a, d, f)) return;
+    __syncthreads();
+    fetch(0);
     for (int64_t l0 = 0; l0 < length; l0 += SMALL) {
-        load_block(l0);
-        clear(c);
-        product(P, xs, std::true_type{}, c);
-#pragma unroll
-        for (int g = 0; g < 4; ++g) {
-            f32x4_t v;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] = value(c, 4 * g + e) * (1.f / (sx * sp));
-            *(f32x4_t*)(cs + m * CP + column(g)) = v;
-        }
+        take_block(l0);
+        product(P, xs, std::true_type{}, side, false, across, cx);
+        each(cx, across, [&](int m, int n, const f32x4_t& v) __attribute__((always_inline)) { *(f32x4_t*)(cs + m * CP + n) = v * (1.f / (sx * sp)); });
         __syncthreads();
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
@@ -1011,7 +1014,9 @@ hipError_t run_batch(const MuonTensor* t, const Layout* l, int count, const Muon
         b.a = a;
         b.q = q;
         for (int i = 0; i < count; ++i) fill(b.t[i], t[i], l[i], sc);
-        hipLaunchKernelGGL(k_muon_small, dim3((unsigned)count), dim3(256), 0, s, b);
+        if (std::all_of(t, t + count, [](const MuonTensor& x) { return std::min(x.rows, x.cols) <= 32; }))
+            hipLaunchKernelGGL(k_muon_small<32>, dim3((unsigned)count), dim3(256), 0, s, b);
+        else hipLaunchKernelGGL(k_muon_small<64>, dim3((unsigned)count), dim3(256), 0, s, b);
         return hipGetLastError();
     }
     {
