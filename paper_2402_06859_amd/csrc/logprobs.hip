@@ -67,6 +67,24 @@ __device__ __forceinline__ float key_of(uint2 g) {  // a group's largest logit; 
     return v == v ? v : NEG_INF;
 }
 
+// The rank of item `at` of n (at most 64) in a wave: up to four lanes an item, each against a part of the others. before(j, i): j is ahead of i.
+template <typename F>
+__device__ __forceinline__ int wave_rank(int n, int& at, bool& writes, F before) {
+    const int lane = threadIdx.x & 63, log = n <= 16 ? 2 : n <= 32 ? 1 : 0, part = lane & ((1 << log) - 1);
+    at = lane >> log;
+    writes = part == 0 && at < n;
+    int r = 0;
+    if (at < n) {
+#pragma unroll 4
+        for (int j = part; j < n; j += 1 << log) r += before(j, at);
+    }
+    const int r1 = __shfl_xor(r, 1);
+    if (log > 0) r += r1;
+    const int r2 = __shfl_xor(r, 2);
+    if (log > 1) r += r2;
+    return r;
+}
+
 // The groups of the `want` largest maxima, ordered, into chosen; returns how many there are (fewer where fewer hold a visible
 // class). Every four threads' largest is ranked among the 64 of them; the want-th of those is no larger than the want-th of all
 // groups, so all that reach it are listed, a few more than wanted, and ranked in turn.
@@ -86,7 +104,6 @@ __device__ __forceinline__ double lane_double(double x, int lane) {
     const uint32_t lo = __builtin_amdgcn_readlane((uint32_t)b, lane), hi = __builtin_amdgcn_readlane((uint32_t)(b >> 32), lane);
     return __longlong_as_double((long long)((uint64_t)hi << 32 | lo));
 }
-__device__ __forceinline__ float lane_value(float x, int lane) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), lane)); }
 
 // `beside` runs where one wave ranks what is listed and the others wait.
 template <typename F>
@@ -136,11 +153,10 @@ __device__ __forceinline__ int choose_groups(const uint2* groups, int n, int wan
     if (listed <= LISTED) {  // (the list's order is by chance, its ranks are not)
         if (listed <= 64) {
             if (wave == 0) {
-                const float k = lane < listed ? c.list_key[lane] : NEG_INF;
-                const int u = lane < listed ? c.list[lane] : 0x7FFFFFFF;
-                int r = 0;
-                for (int j = 0; j < listed; ++j) r += ahead(lane_value(k, j), __builtin_amdgcn_readlane(u, j), k, u);
-                if (lane < listed && r < want) c.group[r] = u, c.key[r] = k, c.bound[r] = c.list_bound[lane];
+                int i;
+                bool writes;
+                const int r = wave_rank(listed, i, writes, [&](int j, int i) { return ahead(c.list_key[j], c.list[j], c.list_key[i], c.list[i]); });
+                if (writes && r < want) c.group[r] = c.list[i], c.key[r] = c.list_key[i], c.bound[r] = c.list_bound[i];
             }
         } else {
             for (int i = tid; i < listed; i += 256) {
@@ -325,16 +341,12 @@ __global__ __launch_bounds__(256) void k_choice_rows(ChoiceRows a) {
     };
     if (n <= 64) {  // one wave ranks them, from its registers
         if (wave > 0) return;
-        const double z = lane < n ? cand_z[lane] : 0.0;
-        const int id = lane < n ? cand[lane] : -1;
-        int r = 0;
-        for (int j = 0; j < n; ++j) {
-            const double zj = lane_double(z, j);
-            r += zj > z || (zj == z && __builtin_amdgcn_readlane(id, j) < id);
-        }
-        const double first = lane_double(z, __ffsll((unsigned long long)__ballot(lane < n && r == 0)) - 1);
+        int i;
+        bool writes;
+        const int r = wave_rank(n, i, writes, [&](int j, int i) { return cand_z[j] > cand_z[i] || (cand_z[j] == cand_z[i] && cand[j] < cand[i]); });
+        const double z = i < n ? cand_z[i] : 0.0, first = lane_double(z, __ffsll((unsigned long long)__ballot(writes && r == 0)) - 1);
         const bool seen = z != -__builtin_huge_val();
-        if (lane < n && r < a.top) put(r, seen ? id : -1, seen ? (float)(z - first) - log_all : NEG_INF);
+        if (writes && r < a.top) put(r, seen ? cand[i] : -1, seen ? (float)(z - first) - log_all : NEG_INF);
         if (lane >= n && lane < a.top) put(lane, -1, NEG_INF);  // fewer visible classes than wanted
         return;
     }
