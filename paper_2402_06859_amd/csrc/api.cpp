@@ -1697,8 +1697,15 @@ rdcn_status rdcn_logprobs_grad(rdcn_handle* h, int64_t rows, int64_t dim, int64_
         const bool last = v + n == classes;
         const SoftProduct px = S.copies > 1 ? soft_product_fine(h, gx, rows, before, acc, grad_x, last, splitk)
                                             : soft_product(h, gx, before, acc, grad_x, last, splitk);
-        const SoftProduct pw = soft_product(h, gw, nullptr, nullptr, (char*)grad_w + (size_t)v * dim * e, true,
+        SoftProduct pw = soft_product(h, gw, nullptr, nullptr, (char*)grad_w + (size_t)v * dim * e, true,
                                             (float*)(sc + S.splitw));
+        // grad_w of few rows in 64 x 64 blocks too, where those are few: both products are then one launch. The whole call and its forward, us, 128 x 128 /
+        // 64 x 64: 100 x 136 x 20000 43.6 / 36.5, 333 x 160 x 20000 60 / 51, 333 x 512 x 5000 41.5 / 38.4; 333 x 320 x 20000 (1565 blocks) 64 / 68, 1000 x 512 x
+        // 5000 63 / 65.
+        if (px.p.bm == 64 && pw.p.bm == 128 && pw.p.splits == 1 && gw.K <= 768 && (n + 63) / 64 * ((dim + 63) / 64) <= 1280) {
+            pw.p.bm = pw.p.bn = 64;
+            pw.p.stages = 3;
+        }
         RDCN_TRY(soft_gradients(h, px, pw, s));
     }
     return RDCN_OK;

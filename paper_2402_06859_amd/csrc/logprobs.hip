@@ -470,8 +470,12 @@ __global__ __launch_bounds__(256) void k_choice_normalize(ChoiceNormalize a) {
 
 hipError_t launch_choice_normalize(const ChoiceNormalize& a, bool bf16, hipStream_t s) {
     if (a.p.rows == 0 || a.width == 0) return hipSuccess;
-    const int64_t per = (a.width / (bf16 ? 8 : 4) + 1023) / 1024, y = a.p.rows < 65535 ? a.p.rows : 65535;  // four vectors a thread
-    const dim3 grid((unsigned)(per > 64 ? 64 : per), (unsigned)y, (unsigned)((a.p.rows + 65534) / 65535));
+    const int64_t vectors = a.width / (bf16 ? 8 : 4), y = a.p.rows < 65535 ? a.p.rows : 65535;
+    int64_t per = (vectors + 1023) / 1024;  // four vectors a thread
+    if (per > 64) per = 64;
+    const int64_t fill = (1024 + a.p.rows - 1) / a.p.rows;  // (or fewer, down to one, until there are 1024 workgroups)
+    if (per < fill) per = fill < (vectors + 255) / 256 ? fill : (vectors + 255) / 256;
+    const dim3 grid((unsigned)per, (unsigned)y, (unsigned)((a.p.rows + 65534) / 65535));
     if (bf16) hipLaunchKernelGGL(k_choice_normalize<bf16_t>, grid, dim3(256), 0, s, a);
     else hipLaunchKernelGGL(k_choice_normalize<float>, grid, dim3(256), 0, s, a);
     return hipGetLastError();
