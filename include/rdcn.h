@@ -679,8 +679,8 @@ rdcn_status rdcn_grad_norm(rdcn_handle* h, const rdcn_adamw_tensor* tensors, int
  *   X  = U / |U| (the 2-norm of its elements; 0 where that is 0),  then `steps` times
  *   X <- a X + b A X + c A A X,  A = X X^T
  *   p' = p (1 - lr weight_decay) - lr scale X
- * |U| is summed in 64 bits; the products carry 22 bits and float sums: X is within 4e-5 of its own norm (the more uneven its
- * singular values, the nearer to that), where float products leave 1e-5; the other operations are one rounding to float each. The weights
+ * |U| is summed in 64 bits; the products carry 22 bits and float sums: X is within 1e-4 of its own norm (2e-6 to 4e-5 over
+ * the spectra measured, most for uneven singular values), where float products leave 1e-5; the other operations are one rounding to float each. The weights
  * are as for rdcn_adamw_step: float, bf16 with a float master, or bf16 alone, rounded to nearest or (stochastic) by chance, with its bits.
  * a, b, c = 3.4445, -4.7750, 2.0315 in 5 steps take all but the smallest singular values to within 0.7 to 1.2; 2, -1.5, 0.5
  * in more steps to 1 itself. Coefficients whose iteration leaves the range of its f16 pairs (|a + b s^2 + c s^4| multiplied up to
