@@ -554,7 +554,8 @@ rdcn_status rdcn_softmax_loss_grad(rdcn_handle* h, int64_t rows, int64_t dim, in
  *   - A masked class has probability 0 and is never among the most probable ones: where fewer than `top` are visible, the
  *     others have id -1 and log probability -inf. A row whose label is masked has logprob -inf; one with every class masked
  *     lse -inf and entropy 0.
- *   - A row whose logits hold NaN or +inf has NaN results, and ids of its own choice (in range, or -1).
+ *   - A row whose logits hold NaN or +inf has NaN results (logprob 0 without a label), and ids of its own choice: in range, or -1 with
+ *     log probability -inf. Its gradient, where it has one, is NaN too.
  * top is 0 (no lists) .. RDCN_LOGPROBS_TOP_MAX; top_ids in the handle's id type. logprob, entropy, lse, top_logprob and stats may
  * be NULL. stats [rows, 4] float, 16-byte aligned, is what the gradient needs of a row. `kept` (or NULL) saves the gradient a
  * product: it takes every class's exponential, as f16 in bf16 models (2^-11 of it, growing from 2^-29 of the largest of the 16 to 64 classes

@@ -369,27 +369,33 @@ __device__ __forceinline__ uint2 choice_group(F value) {
 // exp(d), d = z - top, of N logits whose row's maximum in the tile is top: t[] = exp(d) 2^r, their sum over the classes below the maximum,
 // the count of those at it, and the sum of t d log2 e. One fma takes z to the base-2 exponent, z log2 e - (top log2 e rounded): the
 // rounding r, the same for every class of the row, is undone by choice_stat. CLAMP: z may be -inf, or so large that the product overflows:
-// the difference first, and no r.
+// the difference first, and no r; the clamp is for t d alone, so that a NaN passes by t.
 template <int N, bool CLAMP>
 __device__ __forceinline__ void choice_sums(float (&z)[N], float top, float& below, int& at_top, float& mean) {
     constexpr float L = 1.44269504f;
     const float base = top * L;
 #pragma unroll
     for (int e = 0; e < N; ++e) {
-        const float d = CLAMP ? fmaxf((z[e] - top) * L, -1e4f) : fmaf(z[e], L, -base);
+        const float d = CLAMP ? (z[e] - top) * L : fmaf(z[e], L, -base);
         const bool one = z[e] == top;
         const float t = __builtin_amdgcn_exp2f(d);
         below += one ? 0.f : t;
         at_top += one;
-        mean = fmaf(t, d, mean);
+        mean = fmaf(t, CLAMP ? fmaxf(d, -1e4f) : d, mean);
         z[e] = t;
     }
 }
 // The row's statistics from those sums. log2 e is L + 1.92596299e-8: what a float leaves out of it is put back to first order, by the mean.
+// The largest of NaN is NaN or, in a search that begins at -inf, -inf: the sums tell it from a tile without a visible class. One of
+// +inf has NaN sums too.
 template <bool CLAMP>
 __device__ __forceinline__ ChoiceStat choice_stat(float top, float below, float at_top, float mean, float& undo) {
     constexpr float L = 1.44269504f, LN2 = 0.693147181f, REST = 9.25328596e-9f;  // ln 2 * 1.92596299e-8 / L
-    const float r = CLAMP ? 0.f : fmaf(top, L, -(top * L));
+    if (top == -__builtin_huge_valf()) {
+        undo = 1.f;
+        return below == 0.f ? ChoiceStat{top, -1.f, 0.f, 0.f} : ChoiceStat{below, below, below, 0.f};
+    }
+    const float r = CLAMP ? top - top : fmaf(top, L, -(top * L));
     undo = __builtin_amdgcn_exp2f(-r);
     mean = mean - at_top * (__builtin_amdgcn_exp2f(r) * r);  // (the maximum's own terms: to the bit, so that a class alone leaves 0)
     mean = (mean - r * below) * undo;
@@ -456,8 +462,8 @@ __device__ __forceinline__ void choice_epilogue8(const GemmArgs& g, int64_t m, i
         mean += __shfl_xor(mean, o);
     }
     if (!in) return;
-    float undo = 1.f;
-    const ChoiceStat r = mx == NEG ? ChoiceStat{NEG, -1.f, 0.f, 0.f} : choice_stat<true>(mx, below, at_top, mean, undo);
+    float undo;
+    const ChoiceStat r = choice_stat<true>(mx, below, at_top, mean, undo);
     if (n == tile * (8 * LANES)) g.stat[m * g.tiles + tile] = r;
     if (!g.c) return;
     bool ovf = false;
@@ -1059,8 +1065,8 @@ __device__ __forceinline__ void choice_rows(const GemmArgs& g, int64_t mw, int64
                 at_top += __shfl_xor(at_top, o);
                 mean += __shfl_xor(mean, o);
             }
-            float undo = 1.f;
-            const ChoiceStat r = mx == NEG ? ChoiceStat{NEG, -1.f, 0.f, 0.f} : choice_stat<EDGE || sizeof(T) == 4>(mx, below, at_top, mean, undo);
+            float undo;
+            const ChoiceStat r = choice_stat<EDGE || sizeof(T) == 4>(mx, below, at_top, mean, undo);
             if (in && half == 0) g.stat[m * g.tiles + nw / COLS] = r;
             if (g.c) store(v, m, in, sizeof(T) == 4 ? undo : undo * SOFT_E_SCALE);
         }

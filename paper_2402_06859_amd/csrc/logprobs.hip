@@ -36,7 +36,7 @@ __device__ __forceinline__ int64_t id_of(const void* ids, bool i64, int64_t m) {
 __device__ __forceinline__ ChoiceStat join(const ChoiceStat& p, const ChoiceStat& q) {
     const bool swap = q.max > p.max;
     const ChoiceStat a = swap ? q : p, b = swap ? p : q;
-    // (a range of NaN alone has such a maximum, but not that rest)
+    // (a range that holds NaN may have such a maximum too, but not that rest)
     if (b.max == NEG_INF) return ChoiceStat{a.max, b.rest == -1.f ? a.rest : a.rest + b.rest, a.mean, 0.f};
     const float t = b.max - a.max, e = expf(t), all = 1.f + b.rest;
     return ChoiceStat{a.max, fmaf(e, all, a.rest), e == 0.f ? a.mean : fmaf(e, fmaf(t, all, b.mean), a.mean), 0.f};
