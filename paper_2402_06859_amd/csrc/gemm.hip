@@ -366,9 +366,10 @@ __device__ __forceinline__ uint2 choice_group(F value) {
     return make_uint2(__float_as_uint(top), (((int)b < 0 ? b - 16u : b + 16u) & ~15u) | (uint32_t)at);
 }
 
-// exp(d), d = z - top, of N logits whose row's maximum in the tile is top: t[] = exp(d) 2^r, their sum over the classes below the maximum,
-// the count of those at it, and the sum of t d log2 e. One fma takes z to the base-2 exponent, z log2 e - (top log2 e rounded): the
-// rounding r, the same for every class of the row, is undone by choice_stat. CLAMP: z may be -inf, or so large that the product overflows:
+// exp(d), d = z - top, of N logits whose row's maximum in the tile is top: t[] = exp(d) 2^r, their sum and that of t d log2 e over the
+// classes below the maximum (its own terms, 0 but for r, would take the digits of what lies far below it), and the count of
+// those at it. One fma takes z to the base-2 exponent, z log2 e - (top log2 e rounded): the rounding r, the same for every class of the row, is
+// undone by choice_stat. CLAMP: z may be -inf, or so large that the product overflows:
 // the difference first, and no r; the clamp is for t d alone, so that a NaN passes by t.
 template <int N, bool CLAMP>
 __device__ __forceinline__ void choice_sums(float (&z)[N], float top, float& below, int& at_top, float& mean) {
@@ -378,10 +379,10 @@ __device__ __forceinline__ void choice_sums(float (&z)[N], float top, float& bel
     for (int e = 0; e < N; ++e) {
         const float d = CLAMP ? (z[e] - top) * L : fmaf(z[e], L, -base);
         const bool one = z[e] == top;
-        const float t = __builtin_amdgcn_exp2f(d);
-        below += one ? 0.f : t;
+        const float t = __builtin_amdgcn_exp2f(d), u = one ? 0.f : t;
+        below += u;
         at_top += one;
-        mean = fmaf(t, CLAMP ? fmaxf(d, -1e4f) : d, mean);
+        mean = fmaf(u, CLAMP ? fmaxf(d, -1e4f) : d, mean);
         z[e] = t;
     }
 }
@@ -397,7 +398,6 @@ __device__ __forceinline__ ChoiceStat choice_stat(float top, float below, float 
     }
     const float r = CLAMP ? top - top : fmaf(top, L, -(top * L));
     undo = __builtin_amdgcn_exp2f(-r);
-    mean = mean - at_top * (__builtin_amdgcn_exp2f(r) * r);  // (the maximum's own terms: to the bit, so that a class alone leaves 0)
     mean = (mean - r * below) * undo;
     return ChoiceStat{top, fmaf(below, undo, at_top - 1.f) + REST * mean, mean * LN2, 0.f};
 }
