@@ -551,7 +551,7 @@ rdcn_status rdcn_softmax_loss_grad(rdcn_handle* h, int64_t rows, int64_t dim, in
  *   - labels [rows] in the handle's id type, or NULL: no given classes (logprob then NULL too). A label below 0 marks a
  *     row without one: logprob 0, and no gradient of its entropy either; everything else of the row is written all the same. A label
  *     of `classes` or more does the same and raises the device error word (RDCN_ERR_INDEX).
- *   - A masked class has probability 0 and is never among the most probable ones: where fewer than `top` are visible, the
+ *   - A masked class, or one whose logit is -inf, has probability 0 and is never among the most probable ones: where fewer than `top` are visible, the
  *     others have id -1 and log probability -inf. A row whose label is masked has logprob -inf; one with every class masked
  *     lse -inf and entropy 0.
  *   - A row whose logits hold NaN or +inf has NaN results (logprob 0 without a label), and ids of its own choice: in range, or -1 with

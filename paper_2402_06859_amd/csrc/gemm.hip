@@ -369,8 +369,8 @@ __device__ __forceinline__ uint2 choice_group(F value) {
 // exp(d), d = z - top, of N logits whose row's maximum in the tile is top: t[] = exp(d) 2^r, their sum and that of t d log2 e over the
 // classes below the maximum (its own terms, 0 but for r, would take the digits of what lies far below it), and the count of
 // those at it. One fma takes z to the base-2 exponent, z log2 e - (top log2 e rounded): the rounding r, the same for every class of the row, is
-// undone by choice_stat. CLAMP: z may be -inf, or so large that the product overflows:
-// the difference first, and no r; the clamp is for t d alone, so that a NaN passes by t.
+// undone by choice_stat. CLAMP: z may be -inf, or so large that the product overflows or r does not stay near 0: the difference first, and no
+// r; the clamp is for t d alone, so that a NaN passes by t.
 template <int N, bool CLAMP>
 __device__ __forceinline__ void choice_sums(float (&z)[N], float top, float& below, int& at_top, float& mean) {
     constexpr float L = 1.44269504f;
@@ -389,14 +389,13 @@ __device__ __forceinline__ void choice_sums(float (&z)[N], float top, float& bel
 // The row's statistics from those sums. log2 e is L + 1.92596299e-8: what a float leaves out of it is put back to first order, by the mean.
 // The largest of NaN is NaN or, in a search that begins at -inf, -inf: the sums tell it from a tile without a visible class. One of
 // +inf has NaN sums too.
-template <bool CLAMP>
-__device__ __forceinline__ ChoiceStat choice_stat(float top, float below, float at_top, float mean, float& undo) {
+__device__ __forceinline__ ChoiceStat choice_stat(bool clamp, float top, float below, float at_top, float mean, float& undo) {
     constexpr float L = 1.44269504f, LN2 = 0.693147181f, REST = 9.25328596e-9f;  // ln 2 * 1.92596299e-8 / L
     if (top == -__builtin_huge_valf()) {
         undo = 1.f;
         return below == 0.f ? ChoiceStat{top, -1.f, 0.f, 0.f} : ChoiceStat{below, below, below, 0.f};
     }
-    const float r = CLAMP ? top - top : fmaf(top, L, -(top * L));
+    const float r = clamp ? top - top : fmaf(top, L, -(top * L));
     undo = __builtin_amdgcn_exp2f(-r);
     mean = (mean - r * below) * undo;
     return ChoiceStat{top, fmaf(below, undo, at_top - 1.f) + REST * mean, mean * LN2, 0.f};
@@ -463,7 +462,7 @@ __device__ __forceinline__ void choice_epilogue8(const GemmArgs& g, int64_t m, i
     }
     if (!in) return;
     float undo;
-    const ChoiceStat r = choice_stat<true>(mx, below, at_top, mean, undo);
+    const ChoiceStat r = choice_stat(true, mx, below, at_top, mean, undo);
     if (n == tile * (8 * LANES)) g.stat[m * g.tiles + tile] = r;
     if (!g.c) return;
     bool ovf = false;
@@ -1055,18 +1054,38 @@ __device__ __forceinline__ void choice_rows(const GemmArgs& g, int64_t mw, int64
             }
 #pragma unroll
             for (int o = MT; o < 64; o <<= 1) mx = fmaxf(mx, __shfl_xor(mx, o));
-            float below = 0.f, mean = 0.f;
-            int count = 0;
-            choice_sums<V, EDGE || sizeof(T) == 4>(v, mx == NEG ? 0.f : mx, below, count, mean);
-            float at_top = (float)count;
+            float below, at_top, mean;
+            auto sums = [&](auto clamp) __attribute__((always_inline)) {
+                int count = 0;
+                below = mean = 0.f;
+                choice_sums<V, decltype(clamp)::value>(v, mx == NEG ? 0.f : mx, below, count, mean);
+                at_top = (float)count;
 #pragma unroll
-            for (int o = MT; o < 64; o <<= 1) {
-                below += __shfl_xor(below, o);
-                at_top += __shfl_xor(at_top, o);
-                mean += __shfl_xor(mean, o);
+                for (int o = MT; o < 64; o <<= 1) {
+                    below += __shfl_xor(below, o);
+                    at_top += __shfl_xor(at_top, o);
+                    mean += __shfl_xor(mean, o);
+                }
+            };
+            constexpr bool CLAMP = EDGE || sizeof(T) == 4;
+            sums(std::integral_constant<bool, CLAMP>{});
+            bool clamp = CLAMP;
+            if constexpr (!CLAMP) {
+                // a row of logits beyond 2^20 (r up to 2^-4, and exp2(r) overflows from about 2^31 on), or one whose sums are not numbers, as a
+                // logit of -inf leaves them: again from the accumulators. All lanes of a row agree.
+                clamp = !(fabsf(mx) <= 0x1p20f) || mean != mean;
+                if (__builtin_expect(__ballot(clamp) != 0, 0)) {
+                    if (clamp) {
+#pragma unroll
+                        for (int j = 0; j < TN; ++j)
+#pragma unroll
+                            for (int e = 0; e < 4 * Q; ++e) v[4 * Q * j + e] = acc[i][j][e] * g.scale;
+                        sums(std::true_type{});
+                    }
+                }
             }
             float undo;
-            const ChoiceStat r = choice_stat<EDGE || sizeof(T) == 4>(mx, below, at_top, mean, undo);
+            const ChoiceStat r = choice_stat(clamp, mx, below, at_top, mean, undo);
             if (in && half == 0) g.stat[m * g.tiles + nw / COLS] = r;
             if (g.c) store(v, m, in, sizeof(T) == 4 ? undo : undo * SOFT_E_SCALE);
         }
