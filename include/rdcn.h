@@ -551,9 +551,9 @@ rdcn_status rdcn_softmax_loss_grad(rdcn_handle* h, int64_t rows, int64_t dim, in
  *   - labels [rows] in the handle's id type, or NULL: no given classes (logprob then NULL too). A label below 0 marks a
  *     row without one: logprob 0, and no gradient of its entropy either; everything else of the row is written all the same. A label
  *     of `classes` or more does the same and raises the device error word (RDCN_ERR_INDEX).
- *   - A masked class, or one whose logit is -inf, has probability 0 and is never among the most probable ones: where fewer than `top` are visible, the
- *     others have id -1 and log probability -inf. A row whose label is masked has logprob -inf; one with every class masked
- *     lse -inf and entropy 0.
+ *   - A masked class, or one whose logit is -inf, has probability 0 and is never among the most probable ones: where fewer than `top`
+ *     are visible, the others have id -1 and log probability -inf. A row whose label is masked has logprob -inf; one with every
+ *     class masked lse -inf and entropy 0.
  *   - A row whose logits hold NaN or +inf has NaN results (logprob 0 without a label), and ids of its own choice: in range, or -1 with
  *     log probability -inf. Its gradient, where it has one, is NaN too.
  * top is 0 (no lists) .. RDCN_LOGPROBS_TOP_MAX; top_ids in the handle's id type. logprob, entropy, lse, top_logprob and stats may
@@ -680,8 +680,10 @@ rdcn_status rdcn_grad_norm(rdcn_handle* h, const rdcn_adamw_tensor* tensors, int
  *   X  = U / |U| (the 2-norm of its elements; 0 where that is 0),  then `steps` times
  *   X <- a X + b A X + c A A X,  A = X X^T
  *   p' = p (1 - lr weight_decay) - lr scale X
- * |U| is summed in 64 bits; the products carry 22 bits and float sums: X is within 1e-4 of its own norm (2e-6 to 4e-5 over
- * the spectra measured, most for uneven singular values), where float products leave 1e-5; the other operations are one rounding to float each. The weights
+ * |U| is summed in 64 bits; the products carry 22 bits and float sums; the other operations are one rounding to float each. After the five
+ * steps below X is 2e-7 to 5e-5 of its own norm off over the spectra measured, even ones to falling by 10^6 (products in float: 2e-7 to 7e-5; most
+ * where few singular values are large). What is off grows with the singular values near 0, by up to |a| in every further step, as it does with
+ * products in float: 16 steps of the steepest spectra up to 3e-3 (4e-3). The weights
  * are as for rdcn_adamw_step: float, bf16 with a float master, or bf16 alone, rounded to nearest or (stochastic) by chance, with its bits.
  * a, b, c = 3.4445, -4.7750, 2.0315 in 5 steps take all but the smallest singular values to within 0.7 to 1.2; 2, -1.5, 0.5
  * in more steps to 1 itself. Coefficients whose iteration leaves the range of its f16 pairs (|a + b s^2 + c s^4| multiplied up to
