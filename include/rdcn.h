@@ -683,7 +683,8 @@ rdcn_status rdcn_grad_norm(rdcn_handle* h, const rdcn_adamw_tensor* tensors, int
  * |U| is summed in 64 bits; the products carry 22 bits and float sums; the other operations are one rounding to float each. After the five
  * steps below X is 2e-7 to 5e-5 of its own norm off over the spectra measured, even ones to falling by 10^6 (products in float: 2e-7 to 7e-5; most
  * where few singular values are large). What is off grows with the singular values near 0, by up to |a| in every further step, as it does with
- * products in float: 16 steps of the steepest spectra up to 3e-3 (4e-3). The weights
+ * products in float: 16 steps of the steepest spectra up to 3e-3 (4e-3). What falls below 2^-39 of the largest value that the
+ * coefficients allow at a step is lost: an X that they let vanish, as 0, 1, 0 does, ends as 0. The weights
  * are as for rdcn_adamw_step: float, bf16 with a float master, or bf16 alone, rounded to nearest or (stochastic) by chance, with its bits.
  * a, b, c = 3.4445, -4.7750, 2.0315 in 5 steps take all but the smallest singular values to within 0.7 to 1.2; 2, -1.5, 0.5
  * in more steps to 1 itself. Coefficients whose iteration leaves the range of its f16 pairs (|a + b s^2 + c s^4| multiplied up to

@@ -43,3 +43,25 @@ def test_update_over_spectra(rows, cols, kind):
         ref = newton_schulz(grad, steps=steps)
         off = float((t["param"].double() - ref).norm() / ref.norm())
         assert off <= 2e-4 * ABC[0] ** (steps - 5), "%d steps: %.3g" % (steps, off)
+
+
+@pytest.mark.parametrize("abc", [(2.0, -1.5, 0.5), (1.875, -1.25, 0.375), (3.0, -3.0, 1.0), (-3.4445, 4.7750, -2.0315)])
+@pytest.mark.parametrize("rows,cols", [(48, 80), (130, 300)])
+@pytest.mark.parametrize("kind", ["even", "one large", "i^-0.5", "10^-3"])
+def test_other_coefficients(abc, rows, cols, kind):
+    """The same sum with these coefficients' |a| and |b|, all added up."""
+    need_gpu()
+    lib = handle()
+    g = torch.Generator().manual_seed(1)
+    m = min(rows, cols)
+    u, _ = torch.linalg.qr(torch.randn(rows, m, generator=g, dtype=torch.float64))
+    v, _ = torch.linalg.qr(torch.randn(cols, m, generator=g, dtype=torch.float64))
+    grad = ((u * spectrum(kind, m)) @ v.t()).float()
+    e, a = 2.0 ** -23 / 3 ** 0.5, abs(abc[0])
+    for steps in (1, 2, 3, 4, 5, 8, 12):
+        t = dict(param=torch.zeros(rows, cols, device="cuda"), grad=grad.cuda(), m=torch.zeros(rows, cols, device="cuda"),
+                 weight_decay=0.0, scale=-1.0)
+        step(lib, [t], momentum=0.0, nesterov=False, steps=steps, coefficients=abc)
+        ref = newton_schulz(grad, abc, steps)
+        off = float((t["param"].double() - ref).norm() / ref.norm())
+        assert off <= ((a + abs(abc[1]) + 1) * e * sum(a ** i for i in range(steps)) + e * a ** steps) / 0.7, "%d steps: %.3g" % (steps, off)
