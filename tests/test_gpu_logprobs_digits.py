@@ -21,7 +21,7 @@ pytestmark = pytest.mark.gpu
 
 # whole tiles: streamed blocks, 64 x 64, 128 x 128 in two forms, 256 x 256, and the blocks of few rows
 SIZES = [(16, 64, 4096), (300, 64, 4096), (4096, 64, 8192), (1024, 1024, 2688), (1024, 1024, 8192), (50, 64, 100096),
-         (64, 64, 40064), (9, 64, 30720)]
+         (64, 64, 40064), (9, 64, 30784)]
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])

@@ -13,7 +13,7 @@ pytestmark = pytest.mark.gpu
 
 # every kind of block of the logits product, whole ones and ragged ones (rows, dim, classes)
 SIZES = [(9, 16, 1), (40, 64, 33), (40, 64, 5003), (300, 64, 2048), (300, 64, 2001), (1000, 64, 20000), (1024, 1024, 2688),
-         (1024, 512, 20000), (50, 64, 100096), (40, 72, 40001), (9, 64, 30720)]
+         (1024, 512, 20000), (50, 64, 100096), (40, 72, 40001), (9, 64, 30784)]
 
 
 def results(lib, c, rows, dim, classes, top):
